@@ -450,6 +450,114 @@ COSPEC_API int cospec_rl_advantages(int num_groups, int num_rollouts, int num_ro
                                     float* adv_dec, float* loss, void* ws, size_t ws_bytes,
                                     void* stream);
 
+/* ------------------------------------------------------------------------ */
+/* 6. The 8-bit paged KV cache: appending with the position rotation, attention,
+ *    and attention over pages that a cheap score selects.  (The paper has no
+ *    counterpart; it assumes a cache and positions.  A verify round's attention
+ *    reads half the bytes of the bf16 cache.)
+ *
+ *    Pages of 16 tokens per layer and KV head.  A page's keys and its values are
+ *    held as e4m3 codes with one scale each, a power of two:
+ *      x = code * scale,  scale = pow2(max |x| over the page, 448),
+ *    pow2(a, c) the smallest power of two s with a <= c s, its exponent kept in
+ *    [-100, 120] (2^-100 for a = 0).  A power of two costs an e4m3 code nothing
+ *    in precision, and when a page's scale grows with a later token the older
+ *    codes move to it by an exact product (rounded only below the smallest
+ *    normal code).  A page's summary, for the selection: t[d] = the sum of its
+ *    codes over its tokens (NaN codes count as 0), u = pow2(max |t|, 127),
+ *    summary[d] = rint(t[d] / u) (ties to even), summary_scale = u * the keys' scale in
+ *    fp32 (0 for a page of zeros).
+ *    Infinities and NaN are held as NaN and do not enter a scale or summary.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  int layers, num_pages, num_kv_heads, head_dim;   /* head_dim 64 or 128 */
+  uint8_t* k;            /* e4m3 [layers, num_pages, num_kv_heads, 16, head_dim] */
+  uint8_t* v;            /* e4m3 [layers, num_pages, num_kv_heads, head_dim, 16]: a
+                            dimension's 16 tokens side by side */
+  float* scale;          /* [layers, num_pages, num_kv_heads, 2]: of the keys, of the values */
+  int8_t* summary;       /* [layers, num_pages, num_kv_heads, head_dim], or NULL */
+  float* summary_scale;  /* [layers, num_pages, num_kv_heads]; NULL with summary */
+} cospec_kv8_pool;       /* every array dense and 16-byte aligned */
+
+/* Rotation by position: dimensions below rot_dim are turned in pairs (i, i + rot_dim / 2),
+ * or (2i, 2i + 1) when interleaved, by the angle whose cosine and sine at position p are
+ * cos[p * rot_dim / 2 + i], sin[p * rot_dim / 2 + i].  Products and sums are rounded to fp32
+ * one by one.  rot_dim: a multiple of 8 up to head_dim; the tables 16-byte aligned. */
+typedef struct {
+  const float* cos;
+  const float* sin;
+  int positions;         /* rows of the tables */
+  int rot_dim;
+  int interleaved;
+} cospec_rope;
+
+#define COSPEC_DEVERR_POSITION 32 /* a row's position is outside the rotation's tables */
+
+/* Element strides of a bf16 tensor [layers, batch, rows, heads, head_dim] whose heads and
+ * dimensions are dense: multiples of 8 (parts of a fused projection's output fit). */
+typedef struct {
+  long long layer, batch, row;
+} cospec_kv8_strides;
+
+/* Rows 0..num_rows[b]-1 of sequence b are appended at cache positions start[b].. of layers
+ * first_layer .. first_layer + num_layers - 1 of the pool, keys rotated to their positions
+ * (rope NULL: as they are) and both quantised from fp32.  A page that the rows fill from its
+ * first token takes a new scale; a page with older tokens (positions before start[b]) keeps its
+ * scale or moves all of it to a larger one.  Cells of the pages at or after position start[b] +
+ * num_rows[b] are left as they are.  Where q_out / k_out are given, all `rows` rows of q / k are
+ * also written rotated, rounded to bf16 (dense [num_layers, batch, rows, heads, head_dim]).
+ * pool->k NULL: nothing is appended (v, page_table and num_rows are then not read).
+ *
+ *    q        bf16, q_strides [num_layers, batch, rows, num_q_heads, head_dim] (NULL without q_out)
+ *    k, v     bf16, [num_layers, batch, rows, num_kv_heads, head_dim], 16-byte aligned
+ *    start    int32 [batch]: tokens cached before; the position of row j is start[b] + j
+ *    num_rows int32 [batch] in [0, rows], or NULL: every row
+ *    page_table int32 [batch, max_pages_per_seq]: only pages that receive rows are read
+ * start and num_rows stay as they are.  Sequences that append must not share those pages.  A sequence
+ * whose rows do not fit (COSPEC_DEVERR_CTX), a page id outside the pool (_PAGE) and positions outside
+ * the tables (_POSITION) are skipped and flagged. */
+COSPEC_API int cospec_kv8_append(const cospec_kv8_pool* pool, int first_layer, int num_layers,
+                                 int batch, int rows, int num_q_heads, const cospec_rope* rope,
+                                 const uint16_t* q, const cospec_kv8_strides* q_strides,
+                                 const uint16_t* k, const cospec_kv8_strides* k_strides,
+                                 const uint16_t* v, const cospec_kv8_strides* v_strides,
+                                 const int32_t* page_table, int max_pages_per_seq,
+                                 const int32_t* start, const int32_t* num_rows, uint16_t* q_out,
+                                 uint16_t* k_out, void* stream);
+
+/* The pages of the cache that each block row reads.  For block row j and KV head h, with a =
+ * pow2(max |q| over the G = num_q_heads / num_kv_heads query rows of h, 127) and qi = rint(q / a)
+ * (not finite: 0), page p scores
+ *      (max_g sum_d qi[g][d] * summary[p][d]) * summary_scale[p],
+ * an integer below 2^24 times a power of two, so exact in fp32.  Chosen are the first `sink` and the
+ * last `recent` of the sequence's ceil(ctx_len[b] / 16) pages and, up to `pages` in all, those
+ * of the largest score among the rest, ties to the lower page; all of them when there are no more.
+ *
+ *    sel      int32 [batch, rows, num_kv_heads, pages]: logical pages, ascending, -1 after the last
+ *    dims     the attention's (rows <= 64; num_pages that of the pool; softmax_scale, flags unused)
+ *    1 <= pages; 0 <= sink, recent; sink + recent <= pages; max_pages_per_seq <= 32768 */
+COSPEC_API int cospec_kv8_select(const cospec_attn_dims* dims, const cospec_kv8_pool* pool,
+                                 int layer, const uint16_t* q, const cospec_kv8_strides* q_strides,
+                                 const int32_t* page_table, const int32_t* ctx_len, int pages,
+                                 int sink, int recent, int32_t* sel, void* stream);
+
+/* cospec_verify_attn over an 8-bit cache: the softmax over the ctx_len[b] cached positions of
+ * layer `layer` and the block's rows (their own bf16 keys and values), causal or full inside the
+ * block.  With sel (cospec_kv8_select) row j of KV head h reads only the cached positions of the pages
+ * sel[b][j][h][0..pages-1]: logical pages, no page twice, the list ended by -1; positions at or
+ * after ctx_len[b] are not read.  A page outside the sequence or the pool sets COSPEC_DEVERR_PAGE and
+ * is skipped.
+ *
+ *    q, k_blk, v_blk  bf16 with strides (layer unused); out bf16 [batch, rows, num_q_heads, head_dim]
+ *    max_ctx, dims, flags, supported shapes: as for cospec_verify_attn */
+COSPEC_API int cospec_kv8_attn(const cospec_attn_dims* dims, int max_ctx,
+                               const cospec_kv8_pool* pool, int layer, const uint16_t* q,
+                               const cospec_kv8_strides* q_strides, const uint16_t* k_blk,
+                               const cospec_kv8_strides* k_strides, const uint16_t* v_blk,
+                               const cospec_kv8_strides* v_strides, const int32_t* page_table,
+                               const int32_t* ctx_len, const int32_t* sel, int pages,
+                               uint16_t* out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

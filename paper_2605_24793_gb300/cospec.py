@@ -19,6 +19,7 @@ LIB_PATH = os.path.join(_HERE, "libcospec.so")
 
 POLICY_MLP, POLICY_TARGET, POLICY_DRAFT = 0, 1, 2
 DEVERR_PAGE, DEVERR_CTX, DEVERR_TOKEN, DEVERR_TIMEOUT, DEVERR_OFFSETS = 1, 2, 4, 8, 16
+DEVERR_POSITION = 32
 
 EXPORTED = ("cospec_status_string", "cospec_last_cuda_error", "cospec_get_device_error", "cospec_num_sms",
             "cospec_verify_attn", "cospec_lmhead_workspace", "cospec_lmhead_argmax_features",
@@ -26,7 +27,7 @@ EXPORTED = ("cospec_status_string", "cospec_last_cuda_error", "cospec_get_device
             "cospec_lmhead_sample_features", "cospec_verify_attn_plan", "cospec_rl_workspace",
             "cospec_rl_advantages", "cospec_verify_attn_plan_model",
             "cospec_lmhead_logits_features", "cospec_sps_workspace", "cospec_sps_accept", "cospec_accept_commit_launches",
-            "cospec_verify_attn_variant")
+            "cospec_verify_attn_variant", "cospec_kv8_append", "cospec_kv8_select", "cospec_kv8_attn")
 
 
 class AttnDims(ctypes.Structure):
@@ -51,6 +52,23 @@ ATTN_KV_STABLE = 1
 ATTN_BLOCK_FULL = 2
 
 
+class Kv8PoolC(ctypes.Structure):
+    """cospec_kv8_pool."""
+    _fields_ = [(n, ctypes.c_int) for n in ("layers", "num_pages", "num_kv_heads", "head_dim")] + [
+        (n, ctypes.c_void_p) for n in ("k", "v", "scale", "summary", "summary_scale")]
+
+
+class RopeC(ctypes.Structure):
+    """cospec_rope."""
+    _fields_ = [("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p)] + [
+        (n, ctypes.c_int) for n in ("positions", "rot_dim", "interleaved")]
+
+
+class Strides(ctypes.Structure):
+    """cospec_kv8_strides."""
+    _fields_ = [(n, ctypes.c_longlong) for n in ("layer", "batch", "row")]
+
+
 class CospecError(RuntimeError):
     pass
 
@@ -60,6 +78,7 @@ _lib: Optional[ctypes.CDLL] = None
 _vp, _i, _sz, _f = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_float
 _PDIMS = ctypes.POINTER(AttnDims)
 # cospec_resident_fn: (kernel, rows, block_rows, splits, user) -> resident clusters
+_PPOOL, _PROPE, _PSTR = ctypes.POINTER(Kv8PoolC), ctypes.POINTER(RopeC), ctypes.POINTER(Strides)
 RESIDENT_FN = ctypes.CFUNCTYPE(ctypes.c_longlong, _i, _i, _i, _i, _vp)
 
 
@@ -99,6 +118,11 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "cospec_accept_commit": (_i, [_i, _i, _i, _PDIMS, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                                       ctypes.c_longlong, _vp, _vp, _vp, _vp, _vp]),
         "cospec_accept_commit_launches": (_i, [_PDIMS, _i]),
+        "cospec_kv8_append": (_i, [_PPOOL, _i, _i, _i, _i, _i, _PROPE, _vp, _PSTR, _vp, _PSTR, _vp, _PSTR, _vp,
+                                   _i, _vp, _vp, _vp, _vp, _vp]),
+        "cospec_kv8_select": (_i, [_PDIMS, _PPOOL, _i, _vp, _PSTR, _vp, _vp, _i, _i, _i, _vp, _vp]),
+        "cospec_kv8_attn": (_i, [_PDIMS, _i, _PPOOL, _i, _vp, _PSTR, _vp, _PSTR, _vp, _PSTR, _vp, _vp, _vp, _i,
+                                 _vp, _vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -526,6 +550,185 @@ def accept_commit(draft, argmax, accept, k_blk, v_blk, k_pages, v_pages, page_ta
         _ptr(v_blk), _ptr(k_pages), _ptr(v_pages), layer_stride, _ptr(page_table),
         _ptr(ctx_len), _ptr(accept_len), _ptr(emitted), _stream(stream)))
     return accept_len, emitted
+
+
+# ---------------------------------------------------------------- 8-bit KV cache
+F8 = torch.float8_e4m3fn
+
+
+class Kv8Pool:
+    """The arrays of an 8-bit paged cache (cospec_kv8_pool), checked once: k e4m3
+    [L, pages, Hkv, 16, D], v e4m3 [L, pages, Hkv, D, 16], scale float32
+    [L, pages, Hkv, 2] and, for the page selection, summary int8 [L, pages, Hkv, D] with
+    summary_scale float32 [L, pages, Hkv]."""
+
+    def __init__(self, k, v, scale, summary=None, summary_scale=None):
+        _req(k, F8, "k", 5)
+        _req(v, F8, "v", 5)
+        _req(scale, torch.float32, "scale", 4)
+        L, N, H, P, D = k.shape
+        _need(P == 16 and tuple(v.shape) == (L, N, H, D, P), "k must be [L, pages, Hkv, 16, D] and v [L, pages, Hkv, D, 16]")
+        _need(tuple(scale.shape) == (L, N, H, 2), "scale must be [L, pages, Hkv, 2]")
+        _need((summary is None) == (summary_scale is None), "summary and summary_scale go together")
+        if summary is not None:
+            _req(summary, torch.int8, "summary", 4)
+            _req(summary_scale, torch.float32, "summary_scale", 3)
+            _need(tuple(summary.shape) == (L, N, H, D), "summary must be [L, pages, Hkv, D]")
+            _need(tuple(summary_scale.shape) == (L, N, H), "summary_scale must be [L, pages, Hkv]")
+        self.k, self.v, self.scale, self.summary, self.summary_scale = k, v, scale, summary, summary_scale
+        self.layers, self.num_pages, self.kv_heads, self.head_dim = L, N, H, D
+        self.device = k.device
+        for t in (v, scale, summary, summary_scale):
+            _need(t is None or t.device == k.device, "a pool's arrays must be on one device")
+        self.c = Kv8PoolC(L, N, H, D, *(0 if t is None else t.data_ptr() for t in (k, v, scale, summary, summary_scale)))
+        self.ref = ctypes.byref(self.c)
+
+
+def new_kv8_pool(layers: int, num_pages: int, kv_heads: int, head_dim: int, summaries: bool = True,
+                 device="cuda") -> Kv8Pool:
+    """An empty 8-bit cache."""
+    z = lambda shape, dt: torch.zeros((layers, num_pages, kv_heads) + shape, dtype=dt, device=device)  # noqa: E731
+    return Kv8Pool(z((16, head_dim), torch.uint8).view(F8), z((head_dim, 16), torch.uint8).view(F8),
+                   z((2,), torch.float32), *((z((head_dim,), torch.int8), z((), torch.float32)) if summaries else ()))
+
+
+class Rope:
+    """Tables of the position rotation (cospec_rope): cos, sin float32 [positions, rot_dim / 2]."""
+
+    def __init__(self, cos, sin, interleaved: bool = False):
+        _req(cos, torch.float32, "cos", 2)
+        _req(sin, torch.float32, "sin", 2)
+        _need(tuple(sin.shape) == tuple(cos.shape) and cos.shape[1] % 4 == 0 and cos.numel() > 0,
+              "cos / sin must both be [positions, rot_dim / 2], rot_dim a multiple of 8")
+        _need(sin.device == cos.device, "cos / sin must be on one device")
+        self.cos, self.sin, self.device = cos, sin, cos.device
+        self.c = RopeC(cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1], int(bool(interleaved)))
+        self.ref = ctypes.byref(self.c)
+
+
+def _rows5(t: torch.Tensor, name: str, shape) -> "ctypes._Pointer":
+    """Checks bf16 rows [(layers,) batch, rows, heads, head_dim] whose heads and dimensions are
+    dense, and returns their strides."""
+    if t.dtype != torch.bfloat16:
+        raise TypeError(f"{name}: expected {torch.bfloat16}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: must be a CUDA tensor")
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    st = t.stride()
+    if t.numel() and ((st[-1] != 1 and shape[-1] > 1) or (st[-2] != shape[-1] and shape[-2] > 1)):
+        raise ValueError(f"{name}: heads and dimensions must be dense")
+    return Strides(st[0] if len(st) == 5 else 0, st[-4], st[-3])
+
+
+def _ints(t: torch.Tensor, name: str, shape) -> None:
+    _req(t, torch.int32, name)
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
+
+
+def kv8_append(pool: Kv8Pool, k, v, page_table, start, rows=None, rope: Optional[Rope] = None, layer: Optional[int] = None,
+               q=None, q_out=None, k_out=None, stream=None) -> None:
+    """Append rows of keys (rotated by ``rope``) and values to an 8-bit cache: k, v bf16
+    [L, B, R, Hkv, D] for every layer of the pool or, with ``layer``, [B, R, Hkv, D] for that one; they may
+    be parts of a fused projection's output (any strides of the leading dimensions).  Row j of sequence
+    b enters position start[b] + j for j < rows[b] (all rows without ``rows``).  k_out / q_out receive
+    all rows of k / q rotated, in bf16.  See include/cospec.h."""
+    _need(k.dim() == (5 if layer is None else 4), "k must be [L, B, R, Hkv, D], or [B, R, Hkv, D] with layer")
+    lead = tuple(k.shape[:-2])
+    first, L = (0, k.shape[0]) if layer is None else (int(layer), 1)
+    _need(first >= 0 and (L == pool.layers if layer is None else first < pool.layers), "layer outside the pool")
+    B, R = lead[-2:]
+    shape = lead + (pool.kv_heads, pool.head_dim)
+    ks, vs = _rows5(k, "k", shape), _rows5(v, "v", shape)
+    _need(page_table.dim() == 2, "page_table must be [B, max_pages]")
+    _ints(page_table, "page_table", (B, page_table.shape[1]))
+    _ints(start, "start", (B,))
+    if rows is not None:
+        _ints(rows, "rows", (B,))
+    _launch_append(pool.ref, pool.device, first, L, B, R, rope, q, k, ks, v, vs, page_table, start, rows, q_out, k_out, shape, stream)
+
+
+def kv8_rotate(q, k, rope: Rope, start, q_out, k_out, stream=None) -> None:
+    """The rotation of kv8_append by itself: q [B, R, Hq, D] and k [B, R, Hkv, D] (or with a leading
+    layer dimension) turned to positions start[b] + j, in bf16, nothing appended."""
+    lead = tuple(k.shape[:-2])
+    _need(len(lead) in (2, 3), "k must be [B, R, Hkv, D] or [L, B, R, Hkv, D]")
+    B, R = lead[-2:]
+    ks = _rows5(k, "k", k.shape)
+    _ints(start, "start", (B,))
+    pool = Kv8PoolC(1, 1, k.shape[-2], k.shape[-1], 0, 0, 0, 0, 0)
+    _launch_append(ctypes.byref(pool), k.device, 0, lead[0] if len(lead) == 3 else 1, B, R, rope, q, k, ks, None, None, None, start,
+                   None, q_out, k_out, tuple(k.shape), stream)
+
+
+def _launch_append(pool_ref, device, first, L, B, R, rope, q, k, ks, v, vs, page_table, start, rows, q_out, k_out, shape, stream):
+    _need((q is None) == (q_out is None), "q and q_out go together")
+    Hq, qs = 0, None
+    if q is not None:
+        _need(q.dim() == len(shape) and q.shape[:-2] == shape[:-2] and q.shape[-1] == shape[-1], "q must have k's batch, rows and head_dim")
+        Hq = q.shape[-2]
+        qs = _rows5(q, "q", q.shape)
+        _req(q_out, torch.bfloat16, "q_out")
+        _need(q_out.shape == q.shape, "q_out must have q's shape")
+    if k_out is not None:
+        _req(k_out, torch.bfloat16, "k_out")
+        _need(tuple(k_out.shape) == shape, "k_out must have k's shape")
+    _same_device(k, v, q, q_out, k_out, page_table, start, rows, *(() if rope is None else (rope.cos, rope.sin)))
+    _need(device == k.device, "the pool is on another device")
+    by = ctypes.byref
+    _check(load_library().cospec_kv8_append(
+        pool_ref, first, L, B, R, Hq, None if rope is None else rope.ref, _ptr(q), None if qs is None else by(qs), _ptr(k), by(ks),
+        _ptr(v), None if vs is None else by(vs), _ptr(page_table), 0 if page_table is None else page_table.shape[1], _ptr(start),
+        _ptr(rows), _ptr(q_out), _ptr(k_out), _stream(stream)))
+
+
+def _kv8_dims(q, pool: Kv8Pool, layer: int, page_table, ctx_len, softmax_scale=0.0, flags=0):
+    _need(q.dim() == 4 and q.shape[3] == pool.head_dim, "q must be [B, R, Hq, D] with the pool's D")
+    _need(0 <= layer < pool.layers, "layer outside the pool")
+    B, R, Hq, D = q.shape
+    _need(page_table.dim() == 2, "page_table must be [B, max_pages]")
+    _ints(page_table, "page_table", (B, page_table.shape[1]))
+    _ints(ctx_len, "ctx_len", (B,))
+    return AttnDims(B, R, Hq, pool.kv_heads, D, 16, page_table.shape[1], pool.num_pages, softmax_scale, flags)
+
+
+def kv8_select(q, pool: Kv8Pool, layer: int, page_table, ctx_len, sel, sink: int = 1, recent: int = 2, stream=None) -> torch.Tensor:
+    """The pages each block row reads: sel int32 [B, R, Hkv, pages] receives for row q[b, j] and each
+    KV head the first ``sink`` and last ``recent`` pages of its context and those of the largest
+    scores by the pages' summaries, ascending, -1 after the last."""
+    dims = _kv8_dims(q, pool, layer, page_table, ctx_len)
+    qs = _rows5(q, "q", q.shape)
+    _need(pool.summary is not None, "the pool has no summaries")
+    _need(sel.dim() == 4, "sel must be [B, R, Hkv, pages]")
+    _ints(sel, "sel", (dims.batch, dims.rows, pool.kv_heads, sel.shape[3]))
+    _same_device(q, page_table, ctx_len, sel, pool.k)
+    by = ctypes.byref
+    _check(load_library().cospec_kv8_select(by(dims), pool.ref, layer, _ptr(q), by(qs), _ptr(page_table), _ptr(ctx_len),
+                                            sel.shape[3], int(sink), int(recent), _ptr(sel), _stream(stream)))
+    return sel
+
+
+def kv8_attn(q, k_blk, v_blk, pool: Kv8Pool, layer: int, page_table, ctx_len, out, max_ctx: int, softmax_scale: float = 0.0,
+             sel=None, kv_stable: bool = False, block_full: bool = False, stream=None) -> torch.Tensor:
+    """Verify attention over layer ``layer`` of an 8-bit cache and the block's own bf16 rows; with
+    ``sel`` (kv8_select) over each row's chosen pages only.  q, k_blk and v_blk [B, R, H, D] may be parts of a
+    fused projection's output.  Flags as verify_attn; see include/cospec.h."""
+    dims = _kv8_dims(q, pool, layer, page_table, ctx_len, softmax_scale,
+                     (ATTN_KV_STABLE if kv_stable else 0) | (ATTN_BLOCK_FULL if block_full else 0))
+    shape = (dims.batch, dims.rows, pool.kv_heads, pool.head_dim)
+    qs, ks, vs = _rows5(q, "q", q.shape), _rows5(k_blk, "k_blk", shape), _rows5(v_blk, "v_blk", shape)
+    _req(out, torch.bfloat16, "out")
+    _need(out.shape == q.shape, "out must have q's shape")
+    pages = 0
+    if sel is not None:
+        pages = sel.shape[-1]
+        _ints(sel, "sel", (dims.batch, dims.rows, pool.kv_heads, pages))
+    _same_device(q, k_blk, v_blk, page_table, ctx_len, sel, out, pool.k)
+    by = ctypes.byref
+    _check(load_library().cospec_kv8_attn(by(dims), int(max_ctx), pool.ref, layer, _ptr(q), by(qs), _ptr(k_blk), by(ks), _ptr(v_blk),
+                                          by(vs), _ptr(page_table), _ptr(ctx_len), _ptr(sel), pages, _ptr(out), _stream(stream)))
+    return out
 
 
 def get_device_error(stream=None) -> int:

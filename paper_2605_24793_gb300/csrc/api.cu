@@ -505,4 +505,175 @@ COSPEC_API int cospec_accept_commit_launches(const cospec_attn_dims* dims, int n
   return accept_commit_launches(dims->batch, dims->rows - 1, num_layers, dims->num_kv_heads, dims->head_dim);
 }
 
+// ---------------------------------------------------------------- 8-bit KV cache
+// Checks a pool's geometry and arrays and fills `p` with the addresses of layer `layer`.
+static int kv8_pool(const cospec_kv8_pool* s, int layer, bool summaries, Kv8Pool* p) {
+  CS_CHECK_ARG(s && s->layers >= 1 && s->num_pages >= 1 && s->num_kv_heads >= 1);
+  if (s->head_dim != 64 && s->head_dim != 128) return COSPEC_ERR_UNSUPPORTED;
+  CS_CHECK_ARG(layer >= 0 && layer < s->layers);
+  CS_CHECK_ARG(s->k && s->v && s->scale);
+  CS_CHECK_ARG(!summaries || (s->summary && s->summary_scale));
+  CS_CHECK_ARG((s->summary == nullptr) == (s->summary_scale == nullptr));
+  CS_CHECK_ARG(aligned16(s->k) && aligned16(s->v) && aligned16(s->scale) && aligned16(s->summary) &&
+               aligned16(s->summary_scale));
+  const size_t heads = (size_t)layer * s->num_pages * s->num_kv_heads;
+  p->k = s->k + heads * 16 * s->head_dim;
+  p->v = s->v + heads * 16 * s->head_dim;
+  p->scale = s->scale + heads * 2;
+  p->summary = s->summary ? s->summary + heads * s->head_dim : nullptr;
+  p->summary_scale = s->summary_scale ? s->summary_scale + heads : nullptr;
+  return COSPEC_OK;
+}
+
+static int kv8_src(const uint16_t* x, const cospec_kv8_strides* st, Kv8Src* s) {
+  CS_CHECK_ARG(x && st && aligned16(x));
+  CS_CHECK_ARG(st->layer % 8 == 0 && st->batch % 8 == 0 && st->row % 8 == 0);
+  s->p = reinterpret_cast<const __nv_bfloat16*>(x);
+  s->layer = st->layer;
+  s->batch = st->batch;
+  s->row = st->row;
+  return COSPEC_OK;
+}
+
+// The geometry shared by the selection and the attention.
+static int check_kv8_dims(const cospec_attn_dims* d, const cospec_kv8_pool* pool) {
+  const int st = check_attn_dims(d);
+  if (st != COSPEC_OK) return st;
+  CS_CHECK_ARG(pool && pool->num_pages == d->num_pages && pool->num_kv_heads == d->num_kv_heads &&
+               pool->head_dim == d->head_dim);
+  if ((long long)d->max_pages_per_seq * 16 > 0x7fffffffLL) return COSPEC_ERR_UNSUPPORTED;
+  return COSPEC_OK;
+}
+
+COSPEC_API int cospec_kv8_append(const cospec_kv8_pool* pool, int first_layer, int num_layers,
+                                 int batch, int rows, int num_q_heads, const cospec_rope* rope,
+                                 const uint16_t* q, const cospec_kv8_strides* q_strides,
+                                 const uint16_t* k, const cospec_kv8_strides* k_strides,
+                                 const uint16_t* v, const cospec_kv8_strides* v_strides,
+                                 const int32_t* page_table, int max_pages_per_seq,
+                                 const int32_t* start, const int32_t* num_rows, uint16_t* q_out,
+                                 uint16_t* k_out, void* stream) {
+  CS_CHECK_ARG(pool && num_layers >= 0 && batch >= 0 && rows >= 0);
+  Kv8AppendArgs a{};
+  if (pool->k) {
+    const int st = kv8_pool(pool, first_layer, false, &a.pool);
+    if (st != COSPEC_OK) return st;
+    CS_CHECK_ARG(num_layers <= pool->layers - first_layer);
+  } else {
+    CS_CHECK_ARG(pool->num_kv_heads >= 1);
+    if (pool->head_dim != 64 && pool->head_dim != 128) return COSPEC_ERR_UNSUPPORTED;
+  }
+  if (num_layers == 0 || batch == 0 || rows == 0) return COSPEC_OK;
+  CS_CHECK_ARG(start);
+  int st = COSPEC_OK;
+  if (pool->k || k_out) st = kv8_src(k, k_strides, &a.k);
+  if (st == COSPEC_OK && pool->k) st = kv8_src(v, v_strides, &a.v);
+  if (st == COSPEC_OK && q_out) st = kv8_src(q, q_strides, &a.q);
+  if (st != COSPEC_OK) return st;
+  if (pool->k) {
+    CS_CHECK_ARG(page_table && max_pages_per_seq >= 1);
+    if ((long long)max_pages_per_seq * 16 > 0x7fffffffLL) return COSPEC_ERR_UNSUPPORTED;
+  }
+  CS_CHECK_ARG(!q_out || num_q_heads >= 1);
+  CS_CHECK_ARG(aligned16(q_out) && aligned16(k_out));
+  if (rope) {
+    CS_CHECK_ARG(rope->cos && rope->sin && rope->positions >= 1);
+    CS_CHECK_ARG(aligned16(rope->cos) && aligned16(rope->sin));
+    CS_CHECK_ARG(rope->rot_dim >= 8 && rope->rot_dim % 8 == 0 && rope->rot_dim <= pool->head_dim);
+    a.cos = rope->cos;
+    a.sin = rope->sin;
+    a.positions = rope->positions;
+    a.rot = rope->rot_dim;
+    a.inter = rope->interleaved ? 1 : 0;
+  }
+  a.L = num_layers;
+  a.B = batch;
+  a.R = rows;
+  a.Hq = q_out ? num_q_heads : 0;
+  a.Hkv = pool->num_kv_heads;
+  a.D = pool->head_dim;
+  a.num_pages = pool->num_pages;
+  a.max_pages = max_pages_per_seq;
+  a.page_table = page_table;
+  a.start = start;
+  a.num_rows = num_rows;
+  a.q_out = reinterpret_cast<__nv_bfloat16*>(q_out);
+  a.k_out = reinterpret_cast<__nv_bfloat16*>(k_out);
+  int* err = device_error_word();
+  if (!err) return cuda_lookup_failed();
+  return cuda_status(launch_kv8_append(a, err, static_cast<cudaStream_t>(stream)));
+}
+
+COSPEC_API int cospec_kv8_select(const cospec_attn_dims* d, const cospec_kv8_pool* pool, int layer,
+                                 const uint16_t* q, const cospec_kv8_strides* q_strides,
+                                 const int32_t* page_table, const int32_t* ctx_len, int pages,
+                                 int sink, int recent, int32_t* sel, void* stream) {
+  int st = check_kv8_dims(d, pool);
+  if (st != COSPEC_OK) return st;
+  Kv8SelectArgs a{};
+  st = kv8_pool(pool, layer, true, &a.pool);
+  if (st != COSPEC_OK) return st;
+  CS_CHECK_ARG(pages >= 1 && sink >= 0 && recent >= 0 && sink <= pages && recent <= pages - sink);
+  if (d->max_pages_per_seq > 32768) return COSPEC_ERR_UNSUPPORTED;
+  if (d->batch == 0) return COSPEC_OK;
+  st = kv8_src(q, q_strides, &a.q);
+  if (st != COSPEC_OK) return st;
+  CS_CHECK_ARG(page_table && ctx_len && sel);
+  a.B = d->batch;
+  a.R = d->rows;
+  a.Hq = d->num_q_heads;
+  a.Hkv = d->num_kv_heads;
+  a.D = d->head_dim;
+  a.num_pages = d->num_pages;
+  a.max_pages = d->max_pages_per_seq;
+  a.page_table = page_table;
+  a.ctx_len = ctx_len;
+  a.pages = pages;
+  a.sink = sink;
+  a.recent = recent;
+  a.sel = sel;
+  int* err = device_error_word();
+  if (!err) return cuda_lookup_failed();
+  return cuda_status(launch_kv8_select(a, err, static_cast<cudaStream_t>(stream)));
+}
+
+COSPEC_API int cospec_kv8_attn(const cospec_attn_dims* d, int max_ctx, const cospec_kv8_pool* pool,
+                               int layer, const uint16_t* q, const cospec_kv8_strides* q_strides,
+                               const uint16_t* k_blk, const cospec_kv8_strides* k_strides,
+                               const uint16_t* v_blk, const cospec_kv8_strides* v_strides,
+                               const int32_t* page_table, const int32_t* ctx_len,
+                               const int32_t* sel, int pages, uint16_t* out, void* stream) {
+  int st = check_kv8_dims(d, pool);
+  if (st != COSPEC_OK) return st;
+  CS_CHECK_ARG(max_ctx >= 0 && max_ctx <= d->max_pages_per_seq * d->page_size);
+  Kv8AttnArgs a{};
+  st = kv8_pool(pool, layer, false, &a.pool);
+  if (st != COSPEC_OK) return st;
+  CS_CHECK_ARG(!sel || (pages >= 1 && pages <= 0x7fffffff / 16));
+  if (d->batch == 0) return COSPEC_OK;
+  if ((st = kv8_src(q, q_strides, &a.q)) != COSPEC_OK || (st = kv8_src(k_blk, k_strides, &a.k_blk)) != COSPEC_OK ||
+      (st = kv8_src(v_blk, v_strides, &a.v_blk)) != COSPEC_OK)
+    return st;
+  CS_CHECK_ARG(page_table && ctx_len && out && aligned16(out));
+  a.B = d->batch;
+  a.R = d->rows;
+  a.Hq = d->num_q_heads;
+  a.Hkv = d->num_kv_heads;
+  a.D = d->head_dim;
+  a.num_pages = d->num_pages;
+  a.max_pages = d->max_pages_per_seq;
+  a.page_table = page_table;
+  a.ctx_len = ctx_len;
+  a.sel = sel;
+  a.pages = sel ? pages : 0;
+  a.out = reinterpret_cast<__nv_bfloat16*>(out);
+  a.scale = d->softmax_scale > 0.f ? d->softmax_scale : 1.0f / sqrtf((float)d->head_dim);
+  a.max_ctx = max_ctx;
+  a.kv_stable = (d->flags & COSPEC_ATTN_KV_STABLE) ? 1 : 0;
+  a.block_full = (d->flags & COSPEC_ATTN_BLOCK_FULL) ? 1 : 0;
+  int* err = device_error_word();
+  if (!err) return cuda_lookup_failed();
+  return cuda_status(launch_kv8_attn(a, err, static_cast<cudaStream_t>(stream)));
+}
+
 }  // extern "C"

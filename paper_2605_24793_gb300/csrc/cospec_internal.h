@@ -170,4 +170,56 @@ struct CommitArgs {
 cudaError_t launch_accept_commit(const CommitArgs& a, int* err, cudaStream_t stream);
 int accept_commit_launches(int B, int K, int L, int Hkv, int D);   // kernels such a call launches
 
+// ---------------------------------------------------------------- 8-bit KV cache
+struct Kv8Pool {
+  uint8_t* k;             // [num_pages, Hkv, 16, D] of the first layer, e4m3
+  uint8_t* v;             // [num_pages, Hkv, D, 16]
+  float* scale;           // [num_pages, Hkv, 2]
+  int8_t* summary;        // [num_pages, Hkv, D]
+  float* summary_scale;   // [num_pages, Hkv]
+};
+struct Kv8Src {            // bf16 [layers, batch, rows, heads, D], heads and D dense
+  const __nv_bfloat16* p;
+  long long layer, batch, row;
+};
+struct Kv8AppendArgs {
+  Kv8Pool pool;
+  int L, B, R, Hq, Hkv, D, num_pages, max_pages;
+  Kv8Src q, k, v;
+  const int32_t* page_table;
+  const int32_t* start;
+  const int32_t* num_rows;
+  __nv_bfloat16* q_out;
+  __nv_bfloat16* k_out;
+  const float* cos;        // null: no rotation
+  const float* sin;
+  int positions, rot, inter;
+};
+cudaError_t launch_kv8_append(const Kv8AppendArgs& a, int* err, cudaStream_t stream);
+
+struct Kv8SelectArgs {
+  Kv8Pool pool;
+  int B, R, Hq, Hkv, D, num_pages, max_pages;
+  Kv8Src q;
+  const int32_t* page_table;
+  const int32_t* ctx_len;
+  int pages, sink, recent;
+  int32_t* sel;
+};
+cudaError_t launch_kv8_select(const Kv8SelectArgs& a, int* err, cudaStream_t stream);
+
+struct Kv8AttnArgs {
+  Kv8Pool pool;
+  int B, R, Hq, Hkv, D, num_pages, max_pages;
+  Kv8Src q, k_blk, v_blk;
+  const int32_t* page_table;
+  const int32_t* ctx_len;
+  const int32_t* sel;      // null: every page of the context
+  int pages;
+  __nv_bfloat16* out;
+  float scale;
+  int max_ctx, kv_stable, block_full;
+};
+cudaError_t launch_kv8_attn(const Kv8AttnArgs& a, int* err, cudaStream_t stream);
+
 }  // namespace cospec

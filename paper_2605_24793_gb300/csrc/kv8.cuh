@@ -1,0 +1,76 @@
+// Shared by the kernels of the 8-bit KV cache: e4m3 codes and their power-of-two scales.
+#pragma once
+
+#include "cospec_device.cuh"
+
+namespace cospec {
+
+constexpr int KV8_PAGE = 16;     // tokens of a page
+
+// pow2(a, c) for c = (1 + frac / 2^23) 2^e: the smallest power of two s with a <= c s, its exponent
+// kept in [-100, 120].  a is not negative; below 2^-126 the lower bound holds anyway.
+CS_DEV float kv8_pow2(float a, uint32_t frac, int e) {
+  const uint32_t u = __float_as_uint(a);
+  const int k = (int)(u >> 23) - 127 - e + ((u & 0x7fffffu) > frac ? 1 : 0);
+  return __uint_as_float((uint32_t)(min(max(k, -100), 120) + 127) << 23);
+}
+CS_DEV float kv8_scale_of(float amax) { return kv8_pow2(amax, 0x600000u, 8); }    // c = 448 = 1.75 * 2^8
+CS_DEV float kv8_scale127(float amax) { return kv8_pow2(amax, 0x7e0000u, 6); }    // c = 127 = 1.984375 * 2^6
+// 1 / s of a power of two with its exponent in [-100, 120]
+CS_DEV float kv8_inverse(float s) { return __uint_as_float((254u << 23) - __float_as_uint(s)); }
+
+// |x|, or 0 where x is not finite.
+CS_DEV float kv8_finite_abs(float x) {
+  const float a = fabsf(x);
+  return a <= 3.4028235e38f ? a : 0.f;
+}
+
+// Two values to e4m3, round to nearest even: `lo` in the low byte.  Not finite: NaN.  (The
+// conversion itself would hold an infinity as the largest code; values within a scale never reach that.)
+CS_DEV uint32_t kv8_pack2(float lo, float hi) {
+  lo = fabsf(lo) <= 3.4028235e38f ? lo : __uint_as_float(0x7fffffffu);
+  hi = fabsf(hi) <= 3.4028235e38f ? hi : __uint_as_float(0x7fffffffu);
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// The two codes of `w`'s low half as f16 (exact).
+CS_DEV uint32_t kv8_f16x2(uint32_t w) {
+  uint32_t r;
+  asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %1;\n cvt.rn.f16x2.e4m3x2 %0, l;\n}\n" : "=r"(r) : "r"(w));
+  return r;
+}
+CS_DEV uint32_t kv8_f16x2_hi(uint32_t w) {
+  uint32_t r;
+  asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %1;\n cvt.rn.f16x2.e4m3x2 %0, h;\n}\n" : "=r"(r) : "r"(w));
+  return r;
+}
+CS_DEV float2 kv8_floats(uint32_t w) {       // the low half's codes
+  const uint32_t h = kv8_f16x2(w);
+  float2 f;
+  asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.f32.f16 %0, l;\n cvt.f32.f16 %1, h;\n}\n"
+      : "=f"(f.x), "=f"(f.y)
+      : "r"(h));
+  return f;
+}
+CS_DEV void kv8_floats4(uint32_t w, float (&f)[4]) {
+  const float2 a = kv8_floats(w), b = kv8_floats(w >> 16);
+  f[0] = a.x;
+  f[1] = a.y;
+  f[2] = b.x;
+  f[3] = b.y;
+}
+
+// Four bf16 of a 16-bit row.
+CS_DEV void kv8_load4(const __nv_bfloat16* p, float (&x)[4]) {
+  const uint2 u = *reinterpret_cast<const uint2*>(p);
+  x[0] = __uint_as_float(u.x << 16);
+  x[1] = __uint_as_float(u.x & 0xffff0000u);
+  x[2] = __uint_as_float(u.y << 16);
+  x[3] = __uint_as_float(u.y & 0xffff0000u);
+}
+CS_DEV void kv8_store4(__nv_bfloat16* p, const float (&x)[4]) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+}
+
+}  // namespace cospec
