@@ -1,7 +1,27 @@
 // Attention of a block of rows over the 8-bit paged cache and the block's own bf16 rows.
 //
-// One CTA per (sequence, block row, query head); a warp takes every fourth key, its lanes the
-// dimensions, with a running maximum and sum; the warps' parts meet in shared memory.
+// A unit is (sequence, KV head, up to 32 query rows that read it), or with selected pages (sequence,
+// block row, KV head, up to 32 of its query heads).  Its pages go in pairs (32 keys: a tile) to the warps
+// of a thread-block cluster, tile t to warp t mod (4 S) of S CTAs of four warps: no warp waits for
+// another until the end.  Each warp keeps a ring of its own, three tiles deep (four for 64 dimensions),
+// filled by bulk copies of whole page-heads (2 KB, contiguous) that one lane per copy issues.
+//
+// q . k^T and p . v run on mma.m16n8k16 with f16 operands.  An e4m3 code is exact in f16; q is brought
+// to f16 by a power of two per row (bf16's 8 bits fit f16's 11, values 2^-14 below the row's largest
+// lose bits only below 2^-25 of it); p is held as 2^14 p, so that weights down to 2^-38 count.  The pages'
+// scales are powers of two: the keys' joins the score's factor, the values' the weight, relative to the
+// largest seen so far (the output is rescaled, exactly, when that grows).
+//
+// The contraction's order is free, so every lane converts what it can load wide: of a key it takes 32
+// (16) dimensions side by side, the query rows laid out alike, and of a dimension's values four tokens of
+// each page; accumulator columns 2c and 2c + 1 are then token 4c + i of the two pages, which is what
+// the lane's value codes want.  A pad between the two pages' keys makes the loads conflict-free.
+//
+// The block's keys and values (bf16, up to 64) go 16 at a time to the warps of the cluster's last CTA, on
+// bf16 operands.  The warps' partial (max, sum, output) meet in shared memory, the CTAs' in
+// distributed shared memory, each CTA finishing a slice of the rows.
+#include <math.h>
+
 #include "cospec_internal.h"
 #include "kv8.cuh"
 
@@ -9,101 +29,661 @@ namespace cospec {
 
 namespace {
 
-constexpr int WARPS = 4;
+constexpr int NW = 4;                     // warps of a CTA
+constexpr int MAX_SPLIT = 16;
+constexpr float P_BITS = 14.f;            // weights are held times 2^14
 
-template <int D>
-__global__ void __launch_bounds__(WARPS * 32) kv8_attn_kernel(const Kv8AttnArgs a, int* err) {
-  constexpr int E = D / 32;
-  __shared__ float part[WARPS][D + 2];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int hq = blockIdx.x % a.Hq, j = blockIdx.x / a.Hq % a.R, b = blockIdx.x / a.Hq / a.R;
-  const int G = a.Hq / a.Hkv, h = hq / G;
-  griddep_wait();
-  griddep_launch_dependents();
-  const int C = a.ctx_len[b];
-  const bool bad = C < 0 || C > a.max_pages * KV8_PAGE;
-  if (bad && threadIdx.x == 0 && hq == 0 && j == 0) set_err(err, ERR_CTX);
-  const int32_t* table = a.page_table + (size_t)b * a.max_pages;
-  const int32_t* sel = a.sel ? a.sel + (((size_t)b * a.R + j) * a.Hkv + h) * a.pages : nullptr;
-  const int num = bad ? 0 : (C + KV8_PAGE - 1) / KV8_PAGE;
-  const int entries = sel ? (bad ? 0 : a.pages) : num;
-  float q[E], o[E], m = -INFINITY, sum = 0.f;
-  const __nv_bfloat16* qp = a.q.p + b * a.q.batch + j * a.q.row + (size_t)hq * D;
+template <int D, int MT>
+struct Lay {
+  static constexpr int PB = KV8_PAGE * D;                 // bytes of a page-head
+  static constexpr int PADK = D == 128 ? 16 : 64;
+  static constexpr int KREG = 2 * PB + PADK;
+  static constexpr int STAGE = KREG + 2 * PB;
+  static constexpr int NST = D == 128 ? 3 : 4;
+  static constexpr int RING = NST * STAGE;                // of a warp
+  static constexpr int NR = 16 * MT;
+  static constexpr int PD = D + 8;                        // fp32 row of a partial: O, max, sum, pad
+  static constexpr int ROWB = PD * 4;
+  static constexpr int PART = 0;                          // [NW][NR] rows; the CTA's own result in the first NR
+  static constexpr int RECV = NW * NR * ROWB;             // [S][rows per owner], at most NR + 15 rows
+  static constexpr int MERGE = RECV + (NR + MAX_SPLIT - 1) * ROWB;
+  static constexpr int TOTAL = NW * RING > MERGE ? NW * RING : MERGE;
+  static_assert(STAGE % 16 == 0 && RING % 16 == 0, "bulk copies land on 16 bytes");
+  static_assert(STAGE >= KV8_PAGE * D * 2, "16 bf16 value rows of the block fit a stage");
+};
+
+struct Params {
+  Kv8Pool pool;
+  Kv8Src q, k_blk, v_blk;
+  const int32_t* page_table;
+  const int32_t* ctx_len;
+  const int32_t* sel;
+  int pages;
+  __nv_bfloat16* out;
+  int B, R, Hq, Hkv, G, num_pages, max_pages;
+  int rows;          // query rows of a unit before it is cut into groups: G * R, or G with selected pages
+  int groups;        // groups of NR rows
+  float scale_log2;
+  int kv_stable, block_full;
+  int* err;
+};
+
+CS_DEV void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(dst),
+      "l"(src), "r"(bytes), "r"(smem_u32(bar)), "l"(policy)
+      : "memory");
+}
+CS_DEV void mma_f16(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+CS_DEV uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+CS_DEV uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
+CS_DEV uint32_t lds32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
+  return v;
+}
+
+// What a warp carries from tile to tile: 16 MT rows, this lane's two of each 16 (g and g + 8).
+template <int D, int MT>
+struct State {
+  uint32_t q[MT][D / 16][4];    // f16 queries: the lane's D / 4 dimensions, four a fragment
+  float f[MT][2];               // score factor of a row: its power of two, the softmax scale, log2 e
+  float o[MT][D / 8][4];
+  float m[MT][2], l[MT][2];
+  float vref;                   // o and the weights count in units of this values' scale
+};
+
+// Running maximum, weights and sums of 16 rows for scores s (base 2, masked ones -inf); s becomes the
+// weights times 2^14.
+template <int D, int MT, int N>
+CS_DEV void softmax_step(State<D, MT>& st, int t, float (&s)[N][4]) {
+  float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    q[e] = __bfloat162float(qp[e * 32 + lane]);
-    o[e] = 0.f;
+  for (int i = 0; i < N; ++i) {
+    mx[0] = fmaxf(mx[0], fmaxf(s[i][0], s[i][1]));
+    mx[1] = fmaxf(mx[1], fmaxf(s[i][2], s[i][3]));
   }
-  auto key = [&](const float (&k)[E], const float (&v)[E], float ks, float vs) {
-    float s = 0.f;
+  float base[2], a[2];
+  bool moved = false;
 #pragma unroll
-    for (int e = 0; e < E; ++e) s += q[e] * k[e];
+  for (int r = 0; r < 2; ++r) {
+    mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 1));
+    mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 2));
+    const float mn = fmaxf(st.m[t][r], mx[r]);
+    base[r] = (mn == -INFINITY ? 0.f : mn) - P_BITS;
+    a[r] = exp2_approx(st.m[t][r] - P_BITS - base[r]);
+    moved |= mn != st.m[t][r];
+    st.m[t][r] = mn;
+  }
+  if (__any_sync(0xffffffffu, moved)) {
+    st.l[t][0] *= a[0];
+    st.l[t][1] *= a[1];
 #pragma unroll
-    for (int x = 16; x > 0; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
-    s *= ks * a.scale;
-    const float n = fmaxf(m, s);
-    const float w = expf(s - n), c = m == -INFINITY ? 0.f : expf(m - n);
-    sum = sum * c + w;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = o[e] * c + w * vs * v[e];
-    m = n;
-  };
-  for (int i = 0; i < entries; ++i) {
-    const int p = sel ? sel[i] : i;
-    if (p < 0) break;
-    const int phys = p < num ? table[p] : -1;
-    if ((unsigned)phys >= (unsigned)a.num_pages) {
-      if (lane == 0) set_err(err, ERR_PAGE);
-      continue;
+    for (int i = 0; i < D / 8; ++i) {
+      st.o[t][i][0] *= a[0];
+      st.o[t][i][1] *= a[0];
+      st.o[t][i][2] *= a[1];
+      st.o[t][i][3] *= a[1];
     }
-    const size_t cell = (size_t)phys * a.Hkv + h;
-    const float ks = a.pool.scale[cell * 2], vs = a.pool.scale[cell * 2 + 1];
-    for (int t = warp; t < KV8_PAGE && p * KV8_PAGE + t < C; t += WARPS) {
-      float k[E], v[E];
+  }
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int d = e * 32 + lane;
-        k[e] = kv8_floats(a.pool.k[(cell * KV8_PAGE + t) * D + d]).x;
-        v[e] = kv8_floats(a.pool.v[(cell * D + d) * KV8_PAGE + t]).x;
+  for (int i = 0; i < N; ++i) {
+    s[i][0] = exp2_approx(s[i][0] - base[0]);
+    s[i][1] = exp2_approx(s[i][1] - base[0]);
+    s[i][2] = exp2_approx(s[i][2] - base[1]);
+    s[i][3] = exp2_approx(s[i][3] - base[1]);
+    st.l[t][0] += s[i][0] + s[i][1];
+    st.l[t][1] += s[i][2] + s[i][3];
+  }
+}
+
+// Values of scale `top` are to join the output (the same in every lane).
+template <int D, int MT>
+CS_DEV void raise_unit(State<D, MT>& st, float top) {
+  if (top <= st.vref) return;
+  const float by = st.vref * kv8_inverse(top);
+  st.vref = top;
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) st.o[t][i][e] *= by;
+}
+
+// One tile: two pages' keys at sk and values at sv, ks / vs their scales, n their tokens (16 both
+// unless MASK).
+template <int D, int MT, bool MASK>
+CS_DEV void tile(State<D, MT>& st, uint32_t sk, uint32_t sv, const float (&ks)[2], const float (&vs)[2], int n0, int n1, int lane) {
+  using L = Lay<D, MT>;
+  const int g = lane >> 2, c = lane & 3;
+  float s[MT][4][4];
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[t][i][0] = s[t][i][1] = s[t][i][2] = s[t][i][3] = 0.f;
+  const uint32_t ka = sk + (uint32_t)((g & 1) * (L::PB + L::PADK) + (g >> 1) * 4 * D + c * (D / 4));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int x = 0; x < D / 64; ++x) {
+      const uint4 w = lds128(ka + (uint32_t)(i * D + x * 16));
+      const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const uint32_t b0 = kv8_f16x2(ww[y]), b1 = kv8_f16x2_hi(ww[y]);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) mma_f16(s[t][i], st.q[t][x * 4 + y], b0, b1);
       }
-      key(k, v, ks, vs);
     }
   }
-  for (int t = warp; t < (a.block_full ? a.R : j + 1); t += WARPS) {
-    float k[E], v[E];
+  raise_unit(st, fmaxf(vs[0], vs[1]));
+  const float iv = kv8_inverse(st.vref), v0 = vs[0] * iv, v1 = vs[1] * iv;
+  uint32_t p[MT][2][4];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int d = e * 32 + lane;
-      k[e] = __bfloat162float(a.k_blk.p[b * a.k_blk.batch + t * a.k_blk.row + (size_t)h * D + d]);
-      v[e] = __bfloat162float(a.v_blk.p[b * a.v_blk.batch + t * a.v_blk.row + (size_t)h * D + d]);
+  for (int t = 0; t < MT; ++t) {
+    const float f00 = st.f[t][0] * ks[0], f01 = st.f[t][0] * ks[1], f10 = st.f[t][1] * ks[0], f11 = st.f[t][1] * ks[1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      s[t][i][0] *= f00;
+      s[t][i][1] *= f01;
+      s[t][i][2] *= f10;
+      s[t][i][3] *= f11;
+      if (MASK) {
+        if (4 * c + i >= n0) s[t][i][0] = s[t][i][2] = -INFINITY;
+        if (4 * c + i >= n1) s[t][i][1] = s[t][i][3] = -INFINITY;
+      }
     }
-    key(k, v, 1.f, 1.f);
-  }
+    softmax_step<D, MT, 4>(st, t, s[t]);
 #pragma unroll
-  for (int e = 0; e < E; ++e) part[warp][e * 32 + lane] = o[e];
-  if (lane == 0) {
-    part[warp][D] = m;
-    part[warp][D + 1] = sum;
+    for (int e = 0; e < 2; ++e) {
+      const float v = e ? v1 : v0;
+      p[t][e][0] = pack_f16(s[t][0][e] * v, s[t][1][e] * v);
+      p[t][e][1] = pack_f16(s[t][0][2 + e] * v, s[t][1][2 + e] * v);
+      p[t][e][2] = pack_f16(s[t][2][e] * v, s[t][3][e] * v);
+      p[t][e][3] = pack_f16(s[t][2][2 + e] * v, s[t][3][2 + e] * v);
+    }
+  }
+  // cells behind a page's last token may hold anything, NaN too: they read as 0
+  uint32_t keep[2] = {0xffffffffu, 0xffffffffu};
+  if (MASK) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int have = (e ? n1 : n0) - 4 * c;
+      keep[e] = have >= 4 ? 0xffffffffu : have <= 0 ? 0u : (1u << (8 * have)) - 1u;
+    }
+  }
+  const uint32_t va = sv + (uint32_t)(g * KV8_PAGE + c * 4);
+#pragma unroll
+  for (int d = 0; d < D / 8; ++d) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      uint32_t w = lds32(va + (uint32_t)(e * L::PB + d * 8 * KV8_PAGE));
+      if (MASK) w &= keep[e];
+      const uint32_t b0 = kv8_f16x2(w), b1 = kv8_f16x2_hi(w);
+#pragma unroll
+      for (int t = 0; t < MT; ++t) mma_f16(st.o[t][d], p[t][e], b0, b1);
+    }
+  }
+}
+
+template <int D, int MT, bool SEL>
+__global__ void __launch_bounds__(NW * 32, 2) kv8_attn_kernel(const Params p) {
+  using L = Lay<D, MT>;
+  constexpr int NST = L::NST;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ uint64_t full[NW][NST];
+  __shared__ uint64_t recv_bar;
+  __shared__ int seq_slot;
+  __shared__ float weight[L::NR + MAX_SPLIT];              // [S][rows per owner]
+  const int S = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
+  if (tid == 0) {
+    for (int w = 0; w < NW; ++w)
+      for (int s = 0; s < NST; ++s) mbar_init(&full[w][s], 1);
+    mbar_init(&recv_bar, 1);
+    fence_barrier_init();
   }
   __syncthreads();
-  for (int d = threadIdx.x; d < D; d += WARPS * 32) {
-    float top = -INFINITY, l = 0.f, x = 0.f;
-    for (int w = 0; w < WARPS; ++w) top = fmaxf(top, part[w][D]);
-    for (int w = 0; w < WARPS; ++w) {
-      const float c = part[w][D] == -INFINITY ? 0.f : expf(part[w][D] - top);
-      l += part[w][D + 1] * c;
-      x += part[w][d] * c;
+  // Without the stable-cache promise everything waits for the previous kernel; with it only what that
+  // kernel may have written (q, the block, sel) does.  Dependents may start only then: one under the
+  // promise reads the cache at once.
+  if (!p.kv_stable) griddep_wait();
+  griddep_launch_dependents();
+
+  // ---------------------------------------------------------------- the unit
+  int u = blockIdx.y;
+  const int rg = u % p.groups;
+  u /= p.groups;
+  const int h = u % p.Hkv;
+  const int jj = SEL ? u / p.Hkv : 0;                      // block row of the unit
+  const int b = p.B > 1 && p.B <= RANK_MAX_B ? sequence_by_rank(p.ctx_len, p.B, (int)blockIdx.z, &seq_slot) : (int)blockIdx.z;
+  const int row0 = rg * L::NR, nr = min(L::NR, p.rows - row0);
+  const int C = p.ctx_len[b];
+  const bool bad = C < 0 || C > p.max_pages * KV8_PAGE;
+  if (bad && rank == 0 && blockIdx.y == 0 && tid == 0) set_err(p.err, ERR_CTX);
+  const int num = bad ? 0 : (C + KV8_PAGE - 1) / KV8_PAGE;           // pages of the context
+  if (SEL && p.kv_stable) griddep_wait();                            // the list comes from the kernel before
+  const int entries = SEL ? (bad ? 0 : p.pages) : num;
+  const int tiles = (entries + 1) >> 1, stride = S * NW, mine = rank * NW + warp;
+  const int n = mine < tiles ? (tiles - mine + stride - 1) / stride : 0;      // tiles of this warp
+  const int32_t* table = p.page_table + (size_t)b * p.max_pages;
+  const int32_t* list = SEL ? p.sel + (((size_t)b * p.R + jj) * p.Hkv + h) * p.pages : nullptr;
+  const int block_groups = bad || rank != S - 1 ? 0 : ((SEL && !p.block_full ? jj + 1 : p.R) + 15) / 16;
+  const bool has_block = NW - 1 - warp < block_groups;     // 16 block rows at a time, from the last warp back
+
+  // ---------------------------------------------------------------- the stream of tiles
+  // Lane 2 i + e holds page e of the warp's i-th next tile: where it is, its tokens, its scales.
+  const uint64_t pol = p.groups > 1 || (SEL && p.R > 1) ? l2_policy_evict_normal() : l2_policy_evict_first();
+  uint8_t* ring = smem + warp * L::RING;
+  int phys = 0, count = 0;                                 // of the 16 tiles being issued
+  float2 scale_i = make_float2(0.f, 0.f), scale_c = scale_i;
+  int count_c = 0;
+  unsigned whole = 0u;                                     // of the 16 being consumed: pages of 16 tokens
+  auto look_up = [&](int t0) {                             // tiles t0 .. t0 + 15 of the warp
+    const int e = 2 * (mine + (t0 + (lane >> 1)) * stride) + (lane & 1);
+    int page = -1;
+    if (t0 + (lane >> 1) < n && e < entries) page = SEL ? list[e] : e;
+    count = 0;
+    scale_i = make_float2(0.f, 0.f);
+    if (page >= 0) {
+      phys = page < num ? table[page] : -1;
+      if ((unsigned)phys < (unsigned)p.num_pages) {
+        count = min(KV8_PAGE, C - page * KV8_PAGE);
+        scale_i = *reinterpret_cast<const float2*>(p.pool.scale + ((size_t)phys * p.Hkv + h) * 2);
+      } else {
+        set_err(p.err, ERR_PAGE);
+      }
     }
-    a.out[(((size_t)b * a.R + j) * a.Hq + hq) * D + d] = __float2bfloat16_rn(x / l);
+  };
+  auto issue = [&](int t) {                                // copy the warp's tile t
+    if ((t & 15) == 0) look_up(t);
+    const int st = t % NST, at = 2 * (t & 15);
+    const int e = lane & 1, tensor = (lane >> 1) & 1;      // lanes 0..3: one copy each
+    const int ph = __shfl_sync(0xffffffffu, phys, at + e);
+    const unsigned have = __ballot_sync(0xffffffffu, count > 0) >> at & 3u;
+    if (lane == 0) mbar_arrive_expect_tx(&full[warp][st], (uint32_t)__popc(have) * 2u * L::PB);
+    __syncwarp();
+    if (lane < 4 && (have >> e & 1u)) {
+      const size_t off = ((size_t)ph * p.Hkv + h) * L::PB;
+      const uint32_t dst = smem_u32(ring + st * L::STAGE) + (tensor ? L::KREG + e * L::PB : e * (L::PB + L::PADK));
+      bulk_load(dst, (tensor ? p.pool.v : p.pool.k) + off, L::PB, &full[warp][st], pol);
+    }
+  };
+  const int ahead = has_block ? NST - 1 : NST;             // the block's values take the last stage first
+  for (int t = 0; t < min(n, ahead); ++t) issue(t);
+  if (!SEL && p.kv_stable) griddep_wait();
+
+  // ---------------------------------------------------------------- queries
+  State<D, MT> st;
+  st.vref = 0.f;
+  const __nv_bfloat16* qrow[MT][2];
+  int lim[MT][2];                                          // last block row that the query row sees
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int x = t * 16 + g + 8 * r;
+      const int row = row0 + min(x, nr - 1);
+      const int j = SEL ? jj : row / p.G, head = h * p.G + (SEL ? row : row % p.G);
+      qrow[t][r] = x < nr ? p.q.p + b * p.q.batch + j * p.q.row + (size_t)head * D + c * (D / 4) : nullptr;
+      lim[t][r] = p.block_full ? p.R - 1 : j;
+      st.m[t][r] = -INFINITY;
+      st.l[t][r] = 0.f;
+    }
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) st.o[t][i][0] = st.o[t][i][1] = st.o[t][i][2] = st.o[t][i][3] = 0.f;
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      uint4 w[D / 32];
+      float amax = 0.f;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        w[i] = qrow[t][r] ? *reinterpret_cast<const uint4*>(qrow[t][r] + i * 8) : make_uint4(0u, 0u, 0u, 0u);
+        const uint32_t ww[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          amax = fmaxf(amax, fmaxf(kv8_finite_abs(__uint_as_float(ww[y] << 16)), kv8_finite_abs(__uint_as_float(ww[y] & 0xffff0000u))));
+      }
+      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+      const float sc = kv8_scale127(amax), inv = kv8_inverse(sc);      // |q / sc| <= 127
+      st.f[t][r] = sc * p.scale_log2;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        const uint32_t ww[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+        for (int y = 0; y < 4; ++y)        // pairs of the lane's dimensions 8 i + 2 y: fragment 2 i + y / 2, half y & 1
+          st.q[t][2 * i + (y >> 1)][r + 2 * (y & 1)] =
+              pack_f16(__uint_as_float(ww[y] << 16) * inv, __uint_as_float(ww[y] & 0xffff0000u) * inv);
+      }
+    }
+
+  // ---------------------------------------------------------------- the block's own rows
+  if (has_block) {
+    uint8_t* vbuf = ring + (NST - 1) * L::STAGE;
+    for (int kg = NW - 1 - warp; kg < block_groups; kg += NW) {
+      const int k0 = kg * 16;
+      __syncwarp();
+      // 16 value rows of 2 D bytes, their 16-byte chunks turned by the row against bank conflicts; they
+      // count in units of vref as a page's values do (the weights' bf16 holds its inverse)
+      float vmax = 0.f;
+      for (int e = lane; e < 16 * (D / 8); e += 32) {
+        const int r = e / (D / 8), ch = e % (D / 8);
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (k0 + r < p.R) v = *reinterpret_cast<const uint4*>(p.v_blk.p + b * p.v_blk.batch + (k0 + r) * p.v_blk.row + (size_t)h * D + ch * 8);
+        *reinterpret_cast<uint4*>(vbuf + r * (2 * D) + ((ch ^ (r & 7)) * 16)) = v;
+        const uint32_t vv[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          vmax = fmaxf(vmax, fmaxf(kv8_finite_abs(__uint_as_float(vv[y] << 16)), kv8_finite_abs(__uint_as_float(vv[y] & 0xffff0000u))));
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, o));
+      raise_unit(st, kv8_scale_of(vmax));
+      const float iv = kv8_inverse(st.vref);
+      float s[MT][2][4];
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) s[t][i][0] = s[t][i][1] = s[t][i][2] = s[t][i][3] = 0.f;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int key = k0 + i * 8 + g;
+        const __nv_bfloat16* kr = p.k_blk.p + b * p.k_blk.batch + key * p.k_blk.row + (size_t)h * D + c * (D / 4);
+#pragma unroll
+        for (int x = 0; x < D / 32; ++x) {
+          uint4 w = make_uint4(0u, 0u, 0u, 0u);
+          if (key < p.R) w = *reinterpret_cast<const uint4*>(kr + x * 8);
+#pragma unroll
+          for (int t = 0; t < MT; ++t) {
+            uint4 qa = make_uint4(0u, 0u, 0u, 0u), qb = qa;
+            if (qrow[t][0]) qa = *reinterpret_cast<const uint4*>(qrow[t][0] + x * 8);
+            if (qrow[t][1]) qb = *reinterpret_cast<const uint4*>(qrow[t][1] + x * 8);
+            const uint32_t a0[4] = {qa.x, qb.x, qa.y, qb.y}, a1[4] = {qa.z, qb.z, qa.w, qb.w};
+            mma_16816(s[t][i], a0, w.x, w.y);
+            mma_16816(s[t][i], a1, w.z, w.w);
+          }
+        }
+      }
+      __syncwarp();
+      uint32_t pf[MT][4];
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int key = k0 + i * 8 + 2 * c + e;
+            s[t][i][e] = key <= lim[t][0] ? s[t][i][e] * p.scale_log2 : -INFINITY;
+            s[t][i][2 + e] = key <= lim[t][1] ? s[t][i][2 + e] * p.scale_log2 : -INFINITY;
+          }
+        softmax_step<D, MT, 2>(st, t, s[t]);
+        pf[t][0] = pack_bf16(s[t][0][0] * iv, s[t][0][1] * iv);
+        pf[t][1] = pack_bf16(s[t][0][2] * iv, s[t][0][3] * iv);
+        pf[t][2] = pack_bf16(s[t][1][0] * iv, s[t][1][1] * iv);
+        pf[t][3] = pack_bf16(s[t][1][2] * iv, s[t][1][3] * iv);
+      }
+      const int key = (lane & 7) + ((lane >> 3) & 1) * 8;
+#pragma unroll
+      for (int d = 0; d < D / 8; d += 2) {
+        const int ch = d + (lane >> 4);
+        uint32_t b0, b1, b2, b3;
+        ldsm_x4_t(smem_u32(vbuf) + (uint32_t)(key * (2 * D) + ((ch ^ (key & 7)) * 16)), b0, b1, b2, b3);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+          mma_16816(st.o[t][d], pf[t], b0, b1);
+          mma_16816(st.o[t][d + 1], pf[t], b2, b3);
+        }
+      }
+    }
+    fence_proxy_async_smem();              // the stage is a bulk copy's next
+    __syncwarp();
+    if (ahead < n) issue(ahead);
   }
+
+  // ---------------------------------------------------------------- the cache
+  for (int t = 0; t < n; ++t) {
+    if ((t & 15) == 0) {
+      scale_c = scale_i;                   // (copies run at most NST tiles ahead: still these 16)
+      count_c = count;
+      whole = __ballot_sync(0xffffffffu, count == KV8_PAGE);
+    }
+    const int sg = t % NST, at = 2 * (t & 15);
+    const float ks[2] = {__shfl_sync(0xffffffffu, scale_c.x, at), __shfl_sync(0xffffffffu, scale_c.x, at + 1)};
+    const float vs[2] = {__shfl_sync(0xffffffffu, scale_c.y, at), __shfl_sync(0xffffffffu, scale_c.y, at + 1)};
+    if (!mbar_wait(&full[warp][sg], (uint32_t)(t / NST) & 1u)) set_err(p.err, ERR_TIMEOUT);
+    __syncwarp();
+    const uint32_t sk = smem_u32(ring + sg * L::STAGE);
+    if ((whole >> at & 3u) == 3u) {
+      tile<D, MT, false>(st, sk, sk + L::KREG, ks, vs, KV8_PAGE, KV8_PAGE, lane);
+    } else {
+      const int n0 = __shfl_sync(0xffffffffu, count_c, at), n1 = __shfl_sync(0xffffffffu, count_c, at + 1);
+      if (n0 + n1 > 0) tile<D, MT, true>(st, sk, sk + L::KREG, ks, vs, n0, n1, lane);
+    }
+    __syncwarp();
+    if (t + NST < n) issue(t + NST);
+  }
+  // After a wait that ran out a copy may still be in flight: wait again (bounded) before the ring is reused.
+  for (int s = 0; s < NST && s < n; ++s) mbar_wait(&full[warp][s], (uint32_t)((n - 1 - s) / NST) & 1u);
+
+  // ---------------------------------------------------------------- the warps' parts
+  __syncthreads();                         // every ring is idle
+  const int rpo = (nr + S - 1) / S;        // rows finished by each CTA of the cluster
+  if (S > 1) {
+    if (tid == 0) mbar_arrive_expect_tx(&recv_bar, (uint32_t)(S * rpo * L::ROWB));
+    cluster_arrive_relaxed();
+  }
+  float* part = reinterpret_cast<float*>(smem + L::PART);
+  {
+    const float unit = st.vref * exp2f(-P_BITS), one = exp2f(-P_BITS);
+    float* mypart = part + warp * L::NR * L::PD;
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        float* row = mypart + (t * 16 + g + 8 * r) * L::PD;
+#pragma unroll
+        for (int d = 0; d < D / 8; ++d)
+          *reinterpret_cast<float2*>(row + d * 8 + 2 * c) = make_float2(st.o[t][d][2 * r] * unit, st.o[t][d][2 * r + 1] * unit);
+        float l = st.l[t][r];
+        l += __shfl_xor_sync(0xffffffffu, l, 1);
+        l += __shfl_xor_sync(0xffffffffu, l, 2);
+        if (c == 0) *reinterpret_cast<float2*>(row + D) = make_float2(st.m[t][r], l * one);
+      }
+  }
+  __syncthreads();
+  // A row's NW parts into the first, by a group of D / 4 lanes.
+  constexpr int LPR = D / 4;
+  static_assert(L::NR % (NW * 32 / LPR) == 0, "whole passes over the rows");
+  for (int r0 = 0; r0 < nr; r0 += NW * 32 / LPR) {         // (a last pass may touch rows past nr)
+    const int r = r0 + tid / LPR, x = tid % LPR * 4;
+    float2 ml[NW];
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      ml[w] = *reinterpret_cast<const float2*>(part + (w * L::NR + r) * L::PD + D);
+      top = fmaxf(top, ml[w].x);
+    }
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float l = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float a = ml[w].x == -INFINITY ? 0.f : exp2_approx(ml[w].x - top);
+      const float4 v = *reinterpret_cast<const float4*>(part + (w * L::NR + r) * L::PD + x);
+      acc.x += v.x * a;
+      acc.y += v.y * a;
+      acc.z += v.z * a;
+      acc.w += v.w * a;
+      l += ml[w].y * a;
+    }
+    __syncwarp();                          // every lane of the row has read its maxima and sums
+    *reinterpret_cast<float4*>(part + r * L::PD + x) = acc;
+    if (x == 0) *reinterpret_cast<float2*>(part + r * L::PD + D) = make_float2(top, l);
+  }
+  fence_proxy_async_smem();
+  __syncthreads();
+
+  // ---------------------------------------------------------------- the CTAs' parts
+  const float* src = part;
+  if (S > 1) {
+    cluster_wait();                        // every CTA's receiving rows are free, its barrier armed
+    float* recv = reinterpret_cast<float*>(smem + L::RECV);
+    if (lane == 0) {
+      for (int o = warp; o < S; o += NW)
+        bulk_copy_s2s(dsmem_map(smem_u32(recv) + (uint32_t)(rank * rpo * L::ROWB), (uint32_t)o), smem_u32(part + o * rpo * L::PD),
+                      (uint32_t)(rpo * L::ROWB), dsmem_map(smem_u32(&recv_bar), (uint32_t)o));
+    }
+    if (!mbar_wait(&recv_bar, 0)) set_err(p.err, ERR_TIMEOUT);
+    src = recv;
+    cluster_arrive_relaxed();
+  }
+  const int own0 = rank * rpo;
+  for (int r = warp; r < rpo && own0 + r < nr; r += NW) {
+    const float2 ml = lane < S ? *reinterpret_cast<const float2*>(src + (lane * rpo + r) * L::PD + D) : make_float2(-INFINITY, 0.f);
+    float top = ml.x;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float a = ml.x == -INFINITY ? 0.f : exp2_approx(ml.x - top);
+    float sum = ml.y * a;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane < S) weight[lane * rpo + r] = sum == 0.f ? 0.f : a / sum;   // (0: a skipped sequence)
+  }
+  __syncthreads();
+  for (int e = tid; e < rpo * (D / 4); e += NW * 32) {
+    const int r = e / (D / 4), x = e % (D / 4) * 4;
+    if (own0 + r >= nr) break;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int s = 0; s < S; ++s) {
+      const float a = weight[s * rpo + r];
+      const float4 v = *reinterpret_cast<const float4*>(src + (s * rpo + r) * L::PD + x);
+      acc.x += v.x * a;
+      acc.y += v.y * a;
+      acc.z += v.z * a;
+      acc.w += v.w * a;
+    }
+    const int row = row0 + own0 + r;
+    const int j = SEL ? jj : row / p.G, head = h * p.G + (SEL ? row : row % p.G);
+    *reinterpret_cast<uint2*>(p.out + (((size_t)b * p.R + j) * p.Hq + head) * D + x) = make_uint2(pack_bf16(acc.x, acc.y), pack_bf16(acc.z, acc.w));
+  }
+  if (S > 1) cluster_wait();               // every copy out of this CTA has landed
+}
+
+template <int D, int MT, bool SEL>
+struct Variant {
+  using L = Lay<D, MT>;
+  static KernelLimits& limits() {
+    static KernelLimits lim;
+    return lim;
+  }
+  static void config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute* attr, dim3 grid, int S) {
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(NW * 32);
+    cfg.dynamicSmemBytes = L::TOTAL;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = S;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+  }
+  // Clusters of S CTAs resident at once (cached; the device's answer does not depend on the grid).
+  static int resident(int S) {
+    static std::atomic<int> cache[KL_MAX_DEV][MAX_SPLIT + 1];
+    int dev = 0;
+    cudaGetDevice(&dev);
+    std::atomic<int>& slot = cache[dev < KL_MAX_DEV ? dev : KL_MAX_DEV - 1][S];
+    int c = slot.load(std::memory_order_relaxed);
+    if (c == 0) {
+      cudaLaunchConfig_t cfg = {};
+      cudaLaunchAttribute attr[2];
+      config(cfg, attr, dim3(S, 1024, 1), S);
+      cfg.numAttrs = 1;
+      int n = 0;
+      if (ensure_kernel_limits((const void*)kv8_attn_kernel<D, MT, SEL>, limits(), L::TOTAL, true) != cudaSuccess ||
+          cudaOccupancyMaxActiveClusters(&n, kv8_attn_kernel<D, MT, SEL>, &cfg) != cudaSuccess) {
+        cudaGetLastError();
+        n = 0;
+      }
+      c = n + 1;
+      slot.store(c, std::memory_order_relaxed);
+    }
+    return c - 1;
+  }
+  static cudaError_t launch(const Params& p, int max_tiles, cudaStream_t stream) {
+    const cudaError_t e = ensure_kernel_limits((const void*)kv8_attn_kernel<D, MT, SEL>, limits(), L::TOTAL, true);
+    if (e != cudaSuccess) return e;
+    const long long uy = (long long)p.groups * p.Hkv * (SEL ? p.R : 1), units = uy * p.B;
+    // Splits: about one wave of CTAs, a tile for every warp at least; no cluster that cannot be resident.
+    const long long slots = resident(1) > 0 ? resident(1) : 2 * device_num_sms();
+    int S = 1;
+    while (S < MAX_SPLIT && units * S < slots && 2 * S * NW <= max_tiles) S *= 2;
+    while (S > 1 && resident(S) < 1) S >>= 1;
+    if (uy > 65535) return cudaErrorInvalidValue;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    config(cfg, attr, dim3(S, (unsigned)uy, p.B), S);
+    cfg.stream = stream;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kv8_attn_kernel<D, MT, SEL>, p);
+  }
+};
+
+template <bool SEL>
+cudaError_t pick(Params& p, int D, int tiles, cudaStream_t stream) {
+  const bool two = p.rows > 16;
+  p.groups = (p.rows + (two ? 31 : 15)) / (two ? 32 : 16);
+  if (D == 128) return two ? Variant<128, 2, SEL>::launch(p, tiles, stream) : Variant<128, 1, SEL>::launch(p, tiles, stream);
+  return two ? Variant<64, 2, SEL>::launch(p, tiles, stream) : Variant<64, 1, SEL>::launch(p, tiles, stream);
 }
 
 }  // namespace
 
 cudaError_t launch_kv8_attn(const Kv8AttnArgs& a, int* err, cudaStream_t stream) {
-  const unsigned grid = (unsigned)a.B * a.R * a.Hq;
-  return a.D == 128 ? launch_pdl(kv8_attn_kernel<128>, dim3(grid), dim3(WARPS * 32), 0, stream, a, err)
-                    : launch_pdl(kv8_attn_kernel<64>, dim3(grid), dim3(WARPS * 32), 0, stream, a, err);
+  Params p{};
+  p.pool = a.pool;
+  p.q = a.q;
+  p.k_blk = a.k_blk;
+  p.v_blk = a.v_blk;
+  p.page_table = a.page_table;
+  p.ctx_len = a.ctx_len;
+  p.sel = a.sel;
+  p.pages = a.pages;
+  p.out = a.out;
+  p.B = a.B;
+  p.R = a.R;
+  p.Hq = a.Hq;
+  p.Hkv = a.Hkv;
+  p.G = a.Hq / a.Hkv;
+  p.num_pages = a.num_pages;
+  p.max_pages = a.max_pages;
+  p.rows = a.sel ? p.G : p.G * a.R;
+  p.scale_log2 = a.scale * 1.4426950408889634f;
+  p.kv_stable = a.kv_stable;
+  p.block_full = a.block_full;
+  p.err = err;
+  const int tiles = a.sel ? (a.pages + 1) / 2 : (a.max_ctx + 2 * KV8_PAGE - 1) / (2 * KV8_PAGE);
+  return a.sel ? pick<true>(p, a.D, tiles, stream) : pick<false>(p, a.D, tiles, stream);
 }
 
 }  // namespace cospec
