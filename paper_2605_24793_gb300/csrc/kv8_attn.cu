@@ -8,9 +8,11 @@
 //
 // q . k^T and p . v run on mma.m16n8k16 with f16 operands.  An e4m3 code is exact in f16; q is brought
 // to f16 by a power of two per row (bf16's 8 bits fit f16's 11, values 2^-14 below the row's largest
-// lose bits only below 2^-25 of it); p is held as 2^14 p, so that weights down to 2^-38 count.  The pages'
-// scales are powers of two: the keys' joins the score's factor, the values' the weight, relative to the
-// largest seen so far (the output is rescaled, exactly, when that grows).
+// lose bits only below 2^-25 of it).  p is held as 2^6 p relative to a reference that follows the running
+// maximum only when that has grown by 2^8, so that the output is seldom rescaled; weights down to 2^-30
+// of the largest count.  The pages' scales are powers of two: the keys' joins the score's factor, the
+// values' the weight's exponent, relative to the largest seen so far (the output is rescaled, exactly,
+// when that grows).
 //
 // The contraction's order is free, so every lane converts what it can load wide: of a key it takes 32
 // (16) dimensions side by side, the query rows laid out alike, and of a dimension's values four tokens of
@@ -31,7 +33,8 @@ namespace {
 
 constexpr int NW = 4;                     // warps of a CTA
 constexpr int MAX_SPLIT = 16;
-constexpr float P_BITS = 14.f;            // weights are held times 2^14
+constexpr float P_BITS = 6.f;             // weights are held times 2^6,
+constexpr float P_ROOM = 8.f;             // and may grow by 2^8 before the output is rescaled: below f16's 2^16
 
 template <int D, int MT>
 struct Lay {
@@ -47,7 +50,10 @@ struct Lay {
   static constexpr int PART = 0;                          // [NW][NR] rows; the CTA's own result in the first NR
   static constexpr int RECV = NW * NR * ROWB;             // [S][rows per owner], at most NR + 15 rows
   static constexpr int MERGE = RECV + (NR + MAX_SPLIT - 1) * ROWB;
-  static constexpr int TOTAL = NW * RING > MERGE ? NW * RING : MERGE;
+  static constexpr int BODY = NW * RING > MERGE ? NW * RING : MERGE;
+  // With 32 rows the query fragments, the same for all warps, live in shared memory: [MT][D / 16][32 lanes][16 B]
+  static constexpr bool QS = MT > 1;
+  static constexpr int TOTAL = BODY + (QS ? MT * (D / 16) * 512 : 0);
   static_assert(STAGE % 16 == 0 && RING % 16 == 0, "bulk copies land on 16 bytes");
   static_assert(STAGE >= KV8_PAGE * D * 2, "16 bf16 value rows of the block fit a stage");
 };
@@ -99,34 +105,29 @@ CS_DEV uint32_t lds32(uint32_t a) {
 // What a warp carries from tile to tile: 16 MT rows, this lane's two of each 16 (g and g + 8).
 template <int D, int MT>
 struct State {
-  uint32_t q[MT][D / 16][4];    // f16 queries: the lane's D / 4 dimensions, four a fragment
+  uint32_t q[MT == 1 ? D / 16 : 1][4];   // f16 queries: the lane's D / 4 dimensions, four a fragment
+  uint32_t qs;                  // or where they are in shared memory
   float f[MT][2];               // score factor of a row: its power of two, the softmax scale, log2 e
   float o[MT][D / 8][4];
-  float m[MT][2], l[MT][2];
+  float m[MT][2], l[MT][2];     // reference of the weights (base 2), their sum
   float vref;                   // o and the weights count in units of this values' scale
 };
 
-// Running maximum, weights and sums of 16 rows for scores s (base 2, masked ones -inf); s becomes the
-// weights times 2^14.
-template <int D, int MT, int N>
-CS_DEV void softmax_step(State<D, MT>& st, int t, float (&s)[N][4]) {
-  float mx[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    mx[0] = fmaxf(mx[0], fmaxf(s[i][0], s[i][1]));
-    mx[1] = fmaxf(mx[1], fmaxf(s[i][2], s[i][3]));
-  }
-  float base[2], a[2];
+// The reference of a row's weights after scores whose largest is mx: it stays while that is less than
+// 2^P_ROOM above it.  Where it moves for some row of the warp, sums and outputs follow.
+template <int D, int MT>
+CS_DEV void follow_max(State<D, MT>& st, int t, float mx0, float mx1, float (&base)[2]) {
+  float mx[2] = {mx0, mx1}, a[2];
   bool moved = false;
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
     mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 1));
     mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 2));
-    const float mn = fmaxf(st.m[t][r], mx[r]);
-    base[r] = (mn == -INFINITY ? 0.f : mn) - P_BITS;
-    a[r] = exp2_approx(st.m[t][r] - P_BITS - base[r]);
-    moved |= mn != st.m[t][r];
-    st.m[t][r] = mn;
+    const float was = st.m[t][r], now = mx[r] > was + P_ROOM ? mx[r] : was;
+    moved |= now != was;
+    st.m[t][r] = now;
+    base[r] = (now == -INFINITY ? 0.f : now) - P_BITS;
+    a[r] = exp2_approx(was - P_BITS - base[r]);
   }
   if (__any_sync(0xffffffffu, moved)) {
     st.l[t][0] *= a[0];
@@ -138,15 +139,6 @@ CS_DEV void softmax_step(State<D, MT>& st, int t, float (&s)[N][4]) {
       st.o[t][i][2] *= a[1];
       st.o[t][i][3] *= a[1];
     }
-  }
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    s[i][0] = exp2_approx(s[i][0] - base[0]);
-    s[i][1] = exp2_approx(s[i][1] - base[0]);
-    s[i][2] = exp2_approx(s[i][2] - base[1]);
-    s[i][3] = exp2_approx(s[i][3] - base[1]);
-    st.l[t][0] += s[i][0] + s[i][1];
-    st.l[t][1] += s[i][2] + s[i][3];
   }
 }
 
@@ -177,45 +169,83 @@ CS_DEV void tile(State<D, MT>& st, uint32_t sk, uint32_t sv, const float (&ks)[2
     for (int i = 0; i < 4; ++i) s[t][i][0] = s[t][i][1] = s[t][i][2] = s[t][i][3] = 0.f;
   const uint32_t ka = sk + (uint32_t)((g & 1) * (L::PB + L::PADK) + (g >> 1) * 4 * D + c * (D / 4));
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int x = 0; x < D / 64; ++x) {
+    uint32_t w[4][4];
 #pragma unroll
-    for (int x = 0; x < D / 64; ++x) {
-      const uint4 w = lds128(ka + (uint32_t)(i * D + x * 16));
-      const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+    for (int i = 0; i < 4; ++i) {
+      const uint4 v = lds128(ka + (uint32_t)(i * D + x * 16));
+      w[i][0] = v.x;
+      w[i][1] = v.y;
+      w[i][2] = v.z;
+      w[i][3] = v.w;
+    }
 #pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        const uint32_t b0 = kv8_f16x2(ww[y]), b1 = kv8_f16x2_hi(ww[y]);
+    for (int y = 0; y < 4; ++y) {
+      uint32_t a[MT][4];
 #pragma unroll
-        for (int t = 0; t < MT; ++t) mma_f16(s[t][i], st.q[t][x * 4 + y], b0, b1);
+      for (int t = 0; t < MT; ++t) {
+        if (L::QS) {
+          const uint4 v = lds128(st.qs + (uint32_t)((t * (D / 16) + x * 4 + y) * 512));
+          a[t][0] = v.x;
+          a[t][1] = v.y;
+          a[t][2] = v.z;
+          a[t][3] = v.w;
+        } else {
+#pragma unroll
+          for (int z = 0; z < 4; ++z) a[t][z] = st.q[L::QS ? 0 : x * 4 + y][z];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t b0 = kv8_f16x2(w[i][y]), b1 = kv8_f16x2_hi(w[i][y]);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) mma_f16(s[t][i], a[t], b0, b1);
       }
     }
   }
   raise_unit(st, fmaxf(vs[0], vs[1]));
-  const float iv = kv8_inverse(st.vref), v0 = vs[0] * iv, v1 = vs[1] * iv;
+  // A page's values' scale joins its weights as an exponent and leaves their sum again (60 binary
+  // orders below the largest, nothing of it is left in f16).
+  float ve[2], vi[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int k = max((int)(__float_as_uint(vs[e]) >> 23) - (int)(__float_as_uint(st.vref) >> 23), -60);
+    ve[e] = (float)k;
+    vi[e] = __uint_as_float((uint32_t)(127 - k) << 23);
+  }
   uint32_t p[MT][2][4];
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
-    const float f00 = st.f[t][0] * ks[0], f01 = st.f[t][0] * ks[1], f10 = st.f[t][1] * ks[0], f11 = st.f[t][1] * ks[1];
+    if (MASK) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      s[t][i][0] *= f00;
-      s[t][i][1] *= f01;
-      s[t][i][2] *= f10;
-      s[t][i][3] *= f11;
-      if (MASK) {
+      for (int i = 0; i < 4; ++i) {
         if (4 * c + i >= n0) s[t][i][0] = s[t][i][2] = -INFINITY;
         if (4 * c + i >= n1) s[t][i][1] = s[t][i][3] = -INFINITY;
       }
     }
-    softmax_step<D, MT, 4>(st, t, s[t]);
+    float base[2], mx[2];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const float v = e ? v1 : v0;
-      p[t][e][0] = pack_f16(s[t][0][e] * v, s[t][1][e] * v);
-      p[t][e][1] = pack_f16(s[t][0][2 + e] * v, s[t][1][2 + e] * v);
-      p[t][e][2] = pack_f16(s[t][2][e] * v, s[t][3][e] * v);
-      p[t][e][3] = pack_f16(s[t][2][2 + e] * v, s[t][3][2 + e] * v);
+    for (int r = 0; r < 2; ++r) {
+      const float m0 = fmaxf(fmaxf(s[t][0][2 * r], s[t][1][2 * r]), fmaxf(s[t][2][2 * r], s[t][3][2 * r]));
+      const float m1 = fmaxf(fmaxf(s[t][0][2 * r + 1], s[t][1][2 * r + 1]), fmaxf(s[t][2][2 * r + 1], s[t][3][2 * r + 1]));
+      mx[r] = fmaxf(m0 * (st.f[t][r] * ks[0]), m1 * (st.f[t][r] * ks[1]));     // (NaN, as of -inf and 0, does not count)
     }
+    follow_max(st, t, mx[0], mx[1], base);
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float f = st.f[t][r] * ks[e], to = ve[e] - base[r];
+        float x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[i] = exp2_approx(fmaf(s[t][i][2 * r + e], f, to));
+          if (MASK && 4 * c + i >= (e ? n1 : n0)) x[i] = 0.f;
+        }
+        st.l[t][r] = fmaf((x[0] + x[1]) + (x[2] + x[3]), vi[e], st.l[t][r]);
+        p[t][e][r] = pack_f16(x[0], x[1]);
+        p[t][e][2 + r] = pack_f16(x[2], x[3]);
+      }
   }
   // cells behind a page's last token may hold anything, NaN too: they read as 0
   uint32_t keep[2] = {0xffffffffu, 0xffffffffu};
@@ -228,9 +258,9 @@ CS_DEV void tile(State<D, MT>& st, uint32_t sk, uint32_t sv, const float (&ks)[2
   }
   const uint32_t va = sv + (uint32_t)(g * KV8_PAGE + c * 4);
 #pragma unroll
-  for (int d = 0; d < D / 8; ++d) {
+  for (int e = 0; e < 2; ++e) {
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
+    for (int d = 0; d < D / 8; ++d) {
       uint32_t w = lds32(va + (uint32_t)(e * L::PB + d * 8 * KV8_PAGE));
       if (MASK) w &= keep[e];
       const uint32_t b0 = kv8_f16x2(w), b1 = kv8_f16x2_hi(w);
@@ -370,11 +400,16 @@ __global__ void __launch_bounds__(NW * 32, 2) kv8_attn_kernel(const Params p) {
       for (int i = 0; i < D / 32; ++i) {
         const uint32_t ww[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
 #pragma unroll
-        for (int y = 0; y < 4; ++y)        // pairs of the lane's dimensions 8 i + 2 y: fragment 2 i + y / 2, half y & 1
-          st.q[t][2 * i + (y >> 1)][r + 2 * (y & 1)] =
-              pack_f16(__uint_as_float(ww[y] << 16) * inv, __uint_as_float(ww[y] & 0xffff0000u) * inv);
+        for (int y = 0; y < 4; ++y) {      // pairs of the lane's dimensions 8 i + 2 y: fragment 2 i + y / 2, half y & 1
+          const uint32_t v = pack_f16(__uint_as_float(ww[y] << 16) * inv, __uint_as_float(ww[y] & 0xffff0000u) * inv);
+          const int fr = 2 * i + (y >> 1), z = r + 2 * (y & 1);
+          if (!L::QS) st.q[L::QS ? 0 : fr][z] = v;
+          else if (warp == 0) *reinterpret_cast<uint32_t*>(smem + L::BODY + (t * (D / 16) + fr) * 512 + lane * 16 + z * 4) = v;
+        }
       }
     }
+  st.qs = smem_u32(smem + L::BODY) + lane * 16;
+  if (L::QS) __syncthreads();
 
   // ---------------------------------------------------------------- the block's own rows
   if (has_block) {
@@ -435,7 +470,16 @@ __global__ void __launch_bounds__(NW * 32, 2) kv8_attn_kernel(const Params p) {
             s[t][i][e] = key <= lim[t][0] ? s[t][i][e] * p.scale_log2 : -INFINITY;
             s[t][i][2 + e] = key <= lim[t][1] ? s[t][i][2 + e] * p.scale_log2 : -INFINITY;
           }
-        softmax_step<D, MT, 2>(st, t, s[t]);
+        float base[2];
+        follow_max(st, t, fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][1][0], s[t][1][1])),
+                   fmaxf(fmaxf(s[t][0][2], s[t][0][3]), fmaxf(s[t][1][2], s[t][1][3])), base);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s[t][i][e] = exp2_approx(s[t][i][e] - base[e >> 1]);
+            st.l[t][e >> 1] += s[t][i][e];
+          }
         pf[t][0] = pack_bf16(s[t][0][0] * iv, s[t][0][1] * iv);
         pf[t][1] = pack_bf16(s[t][0][2] * iv, s[t][0][3] * iv);
         pf[t][2] = pack_bf16(s[t][1][0] * iv, s[t][1][1] * iv);
