@@ -25,13 +25,16 @@ CS_DEV float kv8_finite_abs(float x) {
   return a <= 3.4028235e38f ? a : 0.f;
 }
 
-// Two values to e4m3, round to nearest even: `lo` in the low byte.  Not finite: NaN.  (The
-// conversion itself would hold an infinity as the largest code; values within a scale never reach that.)
-CS_DEV uint32_t kv8_pack2(float lo, float hi) {
-  lo = fabsf(lo) <= 3.4028235e38f ? lo : __uint_as_float(0x7fffffffu);
-  hi = fabsf(hi) <= 3.4028235e38f ? hi : __uint_as_float(0x7fffffffu);
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+// x * inv, NaN where x is not finite: an infinity has no code, and the conversion would hold it as the
+// largest one.
+CS_DEV float kv8_scaled(float x, float inv) { return fmaf(x, inv, x * 0.f); }
+// Values within a scale to e4m3, round to nearest even, NaN to NaN; the first in the lowest byte.
+CS_DEV uint32_t kv8_pack4(const float (&x)[4]) {
+  uint32_t r;
+  asm("{\n .reg .b16 l, h;\n cvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n cvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n"
+      " mov.b32 %0, {l, h};\n}\n"
+      : "=r"(r)
+      : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]));
   return r;
 }
 // The two codes of `w`'s low half as f16 (exact).
@@ -62,13 +65,13 @@ CS_DEV void kv8_floats4(uint32_t w, float (&f)[4]) {
 }
 
 // Four bf16 of a 16-bit row.
-CS_DEV void kv8_load4(const __nv_bfloat16* p, float (&x)[4]) {
-  const uint2 u = *reinterpret_cast<const uint2*>(p);
+CS_DEV void kv8_floats_of(uint2 u, float (&x)[4]) {
   x[0] = __uint_as_float(u.x << 16);
   x[1] = __uint_as_float(u.x & 0xffff0000u);
   x[2] = __uint_as_float(u.y << 16);
   x[3] = __uint_as_float(u.y & 0xffff0000u);
 }
+CS_DEV void kv8_load4(const __nv_bfloat16* p, float (&x)[4]) { kv8_floats_of(*reinterpret_cast<const uint2*>(p), x); }
 CS_DEV void kv8_store4(__nv_bfloat16* p, const float (&x)[4]) {
   *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
 }
