@@ -535,7 +535,8 @@ COSPEC_API int cospec_kv8_append(const cospec_kv8_pool* pool, int first_layer, i
  *
  *    sel      int32 [batch, rows, num_kv_heads, pages]: logical pages, ascending, -1 after the last
  *    dims     the attention's (rows <= 64; num_pages that of the pool; softmax_scale, flags unused)
- *    1 <= pages; 0 <= sink, recent; sink + recent <= pages; max_pages_per_seq <= 32768 */
+ *    1 <= pages; 0 <= sink, recent; sink + recent <= pages; max_pages_per_seq <= 32768;
+ *    num_q_heads / num_kv_heads <= 256; batch <= 65535 */
 COSPEC_API int cospec_kv8_select(const cospec_attn_dims* dims, const cospec_kv8_pool* pool,
                                  int layer, const uint16_t* q, const cospec_kv8_strides* q_strides,
                                  const int32_t* page_table, const int32_t* ctx_len, int pages,

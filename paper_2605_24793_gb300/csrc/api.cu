@@ -614,7 +614,8 @@ COSPEC_API int cospec_kv8_select(const cospec_attn_dims* d, const cospec_kv8_poo
   st = kv8_pool(pool, layer, true, &a.pool);
   if (st != COSPEC_OK) return st;
   CS_CHECK_ARG(pages >= 1 && sink >= 0 && recent >= 0 && sink <= pages && recent <= pages - sink);
-  if (d->max_pages_per_seq > 32768) return COSPEC_ERR_UNSUPPORTED;
+  if (d->max_pages_per_seq > 32768 || d->num_q_heads / d->num_kv_heads > 256 || d->batch > 65535)
+    return COSPEC_ERR_UNSUPPORTED;
   if (d->batch == 0) return COSPEC_OK;
   st = kv8_src(q, q_strides, &a.q);
   if (st != COSPEC_OK) return st;
