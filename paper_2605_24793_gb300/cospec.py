@@ -606,25 +606,63 @@ class Rope:
         self.ref = ctypes.byref(self.c)
 
 
-def _rows5(t: torch.Tensor, name: str, shape) -> "ctypes._Pointer":
+# A call's Python side is most of a small call's time: geometry structures are kept by their
+# values, and each check is one comparison on the good path.
+_BF16, _F32, _I32, _I8 = torch.bfloat16, torch.float32, torch.int32, torch.int8
+_KEPT = 4096                      # structures kept of a kind
+_strides_kept: dict = {}
+_dims_kept: dict = {}
+
+
+def _keep(kept: dict, key, make):
+    if len(kept) >= _KEPT:
+        kept.clear()
+    ref = kept[key] = ctypes.byref(make())
+    return ref
+
+
+def _rows_ref(t: torch.Tensor, name: str, shape):
     """Checks bf16 rows [(layers,) batch, rows, heads, head_dim] whose heads and dimensions are
-    dense, and returns their strides."""
-    if t.dtype != torch.bfloat16:
-        raise TypeError(f"{name}: expected {torch.bfloat16}, got {t.dtype}")
-    if not t.is_cuda:
-        raise ValueError(f"{name}: must be a CUDA tensor")
+    dense, and returns a reference to their strides (cospec_kv8_strides)."""
+    if t.dtype is not _BF16:
+        raise TypeError(f"{name}: expected {_BF16}, got {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    st = t.stride()
-    if t.numel() and ((st[-1] != 1 and shape[-1] > 1) or (st[-2] != shape[-1] and shape[-2] > 1)):
+    key = (t.shape, t.stride())
+    ref = _strides_kept.get(key)
+    return ref if ref is not None else _new_strides(t, name, key)
+
+
+def _new_strides(t, name, key):
+    n, st = key
+    if t.numel() and ((st[-1] != 1 and n[-1] > 1) or (st[-2] != n[-1] and n[-2] > 1)):
         raise ValueError(f"{name}: heads and dimensions must be dense")
-    return Strides(st[0] if len(st) == 5 else 0, st[-4], st[-3])
+    lead = [0 if size == 1 else s for size, s in zip(n[:-2], st[:-2])]     # (one element has no stride)
+    return _keep(_strides_kept, key, lambda: Strides(*([0] * (3 - len(lead)) + lead)))
 
 
-def _ints(t: torch.Tensor, name: str, shape) -> None:
-    _req(t, torch.int32, name)
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
+def _dense(t: torch.Tensor, name: str, dtype, shape) -> None:
+    if t.dtype is not dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: must be contiguous")
+
+
+def _on_device(dev: int, *tensors) -> None:
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"a tensor is on {t.device}, but the current device is cuda:{dev}" if t.is_cuda
+                             else "every tensor must be a CUDA tensor")
+
+
+def _stream_ptr(stream, dev: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
 def kv8_append(pool: Kv8Pool, k, v, page_table, start, rows=None, rope: Optional[Rope] = None, layer: Optional[int] = None,
@@ -634,78 +672,77 @@ def kv8_append(pool: Kv8Pool, k, v, page_table, start, rows=None, rope: Optional
     be parts of a fused projection's output (any strides of the leading dimensions).  Row j of sequence
     b enters position start[b] + j for j < rows[b] (all rows without ``rows``).  k_out / q_out receive
     all rows of k / q rotated, in bf16.  See include/cospec.h."""
-    _need(k.dim() == (5 if layer is None else 4), "k must be [L, B, R, Hkv, D], or [B, R, Hkv, D] with layer")
-    lead = tuple(k.shape[:-2])
-    first, L = (0, k.shape[0]) if layer is None else (int(layer), 1)
-    _need(first >= 0 and (L == pool.layers if layer is None else first < pool.layers), "layer outside the pool")
-    B, R = lead[-2:]
-    shape = lead + (pool.kv_heads, pool.head_dim)
-    ks, vs = _rows5(k, "k", shape), _rows5(v, "v", shape)
+    shape = k.shape
+    _need(len(shape) == (5 if layer is None else 4), "k must be [L, B, R, Hkv, D], or [B, R, Hkv, D] with layer")
+    first, L = (0, shape[0]) if layer is None else (int(layer), 1)
+    _need(0 <= first < pool.layers and (layer is not None or L == pool.layers), "layer outside the pool")
+    _need(shape[-2] == pool.kv_heads and shape[-1] == pool.head_dim, "k must have the pool's heads and head_dim")
+    B = shape[-4]
+    vs = _rows_ref(v, "v", shape)
     _need(page_table.dim() == 2, "page_table must be [B, max_pages]")
-    _ints(page_table, "page_table", (B, page_table.shape[1]))
-    _ints(start, "start", (B,))
+    _dense(page_table, "page_table", _I32, (B, page_table.shape[1]))
     if rows is not None:
-        _ints(rows, "rows", (B,))
-    _launch_append(pool.ref, pool.device, first, L, B, R, rope, q, k, ks, v, vs, page_table, start, rows, q_out, k_out, shape, stream)
+        _dense(rows, "rows", _I32, (B,))
+    _need(pool.device == k.device, "the pool is on another device")
+    _launch_append(pool.ref, first, L, shape, rope, q, k, v, vs, page_table, start, rows, q_out, k_out, stream)
 
 
 def kv8_rotate(q, k, rope: Rope, start, q_out, k_out, stream=None) -> None:
     """The rotation of kv8_append by itself: q [B, R, Hq, D] and k [B, R, Hkv, D] (or with a leading
     layer dimension) turned to positions start[b] + j, in bf16, nothing appended."""
-    lead = tuple(k.shape[:-2])
-    _need(len(lead) in (2, 3), "k must be [B, R, Hkv, D] or [L, B, R, Hkv, D]")
-    B, R = lead[-2:]
-    ks = _rows5(k, "k", k.shape)
-    _ints(start, "start", (B,))
-    pool = Kv8PoolC(1, 1, k.shape[-2], k.shape[-1], 0, 0, 0, 0, 0)
-    _launch_append(ctypes.byref(pool), k.device, 0, lead[0] if len(lead) == 3 else 1, B, R, rope, q, k, ks, None, None, None, start,
-                   None, q_out, k_out, tuple(k.shape), stream)
+    shape = k.shape
+    _need(len(shape) in (4, 5), "k must be [B, R, Hkv, D] or [L, B, R, Hkv, D]")
+    pool = _dims_kept.get(shape[-2:]) or _keep(_dims_kept, shape[-2:], lambda: Kv8PoolC(1, 1, shape[-2], shape[-1], 0, 0, 0, 0, 0))
+    _launch_append(pool, 0, shape[0] if len(shape) == 5 else 1, shape, rope, q, k, None, None, None, start, None, q_out, k_out, stream)
 
 
-def _launch_append(pool_ref, device, first, L, B, R, rope, q, k, ks, v, vs, page_table, start, rows, q_out, k_out, shape, stream):
+def _launch_append(pool_ref, first, L, shape, rope, q, k, v, vs, page_table, start, rows, q_out, k_out, stream):
+    ks = _rows_ref(k, "k", shape)
+    B, R = shape[-4], shape[-3]
+    _dense(start, "start", _I32, (B,))
     _need((q is None) == (q_out is None), "q and q_out go together")
     Hq, qs = 0, None
     if q is not None:
-        _need(q.dim() == len(shape) and q.shape[:-2] == shape[:-2] and q.shape[-1] == shape[-1], "q must have k's batch, rows and head_dim")
+        _need(q.shape[:-2] == shape[:-2] and q.shape[-1] == shape[-1], "q must have k's batch, rows and head_dim")
         Hq = q.shape[-2]
-        qs = _rows5(q, "q", q.shape)
-        _req(q_out, torch.bfloat16, "q_out")
-        _need(q_out.shape == q.shape, "q_out must have q's shape")
+        qs = _rows_ref(q, "q", q.shape)
+        _dense(q_out, "q_out", _BF16, q.shape)
     if k_out is not None:
-        _req(k_out, torch.bfloat16, "k_out")
-        _need(tuple(k_out.shape) == shape, "k_out must have k's shape")
-    _same_device(k, v, q, q_out, k_out, page_table, start, rows, *(() if rope is None else (rope.cos, rope.sin)))
-    _need(device == k.device, "the pool is on another device")
-    by = ctypes.byref
-    _check(load_library().cospec_kv8_append(
-        pool_ref, first, L, B, R, Hq, None if rope is None else rope.ref, _ptr(q), None if qs is None else by(qs), _ptr(k), by(ks),
-        _ptr(v), None if vs is None else by(vs), _ptr(page_table), 0 if page_table is None else page_table.shape[1], _ptr(start),
-        _ptr(rows), _ptr(q_out), _ptr(k_out), _stream(stream)))
+        _dense(k_out, "k_out", _BF16, shape)
+    dev = torch._C._cuda_getDevice()
+    _on_device(dev, k, v, q, q_out, k_out, page_table, start, rows, None if rope is None else rope.cos)
+    _check((_lib or load_library()).cospec_kv8_append(
+        pool_ref, first, L, B, R, Hq, None if rope is None else rope.ref, _at(q), qs, k.data_ptr(), ks, _at(v), vs, _at(page_table),
+        0 if page_table is None else page_table.shape[1], start.data_ptr(), _at(rows), _at(q_out), _at(k_out), _stream_ptr(stream, dev)))
 
 
 def _kv8_dims(q, pool: Kv8Pool, layer: int, page_table, ctx_len, softmax_scale=0.0, flags=0):
-    _need(q.dim() == 4 and q.shape[3] == pool.head_dim, "q must be [B, R, Hq, D] with the pool's D")
+    """The call's checked geometry: q's shape and a reference to cospec_attn_dims."""
+    shape, table = q.shape, page_table.shape
+    _need(len(shape) == 4 and shape[3] == pool.head_dim, "q must be [B, R, Hq, D] with the pool's D")
     _need(0 <= layer < pool.layers, "layer outside the pool")
-    B, R, Hq, D = q.shape
-    _need(page_table.dim() == 2, "page_table must be [B, max_pages]")
-    _ints(page_table, "page_table", (B, page_table.shape[1]))
-    _ints(ctx_len, "ctx_len", (B,))
-    return AttnDims(B, R, Hq, pool.kv_heads, D, 16, page_table.shape[1], pool.num_pages, softmax_scale, flags)
+    _need(len(table) == 2, "page_table must be [B, max_pages]")
+    B = shape[0]
+    _dense(page_table, "page_table", _I32, (B, table[1]))
+    _dense(ctx_len, "ctx_len", _I32, (B,))
+    key = (shape, table[1], pool.kv_heads, pool.num_pages, softmax_scale, flags)
+    return shape, _dims_kept.get(key) or _keep(_dims_kept, key, lambda: AttnDims(
+        B, shape[1], shape[2], pool.kv_heads, shape[3], 16, table[1], pool.num_pages, softmax_scale, flags))
 
 
 def kv8_select(q, pool: Kv8Pool, layer: int, page_table, ctx_len, sel, sink: int = 1, recent: int = 2, stream=None) -> torch.Tensor:
     """The pages each block row reads: sel int32 [B, R, Hkv, pages] receives for row q[b, j] and each
     KV head the first ``sink`` and last ``recent`` pages of its context and those of the largest
     scores by the pages' summaries, ascending, -1 after the last."""
-    dims = _kv8_dims(q, pool, layer, page_table, ctx_len)
-    qs = _rows5(q, "q", q.shape)
+    shape, dims = _kv8_dims(q, pool, layer, page_table, ctx_len)
+    qs = _rows_ref(q, "q", shape)
     _need(pool.summary is not None, "the pool has no summaries")
-    _need(sel.dim() == 4, "sel must be [B, R, Hkv, pages]")
-    _ints(sel, "sel", (dims.batch, dims.rows, pool.kv_heads, sel.shape[3]))
-    _same_device(q, page_table, ctx_len, sel, pool.k)
-    by = ctypes.byref
-    _check(load_library().cospec_kv8_select(by(dims), pool.ref, layer, _ptr(q), by(qs), _ptr(page_table), _ptr(ctx_len),
-                                            sel.shape[3], int(sink), int(recent), _ptr(sel), _stream(stream)))
+    pages = sel.shape[-1]
+    _dense(sel, "sel", _I32, (shape[0], shape[1], pool.kv_heads, pages))
+    dev = torch._C._cuda_getDevice()
+    _on_device(dev, q, page_table, ctx_len, sel, pool.k)
+    _check((_lib or load_library()).cospec_kv8_select(dims, pool.ref, layer, q.data_ptr(), qs, page_table.data_ptr(), ctx_len.data_ptr(),
+                                                      pages, int(sink), int(recent), sel.data_ptr(), _stream_ptr(stream, dev)))
     return sel
 
 
@@ -714,20 +751,20 @@ def kv8_attn(q, k_blk, v_blk, pool: Kv8Pool, layer: int, page_table, ctx_len, ou
     """Verify attention over layer ``layer`` of an 8-bit cache and the block's own bf16 rows; with
     ``sel`` (kv8_select) over each row's chosen pages only.  q, k_blk and v_blk [B, R, H, D] may be parts of a
     fused projection's output.  Flags as verify_attn; see include/cospec.h."""
-    dims = _kv8_dims(q, pool, layer, page_table, ctx_len, softmax_scale,
-                     (ATTN_KV_STABLE if kv_stable else 0) | (ATTN_BLOCK_FULL if block_full else 0))
-    shape = (dims.batch, dims.rows, pool.kv_heads, pool.head_dim)
-    qs, ks, vs = _rows5(q, "q", q.shape), _rows5(k_blk, "k_blk", shape), _rows5(v_blk, "v_blk", shape)
-    _req(out, torch.bfloat16, "out")
-    _need(out.shape == q.shape, "out must have q's shape")
+    shape, dims = _kv8_dims(q, pool, layer, page_table, ctx_len, softmax_scale,
+                            (ATTN_KV_STABLE if kv_stable else 0) | (ATTN_BLOCK_FULL if block_full else 0))
+    block = (shape[0], shape[1], pool.kv_heads, pool.head_dim)
+    qs, ks, vs = _rows_ref(q, "q", shape), _rows_ref(k_blk, "k_blk", block), _rows_ref(v_blk, "v_blk", block)
+    _dense(out, "out", _BF16, shape)
     pages = 0
     if sel is not None:
         pages = sel.shape[-1]
-        _ints(sel, "sel", (dims.batch, dims.rows, pool.kv_heads, pages))
-    _same_device(q, k_blk, v_blk, page_table, ctx_len, sel, out, pool.k)
-    by = ctypes.byref
-    _check(load_library().cospec_kv8_attn(by(dims), int(max_ctx), pool.ref, layer, _ptr(q), by(qs), _ptr(k_blk), by(ks), _ptr(v_blk),
-                                          by(vs), _ptr(page_table), _ptr(ctx_len), _ptr(sel), pages, _ptr(out), _stream(stream)))
+        _dense(sel, "sel", _I32, (shape[0], shape[1], pool.kv_heads, pages))
+    dev = torch._C._cuda_getDevice()
+    _on_device(dev, q, k_blk, v_blk, page_table, ctx_len, sel, out, pool.k)
+    _check((_lib or load_library()).cospec_kv8_attn(
+        dims, int(max_ctx), pool.ref, layer, q.data_ptr(), qs, k_blk.data_ptr(), ks, v_blk.data_ptr(), vs, page_table.data_ptr(),
+        ctx_len.data_ptr(), _at(sel), pages, out.data_ptr(), _stream_ptr(stream, dev)))
     return out
 
 

@@ -108,6 +108,14 @@ def test_the_binding_refuses_host_tensors_and_types():
         C.Rope(torch.zeros((4, 32)), torch.zeros((4, 32)))
     x = torch.zeros((2, 3, 4, 64))
     with pytest.raises(TypeError):
-        C._rows5(x, "q", x.shape)
+        C._rows_ref(x, "q", x.shape)
+    with pytest.raises(ValueError, match="dense"):
+        C._rows_ref(x.to(torch.bfloat16).transpose(1, 2), "q", (2, 4, 3, 64))
     with pytest.raises(ValueError, match="CUDA"):
-        C._rows5(x.to(torch.bfloat16), "q", x.shape)
+        C._on_device(0, None, x)
+    # the layers', batch's and rows' strides, of fused projections too; one element has none
+    y = torch.zeros((2, 3, 10, 64), dtype=torch.bfloat16)
+    st = C._rows_ref(y[:, :, 2:6], "k", (2, 3, 4, 64))._obj
+    assert (st.layer, st.batch, st.row) == (0, 1920, 640)
+    st = C._rows_ref(y[None, :1, :, :1], "k", (1, 1, 3, 1, 64))._obj
+    assert (st.layer, st.batch, st.row) == (0, 0, 640)
