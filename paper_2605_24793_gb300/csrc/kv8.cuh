@@ -64,6 +64,25 @@ CS_DEV void kv8_floats4(uint32_t w, float (&f)[4]) {
   f[3] = b.y;
 }
 
+// 16 bytes to shared memory, asynchronously, past L1; a warp's copies are counted in groups.  (Against bulk copies of
+// whole page-heads with a barrier each: the same times, and nothing that could be waited for in vain.)
+CS_DEV void kv8_copy16(uint32_t dst, const void* src, uint64_t policy) {
+  asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
+}
+CS_DEV uint4 kv8_load16(const void* src, uint64_t policy) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(src), "l"(policy)
+               : "memory");
+  return v;
+}
+CS_DEV void kv8_copy_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+CS_DEV void kv8_copy_wait() {               // all but the newest N groups have landed
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
 // Four bf16 of a 16-bit row.
 CS_DEV void kv8_floats_of(uint2 u, float (&x)[4]) {
   x[0] = __uint_as_float(u.x << 16);

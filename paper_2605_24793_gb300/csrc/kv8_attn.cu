@@ -4,7 +4,7 @@
 // block row, KV head, up to 32 of its query heads).  Its pages go in pairs (32 keys: a tile) to the warps
 // of a thread-block cluster, tile t to warp t mod (4 S) of S CTAs of four warps: no warp waits for
 // another until the end.  Each warp keeps a ring of its own, three tiles deep (four for 64 dimensions),
-// filled by bulk copies of whole page-heads (2 KB, contiguous) that one lane per copy issues.
+// filled by its own asynchronous copies.
 //
 // q . k^T and p . v run on mma.m16n8k16 with f16 operands.  An e4m3 code is exact in f16; q is brought
 // to f16 by a power of two per row (bf16's 8 bits fit f16's 11, values 2^-14 below the row's largest
@@ -26,6 +26,7 @@
 
 #include "cospec_internal.h"
 #include "kv8.cuh"
+#include "kv8_attn.h"
 
 namespace cospec {
 
@@ -54,32 +55,12 @@ struct Lay {
   // With 32 rows the query fragments, the same for all warps, live in shared memory: [MT][D / 16][32 lanes][16 B]
   static constexpr bool QS = MT > 1;
   static constexpr int TOTAL = BODY + (QS ? MT * (D / 16) * 512 : 0);
-  static_assert(STAGE % 16 == 0 && RING % 16 == 0, "bulk copies land on 16 bytes");
+  static_assert(STAGE % 16 == 0 && RING % 16 == 0 && ROWB % 16 == 0, "copies land on 16 bytes");
   static_assert(STAGE >= KV8_PAGE * D * 2, "16 bf16 value rows of the block fit a stage");
 };
 
-struct Params {
-  Kv8Pool pool;
-  Kv8Src q, k_blk, v_blk;
-  const int32_t* page_table;
-  const int32_t* ctx_len;
-  const int32_t* sel;
-  int pages;
-  __nv_bfloat16* out;
-  int B, R, Hq, Hkv, G, num_pages, max_pages;
-  int rows;          // query rows of a unit before it is cut into groups: G * R, or G with selected pages
-  int groups;        // groups of NR rows
-  float scale_log2;
-  int kv_stable, block_full;
-  int* err;
-};
+using Params = Kv8Params;
 
-CS_DEV void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar, uint64_t policy) {
-  asm volatile(
-      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(dst),
-      "l"(src), "r"(bytes), "r"(smem_u32(bar)), "l"(policy)
-      : "memory");
-}
 CS_DEV void mma_f16(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
@@ -275,15 +256,12 @@ __global__ void __launch_bounds__(NW * 32, 2) kv8_attn_kernel(const Params p) {
   using L = Lay<D, MT>;
   constexpr int NST = L::NST;
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ uint64_t full[NW][NST];
   __shared__ uint64_t recv_bar;
   __shared__ int seq_slot;
   __shared__ float weight[L::NR + MAX_SPLIT];              // [S][rows per owner]
   const int S = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
   if (tid == 0) {
-    for (int w = 0; w < NW; ++w)
-      for (int s = 0; s < NST; ++s) mbar_init(&full[w][s], 1);
     mbar_init(&recv_bar, 1);
     fence_barrier_init();
   }
@@ -341,20 +319,24 @@ __global__ void __launch_bounds__(NW * 32, 2) kv8_attn_kernel(const Params p) {
   };
   auto issue = [&](int t) {                                // copy the warp's tile t
     if ((t & 15) == 0) look_up(t);
-    const int st = t % NST, at = 2 * (t & 15);
-    const int e = lane & 1, tensor = (lane >> 1) & 1;      // lanes 0..3: one copy each
-    const int ph = __shfl_sync(0xffffffffu, phys, at + e);
-    const unsigned have = __ballot_sync(0xffffffffu, count > 0) >> at & 3u;
-    if (lane == 0) mbar_arrive_expect_tx(&full[warp][st], (uint32_t)__popc(have) * 2u * L::PB);
-    __syncwarp();
-    if (lane < 4 && (have >> e & 1u)) {
-      const size_t off = ((size_t)ph * p.Hkv + h) * L::PB;
-      const uint32_t dst = smem_u32(ring + st * L::STAGE) + (tensor ? L::KREG + e * L::PB : e * (L::PB + L::PADK));
-      bulk_load(dst, (tensor ? p.pool.v : p.pool.k) + off, L::PB, &full[warp][st], pol);
+    const int at = 2 * (t & 15);
+    const unsigned have = __ballot_sync(0xffffffffu, count > 0) >> at;
+    const uint32_t dst = smem_u32(ring + (t % NST) * L::STAGE) + lane * 16;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int ph = __shfl_sync(0xffffffffu, phys, at + e);
+      if (have >> e & 1u) {
+        const size_t off = ((size_t)ph * p.Hkv + h) * L::PB + lane * 16;
+#pragma unroll
+        for (int i = 0; i < L::PB; i += 512) kv8_copy16(dst + e * (L::PB + L::PADK) + i, p.pool.k + off + i, pol);
+#pragma unroll
+        for (int i = 0; i < L::PB; i += 512) kv8_copy16(dst + L::KREG + e * L::PB + i, p.pool.v + off + i, pol);
+      }
     }
+    kv8_copy_group();
   };
   const int ahead = has_block ? NST - 1 : NST;             // the block's values take the last stage first
-  for (int t = 0; t < min(n, ahead); ++t) issue(t);
+  for (int t = 0; t < ahead; ++t) issue(t);
   if (!SEL && p.kv_stable) griddep_wait();
 
   // ---------------------------------------------------------------- queries
@@ -498,9 +480,8 @@ __global__ void __launch_bounds__(NW * 32, 2) kv8_attn_kernel(const Params p) {
         }
       }
     }
-    fence_proxy_async_smem();              // the stage is a bulk copy's next
     __syncwarp();
-    if (ahead < n) issue(ahead);
+    issue(ahead);
   }
 
   // ---------------------------------------------------------------- the cache
@@ -513,7 +494,7 @@ __global__ void __launch_bounds__(NW * 32, 2) kv8_attn_kernel(const Params p) {
     const int sg = t % NST, at = 2 * (t & 15);
     const float ks[2] = {__shfl_sync(0xffffffffu, scale_c.x, at), __shfl_sync(0xffffffffu, scale_c.x, at + 1)};
     const float vs[2] = {__shfl_sync(0xffffffffu, scale_c.y, at), __shfl_sync(0xffffffffu, scale_c.y, at + 1)};
-    if (!mbar_wait(&full[warp][sg], (uint32_t)(t / NST) & 1u)) set_err(p.err, ERR_TIMEOUT);
+    kv8_copy_wait<NST - 1>();
     __syncwarp();
     const uint32_t sk = smem_u32(ring + sg * L::STAGE);
     if ((whole >> at & 3u) == 3u) {
@@ -523,10 +504,9 @@ __global__ void __launch_bounds__(NW * 32, 2) kv8_attn_kernel(const Params p) {
       if (n0 + n1 > 0) tile<D, MT, true>(st, sk, sk + L::KREG, ks, vs, n0, n1, lane);
     }
     __syncwarp();
-    if (t + NST < n) issue(t + NST);
+    issue(t + NST);                        // (past the last tile an empty group)
   }
-  // After a wait that ran out a copy may still be in flight: wait again (bounded) before the ring is reused.
-  for (int s = 0; s < NST && s < n; ++s) mbar_wait(&full[warp][s], (uint32_t)((n - 1 - s) / NST) & 1u);
+  kv8_copy_wait<0>();
 
   // ---------------------------------------------------------------- the warps' parts
   __syncthreads();                         // every ring is idle
@@ -632,6 +612,37 @@ __global__ void __launch_bounds__(NW * 32, 2) kv8_attn_kernel(const Params p) {
   if (S > 1) cluster_wait();               // every copy out of this CTA has landed
 }
 
+// What a CTA takes (us): to start and end, and for a tile of each of its lanes (warps, or itself) when few CTAs
+// share the device and when all that fit do.
+struct Cost {
+  double start, alone, full;
+};
+
+// CTAs of a unit's cluster: the smallest estimate, for equal contexts (whole waves) and for contexts that average
+// 0.65 of the longest, weighted 0.35 to 0.65 since only the longest is known.
+template <typename Resident>
+int splits(long long units, int tiles, int lanes, Cost c, Resident resident) {
+  const double slots = resident(1) > 0 ? resident(1) : device_num_sms();
+  int best = 1;
+  double best_t = -1.0;
+  for (int s = 1; s <= MAX_SPLIT; ++s) {
+    if (s > 1 && (s - 1) * lanes >= tiles) break;          // a CTA without a tile
+    const int fit = resident(s);
+    if (fit < 1) continue;
+    const double filled = (double)units * s / slots < 1.0 ? (double)units * s / slots : 1.0;
+    const double per = c.full * filled > c.alone ? c.full * filled : c.alone;
+    const double longest = c.start + per * ((tiles + s * lanes - 1) / (s * lanes));
+    const double waves = (double)((units + fit - 1) / fit);
+    const double spread = (double)units / fit * (c.start + per * 0.65 * tiles / (s * lanes));
+    const double t = 0.35 * waves * longest + 0.65 * (longest > spread ? longest : spread);
+    if (best_t < 0.0 || t < 0.98 * best_t) {               // (a larger split has to be worth it)
+      best_t = t;
+      best = s;
+    }
+  }
+  return best;
+}
+
 template <int D, int MT, bool SEL>
 struct Variant {
   using L = Lay<D, MT>;
@@ -674,16 +685,12 @@ struct Variant {
     }
     return c - 1;
   }
-  static cudaError_t launch(const Params& p, int max_tiles, cudaStream_t stream) {
+  static cudaError_t launch(const Params& p, int tiles, cudaStream_t stream) {
     const cudaError_t e = ensure_kernel_limits((const void*)kv8_attn_kernel<D, MT, SEL>, limits(), L::TOTAL, true);
     if (e != cudaSuccess) return e;
-    const long long uy = (long long)p.groups * p.Hkv * (SEL ? p.R : 1), units = uy * p.B;
-    // Splits: about one wave of CTAs, a tile for every warp at least; no cluster that cannot be resident.
-    const long long slots = resident(1) > 0 ? resident(1) : 2 * device_num_sms();
-    int S = 1;
-    while (S < MAX_SPLIT && units * S < slots && 2 * S * NW <= max_tiles) S *= 2;
-    while (S > 1 && resident(S) < 1) S >>= 1;
+    const long long uy = (long long)p.groups * p.Hkv * (SEL ? p.R : 1);
     if (uy > 65535) return cudaErrorInvalidValue;
+    const int S = splits(uy * p.B, tiles, NW, MT == 1 ? Cost{7.0, 0.95, 1.45} : Cost{10.0, 1.32, 1.96}, resident);
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
     config(cfg, attr, dim3(S, (unsigned)uy, p.B), S);
@@ -693,9 +700,31 @@ struct Variant {
   }
 };
 
+int resident_tc(int D, int S) {
+  static std::atomic<int> cache[KL_MAX_DEV][2][MAX_SPLIT + 1];
+  int dev = 0;
+  cudaGetDevice(&dev);
+  std::atomic<int>& slot = cache[dev < KL_MAX_DEV ? dev : KL_MAX_DEV - 1][D == 128][S];
+  int c = slot.load(std::memory_order_relaxed);
+  if (c == 0) {
+    c = kv8_attn_tc_resident(D, S) + 1;
+    slot.store(c, std::memory_order_relaxed);
+  }
+  return c - 1;
+}
+
 template <bool SEL>
-cudaError_t pick(Params& p, int D, int tiles, cudaStream_t stream) {
+cudaError_t pick(Params& p, int D, int pages, cudaStream_t stream) {
+  if (!SEL && p.rows > 32 && p.G <= 128) {
+    const int jb = 128 / p.G;
+    p.groups = (p.R + jb - 1) / jb;
+    if ((long long)p.groups * p.Hkv > 65535) return cudaErrorInvalidValue;
+    const int S = splits((long long)p.groups * p.Hkv * p.B, (pages + 7) / 8, 1, Cost{8.0, 0.95, 0.95},
+                         [D](int s) { return resident_tc(D, s); });
+    return launch_kv8_attn_tc(p, D, S, stream);
+  }
   const bool two = p.rows > 16;
+  const int tiles = (pages + 1) / 2;
   p.groups = (p.rows + (two ? 31 : 15)) / (two ? 32 : 16);
   if (D == 128) return two ? Variant<128, 2, SEL>::launch(p, tiles, stream) : Variant<128, 1, SEL>::launch(p, tiles, stream);
   return two ? Variant<64, 2, SEL>::launch(p, tiles, stream) : Variant<64, 1, SEL>::launch(p, tiles, stream);
@@ -726,8 +755,8 @@ cudaError_t launch_kv8_attn(const Kv8AttnArgs& a, int* err, cudaStream_t stream)
   p.kv_stable = a.kv_stable;
   p.block_full = a.block_full;
   p.err = err;
-  const int tiles = a.sel ? (a.pages + 1) / 2 : (a.max_ctx + 2 * KV8_PAGE - 1) / (2 * KV8_PAGE);
-  return a.sel ? pick<true>(p, a.D, tiles, stream) : pick<false>(p, a.D, tiles, stream);
+  const int pages = a.sel ? a.pages : (a.max_ctx + KV8_PAGE - 1) / KV8_PAGE;
+  return a.sel ? pick<true>(p, a.D, pages, stream) : pick<false>(p, a.D, pages, stream);
 }
 
 }  // namespace cospec
