@@ -719,7 +719,7 @@ cudaError_t pick(Params& p, int D, int pages, cudaStream_t stream) {
     const int jb = 128 / p.G;
     p.groups = (p.R + jb - 1) / jb;
     if ((long long)p.groups * p.Hkv > 65535) return cudaErrorInvalidValue;
-    const int S = splits((long long)p.groups * p.Hkv * p.B, (pages + 7) / 8, 1, Cost{8.0, 0.95, 0.95},
+    const int S = splits((long long)p.groups * p.Hkv * p.B, (pages + 7) / 8, 1, Cost{13.0, 1.35, 1.65},
                          [D](int s) { return resident_tc(D, s); });
     return launch_kv8_attn_tc(p, D, S, stream);
   }

@@ -4,7 +4,7 @@
 // One CTA owns (sequence, KV head, up to 128 query rows: MMA M, split); the splits of a unit are a
 // thread-block cluster and merge in distributed shared memory.  Tile t of 128 keys (8 pages) belongs to
 // split t mod S.  Roles by warp:
-//   warps 0-6   bring the cache in and convert it, a page's keys or values at a time, through a ring each: e4m3 to
+//   warps 0-6   bring the cache in and convert it, two pages' keys or values at a time, through a ring each: e4m3 to
 //               f16 (exact) into the 128-byte-swizzled K-major operand tiles, the keys of a tile ahead of the
 //               values of the one before; of the block they make a last tile;
 //   warps 8-15  softmax, two groups of four warps (a TMEM lane quarter each): group h has keys 64 h .. 64 h + 63
@@ -35,7 +35,7 @@ constexpr int MMA_WARP = 7;
 constexpr int SOFT0 = 8;                  // first softmax warp
 constexpr int THREADS = 16 * 32;
 constexpr int NS = 2;                     // operand stages
-constexpr int SLOTS = 4;                  // pages' keys or values on their way per converting warp
+constexpr int SLOTS = 2;                  // pieces (two pages' keys or values) on their way per converting warp
 constexpr float P_BITS = 6.f, P_ROOM = 8.f;
 constexpr float TINY = 1.2e-38f;          // a score factor is never 0: -inf stays -inf
 constexpr uint64_t WAIT_NS = 2000000000ull;
@@ -49,12 +49,12 @@ struct TL {
   static constexpr int VH = D * 128;                    // 64 keys of a tile's values
   static constexpr int KB = H * KH, VB = 2 * VH;
   static constexpr int TILES = H * QH;                  // [NS]: K then V
-  static constexpr int STG = TILES + NS * (KB + VB);    // [CONV][SLOTS]: a page's keys, or its values
-  static constexpr int FAC = STG + CONV * SLOTS * PB;   // [TM]: the rows' score factors
+  static constexpr int STG = TILES + NS * (KB + VB);    // [CONV][SLOTS]: two pages' keys, or their values
+  static constexpr int FAC = STG + CONV * SLOTS * 2 * PB;   // [TM]: the rows' score factors
   static constexpr int MISC = FAC + TM * 4;
   // k_full, v_full, k_empty, v_empty [NS], q_full, s_full [2], p_full [2][2], pv_done [2],
-  // mma_done, recv, block's maxima, block's scales
-  static constexpr int NBAR = 4 * NS + 13;
+  // mma_done, recv, the block's maxima, its scales, its operands [2]
+  static constexpr int NBAR = 4 * NS + 15;
   static constexpr int HOLDER = MISC + NBAR * 8;        // TMEM base, abort, sequence, block's maxima [2][CONV]
   static constexpr int NEED = HOLDER + 16 + 2 * CONV * 4 + 16;
   static constexpr int PD = D + 4;                      // fp32 row of a partial: O, max, sum, pad
@@ -135,6 +135,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
   uint64_t* recv_bar = mma_done + 1;
   uint64_t* max_bar = recv_bar + 1;         // the converting warps' maxima over the block are there
   uint64_t* blk_bar = max_bar + 1;          // its scales are
+  uint64_t* blk_done = blk_bar + 1;         // [2]: its keys, its values have been written
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem + L::HOLDER);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
   volatile int* seq_slot = abort_flag + 1;
@@ -150,8 +151,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
 
   if (tid == 0) {
     for (int s = 0; s < NS; ++s) {
-      mbar_init(&k_full[s], TP);            // a page each
-      mbar_init(&v_full[s], TP);
+      mbar_init(&k_full[s], TP / 2);        // two pages each
+      mbar_init(&v_full[s], TP / 2);
       mbar_init(&k_empty[s], 1);
       mbar_init(&v_empty[s], 1);
     }
@@ -166,6 +167,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
     mbar_init(recv_bar, 1);
     mbar_init(max_bar, CONV);
     mbar_init(blk_bar, 1);
+    mbar_init(&blk_done[0], CONV);
+    mbar_init(&blk_done[1], CONV);
     *abort_flag = 0;
     fence_barrier_init();
   }
@@ -197,49 +200,61 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
 
   if (warp < CONV) {
     // ---------------------------------------------------------------- cache in, to f16
-    // The work is pieces of a page's keys or values, eight to a group: the keys of tile 0, then for every tile t the
-    // keys of t + 1 and the values of t, so that scores run ahead.  Piece u is warp u mod CONV's.
-    constexpr int NX = D / 32;                            // 16-byte parts of a lane per piece
-    uint8_t* ring = smem + L::STG + warp * (SLOTS * L::PB);
+    // The work is pieces of two pages' keys or values, four to a group: the keys of tile 0, then for every tile t the
+    // keys of t + 1 and the values of t, so that scores run ahead.  Piece u is warp u mod CONV's.  (Its fixed part,
+    // waits, fences and addresses, is as long as the conversion of a page: pages one by one took 2500 cycles a tile.)
+    constexpr int GP = TP / 2;                            // pieces of a group
+    constexpr int NX = D / 32;                            // 16-byte parts of a lane per page
+    constexpr uint32_t NONE = 0xffffffffu;
+    uint8_t* ring = smem + L::STG + warp * (SLOTS * 2 * L::PB);
     const uint64_t pol = p.groups > 1 ? l2_policy_evict_normal() : l2_policy_evict_first();
-    const int total = n > 0 ? (TP * (2 * n + 1) - warp + CONV - 1) / CONV : 0;     // pieces of this warp
+    const int total = n > 0 ? (GP * (2 * n + 1) - warp + CONV - 1) / CONV : 0;     // pieces of this warp
     auto piece = [&](int k, bool& values, int& t, int& e) {
-      const int u = warp + k * CONV, grp = u / TP;
+      const int u = warp + k * CONV, grp = u / GP;
       values = grp > 0 && !(grp & 1);
       t = values ? grp / 2 - 1 : (grp + 1) / 2;
-      e = u % TP;
+      e = u % GP;
     };
-    int phys = 0, count = 0, count_c = 0;
-    auto look_up = [&](int k0) {                          // lane: piece k0 + lane
+    // Lane 2 i + x: page x of piece k0 + i, as its place among the pool's page-heads, and its tokens.
+    uint32_t cell = NONE;
+    int count = 0, count_c = 0;
+    auto look_up = [&](int k0) {
       bool values;
       int t, e;
-      piece(k0 + lane, values, t, e);
-      const int page = (rank + t * S) * TP + e;
+      piece(k0 + (lane >> 1), values, t, e);
+      const int page = (rank + t * S) * TP + 2 * e + (lane & 1);
       count = 0;
-      if (k0 + lane < total && t < n && page < num) {
-        phys = table[page];
-        if ((unsigned)phys < (unsigned)p.num_pages) count = min(KV8_PAGE, C - page * KV8_PAGE);
-        else set_err(p.err, ERR_PAGE);
+      cell = NONE;
+      if (k0 + (lane >> 1) < total && t < n && page < num) {
+        const int phys = table[page];
+        if ((unsigned)phys < (unsigned)p.num_pages) {
+          count = min(KV8_PAGE, C - page * KV8_PAGE);
+          cell = (uint32_t)phys * (uint32_t)p.Hkv + (uint32_t)h;
+        } else {
+          set_err(p.err, ERR_PAGE);
+        }
       }
     };
-    auto issue = [&](int k) {                             // one group, empty where there is no such page
-      if ((k & 31) == 0) look_up(k);
-      const int ph = __shfl_sync(0xffffffffu, phys, k & 31);
-      if (__shfl_sync(0xffffffffu, count, k & 31) > 0) {
-        bool values;
-        int t, e;
-        piece(k, values, t, e);
-        const uint8_t* src = (values ? p.pool.v : p.pool.k) + ((size_t)ph * p.Hkv + h) * L::PB + lane * 16;
-        const uint32_t dst = smem_u32(ring + (k % SLOTS) * L::PB) + lane * 16;
+    auto issue = [&](int k) {                             // one group, empty where there are no such pages
+      if ((k & 15) == 0) look_up(k);
+      bool values;
+      int t, e;
+      piece(k, values, t, e);
+      const uint8_t* pool = (values ? p.pool.v : p.pool.k) + lane * 16;
+      const uint32_t dst = smem_u32(ring + (k % SLOTS) * 2 * L::PB) + lane * 16;
 #pragma unroll
-        for (int i = 0; i < L::PB; i += 512) kv8_copy16(dst + i, src + i, pol);
+      for (int x = 0; x < 2; ++x) {
+        const uint32_t at = __shfl_sync(0xffffffffu, cell, 2 * (k & 15) + x);
+        if (at != NONE)
+#pragma unroll
+          for (int i = 0; i < L::PB; i += 512) kv8_copy16(dst + x * L::PB + i, pool + (size_t)at * L::PB + i, pol);
       }
       kv8_copy_group();
     };
     bool ok = true;
     auto wait = [&](uint64_t* bar, int phase) { ok = ok && mbar_wait(bar, (uint32_t)phase & 1u, WAIT_NS); };
     auto convert = [&](int k) {
-      if ((k & 31) == 0) count_c = count;                 // (copies run at most SLOTS ahead: still these 32)
+      if ((k & 15) == 0) count_c = count;                 // (copies run at most SLOTS ahead: still these 16)
       bool values;
       int t, e;
       piece(k, values, t, e);
@@ -247,54 +262,63 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
       const int st = t % NS;
       uint8_t* kt = smem + L::TILES + st * (L::KB + L::VB);
       uint8_t* vt = kt + L::KB;
-      const uint8_t* src = ring + (k % SLOTS) * L::PB;
+      const uint8_t* src = ring + (k % SLOTS) * 2 * L::PB;
       kv8_copy_wait<SLOTS - 1>();
       __syncwarp();
-      uint4 v[NX];                                        // (all loads before the first store)
+      uint4 v[2][NX];                                     // (all loads before the first store)
       if (t >= NS) wait(values ? &v_empty[st] : &k_empty[st], t / NS - 1);
       if (!values) {
         // a lane: 16 dimensions (chunk ch of the key's row) of every (512 / D)-th key; the two 16-byte halves in an order
         // that spreads a quarter-warp over all banks
         constexpr int CH = D / 16, KPI = 32 / CH;
-        static_assert(NX == KV8_PAGE / KPI, "a piece is as many loads either way");
+        static_assert(NX == KV8_PAGE / KPI, "a page is as many loads either way");
         const int ch = lane % CH;
         const bool flip = H == 2 && ch >= 4;
 #pragma unroll
-        for (int x = 0; x < NX; ++x) v[x] = *reinterpret_cast<const uint4*>(src + (x * KPI + lane / CH) * D + ch * 16);
+        for (int x = 0; x < 2 * NX; ++x) v[x / NX][x % NX] = *reinterpret_cast<const uint4*>(src + (x * KPI + lane / CH) * D + ch * 16);
+        uint8_t* dst = kt + (ch >> 2) * L::KH + (e * 2 * KV8_PAGE + lane / CH) * 128;
 #pragma unroll
-        for (int x = 0; x < NX; ++x) {
-          const int row = e * KV8_PAGE + x * KPI + lane / CH;
-          uint8_t* dst = kt + (ch >> 2) * L::KH + row * 128;
-          const int at = ((ch & 3) * 2 + (flip ? 1 : 0)) ^ (row & 7);
-          *reinterpret_cast<uint4*>(dst + at * 16) = codes_f16(flip ? v[x].z : v[x].x, flip ? v[x].w : v[x].y);
-          *reinterpret_cast<uint4*>(dst + (at ^ 1) * 16) = codes_f16(flip ? v[x].x : v[x].z, flip ? v[x].y : v[x].w);
+        for (int x = 0; x < 2 * NX; ++x) {
+          const int at = ((ch & 3) * 2 + (flip ? 1 : 0)) ^ ((x * KPI + lane / CH) & 7);
+          const uint4& w = v[x / NX][x % NX];
+          *reinterpret_cast<uint4*>(dst + x * KPI * 128 + at * 16) = codes_f16(flip ? w.z : w.x, flip ? w.w : w.y);
+          *reinterpret_cast<uint4*>(dst + x * KPI * 128 + (at ^ 1) * 16) = codes_f16(flip ? w.x : w.z, flip ? w.y : w.w);
         }
       } else {
         // a lane: 16 tokens of every 32nd dimension; cells behind a page's last token may hold anything: they enter as 0
 #pragma unroll
-        for (int x = 0; x < NX; ++x) v[x] = *reinterpret_cast<const uint4*>(src + (x * 32 + lane) * KV8_PAGE);
-        const int have = __shfl_sync(0xffffffffu, count_c, k & 31);
-        if (have < KV8_PAGE) {
-          uint32_t keep[4];
+        for (int x = 0; x < 2; ++x) {
 #pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const int m = have - 4 * y;
-            keep[y] = m >= 4 ? 0xffffffffu : m <= 0 ? 0u : (1u << (8 * m)) - 1u;
-          }
-#pragma unroll
-          for (int x = 0; x < NX; ++x) {
-            v[x].x &= keep[0];
-            v[x].y &= keep[1];
-            v[x].z &= keep[2];
-            v[x].w &= keep[3];
-          }
+          for (int y = 0; y < NX; ++y) v[x][y] = *reinterpret_cast<const uint4*>(src + x * L::PB + (y * 32 + lane) * KV8_PAGE);
         }
 #pragma unroll
-        for (int x = 0; x < NX; ++x) {
-          const int d = x * 32 + lane, at = ((e & 3) * 2) ^ (d & 7);
-          uint8_t* dst = vt + (e >> 2) * L::VH + d * 128;
-          *reinterpret_cast<uint4*>(dst + at * 16) = codes_f16(v[x].x, v[x].y);
-          *reinterpret_cast<uint4*>(dst + (at ^ 1) * 16) = codes_f16(v[x].z, v[x].w);
+        for (int x = 0; x < 2; ++x) {
+          const int have = __shfl_sync(0xffffffffu, count_c, 2 * (k & 15) + x);
+          if (have < KV8_PAGE) {
+            uint32_t keep[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              const int m = have - 4 * y;
+              keep[y] = m >= 4 ? 0xffffffffu : m <= 0 ? 0u : (1u << (8 * m)) - 1u;
+            }
+#pragma unroll
+            for (int y = 0; y < NX; ++y) {
+              v[x][y].x &= keep[0];
+              v[x][y].y &= keep[1];
+              v[x][y].z &= keep[2];
+              v[x][y].w &= keep[3];
+            }
+          }
+        }
+        uint8_t* dst = vt + (e >> 1) * L::VH + lane * 128;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int at = ((e & 1) * 4 + 2 * x) ^ (lane & 7);
+#pragma unroll
+          for (int y = 0; y < NX; ++y) {
+            *reinterpret_cast<uint4*>(dst + y * 32 * 128 + at * 16) = codes_f16(v[x][y].x, v[x][y].y);
+            *reinterpret_cast<uint4*>(dst + y * 32 * 128 + (at ^ 1) * 16) = codes_f16(v[x][y].z, v[x][y].w);
+          }
         }
       }
       fence_proxy_async_smem();
@@ -359,8 +383,11 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
         }
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&k_full[st]);
-        if (lane == 0 && warp < TP - CONV) mbar_arrive(&k_full[st]);
+        if (lane == 0) mbar_arrive(&blk_done[0]);
+        if (warp < TP / 2) {                                // (a quarter of a tile each, once all have written)
+          wait_all(&blk_done[0], 0);
+          if (lane == 0 && ok) mbar_arrive(&k_full[st]);
+        }
       }
       if (ok && (n < NS || wait_all(&v_empty[st], n / NS - 1))) {
         // two rows' eight dimensions turned into eight dimensions' two keys; rows from R on are zeros
@@ -378,8 +405,11 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
         }
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&v_full[st]);
-        if (lane == 0 && warp < TP - CONV) mbar_arrive(&v_full[st]);
+        if (lane == 0) mbar_arrive(&blk_done[1]);
+        if (warp < TP / 2) {
+          wait_all(&blk_done[1], 0);
+          if (lane == 0 && ok) mbar_arrive(&v_full[st]);
+        }
       }
     }
     if (!ok && lane == 0) {
