@@ -1,10 +1,18 @@
 // Attention of a block of rows over the 8-bit paged cache and the block's own bf16 rows.
 //
-// A unit is (sequence, KV head, up to 32 query rows that read it), or with selected pages (sequence,
-// block row, KV head, up to 32 of its query heads).  Its pages go in pairs (32 keys: a tile) to the warps
-// of a thread-block cluster, tile t to warp t mod (4 S) of S CTAs of four warps: no warp waits for
-// another until the end.  Each warp keeps a ring of its own, three tiles deep (four for 64 dimensions),
-// filled by its own asynchronous copies.
+// A unit is (sequence, KV head, up to 32 query rows that read it), or with selected pages (sequence, block
+// row, KV head, up to 32 of its query heads).  Its pages go in pairs (32 keys: a tile) to the rings of a
+// thread-block cluster: a CTA of four warps has four, or two for two warps each, and tile t of the unit is ring t
+// mod (rings S)'s.  No ring waits for another until the end.  A ring's warps bring its tiles in together,
+// asynchronously, and each puts its own 16 or 32 rows to them.  Three variants:
+//   up to 16 rows: a warp a ring (two CTAs an SM with rings of three tiles: with three of two tiles batch 64 at 8192 to
+//   32768 tokens took 460 us for 395);
+//   up to 32 rows: a warp of 32 rows a ring (each code converted once), or two of 16 (half the registers, so three CTAs an
+//   SM, and shorter steps).  Measured at 24 to 32 rows and dimension 128: one user at 4096 tokens 13.1 against 12.1 us,
+//   batch 8 28.9 against 27.2, but batch 32 at 2048 to 16384 tokens 140 against 155 and batch 64 at 8192 to 32768 544
+//   against 625: the estimates below choose.
+// More rows go to the tcgen05 kernel (kv8_attn_tc.cu): at 64 rows two groups of 32 here took 95 us where that takes 70
+// (batch 16, 2048 to 8192 tokens), at 40 91 and 70, at 32 66 and 68; batch 64 540 and 756 at 32 rows, 1011 and 759 at 40.
 //
 // q . k^T and p . v run on mma.m16n8k16 with f16 operands.  An e4m3 code is exact in f16; q is brought
 // to f16 by a power of two per row (bf16's 8 bits fit f16's 11, values 2^-14 below the row's largest
@@ -37,24 +45,27 @@ constexpr int MAX_SPLIT = 16;
 constexpr float P_BITS = 6.f;             // weights are held times 2^6,
 constexpr float P_ROOM = 8.f;             // and may grow by 2^8 before the output is rescaled: below f16's 2^16
 
-template <int D, int MT>
+template <int D, int MT, int RW>
 struct Lay {
+  static constexpr int KW = NW / RW;                      // rings of a CTA, RW warps of 16 MT rows each
   static constexpr int PB = KV8_PAGE * D;                 // bytes of a page-head
   static constexpr int PADK = D == 128 ? 16 : 64;
   static constexpr int KREG = 2 * PB + PADK;
   static constexpr int STAGE = KREG + 2 * PB;
-  static constexpr int NST = D == 128 ? 3 : 4;
-  static constexpr int RING = NST * STAGE;                // of a warp
-  static constexpr int NR = 16 * MT;
+  static constexpr int CTAS = RW == 2 ? 3 : 2;            // of an SM
+  static constexpr int NST = D == 64 || RW == 2 ? 4 : 3;  // tiles of a ring
+  static constexpr int RING = NST * STAGE;
+  static constexpr int NR = 16 * MT * RW;
   static constexpr int PD = D + 8;                        // fp32 row of a partial: O, max, sum, pad
   static constexpr int ROWB = PD * 4;
-  static constexpr int PART = 0;                          // [NW][NR] rows; the CTA's own result in the first NR
-  static constexpr int RECV = NW * NR * ROWB;             // [S][rows per owner], at most NR + 15 rows
+  static constexpr int PART = 0;                          // [KW][NR] rows; the CTA's own result in the first NR
+  static constexpr int RECV = KW * NR * ROWB;             // [S][rows per owner], at most NR + 15 rows
   static constexpr int MERGE = RECV + (NR + MAX_SPLIT - 1) * ROWB;
-  static constexpr int BODY = NW * RING > MERGE ? NW * RING : MERGE;
-  // With 32 rows the query fragments, the same for all warps, live in shared memory: [MT][D / 16][32 lanes][16 B]
+  static constexpr int BODY = KW * RING > MERGE ? KW * RING : MERGE;
+  // With 32 rows a warp the query fragments, the same for all warps, live in shared memory: [MT][D / 16][32 lanes][16 B]
   static constexpr bool QS = MT > 1;
   static constexpr int TOTAL = BODY + (QS ? MT * (D / 16) * 512 : 0);
+  static_assert(MT == 1 || RW == 1, "the warps share their query rows, or a ring");
   static_assert(STAGE % 16 == 0 && RING % 16 == 0 && ROWB % 16 == 0, "copies land on 16 bytes");
   static_assert(STAGE >= KV8_PAGE * D * 2, "16 bf16 value rows of the block fit a stage");
 };
@@ -141,7 +152,7 @@ CS_DEV void raise_unit(State<D, MT>& st, float top) {
 // unless MASK).
 template <int D, int MT, bool MASK>
 CS_DEV void tile(State<D, MT>& st, uint32_t sk, uint32_t sv, const float (&ks)[2], const float (&vs)[2], int n0, int n1, int lane) {
-  using L = Lay<D, MT>;
+  using L = Lay<D, MT, 1>;
   const int g = lane >> 2, c = lane & 3;
   float s[MT][4][4];
 #pragma unroll
@@ -251,16 +262,17 @@ CS_DEV void tile(State<D, MT>& st, uint32_t sk, uint32_t sv, const float (&ks)[2
   }
 }
 
-template <int D, int MT, bool SEL>
-__global__ void __launch_bounds__(NW * 32, 2) kv8_attn_kernel(const Params p) {
-  using L = Lay<D, MT>;
-  constexpr int NST = L::NST;
+template <int D, int MT, int RW, bool SEL>
+__global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW>::CTAS) kv8_attn_kernel(const Params p) {
+  using L = Lay<D, MT, RW>;
+  constexpr int NST = L::NST, KW = L::KW;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint64_t recv_bar;
   __shared__ int seq_slot;
   __shared__ float weight[L::NR + MAX_SPLIT];              // [S][rows per owner]
   const int S = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
+  const int kw = warp / RW, rw = warp % RW;                // ring and group of rows of this warp
   if (tid == 0) {
     mbar_init(&recv_bar, 1);
     fence_barrier_init();
@@ -286,22 +298,21 @@ __global__ void __launch_bounds__(NW * 32, 2) kv8_attn_kernel(const Params p) {
   const int num = bad ? 0 : (C + KV8_PAGE - 1) / KV8_PAGE;           // pages of the context
   if (SEL && p.kv_stable) griddep_wait();                            // the list comes from the kernel before
   const int entries = SEL ? (bad ? 0 : p.pages) : num;
-  const int tiles = (entries + 1) >> 1, stride = S * NW, mine = rank * NW + warp;
-  const int n = mine < tiles ? (tiles - mine + stride - 1) / stride : 0;      // tiles of this warp
+  const int tiles = (entries + 1) >> 1, stride = S * KW, mine = rank * KW + kw;
+  const int n = mine < tiles ? (tiles - mine + stride - 1) / stride : 0;      // tiles of this ring
   const int32_t* table = p.page_table + (size_t)b * p.max_pages;
   const int32_t* list = SEL ? p.sel + (((size_t)b * p.R + jj) * p.Hkv + h) * p.pages : nullptr;
   const int block_groups = bad || rank != S - 1 ? 0 : ((SEL && !p.block_full ? jj + 1 : p.R) + 15) / 16;
-  const bool has_block = NW - 1 - warp < block_groups;     // 16 block rows at a time, from the last warp back
 
   // ---------------------------------------------------------------- the stream of tiles
-  // Lane 2 i + e holds page e of the warp's i-th next tile: where it is, its tokens, its scales.
+  // Lane 2 i + e holds page e of the ring's i-th next tile: where it is, its tokens, its scales.
   const uint64_t pol = p.groups > 1 || (SEL && p.R > 1) ? l2_policy_evict_normal() : l2_policy_evict_first();
-  uint8_t* ring = smem + warp * L::RING;
+  uint8_t* ring = smem + kw * L::RING;
   int phys = 0, count = 0;                                 // of the 16 tiles being issued
   float2 scale_i = make_float2(0.f, 0.f), scale_c = scale_i;
   int count_c = 0;
   unsigned whole = 0u;                                     // of the 16 being consumed: pages of 16 tokens
-  auto look_up = [&](int t0) {                             // tiles t0 .. t0 + 15 of the warp
+  auto look_up = [&](int t0) {                             // tiles t0 .. t0 + 15 of the ring
     const int e = 2 * (mine + (t0 + (lane >> 1)) * stride) + (lane & 1);
     int page = -1;
     if (t0 + (lane >> 1) < n && e < entries) page = SEL ? list[e] : e;
@@ -317,13 +328,18 @@ __global__ void __launch_bounds__(NW * 32, 2) kv8_attn_kernel(const Params p) {
       }
     }
   };
-  auto issue = [&](int t) {                                // copy the warp's tile t
+  auto together = [&]() {                                  // the ring's warps
+    if (RW == 1) __syncwarp();
+    else named_bar_sync(1 + kw, RW * 32);
+  };
+  auto issue = [&](int t) {                                // this warp's part of the ring's tile t: all of it, or a page
     if ((t & 15) == 0) look_up(t);
     const int at = 2 * (t & 15);
     const unsigned have = __ballot_sync(0xffffffffu, count > 0) >> at;
     const uint32_t dst = smem_u32(ring + (t % NST) * L::STAGE) + lane * 16;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
+      if (RW > 1 && e != rw) continue;
       const int ph = __shfl_sync(0xffffffffu, phys, at + e);
       if (have >> e & 1u) {
         const size_t off = ((size_t)ph * p.Hkv + h) * L::PB + lane * 16;
@@ -335,8 +351,7 @@ __global__ void __launch_bounds__(NW * 32, 2) kv8_attn_kernel(const Params p) {
     }
     kv8_copy_group();
   };
-  const int ahead = has_block ? NST - 1 : NST;             // the block's values take the last stage first
-  for (int t = 0; t < ahead; ++t) issue(t);
+  for (int t = 0; t < NST - 1; ++t) issue(t);
   if (!SEL && p.kv_stable) griddep_wait();
 
   // ---------------------------------------------------------------- queries
@@ -348,7 +363,7 @@ __global__ void __launch_bounds__(NW * 32, 2) kv8_attn_kernel(const Params p) {
   for (int t = 0; t < MT; ++t)
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      const int x = t * 16 + g + 8 * r;
+      const int x = (rw * MT + t) * 16 + g + 8 * r;
       const int row = row0 + min(x, nr - 1);
       const int j = SEL ? jj : row / p.G, head = h * p.G + (SEL ? row : row % p.G);
       qrow[t][r] = x < nr ? p.q.p + b * p.q.batch + j * p.q.row + (size_t)head * D + c * (D / 4) : nullptr;
@@ -394,108 +409,106 @@ __global__ void __launch_bounds__(NW * 32, 2) kv8_attn_kernel(const Params p) {
   if (L::QS) __syncthreads();
 
   // ---------------------------------------------------------------- the block's own rows
-  if (has_block) {
+  // 16 at a time to the rings, from the last one back; the ring's last stage, which its tiles reach later, holds
+  // their values: 2 D bytes a row, the 16-byte chunks turned by the row against bank conflicts.  They count in units
+  // of vref as a page's values do (the weights' bf16 holds its inverse).
+  for (int kg = KW - 1 - kw; kg < block_groups; kg += KW) {
+    const int k0 = kg * 16;
     uint8_t* vbuf = ring + (NST - 1) * L::STAGE;
-    for (int kg = NW - 1 - warp; kg < block_groups; kg += NW) {
-      const int k0 = kg * 16;
-      __syncwarp();
-      // 16 value rows of 2 D bytes, their 16-byte chunks turned by the row against bank conflicts; they
-      // count in units of vref as a page's values do (the weights' bf16 holds its inverse)
-      float vmax = 0.f;
-      for (int e = lane; e < 16 * (D / 8); e += 32) {
-        const int r = e / (D / 8), ch = e % (D / 8);
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (k0 + r < p.R) v = *reinterpret_cast<const uint4*>(p.v_blk.p + b * p.v_blk.batch + (k0 + r) * p.v_blk.row + (size_t)h * D + ch * 8);
-        *reinterpret_cast<uint4*>(vbuf + r * (2 * D) + ((ch ^ (r & 7)) * 16)) = v;
-        const uint32_t vv[4] = {v.x, v.y, v.z, v.w};
+    together();
+    float vmax = 0.f;
+    for (int e = lane; e < 16 * (D / 8); e += 32) {        // (every warp looks at all of them for the maximum)
+      const int r = e / (D / 8), ch = e % (D / 8);
+      uint4 v = make_uint4(0u, 0u, 0u, 0u);
+      if (k0 + r < p.R) v = *reinterpret_cast<const uint4*>(p.v_blk.p + b * p.v_blk.batch + (k0 + r) * p.v_blk.row + (size_t)h * D + ch * 8);
+      if (RW == 1 || r % RW == rw) *reinterpret_cast<uint4*>(vbuf + r * (2 * D) + ((ch ^ (r & 7)) * 16)) = v;
+      const uint32_t vv[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int y = 0; y < 4; ++y)
-          vmax = fmaxf(vmax, fmaxf(kv8_finite_abs(__uint_as_float(vv[y] << 16)), kv8_finite_abs(__uint_as_float(vv[y] & 0xffff0000u))));
-      }
+      for (int y = 0; y < 4; ++y)
+        vmax = fmaxf(vmax, fmaxf(kv8_finite_abs(__uint_as_float(vv[y] << 16)), kv8_finite_abs(__uint_as_float(vv[y] & 0xffff0000u))));
+    }
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, o));
-      raise_unit(st, kv8_scale_of(vmax));
-      const float iv = kv8_inverse(st.vref);
-      float s[MT][2][4];
+    for (int o = 16; o > 0; o >>= 1) vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, o));
+    raise_unit(st, kv8_scale_of(vmax));
+    const float iv = kv8_inverse(st.vref);
+    float s[MT][2][4];
 #pragma unroll
-      for (int t = 0; t < MT; ++t)
+    for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) s[t][i][0] = s[t][i][1] = s[t][i][2] = s[t][i][3] = 0.f;
+      for (int i = 0; i < 2; ++i) s[t][i][0] = s[t][i][1] = s[t][i][2] = s[t][i][3] = 0.f;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int key = k0 + i * 8 + g;
-        const __nv_bfloat16* kr = p.k_blk.p + b * p.k_blk.batch + key * p.k_blk.row + (size_t)h * D + c * (D / 4);
+    for (int i = 0; i < 2; ++i) {
+      const int key = k0 + i * 8 + g;
+      const __nv_bfloat16* kr = p.k_blk.p + b * p.k_blk.batch + key * p.k_blk.row + (size_t)h * D + c * (D / 4);
 #pragma unroll
-        for (int x = 0; x < D / 32; ++x) {
-          uint4 w = make_uint4(0u, 0u, 0u, 0u);
-          if (key < p.R) w = *reinterpret_cast<const uint4*>(kr + x * 8);
-#pragma unroll
-          for (int t = 0; t < MT; ++t) {
-            uint4 qa = make_uint4(0u, 0u, 0u, 0u), qb = qa;
-            if (qrow[t][0]) qa = *reinterpret_cast<const uint4*>(qrow[t][0] + x * 8);
-            if (qrow[t][1]) qb = *reinterpret_cast<const uint4*>(qrow[t][1] + x * 8);
-            const uint32_t a0[4] = {qa.x, qb.x, qa.y, qb.y}, a1[4] = {qa.z, qb.z, qa.w, qb.w};
-            mma_16816(s[t][i], a0, w.x, w.y);
-            mma_16816(s[t][i], a1, w.z, w.w);
-          }
-        }
-      }
-      __syncwarp();
-      uint32_t pf[MT][4];
-#pragma unroll
-      for (int t = 0; t < MT; ++t) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int key = k0 + i * 8 + 2 * c + e;
-            s[t][i][e] = key <= lim[t][0] ? s[t][i][e] * p.scale_log2 : -INFINITY;
-            s[t][i][2 + e] = key <= lim[t][1] ? s[t][i][2 + e] * p.scale_log2 : -INFINITY;
-          }
-        float base[2];
-        follow_max(st, t, fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][1][0], s[t][1][1])),
-                   fmaxf(fmaxf(s[t][0][2], s[t][0][3]), fmaxf(s[t][1][2], s[t][1][3])), base);
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            s[t][i][e] = exp2_approx(s[t][i][e] - base[e >> 1]);
-            st.l[t][e >> 1] += s[t][i][e];
-          }
-        pf[t][0] = pack_bf16(s[t][0][0] * iv, s[t][0][1] * iv);
-        pf[t][1] = pack_bf16(s[t][0][2] * iv, s[t][0][3] * iv);
-        pf[t][2] = pack_bf16(s[t][1][0] * iv, s[t][1][1] * iv);
-        pf[t][3] = pack_bf16(s[t][1][2] * iv, s[t][1][3] * iv);
-      }
-      const int key = (lane & 7) + ((lane >> 3) & 1) * 8;
-#pragma unroll
-      for (int d = 0; d < D / 8; d += 2) {
-        const int ch = d + (lane >> 4);
-        uint32_t b0, b1, b2, b3;
-        ldsm_x4_t(smem_u32(vbuf) + (uint32_t)(key * (2 * D) + ((ch ^ (key & 7)) * 16)), b0, b1, b2, b3);
+      for (int x = 0; x < D / 32; ++x) {
+        uint4 w = make_uint4(0u, 0u, 0u, 0u);
+        if (key < p.R) w = *reinterpret_cast<const uint4*>(kr + x * 8);
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-          mma_16816(st.o[t][d], pf[t], b0, b1);
-          mma_16816(st.o[t][d + 1], pf[t], b2, b3);
+          uint4 qa = make_uint4(0u, 0u, 0u, 0u), qb = qa;
+          if (qrow[t][0]) qa = *reinterpret_cast<const uint4*>(qrow[t][0] + x * 8);
+          if (qrow[t][1]) qb = *reinterpret_cast<const uint4*>(qrow[t][1] + x * 8);
+          const uint32_t a0[4] = {qa.x, qb.x, qa.y, qb.y}, a1[4] = {qa.z, qb.z, qa.w, qb.w};
+          mma_16816(s[t][i], a0, w.x, w.y);
+          mma_16816(s[t][i], a1, w.z, w.w);
         }
       }
     }
-    __syncwarp();
-    issue(ahead);
+    together();
+    uint32_t pf[MT][4];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int key = k0 + i * 8 + 2 * c + e;
+          s[t][i][e] = key <= lim[t][0] ? s[t][i][e] * p.scale_log2 : -INFINITY;
+          s[t][i][2 + e] = key <= lim[t][1] ? s[t][i][2 + e] * p.scale_log2 : -INFINITY;
+        }
+      float base[2];
+      follow_max(st, t, fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][1][0], s[t][1][1])),
+                 fmaxf(fmaxf(s[t][0][2], s[t][0][3]), fmaxf(s[t][1][2], s[t][1][3])), base);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s[t][i][e] = exp2_approx(s[t][i][e] - base[e >> 1]);
+          st.l[t][e >> 1] += s[t][i][e];
+        }
+      pf[t][0] = pack_bf16(s[t][0][0] * iv, s[t][0][1] * iv);
+      pf[t][1] = pack_bf16(s[t][0][2] * iv, s[t][0][3] * iv);
+      pf[t][2] = pack_bf16(s[t][1][0] * iv, s[t][1][1] * iv);
+      pf[t][3] = pack_bf16(s[t][1][2] * iv, s[t][1][3] * iv);
+    }
+    const int key = (lane & 7) + ((lane >> 3) & 1) * 8;
+#pragma unroll
+    for (int d = 0; d < D / 8; d += 2) {
+      const int ch = d + (lane >> 4);
+      uint32_t b0, b1, b2, b3;
+      ldsm_x4_t(smem_u32(vbuf) + (uint32_t)(key * (2 * D) + ((ch ^ (key & 7)) * 16)), b0, b1, b2, b3);
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+        mma_16816(st.o[t][d], pf[t], b0, b1);
+        mma_16816(st.o[t][d + 1], pf[t], b2, b3);
+      }
+    }
   }
 
   // ---------------------------------------------------------------- the cache
   for (int t = 0; t < n; ++t) {
     if ((t & 15) == 0) {
-      scale_c = scale_i;                   // (copies run at most NST tiles ahead: still these 16)
+      scale_c = scale_i;                   // (copies run less than NST tiles ahead: still these 16)
       count_c = count;
       whole = __ballot_sync(0xffffffffu, count == KV8_PAGE);
     }
     const int sg = t % NST, at = 2 * (t & 15);
+    kv8_copy_wait<NST - 2>();
+    together();                            // tile t is there, and every warp is through with tile t - 1
+    issue(t + NST - 1);                    // (past the last tile an empty group)
     const float ks[2] = {__shfl_sync(0xffffffffu, scale_c.x, at), __shfl_sync(0xffffffffu, scale_c.x, at + 1)};
     const float vs[2] = {__shfl_sync(0xffffffffu, scale_c.y, at), __shfl_sync(0xffffffffu, scale_c.y, at + 1)};
-    kv8_copy_wait<NST - 1>();
-    __syncwarp();
     const uint32_t sk = smem_u32(ring + sg * L::STAGE);
     if ((whole >> at & 3u) == 3u) {
       tile<D, MT, false>(st, sk, sk + L::KREG, ks, vs, KV8_PAGE, KV8_PAGE, lane);
@@ -503,8 +516,6 @@ __global__ void __launch_bounds__(NW * 32, 2) kv8_attn_kernel(const Params p) {
       const int n0 = __shfl_sync(0xffffffffu, count_c, at), n1 = __shfl_sync(0xffffffffu, count_c, at + 1);
       if (n0 + n1 > 0) tile<D, MT, true>(st, sk, sk + L::KREG, ks, vs, n0, n1, lane);
     }
-    __syncwarp();
-    issue(t + NST);                        // (past the last tile an empty group)
   }
   kv8_copy_wait<0>();
 
@@ -518,7 +529,7 @@ __global__ void __launch_bounds__(NW * 32, 2) kv8_attn_kernel(const Params p) {
   float* part = reinterpret_cast<float*>(smem + L::PART);
   {
     const float unit = st.vref * exp2f(-P_BITS), one = exp2f(-P_BITS);
-    float* mypart = part + warp * L::NR * L::PD;
+    float* mypart = part + (kw * L::NR + rw * 16) * L::PD;
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -534,22 +545,22 @@ __global__ void __launch_bounds__(NW * 32, 2) kv8_attn_kernel(const Params p) {
       }
   }
   __syncthreads();
-  // A row's NW parts into the first, by a group of D / 4 lanes.
+  // A row's KW parts into the first, by a group of D / 4 lanes.
   constexpr int LPR = D / 4;
   static_assert(L::NR % (NW * 32 / LPR) == 0, "whole passes over the rows");
   for (int r0 = 0; r0 < nr; r0 += NW * 32 / LPR) {         // (a last pass may touch rows past nr)
     const int r = r0 + tid / LPR, x = tid % LPR * 4;
-    float2 ml[NW];
+    float2 ml[KW];
     float top = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
+    for (int w = 0; w < KW; ++w) {
       ml[w] = *reinterpret_cast<const float2*>(part + (w * L::NR + r) * L::PD + D);
       top = fmaxf(top, ml[w].x);
     }
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float l = 0.f;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
+    for (int w = 0; w < KW; ++w) {
       const float a = ml[w].x == -INFINITY ? 0.f : exp2_approx(ml[w].x - top);
       const float4 v = *reinterpret_cast<const float4*>(part + (w * L::NR + r) * L::PD + x);
       acc.x += v.x * a;
@@ -612,19 +623,22 @@ __global__ void __launch_bounds__(NW * 32, 2) kv8_attn_kernel(const Params p) {
   if (S > 1) cluster_wait();               // every copy out of this CTA has landed
 }
 
-// What a CTA takes (us): to start and end, and for a tile of each of its lanes (warps, or itself) when few CTAs
-// share the device and when all that fit do.
+// What a CTA takes (us): to start and end, and for a tile of each of its lanes (rings, or itself) when few CTAs
+// share the device and when all that fit do.  As measured at head dimension 128; the figures of 64 are within a fifth.
 struct Cost {
   double start, alone, full;
 };
+struct Split {
+  int S;                                  // CTAs of a unit's cluster
+  double us;
+};
 
-// CTAs of a unit's cluster: the smallest estimate, for equal contexts (whole waves) and for contexts that average
-// 0.65 of the longest, weighted 0.35 to 0.65 since only the longest is known.
+// The split of the smallest estimate, put together for equal contexts (whole waves) and for contexts that average
+// 0.65 of the longest, weighted 0.25 to 0.75 since only the longest is known.
 template <typename Resident>
-int splits(long long units, int tiles, int lanes, Cost c, Resident resident) {
+Split split_of(long long units, int tiles, int lanes, Cost c, Resident resident) {
   const double slots = resident(1) > 0 ? resident(1) : device_num_sms();
-  int best = 1;
-  double best_t = -1.0;
+  Split best = {1, -1.0};
   for (int s = 1; s <= MAX_SPLIT; ++s) {
     if (s > 1 && (s - 1) * lanes >= tiles) break;          // a CTA without a tile
     const int fit = resident(s);
@@ -634,18 +648,15 @@ int splits(long long units, int tiles, int lanes, Cost c, Resident resident) {
     const double longest = c.start + per * ((tiles + s * lanes - 1) / (s * lanes));
     const double waves = (double)((units + fit - 1) / fit);
     const double spread = (double)units / fit * (c.start + per * 0.65 * tiles / (s * lanes));
-    const double t = 0.35 * waves * longest + 0.65 * (longest > spread ? longest : spread);
-    if (best_t < 0.0 || t < 0.98 * best_t) {               // (a larger split has to be worth it)
-      best_t = t;
-      best = s;
-    }
+    const double t = 0.25 * waves * longest + 0.75 * (longest > spread ? longest : spread);
+    if (best.us < 0.0 || t < 0.98 * best.us) best = {s, t};           // (a larger split has to be worth it)
   }
   return best;
 }
 
-template <int D, int MT, bool SEL>
+template <int D, int MT, int RW, bool SEL>
 struct Variant {
-  using L = Lay<D, MT>;
+  using L = Lay<D, MT, RW>;
   static KernelLimits& limits() {
     static KernelLimits lim;
     return lim;
@@ -675,8 +686,8 @@ struct Variant {
       config(cfg, attr, dim3(S, 1024, 1), S);
       cfg.numAttrs = 1;
       int n = 0;
-      if (ensure_kernel_limits((const void*)kv8_attn_kernel<D, MT, SEL>, limits(), L::TOTAL, true) != cudaSuccess ||
-          cudaOccupancyMaxActiveClusters(&n, kv8_attn_kernel<D, MT, SEL>, &cfg) != cudaSuccess) {
+      if (ensure_kernel_limits((const void*)kv8_attn_kernel<D, MT, RW, SEL>, limits(), L::TOTAL, true) != cudaSuccess ||
+          cudaOccupancyMaxActiveClusters(&n, kv8_attn_kernel<D, MT, RW, SEL>, &cfg) != cudaSuccess) {
         cudaGetLastError();
         n = 0;
       }
@@ -685,18 +696,23 @@ struct Variant {
     }
     return c - 1;
   }
-  static cudaError_t launch(const Params& p, int tiles, cudaStream_t stream) {
-    const cudaError_t e = ensure_kernel_limits((const void*)kv8_attn_kernel<D, MT, SEL>, limits(), L::TOTAL, true);
+  static long long units(const Params& p) { return (long long)groups(p) * p.Hkv * (SEL ? p.R : 1) * p.B; }
+  static int groups(const Params& p) { return (p.rows + L::NR - 1) / L::NR; }
+  static Split split(const Params& p, int tiles) {
+    return split_of(units(p), tiles, L::KW, MT == 2 ? Cost{10.0, 1.32, 1.96} : RW == 2 ? Cost{7.5, 0.88, 1.5} : Cost{7.0, 0.95, 1.45}, resident);
+  }
+  static cudaError_t launch(Params& p, int S, cudaStream_t stream) {
+    const cudaError_t e = ensure_kernel_limits((const void*)kv8_attn_kernel<D, MT, RW, SEL>, limits(), L::TOTAL, true);
     if (e != cudaSuccess) return e;
-    const long long uy = (long long)p.groups * p.Hkv * (SEL ? p.R : 1);
+    p.groups = groups(p);
+    const long long uy = units(p) / p.B;
     if (uy > 65535) return cudaErrorInvalidValue;
-    const int S = splits(uy * p.B, tiles, NW, MT == 1 ? Cost{7.0, 0.95, 1.45} : Cost{10.0, 1.32, 1.96}, resident);
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
     config(cfg, attr, dim3(S, (unsigned)uy, p.B), S);
     cfg.stream = stream;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kv8_attn_kernel<D, MT, SEL>, p);
+    return cudaLaunchKernelEx(&cfg, kv8_attn_kernel<D, MT, RW, SEL>, p);
   }
 };
 
@@ -713,21 +729,19 @@ int resident_tc(int D, int S) {
   return c - 1;
 }
 
-template <bool SEL>
-cudaError_t pick(Params& p, int D, int pages, cudaStream_t stream) {
+template <int D, bool SEL>
+cudaError_t pick(Params& p, int pages, cudaStream_t stream) {
   if (!SEL && p.rows > 32 && p.G <= 128) {
     const int jb = 128 / p.G;
     p.groups = (p.R + jb - 1) / jb;
     if ((long long)p.groups * p.Hkv > 65535) return cudaErrorInvalidValue;
-    const int S = splits((long long)p.groups * p.Hkv * p.B, (pages + 7) / 8, 1, Cost{13.0, 1.35, 1.65},
-                         [D](int s) { return resident_tc(D, s); });
-    return launch_kv8_attn_tc(p, D, S, stream);
+    const Split s = split_of((long long)p.groups * p.Hkv * p.B, (pages + 7) / 8, 1, Cost{13.0, 1.05, 1.4}, [](int n) { return resident_tc(D, n); });
+    return launch_kv8_attn_tc(p, D, s.S, stream);
   }
-  const bool two = p.rows > 16;
   const int tiles = (pages + 1) / 2;
-  p.groups = (p.rows + (two ? 31 : 15)) / (two ? 32 : 16);
-  if (D == 128) return two ? Variant<128, 2, SEL>::launch(p, tiles, stream) : Variant<128, 1, SEL>::launch(p, tiles, stream);
-  return two ? Variant<64, 2, SEL>::launch(p, tiles, stream) : Variant<64, 1, SEL>::launch(p, tiles, stream);
+  if (p.rows <= 16) return Variant<D, 1, 1, SEL>::launch(p, Variant<D, 1, 1, SEL>::split(p, tiles).S, stream);
+  const Split wide = Variant<D, 2, 1, SEL>::split(p, tiles), pair = Variant<D, 1, 2, SEL>::split(p, tiles);
+  return wide.us < pair.us ? Variant<D, 2, 1, SEL>::launch(p, wide.S, stream) : Variant<D, 1, 2, SEL>::launch(p, pair.S, stream);
 }
 
 }  // namespace
@@ -756,7 +770,8 @@ cudaError_t launch_kv8_attn(const Kv8AttnArgs& a, int* err, cudaStream_t stream)
   p.block_full = a.block_full;
   p.err = err;
   const int pages = a.sel ? a.pages : (a.max_ctx + KV8_PAGE - 1) / KV8_PAGE;
-  return a.sel ? pick<true>(p, a.D, pages, stream) : pick<false>(p, a.D, pages, stream);
+  if (a.D == 128) return a.sel ? pick<128, true>(p, pages, stream) : pick<128, false>(p, pages, stream);
+  return a.sel ? pick<64, true>(p, pages, stream) : pick<64, false>(p, pages, stream);
 }
 
 }  // namespace cospec
