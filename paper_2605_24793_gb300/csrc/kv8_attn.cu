@@ -67,7 +67,7 @@ struct Lay {
   static constexpr int TOTAL = BODY + (QS ? MT * (D / 16) * 512 : 0);
   static_assert(MT == 1 || RW == 1, "the warps share their query rows, or a ring");
   static_assert(STAGE % 16 == 0 && RING % 16 == 0 && ROWB % 16 == 0, "copies land on 16 bytes");
-  static_assert(STAGE >= KV8_PAGE * D * 2, "16 bf16 value rows of the block fit a stage");
+  static_assert(STAGE >= KV8_PAGE * D * 4, "16 bf16 rows of the block fit a stage");
 };
 
 using Params = Kv8Params;
@@ -353,6 +353,24 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW>::CTAS) kv8_attn_kernel
   };
   for (int t = 0; t < NST - 1; ++t) issue(t);
   if (!SEL && p.kv_stable) griddep_wait();
+  // Sixteen of the block's rows, into the ring's last stage, which its tiles reach later: keys and then values, 2 D bytes
+  // a row, the 16-byte chunks turned by the row against bank conflicts.
+  uint8_t* kbuf = ring + (NST - 1) * L::STAGE;
+  uint8_t* vbuf = kbuf + KV8_PAGE * D * 2;
+  const uint64_t blk_pol = l2_policy_evict_normal();
+  auto issue_block = [&](int k0) {
+    for (int e = rw * 32 + lane; e < 16 * (D / 8); e += RW * 32) {
+      const int r = e / (D / 8), ch = e % (D / 8), at = r * (2 * D) + ((ch ^ (r & 7)) * 16);
+      if (k0 + r < p.R) {
+        kv8_copy16(smem_u32(kbuf + at), p.k_blk.p + b * p.k_blk.batch + (k0 + r) * p.k_blk.row + (size_t)h * D + ch * 8, blk_pol);
+        kv8_copy16(smem_u32(vbuf + at), p.v_blk.p + b * p.v_blk.batch + (k0 + r) * p.v_blk.row + (size_t)h * D + ch * 8, blk_pol);
+      } else {
+        *reinterpret_cast<uint4*>(kbuf + at) = *reinterpret_cast<uint4*>(vbuf + at) = make_uint4(0u, 0u, 0u, 0u);
+      }
+    }
+    kv8_copy_group();
+  };
+  if (KW - 1 - kw < block_groups) issue_block((KW - 1 - kw) * 16);
 
   // ---------------------------------------------------------------- queries
   State<D, MT> st;
@@ -409,19 +427,19 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW>::CTAS) kv8_attn_kernel
   if (L::QS) __syncthreads();
 
   // ---------------------------------------------------------------- the block's own rows
-  // 16 at a time to the rings, from the last one back; the ring's last stage, which its tiles reach later, holds
-  // their values: 2 D bytes a row, the 16-byte chunks turned by the row against bank conflicts.  They count in units
-  // of vref as a page's values do (the weights' bf16 holds its inverse).
+  // 16 at a time to the rings, from the last one back.  They count in units of vref as a page's values do (the weights'
+  // bf16 holds its inverse).
   for (int kg = KW - 1 - kw; kg < block_groups; kg += KW) {
     const int k0 = kg * 16;
-    uint8_t* vbuf = ring + (NST - 1) * L::STAGE;
+    if (kg >= KW) {
+      together();
+      issue_block(k0);
+    }
+    kv8_copy_wait<0>();
     together();
     float vmax = 0.f;
-    for (int e = lane; e < 16 * (D / 8); e += 32) {        // (every warp looks at all of them for the maximum)
-      const int r = e / (D / 8), ch = e % (D / 8);
-      uint4 v = make_uint4(0u, 0u, 0u, 0u);
-      if (k0 + r < p.R) v = *reinterpret_cast<const uint4*>(p.v_blk.p + b * p.v_blk.batch + (k0 + r) * p.v_blk.row + (size_t)h * D + ch * 8);
-      if (RW == 1 || r % RW == rw) *reinterpret_cast<uint4*>(vbuf + r * (2 * D) + ((ch ^ (r & 7)) * 16)) = v;
+    for (int e = lane; e < 16 * (D / 8); e += 32) {        // (every warp looks at all of them)
+      const uint4 v = *reinterpret_cast<const uint4*>(vbuf + e * 16);
       const uint32_t vv[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
       for (int y = 0; y < 4; ++y)
@@ -438,12 +456,10 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW>::CTAS) kv8_attn_kernel
       for (int i = 0; i < 2; ++i) s[t][i][0] = s[t][i][1] = s[t][i][2] = s[t][i][3] = 0.f;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int key = k0 + i * 8 + g;
-      const __nv_bfloat16* kr = p.k_blk.p + b * p.k_blk.batch + key * p.k_blk.row + (size_t)h * D + c * (D / 4);
+      const uint8_t* kr = kbuf + (i * 8 + g) * (2 * D);
 #pragma unroll
       for (int x = 0; x < D / 32; ++x) {
-        uint4 w = make_uint4(0u, 0u, 0u, 0u);
-        if (key < p.R) w = *reinterpret_cast<const uint4*>(kr + x * 8);
+        const uint4 w = *reinterpret_cast<const uint4*>(kr + ((c * (D / 32) + x) ^ g) * 16);
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
           uint4 qa = make_uint4(0u, 0u, 0u, 0u), qb = qa;
@@ -455,7 +471,6 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW>::CTAS) kv8_attn_kernel
         }
       }
     }
-    together();
     uint32_t pf[MT][4];
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
