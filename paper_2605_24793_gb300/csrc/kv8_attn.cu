@@ -2,15 +2,16 @@
 //
 // A unit is (sequence, KV head, up to 32 query rows that read it), or with selected pages (sequence, block
 // row, KV head, up to 32 of its query heads).  Its pages go in pairs (32 keys: a tile) to the rings of a
-// thread-block cluster: a CTA of four warps has four, or two for two warps each, and tile t of the unit is ring t
-// mod (rings S)'s.  No ring waits for another until the end.  A ring's warps bring its tiles in together,
-// asynchronously, and each puts its own 16 or 32 rows to them.  Three variants:
-//   up to 16 rows: a warp a ring (two CTAs an SM with rings of three tiles: with three of two tiles batch 64 at 8192 to
-//   32768 tokens took 460 us for 395);
-//   up to 32 rows: a warp of 32 rows a ring (each code converted once), or two of 16 (half the registers, so three CTAs an
-//   SM, and shorter steps).  Measured at 24 to 32 rows and dimension 128: one user at 4096 tokens 13.1 against 12.1 us,
-//   batch 8 28.9 against 27.2, but batch 32 at 2048 to 16384 tokens 140 against 155 and batch 64 at 8192 to 32768 544
-//   against 625: the estimates below choose.
+// thread-block cluster, tile t of the unit to ring t mod (rings S).  A ring belongs to one warp or to two,
+// and no ring waits for another until the end.  A ring's warps bring its tiles in together, asynchronously, and each puts
+// its own 16 or 32 rows to them.  Variants, chosen by the estimates below:
+//   up to 16 rows: a warp a ring, four to a CTA and two CTAs an SM (rings of three tiles: with three CTAs and rings of two
+//   batch 64 at 8192 to 32768 tokens took 460 us for 395), or eight to a CTA, which fills the SMs that a few clusters
+//   get: one user at 4096 tokens 8.3 us with four warps and 9.0 with eight, at 32768 tokens 26.5 and 22.3;
+//   up to 32 rows: a warp of 32 rows a ring (each code converted once), or two of 16 (half the registers, shorter steps),
+//   these with four warps and three CTAs an SM or with eight.  At 24 to 32 rows, with 32 rows a warp, two warps of four,
+//   two warps of eight: one user at 4096 tokens 13.1, 11.7, 10.4 us; batch 8 28.9, 27.1, 28.2; batch 32 at 2048 to 16384
+//   140, 157, 164; batch 64 at 8192 to 32768 544, 627, 706.
 // More rows go to the tcgen05 kernel (kv8_attn_tc.cu): at 64 rows two groups of 32 here took 95 us where that takes 70
 // (batch 16, 2048 to 8192 tokens), at 40 91 and 70, at 32 66 and 68; batch 64 540 and 756 at 32 rows, 1011 and 759 at 40.
 //
@@ -40,19 +41,20 @@ namespace cospec {
 
 namespace {
 
-constexpr int NW = 4;                     // warps of a CTA
-constexpr int MAX_SPLIT = 16;
+// Larger clusters do not all find an SM for each CTA and start later: one user at 4096 tokens took 8.3 us with clusters of
+// 12, 9.6 with 14 and 9.2 with 16; with 6 rows of 24 queries 11.7, 13.2 and 12.5.
+constexpr int MAX_SPLIT = 12;
 constexpr float P_BITS = 6.f;             // weights are held times 2^6,
 constexpr float P_ROOM = 8.f;             // and may grow by 2^8 before the output is rescaled: below f16's 2^16
 
-template <int D, int MT, int RW>
+template <int D, int MT, int RW, int NW>
 struct Lay {
   static constexpr int KW = NW / RW;                      // rings of a CTA, RW warps of 16 MT rows each
   static constexpr int PB = KV8_PAGE * D;                 // bytes of a page-head
   static constexpr int PADK = D == 128 ? 16 : 64;
   static constexpr int KREG = 2 * PB + PADK;
   static constexpr int STAGE = KREG + 2 * PB;
-  static constexpr int CTAS = RW == 2 ? 3 : 2;            // of an SM
+  static constexpr int CTAS = NW == 8 ? 1 : RW == 2 ? 3 : 2;            // of an SM
   static constexpr int NST = D == 64 || RW == 2 ? 4 : 3;  // tiles of a ring
   static constexpr int RING = NST * STAGE;
   static constexpr int NR = 16 * MT * RW;
@@ -152,7 +154,7 @@ CS_DEV void raise_unit(State<D, MT>& st, float top) {
 // unless MASK).
 template <int D, int MT, bool MASK>
 CS_DEV void tile(State<D, MT>& st, uint32_t sk, uint32_t sv, const float (&ks)[2], const float (&vs)[2], int n0, int n1, int lane) {
-  using L = Lay<D, MT, 1>;
+  using L = Lay<D, MT, 1, 4>;
   const int g = lane >> 2, c = lane & 3;
   float s[MT][4][4];
 #pragma unroll
@@ -262,9 +264,9 @@ CS_DEV void tile(State<D, MT>& st, uint32_t sk, uint32_t sv, const float (&ks)[2
   }
 }
 
-template <int D, int MT, int RW, bool SEL>
-__global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW>::CTAS) kv8_attn_kernel(const Params p) {
-  using L = Lay<D, MT, RW>;
+template <int D, int MT, int RW, int NW, bool SEL>
+__global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_kernel(const Params p) {
+  using L = Lay<D, MT, RW, NW>;
   constexpr int NST = L::NST, KW = L::KW;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint64_t recv_bar;
@@ -669,9 +671,9 @@ Split split_of(long long units, int tiles, int lanes, Cost c, Resident resident)
   return best;
 }
 
-template <int D, int MT, int RW, bool SEL>
+template <int D, int MT, int RW, int NW, bool SEL>
 struct Variant {
-  using L = Lay<D, MT, RW>;
+  using L = Lay<D, MT, RW, NW>;
   static KernelLimits& limits() {
     static KernelLimits lim;
     return lim;
@@ -701,8 +703,8 @@ struct Variant {
       config(cfg, attr, dim3(S, 1024, 1), S);
       cfg.numAttrs = 1;
       int n = 0;
-      if (ensure_kernel_limits((const void*)kv8_attn_kernel<D, MT, RW, SEL>, limits(), L::TOTAL, true) != cudaSuccess ||
-          cudaOccupancyMaxActiveClusters(&n, kv8_attn_kernel<D, MT, RW, SEL>, &cfg) != cudaSuccess) {
+      if (ensure_kernel_limits((const void*)kv8_attn_kernel<D, MT, RW, NW, SEL>, limits(), L::TOTAL, true) != cudaSuccess ||
+          cudaOccupancyMaxActiveClusters(&n, kv8_attn_kernel<D, MT, RW, NW, SEL>, &cfg) != cudaSuccess) {
         cudaGetLastError();
         n = 0;
       }
@@ -714,10 +716,14 @@ struct Variant {
   static long long units(const Params& p) { return (long long)groups(p) * p.Hkv * (SEL ? p.R : 1) * p.B; }
   static int groups(const Params& p) { return (p.rows + L::NR - 1) / L::NR; }
   static Split split(const Params& p, int tiles) {
-    return split_of(units(p), tiles, L::KW, MT == 2 ? Cost{10.0, 1.32, 1.96} : RW == 2 ? Cost{7.5, 0.88, 1.5} : Cost{7.0, 0.95, 1.45}, resident);
+    return split_of(units(p), tiles, L::KW,
+                    MT == 2   ? Cost{10.0, 1.32, 1.96}
+                    : RW == 2 ? (NW == 8 ? Cost{7.3, 1.15, 1.15} : Cost{6.8, 0.88, 1.5})
+                              : (NW == 8 ? Cost{7.3, 1.27, 1.27} : Cost{6.0, 0.95, 1.45}),
+                    resident);
   }
   static cudaError_t launch(Params& p, int S, cudaStream_t stream) {
-    const cudaError_t e = ensure_kernel_limits((const void*)kv8_attn_kernel<D, MT, RW, SEL>, limits(), L::TOTAL, true);
+    const cudaError_t e = ensure_kernel_limits((const void*)kv8_attn_kernel<D, MT, RW, NW, SEL>, limits(), L::TOTAL, true);
     if (e != cudaSuccess) return e;
     p.groups = groups(p);
     const long long uy = units(p) / p.B;
@@ -727,7 +733,7 @@ struct Variant {
     config(cfg, attr, dim3(S, (unsigned)uy, p.B), S);
     cfg.stream = stream;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kv8_attn_kernel<D, MT, RW, SEL>, p);
+    return cudaLaunchKernelEx(&cfg, kv8_attn_kernel<D, MT, RW, NW, SEL>, p);
   }
 };
 
@@ -754,9 +760,14 @@ cudaError_t pick(Params& p, int pages, cudaStream_t stream) {
     return launch_kv8_attn_tc(p, D, s.S, stream);
   }
   const int tiles = (pages + 1) / 2;
-  if (p.rows <= 16) return Variant<D, 1, 1, SEL>::launch(p, Variant<D, 1, 1, SEL>::split(p, tiles).S, stream);
-  const Split wide = Variant<D, 2, 1, SEL>::split(p, tiles), pair = Variant<D, 1, 2, SEL>::split(p, tiles);
-  return wide.us < pair.us ? Variant<D, 2, 1, SEL>::launch(p, wide.S, stream) : Variant<D, 1, 2, SEL>::launch(p, pair.S, stream);
+  if (p.rows <= 16) {
+    const Split four = Variant<D, 1, 1, 4, SEL>::split(p, tiles), eight = Variant<D, 1, 1, 8, SEL>::split(p, tiles);
+    return four.us < eight.us ? Variant<D, 1, 1, 4, SEL>::launch(p, four.S, stream) : Variant<D, 1, 1, 8, SEL>::launch(p, eight.S, stream);
+  }
+  const Split wide = Variant<D, 2, 1, 4, SEL>::split(p, tiles), four = Variant<D, 1, 2, 4, SEL>::split(p, tiles);
+  const Split eight = Variant<D, 1, 2, 8, SEL>::split(p, tiles);
+  if (wide.us < four.us && wide.us < eight.us) return Variant<D, 2, 1, 4, SEL>::launch(p, wide.S, stream);
+  return four.us < eight.us ? Variant<D, 1, 2, 4, SEL>::launch(p, four.S, stream) : Variant<D, 1, 2, 8, SEL>::launch(p, eight.S, stream);
 }
 
 }  // namespace
