@@ -283,6 +283,35 @@ def test_attention_of_large_small_and_uneven_values(std, qstd, spread, R, Hq, H,
     assert np.all(err <= 2.0 ** -8 * (np.abs(o) + mag) + extra * mag), float((err / (np.abs(o) + mag)).max())
 
 
+@pytest.mark.parametrize("ctx,R,Hq,H,D", [([700], 1, 32, 8, 128), ([130, 513], 6, 32, 8, 128), ([300], 8, 16, 4, 64), ([90, 0, 410], 12, 16, 4, 128),
+                                          ([257], 3, 8, 2, 64)])
+def test_attention_under_every_plan(ctx, R, Hq, H, D):
+    """Rings, warps and split are planned from the longest context that the caller expects, or the pages it selects: none
+    may change what comes out."""
+    rng = np.random.default_rng(sum(ctx) + 7 * R)
+    B, wide = len(ctx), 8192
+    pool, ref, table = _cached(rng, ctx, R, H, D)
+    padded = np.full((B, wide), -1, np.int32)
+    padded[:, :table.shape[1]] = table
+    q, kb, vb = _fused(rng, (B, R), Hq, H, D)
+    out = torch.empty((B, R, Hq, D), dtype=torch.bfloat16, device="cuda")
+    want = K.attention(_np(q), _np(kb), _np(vb), ref, 0, table, ctx)
+    for max_ctx in (16, 256, 1024, 4096, 12000, 32768, 16 * wide):
+        out.fill_(math.nan)
+        C.kv8_attn(q, kb, vb, pool, 0, _ints(padded), _ints(ctx), out, max_ctx)
+        assert C.get_device_error() == 0
+        _assert_attn(out, *want, what=f"max_ctx {max_ctx}")
+    chosen = K.select(_np(q), ref, 0, table, ctx, 9, 1, 2)
+    want = K.attention(_np(q), _np(kb), _np(vb), ref, 0, table, ctx, sel=chosen)
+    for pages in (9, 64, 300, 2000):
+        sel = np.full(chosen.shape[:3] + (pages,), -1, np.int32)
+        sel[..., :9] = chosen
+        out.fill_(math.nan)
+        C.kv8_attn(q, kb, vb, pool, 0, _ints(padded), _ints(ctx), out, max(ctx), sel=_ints(sel))
+        assert C.get_device_error() == 0
+        _assert_attn(out, *want, what=f"{pages} pages")
+
+
 def test_attention_scale_layer_and_short_table():
     rng = np.random.default_rng(11)
     ctx = [48, 80]
