@@ -69,14 +69,6 @@ CS_DEV void kv8_floats4(uint32_t w, float (&f)[4]) {
 CS_DEV void kv8_copy16(uint32_t dst, const void* src, uint64_t policy) {
   asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
 }
-CS_DEV uint4 kv8_load16(const void* src, uint64_t policy) {
-  uint4 v;
-  asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-               : "l"(src), "l"(policy)
-               : "memory");
-  return v;
-}
 CS_DEV void kv8_copy_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 CS_DEV void kv8_copy_wait() {               // all but the newest N groups have landed
@@ -90,7 +82,6 @@ CS_DEV void kv8_floats_of(uint2 u, float (&x)[4]) {
   x[2] = __uint_as_float(u.y << 16);
   x[3] = __uint_as_float(u.y & 0xffff0000u);
 }
-CS_DEV void kv8_load4(const __nv_bfloat16* p, float (&x)[4]) { kv8_floats_of(*reinterpret_cast<const uint2*>(p), x); }
 CS_DEV void kv8_store4(__nv_bfloat16* p, const float (&x)[4]) {
   *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
 }

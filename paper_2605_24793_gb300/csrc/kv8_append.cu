@@ -65,7 +65,7 @@ CS_DEV float head_max(float v) {
 }
 
 template <int D>
-__global__ void __launch_bounds__(WARPS * 32)
+__global__ void __launch_bounds__(WARPS * 32, 5)
     kv8_append_kernel(const Kv8AppendArgs a, const Geometry g, int* err) {
   constexpr int LPH = D / 4;               // lanes of a head
   constexpr int HPW = 32 / LPH;            // heads of a warp
@@ -160,15 +160,20 @@ __global__ void __launch_bounds__(WARPS * 32)
   }
   if (first >= shown) return;
   const bool fresh = first < last;          // the page receives rows (else k_out alone does)
-  const int phys = fresh ? a.page_table[(size_t)b * a.max_pages + page] : -1;
-
   const Kv8Src& src = which ? a.v : a.k;
   const __nv_bfloat16* row0 = src.p + l * src.layer + b * src.batch + (long long)j0 * src.row + (size_t)(live ? h : 0) * D + d;
+  // Rows and older codes are asked for as soon as their addresses are known: a lane half a row of 128 dimensions, and
+  // 64 bytes of the page.
+  if (first <= lane >> 1 && lane >> 1 < shown)
+    prefetch_l2(src.p + l * src.layer + b * src.batch + (long long)(j0 + (lane >> 1)) * src.row + (size_t)min(hg * 128 + (lane & 1) * 64, a.Hkv * D - 1));
+  const int phys = fresh ? a.page_table[(size_t)b * a.max_pages + page] : -1;
+
   const bool bad = fresh && (unsigned)phys >= (unsigned)a.num_pages;
   if (bad && lane == 0) set_err(err, ERR_PAGE);
   const bool put = fresh && !bad;
   const size_t cell = ((size_t)l * a.num_pages + (put ? phys : 0)) * a.Hkv + (live ? h : 0);   // this layer's page and head
   const bool old = put && first > 0;
+  if (old && live) prefetch_l2((which ? a.pool.v : a.pool.k) + cell * (KV8_PAGE * D) + lane % LPH * 64);
   const float was_scale = old ? a.pool.scale[cell * 2 + which] : 0.f;
   float4* mine = &held[warp][0][lane];                     // this lane's row i: mine[32 * i]
   float amax = 0.f;
