@@ -4,10 +4,13 @@
 // row, KV head, up to 32 of its query heads).  Its pages go in pairs (32 keys: a tile) to the rings of a
 // thread-block cluster, tile t of the unit to ring t mod (rings S).  A ring belongs to one warp or to two,
 // and no ring waits for another until the end.  A ring's warps bring its tiles in together, asynchronously, and each puts
-// its own 16 or 32 rows to them.  Variants, chosen by the estimates below:
-//   up to 16 rows: a warp a ring, four to a CTA and two CTAs an SM (rings of three tiles: with three CTAs and rings of two
-//   batch 64 at 8192 to 32768 tokens took 460 us for 395), or eight to a CTA, which fills the SMs that a few clusters
-//   get: one user at 4096 tokens 8.3 us with four warps and 9.0 with eight, at 32768 tokens 26.5 and 22.3;
+// its own rows to them.  Variants, chosen by the estimates below:
+//   up to 8 rows (a token of up to 8 heads): keys and values are the products' rows and the query rows their columns, half
+//   the instructions of 16 padded rows.  A warp a ring, four to a CTA and two CTAs an SM, or eight to a CTA, which fills
+//   the SMs that a few clusters get.  One user at 4096 tokens: 7.5 us with four warps, 7.9 with eight, 8.3 with the rows
+//   padded; at 32768 24.3, 20.2 and 26.5; 128 selected pages for each of 128 rows 91, padded 103;
+//   up to 16 rows: the same two with rows padded to 16 (rings of three tiles: with three CTAs and rings of two batch 64 at
+//   8192 to 32768 tokens took 460 us for 395);
 //   up to 32 rows: a warp of 32 rows a ring (each code converted once), or two of 16 (half the registers, shorter steps),
 //   these with four warps and three CTAs an SM or with eight.  At 24 to 32 rows, with 32 rows a warp, two warps of four,
 //   two warps of eight: one user at 4096 tokens 13.1, 11.7, 10.4 us; batch 8 28.9, 27.1, 28.2; batch 32 at 2048 to 16384
@@ -26,7 +29,7 @@
 // The contraction's order is free, so every lane converts what it can load wide: of a key it takes 32
 // (16) dimensions side by side, the query rows laid out alike, and of a dimension's values four tokens of
 // each page; accumulator columns 2c and 2c + 1 are then token 4c + i of the two pages, which is what
-// the lane's value codes want.  A pad between the two pages' keys makes the loads conflict-free.
+// the lane's value codes want (with the query rows as columns the weights are turned by movmatrix first).  A pad between the two pages' keys makes the loads conflict-free.
 //
 // The block's keys and values (bf16, up to 64) go 16 at a time to the warps of the cluster's last CTA, on
 // bf16 operands.  The warps' partial (max, sum, output) meet in shared memory, the CTAs' in
@@ -57,8 +60,8 @@ struct Lay {
   static constexpr int CTAS = NW == 8 ? 1 : RW == 2 ? 3 : 2;            // of an SM
   static constexpr int NST = D == 64 || RW == 2 ? 4 : 3;  // tiles of a ring
   static constexpr int RING = NST * STAGE;
-  static constexpr int NR = 16 * MT * RW;
-  static constexpr int PD = D + 8;                        // fp32 row of a partial: O, max, sum, pad
+  static constexpr int NR = MT ? 16 * MT * RW : 8;
+  static constexpr int PD = D + (MT ? 8 : 4);             // fp32 row of a partial: O, max, sum, pad
   static constexpr int ROWB = PD * 4;
   static constexpr int PART = 0;                          // [KW][NR] rows; the CTA's own result in the first NR
   static constexpr int RECV = KW * NR * ROWB;             // [S][rows per owner], at most NR + 15 rows
@@ -105,6 +108,16 @@ struct State {
   float o[MT][D / 8][4];
   float m[MT][2], l[MT][2];     // reference of the weights (base 2), their sum
   float vref;                   // o and the weights count in units of this values' scale
+  CS_DEV void clear() {
+    vref = 0.f;
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      m[t][0] = m[t][1] = -INFINITY;
+      l[t][0] = l[t][1] = 0.f;
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) o[t][i][0] = o[t][i][1] = o[t][i][2] = o[t][i][3] = 0.f;
+    }
+  }
 };
 
 // The reference of a row's weights after scores whose largest is mx: it stays while that is less than
@@ -134,6 +147,65 @@ CS_DEV void follow_max(State<D, MT>& st, int t, float mx0, float mx1, float (&ba
       st.o[t][i][3] *= a[1];
     }
   }
+}
+
+// Up to eight rows: they are the columns, this lane's 2 c and 2 c + 1, of products whose rows are keys or dimensions.
+template <int D>
+struct State<D, 0> {
+  uint32_t q[D / 16][2];        // of row g: the lane's D / 4 dimensions, four a fragment
+  float f[2];
+  float o[D / 16][4];           // dimensions 16 i + g of the two columns, then 16 i + 8 + g
+  float m[2], l[2];
+  float vref;
+  CS_DEV void clear() {
+    vref = 0.f;
+    m[0] = m[1] = -INFINITY;
+    l[0] = l[1] = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+  }
+};
+template <int D>
+CS_DEV void follow_max(State<D, 0>& st, float mx0, float mx1, float (&base)[2]) {
+  float mx[2] = {mx0, mx1}, a[2];
+  bool moved = false;
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+#pragma unroll
+    for (int x = 4; x < 32; x *= 2) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], x));
+    const float was = st.m[e], now = mx[e] > was + P_ROOM ? mx[e] : was;
+    moved |= now != was;
+    st.m[e] = now;
+    base[e] = (now == -INFINITY ? 0.f : now) - P_BITS;
+    a[e] = exp2_approx(was - P_BITS - base[e]);
+  }
+  if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      st.l[e] *= a[e];
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        st.o[i][e] *= a[e];
+        st.o[i][2 + e] *= a[e];
+      }
+    }
+  }
+}
+template <int D>
+CS_DEV void raise_unit(State<D, 0>& st, float top) {
+  if (top <= st.vref) return;
+  const float by = st.vref * kv8_inverse(top);
+  st.vref = top;
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) st.o[i][e] *= by;
+}
+// An 8 x 8 matrix of 16-bit numbers, a row in four lanes, turned.
+CS_DEV uint32_t turn8(uint32_t x) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
 }
 
 // Values of scale `top` are to join the output (the same in every lane).
@@ -264,6 +336,90 @@ CS_DEV void tile(State<D, MT>& st, uint32_t sk, uint32_t sv, const float (&ks)[2
   }
 }
 
+// The same for up to eight rows: keys times rows, then dimensions times rows.  The same loads as above: here tokens
+// 4 (g / 2) + i of page g mod 2 are rows g (i even) and g + 8 (i odd) of product i / 2.
+template <int D, bool MASK>
+CS_DEV void tile(State<D, 0>& st, uint32_t sk, uint32_t sv, const float (&ks)[2], const float (&vs)[2], int n0, int n1, int lane) {
+  using L = Lay<D, 0, 1, 4>;
+  const int g = lane >> 2, c = lane & 3;
+  float s[2][4] = {};
+  const uint32_t ka = sk + (uint32_t)((g & 1) * (L::PB + L::PADK) + (g >> 1) * 4 * D + c * (D / 4));
+#pragma unroll
+  for (int x = 0; x < D / 64; ++x) {
+    uint32_t w[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint4 v = lds128(ka + (uint32_t)(i * D + x * 16));
+      w[i][0] = v.x;
+      w[i][1] = v.y;
+      w[i][2] = v.z;
+      w[i][3] = v.w;
+    }
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t a[4] = {kv8_f16x2(w[2 * j][y]), kv8_f16x2(w[2 * j + 1][y]), kv8_f16x2_hi(w[2 * j][y]), kv8_f16x2_hi(w[2 * j + 1][y])};
+        mma_f16(s[j], a, st.q[x * 4 + y][0], st.q[x * 4 + y][1]);
+      }
+  }
+  raise_unit(st, fmaxf(vs[0], vs[1]));
+  const float kscale = g & 1 ? ks[1] : ks[0];
+  const int k = max((int)(__float_as_uint(g & 1 ? vs[1] : vs[0]) >> 23) - (int)(__float_as_uint(st.vref) >> 23), -60);
+  const float ve = (float)k, vi = __uint_as_float((uint32_t)(127 - k) << 23);
+  const int have = (g & 1 ? n1 : n0) - 4 * (g >> 1);       // of this lane's four tokens
+  float base[2], mx[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    if (MASK) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i >= have) s[i >> 1][2 * (i & 1) + e] = -INFINITY;
+    }
+    mx[e] = fmaxf(fmaxf(s[0][e], s[0][2 + e]), fmaxf(s[1][e], s[1][2 + e])) * (st.f[e] * kscale);      // (NaN, as of -inf and 0, does not count)
+  }
+  follow_max(st, mx[0], mx[1], base);
+  uint32_t t[4];
+  {
+    float x[4][2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const float f = st.f[e] * kscale, to = ve - base[e];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[i][e] = exp2_approx(fmaf(s[i >> 1][2 * (i & 1) + e], f, to));
+        if (MASK && i >= have) x[i][e] = 0.f;
+      }
+      st.l[e] = fmaf((x[0][e] + x[1][e]) + (x[2][e] + x[3][e]), vi, st.l[e]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = turn8(pack_f16(x[i][0], x[i][1]));  // row g's weights of token 4 c + i of the two pages
+  }
+  uint32_t keep[2] = {0xffffffffu, 0xffffffffu};           // cells behind a page's last token read as 0
+  if (MASK) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int left = (e ? n1 : n0) - 4 * c;
+      keep[e] = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+    }
+  }
+  const uint32_t va = sv + (uint32_t)(g * KV8_PAGE + c * 4);
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const uint32_t b0 = __byte_perm(t[0], t[1], e ? 0x7632 : 0x5410), b1 = __byte_perm(t[2], t[3], e ? 0x7632 : 0x5410);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      uint32_t w0 = lds32(va + (uint32_t)(e * L::PB + i * 16 * KV8_PAGE)), w1 = lds32(va + (uint32_t)(e * L::PB + (i * 16 + 8) * KV8_PAGE));
+      if (MASK) {
+        w0 &= keep[e];
+        w1 &= keep[e];
+      }
+      const uint32_t a[4] = {kv8_f16x2(w0), kv8_f16x2(w1), kv8_f16x2_hi(w0), kv8_f16x2_hi(w1)};
+      mma_f16(st.o[i], a, b0, b1);
+    }
+  }
+}
+
 template <int D, int MT, int RW, int NW, bool SEL>
 __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_kernel(const Params p) {
   using L = Lay<D, MT, RW, NW>;
@@ -376,29 +532,28 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
 
   // ---------------------------------------------------------------- queries
   State<D, MT> st;
-  st.vref = 0.f;
-  const __nv_bfloat16* qrow[MT][2];
-  int lim[MT][2];                                          // last block row that the query row sees
+  constexpr int MR = MT ? MT : 1, RR = MT ? 2 : 1;         // (eight rows: row g only)
+  const __nv_bfloat16* qrow[MR][2];
+  int lim[MR][2];                                          // last block row that the query row sees
 #pragma unroll
-  for (int t = 0; t < MT; ++t)
+  for (int t = 0; t < MR; ++t)
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
+    for (int r = 0; r < RR; ++r) {
       const int x = (rw * MT + t) * 16 + g + 8 * r;
       const int row = row0 + min(x, nr - 1);
       const int j = SEL ? jj : row / p.G, head = h * p.G + (SEL ? row : row % p.G);
       qrow[t][r] = x < nr ? p.q.p + b * p.q.batch + j * p.q.row + (size_t)head * D + c * (D / 4) : nullptr;
       lim[t][r] = p.block_full ? p.R - 1 : j;
-      st.m[t][r] = -INFINITY;
-      st.l[t][r] = 0.f;
     }
+  if constexpr (MT == 0) {                                 // (of the columns)
 #pragma unroll
-  for (int t = 0; t < MT; ++t)
+    for (int e = 0; e < 2; ++e) lim[0][e] = p.block_full ? p.R - 1 : SEL ? jj : (row0 + min(2 * c + e, nr - 1)) / p.G;
+  }
+  st.clear();
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) st.o[t][i][0] = st.o[t][i][1] = st.o[t][i][2] = st.o[t][i][3] = 0.f;
+  for (int t = 0; t < MR; ++t)
 #pragma unroll
-  for (int t = 0; t < MT; ++t)
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
+    for (int r = 0; r < RR; ++r) {
       uint4 w[D / 32];
       float amax = 0.f;
 #pragma unroll
@@ -412,7 +567,12 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
       amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
       amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
       const float sc = kv8_scale127(amax), inv = kv8_inverse(sc);      // |q / sc| <= 127
-      st.f[t][r] = sc * p.scale_log2;
+      if constexpr (MT == 0) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) st.f[e] = __shfl_sync(0xffffffffu, sc, 8 * c + 4 * e) * p.scale_log2;
+      } else {
+        st.f[t][r] = sc * p.scale_log2;
+      }
 #pragma unroll
       for (int i = 0; i < D / 32; ++i) {
         const uint32_t ww[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
@@ -420,12 +580,13 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
         for (int y = 0; y < 4; ++y) {      // pairs of the lane's dimensions 8 i + 2 y: fragment 2 i + y / 2, half y & 1
           const uint32_t v = pack_f16(__uint_as_float(ww[y] << 16) * inv, __uint_as_float(ww[y] & 0xffff0000u) * inv);
           const int fr = 2 * i + (y >> 1), z = r + 2 * (y & 1);
-          if (!L::QS) st.q[L::QS ? 0 : fr][z] = v;
+          if constexpr (MT == 0) st.q[fr][y & 1] = v;
+          else if (!L::QS) st.q[L::QS ? 0 : fr][z] = v;
           else if (warp == 0) *reinterpret_cast<uint32_t*>(smem + L::BODY + (t * (D / 16) + fr) * 512 + lane * 16 + z * 4) = v;
         }
       }
     }
-  st.qs = smem_u32(smem + L::BODY) + lane * 16;
+  if constexpr (MT != 0) st.qs = smem_u32(smem + L::BODY) + lane * 16;
   if (L::QS) __syncthreads();
 
   // ---------------------------------------------------------------- the block's own rows
@@ -451,64 +612,95 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
     for (int o = 16; o > 0; o >>= 1) vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, o));
     raise_unit(st, kv8_scale_of(vmax));
     const float iv = kv8_inverse(st.vref);
-    float s[MT][2][4];
-#pragma unroll
-    for (int t = 0; t < MT; ++t)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) s[t][i][0] = s[t][i][1] = s[t][i][2] = s[t][i][3] = 0.f;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint8_t* kr = kbuf + (i * 8 + g) * (2 * D);
+    if constexpr (MT == 0) {
+      float s[4] = {};
 #pragma unroll
       for (int x = 0; x < D / 32; ++x) {
-        const uint4 w = *reinterpret_cast<const uint4*>(kr + ((c * (D / 32) + x) ^ g) * 16);
+        const uint8_t* kr = kbuf + g * (2 * D) + ((c * (D / 32) + x) ^ g) * 16;
+        const uint4 w = *reinterpret_cast<const uint4*>(kr), w8 = *reinterpret_cast<const uint4*>(kr + 8 * 2 * D);
+        const uint4 qv = qrow[0][0] ? *reinterpret_cast<const uint4*>(qrow[0][0] + x * 8) : make_uint4(0u, 0u, 0u, 0u);
+        const uint32_t a0[4] = {w.x, w8.x, w.y, w8.y}, a1[4] = {w.z, w8.z, w.w, w8.w};
+        mma_16816(s, a0, qv.x, qv.y);
+        mma_16816(s, a1, qv.z, qv.w);
+      }
+      float base[2];
 #pragma unroll
-        for (int t = 0; t < MT; ++t) {
-          uint4 qa = make_uint4(0u, 0u, 0u, 0u), qb = qa;
-          if (qrow[t][0]) qa = *reinterpret_cast<const uint4*>(qrow[t][0] + x * 8);
-          if (qrow[t][1]) qb = *reinterpret_cast<const uint4*>(qrow[t][1] + x * 8);
-          const uint32_t a0[4] = {qa.x, qb.x, qa.y, qb.y}, a1[4] = {qa.z, qb.z, qa.w, qb.w};
-          mma_16816(s[t][i], a0, w.x, w.y);
-          mma_16816(s[t][i], a1, w.z, w.w);
+      for (int e = 0; e < 4; ++e) s[e] = k0 + g + 8 * (e >> 1) <= lim[0][e & 1] ? s[e] * p.scale_log2 : -INFINITY;
+      follow_max(st, fmaxf(s[0], s[2]), fmaxf(s[1], s[3]), base);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[e] = exp2_approx(s[e] - base[e & 1]);
+        st.l[e & 1] += s[e];
+      }
+      const uint32_t b0 = turn8(pack_bf16(s[0] * iv, s[1] * iv)), b1 = turn8(pack_bf16(s[2] * iv, s[3] * iv));
+      const int key = (lane & 7) + (lane >> 4) * 8;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        const int ch = 2 * i + ((lane >> 3) & 1);
+        uint32_t a[4];
+        ldsm_x4_t(smem_u32(vbuf) + (uint32_t)(key * (2 * D) + ((ch ^ (key & 7)) * 16)), a[0], a[1], a[2], a[3]);
+        mma_16816(st.o[i], a, b0, b1);
+      }
+    } else {
+      float s[MT][2][4];
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) s[t][i][0] = s[t][i][1] = s[t][i][2] = s[t][i][3] = 0.f;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint8_t* kr = kbuf + (i * 8 + g) * (2 * D);
+#pragma unroll
+        for (int x = 0; x < D / 32; ++x) {
+          const uint4 w = *reinterpret_cast<const uint4*>(kr + ((c * (D / 32) + x) ^ g) * 16);
+#pragma unroll
+          for (int t = 0; t < MT; ++t) {
+            uint4 qa = make_uint4(0u, 0u, 0u, 0u), qb = qa;
+            if (qrow[t][0]) qa = *reinterpret_cast<const uint4*>(qrow[t][0] + x * 8);
+            if (qrow[t][1]) qb = *reinterpret_cast<const uint4*>(qrow[t][1] + x * 8);
+            const uint32_t a0[4] = {qa.x, qb.x, qa.y, qb.y}, a1[4] = {qa.z, qb.z, qa.w, qb.w};
+            mma_16816(s[t][i], a0, w.x, w.y);
+            mma_16816(s[t][i], a1, w.z, w.w);
+          }
         }
       }
-    }
-    uint32_t pf[MT][4];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int key = k0 + i * 8 + 2 * c + e;
-          s[t][i][e] = key <= lim[t][0] ? s[t][i][e] * p.scale_log2 : -INFINITY;
-          s[t][i][2 + e] = key <= lim[t][1] ? s[t][i][2 + e] * p.scale_log2 : -INFINITY;
-        }
-      float base[2];
-      follow_max(st, t, fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][1][0], s[t][1][1])),
-                 fmaxf(fmaxf(s[t][0][2], s[t][0][3]), fmaxf(s[t][1][2], s[t][1][3])), base);
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s[t][i][e] = exp2_approx(s[t][i][e] - base[e >> 1]);
-          st.l[t][e >> 1] += s[t][i][e];
-        }
-      pf[t][0] = pack_bf16(s[t][0][0] * iv, s[t][0][1] * iv);
-      pf[t][1] = pack_bf16(s[t][0][2] * iv, s[t][0][3] * iv);
-      pf[t][2] = pack_bf16(s[t][1][0] * iv, s[t][1][1] * iv);
-      pf[t][3] = pack_bf16(s[t][1][2] * iv, s[t][1][3] * iv);
-    }
-    const int key = (lane & 7) + ((lane >> 3) & 1) * 8;
-#pragma unroll
-    for (int d = 0; d < D / 8; d += 2) {
-      const int ch = d + (lane >> 4);
-      uint32_t b0, b1, b2, b3;
-      ldsm_x4_t(smem_u32(vbuf) + (uint32_t)(key * (2 * D) + ((ch ^ (key & 7)) * 16)), b0, b1, b2, b3);
+      uint32_t pf[MT][4];
 #pragma unroll
       for (int t = 0; t < MT; ++t) {
-        mma_16816(st.o[t][d], pf[t], b0, b1);
-        mma_16816(st.o[t][d + 1], pf[t], b2, b3);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int key = k0 + i * 8 + 2 * c + e;
+            s[t][i][e] = key <= lim[t][0] ? s[t][i][e] * p.scale_log2 : -INFINITY;
+            s[t][i][2 + e] = key <= lim[t][1] ? s[t][i][2 + e] * p.scale_log2 : -INFINITY;
+          }
+        float base[2];
+        follow_max(st, t, fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][1][0], s[t][1][1])),
+                   fmaxf(fmaxf(s[t][0][2], s[t][0][3]), fmaxf(s[t][1][2], s[t][1][3])), base);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s[t][i][e] = exp2_approx(s[t][i][e] - base[e >> 1]);
+            st.l[t][e >> 1] += s[t][i][e];
+          }
+        pf[t][0] = pack_bf16(s[t][0][0] * iv, s[t][0][1] * iv);
+        pf[t][1] = pack_bf16(s[t][0][2] * iv, s[t][0][3] * iv);
+        pf[t][2] = pack_bf16(s[t][1][0] * iv, s[t][1][1] * iv);
+        pf[t][3] = pack_bf16(s[t][1][2] * iv, s[t][1][3] * iv);
+      }
+      const int key = (lane & 7) + ((lane >> 3) & 1) * 8;
+#pragma unroll
+      for (int d = 0; d < D / 8; d += 2) {
+        const int ch = d + (lane >> 4);
+        uint32_t b0, b1, b2, b3;
+        ldsm_x4_t(smem_u32(vbuf) + (uint32_t)(key * (2 * D) + ((ch ^ (key & 7)) * 16)), b0, b1, b2, b3);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+          mma_16816(st.o[t][d], pf[t], b0, b1);
+          mma_16816(st.o[t][d + 1], pf[t], b2, b3);
+        }
       }
     }
   }
@@ -528,10 +720,14 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
     const float vs[2] = {__shfl_sync(0xffffffffu, scale_c.y, at), __shfl_sync(0xffffffffu, scale_c.y, at + 1)};
     const uint32_t sk = smem_u32(ring + sg * L::STAGE);
     if ((whole >> at & 3u) == 3u) {
-      tile<D, MT, false>(st, sk, sk + L::KREG, ks, vs, KV8_PAGE, KV8_PAGE, lane);
+      if constexpr (MT == 0) tile<D, false>(st, sk, sk + L::KREG, ks, vs, KV8_PAGE, KV8_PAGE, lane);
+      else tile<D, MT, false>(st, sk, sk + L::KREG, ks, vs, KV8_PAGE, KV8_PAGE, lane);
     } else {
       const int n0 = __shfl_sync(0xffffffffu, count_c, at), n1 = __shfl_sync(0xffffffffu, count_c, at + 1);
-      if (n0 + n1 > 0) tile<D, MT, true>(st, sk, sk + L::KREG, ks, vs, n0, n1, lane);
+      if (n0 + n1 > 0) {
+        if constexpr (MT == 0) tile<D, true>(st, sk, sk + L::KREG, ks, vs, n0, n1, lane);
+        else tile<D, MT, true>(st, sk, sk + L::KREG, ks, vs, n0, n1, lane);
+      }
     }
   }
   kv8_copy_wait<0>();
@@ -547,26 +743,43 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
   {
     const float unit = st.vref * exp2f(-P_BITS), one = exp2f(-P_BITS);
     float* mypart = part + (kw * L::NR + rw * 16) * L::PD;
+    if constexpr (MT == 0) {
 #pragma unroll
-    for (int t = 0; t < MT; ++t)
+      for (int e = 0; e < 2; ++e) {
+        float* row = mypart + (2 * c + e) * L::PD;
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        float* row = mypart + (t * 16 + g + 8 * r) * L::PD;
+        for (int i = 0; i < D / 16; ++i) {
+          row[16 * i + g] = st.o[i][e] * unit;
+          row[16 * i + 8 + g] = st.o[i][2 + e] * unit;
+        }
+        float l = st.l[e];
 #pragma unroll
-        for (int d = 0; d < D / 8; ++d)
-          *reinterpret_cast<float2*>(row + d * 8 + 2 * c) = make_float2(st.o[t][d][2 * r] * unit, st.o[t][d][2 * r + 1] * unit);
-        float l = st.l[t][r];
-        l += __shfl_xor_sync(0xffffffffu, l, 1);
-        l += __shfl_xor_sync(0xffffffffu, l, 2);
-        if (c == 0) *reinterpret_cast<float2*>(row + D) = make_float2(st.m[t][r], l * one);
+        for (int x = 4; x < 32; x *= 2) l += __shfl_xor_sync(0xffffffffu, l, x);
+        if (g == 0) *reinterpret_cast<float2*>(row + D) = make_float2(st.m[e], l * one);
       }
+    } else {
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          float* row = mypart + (t * 16 + g + 8 * r) * L::PD;
+#pragma unroll
+          for (int d = 0; d < D / 8; ++d)
+            *reinterpret_cast<float2*>(row + d * 8 + 2 * c) = make_float2(st.o[t][d][2 * r] * unit, st.o[t][d][2 * r + 1] * unit);
+          float l = st.l[t][r];
+          l += __shfl_xor_sync(0xffffffffu, l, 1);
+          l += __shfl_xor_sync(0xffffffffu, l, 2);
+          if (c == 0) *reinterpret_cast<float2*>(row + D) = make_float2(st.m[t][r], l * one);
+        }
+    }
   }
   __syncthreads();
   // A row's KW parts into the first, by a group of D / 4 lanes.
   constexpr int LPR = D / 4;
-  static_assert(L::NR % (NW * 32 / LPR) == 0, "whole passes over the rows");
+  static_assert(L::NR % (32 / LPR) == 0, "a warp's rows are all there, or none");
   for (int r0 = 0; r0 < nr; r0 += NW * 32 / LPR) {         // (a last pass may touch rows past nr)
     const int r = r0 + tid / LPR, x = tid % LPR * 4;
+    if (r >= L::NR) continue;
     float2 ml[KW];
     float top = -INFINITY;
 #pragma unroll
@@ -718,6 +931,7 @@ struct Variant {
   static Split split(const Params& p, int tiles) {
     return split_of(units(p), tiles, L::KW,
                     MT == 2   ? Cost{10.0, 1.32, 1.96}
+                    : MT == 0 ? (NW == 8 ? Cost{6.8, 1.1, 1.3} : Cost{5.5, 0.79, 1.45})
                     : RW == 2 ? (NW == 8 ? Cost{7.3, 1.15, 1.15} : Cost{6.8, 0.88, 1.5})
                               : (NW == 8 ? Cost{7.3, 1.27, 1.27} : Cost{6.0, 0.95, 1.45}),
                     resident);
@@ -760,6 +974,10 @@ cudaError_t pick(Params& p, int pages, cudaStream_t stream) {
     return launch_kv8_attn_tc(p, D, s.S, stream);
   }
   const int tiles = (pages + 1) / 2;
+  if (p.rows <= 8) {
+    const Split four = Variant<D, 0, 1, 4, SEL>::split(p, tiles), eight = Variant<D, 0, 1, 8, SEL>::split(p, tiles);
+    return four.us < eight.us ? Variant<D, 0, 1, 4, SEL>::launch(p, four.S, stream) : Variant<D, 0, 1, 8, SEL>::launch(p, eight.S, stream);
+  }
   if (p.rows <= 16) {
     const Split four = Variant<D, 1, 1, 4, SEL>::split(p, tiles), eight = Variant<D, 1, 1, 8, SEL>::split(p, tiles);
     return four.us < eight.us ? Variant<D, 1, 1, 4, SEL>::launch(p, four.S, stream) : Variant<D, 1, 1, 8, SEL>::launch(p, eight.S, stream);
