@@ -5,16 +5,17 @@
 // thread-block cluster, tile t of the unit to ring t mod (rings S).  A ring belongs to one warp or to two,
 // and no ring waits for another until the end.  A ring's warps bring its tiles in together, asynchronously, and each puts
 // its own rows to them.  Variants, chosen by the estimates below:
-//   up to 8 rows (a token of up to 8 heads): keys and values are the products' rows and the query rows their columns, half
-//   the instructions of 16 padded rows.  A warp a ring, four to a CTA and two CTAs an SM, or eight to a CTA, which fills
-//   the SMs that a few clusters get.  One user at 4096 tokens: 7.5 us with four warps, 7.9 with eight, 8.3 with the rows
-//   padded; at 32768 24.3, 20.2 and 26.5; 128 selected pages for each of 128 rows 91, padded 103;
-//   up to 16 rows: the same two with rows padded to 16 (rings of three tiles: with three CTAs and rings of two batch 64 at
-//   8192 to 32768 tokens took 460 us for 395);
-//   up to 32 rows: a warp of 32 rows a ring (each code converted once), or two of 16 (half the registers, shorter steps),
-//   these with four warps and three CTAs an SM or with eight.  At 24 to 32 rows, with 32 rows a warp, two warps of four,
-//   two warps of eight: one user at 4096 tokens 13.1, 11.7, 10.4 us; batch 8 28.9, 27.1, 28.2; batch 32 at 2048 to 16384
-//   140, 157, 164; batch 64 at 8192 to 32768 544, 627, 706.
+//   columns: the query rows are the products' columns, eight at a time, keys and values their rows, so that up to 8 and 17
+//   to 24 rows are padded less than by 16.  A warp a ring, four to a CTA and two CTAs an SM; up to 8 rows also eight to a
+//   CTA, which fills the SMs that a few clusters get.  Up to 8 rows: one user at 4096 tokens 7.5 us with four warps, 7.9
+//   with eight, 8.3 with padded rows; at 32768 24.3, 20.2 and 26.5; 128 selected pages for each of 128 rows 91, padded
+//   103.  At 24 rows: batch 16 at 2048 to 8192 tokens 52 us, padded 59; batch 64 at 8192 to 32768 484, padded 538;
+//   rows: the query rows are the products' rows, by 16, which is as good where they fill them and has fewer shuffles: batch
+//   64 at 32 rows 538 us for 564, at 12 rows one user 8.3 for 9.2.  Up to 16 a warp a ring, as above (rings of three
+//   tiles: with three CTAs and rings of two batch 64 at 8192 to 32768 tokens took 460 us for 395); up to 32 a warp of 32
+//   rows a ring (each code converted once), or two of 16 (half the registers, shorter steps) with four warps and three
+//   CTAs an SM or with eight.  A warp of 32, two of four, two of eight at 32 rows: one user at 4096 tokens 12.1, 11.7,
+//   10.4 us; batch 32 at 2048 to 16384 138, 157, 164; batch 64 at 8192 to 32768 537, 627, 706.
 // More rows go to the tcgen05 kernel (kv8_attn_tc.cu): at 64 rows two groups of 32 here took 95 us where that takes 70
 // (batch 16, 2048 to 8192 tokens), at 40 91 and 70, at 32 66 and 68; batch 64 540 and 756 at 32 rows, 1011 and 759 at 40.
 //
@@ -29,12 +30,15 @@
 // The contraction's order is free, so every lane converts what it can load wide: of a key it takes 32
 // (16) dimensions side by side, the query rows laid out alike, and of a dimension's values four tokens of
 // each page; accumulator columns 2c and 2c + 1 are then token 4c + i of the two pages, which is what
-// the lane's value codes want (with the query rows as columns the weights are turned by movmatrix first).  A pad between the two pages' keys makes the loads conflict-free.
+// the lane's value codes want (with the query rows as columns the weights are turned by movmatrix first).  A pad between
+// the two pages' keys makes the loads conflict-free.
 //
 // The block's keys and values (bf16, up to 64) go 16 at a time to the warps of the cluster's last CTA, on
 // bf16 operands.  The warps' partial (max, sum, output) meet in shared memory, the CTAs' in
 // distributed shared memory, each CTA finishing a slice of the rows.
 #include <math.h>
+
+#include <type_traits>
 
 #include "cospec_internal.h"
 #include "kv8.cuh"
@@ -50,9 +54,11 @@ constexpr int MAX_SPLIT = 12;
 constexpr float P_BITS = 6.f;             // weights are held times 2^6,
 constexpr float P_ROOM = 8.f;             // and may grow by 2^8 before the output is rescaled: below f16's 2^16
 
+// MT > 0: 16 MT rows a warp, padded to the products' rows; MT < 0: 8 NT = -8 MT rows, the products' columns.
 template <int D, int MT, int RW, int NW>
 struct Lay {
-  static constexpr int KW = NW / RW;                      // rings of a CTA, RW warps of 16 MT rows each
+  static constexpr int NT = -MT;
+  static constexpr int KW = NW / RW;                      // rings of a CTA, of RW warps
   static constexpr int PB = KV8_PAGE * D;                 // bytes of a page-head
   static constexpr int PADK = D == 128 ? 16 : 64;
   static constexpr int KREG = 2 * PB + PADK;
@@ -60,16 +66,17 @@ struct Lay {
   static constexpr int CTAS = NW == 8 ? 1 : RW == 2 ? 3 : 2;            // of an SM
   static constexpr int NST = D == 64 || RW == 2 ? 4 : 3;  // tiles of a ring
   static constexpr int RING = NST * STAGE;
-  static constexpr int NR = MT ? 16 * MT * RW : 8;
-  static constexpr int PD = D + (MT ? 8 : 4);             // fp32 row of a partial: O, max, sum, pad
+  static constexpr int NR = RW * (MT > 0 ? 16 * MT : 8 * NT);
+  static constexpr int PD = D + (MT > 0 ? 8 : 4);            // fp32 row of a partial: O, max, sum, pad
   static constexpr int ROWB = PD * 4;
   static constexpr int PART = 0;                          // [KW][NR] rows; the CTA's own result in the first NR
   static constexpr int RECV = KW * NR * ROWB;             // [S][rows per owner], at most NR + 15 rows
   static constexpr int MERGE = RECV + (NR + MAX_SPLIT - 1) * ROWB;
   static constexpr int BODY = KW * RING > MERGE ? KW * RING : MERGE;
-  // With 32 rows a warp the query fragments, the same for all warps, live in shared memory: [MT][D / 16][32 lanes][16 B]
-  static constexpr bool QS = MT > 1;
-  static constexpr int TOTAL = BODY + (QS ? MT * (D / 16) * 512 : 0);
+  // With many rows a warp the query fragments, the same for all warps, live in shared memory: [MT][D / 16][32 lanes][16 B],
+  // [NT][D / 16][32 lanes][8 B]
+  static constexpr bool QS = MT > 1 || NT > 2;
+  static constexpr int TOTAL = BODY + (QS ? (MT > 0 ? MT * 512 : NT * 256) * (D / 16) : 0);
   static_assert(MT == 1 || RW == 1, "the warps share their query rows, or a ring");
   static_assert(STAGE % 16 == 0 && RING % 16 == 0 && ROWB % 16 == 0, "copies land on 16 bytes");
   static_assert(STAGE >= KV8_PAGE * D * 4, "16 bf16 rows of the block fit a stage");
@@ -91,6 +98,11 @@ CS_DEV uint32_t pack_f16(float lo, float hi) {
 CS_DEV uint4 lds128(uint32_t a) {
   uint4 v;
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
+CS_DEV uint2 lds64(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
   return v;
 }
 CS_DEV uint32_t lds32(uint32_t a) {
@@ -149,57 +161,65 @@ CS_DEV void follow_max(State<D, MT>& st, int t, float mx0, float mx1, float (&ba
   }
 }
 
-// Up to eight rows: they are the columns, this lane's 2 c and 2 c + 1, of products whose rows are keys or dimensions.
-template <int D>
-struct State<D, 0> {
-  uint32_t q[D / 16][2];        // of row g: the lane's D / 4 dimensions, four a fragment
-  float f[2];
-  float o[D / 16][4];           // dimensions 16 i + g of the two columns, then 16 i + 8 + g
-  float m[2], l[2];
-  float vref;
+// The same with 8 NT rows, the columns of products whose rows are keys or dimensions; this lane's are 8 t + 2 c and
+// 8 t + 2 c + 1.
+template <int D, int NT>
+struct Cols {
+  uint32_t q[NT > 2 ? 1 : NT][D / 16][2];                  // f16 queries of row 8 t + g: the lane's D / 4 dimensions, four a fragment
+  uint32_t qs;                  // or where they are in shared memory
+  float f[NT][2];               // score factor of a row: its power of two, the softmax scale, log2 e
+  float o[NT][D / 16][4];       // dimensions 16 i + g of the two columns, then 16 i + 8 + g
+  float m[NT][2], l[NT][2];     // reference of the weights (base 2), their sum
+  float vref;                   // o and the weights count in units of this values' scale
   CS_DEV void clear() {
     vref = 0.f;
-    m[0] = m[1] = -INFINITY;
-    l[0] = l[1] = 0.f;
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+    for (int t = 0; t < NT; ++t) {
+      m[t][0] = m[t][1] = -INFINITY;
+      l[t][0] = l[t][1] = 0.f;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) o[t][i][0] = o[t][i][1] = o[t][i][2] = o[t][i][3] = 0.f;
+    }
   }
 };
-template <int D>
-CS_DEV void follow_max(State<D, 0>& st, float mx0, float mx1, float (&base)[2]) {
+
+template <int D, int NT>
+CS_DEV void follow_max(Cols<D, NT>& st, int t, float mx0, float mx1, float (&base)[2]) {
   float mx[2] = {mx0, mx1}, a[2];
   bool moved = false;
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
 #pragma unroll
     for (int x = 4; x < 32; x *= 2) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], x));
-    const float was = st.m[e], now = mx[e] > was + P_ROOM ? mx[e] : was;
+    const float was = st.m[t][e], now = mx[e] > was + P_ROOM ? mx[e] : was;
     moved |= now != was;
-    st.m[e] = now;
+    st.m[t][e] = now;
     base[e] = (now == -INFINITY ? 0.f : now) - P_BITS;
     a[e] = exp2_approx(was - P_BITS - base[e]);
   }
   if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      st.l[e] *= a[e];
+      st.l[t][e] *= a[e];
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) {
-        st.o[i][e] *= a[e];
-        st.o[i][2 + e] *= a[e];
+        st.o[t][i][e] *= a[e];
+        st.o[t][i][2 + e] *= a[e];
       }
     }
   }
 }
-template <int D>
-CS_DEV void raise_unit(State<D, 0>& st, float top) {
+template <int D, int NT>
+CS_DEV void raise_unit(Cols<D, NT>& st, float top) {
   if (top <= st.vref) return;
   const float by = st.vref * kv8_inverse(top);
   st.vref = top;
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i)
+  for (int t = 0; t < NT; ++t)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) st.o[i][e] *= by;
+    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) st.o[t][i][e] *= by;
 }
 // An 8 x 8 matrix of 16-bit numbers, a row in four lanes, turned.
 CS_DEV uint32_t turn8(uint32_t x) {
@@ -336,13 +356,17 @@ CS_DEV void tile(State<D, MT>& st, uint32_t sk, uint32_t sv, const float (&ks)[2
   }
 }
 
-// The same for up to eight rows: keys times rows, then dimensions times rows.  The same loads as above: here tokens
-// 4 (g / 2) + i of page g mod 2 are rows g (i even) and g + 8 (i odd) of product i / 2.
-template <int D, bool MASK>
-CS_DEV void tile(State<D, 0>& st, uint32_t sk, uint32_t sv, const float (&ks)[2], const float (&vs)[2], int n0, int n1, int lane) {
-  using L = Lay<D, 0, 1, 4>;
+// The same with the rows as columns: keys times rows, then dimensions times rows.  The same loads: here tokens
+// 4 (g / 2) + i of page g mod 2 are rows g (i even) and g + 8 (i odd) of the score product i / 2.
+template <int D, int NT, bool MASK>
+CS_DEV void tile(Cols<D, NT>& st, uint32_t sk, uint32_t sv, const float (&ks)[2], const float (&vs)[2], int n0, int n1, int lane) {
+  using L = Lay<D, -NT, 1, 4>;
   const int g = lane >> 2, c = lane & 3;
-  float s[2][4] = {};
+  float s[NT][2][4];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) s[t][j][0] = s[t][j][1] = s[t][j][2] = s[t][j][3] = 0.f;
   const uint32_t ka = sk + (uint32_t)((g & 1) * (L::PB + L::PADK) + (g >> 1) * 4 * D + c * (D / 4));
 #pragma unroll
   for (int x = 0; x < D / 64; ++x) {
@@ -356,44 +380,56 @@ CS_DEV void tile(State<D, 0>& st, uint32_t sk, uint32_t sv, const float (&ks)[2]
       w[i][3] = v.w;
     }
 #pragma unroll
-    for (int y = 0; y < 4; ++y)
+    for (int y = 0; y < 4; ++y) {
+      uint2 q[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) q[t] = L::QS ? lds64(st.qs + (uint32_t)((t * (D / 16) + x * 4 + y) * 256)) : make_uint2(st.q[L::QS ? 0 : t][x * 4 + y][0], st.q[L::QS ? 0 : t][x * 4 + y][1]);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const uint32_t a[4] = {kv8_f16x2(w[2 * j][y]), kv8_f16x2(w[2 * j + 1][y]), kv8_f16x2_hi(w[2 * j][y]), kv8_f16x2_hi(w[2 * j + 1][y])};
-        mma_f16(s[j], a, st.q[x * 4 + y][0], st.q[x * 4 + y][1]);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) mma_f16(s[t][j], a, q[t].x, q[t].y);
       }
+    }
   }
   raise_unit(st, fmaxf(vs[0], vs[1]));
   const float kscale = g & 1 ? ks[1] : ks[0];
   const int k = max((int)(__float_as_uint(g & 1 ? vs[1] : vs[0]) >> 23) - (int)(__float_as_uint(st.vref) >> 23), -60);
   const float ve = (float)k, vi = __uint_as_float((uint32_t)(127 - k) << 23);
   const int have = (g & 1 ? n1 : n0) - 4 * (g >> 1);       // of this lane's four tokens
-  float base[2], mx[2];
+  uint32_t p[NT][2][2];
 #pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    if (MASK) {
+  for (int t = 0; t < NT; ++t) {
+    float base[2], mx[2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (i >= have) s[i >> 1][2 * (i & 1) + e] = -INFINITY;
+    for (int e = 0; e < 2; ++e) {
+      if (MASK) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (i >= have) s[t][i >> 1][2 * (i & 1) + e] = -INFINITY;
+      }
+      // (NaN, as of -inf and 0, does not count)
+      mx[e] = fmaxf(fmaxf(s[t][0][e], s[t][0][2 + e]), fmaxf(s[t][1][e], s[t][1][2 + e])) * (st.f[t][e] * kscale);
     }
-    mx[e] = fmaxf(fmaxf(s[0][e], s[0][2 + e]), fmaxf(s[1][e], s[1][2 + e])) * (st.f[e] * kscale);      // (NaN, as of -inf and 0, does not count)
-  }
-  follow_max(st, mx[0], mx[1], base);
-  uint32_t t[4];
-  {
+    follow_max(st, t, mx[0], mx[1], base);
     float x[4][2];
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const float f = st.f[e] * kscale, to = ve - base[e];
+      const float f = st.f[t][e] * kscale, to = ve - base[e];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        x[i][e] = exp2_approx(fmaf(s[i >> 1][2 * (i & 1) + e], f, to));
+        x[i][e] = exp2_approx(fmaf(s[t][i >> 1][2 * (i & 1) + e], f, to));
         if (MASK && i >= have) x[i][e] = 0.f;
       }
-      st.l[e] = fmaf((x[0][e] + x[1][e]) + (x[2][e] + x[3][e]), vi, st.l[e]);
+      st.l[t][e] = fmaf((x[0][e] + x[1][e]) + (x[2][e] + x[3][e]), vi, st.l[t][e]);
     }
+    uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) t[i] = turn8(pack_f16(x[i][0], x[i][1]));  // row g's weights of token 4 c + i of the two pages
+    for (int i = 0; i < 4; ++i) w[i] = turn8(pack_f16(x[i][0], x[i][1]));  // row g's weights of token 4 c + i of the two pages
+    p[t][0][0] = __byte_perm(w[0], w[1], 0x5410);
+    p[t][0][1] = __byte_perm(w[2], w[3], 0x5410);
+    p[t][1][0] = __byte_perm(w[0], w[1], 0x7632);
+    p[t][1][1] = __byte_perm(w[2], w[3], 0x7632);
   }
   uint32_t keep[2] = {0xffffffffu, 0xffffffffu};           // cells behind a page's last token read as 0
   if (MASK) {
@@ -405,8 +441,7 @@ CS_DEV void tile(State<D, 0>& st, uint32_t sk, uint32_t sv, const float (&ks)[2]
   }
   const uint32_t va = sv + (uint32_t)(g * KV8_PAGE + c * 4);
 #pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    const uint32_t b0 = __byte_perm(t[0], t[1], e ? 0x7632 : 0x5410), b1 = __byte_perm(t[2], t[3], e ? 0x7632 : 0x5410);
+  for (int e = 0; e < 2; ++e)
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
       uint32_t w0 = lds32(va + (uint32_t)(e * L::PB + i * 16 * KV8_PAGE)), w1 = lds32(va + (uint32_t)(e * L::PB + (i * 16 + 8) * KV8_PAGE));
@@ -415,9 +450,9 @@ CS_DEV void tile(State<D, 0>& st, uint32_t sk, uint32_t sv, const float (&ks)[2]
         w1 &= keep[e];
       }
       const uint32_t a[4] = {kv8_f16x2(w0), kv8_f16x2(w1), kv8_f16x2_hi(w0), kv8_f16x2_hi(w1)};
-      mma_f16(st.o[i], a, b0, b1);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) mma_f16(st.o[t][i], a, p[t][e][0], p[t][e][1]);
     }
-  }
 }
 
 template <int D, int MT, int RW, int NW, bool SEL>
@@ -531,34 +566,67 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
   if (KW - 1 - kw < block_groups) issue_block((KW - 1 - kw) * 16);
 
   // ---------------------------------------------------------------- queries
-  State<D, MT> st;
-  constexpr int MR = MT ? MT : 1, RR = MT ? 2 : 1;         // (eight rows: row g only)
+  std::conditional_t<(MT > 0), State<D, (MT > 0 ? MT : 1)>, Cols<D, (MT > 0 ? 1 : L::NT)>> st;
+  st.clear();
+  st.qs = smem_u32(smem + L::BODY) + lane * (MT > 0 ? 16 : 8);
+  auto row_of = [&](int x) { return row0 + min(x, nr - 1); };
+  auto q_row = [&](int t) {                                // row 8 t + g, this lane's dimensions
+    const int x = 8 * t + g, row = row_of(x);
+    const int j = SEL ? jj : row / p.G, head = h * p.G + (SEL ? row : row % p.G);
+    return x < nr ? p.q.p + b * p.q.batch + j * p.q.row + (size_t)head * D + c * (D / 4) : nullptr;
+  };
+  constexpr int MR = MT > 0 ? MT : 1;
   const __nv_bfloat16* qrow[MR][2];
   int lim[MR][2];                                          // last block row that the query row sees
+  if constexpr (MT > 0) {
 #pragma unroll
-  for (int t = 0; t < MR; ++t)
+    for (int t = 0; t < MT; ++t)
 #pragma unroll
-    for (int r = 0; r < RR; ++r) {
-      const int x = (rw * MT + t) * 16 + g + 8 * r;
-      const int row = row0 + min(x, nr - 1);
-      const int j = SEL ? jj : row / p.G, head = h * p.G + (SEL ? row : row % p.G);
-      qrow[t][r] = x < nr ? p.q.p + b * p.q.batch + j * p.q.row + (size_t)head * D + c * (D / 4) : nullptr;
-      lim[t][r] = p.block_full ? p.R - 1 : j;
-    }
-  if constexpr (MT == 0) {                                 // (of the columns)
+      for (int r = 0; r < 2; ++r) {
+        const int x = (rw * MT + t) * 16 + g + 8 * r, row = row_of(x);
+        const int j = SEL ? jj : row / p.G, head = h * p.G + (SEL ? row : row % p.G);
+        qrow[t][r] = x < nr ? p.q.p + b * p.q.batch + j * p.q.row + (size_t)head * D + c * (D / 4) : nullptr;
+        lim[t][r] = p.block_full ? p.R - 1 : j;
+      }
 #pragma unroll
-    for (int e = 0; e < 2; ++e) lim[0][e] = p.block_full ? p.R - 1 : SEL ? jj : (row0 + min(2 * c + e, nr - 1)) / p.G;
-  }
-  st.clear();
+    for (int t = 0; t < MT; ++t)
 #pragma unroll
-  for (int t = 0; t < MR; ++t)
+      for (int r = 0; r < 2; ++r) {
+        uint4 w[D / 32];
+        float amax = 0.f;
 #pragma unroll
-    for (int r = 0; r < RR; ++r) {
+        for (int i = 0; i < D / 32; ++i) {
+          w[i] = qrow[t][r] ? *reinterpret_cast<const uint4*>(qrow[t][r] + i * 8) : make_uint4(0u, 0u, 0u, 0u);
+          const uint32_t ww[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+            amax = fmaxf(amax, fmaxf(kv8_finite_abs(__uint_as_float(ww[y] << 16)), kv8_finite_abs(__uint_as_float(ww[y] & 0xffff0000u))));
+        }
+        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+        const float sc = kv8_scale127(amax), inv = kv8_inverse(sc);      // |q / sc| <= 127
+        st.f[t][r] = sc * p.scale_log2;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+          const uint32_t ww[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {      // pairs of the lane's dimensions 8 i + 2 y: fragment 2 i + y / 2, half y & 1
+            const uint32_t v = pack_f16(__uint_as_float(ww[y] << 16) * inv, __uint_as_float(ww[y] & 0xffff0000u) * inv);
+            const int fr = 2 * i + (y >> 1), z = r + 2 * (y & 1);
+            if (!L::QS) st.q[L::QS ? 0 : fr][z] = v;
+            else if (warp == 0) *reinterpret_cast<uint32_t*>(smem + L::BODY + (t * (D / 16) + fr) * 512 + lane * 16 + z * 4) = v;
+          }
+        }
+      }
+  } else {
+#pragma unroll
+    for (int t = 0; t < L::NT; ++t) {
+      const __nv_bfloat16* src = q_row(t);
       uint4 w[D / 32];
       float amax = 0.f;
 #pragma unroll
       for (int i = 0; i < D / 32; ++i) {
-        w[i] = qrow[t][r] ? *reinterpret_cast<const uint4*>(qrow[t][r] + i * 8) : make_uint4(0u, 0u, 0u, 0u);
+        w[i] = src ? *reinterpret_cast<const uint4*>(src + i * 8) : make_uint4(0u, 0u, 0u, 0u);
         const uint32_t ww[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
 #pragma unroll
         for (int y = 0; y < 4; ++y)
@@ -566,27 +634,27 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
       }
       amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
       amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-      const float sc = kv8_scale127(amax), inv = kv8_inverse(sc);      // |q / sc| <= 127
-      if constexpr (MT == 0) {
+      const float sc = kv8_scale127(amax), inv = kv8_inverse(sc);        // |q / sc| <= 127
 #pragma unroll
-        for (int e = 0; e < 2; ++e) st.f[e] = __shfl_sync(0xffffffffu, sc, 8 * c + 4 * e) * p.scale_log2;
-      } else {
-        st.f[t][r] = sc * p.scale_log2;
-      }
+      for (int e = 0; e < 2; ++e) st.f[t][e] = __shfl_sync(0xffffffffu, sc, 8 * c + 4 * e) * p.scale_log2;
 #pragma unroll
       for (int i = 0; i < D / 32; ++i) {
         const uint32_t ww[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+        uint32_t v[4];
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {      // pairs of the lane's dimensions 8 i + 2 y: fragment 2 i + y / 2, half y & 1
-          const uint32_t v = pack_f16(__uint_as_float(ww[y] << 16) * inv, __uint_as_float(ww[y] & 0xffff0000u) * inv);
-          const int fr = 2 * i + (y >> 1), z = r + 2 * (y & 1);
-          if constexpr (MT == 0) st.q[fr][y & 1] = v;
-          else if (!L::QS) st.q[L::QS ? 0 : fr][z] = v;
-          else if (warp == 0) *reinterpret_cast<uint32_t*>(smem + L::BODY + (t * (D / 16) + fr) * 512 + lane * 16 + z * 4) = v;
+        for (int y = 0; y < 4; ++y) v[y] = pack_f16(__uint_as_float(ww[y] << 16) * inv, __uint_as_float(ww[y] & 0xffff0000u) * inv);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {        // the lane's dimensions 8 i + 4 y ..
+          if (!L::QS) {
+            st.q[L::QS ? 0 : t][2 * i + y][0] = v[2 * y];
+            st.q[L::QS ? 0 : t][2 * i + y][1] = v[2 * y + 1];
+          } else if (warp == 0) {
+            *reinterpret_cast<uint2*>(smem + L::BODY + (t * (D / 16) + 2 * i + y) * 256 + lane * 8) = make_uint2(v[2 * y], v[2 * y + 1]);
+          }
         }
       }
     }
-  if constexpr (MT != 0) st.qs = smem_u32(smem + L::BODY) + lane * 16;
+  }
   if (L::QS) __syncthreads();
 
   // ---------------------------------------------------------------- the block's own rows
@@ -612,34 +680,53 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
     for (int o = 16; o > 0; o >>= 1) vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, o));
     raise_unit(st, kv8_scale_of(vmax));
     const float iv = kv8_inverse(st.vref);
-    if constexpr (MT == 0) {
-      float s[4] = {};
+    if constexpr (MT < 0) {
+      float s[L::NT][4];
+      const __nv_bfloat16* src[L::NT];
+#pragma unroll
+      for (int t = 0; t < L::NT; ++t) {
+        s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.f;
+        src[t] = q_row(t);
+      }
 #pragma unroll
       for (int x = 0; x < D / 32; ++x) {
         const uint8_t* kr = kbuf + g * (2 * D) + ((c * (D / 32) + x) ^ g) * 16;
         const uint4 w = *reinterpret_cast<const uint4*>(kr), w8 = *reinterpret_cast<const uint4*>(kr + 8 * 2 * D);
-        const uint4 qv = qrow[0][0] ? *reinterpret_cast<const uint4*>(qrow[0][0] + x * 8) : make_uint4(0u, 0u, 0u, 0u);
         const uint32_t a0[4] = {w.x, w8.x, w.y, w8.y}, a1[4] = {w.z, w8.z, w.w, w8.w};
-        mma_16816(s, a0, qv.x, qv.y);
-        mma_16816(s, a1, qv.z, qv.w);
-      }
-      float base[2];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] = k0 + g + 8 * (e >> 1) <= lim[0][e & 1] ? s[e] * p.scale_log2 : -INFINITY;
-      follow_max(st, fmaxf(s[0], s[2]), fmaxf(s[1], s[3]), base);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        s[e] = exp2_approx(s[e] - base[e & 1]);
-        st.l[e & 1] += s[e];
+        for (int t = 0; t < L::NT; ++t) {
+          const uint4 qv = src[t] ? *reinterpret_cast<const uint4*>(src[t] + x * 8) : make_uint4(0u, 0u, 0u, 0u);
+          mma_16816(s[t], a0, qv.x, qv.y);
+          mma_16816(s[t], a1, qv.z, qv.w);
+        }
       }
-      const uint32_t b0 = turn8(pack_bf16(s[0] * iv, s[1] * iv)), b1 = turn8(pack_bf16(s[2] * iv, s[3] * iv));
+      uint32_t pf[L::NT][2];
+#pragma unroll
+      for (int t = 0; t < L::NT; ++t) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          // row g + 8 (e / 2) of the keys, this lane's column e mod 2: the last block row that its query row sees
+          const int last = p.block_full ? p.R - 1 : SEL ? jj : row_of(8 * t + 2 * c + (e & 1)) / p.G;
+          s[t][e] = k0 + g + 8 * (e >> 1) <= last ? s[t][e] * p.scale_log2 : -INFINITY;
+        }
+        float base[2];
+        follow_max(st, t, fmaxf(s[t][0], s[t][2]), fmaxf(s[t][1], s[t][3]), base);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s[t][e] = exp2_approx(s[t][e] - base[e & 1]);
+          st.l[t][e & 1] += s[t][e];
+        }
+        pf[t][0] = turn8(pack_bf16(s[t][0] * iv, s[t][1] * iv));
+        pf[t][1] = turn8(pack_bf16(s[t][2] * iv, s[t][3] * iv));
+      }
       const int key = (lane & 7) + (lane >> 4) * 8;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) {
         const int ch = 2 * i + ((lane >> 3) & 1);
         uint32_t a[4];
         ldsm_x4_t(smem_u32(vbuf) + (uint32_t)(key * (2 * D) + ((ch ^ (key & 7)) * 16)), a[0], a[1], a[2], a[3]);
-        mma_16816(st.o[i], a, b0, b1);
+#pragma unroll
+        for (int t = 0; t < L::NT; ++t) mma_16816(st.o[t][i], a, pf[t][0], pf[t][1]);
       }
     } else {
       float s[MT][2][4];
@@ -720,12 +807,12 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
     const float vs[2] = {__shfl_sync(0xffffffffu, scale_c.y, at), __shfl_sync(0xffffffffu, scale_c.y, at + 1)};
     const uint32_t sk = smem_u32(ring + sg * L::STAGE);
     if ((whole >> at & 3u) == 3u) {
-      if constexpr (MT == 0) tile<D, false>(st, sk, sk + L::KREG, ks, vs, KV8_PAGE, KV8_PAGE, lane);
+      if constexpr (MT < 0) tile<D, L::NT, false>(st, sk, sk + L::KREG, ks, vs, KV8_PAGE, KV8_PAGE, lane);
       else tile<D, MT, false>(st, sk, sk + L::KREG, ks, vs, KV8_PAGE, KV8_PAGE, lane);
     } else {
       const int n0 = __shfl_sync(0xffffffffu, count_c, at), n1 = __shfl_sync(0xffffffffu, count_c, at + 1);
       if (n0 + n1 > 0) {
-        if constexpr (MT == 0) tile<D, true>(st, sk, sk + L::KREG, ks, vs, n0, n1, lane);
+        if constexpr (MT < 0) tile<D, L::NT, true>(st, sk, sk + L::KREG, ks, vs, n0, n1, lane);
         else tile<D, MT, true>(st, sk, sk + L::KREG, ks, vs, n0, n1, lane);
       }
     }
@@ -743,20 +830,22 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
   {
     const float unit = st.vref * exp2f(-P_BITS), one = exp2f(-P_BITS);
     float* mypart = part + (kw * L::NR + rw * 16) * L::PD;
-    if constexpr (MT == 0) {
+    if constexpr (MT < 0) {
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float* row = mypart + (2 * c + e) * L::PD;
+      for (int t = 0; t < L::NT; ++t)
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-          row[16 * i + g] = st.o[i][e] * unit;
-          row[16 * i + 8 + g] = st.o[i][2 + e] * unit;
+        for (int e = 0; e < 2; ++e) {
+          float* row = mypart + (8 * t + 2 * c + e) * L::PD;
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) {
+            row[16 * i + g] = st.o[t][i][e] * unit;
+            row[16 * i + 8 + g] = st.o[t][i][2 + e] * unit;
+          }
+          float l = st.l[t][e];
+#pragma unroll
+          for (int x = 4; x < 32; x *= 2) l += __shfl_xor_sync(0xffffffffu, l, x);
+          if (g == 0) *reinterpret_cast<float2*>(row + D) = make_float2(st.m[t][e], l * one);
         }
-        float l = st.l[e];
-#pragma unroll
-        for (int x = 4; x < 32; x *= 2) l += __shfl_xor_sync(0xffffffffu, l, x);
-        if (g == 0) *reinterpret_cast<float2*>(row + D) = make_float2(st.m[e], l * one);
-      }
     } else {
 #pragma unroll
       for (int t = 0; t < MT; ++t)
@@ -931,8 +1020,9 @@ struct Variant {
   static Split split(const Params& p, int tiles) {
     return split_of(units(p), tiles, L::KW,
                     MT == 2   ? Cost{10.0, 1.32, 1.96}
-                    : MT == 0 ? (NW == 8 ? Cost{6.8, 1.1, 1.3} : Cost{5.5, 0.79, 1.45})
-                    : RW == 2 ? (NW == 8 ? Cost{7.3, 1.15, 1.15} : Cost{6.8, 0.88, 1.5})
+                    : MT == -1 ? (NW == 8 ? Cost{6.8, 1.1, 1.3} : Cost{5.5, 0.79, 1.45})
+                    : MT == -3 ? Cost{8.3, 1.2, 1.75}
+                    : RW == 2 ? (NW == 8 ? Cost{7.3, 1.15, 1.15} : Cost{6.8, 0.88, 2.2})
                               : (NW == 8 ? Cost{7.3, 1.27, 1.27} : Cost{6.0, 0.95, 1.45}),
                     resident);
   }
@@ -975,16 +1065,18 @@ cudaError_t pick(Params& p, int pages, cudaStream_t stream) {
   }
   const int tiles = (pages + 1) / 2;
   if (p.rows <= 8) {
-    const Split four = Variant<D, 0, 1, 4, SEL>::split(p, tiles), eight = Variant<D, 0, 1, 8, SEL>::split(p, tiles);
-    return four.us < eight.us ? Variant<D, 0, 1, 4, SEL>::launch(p, four.S, stream) : Variant<D, 0, 1, 8, SEL>::launch(p, eight.S, stream);
+    const Split four = Variant<D, -1, 1, 4, SEL>::split(p, tiles), eight = Variant<D, -1, 1, 8, SEL>::split(p, tiles);
+    return four.us < eight.us ? Variant<D, -1, 1, 4, SEL>::launch(p, four.S, stream) : Variant<D, -1, 1, 8, SEL>::launch(p, eight.S, stream);
   }
   if (p.rows <= 16) {
     const Split four = Variant<D, 1, 1, 4, SEL>::split(p, tiles), eight = Variant<D, 1, 1, 8, SEL>::split(p, tiles);
     return four.us < eight.us ? Variant<D, 1, 1, 4, SEL>::launch(p, four.S, stream) : Variant<D, 1, 1, 8, SEL>::launch(p, eight.S, stream);
   }
-  const Split wide = Variant<D, 2, 1, 4, SEL>::split(p, tiles), four = Variant<D, 1, 2, 4, SEL>::split(p, tiles);
+  const Split wide = p.rows <= 24 ? Variant<D, -3, 1, 4, SEL>::split(p, tiles) : Variant<D, 2, 1, 4, SEL>::split(p, tiles);
+  const Split four = Variant<D, 1, 2, 4, SEL>::split(p, tiles);
   const Split eight = Variant<D, 1, 2, 8, SEL>::split(p, tiles);
-  if (wide.us < four.us && wide.us < eight.us) return Variant<D, 2, 1, 4, SEL>::launch(p, wide.S, stream);
+  if (wide.us < four.us && wide.us < eight.us)
+    return p.rows <= 24 ? Variant<D, -3, 1, 4, SEL>::launch(p, wide.S, stream) : Variant<D, 2, 1, 4, SEL>::launch(p, wide.S, stream);
   return four.us < eight.us ? Variant<D, 1, 2, 4, SEL>::launch(p, four.S, stream) : Variant<D, 1, 2, 8, SEL>::launch(p, eight.S, stream);
 }
 
