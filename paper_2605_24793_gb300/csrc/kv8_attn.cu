@@ -6,16 +6,17 @@
 // and no ring waits for another until the end.  A ring's warps bring its tiles in together, asynchronously, and each puts
 // its own rows to them.  Variants, chosen by the estimates below:
 //   columns: the query rows are the products' columns, eight at a time, keys and values their rows, so that up to 8 and 17
-//   to 24 rows are padded less than by 16.  A warp a ring, four to a CTA and two CTAs an SM; up to 8 rows also eight to a
-//   CTA, which fills the SMs that a few clusters get.  Up to 8 rows: one user at 4096 tokens 7.5 us with four warps, 7.9
-//   with eight, 8.3 with padded rows; at 32768 24.3, 20.2 and 26.5; 128 selected pages for each of 128 rows 91, padded
-//   103.  At 24 rows: batch 16 at 2048 to 8192 tokens 52 us, padded 59; batch 64 at 8192 to 32768 484, padded 538;
+//   to 24 rows are padded less than by 16.  A warp a ring and two CTAs an SM: six warps with rings of two tiles up to 8
+//   rows, four with rings of three at 24 (as registers allow).  Up to 8 rows, with six warps, four, eight (one CTA an SM)
+//   and padded: one user at 4096 tokens 7.3, 7.5, 7.9, 8.3 us, at 32768 20.5, 24.3, 20.2, 26.5; 128 selected pages for
+//   each of 128 rows 83, 91, -, 103.  At 24 rows: batch 16 at 2048 to 8192 tokens 52 us, padded 59; batch 64 at 8192 to
+//   32768 484, padded 538;
 //   rows: the query rows are the products' rows, by 16, which is as good where they fill them and has fewer shuffles: batch
-//   64 at 32 rows 538 us for 564, at 12 rows one user 8.3 for 9.2.  Up to 16 a warp a ring, as above (rings of three
-//   tiles: with three CTAs and rings of two batch 64 at 8192 to 32768 tokens took 460 us for 395); up to 32 a warp of 32
-//   rows a ring (each code converted once), or two of 16 (half the registers, shorter steps) with four warps and three
-//   CTAs an SM or with eight.  A warp of 32, two of four, two of eight at 32 rows: one user at 4096 tokens 12.1, 11.7,
-//   10.4 us; batch 32 at 2048 to 16384 138, 157, 164; batch 64 at 8192 to 32768 537, 627, 706.
+//   64 at 32 rows 538 us for 564, at 12 rows one user 8.3 for 9.2.  Up to 16 a warp a ring, four warps and two CTAs an SM
+//   or eight and one (long contexts of few users: one user at 32768 tokens 26.5 us and 22.3, at 4096 8.3 and 9.0); up to
+//   32 a warp of 32 rows a ring (each code converted once), or two of 16 (half the registers, shorter steps) with four
+//   warps and three CTAs an SM or with eight.  A warp of 32, two of four, two of eight at 32 rows: one user at 4096 tokens
+//   12.1, 11.7, 10.4 us; batch 32 at 2048 to 16384 138, 157, 164; batch 64 at 8192 to 32768 537, 627, 706.
 // More rows go to the tcgen05 kernel (kv8_attn_tc.cu): at 64 rows two groups of 32 here took 95 us where that takes 70
 // (batch 16, 2048 to 8192 tokens), at 40 91 and 70, at 32 66 and 68; batch 64 540 and 756 at 32 rows, 1011 and 759 at 40.
 //
@@ -64,7 +65,7 @@ struct Lay {
   static constexpr int KREG = 2 * PB + PADK;
   static constexpr int STAGE = KREG + 2 * PB;
   static constexpr int CTAS = NW == 8 ? 1 : RW == 2 ? 3 : 2;            // of an SM
-  static constexpr int NST = D == 64 || RW == 2 ? 4 : 3;  // tiles of a ring
+  static constexpr int NST = D == 64 || RW == 2 ? 4 : NW == 6 ? 2 : 3;  // tiles of a ring
   static constexpr int RING = NST * STAGE;
   static constexpr int NR = RW * (MT > 0 ? 16 * MT : 8 * NT);
   static constexpr int PD = D + (MT > 0 ? 8 : 4);            // fp32 row of a partial: O, max, sum, pad
@@ -1020,7 +1021,7 @@ struct Variant {
   static Split split(const Params& p, int tiles) {
     return split_of(units(p), tiles, L::KW,
                     MT == 2   ? Cost{10.0, 1.32, 1.96}
-                    : MT == -1 ? (NW == 8 ? Cost{6.8, 1.1, 1.3} : Cost{5.5, 0.79, 1.45})
+                    : MT == -1 ? Cost{5.5, 0.95, 2.2}
                     : MT == -3 ? Cost{8.3, 1.2, 1.75}
                     : RW == 2 ? (NW == 8 ? Cost{7.3, 1.15, 1.15} : Cost{6.8, 0.88, 2.2})
                               : (NW == 8 ? Cost{7.3, 1.27, 1.27} : Cost{6.0, 0.95, 1.45}),
@@ -1064,10 +1065,7 @@ cudaError_t pick(Params& p, int pages, cudaStream_t stream) {
     return launch_kv8_attn_tc(p, D, s.S, stream);
   }
   const int tiles = (pages + 1) / 2;
-  if (p.rows <= 8) {
-    const Split four = Variant<D, -1, 1, 4, SEL>::split(p, tiles), eight = Variant<D, -1, 1, 8, SEL>::split(p, tiles);
-    return four.us < eight.us ? Variant<D, -1, 1, 4, SEL>::launch(p, four.S, stream) : Variant<D, -1, 1, 8, SEL>::launch(p, eight.S, stream);
-  }
+  if (p.rows <= 8) return Variant<D, -1, 1, 6, SEL>::launch(p, Variant<D, -1, 1, 6, SEL>::split(p, tiles).S, stream);
   if (p.rows <= 16) {
     const Split four = Variant<D, 1, 1, 4, SEL>::split(p, tiles), eight = Variant<D, 1, 1, 8, SEL>::split(p, tiles);
     return four.us < eight.us ? Variant<D, 1, 1, 4, SEL>::launch(p, four.S, stream) : Variant<D, 1, 1, 8, SEL>::launch(p, eight.S, stream);
