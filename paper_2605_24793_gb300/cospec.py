@@ -577,7 +577,7 @@ class Kv8Pool:
             _need(tuple(summary_scale.shape) == (L, N, H), "summary_scale must be [L, pages, Hkv]")
         self.k, self.v, self.scale, self.summary, self.summary_scale = k, v, scale, summary, summary_scale
         self.layers, self.num_pages, self.kv_heads, self.head_dim = L, N, H, D
-        self.device = k.device
+        self.device, self.index = k.device, k.get_device()
         for t in (v, scale, summary, summary_scale):
             _need(t is None or t.device == k.device, "a pool's arrays must be on one device")
         self.c = Kv8PoolC(L, N, H, D, *(0 if t is None else t.data_ptr() for t in (k, v, scale, summary, summary_scale)))
@@ -626,9 +626,10 @@ def _rows_ref(t: torch.Tensor, name: str, shape):
     dense, and returns a reference to their strides (cospec_kv8_strides)."""
     if t.dtype is not _BF16:
         raise TypeError(f"{name}: expected {_BF16}, got {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    key = (t.shape, t.stride())
+    n = t.shape
+    if n != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(n)}")
+    key = (n, t.stride())
     ref = _strides_kept.get(key)
     return ref if ref is not None else _new_strides(t, name, key)
 
@@ -651,10 +652,14 @@ def _dense(t: torch.Tensor, name: str, dtype, shape) -> None:
 
 
 def _on_device(dev: int, *tensors) -> None:
+    """Names the tensor that is not on the current device (the calls compare the indices themselves)."""
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError(f"a tensor is on {t.device}, but the current device is cuda:{dev}" if t.is_cuda
                              else "every tensor must be a CUDA tensor")
+
+
+_current = torch._C._cuda_getDevice
 
 
 def _stream_ptr(stream, dev: int) -> int:
@@ -709,8 +714,10 @@ def _launch_append(pool_ref, first, L, shape, rope, q, k, v, vs, page_table, sta
         _dense(q_out, "q_out", _BF16, q.shape)
     if k_out is not None:
         _dense(k_out, "k_out", _BF16, shape)
-    dev = torch._C._cuda_getDevice()
-    _on_device(dev, k, v, q, q_out, k_out, page_table, start, rows, None if rope is None else rope.cos)
+    dev = _current()
+    for t in (k, v, q, q_out, k_out, page_table, start, rows, None if rope is None else rope.cos):
+        if t is not None and t.get_device() != dev:
+            _on_device(dev, t)
     _check((_lib or load_library()).cospec_kv8_append(
         pool_ref, first, L, B, R, Hq, None if rope is None else rope.ref, _at(q), qs, k.data_ptr(), ks, _at(v), vs, _at(page_table),
         0 if page_table is None else page_table.shape[1], start.data_ptr(), _at(rows), _at(q_out), _at(k_out), _stream_ptr(stream, dev)))
@@ -719,9 +726,12 @@ def _launch_append(pool_ref, first, L, shape, rope, q, k, v, vs, page_table, sta
 def _kv8_dims(q, pool: Kv8Pool, layer: int, page_table, ctx_len, softmax_scale=0.0, flags=0):
     """The call's checked geometry: q's shape and a reference to cospec_attn_dims."""
     shape, table = q.shape, page_table.shape
-    _need(len(shape) == 4 and shape[3] == pool.head_dim, "q must be [B, R, Hq, D] with the pool's D")
-    _need(0 <= layer < pool.layers, "layer outside the pool")
-    _need(len(table) == 2, "page_table must be [B, max_pages]")
+    if len(shape) != 4 or shape[3] != pool.head_dim:
+        raise ValueError("q must be [B, R, Hq, D] with the pool's D")
+    if not 0 <= layer < pool.layers:
+        raise ValueError("layer outside the pool")
+    if len(table) != 2:
+        raise ValueError("page_table must be [B, max_pages]")
     B = shape[0]
     _dense(page_table, "page_table", _I32, (B, table[1]))
     _dense(ctx_len, "ctx_len", _I32, (B,))
@@ -739,8 +749,9 @@ def kv8_select(q, pool: Kv8Pool, layer: int, page_table, ctx_len, sel, sink: int
     _need(pool.summary is not None, "the pool has no summaries")
     pages = sel.shape[-1]
     _dense(sel, "sel", _I32, (shape[0], shape[1], pool.kv_heads, pages))
-    dev = torch._C._cuda_getDevice()
-    _on_device(dev, q, page_table, ctx_len, sel, pool.k)
+    dev = _current()
+    if not dev == q.get_device() == page_table.get_device() == ctx_len.get_device() == sel.get_device() == pool.index:
+        _on_device(dev, q, page_table, ctx_len, sel, pool.k)
     _check((_lib or load_library()).cospec_kv8_select(dims, pool.ref, layer, q.data_ptr(), qs, page_table.data_ptr(), ctx_len.data_ptr(),
                                                       pages, int(sink), int(recent), sel.data_ptr(), _stream_ptr(stream, dev)))
     return sel
@@ -760,8 +771,10 @@ def kv8_attn(q, k_blk, v_blk, pool: Kv8Pool, layer: int, page_table, ctx_len, ou
     if sel is not None:
         pages = sel.shape[-1]
         _dense(sel, "sel", _I32, (shape[0], shape[1], pool.kv_heads, pages))
-    dev = torch._C._cuda_getDevice()
-    _on_device(dev, q, k_blk, v_blk, page_table, ctx_len, sel, out, pool.k)
+    dev = _current()
+    if not (dev == q.get_device() == k_blk.get_device() == v_blk.get_device() == page_table.get_device() == ctx_len.get_device()
+            == out.get_device() == pool.index) or (sel is not None and sel.get_device() != dev):
+        _on_device(dev, q, k_blk, v_blk, page_table, ctx_len, sel, out, pool.k)
     _check((_lib or load_library()).cospec_kv8_attn(
         dims, int(max_ctx), pool.ref, layer, q.data_ptr(), qs, k_blk.data_ptr(), ks, v_blk.data_ptr(), vs, page_table.data_ptr(),
         ctx_len.data_ptr(), _at(sel), pages, out.data_ptr(), _stream_ptr(stream, dev)))
