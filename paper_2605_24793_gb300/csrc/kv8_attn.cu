@@ -37,6 +37,10 @@
 // The block's keys and values (bf16, up to 64) go 16 at a time to the warps of the cluster's last CTA, on
 // bf16 operands.  The warps' partial (max, sum, output) meet in shared memory, the CTAs' in
 // distributed shared memory, each CTA finishing a slice of the rows.
+//
+// One row at batch 64, 8192 to 32768 tokens (dimension 128, 8 KV heads): 400 us, 6.7 TB/s, the memory's rate.  32 rows
+// there: 538 us, 5.0 TB/s, the products' rate (a tile's 192 take 390 of its 500 cycles an SM).  One user is latency: at
+// 4096 tokens 2.5 us to the first tile, 1.3 a tile of 24 rows, 2 to 3 for the parts.
 #include <math.h>
 
 #include <type_traits>

@@ -17,6 +17,10 @@
 // weight's exponent, relative to the largest seen by the group; weights are held times 2^6 in f16 and the
 // reference moves when a score exceeds it by 2^8, as on mma.sync.  The block's bf16 keys and values come
 // to f16 by one power of two each: 2^-25 of the block's largest value is what can be lost.
+//
+// 104 rows, batch 16 at 2048 to 8192 tokens: 76 us; a tile takes a CTA 1.05 us alone and 1.4 with all SMs at work: shared
+// memory carries each code in, to the converting warps, out as f16 and to the tensor core.  Codes loaded to registers past
+// the ring, behind prefetches to L2, took 86 us.
 #include <math.h>
 
 #include "cospec_internal.h"
