@@ -15,8 +15,8 @@
 // sums of at most 16 codes), so the codes, scales and summaries are the same on every run and in any
 // other program that follows the definition in 32 bits.
 //
-// Bound by instructions and their latencies at 17 warps an SM: 36 layers x 16 sequences x 8 rows 22.9 us (issue slots
-// 46 % busy; more blocks an SM need fewer registers: 23.4 to 30 us), 4096 rows x 2 layers with queries 47.5 us, 0.62
+// Bound by instructions and their latencies at 17 warps an SM: 36 layers x 16 sequences x 8 rows 22.3 us (issue slots
+// 46 % busy; more blocks an SM need fewer registers: 23.4 to 30 us), 4096 rows x 2 layers with queries 42.9 us, 0.69
 // of the copy rate; one row of a small layer 3 us.
 #include "cospec_internal.h"
 #include "kv8.cuh"
@@ -35,8 +35,9 @@ struct Geometry {
   int q_groups;           // warps of a query row
 };
 
-constexpr int QU = 4;     // heads in flight per lane
-constexpr int UR = 4;     // rows in flight per lane
+constexpr int QU = 8;     // heads in flight per lane (4096 rows of 32 heads: 2 59.7, 4 47.6, 8 42.9, 16 44.6 us)
+constexpr int UR = 4;     // rows in flight per lane,
+constexpr int UO = 8;     // and older codes' rows
 constexpr float FINITE = 3.4028235e38f;
 
 // Four products and sums, each rounded by itself: y = x c - o s in the low half, x c + o s in the high one.
@@ -316,13 +317,13 @@ __global__ void __launch_bounds__(WARPS * 32, 5)
     for (int e = 0; e < 4; ++e) sum[e] += checked && y[e] != y[e] ? 0.f : y[e];
   };
   if (sums || moved != 1.f) {
-    for (int i0 = 0; i0 < first; i0 += UR) {
-      uint32_t w[UR];
+    for (int i0 = 0; i0 < first; i0 += UO) {
+      uint32_t w[UO];
 #pragma unroll
-      for (int i = 0; i < UR; ++i)
+      for (int i = 0; i < UO; ++i)
         if (i0 + i < first) w[i] = *reinterpret_cast<const uint32_t*>(dst + (i0 + i) * D);
 #pragma unroll
-      for (int i = 0; i < UR; ++i) {
+      for (int i = 0; i < UO; ++i) {
         if (i0 + i >= first) break;
         if (moved != 1.f) {
           w[i] = move(w[i]);
