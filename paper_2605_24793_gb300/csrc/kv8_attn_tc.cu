@@ -18,9 +18,11 @@
 // reference moves when a score exceeds it by 2^8, as on mma.sync.  The block's bf16 keys and values come
 // to f16 by one power of two each: 2^-25 of the block's largest value is what can be lost.
 //
-// 104 rows, batch 16 at 2048 to 8192 tokens: 76 us; a tile takes a CTA 1.05 us alone and 1.4 with all SMs at work: shared
-// memory carries each code in, to the converting warps, out as f16 and to the tensor core.  Codes loaded to registers past
-// the ring, behind prefetches to L2, took 86 us.
+// 104 rows, batch 16 at 2048 to 8192 tokens: 76 us.  A tile takes 2500 cycles, of which a softmax warp works 2000 (560 for
+// the maxima of 64 keys, 880 for their weights, 270 for the scores out of TMEM) beside the converting warps on its
+// scheduler, which wait a quarter of theirs for free stages: instructions bound it, the tensor pipe is busy for 25 %, shared
+// memory for 23.  Codes loaded to registers past the ring, behind prefetches to L2, took 86 us, the next tile's scores
+// loaded behind this one's weights 81.
 #include <math.h>
 
 #include "cospec_internal.h"
