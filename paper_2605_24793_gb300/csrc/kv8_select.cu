@@ -14,9 +14,9 @@
 // eight bits a pass, until 64 keys or fewer are left, which are ranked by comparison; one pass in page order
 // writes what lies above it and, of the pages equal to it, the first ones.
 //
-// One user at 32768 tokens takes 10 us: 2 to the queries, 1.7 for the scores, the rest for the m-th key and the list.  64
-// sequences at 8192 to 32768 take 36 us: a CTA's step of 256 pages (32 KB of scattered rows) 3 us with three CTAs an SM,
-// the longest has 8.  16 sequences of 8 rows 35.5 us: 1024 rows' lists on 456 resident CTAs.
+// One user at 32768 tokens takes 9 us: 1.8 to the queries, 1.2 for the scores, the rest for the m-th key and the list.  64
+// sequences at 8192 to 32768 take 29 us: a CTA's step of 256 pages (32 KB of scattered rows) 1.8 us with three CTAs an SM,
+// the longest has 8.  16 sequences of 8 rows 32 us: 1024 rows' lists on 456 resident CTAs.
 #include "cospec_internal.h"
 #include "kv8.cuh"
 
@@ -87,12 +87,19 @@ CS_DEV int sequence_of(const int32_t* ctx_len, int B, int z, int* room, int& ctx
   return b;
 }
 
-template <int D>
-__global__ void __launch_bounds__(CT, 3) kv8_select_kernel(const Kv8SelectArgs a, const Plan pl, int* err) {
+// KIND: ONE tile for all the rows (a token of up to 8 heads), SOME rows a tile, or a ROW of more than 8 heads over several.
+// (Registers decide: in one form, with spills at three CTAs an SM, a token of 64 sequences took 36.4 us for 28.8.)
+// CTAS of an SM: with several tiles of dimension 128 three still spill some words, which is worth it where many CTAs wait
+// for their turn (16 sequences of 16 rows: 48.8 us, with two 57.6) and not where few do (one user's 6 rows 11.3 and
+// 10.2 us, 16 sequences of 4 rows of 64 heads 18.7 and 16.8).
+enum { ONE, SOME, ROW };
+template <int D, int KIND, int CTAS>
+__global__ void __launch_bounds__(CT, CTAS) kv8_select_kernel(const Kv8SelectArgs a, const Plan pl, int* err) {
+  const int tiles = KIND == ONE ? 1 : pl.tiles, tiles_per_row = KIND == ROW ? pl.tiles_per_row : 0;
   extern __shared__ __align__(16) uint8_t smem[];
   uint2* qf = reinterpret_cast<uint2*>(smem);              // query fragments [tiles][D / 16][32 lanes]
-  float* qsum = reinterpret_cast<float*>(smem + (size_t)pl.tiles * (D / 16) * 256);        // [tiles][8]: where the sums start
-  uint32_t* key = reinterpret_cast<uint32_t*>(qsum + pl.tiles * 8);                        // this CTA's row: [pages from lo on]
+  float* qsum = reinterpret_cast<float*>(smem + (size_t)tiles * (D / 16) * 256);        // [tiles][8]: where the sums start
+  uint32_t* key = reinterpret_cast<uint32_t*>(qsum + tiles * 8);                        // this CTA's row: [pages from lo on]
   __shared__ __align__(16) int slot[RANK_MAX_B + 1];
   __shared__ int amax_bits[ROWS];
   __shared__ int hist[256];
@@ -111,8 +118,9 @@ __global__ void __launch_bounds__(CT, 3) kv8_select_kernel(const Kv8SelectArgs a
   const bool bad = C < 0 || C > a.max_pages * KV8_PAGE;
   if (bad && tid == 0 && rank == 0 && blockIdx.y == 0) set_err(err, ERR_CTX);
   const int num = bad ? 0 : (C + KV8_PAGE - 1) / KV8_PAGE;
-  int32_t* sel = a.sel + (((size_t)b * a.R + j0 + rank) * a.Hkv + h) * a.pages;   // of this CTA's row
+  auto list = [&]() { return a.sel + (((size_t)b * a.R + j0 + rank) * a.Hkv + h) * a.pages; };   // of this CTA's row
   if (num <= a.pages) {                    // every page (the same in all CTAs of the cluster)
+    int32_t* sel = list();
     if (rank < nrow)
       for (int p = tid; p < a.pages; p += CT) sel[p] = p < num ? p : -1;
     return;
@@ -123,7 +131,17 @@ __global__ void __launch_bounds__(CT, 3) kv8_select_kernel(const Kv8SelectArgs a
   const int lo = min(a.sink, num), hi = max(lo, num - a.recent);   // pages chosen anyway lie outside [lo, hi)
   const int32_t* table = a.page_table + (size_t)b * a.max_pages;
   const int stride = S * NW * STEP;
-  int p0 = lo + (rank * NW + warp) * STEP;
+  int p0 = lo + (rank * NW + warp) * STEP, t0 = 0, t1 = tiles;
+  // Where 32 pages a warp leave warps without work (16 sequences of 8 rows: 12 to 32 steps for 64 warps), a warp takes a
+  // part of the tiles, of whole rows where a row has several; that is then all it does (35.5 -> 32.5 us).
+  const int steps = (hi - lo + STEP - 1) / STEP;
+  if (KIND != ONE && 2 * steps <= S * NW) {
+    const int row_tiles = max(tiles_per_row, 1), each = tiles / row_tiles, most = min(each, S * NW / steps);
+    const int per = (each + most - 1) / most, parts = (each + per - 1) / per, u = rank * NW + warp;
+    p0 = u < steps * parts ? lo + u / parts * STEP : hi;
+    t0 = u % parts * per * row_tiles;
+    t1 = min(tiles, t0 + per * row_tiles);
+  }
   // Two steps ahead a lane reads its page's place, one step ahead the warp's summaries and their scales
   // are on their way: nothing waits for a load before the loads that do not need it are out.
   auto look_up = [&](int p) { return p + lane < hi ? table[p + lane] : -1; };
@@ -142,11 +160,11 @@ __global__ void __launch_bounds__(CT, 3) kv8_select_kernel(const Kv8SelectArgs a
   // ---------------------------------------------------------------- queries
   // A thread has a column's lane: D / 4 dimensions of a head, four of them a fragment.  (With more than CTA / 32
   // tiles the later columns are read twice.)
-  const int cols = pl.tiles * 32;
+  const int cols = tiles * 32;
   auto column = [&](int e, int& j, uint2 (&v)[D / 16]) {
     const int t = e >> 5, col = (e & 31) >> 2;
-    j = pl.tiles_per_row ? t / pl.tiles_per_row : (t << (3 - pl.log_heads)) + (col >> pl.log_heads);
-    const int head = min(pl.tiles_per_row ? t % pl.tiles_per_row * 8 + col : col & (heads - 1), G - 1);
+    j = tiles_per_row ? t / tiles_per_row : (t << (3 - pl.log_heads)) + (col >> pl.log_heads);
+    const int head = min(tiles_per_row ? t % tiles_per_row * 8 + col : col & (heads - 1), G - 1);
     const __nv_bfloat16* row = q + j * a.q.row + (size_t)head * D + (e & 3) * (D / 4);
 #pragma unroll
     for (int f = 0; f < D / 16; f += 2) {
@@ -215,7 +233,7 @@ __global__ void __launch_bounds__(CT, 3) kv8_select_kernel(const Kv8SelectArgs a
     float sc[4];                           // 2^24 times the scales of this lane's pages g, g + 8, g + 16, g + 24
 #pragma unroll
     for (int i = 0; i < 4; ++i) sc[i] = __shfl_sync(0xffffffffu, scale, i * 8 + g) * 0x1p24f;
-    for (int t = 0; t < pl.tiles; ++t) {
+    for (int t = KIND == ONE ? 0 : t0; t < (KIND == ONE ? 1 : t1); ++t) {
       float acc[2][4];
       const float2 z = *reinterpret_cast<const float2*>(qsum + t * 8 + 2 * c);
 #pragma unroll
@@ -238,7 +256,7 @@ __global__ void __launch_bounds__(CT, 3) kv8_select_kernel(const Kv8SelectArgs a
                   __byte_perm(y[2 * i + 1], 0u, 0x4342), v);
       }
       // page g + 8 i: its two columns are parts 2 (i & 1) and 2 (i & 1) + 1 of tile i >> 1
-      const int jt = pl.tiles_per_row ? t / pl.tiles_per_row : t << (3 - pl.log_heads);
+      const int jt = tiles_per_row ? t / tiles_per_row : t << (3 - pl.log_heads);
       if (pl.log_heads == 0) {             // a column is a block row
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -258,11 +276,11 @@ __global__ void __launch_bounds__(CT, 3) kv8_select_kernel(const Kv8SelectArgs a
         if (pl.log_heads >= 2) best[i] = fmaxf(best[i], __shfl_xor_sync(0xffffffffu, best[i], 1));
         if (pl.log_heads >= 3) best[i] = fmaxf(best[i], __shfl_xor_sync(0xffffffffu, best[i], 2));
       }
-      if (pl.tiles_per_row) {
-        const int part = t % pl.tiles_per_row;
+      if (tiles_per_row) {
+        const int part = t % tiles_per_row;
 #pragma unroll
         for (int i = 0; i < 4; ++i) best[i] = keep[i] = part ? fmaxf(keep[i], best[i]) : best[i];
-        if (part + 1 < pl.tiles_per_row) continue;
+        if (part + 1 < tiles_per_row) continue;
       }
       // the lanes of a block row (1, 2 or 4) all have its maxima: they share its pages' keys
       const int lanes = heads >> 1, j = jt + (c >> (pl.log_heads - 1));
@@ -425,6 +443,7 @@ __global__ void __launch_bounds__(CT, 3) kv8_select_kernel(const Kv8SelectArgs a
     eq += w < warp ? sums2[w] : 0;
   }
   const unsigned below = (1u << lane) - 1u;
+  int32_t* sel = list();
   for (int p = r0; p < r1; p += 128) {
     if (r1 - r0 > 128) kinds(p, ms, me);   // (else the first pass left them)
 #pragma unroll
@@ -456,8 +475,14 @@ cudaError_t launch(const Kv8SelectArgs& a, int* err, cudaStream_t stream) {
   while (pl.S < pl.rows) pl.S *= 2;
   while (pl.S < MAX_CLUSTER && clusters * pl.S < 2 * device_num_sms() && pl.S * NW * STEP < a.max_pages) pl.S *= 2;
   if (a.B > 65535 || (long long)pl.groups * a.Hkv > 65535) return cudaErrorInvalidValue;
-  static KernelLimits lim;
-  const cudaError_t e = ensure_kernel_limits((const void*)kv8_select_kernel<D>, lim, pl.smem, true);
+  static KernelLimits lim[5];
+  const int kind = pl.tiles_per_row ? ROW : pl.tiles == 1 ? ONE : SOME;
+  const bool few = D == 128 && kind != ONE && clusters * pl.S <= 4 * device_num_sms();
+  constexpr int C2 = D == 128 ? 2 : 3;
+  const auto kernel = kind == ROW   ? (few ? kv8_select_kernel<D, ROW, C2> : kv8_select_kernel<D, ROW, 3>)
+                      : kind == ONE ? kv8_select_kernel<D, ONE, 3>
+                                    : (few ? kv8_select_kernel<D, SOME, C2> : kv8_select_kernel<D, SOME, 3>);
+  const cudaError_t e = ensure_kernel_limits((const void*)kernel, lim[kind + (few ? 2 : 0)], pl.smem, true);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(pl.S, (unsigned)(pl.groups * a.Hkv), a.B);
@@ -473,7 +498,7 @@ cudaError_t launch(const Kv8SelectArgs& a, int* err, cudaStream_t stream) {
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kv8_select_kernel<D>, a, pl, err);
+  return cudaLaunchKernelEx(&cfg, kernel, a, pl, err);
 }
 
 }  // namespace
