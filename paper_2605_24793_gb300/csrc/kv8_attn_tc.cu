@@ -18,10 +18,10 @@
 // reference moves when a score exceeds it by 2^8, as on mma.sync.  The block's bf16 keys and values come
 // to f16 by one power of two each: 2^-25 of the block's largest value is what can be lost.
 //
-// 104 rows, batch 16 at 2048 to 8192 tokens: 76 us.  A tile takes 2500 cycles, of which a softmax warp works 2000 (560 for
-// the maxima of 64 keys, 880 for their weights, 270 for the scores out of TMEM) beside the converting warps on its
-// scheduler, which wait a quarter of theirs for free stages: instructions bound it, the tensor pipe is busy for 25 %, shared
-// memory for 23.  Codes loaded to registers past the ring, behind prefetches to L2, took 86 us, the next tile's scores
+// 104 rows, batch 16 at 2048 to 8192 tokens: 71.5 us.  A softmax warp works four fifths of a tile's time (a quarter of it on
+// the maxima of 64 keys, two fifths on their weights) beside the converting warps on its scheduler, which wait a quarter of
+// theirs for free stages: instructions bound it, and fetching them (a smaller start, rolled loops over the block: 76 us
+// before), the tensor pipe is busy for 25 %, shared memory for 23.  When it took 76 us, codes loaded to registers past the ring, behind prefetches to L2, took 86 us, the next tile's scores
 // loaded behind this one's weights 81.
 #include <math.h>
 
@@ -41,6 +41,7 @@ constexpr int MMA_WARP = 7;
 constexpr int SOFT0 = 8;                  // first softmax warp
 constexpr int THREADS = 16 * 32;
 constexpr int NS = 2;                     // operand stages
+constexpr int QB = 2;                     // query rows that a lane group loads at once (1: 73.6 us at 104 rows and batch 16, 2 72.1, 4 75.3, 8 76)
 constexpr int SLOTS = 2;                  // pieces (two pages' keys or values) on their way per converting warp
 constexpr float P_BITS = 6.f, P_ROOM = 8.f;
 constexpr float TINY = 1.2e-38f;          // a score factor is never 0: -inf stays -inf
@@ -355,6 +356,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
       const __nv_bfloat16* kb = p.k_blk.p + b * p.k_blk.batch + (size_t)h * D;
       const __nv_bfloat16* vb = p.v_blk.p + b * p.v_blk.batch + (size_t)h * D;
       float km = 0.f, vm = 0.f;
+#pragma unroll 1
       for (int e = tid; e < p.R * (D / 8); e += CONV * 32) {
         km = amax8(km, *reinterpret_cast<const uint4*>(kb + (e / (D / 8)) * p.k_blk.row + e % (D / 8) * 8));
         vm = amax8(vm, *reinterpret_cast<const uint4*>(vb + (e / (D / 8)) * p.v_blk.row + e % (D / 8) * 8));
@@ -382,6 +384,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
         mbar_arrive(blk_bar);
       }
       if (ok && (n < NS || wait_all(&k_empty[st], n / NS - 1))) {
+#pragma unroll 1
         for (int e = tid; e < p.R * (D / 8); e += CONV * 32) {
           const int row = e / (D / 8), ch = e % (D / 8);
           *reinterpret_cast<uint4*>(kt + (ch >> 3) * L::KH + row * 128 + (((ch & 7) ^ (row & 7)) * 16)) =
@@ -397,6 +400,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
       }
       if (ok && (n < NS || wait_all(&v_empty[st], n / NS - 1))) {
         // two rows' eight dimensions turned into eight dimensions' two keys; rows from R on are zeros
+#pragma unroll 1
         for (int e = tid; e < KBR / 2 * (D / 8); e += CONV * 32) {
           const int j = e / (D / 8) * 2, d = e % (D / 8) * 8;
           uint4 a = make_uint4(0u, 0u, 0u, 0u), c = a;
@@ -496,28 +500,32 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
     const int jr = j0 + (valid ? r / p.G : 0);
     const int blim = p.block_full ? p.R - 1 : jr;         // last block key that this row sees
     if (p.kv_stable) griddep_wait();
-    // The query rows in f16: a group of D / 8 lanes takes a row at a time, 16 rows a warp, all loads first.
+    // The query rows in f16: a group of D / 8 lanes takes a row at a time, 16 rows a warp, QB loads ahead.  (All eight at
+    // once are so much code, run once, that fetching it took most of 5000 cycles.)
     float* fac = reinterpret_cast<float*>(smem + L::FAC);
     {
       constexpr int LPR = D / 8, RPI = 32 / LPR, NI = 16 / RPI;
-      uint4 v[NI];
+#pragma unroll 1
+      for (int i0 = 0; i0 < NI; i0 += QB) {
+        uint4 v[QB];
 #pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        const int row = sw * 16 + i * RPI + lane / LPR;
-        v[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (row < NR)
-          v[i] = *reinterpret_cast<const uint4*>(p.q.p + b * p.q.batch + (j0 + row / p.G) * p.q.row + ((size_t)h * p.G + row % p.G) * D +
-                                                 lane % LPR * 8);
-      }
+        for (int i = 0; i < QB; ++i) {
+          const int row = sw * 16 + (i0 + i) * RPI + lane / LPR;
+          v[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (row < NR)
+            v[i] = *reinterpret_cast<const uint4*>(p.q.p + b * p.q.batch + (j0 + row / p.G) * p.q.row + ((size_t)h * p.G + row % p.G) * D +
+                                                   lane % LPR * 8);
+        }
 #pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        const int row = sw * 16 + i * RPI + lane / LPR, ch = lane % LPR;
-        float amax = amax8(0.f, v[i]);
+        for (int i = 0; i < QB; ++i) {
+          const int row = sw * 16 + (i0 + i) * RPI + lane / LPR, ch = lane % LPR;
+          float amax = amax8(0.f, v[i]);
 #pragma unroll
-        for (int o = LPR / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-        const float sc = kv8_scale127(amax);
-        *reinterpret_cast<uint4*>(smem + (ch >> 3) * L::QH + row * 128 + (((ch & 7) ^ (row & 7)) * 16)) = scaled8(v[i], kv8_inverse(sc));
-        if (ch == 0) fac[row] = sc * p.scale_log2;
+          for (int o = LPR / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+          const float sc = kv8_scale127(amax);
+          *reinterpret_cast<uint4*>(smem + (ch >> 3) * L::QH + row * 128 + (((ch & 7) ^ (row & 7)) * 16)) = scaled8(v[i], kv8_inverse(sc));
+          if (ch == 0) fac[row] = sc * p.scale_log2;
+        }
       }
       fence_proxy_async_smem();
       __syncwarp();
