@@ -9,8 +9,8 @@
 //   to 24 rows are padded less than by 16.  A warp a ring and two CTAs an SM: six warps with rings of two tiles up to 8
 //   rows, four with rings of three at 24 (as registers allow).  Up to 8 rows, with six warps, four, eight (one CTA an SM)
 //   and padded: one user at 4096 tokens 7.3, 7.5, 7.9, 8.3 us, at 32768 20.5, 24.3, 20.2, 26.5; 128 selected pages for
-//   each of 128 rows 83, 91, -, 103.  At 24 rows: batch 16 at 2048 to 8192 tokens 52 us, padded 59; batch 64 at 8192 to
-//   32768 484, padded 538;
+//   each of 128 rows 83, 91, -, 103.  At 24 rows: batch 16 at 2048 to 8192 tokens 50 us, padded 57; batch 64 at 8192 to
+//   32768 472, padded 538;
 //   rows: the query rows are the products' rows, by 16, which is as good where they fill them and has fewer shuffles: batch
 //   64 at 32 rows 538 us for 564, at 12 rows one user 8.3 for 9.2.  Up to 16 a warp a ring, four warps and two CTAs an SM
 //   or eight and one (long contexts of few users: one user at 32768 tokens 26.5 us and 22.3, at 4096 8.3 and 9.0); up to
@@ -467,6 +467,7 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint64_t recv_bar;
   __shared__ int seq_slot;
+  __shared__ float factor[L::QS ? L::NR : 1];
   __shared__ float weight[L::NR + MAX_SPLIT];              // [S][rows per owner]
   const int S = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
@@ -580,6 +581,31 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
     const int j = SEL ? jj : row / p.G, head = h * p.G + (SEL ? row : row % p.G);
     return x < nr ? p.q.p + b * p.q.batch + j * p.q.row + (size_t)head * D + c * (D / 4) : nullptr;
   };
+  // A row's values of this lane as f16 pairs, dimensions 2 y and 2 y + 1 in v[y], times the inverse of the power of two
+  // returned: |q / sc| <= 127.
+  auto take = [&](const __nv_bfloat16* src, uint32_t (&v)[D / 8]) {
+    uint4 w[D / 32];
+    float amax = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) w[i] = src ? *reinterpret_cast<const uint4*>(src + i * 8) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      const uint32_t ww[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        amax = fmaxf(amax, fmaxf(kv8_finite_abs(__uint_as_float(ww[y] << 16)), kv8_finite_abs(__uint_as_float(ww[y] & 0xffff0000u))));
+    }
+    amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+    amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+    const float sc = kv8_scale127(amax), inv = kv8_inverse(sc);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      const uint32_t ww[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+      for (int y = 0; y < 4; ++y) v[4 * i + y] = pack_f16(__uint_as_float(ww[y] << 16) * inv, __uint_as_float(ww[y] & 0xffff0000u) * inv);
+    }
+    return sc;
+  };
   constexpr int MR = MT > 0 ? MT : 1;
   const __nv_bfloat16* qrow[MR][2];
   int lim[MR][2];                                          // last block row that the query row sees
@@ -593,74 +619,62 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
         qrow[t][r] = x < nr ? p.q.p + b * p.q.batch + j * p.q.row + (size_t)head * D + c * (D / 4) : nullptr;
         lim[t][r] = p.block_full ? p.R - 1 : j;
       }
+  }
+  if constexpr (L::QS) {                                   // eight rows a warp, to all
+    constexpr int UNITS = MT > 0 ? 2 * MT : L::NT;
+    static_assert(UNITS <= NW, "a warp each");
+    if (warp < UNITS) {
+      uint32_t v[D / 8];
+      const float sc = take(q_row(warp), v);
+      if (c == 0) factor[warp * 8 + g] = sc * p.scale_log2;
 #pragma unroll
-    for (int t = 0; t < MT; ++t)
+      for (int fr = 0; fr < D / 16; ++fr) {
+        if constexpr (MT > 0) {
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        uint4 w[D / 32];
-        float amax = 0.f;
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-          w[i] = qrow[t][r] ? *reinterpret_cast<const uint4*>(qrow[t][r] + i * 8) : make_uint4(0u, 0u, 0u, 0u);
-          const uint32_t ww[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-#pragma unroll
-          for (int y = 0; y < 4; ++y)
-            amax = fmaxf(amax, fmaxf(kv8_finite_abs(__uint_as_float(ww[y] << 16)), kv8_finite_abs(__uint_as_float(ww[y] & 0xffff0000u))));
-        }
-        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-        const float sc = kv8_scale127(amax), inv = kv8_inverse(sc);      // |q / sc| <= 127
-        st.f[t][r] = sc * p.scale_log2;
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-          const uint32_t ww[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-#pragma unroll
-          for (int y = 0; y < 4; ++y) {      // pairs of the lane's dimensions 8 i + 2 y: fragment 2 i + y / 2, half y & 1
-            const uint32_t v = pack_f16(__uint_as_float(ww[y] << 16) * inv, __uint_as_float(ww[y] & 0xffff0000u) * inv);
-            const int fr = 2 * i + (y >> 1), z = r + 2 * (y & 1);
-            if (!L::QS) st.q[L::QS ? 0 : fr][z] = v;
-            else if (warp == 0) *reinterpret_cast<uint32_t*>(smem + L::BODY + (t * (D / 16) + fr) * 512 + lane * 16 + z * 4) = v;
-          }
-        }
-      }
-  } else {
-#pragma unroll
-    for (int t = 0; t < L::NT; ++t) {
-      const __nv_bfloat16* src = q_row(t);
-      uint4 w[D / 32];
-      float amax = 0.f;
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) {
-        w[i] = src ? *reinterpret_cast<const uint4*>(src + i * 8) : make_uint4(0u, 0u, 0u, 0u);
-        const uint32_t ww[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-#pragma unroll
-        for (int y = 0; y < 4; ++y)
-          amax = fmaxf(amax, fmaxf(kv8_finite_abs(__uint_as_float(ww[y] << 16)), kv8_finite_abs(__uint_as_float(ww[y] & 0xffff0000u))));
-      }
-      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-      const float sc = kv8_scale127(amax), inv = kv8_inverse(sc);        // |q / sc| <= 127
-#pragma unroll
-      for (int e = 0; e < 2; ++e) st.f[t][e] = __shfl_sync(0xffffffffu, sc, 8 * c + 4 * e) * p.scale_log2;
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) {
-        const uint32_t ww[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-        uint32_t v[4];
-#pragma unroll
-        for (int y = 0; y < 4; ++y) v[y] = pack_f16(__uint_as_float(ww[y] << 16) * inv, __uint_as_float(ww[y] & 0xffff0000u) * inv);
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {        // the lane's dimensions 8 i + 4 y ..
-          if (!L::QS) {
-            st.q[L::QS ? 0 : t][2 * i + y][0] = v[2 * y];
-            st.q[L::QS ? 0 : t][2 * i + y][1] = v[2 * y + 1];
-          } else if (warp == 0) {
-            *reinterpret_cast<uint2*>(smem + L::BODY + (t * (D / 16) + 2 * i + y) * 256 + lane * 8) = make_uint2(v[2 * y], v[2 * y + 1]);
-          }
+          for (int y = 0; y < 2; ++y)
+            *reinterpret_cast<uint32_t*>(smem + L::BODY + ((warp >> 1) * (D / 16) + fr) * 512 + lane * 16 + ((warp & 1) + 2 * y) * 4) = v[2 * fr + y];
+        } else {
+          *reinterpret_cast<uint2*>(smem + L::BODY + (warp * (D / 16) + fr) * 256 + lane * 8) = make_uint2(v[2 * fr], v[2 * fr + 1]);
         }
       }
     }
+    __syncthreads();
+    if constexpr (MT > 0) {
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) st.f[t][r] = factor[t * 16 + g + 8 * r];
+    } else {
+#pragma unroll
+      for (int t = 0; t < L::NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) st.f[t][e] = factor[8 * t + 2 * c + e];
+    }
+  } else if constexpr (MT > 0) {
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      uint32_t v[D / 8];
+      st.f[0][r] = take(qrow[0][r], v) * p.scale_log2;
+#pragma unroll
+      for (int fr = 0; fr < D / 16; ++fr) {
+        st.q[fr][r] = v[2 * fr];
+        st.q[fr][r + 2] = v[2 * fr + 1];
+      }
+    }
+  } else {
+#pragma unroll
+    for (int t = 0; t < L::NT; ++t) {
+      uint32_t v[D / 8];
+      const float sc = take(q_row(t), v);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) st.f[t][e] = __shfl_sync(0xffffffffu, sc, 8 * c + 4 * e) * p.scale_log2;
+#pragma unroll
+      for (int fr = 0; fr < D / 16; ++fr) {
+        st.q[t][fr][0] = v[2 * fr];
+        st.q[t][fr][1] = v[2 * fr + 1];
+      }
+    }
   }
-  if (L::QS) __syncthreads();
 
   // ---------------------------------------------------------------- the block's own rows
   // 16 at a time to the rings, from the last one back.  They count in units of vref as a page's values do (the weights'
