@@ -1079,7 +1079,7 @@ cudaError_t pick(Params& p, int pages, cudaStream_t stream) {
     const int jb = 128 / p.G;
     p.groups = (p.R + jb - 1) / jb;
     if ((long long)p.groups * p.Hkv > 65535) return cudaErrorInvalidValue;
-    const Split s = split_of((long long)p.groups * p.Hkv * p.B, (pages + 7) / 8, 1, Cost{13.0, 1.05, 1.4}, [](int n) { return resident_tc(D, n); });
+    const Split s = split_of((long long)p.groups * p.Hkv * p.B, (pages + 7) / 8, 1, Cost{12.0, 1.03, 1.2}, [](int n) { return resident_tc(D, n); });
     return launch_kv8_attn_tc(p, D, s.S, stream);
   }
   const int tiles = (pages + 1) / 2;

@@ -20,9 +20,9 @@
 //
 // 104 rows, batch 16 at 2048 to 8192 tokens: 71.5 us.  A softmax warp works four fifths of a tile's time (a quarter of it on
 // the maxima of 64 keys, two fifths on their weights) beside the converting warps on its scheduler, which wait a quarter of
-// theirs for free stages: instructions bound it, and fetching them (a smaller start, rolled loops over the block: 76 us
-// before), the tensor pipe is busy for 25 %, shared memory for 23.  When it took 76 us, codes loaded to registers past the ring, behind prefetches to L2, took 86 us, the next tile's scores
-// loaded behind this one's weights 81.
+// theirs for free stages: instructions bound it, and fetching them (75.6 us before the start and the block were in rolled
+// loops); the tensor pipe is busy for 25 %, shared memory for 23.  Codes loaded to registers past the ring, behind
+// prefetches to L2, cost 10 us, the next tile's scores loaded behind this one's weights 5.
 #include <math.h>
 
 #include "cospec_internal.h"
