@@ -39,8 +39,8 @@
 // distributed shared memory, each CTA finishing a slice of the rows.
 //
 // One row at batch 64, 8192 to 32768 tokens (dimension 128, 8 KV heads): 400 us, 6.7 TB/s, the memory's rate.  32 rows
-// there: 538 us, 5.0 TB/s, the products' rate (a tile's 192 take 390 of its 500 cycles an SM).  One user is latency: at
-// 4096 tokens 2.5 us to the first tile, 1.3 a tile of 24 rows, 2 to 3 for the parts.
+// there: 538 us, 5.0 TB/s: a tile takes an SM 500 cycles, its 128 products 260 of them, the rest latencies that two warps
+// a scheduler leave.  One user is latency: at 4096 tokens 2 us to the first tile, 0.8 to 1.3 a tile, 2 to 3 for the parts.
 #include <math.h>
 
 #include <type_traits>
