@@ -227,12 +227,15 @@ __global__ void __launch_bounds__(CT, CTAS) kv8_select_kernel(const Kv8SelectArg
     if (S > 1) dsmem_store_u32(to, k);
     else asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(k) : "memory");
   };
-  auto key_of = [](float dot, float s) { return s == s ? ordered(fmaf(dot, s, 0.f)) : 0u; };   // (no -0; key 0, below every score: no such page)
+  // Scores are compared times 2^-24, as the products come: below 2^123 even at the largest scales, exact down to the least that
+  // a page with a summary has (2^-115), where the score itself would pass fp32's end and 0 times infinity would be NaN, above
+  // every score.  (no -0; key 0, below every score: no such page, or a scale that is not finite)
+  auto key_of = [](float dot, float s) { return fabsf(s) <= 3.4028235e38f ? ordered(fmaf(dot, s, 0.f)) : 0u; };
   auto score = [&](int p0, const uint4 (&w)[4][D / 64], float scale) {
     float keep[4] = {0.f, 0.f, 0.f, 0.f};  // of a block row over several tiles
-    float sc[4];                           // 2^24 times the scales of this lane's pages g, g + 8, g + 16, g + 24
+    float sc[4];                           // the scales of this lane's pages g, g + 8, g + 16, g + 24
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sc[i] = __shfl_sync(0xffffffffu, scale, i * 8 + g) * 0x1p24f;
+    for (int i = 0; i < 4; ++i) sc[i] = __shfl_sync(0xffffffffu, scale, i * 8 + g);
     for (int t = KIND == ONE ? 0 : t0; t < (KIND == ONE ? 1 : t1); ++t) {
       float acc[2][4];
       const float2 z = *reinterpret_cast<const float2*>(qsum + t * 8 + 2 * c);
@@ -444,12 +447,15 @@ __global__ void __launch_bounds__(CT, CTAS) kv8_select_kernel(const Kv8SelectArg
   }
   const unsigned below = (1u << lane) - 1u;
   int32_t* sel = list();
+  const int end = a.pages;
   for (int p = r0; p < r1; p += 128) {
     if (r1 - r0 > 128) kinds(p, ms, me);   // (else the first pass left them)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int e = eq + __popc(me[i] & below);            // equal pages before this one
-      if (ms[i] >> lane & 1u || (me[i] >> lane & 1u && e < m)) sel[sure + __popc(ms[i] & below) + min(e, m)] = p + 32 * i + lane;
+      const int at = sure + __popc(ms[i] & below) + min(e, m);
+      const unsigned in = ms[i] | (e < m ? me[i] : 0u);
+      if (in >> lane & 1u && at < end) sel[at] = p + 32 * i + lane;
       sure += __popc(ms[i]);
       eq += __popc(me[i]);
     }
