@@ -25,8 +25,10 @@
 // lose bits only below 2^-25 of it).  p is held as 2^6 p relative to a reference that follows the running
 // maximum only when that has grown by 2^8, so that the output is seldom rescaled; weights down to 2^-30
 // of the largest count.  The pages' scales are powers of two: the keys' joins the score's factor, the
-// values' the weight's exponent, relative to the largest seen so far (the output is rescaled, exactly,
-// when that grows).
+// values' the weight's exponent, relative to a unit, the largest scale met that is within 2^8 of the least (the output is
+// rescaled, exactly, when it moves).  Pages that are further above or below would take weights out of f16, theirs or,
+// through the unit, all others', whatever the softmax makes of them: a tile with such a page takes bf16 weights
+// and codes (f16's range is the reason, not its precision: 2^-9 of each product is lost for 2^-12).
 //
 // The contraction's order is free, so every lane converts what it can load wide: of a key it takes 32
 // (16) dimensions side by side, the query rows laid out alike, and of a dimension's values four tokens of
@@ -58,6 +60,8 @@ namespace {
 constexpr int MAX_SPLIT = 12;
 constexpr float P_BITS = 6.f;             // weights are held times 2^6,
 constexpr float P_ROOM = 8.f;             // and may grow by 2^8 before the output is rescaled: below f16's 2^16
+constexpr int V_ROOM = 8;                 // values' scales up to 2^8 above the least are met with f16 weights,
+constexpr int V_FAR = 64;                 // and the unit is at most 2^64 below the largest: outputs stay within fp32
 
 // MT > 0: 16 MT rows a warp, padded to the products' rows; MT < 0: 8 NT = -8 MT rows, the products' columns.
 template <int D, int MT, int RW, int NW>
@@ -116,6 +120,49 @@ CS_DEV uint32_t lds32(uint32_t a) {
   return v;
 }
 
+CS_DEV float pow2_of(int k) { return __uint_as_float((uint32_t)(127 + k) << 23); }       // -126 <= k <= 127, 0 for -127
+
+// The values' scale in whose units outputs and weights count.  Exponents of scales are biased as fp32 holds them; 0: none.
+struct Unit {
+  int e = 0;                    // of the unit
+  int span = 0;                 // exponents in (e - span, e] are met with f16 weights
+  int ends = 0;                 // the least exponent so far (0: none yet), 8 bits of the largest
+  CS_DEV bool covers(int x) const { return (unsigned)(e - x) < (unsigned)span; }
+  CS_DEV float scale() const { return __uint_as_float((uint32_t)e << 23); }
+};
+constexpr int ZERO_EXP = 27;    // of 2^-100, the scale of a page of zeros: it moves no unit
+
+// The unit for a tile whose pages have the exponents e0 and e1 (0: no such page); outputs so far are to be multiplied by
+// 2^by.  Returns whether the tile needs bf16 weights.
+CS_DEV bool take_scales(Unit& u, int e0, int e1, int& by) {
+  const int a0 = e0 > ZERO_EXP ? e0 : 0, a1 = e1 > ZERO_EXP ? e1 : 0;
+  const int hi = max(a0, a1), lo = a0 && a1 ? min(a0, a1) : hi, was = u.e;
+  if (hi) {
+    const int met = u.ends >> 8, least = met ? min(met, lo) : lo, most = max(u.ends & 255, hi), cap = least + V_ROOM;
+    u.e = met && was <= cap ? (hi <= cap ? max(was, hi) : was) : (hi <= cap ? hi : least);
+    u.span = max(u.e - least + 1, 0);
+    if (u.e < most - V_FAR) {
+      u.e = most - V_FAR;
+      u.span = 0;
+    }
+    u.ends = least << 8 | most;
+  } else if (was == 0 && max(e0, e1) > 0) {
+    u.e = ZERO_EXP;
+    u.span = 1;
+  }
+  by = was ? was - u.e : 0;
+  return (e0 && !u.covers(e0)) || (e1 && !u.covers(e1));
+}
+// The same for block rows of exponents from lo to hi (0: zeros alone), whose weights are bf16 in any case: the largest may not
+// take the outputs out of fp32, and what the least ones contribute counts beside the pages.
+CS_DEV void take_block_scales(Unit& u, int lo, int hi, int& by) {
+  const int was = u.e, met = u.ends >> 8, most = max(u.ends & 255, hi);
+  u.ends = (met && lo ? min(met, lo) : max(met, lo)) << 8 | most;
+  u.e = max(max(was, ZERO_EXP), most - V_FAR);
+  u.span = 0;                              // (the next tile finds it)
+  by = was ? was - u.e : 0;
+}
+
 // What a warp carries from tile to tile: 16 MT rows, this lane's two of each 16 (g and g + 8).
 template <int D, int MT>
 struct State {
@@ -124,9 +171,8 @@ struct State {
   float f[MT][2];               // score factor of a row: its power of two, the softmax scale, log2 e
   float o[MT][D / 8][4];
   float m[MT][2], l[MT][2];     // reference of the weights (base 2), their sum
-  float vref;                   // o and the weights count in units of this values' scale
+  Unit v;
   CS_DEV void clear() {
-    vref = 0.f;
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
       m[t][0] = m[t][1] = -INFINITY;
@@ -175,9 +221,8 @@ struct Cols {
   float f[NT][2];               // score factor of a row: its power of two, the softmax scale, log2 e
   float o[NT][D / 16][4];       // dimensions 16 i + g of the two columns, then 16 i + 8 + g
   float m[NT][2], l[NT][2];     // reference of the weights (base 2), their sum
-  float vref;                   // o and the weights count in units of this values' scale
+  Unit v;
   CS_DEV void clear() {
-    vref = 0.f;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       m[t][0] = m[t][1] = -INFINITY;
@@ -215,16 +260,14 @@ CS_DEV void follow_max(Cols<D, NT>& st, int t, float mx0, float mx1, float (&bas
   }
 }
 template <int D, int NT>
-CS_DEV void raise_unit(Cols<D, NT>& st, float top) {
-  if (top <= st.vref) return;
-  const float by = st.vref * kv8_inverse(top);
-  st.vref = top;
+CS_DEV void rescale(Cols<D, NT>& st, int by) {
+  const float a = pow2_of(by / 2), b = pow2_of(by - by / 2);               // (the whole may lie outside fp32)
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
     for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) st.o[t][i][e] *= by;
+      for (int e = 0; e < 4; ++e) st.o[t][i][e] = st.o[t][i][e] * a * b;
 }
 // An 8 x 8 matrix of 16-bit numbers, a row in four lanes, turned.
 CS_DEV uint32_t turn8(uint32_t x) {
@@ -233,24 +276,40 @@ CS_DEV uint32_t turn8(uint32_t x) {
   return r;
 }
 
-// Values of scale `top` are to join the output (the same in every lane).
 template <int D, int MT>
-CS_DEV void raise_unit(State<D, MT>& st, float top) {
-  if (top <= st.vref) return;
-  const float by = st.vref * kv8_inverse(top);
-  st.vref = top;
+CS_DEV void rescale(State<D, MT>& st, int by) {
+  const float a = pow2_of(by / 2), b = pow2_of(by - by / 2);               // (the whole may lie outside fp32)
 #pragma unroll
   for (int t = 0; t < MT; ++t)
 #pragma unroll
     for (int i = 0; i < D / 8; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) st.o[t][i][e] *= by;
+      for (int e = 0; e < 4; ++e) st.o[t][i][e] = st.o[t][i][e] * a * b;
+}
+
+// A page's values' scale joins its weights as an exponent and leaves their sum again.  It joins them no further down than
+// 2^-60, where nothing is left of it in f16 but the sum needs the weights; `rest` brings bf16 ones the rest of the way.
+struct PageScale {
+  float to, back, rest;
+  CS_DEV PageScale(float scale, const Unit& u) {
+    const int k = (int)(__float_as_uint(scale) >> 23) - u.e, kx = max(k, -60);
+    to = (float)kx;
+    back = pow2_of(-kx);
+    rest = exp2f((float)(k - kx));
+  }
+};
+// Four codes as bf16 (exact), the lower two in `a`.
+CS_DEV void codes_bf16(uint32_t w, uint32_t& a, uint32_t& b) {
+  float x[4];
+  kv8_floats4(w, x);
+  a = pack_bf16(x[0], x[1]);
+  b = pack_bf16(x[2], x[3]);
 }
 
 // One tile: two pages' keys at sk and values at sv, ks / vs their scales, n their tokens (16 both
-// unless MASK).
+// unless MASK); wide, with MASK only: with bf16 weights.
 template <int D, int MT, bool MASK>
-CS_DEV void tile(State<D, MT>& st, uint32_t sk, uint32_t sv, const float (&ks)[2], const float (&vs)[2], int n0, int n1, int lane) {
+CS_DEV void tile(State<D, MT>& st, uint32_t sk, uint32_t sv, const float (&ks)[2], const float (&vs)[2], int n0, int n1, bool wide, int lane) {
   using L = Lay<D, MT, 1, 4>;
   const int g = lane >> 2, c = lane & 3;
   float s[MT][4][4];
@@ -294,16 +353,7 @@ CS_DEV void tile(State<D, MT>& st, uint32_t sk, uint32_t sv, const float (&ks)[2
       }
     }
   }
-  raise_unit(st, fmaxf(vs[0], vs[1]));
-  // A page's values' scale joins its weights as an exponent and leaves their sum again (60 binary
-  // orders below the largest, nothing of it is left in f16).
-  float ve[2], vi[2];
-#pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    const int k = max((int)(__float_as_uint(vs[e]) >> 23) - (int)(__float_as_uint(st.vref) >> 23), -60);
-    ve[e] = (float)k;
-    vi[e] = __uint_as_float((uint32_t)(127 - k) << 23);
-  }
+  const PageScale pv[2] = {PageScale(vs[0], st.v), PageScale(vs[1], st.v)};
   uint32_t p[MT][2][4];
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
@@ -326,16 +376,17 @@ CS_DEV void tile(State<D, MT>& st, uint32_t sk, uint32_t sv, const float (&ks)[2
     for (int r = 0; r < 2; ++r)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float f = st.f[t][r] * ks[e], to = ve[e] - base[r];
+        const float f = st.f[t][r] * ks[e], to = pv[e].to - base[r];
         float x[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           x[i] = exp2_approx(fmaf(s[t][i][2 * r + e], f, to));
           if (MASK && 4 * c + i >= (e ? n1 : n0)) x[i] = 0.f;
         }
-        st.l[t][r] = fmaf((x[0] + x[1]) + (x[2] + x[3]), vi[e], st.l[t][r]);
-        p[t][e][r] = pack_f16(x[0], x[1]);
-        p[t][e][2 + r] = pack_f16(x[2], x[3]);
+        st.l[t][r] = fmaf((x[0] + x[1]) + (x[2] + x[3]), pv[e].back, st.l[t][r]);
+        const float w = pv[e].rest;
+        p[t][e][r] = MASK && wide ? pack_bf16(x[0] * w, x[1] * w) : pack_f16(x[0], x[1]);
+        p[t][e][2 + r] = MASK && wide ? pack_bf16(x[2] * w, x[3] * w) : pack_f16(x[2], x[3]);
       }
   }
   // cells behind a page's last token may hold anything, NaN too: they read as 0
@@ -348,23 +399,36 @@ CS_DEV void tile(State<D, MT>& st, uint32_t sk, uint32_t sv, const float (&ks)[2
     }
   }
   const uint32_t va = sv + (uint32_t)(g * KV8_PAGE + c * 4);
+  auto load = [&](int e, int d) {
+    const uint32_t w = lds32(va + (uint32_t)(e * L::PB + d * 8 * KV8_PAGE));
+    return MASK ? w & keep[e] : w;
+  };
+  if (MASK && wide) {
 #pragma unroll
-  for (int e = 0; e < 2; ++e) {
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int d = 0; d < D / 8; ++d) {
+        uint32_t b0, b1;
+        codes_bf16(load(e, d), b0, b1);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) mma_16816(st.o[t][d], p[t][e], b0, b1);
+      }
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
 #pragma unroll
     for (int d = 0; d < D / 8; ++d) {
-      uint32_t w = lds32(va + (uint32_t)(e * L::PB + d * 8 * KV8_PAGE));
-      if (MASK) w &= keep[e];
-      const uint32_t b0 = kv8_f16x2(w), b1 = kv8_f16x2_hi(w);
+      const uint32_t w = load(e, d), b0 = kv8_f16x2(w), b1 = kv8_f16x2_hi(w);
 #pragma unroll
       for (int t = 0; t < MT; ++t) mma_f16(st.o[t][d], p[t][e], b0, b1);
     }
-  }
 }
 
 // The same with the rows as columns: keys times rows, then dimensions times rows.  The same loads: here tokens
 // 4 (g / 2) + i of page g mod 2 are rows g (i even) and g + 8 (i odd) of the score product i / 2.
 template <int D, int NT, bool MASK>
-CS_DEV void tile(Cols<D, NT>& st, uint32_t sk, uint32_t sv, const float (&ks)[2], const float (&vs)[2], int n0, int n1, int lane) {
+CS_DEV void tile(Cols<D, NT>& st, uint32_t sk, uint32_t sv, const float (&ks)[2], const float (&vs)[2], int n0, int n1, bool wide, int lane) {
   using L = Lay<D, -NT, 1, 4>;
   const int g = lane >> 2, c = lane & 3;
   float s[NT][2][4];
@@ -397,10 +461,8 @@ CS_DEV void tile(Cols<D, NT>& st, uint32_t sk, uint32_t sv, const float (&ks)[2]
       }
     }
   }
-  raise_unit(st, fmaxf(vs[0], vs[1]));
   const float kscale = g & 1 ? ks[1] : ks[0];
-  const int k = max((int)(__float_as_uint(g & 1 ? vs[1] : vs[0]) >> 23) - (int)(__float_as_uint(st.vref) >> 23), -60);
-  const float ve = (float)k, vi = __uint_as_float((uint32_t)(127 - k) << 23);
+  const PageScale pv(g & 1 ? vs[1] : vs[0], st.v);
   const int have = (g & 1 ? n1 : n0) - 4 * (g >> 1);       // of this lane's four tokens
   uint32_t p[NT][2][2];
 #pragma unroll
@@ -420,17 +482,17 @@ CS_DEV void tile(Cols<D, NT>& st, uint32_t sk, uint32_t sv, const float (&ks)[2]
     float x[4][2];
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const float f = st.f[t][e] * kscale, to = ve - base[e];
+      const float f = st.f[t][e] * kscale, to = pv.to - base[e];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         x[i][e] = exp2_approx(fmaf(s[t][i >> 1][2 * (i & 1) + e], f, to));
         if (MASK && i >= have) x[i][e] = 0.f;
       }
-      st.l[t][e] = fmaf((x[0][e] + x[1][e]) + (x[2][e] + x[3][e]), vi, st.l[t][e]);
+      st.l[t][e] = fmaf((x[0][e] + x[1][e]) + (x[2][e] + x[3][e]), pv.back, st.l[t][e]);
     }
     uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = turn8(pack_f16(x[i][0], x[i][1]));  // row g's weights of token 4 c + i of the two pages
+    for (int i = 0; i < 4; ++i) w[i] = turn8(MASK && wide ? pack_bf16(x[i][0] * pv.rest, x[i][1] * pv.rest) : pack_f16(x[i][0], x[i][1]));  // row g's weights of token 4 c + i of the two pages
     p[t][0][0] = __byte_perm(w[0], w[1], 0x5410);
     p[t][0][1] = __byte_perm(w[2], w[3], 0x5410);
     p[t][1][0] = __byte_perm(w[0], w[1], 0x7632);
@@ -445,15 +507,28 @@ CS_DEV void tile(Cols<D, NT>& st, uint32_t sk, uint32_t sv, const float (&ks)[2]
     }
   }
   const uint32_t va = sv + (uint32_t)(g * KV8_PAGE + c * 4);
+  auto load = [&](int e, int d) {
+    const uint32_t w = lds32(va + (uint32_t)(e * L::PB + d * 8 * KV8_PAGE));
+    return MASK ? w & keep[e] : w;
+  };
+  if (MASK && wide) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        uint32_t a[4];
+        codes_bf16(load(e, 2 * i), a[0], a[2]);
+        codes_bf16(load(e, 2 * i + 1), a[1], a[3]);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) mma_16816(st.o[t][i], a, p[t][e][0], p[t][e][1]);
+      }
+    return;
+  }
 #pragma unroll
   for (int e = 0; e < 2; ++e)
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
-      uint32_t w0 = lds32(va + (uint32_t)(e * L::PB + i * 16 * KV8_PAGE)), w1 = lds32(va + (uint32_t)(e * L::PB + (i * 16 + 8) * KV8_PAGE));
-      if (MASK) {
-        w0 &= keep[e];
-        w1 &= keep[e];
-      }
+      const uint32_t w0 = load(e, 2 * i), w1 = load(e, 2 * i + 1);
       const uint32_t a[4] = {kv8_f16x2(w0), kv8_f16x2(w1), kv8_f16x2_hi(w0), kv8_f16x2_hi(w1)};
 #pragma unroll
       for (int t = 0; t < NT; ++t) mma_f16(st.o[t][i], a, p[t][e][0], p[t][e][1]);
@@ -677,8 +752,8 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
   }
 
   // ---------------------------------------------------------------- the block's own rows
-  // 16 at a time to the rings, from the last one back.  They count in units of vref as a page's values do (the weights'
-  // bf16 holds its inverse).
+  // 16 at a time to the rings, from the last one back.  Their values come as they are, so the weights hold the unit's inverse,
+  // in bf16, whose range that takes: 2^-9 of each product is lost.
   for (int kg = KW - 1 - kw; kg < block_groups; kg += KW) {
     const int k0 = kg * 16;
     if (kg >= KW) {
@@ -687,18 +762,23 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
     }
     kv8_copy_wait<0>();
     together();
-    float vmax = 0.f;
-    for (int e = lane; e < 16 * (D / 8); e += 32) {        // (every warp looks at all of them)
-      const uint4 v = *reinterpret_cast<const uint4*>(vbuf + e * 16);
+    float vmax = 0.f;                      // half of key lane / 2 (every warp looks at all of them)
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      const int r = lane >> 1, ch = (lane & 1) * (D / 16) + i;
+      const uint4 v = *reinterpret_cast<const uint4*>(vbuf + r * (2 * D) + ((ch ^ (r & 7)) * 16));
       const uint32_t vv[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
       for (int y = 0; y < 4; ++y)
         vmax = fmaxf(vmax, fmaxf(kv8_finite_abs(__uint_as_float(vv[y] << 16)), kv8_finite_abs(__uint_as_float(vv[y] & 0xffff0000u))));
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, o));
-    raise_unit(st, kv8_scale_of(vmax));
-    const float iv = kv8_inverse(st.vref);
+    vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, 1));
+    const int ve = (int)(__float_as_uint(kv8_scale_of(vmax)) >> 23), vlo = (int)__reduce_min_sync(0xffffffffu, ve > ZERO_EXP ? (unsigned)ve : 255u),
+              vhi = (int)__reduce_max_sync(0xffffffffu, (unsigned)ve);
+    int by;
+    take_block_scales(st.v, vhi > ZERO_EXP ? vlo : 0, vhi > ZERO_EXP ? vhi : 0, by);
+    if (by != 0) rescale(st, by);
+    const float iv = kv8_inverse(st.v.scale());
     if constexpr (MT < 0) {
       float s[L::NT][4];
       const __nv_bfloat16* src[L::NT];
@@ -825,15 +905,19 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
     const float ks[2] = {__shfl_sync(0xffffffffu, scale_c.x, at), __shfl_sync(0xffffffffu, scale_c.x, at + 1)};
     const float vs[2] = {__shfl_sync(0xffffffffu, scale_c.y, at), __shfl_sync(0xffffffffu, scale_c.y, at + 1)};
     const uint32_t sk = smem_u32(ring + sg * L::STAGE);
-    if ((whole >> at & 3u) == 3u) {
-      if constexpr (MT < 0) tile<D, L::NT, false>(st, sk, sk + L::KREG, ks, vs, KV8_PAGE, KV8_PAGE, lane);
-      else tile<D, MT, false>(st, sk, sk + L::KREG, ks, vs, KV8_PAGE, KV8_PAGE, lane);
+    constexpr int X = MT < 0 ? L::NT : MT;
+    const int e0 = (int)(__float_as_uint(vs[0]) >> 23), e1 = (int)(__float_as_uint(vs[1]) >> 23);
+    bool wide = false;
+    if (!st.v.covers(e0) || !st.v.covers(e1)) {
+      int by;
+      wide = take_scales(st.v, e0, e1, by);
+      if (by != 0) rescale(st, by);
+    }
+    if ((whole >> at & 3u) == 3u && !wide) {
+      tile<D, X, false>(st, sk, sk + L::KREG, ks, vs, KV8_PAGE, KV8_PAGE, false, lane);
     } else {
       const int n0 = __shfl_sync(0xffffffffu, count_c, at), n1 = __shfl_sync(0xffffffffu, count_c, at + 1);
-      if (n0 + n1 > 0) {
-        if constexpr (MT < 0) tile<D, L::NT, true>(st, sk, sk + L::KREG, ks, vs, n0, n1, lane);
-        else tile<D, MT, true>(st, sk, sk + L::KREG, ks, vs, n0, n1, lane);
-      }
+      if (n0 + n1 > 0) tile<D, X, true>(st, sk, sk + L::KREG, ks, vs, n0, n1, wide, lane);
     }
   }
   kv8_copy_wait<0>();
@@ -847,7 +931,7 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
   }
   float* part = reinterpret_cast<float*>(smem + L::PART);
   {
-    const float unit = st.vref * exp2f(-P_BITS), one = exp2f(-P_BITS);
+    const float unit = st.v.scale() * exp2f(-P_BITS), one = exp2f(-P_BITS);
     float* mypart = part + (kw * L::NR + rw * 16) * L::PD;
     if constexpr (MT < 0) {
 #pragma unroll
