@@ -14,11 +14,13 @@
 //               (N = D, K = 64) with P_h in TMEM over its scores.
 // The values' pages hold a dimension's tokens side by side, so V too is a K-major operand as it comes.
 // The pages' scales are powers of two: the keys' joins the score's factor in the softmax, the values' the
-// weight's exponent, relative to the largest seen by the group; weights are held times 2^6 in f16 and the
-// reference moves when a score exceeds it by 2^8, as on mma.sync.  The block's bf16 keys and values come
-// to f16 by one power of two each: 2^-25 of the block's largest value is what can be lost.
+// weight's exponent, relative to a unit; weights are held times 2^6 in f16 and the reference moves when a
+// score exceeds it by 2^8, as on mma.sync.  The softmax warps look at the scales of all the CTA's pages first, while
+// they convert the queries: the unit is the largest, and where that is more than 2^8 above the least the CTA takes bf16 weights
+// and values for all of them (kv8_attn.cu says why).  The block's keys come to f16 by a power of two per key, its values stay
+// bf16 and its weights are two bf16 numbers each, the second what the first leaves over.
 //
-// 104 rows, batch 16 at 2048 to 8192 tokens: 71.5 us.  A softmax warp works four fifths of a tile's time (a quarter of it on
+// 104 rows, batch 16 at 2048 to 8192 tokens: 73 us.  A softmax warp works four fifths of a tile's time (a quarter of it on
 // the maxima of 64 keys, two fifths on their weights) beside the converting warps on its scheduler, which wait a quarter of
 // theirs for free stages: instructions bound it, and fetching them (75.6 us before the start and the block were in rolled
 // loops); the tensor pipe is busy for 25 %, shared memory for 23.  Codes loaded to registers past the ring, behind
@@ -44,6 +46,8 @@ constexpr int NS = 2;                     // operand stages
 constexpr int QB = 2;                     // query rows that a lane group loads at once (1: 73.6 us at 104 rows and batch 16, 2 72.1, 4 75.3, 8 76)
 constexpr int SLOTS = 2;                  // pieces (two pages' keys or values) on their way per converting warp
 constexpr float P_BITS = 6.f, P_ROOM = 8.f;
+constexpr int V_ROOM = 8, V_FAR = 64;     // as in kv8_attn.cu
+constexpr int ZERO_EXP = 27;
 constexpr float TINY = 1.2e-38f;          // a score factor is never 0: -inf stays -inf
 constexpr uint64_t WAIT_NS = 2000000000ull;
 
@@ -60,10 +64,11 @@ struct TL {
   static constexpr int FAC = STG + CONV * SLOTS * 2 * PB;   // [TM]: the rows' score factors
   static constexpr int MISC = FAC + TM * 4;
   // k_full, v_full, k_empty, v_empty [NS], q_full, s_full [2], p_full [2][2], pv_done [2],
-  // mma_done, recv, the block's maxima, its scales, its operands [2]
-  static constexpr int NBAR = 4 * NS + 15;
-  static constexpr int HOLDER = MISC + NBAR * 8;        // TMEM base, abort, sequence, block's maxima [2][CONV]
-  static constexpr int NEED = HOLDER + 16 + 2 * CONV * 4 + 16;
+  // mma_done, recv, the values' scales, the block's operands [2]
+  static constexpr int NBAR = 4 * NS + 14;
+  static constexpr int HOLDER = MISC + NBAR * 8;        // TMEM base, abort, sequence, the exponents' ends [2], the
+  static constexpr int BLK = HOLDER + 32;               // block's largest, whether a page is odd, the block keys' scales [64]
+  static constexpr int NEED = BLK + 64 * 4;
   static constexpr int PD = D + 4;                      // fp32 row of a partial: O, max, sum, pad
   static constexpr int ROWB = PD * 4;
   static constexpr int PART = 0, RECV = TM * ROWB;      // after the last tile, over everything before MISC
@@ -75,6 +80,8 @@ struct TL {
   static_assert(BYTES <= 232448, "shared memory of an SM");
 };
 
+// (both operands f16, or with `wide` both bf16)
+constexpr uint32_t BF16_BOTH = (1u << 7) | (1u << 10);
 constexpr uint32_t idesc_f16(int M, int N) { return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24); }
 
 CS_DEV uint32_t pack_f16(float lo, float hi) {
@@ -85,6 +92,13 @@ CS_DEV uint32_t pack_f16(float lo, float hi) {
 CS_DEV uint4 codes_f16(uint32_t a, uint32_t b) {        // eight codes
   return make_uint4(kv8_f16x2(a), kv8_f16x2_hi(a), kv8_f16x2(b), kv8_f16x2_hi(b));
 }
+CS_DEV uint4 codes_bf16(uint32_t a, uint32_t b) {       // the same in bf16 (exact)
+  float x[4], y[4];
+  kv8_floats4(a, x);
+  kv8_floats4(b, y);
+  return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+}
+CS_DEV float pow2_of(int k) { return __uint_as_float((uint32_t)(127 + k) << 23); }       // -126 <= k <= 127, 0 for -127
 CS_DEV float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 CS_DEV float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 CS_DEV float amax8(float m, uint4 v) {
@@ -124,6 +138,125 @@ CS_DEV void umma_tmem_a_k64_on(uint32_t on, uint32_t d_tmem, uint32_t a_tmem, ui
       : "memory");
 }
 
+// What only some tiles need has loops of its own: those of all roles have to stay in the instruction cache together.
+//
+// Two pages' values, piece e of a tile, `have` tokens of each; cells behind a page's last token may hold anything: they enter
+// as 0.  In f16, or `wide` in bf16.
+template <int D>
+CS_DEV void convert_values(const uint8_t* src, uint8_t* vt, int e, int have0, int have1, bool wide) {
+  const int lane = threadIdx.x & 31;
+  uint8_t* dst = vt + (e >> 1) * TL<D>::VH + lane * 128;
+#pragma unroll 1
+  for (int i = 0; i < 2 * (D / 32); ++i) {
+    const int x = i & 1, y = i >> 1, have = x ? have1 : have0, at = ((e & 1) * 4 + 2 * x) ^ (lane & 7);
+    const uint4 v = *reinterpret_cast<const uint4*>(src + x * TL<D>::PB + (y * 32 + lane) * KV8_PAGE);
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int m = have - 4 * k;
+      w[k] &= m >= 4 ? 0xffffffffu : m <= 0 ? 0u : (1u << (8 * m)) - 1u;
+    }
+    *reinterpret_cast<uint4*>(dst + y * 32 * 128 + at * 16) = wide ? codes_bf16(w[0], w[1]) : codes_f16(w[0], w[1]);
+    *reinterpret_cast<uint4*>(dst + y * 32 * 128 + (at ^ 1) * 16) = wide ? codes_bf16(w[2], w[3]) : codes_f16(w[2], w[3]);
+  }
+}
+
+CS_DEV void tq_ld8(uint32_t taddr, float (&v)[8]) {
+  uint32_t r[8];
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr));
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])::"memory");
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+}
+CS_DEV void tq_st4(uint32_t taddr, const uint32_t (&v)[4]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+}
+// A softmax thread's row and reference, sum and unit.
+struct RowState {
+  float m, l;
+  int unit, ok;
+};
+// Half a tile that is not all of pages in the ordinary way, in parts of 8 keys: of a context's end or with a page that is not
+// of the pool (weights in f16), of pages whose scales lie apart (`wide`: bf16), or of the block (`key_scale`), whose values
+// come as they are, so that the unit's inverse is with the weights, in bf16, and what that drops is left over for a second
+// product; they are at most 448 times the scale of exponent `most`.  Page c's scales are in lane 4 (t mod 8) + c, the keys'
+// below 0 for one that is not of the pool.  Keys 0 .. lim are seen.  The output so far is at `orow`, complete with phase t - 1 of
+// pv_bar.
+template <int D>
+CS_DEV RowState soft_parts(uint32_t srow, uint32_t orow, int parts, int lim, float f, float2 scales, bool wide,
+                           const float* key_scale, int most, uint64_t* pv_bar, int t, RowState st) {
+  const bool blk = key_scale != nullptr;
+  auto scores = [&](int c, float (&x)[8]) {
+    tq_ld8(srow + c * 8, x);
+    const float ks = __shfl_sync(0xffffffffu, scales.x, (t & 7) * 4 + (c >> 1)), fk = blk ? f : fmaxf(f * ks, TINY);
+    const int last = blk || ks >= 0.f ? lim - 8 * c : -1;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float y = x[k] * (blk ? fk * key_scale[8 * c + k] : fk);
+      x[k] = k <= last ? y : -INFINITY;
+    }
+  };
+  float x[8], mx = -INFINITY, alpha = 1.f;
+#pragma unroll 1
+  for (int c = 0; c < parts; ++c) {
+    scores(c, x);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) mx = fmaxf(mx, x[k]);
+  }
+  if (mx > st.m + P_ROOM) {
+    alpha = st.m == -INFINITY ? 0.f : exp2_approx(st.m - mx);
+    st.m = mx;
+    st.l *= alpha;
+  }
+  if (blk) {                                              // its values may not take the outputs out of fp32
+    const int was = st.unit, far = most - V_FAR;
+    st.unit = max(max(was, ZERO_EXP), was ? min(far, was + 126) : far);
+    if (was) alpha *= pow2_of(was - st.unit);
+  }
+  st.ok = 1;
+  if (__any_sync(0xffffffffu, alpha != 1.f && t > 0)) {
+    st.ok = __all_sync(0xffffffffu, mbar_wait(pv_bar, (uint32_t)(t - 1) & 1u, WAIT_NS));
+    tc_fence_after();
+    if (st.ok) {
+#pragma unroll 1
+      for (int c = 0; c < D / 8; ++c) {
+        tq_ld8(orow + c * 8, x);
+        uint32_t w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(x[k] * alpha);
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(orow + c * 8), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                     "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                     : "memory");
+      }
+    }
+  }
+  const float nb = P_BITS - (st.m == -INFINITY ? 0.f : st.m);
+#pragma unroll 1
+  for (int c = 0; c < parts; ++c) {
+    scores(c, x);
+    // (no further down than 2^-60, which the sum needs; the rest of the way by a factor)
+    const float vs = __shfl_sync(0xffffffffu, scales.y, (t & 7) * 4 + (c >> 1));
+    const int k0 = blk ? 127 - st.unit : (int)(__float_as_uint(vs) >> 23) - st.unit, kx = blk ? 0 : max(k0, -60);
+    const float to = nb + (float)kx, w = pow2_of(max(k0 - kx, -127));
+    float sum = 0.f;
+    uint32_t pk[4], rest[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float a = exp2_approx(x[2 * k] + to), b = exp2_approx(x[2 * k + 1] + to);
+      sum += a + b;
+      pk[k] = blk || wide ? pack_bf16(a * w, b * w) : pack_f16(a, b);
+      rest[k] = pack_bf16(fmaf(a, w, -bf_lo(pk[k])), fmaf(b, w, -bf_hi(pk[k])));
+    }
+    st.l = fmaf(sum, pow2_of(-kx), st.l);
+    tq_st4(srow + c * 4, pk);                             // over scores that have been read
+    if (blk) tq_st4(srow + 64 + c * 4, rest);             // the other half's, which the block does not use
+  }
+  return st;
+}
+
 template <int D>
 __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params p) {
   using L = TL<D>;
@@ -140,14 +273,15 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
   uint64_t* pv_done = p_full + 4;           // [2]
   uint64_t* mma_done = pv_done + 2;
   uint64_t* recv_bar = mma_done + 1;
-  uint64_t* max_bar = recv_bar + 1;         // the converting warps' maxima over the block are there
-  uint64_t* blk_bar = max_bar + 1;          // its scales are
-  uint64_t* blk_done = blk_bar + 1;         // [2]: its keys, its values have been written
+  uint64_t* ends_bar = recv_bar + 1;        // the least and the largest exponent of the pages' values are there
+  uint64_t* blk_done = ends_bar + 1;        // [2]: the block's keys and their scales, its values have been written
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem + L::HOLDER);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
   volatile int* seq_slot = abort_flag + 1;
-  volatile float* blk_max = reinterpret_cast<volatile float*>(smem + L::HOLDER + 16);   // [2][CONV]
-  volatile float* blk_scale = blk_max + 2 * CONV;                                       // [2]
+  int* ends = reinterpret_cast<int*>(smem + L::HOLDER + 16);       // least (255: no page), largest (0)
+  int* blk_most = ends + 2;                                        // the same of the block's values
+  int* odd = ends + 3;                                             // a page is not of the pool, or has no scale
+  float* blk_scale = reinterpret_cast<float*>(smem + L::BLK);
 
   const int S = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
   const int h = blockIdx.y / p.groups, rg = blockIdx.y % p.groups;
@@ -172,11 +306,12 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
     }
     mbar_init(mma_done, 1);
     mbar_init(recv_bar, 1);
-    mbar_init(max_bar, CONV);
-    mbar_init(blk_bar, 1);
+    mbar_init(ends_bar, 8);
     mbar_init(&blk_done[0], CONV);
     mbar_init(&blk_done[1], CONV);
     *abort_flag = 0;
+    ends[0] = 255;
+    ends[1] = *blk_most = *odd = 0;
     fence_barrier_init();
   }
   if (warp == MMA_WARP) {
@@ -204,6 +339,10 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
   const int KBR = (p.R + 15) & ~15;
   const int32_t* table = p.page_table + (size_t)b * p.max_pages;
   float mref = -INFINITY, l = 0.f, vref = 0.f;            // softmax threads: of this row and half
+  // (once they are there)
+  auto is_wide = [&]() { return *(volatile int*)(ends + 1) - *(volatile int*)ends > V_ROOM; };
+  auto is_odd = [&]() { return is_wide() || *(volatile int*)odd != 0; };
+  const bool cut = (rank + (n - 1) * S) * TK + TK > C;    // the last cache tile is not all of the context's keys
 
   if (warp < CONV) {
     // ---------------------------------------------------------------- cache in, to f16
@@ -258,9 +397,10 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
       }
       kv8_copy_group();
     };
-    bool ok = true;
+    bool ok = true, wide = false;
     auto wait = [&](uint64_t* bar, int phase) { ok = ok && mbar_wait(bar, (uint32_t)phase & 1u, WAIT_NS); };
-    auto convert = [&](int k) {
+    // (`plain`: full pages of values, to f16)
+    auto convert = [&](int k, bool plain) {
       if ((k & 15) == 0) count_c = count;                 // (copies run at most SLOTS ahead: still these 16)
       bool values;
       int t, e;
@@ -291,31 +431,14 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
           *reinterpret_cast<uint4*>(dst + x * KPI * 128 + at * 16) = codes_f16(flip ? w.z : w.x, flip ? w.w : w.y);
           *reinterpret_cast<uint4*>(dst + x * KPI * 128 + (at ^ 1) * 16) = codes_f16(flip ? w.x : w.z, flip ? w.y : w.w);
         }
+      } else if (!plain) {
+        convert_values<D>(src, vt, e, __shfl_sync(0xffffffffu, count_c, 2 * (k & 15)), __shfl_sync(0xffffffffu, count_c, 2 * (k & 15) + 1), wide);
       } else {
-        // a lane: 16 tokens of every 32nd dimension; cells behind a page's last token may hold anything: they enter as 0
+        // a lane: 16 tokens of every 32nd dimension
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
 #pragma unroll
           for (int y = 0; y < NX; ++y) v[x][y] = *reinterpret_cast<const uint4*>(src + x * L::PB + (y * 32 + lane) * KV8_PAGE);
-        }
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const int have = __shfl_sync(0xffffffffu, count_c, 2 * (k & 15) + x);
-          if (have < KV8_PAGE) {
-            uint32_t keep[4];
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-              const int m = have - 4 * y;
-              keep[y] = m >= 4 ? 0xffffffffu : m <= 0 ? 0u : (1u << (8 * m)) - 1u;
-            }
-#pragma unroll
-            for (int y = 0; y < NX; ++y) {
-              v[x][y].x &= keep[0];
-              v[x][y].y &= keep[1];
-              v[x][y].z &= keep[2];
-              v[x][y].w &= keep[3];
-            }
-          }
         }
         uint8_t* dst = vt + (e >> 1) * L::VH + lane * 128;
 #pragma unroll
@@ -333,15 +456,26 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
       if (lane == 0) mbar_arrive(values ? &v_full[st] : &k_full[st]);
     };
     for (int k = 0; k < SLOTS; ++k) issue(k);
+    int k = 0, few = total - (cut && total > 0 && (warp + (total - 1) * CONV) / GP == 2 * n ? 1 : 0);   // pieces of whole pages
+    bool go = true;
 #pragma unroll 1
-    for (int k = 0; k < total; ++k) {
-      convert(k);
+    for (; go && k < few; ++k) {
+      convert(k, true);
       issue(k + SLOTS);                                   // (the slot has been read)
-      if ((k & 7) == 7) {                                 // (a wait that ran out makes the rest useless)
-        ok = __all_sync(0xffffffffu, ok && !*abort_flag);
-        if (!ok) break;
+      if (k == 0) {                                       // (a warp's first piece is of keys)
+        wait(ends_bar, 0);
+        wide = is_wide();
+        if (is_odd()) few = 1;
       }
+      if ((k & 7) == 7) go = __all_sync(0xffffffffu, ok && !*abort_flag);     // (a wait that ran out makes the rest useless)
     }
+#pragma unroll 1
+    for (; go && k < total; ++k) {
+      convert(k, false);
+      issue(k + SLOTS);
+      if ((k & 7) == 7) go = __all_sync(0xffffffffu, ok && !*abort_flag);
+    }
+    ok = go && ok;
     kv8_copy_wait<0>();                                   // no copy may be in flight when the ring is reused
     auto wait_all = [&](uint64_t* bar, int phase) {
       ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, (uint32_t)phase & 1u, WAIT_NS)) && !*abort_flag;
@@ -355,41 +489,28 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
       uint8_t* vt = kt + L::KB;
       const __nv_bfloat16* kb = p.k_blk.p + b * p.k_blk.batch + (size_t)h * D;
       const __nv_bfloat16* vb = p.v_blk.p + b * p.v_blk.batch + (size_t)h * D;
-      float km = 0.f, vm = 0.f;
-#pragma unroll 1
-      for (int e = tid; e < p.R * (D / 8); e += CONV * 32) {
-        km = amax8(km, *reinterpret_cast<const uint4*>(kb + (e / (D / 8)) * p.k_blk.row + e % (D / 8) * 8));
-        vm = amax8(vm, *reinterpret_cast<const uint4*>(vb + (e / (D / 8)) * p.v_blk.row + e % (D / 8) * 8));
-      }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) {
-        km = fmaxf(km, __shfl_xor_sync(0xffffffffu, km, o));
-        vm = fmaxf(vm, __shfl_xor_sync(0xffffffffu, vm, o));
-      }
-      if (lane == 0) {
-        blk_max[warp] = km;
-        blk_max[CONV + warp] = vm;
-        mbar_arrive(max_bar);
-      }
-      wait_all(max_bar, 0);                     // (bounded: a warp that gave up does not come)
-#pragma unroll
-      for (int w = 0; w < CONV; ++w) {
-        km = fmaxf(km, blk_max[w]);
-        vm = fmaxf(vm, blk_max[CONV + w]);
-      }
-      const float ks = kv8_scale_of(km), vs = kv8_scale_of(vm), ki = kv8_inverse(ks), vi = kv8_inverse(vs);
-      if (tid == 0) {
-        blk_scale[0] = ks;
-        blk_scale[1] = vs;
-        mbar_arrive(blk_bar);
-      }
       if (ok && (n < NS || wait_all(&k_empty[st], n / NS - 1))) {
+        // a group of D / 8 lanes takes a row
+        float vm = 0.f;
 #pragma unroll 1
-        for (int e = tid; e < p.R * (D / 8); e += CONV * 32) {
-          const int row = e / (D / 8), ch = e % (D / 8);
-          *reinterpret_cast<uint4*>(kt + (ch >> 3) * L::KH + row * 128 + (((ch & 7) ^ (row & 7)) * 16)) =
-              scaled8(*reinterpret_cast<const uint4*>(kb + row * p.k_blk.row + ch * 8), ki);
+        for (int e0 = warp * 32; e0 < p.R * (D / 8); e0 += CONV * 32) {
+          const int row = (e0 + lane) / (D / 8), ch = lane % (D / 8);
+          const bool live = row < p.R;
+          uint4 k = make_uint4(0u, 0u, 0u, 0u), v = k;
+          if (live) {
+            k = *reinterpret_cast<const uint4*>(kb + row * p.k_blk.row + ch * 8);
+            v = *reinterpret_cast<const uint4*>(vb + row * p.v_blk.row + ch * 8);
+          }
+          float km = amax8(0.f, k);
+          vm = amax8(vm, v);
+#pragma unroll
+          for (int o = D / 16; o > 0; o >>= 1) km = fmaxf(km, __shfl_xor_sync(0xffffffffu, km, o));
+          const float ks = kv8_scale_of(km);
+          if (live) *reinterpret_cast<uint4*>(kt + (ch >> 3) * L::KH + row * 128 + (((ch & 7) ^ (row & 7)) * 16)) = scaled8(k, kv8_inverse(ks));
+          if (live && ch == 0) blk_scale[row] = ks;
         }
+        const unsigned most = __reduce_max_sync(0xffffffffu, __float_as_uint(kv8_scale_of(vm)) >> 23);
+        if (lane == 0) atomicMax(blk_most, (int)most);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(&blk_done[0]);
@@ -408,10 +529,9 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
           if (j + 1 < p.R) c = *reinterpret_cast<const uint4*>(vb + (j + 1) * p.v_blk.row + d);
           const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, cw[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            const float lo = x & 1 ? bf_hi(aw[x >> 1]) : bf_lo(aw[x >> 1]), hi = x & 1 ? bf_hi(cw[x >> 1]) : bf_lo(cw[x >> 1]);
-            *reinterpret_cast<uint32_t*>(vt + (d + x) * 128 + (((j >> 3) ^ x) * 16) + (j & 7) * 2) = pack_f16(lo * vi, hi * vi);
-          }
+          for (int x = 0; x < 8; ++x)
+            *reinterpret_cast<uint32_t*>(vt + (d + x) * 128 + (((j >> 3) ^ x) * 16) + (j & 7) * 2) =
+                __byte_perm(aw[x >> 1], cw[x >> 1], x & 1 ? 0x7632 : 0x5410);
         }
         fence_proxy_async_smem();
         __syncwarp();
@@ -433,7 +553,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
       const uint32_t sbase = smem_u32(smem);
       const uint64_t q_desc = smem_desc_sw128(sbase), k_desc = smem_desc_sw128(sbase + L::TILES);
       constexpr uint64_t STAGE16 = (uint64_t)((L::KB + L::VB) >> 4);
-      bool ok = __all_sync(0xffffffffu, mbar_wait(q_full, 0, WAIT_NS));
+      bool ok = __all_sync(0xffffffffu, mbar_wait(q_full, 0, WAIT_NS) && mbar_wait(ends_bar, 0, WAIT_NS));
+      const bool wide = is_wide();
       tc_fence_after();
       auto issue_s = [&](int t) {
         const int nk = do_blk && t == n ? KBR : TK;
@@ -448,11 +569,15 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
       auto issue_pv = [&](int u, int x) {
         const uint64_t vd = k_desc + (uint64_t)(u % NS) * STAGE16 + (uint64_t)((L::KB + x * L::VH) >> 4);
         const uint32_t src = tmem + (uint32_t)((u & 1) * TK + x * 64), dst = tmem + L::OCOL + (uint32_t)(x * D);
-        if (do_blk && u == n && KBR < 64) {
-          for (int ks = 0; ks < KBR / 16; ++ks)
-            umma_bf16_tmem_a_on(on, dst, src + (uint32_t)(ks * 8), vd + (uint64_t)(ks * 2), idesc_f16(TM, D), (u | ks) != 0 ? 1u : 0u);
+        if (do_blk && u == n) {
+#pragma unroll 1
+          for (int ks = 0; ks < KBR / 16; ++ks) {         // the weights' first parts, then the second
+            umma_bf16_tmem_a_on(on, dst, src + (uint32_t)(ks * 8), vd + (uint64_t)(ks * 2), idesc_f16(TM, D) | BF16_BOTH, (u | ks) != 0 ? 1u : 0u);
+            umma_bf16_tmem_a_on(on, dst, src + (uint32_t)(64 + ks * 8), vd + (uint64_t)(ks * 2), idesc_f16(TM, D) | BF16_BOTH, 1u);
+          }
         } else {
-          umma_tmem_a_k64_on(on, dst, src, vd, idesc_f16(TM, D), u ? 1u : 0u);
+          if (wide) umma_tmem_a_k64_on(on, dst, src, vd, idesc_f16(TM, D) | BF16_BOTH, u ? 1u : 0u);
+          else umma_tmem_a_k64_on(on, dst, src, vd, idesc_f16(TM, D), u ? 1u : 0u);
         }
         umma_commit_on(on, &pv_done[x]);
       };
@@ -499,6 +624,26 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
     const bool valid = r < NR;
     const int jr = j0 + (valid ? r / p.G : 0);
     const int blim = p.block_full ? p.R - 1 : jr;         // last block key that this row sees
+    // The values' exponents of the CTA's pages, 256 at a time; the first 256 on the way while queries are converted.
+    auto place = [&](int i) {
+      const int page = (rank + i / TP * S) * TP + i % TP;
+      return i < n * TP && page < num ? table[page] : -2;
+    };
+    auto exponent = [&](int ph) {
+      return (unsigned)ph < (unsigned)p.num_pages ? __float_as_uint(p.pool.scale[((size_t)ph * p.Hkv + h) * 2 + 1]) >> 23 : 0u;
+    };
+    unsigned lo = 255u, hi = 0u, first = 0u;
+    bool none = false;
+    auto join = [&](int ph, unsigned e) {
+      none |= ph != -2 && e == 0u;
+      lo = min(lo, e ? e : 255u);
+      hi = max(hi, e);
+    };
+    const int first_ph = place(sw * 32 + lane);
+    for (int i = sw * 32 + lane + 256; i < n * TP; i += 256) {
+      const int ph = place(i);
+      join(ph, exponent(ph));
+    }
     if (p.kv_stable) griddep_wait();
     // The query rows in f16: a group of D / 8 lanes takes a row at a time, 16 rows a warp, QB loads ahead.  (All eight at
     // once are so much code, run once, that fetching it took most of 5000 cycles.)
@@ -507,6 +652,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
       constexpr int LPR = D / 8, RPI = 32 / LPR, NI = 16 / RPI;
 #pragma unroll 1
       for (int i0 = 0; i0 < NI; i0 += QB) {
+        if (i0 == QB) first = exponent(first_ph);
         uint4 v[QB];
 #pragma unroll
         for (int i = 0; i < QB; ++i) {
@@ -530,30 +676,40 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(q_full);
-      named_bar_sync(1, 256);               // the rows' factors, from all eight warps
+      join(first_ph, first);
+      lo = __reduce_min_sync(0xffffffffu, lo);
+      hi = __reduce_max_sync(0xffffffffu, hi);
+      none = __any_sync(0xffffffffu, none);
+      if (lane == 0) {
+        atomicMin(ends, (int)lo);
+        atomicMax(ends + 1, (int)hi);
+        if (none) *(volatile int*)odd = 1;
+        mbar_arrive(ends_bar);
+      }
+      named_bar_sync(1, 256);               // the rows' factors and the exponents' ends, from all eight warps
     }
+    const bool wide = is_wide();
+    int unit = wide ? max(ends[0], ends[1] - V_FAR) : ends[1];     // biased, as fp32 holds it; 0: no pages
     const float f = fac[r];
     const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16);
     const uint32_t ocol = L::OCOL + (uint32_t)(grp * D);
+    // (below 0: not of the pool; 0 of the values then, or where there is no page.)
     // Lane 4 i + e: the scales of page e of this half of the (8 c + i)-th tile; the next eight tiles' are on their way.
     auto scales = [&](int t0) {
       const int t = t0 + (lane >> 2), page = (rank + t * S) * TP + grp * 4 + (lane & 3);
       float2 s = make_float2(1.f, 0.f);
       if (t < n && page < num) {
         const int ph = table[page];
+        s.x = -1.f;
         if ((unsigned)ph < (unsigned)p.num_pages) s = *reinterpret_cast<const float2*>(p.pool.scale + ((size_t)ph * p.Hkv + h) * 2);
       }
       return s;
     };
-    auto there = [&](int t, int e) {                      // the page is in the pool (a bad one's scores are masked)
-      const int page = (rank + t * S) * TP + grp * 4 + e;
-      return page >= num || (unsigned)table[page] < (unsigned)p.num_pages;
-    };
     const int mine = grp ? n : T;                         // the block's keys are all in half 0
     if (quarter < nsw) {
       float2 now = scales(0), next = scales(8);
-      for (int t = 0; t < mine; ++t) {
-        const bool blk = do_blk && t == n;
+      bool go = true;
+      auto begin = [&](int t) {
         if ((t & 7) == 0 && t > 0) {
           now = next;
           next = scales(t + 8);
@@ -563,44 +719,33 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
             set_err(p.err, ERR_TIMEOUT);
             *abort_flag = 1;
           }
-          break;
+          go = false;
         }
         tc_fence_after();
+        return go;
+      };
+      auto end = [&](int t) {
+        tq_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_full[2 * (t & 1) + grp]);
+      };
+      // Tiles of whole pages in the pool, with weights in f16; then the rest, the context's end and the block, or all of them.
+      const int plain = is_odd() ? 0 : n - (cut ? 1 : 0);
+      int t = 0;
+      for (; t < plain && begin(t); ++t) {
         const uint32_t srow = lane_base + (uint32_t)((t & 1) * TK + grp * 64);
         float x0[32], x1[32];
         tq_ld32(srow, x0);
         tq_ld32(srow + 32, x1);
         float ks[4], vs[4];
-        if (blk) {
-          mbar_wait(blk_bar, 0, WAIT_NS);
-          ks[0] = ks[1] = ks[2] = ks[3] = blk_scale[0];
-          vs[0] = vs[1] = vs[2] = vs[3] = blk_scale[1];
-        } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            ks[e] = __shfl_sync(0xffffffffu, now.x, (t & 7) * 4 + e);
-            vs[e] = __shfl_sync(0xffffffffu, now.y, (t & 7) * 4 + e);
-          }
+        for (int e = 0; e < 4; ++e) {
+          ks[e] = __shfl_sync(0xffffffffu, now.x, (t & 7) * 4 + e);
+          vs[e] = __shfl_sync(0xffffffffu, now.y, (t & 7) * 4 + e);
         }
         tq_wait_ld32(x0);
         tq_wait_ld32(x1);
-        // keys 0..lim of this half are seen by this row
-        const int left = C - (rank + t * S) * TK - grp * 64;
-        const int lim = blk ? blim : min(64, left) - 1;
-        if (blk || lim < 63) {
-#pragma unroll
-          for (int k = 0; k < 32; ++k) {
-            x0[k] = k <= lim ? x0[k] : -INFINITY;
-            x1[k] = 32 + k <= lim ? x1[k] : -INFINITY;
-          }
-        }
-        if (!blk && vs[0] * vs[1] * vs[2] * vs[3] == 0.f) {         // (a page without a scale: none, or not of the pool)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (!there(t, e))
-#pragma unroll
-              for (int k = 0; k < 16; ++k) (e < 2 ? x0 : x1)[(e & 1) * 16 + k] = -INFINITY;
-        }
         float fk[4], mx = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -618,13 +763,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
           mref = mx;
           l *= alpha;
         }
-        const float top = fmaxf(fmaxf(vs[0], vs[1]), fmaxf(vs[2], vs[3]));
-        const bool raise = top > vref;                    // (the same in the whole group)
-        if (raise) {
-          alpha *= vref * kv8_inverse(top);
-          vref = top;
-        }
-        if (__any_sync(0xffffffffu, (up || raise) && t > 0)) {
+        if (__any_sync(0xffffffffu, up && t > 0)) {
           // O_h holds tiles 0 .. t - 1: wait for the last of them, then scale the row
           const bool okp = __all_sync(0xffffffffu, mbar_wait(&pv_done[grp], (uint32_t)(t - 1) & 1u, WAIT_NS));
           tc_fence_after();
@@ -649,7 +788,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
           uint32_t pk[16];
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const int kx = max((int)(__float_as_uint(vs[e0 + e]) >> 23) - (int)(__float_as_uint(vref) >> 23), -60);
+            const int kx = max((int)(__float_as_uint(vs[e0 + e]) >> 23) - unit, -60);
             const float to = nb + (float)kx;
             const float2 f2 = make_float2(fk[e0 + e], fk[e0 + e]), to2 = make_float2(to, to);
             float2 s2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
@@ -662,16 +801,26 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
               pk[e * 8 + k] = pack_f16(a.x, a.y);
             }
             s2[0] = add2(s2[0], s2[1]);
-            l = fmaf(s2[0].x + s2[0].y, __uint_as_float((uint32_t)(127 - kx) << 23), l);
+            l = fmaf(s2[0].x + s2[0].y, pow2_of(-kx), l);
           }
           tq_st16(srow + e0 * 8, pk);
         };
         weights(x0, 0);
         weights(x1, 2);
-        tq_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&p_full[2 * (t & 1) + grp]);
+        end(t);
+      }
+      for (; go && t < mine && begin(t); ++t) {
+        const bool blk = do_blk && t == n;
+        if (blk) mbar_wait(&blk_done[0], 0, WAIT_NS);
+        // keys 0..lim of this half are seen by this row
+        const int lim = blk ? blim : min(64, C - (rank + t * S) * TK - grp * 64) - 1;
+        const RowState r = soft_parts<D>(lane_base + (uint32_t)((t & 1) * TK + grp * 64), lane_base + ocol, blk ? KBR / 8 : 8, lim, f, now, wide,
+                                         blk ? blk_scale : nullptr, *(volatile int*)blk_most, &pv_done[grp], t, RowState{mref, l, unit, 1});
+        mref = r.m;
+        l = r.l;
+        unit = r.unit;
+        if (!r.ok && lane == 0) set_err(p.err, ERR_TIMEOUT);
+        end(t);
       }
       if (mine > 0 && !*abort_flag) {
         if (!__all_sync(0xffffffffu, mbar_wait(&pv_done[grp], (uint32_t)(mine - 1) & 1u, WAIT_NS)) && lane == 0) {
@@ -679,6 +828,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
           *abort_flag = 1;
         }
       }
+      vref = __uint_as_float((uint32_t)unit << 23);
       // this half's (reference, sum, unit) for the row's other half, through score columns that are free
       tq_st2(lane_base + (uint32_t)(grp * 64 + 32), mref, l);
       tq_st2(lane_base + (uint32_t)(grp * 64 + 34), vref, 0.f);

@@ -168,3 +168,44 @@ def test_selected_pages_far_from_the_others(R, Hq, H, D, n, bits):
             k[0, p * 16:p * 16 + 16, :, 0] = _key(bits, D)
             v[0, p * 16:p * 16 + 16] *= 2.0 ** n
         _check(k, v, q, kb, vb, ctx, f"pages {pages}", sel=sel)
+
+
+# ---------------------------------------------------------------- above 32 rows per KV head: tcgen05
+TC_SHAPES = [(10, 16, 4, 64), (26, 8, 2, 128), (64, 4, 2, 64), (64, 8, 2, 128)]
+
+
+@pytest.mark.parametrize("R,Hq,H,D", TC_SHAPES)
+@pytest.mark.parametrize("n,bits", UNEVEN)
+def test_a_page_far_from_the_others_above_32_rows(R, Hq, H, D, n, bits):
+    test_a_page_far_from_the_others(R, Hq, H, D, n, bits)
+
+
+@pytest.mark.parametrize("R,Hq,H,D", TC_SHAPES)
+@pytest.mark.parametrize("n", [16, 30, 60])
+def test_a_token_and_a_channel_far_from_the_others_above_32_rows(R, Hq, H, D, n):
+    test_a_token_and_a_channel_far_from_the_others(R, Hq, H, D, n)
+
+
+@pytest.mark.parametrize("R,Hq,H,D", TC_SHAPES)
+def test_pages_of_every_magnitude_above_32_rows(R, Hq, H, D):
+    for n in (30, 60):
+        test_every_page_but_one_far_above(R, Hq, H, D, n)
+    test_pages_of_every_magnitude_and_of_zeros(R, Hq, H, D)
+
+
+@pytest.mark.parametrize("R,Hq,H,D", TC_SHAPES)
+@pytest.mark.parametrize("n", [12, 40, 100])
+def test_block_rows_far_from_the_cache_above_32_rows(R, Hq, H, D, n):
+    test_block_rows_far_from_the_cache(R, Hq, H, D, n)
+
+
+@pytest.mark.parametrize("R,Hq,H,D", [(3, 8, 2, 128), (8, 8, 2, 64)] + TC_SHAPES)
+@pytest.mark.parametrize("n", [12, 40, 70])
+def test_a_block_key_far_from_the_others(R, Hq, H, D, n):
+    """A key of the block 2^n times the rest, hidden from the rows before it: their scores stay as precise as ever."""
+    rng = np.random.default_rng(7000 * R + Hq + n)
+    ctx = [100, 0, 45]
+    k, v, q, kb, vb = _inputs(rng, ctx, R, Hq, H, D)
+    kb[:, R - 1] *= 2.0 ** n
+    kb[:, R - 1, :, 0] = _key(200, D) * 2.0 ** n           # (and its own row passes it over)
+    _check(k, v, q, kb, vb, ctx, "hidden")
