@@ -931,7 +931,8 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
   }
   float* part = reinterpret_cast<float*>(smem + L::PART);
   {
-    const float unit = st.v.scale() * exp2f(-P_BITS), one = exp2f(-P_BITS);
+    // A row: outputs as they are, in the values' unit (a product with it could leave fp32), reference, sum, the unit's exponent.
+    const float unit = (float)(st.v.e - 127);
     float* mypart = part + (kw * L::NR + rw * 16) * L::PD;
     if constexpr (MT < 0) {
 #pragma unroll
@@ -941,13 +942,13 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
           float* row = mypart + (8 * t + 2 * c + e) * L::PD;
 #pragma unroll
           for (int i = 0; i < D / 16; ++i) {
-            row[16 * i + g] = st.o[t][i][e] * unit;
-            row[16 * i + 8 + g] = st.o[t][i][2 + e] * unit;
+            row[16 * i + g] = st.o[t][i][e];
+            row[16 * i + 8 + g] = st.o[t][i][2 + e];
           }
           float l = st.l[t][e];
 #pragma unroll
           for (int x = 4; x < 32; x *= 2) l += __shfl_xor_sync(0xffffffffu, l, x);
-          if (g == 0) *reinterpret_cast<float2*>(row + D) = make_float2(st.m[t][e], l * one);
+          if (g == 0) *reinterpret_cast<float4*>(row + D) = make_float4(st.m[t][e], l, unit, 0.f);
         }
     } else {
 #pragma unroll
@@ -957,11 +958,11 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
           float* row = mypart + (t * 16 + g + 8 * r) * L::PD;
 #pragma unroll
           for (int d = 0; d < D / 8; ++d)
-            *reinterpret_cast<float2*>(row + d * 8 + 2 * c) = make_float2(st.o[t][d][2 * r] * unit, st.o[t][d][2 * r + 1] * unit);
+            *reinterpret_cast<float2*>(row + d * 8 + 2 * c) = make_float2(st.o[t][d][2 * r], st.o[t][d][2 * r + 1]);
           float l = st.l[t][r];
           l += __shfl_xor_sync(0xffffffffu, l, 1);
           l += __shfl_xor_sync(0xffffffffu, l, 2);
-          if (c == 0) *reinterpret_cast<float2*>(row + D) = make_float2(st.m[t][r], l * one);
+          if (c == 0) *reinterpret_cast<float4*>(row + D) = make_float4(st.m[t][r], l, unit, 0.f);
         }
     }
   }
@@ -972,28 +973,30 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
   for (int r0 = 0; r0 < nr; r0 += NW * 32 / LPR) {         // (a last pass may touch rows past nr)
     const int r = r0 + tid / LPR, x = tid % LPR * 4;
     if (r >= L::NR) continue;
-    float2 ml[KW];
-    float top = -INFINITY;
+    float4 ml[KW];
+    float top = -INFINITY, most = -INFINITY;               // of the weights, and of outputs with their units
 #pragma unroll
     for (int w = 0; w < KW; ++w) {
-      ml[w] = *reinterpret_cast<const float2*>(part + (w * L::NR + r) * L::PD + D);
+      ml[w] = *reinterpret_cast<const float4*>(part + (w * L::NR + r) * L::PD + D);
       top = fmaxf(top, ml[w].x);
+      most = fmaxf(most, ml[w].x + ml[w].z);
     }
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float l = 0.f;
 #pragma unroll
     for (int w = 0; w < KW; ++w) {
-      const float a = ml[w].x == -INFINITY ? 0.f : exp2_approx(ml[w].x - top);
+      const bool some = ml[w].x != -INFINITY;
+      const float a = some ? exp2_approx(ml[w].x - top) : 0.f, b = some ? exp2_approx(ml[w].x + ml[w].z - most) : 0.f;
       const float4 v = *reinterpret_cast<const float4*>(part + (w * L::NR + r) * L::PD + x);
-      acc.x += v.x * a;
-      acc.y += v.y * a;
-      acc.z += v.z * a;
-      acc.w += v.w * a;
+      acc.x += v.x * b;
+      acc.y += v.y * b;
+      acc.z += v.z * b;
+      acc.w += v.w * b;
       l += ml[w].y * a;
     }
     __syncwarp();                          // every lane of the row has read its maxima and sums
     *reinterpret_cast<float4*>(part + r * L::PD + x) = acc;
-    if (x == 0) *reinterpret_cast<float2*>(part + r * L::PD + D) = make_float2(top, l);
+    if (x == 0) *reinterpret_cast<float4*>(part + r * L::PD + D) = make_float4(top, l, most - top, 0.f);
   }
   fence_proxy_async_smem();
   __syncthreads();
@@ -1014,15 +1017,15 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
   }
   const int own0 = rank * rpo;
   for (int r = warp; r < rpo && own0 + r < nr; r += NW) {
-    const float2 ml = lane < S ? *reinterpret_cast<const float2*>(src + (lane * rpo + r) * L::PD + D) : make_float2(-INFINITY, 0.f);
+    const float4 ml = lane < S ? *reinterpret_cast<const float4*>(src + (lane * rpo + r) * L::PD + D) : make_float4(-INFINITY, 0.f, 0.f, 0.f);
     float top = ml.x;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const float a = ml.x == -INFINITY ? 0.f : exp2_approx(ml.x - top);
-    float sum = ml.y * a;
+    const bool some = ml.x != -INFINITY;
+    float sum = some ? ml.y * exp2_approx(ml.x - top) : 0.f * ml.y;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane < S) weight[lane * rpo + r] = sum == 0.f ? 0.f : a / sum;   // (0: a skipped sequence)
+    if (lane < S) weight[lane * rpo + r] = sum == 0.f ? 0.f : (some ? exp2f(ml.x - top + ml.z) : 0.f) / sum;    // (0: a skipped sequence)
   }
   __syncthreads();
   for (int e = tid; e < rpo * (D / 4); e += NW * 32) {

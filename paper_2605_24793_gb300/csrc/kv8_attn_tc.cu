@@ -98,6 +98,7 @@ CS_DEV uint4 codes_bf16(uint32_t a, uint32_t b) {       // the same in bf16 (exa
   kv8_floats4(b, y);
   return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
 }
+CS_DEV float exponent_of(float s) { return (float)((int)(__float_as_uint(s) >> 23) - 127); }
 CS_DEV float pow2_of(int k) { return __uint_as_float((uint32_t)(127 + k) << 23); }       // -126 <= k <= 127, 0 for -127
 CS_DEV float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 CS_DEV float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
@@ -859,11 +860,14 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
     const float wm = mref == -INFINITY ? 0.f : exp2_approx(mref - mm), wo = mo == -INFINITY ? 0.f : exp2_approx(mo - mm);
     // (in one order in both groups: the sum is the same number)
     const float sum = grp ? lo * wo + l * wm : l * wm + lo * wo;
-    const float w0 = grp ? wo * vo : wm * vref, w1 = grp ? wm * vref : wo * vo;
+    // Outputs stay in units of the values' until a weight takes the exponent in: a product with the unit could leave fp32.
+    const float tm = mref + exponent_of(vref), to = mo + exponent_of(vo), most = fmaxf(tm, to);
+    const float pm = mref == -INFINITY ? 0.f : exp2_approx(tm - most), po = mo == -INFINITY ? 0.f : exp2_approx(to - most);
+    const float w0 = grp ? po : pm, w1 = grp ? pm : po;
     const bool have1 = have && n > 0;       // half 1 holds cache tiles only
     const int j = j0 + (valid ? r / p.G : 0), g = valid ? r % p.G : 0;
     __nv_bfloat16* dst = p.out + (((size_t)b * p.R + j) * p.Hq + (size_t)h * p.G + g) * D;
-    const float inv = have && sum != 0.f ? 1.f / sum : 0.f;         // (NaN stays)
+    const float inv = have && sum != 0.f ? exp2f(most - mm) / sum : 0.f;         // (NaN stays)
     float* prow = part + r * PD;
 #pragma unroll 1
     for (int c = grp * (D / 32); c < (grp + 1) * (D / 32); ++c) {
@@ -890,6 +894,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
     if (S > 1 && valid && grp == 0) {
       prow[D] = have ? mm : -INFINITY;
       prow[D + 1] = have ? sum : 0.f;
+      prow[D + 2] = most - mm;
     }
   }
   if (S > 1) {
@@ -907,15 +912,15 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
     const int row0 = rank * rpo;
     float* scl = reinterpret_cast<float*>(smem + L::SCL);          // [S][rpo]
     for (int rr = warp; rr < rpo && row0 + rr < NR; rr += THREADS / 32) {
-      const float2 ml = lane < S ? *reinterpret_cast<const float2*>(recv + (lane * rpo + rr) * PD + D) : make_float2(-INFINITY, 0.f);
+      const float4 ml = lane < S ? *reinterpret_cast<const float4*>(recv + (lane * rpo + rr) * PD + D) : make_float4(-INFINITY, 0.f, 0.f, 0.f);
       float M = ml.x;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-      const float a = ml.x == -INFINITY ? 0.f : exp2_approx(ml.x - M);
-      float sum = ml.y * a;
+      const bool some = ml.x != -INFINITY;
+      float sum = some ? ml.y * exp2_approx(ml.x - M) : 0.f * ml.y;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      if (lane < S) scl[lane * rpo + rr] = sum == 0.f ? 0.f : a / sum;
+      if (lane < S) scl[lane * rpo + rr] = sum == 0.f ? 0.f : (some ? exp2f(ml.x - M + ml.z) : 0.f) / sum;
     }
     __syncthreads();
     for (int e = tid; e < rpo * (D / 4); e += THREADS) {

@@ -209,3 +209,24 @@ def test_a_block_key_far_from_the_others(R, Hq, H, D, n):
     kb[:, R - 1] *= 2.0 ** n
     kb[:, R - 1, :, 0] = _key(200, D) * 2.0 ** n           # (and its own row passes it over)
     _check(k, v, q, kb, vb, ctx, "hidden")
+
+
+@pytest.mark.parametrize("R,Hq,H,D", SHAPES + TC_SHAPES + [(1, 8, 1, 64), (26, 16, 4, 64)])
+@pytest.mark.parametrize("n", [120, 124, -90, -104])
+def test_values_near_the_types_ends(R, Hq, H, D, n):
+    """All values 2^n times ordinary ones: their sums before the division leave fp32, the result does not."""
+    rng = np.random.default_rng(8000 * R + Hq + n + 200)
+    for ctx in ([700, 45], [2000, 0]):
+        k, v, q, kb, vb = _inputs(rng, ctx, R, Hq, H, D)
+        _check(k, v * 2.0 ** n, q, kb, vb * 2.0 ** n, ctx, f"contexts {ctx}")
+
+
+@pytest.mark.parametrize("R,Hq,H,D", [(3, 24, 2, 128), (1, 2, 2, 64)])
+def test_selected_values_near_the_types_end(R, Hq, H, D):
+    rng = np.random.default_rng(9000 * R)
+    ctx = [700, 45]
+    sel = np.full((2, R, H, 40), -1, np.int32)
+    sel[0] = np.arange(4, 44)
+    sel[1, ..., :3] = (0, 1, 2)
+    k, v, q, kb, vb = _inputs(rng, ctx, R, Hq, H, D)
+    _check(k, v * 2.0 ** 124, q, kb, vb * 2.0 ** 124, ctx, "sel", sel=sel)
