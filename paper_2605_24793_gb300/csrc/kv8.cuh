@@ -75,6 +75,9 @@ CS_DEV void kv8_copy_wait() {               // all but the newest N groups have 
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
+// Two bf16 with 0 in the place of infinities and NaN.
+CS_DEV uint32_t kv8_finite_bf16x2(uint32_t w) { return w & ~__vcmpeq2(w & 0x7f807f80u, 0x7f807f80u); }
+
 // Four bf16 of a 16-bit row.
 CS_DEV void kv8_floats_of(uint2 u, float (&x)[4]) {
   x[0] = __uint_as_float(u.x << 16);

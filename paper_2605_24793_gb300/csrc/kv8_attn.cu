@@ -76,7 +76,7 @@ struct Lay {
   static constexpr int NST = D == 64 || RW == 2 ? 4 : NW == 6 ? 2 : 3;  // tiles of a ring
   static constexpr int RING = NST * STAGE;
   static constexpr int NR = RW * (MT > 0 ? 16 * MT : 8 * NT);
-  static constexpr int PD = D + (MT > 0 ? 8 : 4);            // fp32 row of a partial: O, max, sum, pad
+  static constexpr int PD = D + (MT > 0 ? 8 : 4);            // fp32 row of a partial: O, max, sum, unit, flag
   static constexpr int ROWB = PD * 4;
   static constexpr int PART = 0;                          // [KW][NR] rows; the CTA's own result in the first NR
   static constexpr int RECV = KW * NR * ROWB;             // [S][rows per owner], at most NR + 15 rows
@@ -754,6 +754,7 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
   // ---------------------------------------------------------------- the block's own rows
   // 16 at a time to the rings, from the last one back.  Their values come as they are, so the weights hold the unit's inverse,
   // in bf16, whose range that takes: 2^-9 of each product is lost.
+  float odd_values = 0.f;
   for (int kg = KW - 1 - kw; kg < block_groups; kg += KW) {
     const int k0 = kg * 16;
     if (kg >= KW) {
@@ -762,19 +763,29 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
     }
     kv8_copy_wait<0>();
     together();
-    float vmax = 0.f;                      // half of key lane / 2 (every warp looks at all of them)
+    // The exponents of its values; a lane has half of key lane / 2 (and every warp all of them).
+    uint32_t top2 = 0u;                    // largest magnitudes as bits
+    auto half_row = [&](bool mend) {
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) {
-      const int r = lane >> 1, ch = (lane & 1) * (D / 16) + i;
-      const uint4 v = *reinterpret_cast<const uint4*>(vbuf + r * (2 * D) + ((ch ^ (r & 7)) * 16));
-      const uint32_t vv[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int y = 0; y < 4; ++y)
-        vmax = fmaxf(vmax, fmaxf(kv8_finite_abs(__uint_as_float(vv[y] << 16)), kv8_finite_abs(__uint_as_float(vv[y] & 0xffff0000u))));
+      for (int i = 0; i < D / 16; ++i) {
+        const int r = lane >> 1, ch = (lane & 1) * (D / 16) + i;
+        uint4* at = reinterpret_cast<uint4*>(vbuf + r * (2 * D) + ((ch ^ (r & 7)) * 16));
+        uint4 v = *at;
+        if (mend) *at = v = make_uint4(kv8_finite_bf16x2(v.x), kv8_finite_bf16x2(v.y), kv8_finite_bf16x2(v.z), kv8_finite_bf16x2(v.w));
+        top2 = __vmaxu2(__vmaxu2(__vmaxu2(top2, v.x & 0x7fff7fffu), v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+      }
+      return max(top2 & 0xffffu, top2 >> 16);
+    };
+    uint32_t vtop = half_row(false);
+    if (__any_sync(0xffffffffu, vtop >= 0x7f80u)) {        // not finite: see kv8_add_nonfinite
+      top2 = 0u;
+      vtop = half_row(true);
+      odd_values = 1.f;
+      __syncwarp();
     }
-    vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, 1));
-    const int ve = (int)(__float_as_uint(kv8_scale_of(vmax)) >> 23), vlo = (int)__reduce_min_sync(0xffffffffu, ve > ZERO_EXP ? (unsigned)ve : 255u),
-              vhi = (int)__reduce_max_sync(0xffffffffu, (unsigned)ve);
+    vtop = max(vtop, __shfl_xor_sync(0xffffffffu, vtop, 1));
+    const int ve = (int)(__float_as_uint(kv8_scale_of(__uint_as_float(vtop << 16))) >> 23),
+              vlo = (int)__reduce_min_sync(0xffffffffu, ve > ZERO_EXP ? (unsigned)ve : 255u), vhi = (int)__reduce_max_sync(0xffffffffu, (unsigned)ve);
     int by;
     take_block_scales(st.v, vhi > ZERO_EXP ? vlo : 0, vhi > ZERO_EXP ? vhi : 0, by);
     if (by != 0) rescale(st, by);
@@ -948,7 +959,7 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
           float l = st.l[t][e];
 #pragma unroll
           for (int x = 4; x < 32; x *= 2) l += __shfl_xor_sync(0xffffffffu, l, x);
-          if (g == 0) *reinterpret_cast<float4*>(row + D) = make_float4(st.m[t][e], l, unit, 0.f);
+          if (g == 0) *reinterpret_cast<float4*>(row + D) = make_float4(st.m[t][e], l, unit, odd_values);
         }
     } else {
 #pragma unroll
@@ -962,7 +973,7 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
           float l = st.l[t][r];
           l += __shfl_xor_sync(0xffffffffu, l, 1);
           l += __shfl_xor_sync(0xffffffffu, l, 2);
-          if (c == 0) *reinterpret_cast<float4*>(row + D) = make_float4(st.m[t][r], l, unit, 0.f);
+          if (c == 0) *reinterpret_cast<float4*>(row + D) = make_float4(st.m[t][r], l, unit, odd_values);
         }
     }
   }
@@ -982,7 +993,7 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
       most = fmaxf(most, ml[w].x + ml[w].z);
     }
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l = 0.f;
+    float l = 0.f, odd = 0.f;
 #pragma unroll
     for (int w = 0; w < KW; ++w) {
       const bool some = ml[w].x != -INFINITY;
@@ -993,10 +1004,11 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
       acc.z += v.z * b;
       acc.w += v.w * b;
       l += ml[w].y * a;
+      odd = fmaxf(odd, ml[w].w);
     }
     __syncwarp();                          // every lane of the row has read its maxima and sums
     *reinterpret_cast<float4*>(part + r * L::PD + x) = acc;
-    if (x == 0) *reinterpret_cast<float4*>(part + r * L::PD + D) = make_float4(top, l, most - top, 0.f);
+    if (x == 0) *reinterpret_cast<float4*>(part + r * L::PD + D) = make_float4(top, l, most - top, odd);
   }
   fence_proxy_async_smem();
   __syncthreads();
@@ -1044,6 +1056,11 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
     const int row = row0 + own0 + r;
     const int j = SEL ? jj : row / p.G, head = h * p.G + (SEL ? row : row % p.G);
     *reinterpret_cast<uint2*>(p.out + (((size_t)b * p.R + j) * p.Hq + head) * D + x) = make_uint2(pack_bf16(acc.x, acc.y), pack_bf16(acc.z, acc.w));
+  }
+  // (the block is the last CTA's; its flag came with its rows)
+  if (own0 < nr && src[(S - 1) * rpo * L::PD + D + 3] != 0.f) {
+    __syncthreads();
+    kv8_add_nonfinite(p, D, SEL, jj, b, h, row0 + own0, min(rpo, nr - own0));
   }
   if (S > 1) cluster_wait();               // every copy out of this CTA has landed
 }

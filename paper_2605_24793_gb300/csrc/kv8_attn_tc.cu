@@ -69,7 +69,7 @@ struct TL {
   static constexpr int HOLDER = MISC + NBAR * 8;        // TMEM base, abort, sequence, the exponents' ends [2], the
   static constexpr int BLK = HOLDER + 32;               // block's largest, whether a page is odd, the block keys' scales [64]
   static constexpr int NEED = BLK + 64 * 4;
-  static constexpr int PD = D + 4;                      // fp32 row of a partial: O, max, sum, pad
+  static constexpr int PD = D + 4;                      // fp32 row of a partial: O, max, sum, unit, flag
   static constexpr int ROWB = PD * 4;
   static constexpr int PART = 0, RECV = TM * ROWB;      // after the last tile, over everything before MISC
   static constexpr int SCL = RECV + (TM + 15) * ROWB;   // [S][rows per owner]
@@ -279,6 +279,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem + L::HOLDER);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
   volatile int* seq_slot = abort_flag + 1;
+  volatile int* odd_values = seq_slot + 1;                         // the block has values that are not finite
   int* ends = reinterpret_cast<int*>(smem + L::HOLDER + 16);       // least (255: no page), largest (0)
   int* blk_most = ends + 2;                                        // the same of the block's values
   int* odd = ends + 3;                                             // a page is not of the pool, or has no scale
@@ -312,7 +313,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
     mbar_init(&blk_done[1], CONV);
     *abort_flag = 0;
     ends[0] = 255;
-    ends[1] = *blk_most = *odd = 0;
+    ends[1] = *blk_most = *odd = *odd_values = 0;
     fence_barrier_init();
   }
   if (warp == MMA_WARP) {
@@ -528,7 +529,16 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
           uint4 a = make_uint4(0u, 0u, 0u, 0u), c = a;
           if (j < p.R) a = *reinterpret_cast<const uint4*>(vb + j * p.v_blk.row + d);
           if (j + 1 < p.R) c = *reinterpret_cast<const uint4*>(vb + (j + 1) * p.v_blk.row + d);
-          const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, cw[4] = {c.x, c.y, c.z, c.w};
+          uint32_t aw[4] = {a.x, a.y, a.z, a.w}, cw[4] = {c.x, c.y, c.z, c.w};
+          uint32_t odd_bits = 0u;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {                     // (see kv8_add_nonfinite)
+            const uint32_t fa = kv8_finite_bf16x2(aw[x]), fc = kv8_finite_bf16x2(cw[x]);
+            odd_bits |= (fa ^ aw[x]) | (fc ^ cw[x]);
+            aw[x] = fa;
+            cw[x] = fc;
+          }
+          if (odd_bits) *odd_values = 1;
 #pragma unroll
           for (int x = 0; x < 8; ++x)
             *reinterpret_cast<uint32_t*>(vt + (d + x) * 128 + (((j >> 3) ^ x) * 16) + (j & 7) * 2) =
@@ -895,6 +905,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
       prow[D] = have ? mm : -INFINITY;
       prow[D + 1] = have ? sum : 0.f;
       prow[D + 2] = most - mm;
+      prow[D + 3] = do_blk && *odd_values ? 1.f : 0.f;
     }
   }
   if (S > 1) {
@@ -940,7 +951,15 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
       *reinterpret_cast<uint2*>(p.out + (((size_t)b * p.R + j) * p.Hq + (size_t)h * p.G + g) * D + c) =
           make_uint2(pack_bf16(acc.x, acc.y), pack_bf16(acc.z, acc.w));
     }
+    // (the block is the last CTA's; its flag came with its rows)
+    if (row0 < NR && recv[(S - 1) * rpo * PD + D + 3] != 0.f) {
+      __syncthreads();
+      kv8_add_nonfinite(p, D, false, 0, b, h, j0 * p.G + row0, min(rpo, NR - row0));
+    }
     cluster_wait();                         // every copy out of this CTA has landed
+  } else if (*odd_values) {
+    __syncthreads();
+    kv8_add_nonfinite(p, D, false, 0, b, h, j0 * p.G, NR);
   }
   tc_fence_before();
   __syncthreads();
