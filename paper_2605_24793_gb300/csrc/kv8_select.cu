@@ -27,7 +27,7 @@ namespace {
 constexpr int NW = 8;
 constexpr int CT = NW * 32;
 constexpr int ROWS = 8;                   // block rows of a cluster
-constexpr int MAX_CLUSTER = 16;
+constexpr int MAX_CLUSTER = 16;           // where it fits, else 8 (>= ROWS)
 constexpr int STEP = 32;                  // pages that a warp scores at once
 constexpr int FEW = 64;                   // keys ranked by comparison
 
@@ -462,6 +462,45 @@ __global__ void __launch_bounds__(CT, CTAS) kv8_select_kernel(const Kv8SelectArg
   }
 }
 
+void config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute* attr, dim3 grid, size_t smem) {
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(CT);
+  cfg.dynamicSmemBytes = smem;
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = grid.x;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+}
+
+using Kernel = void (*)(const Kv8SelectArgs, const Plan, int*);
+constexpr size_t ROOM = 8192;             // shared memory is asked for in these steps (at most 25 of them: 32768 pages)
+// Whether a cluster of MAX_CLUSTER CTAs finds room (up to 8 always do, the portable size): the device is asked once for each
+// kernel and step of shared memory.
+bool largest_fits(Kernel kernel, int which, size_t room) {
+  static std::atomic<signed char> cache[KL_MAX_DEV][10][32];         // 0: not asked, 1: it does, -1: it does not
+  int dev = 0;
+  cudaGetDevice(&dev);
+  std::atomic<signed char>& slot = cache[dev < KL_MAX_DEV ? dev : KL_MAX_DEV - 1][which][room / ROOM < 32 ? room / ROOM : 31];
+  signed char c = slot.load(std::memory_order_relaxed);
+  if (c == 0) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    config(cfg, attr, dim3(MAX_CLUSTER, 1, 1), room);
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+      cudaGetLastError();
+      n = 0;
+    }
+    c = n >= 1 ? 1 : -1;
+    slot.store(c, std::memory_order_relaxed);
+  }
+  return c > 0;
+}
+
 template <int D>
 cudaError_t launch(const Kv8SelectArgs& a, int* err, cudaStream_t stream) {
   const int G = a.Hq / a.Hkv;
@@ -485,24 +524,18 @@ cudaError_t launch(const Kv8SelectArgs& a, int* err, cudaStream_t stream) {
   const int kind = pl.tiles_per_row ? ROW : pl.tiles == 1 ? ONE : SOME;
   const bool few = D == 128 && kind != ONE && clusters * pl.S <= 4 * device_num_sms();
   constexpr int C2 = D == 128 ? 2 : 3;
-  const auto kernel = kind == ROW   ? (few ? kv8_select_kernel<D, ROW, C2> : kv8_select_kernel<D, ROW, 3>)
+  const Kernel kernel = kind == ROW   ? (few ? kv8_select_kernel<D, ROW, C2> : kv8_select_kernel<D, ROW, 3>)
                       : kind == ONE ? kv8_select_kernel<D, ONE, 3>
                                     : (few ? kv8_select_kernel<D, SOME, C2> : kv8_select_kernel<D, SOME, 3>);
-  const cudaError_t e = ensure_kernel_limits((const void*)kernel, lim[kind + (few ? 2 : 0)], pl.smem, true);
+  const int variant = kind + (few ? 2 : 0);
+  const size_t room = (pl.smem + ROOM - 1) / ROOM * ROOM;
+  const cudaError_t e = ensure_kernel_limits((const void*)kernel, lim[variant], room, true);
   if (e != cudaSuccess) return e;
+  if (pl.S == MAX_CLUSTER && !largest_fits(kernel, variant + (D == 128 ? 5 : 0), room)) pl.S = MAX_CLUSTER / 2;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(pl.S, (unsigned)(pl.groups * a.Hkv), a.B);
-  cfg.blockDim = dim3(CT);
-  cfg.dynamicSmemBytes = pl.smem;
-  cfg.stream = stream;
   cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = pl.S;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[1].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
+  config(cfg, attr, dim3(pl.S, (unsigned)(pl.groups * a.Hkv), a.B), pl.smem);
+  cfg.stream = stream;
   cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kernel, a, pl, err);
 }
