@@ -96,3 +96,65 @@ def test_a_scale_that_is_not_finite_is_no_page():
         pool.summary_scale[0, int(table[0, p]), 0] = x
     got = _select(q, pool, table, [pages * 16], n, 0, 0)[0, 0, 0]
     assert got.tolist() == [p for p in want.tolist() if p not in dropped]
+
+
+# ---------------------------------------------------------------- long contexts
+def _long(rng, ctx, H, D, width=None):
+    """Pools and shuffled tables of contexts of many pages: B tables in one pool, -1 behind each context."""
+    need = [-(-c // 16) for c in ctx]
+    width = max(need) if width is None else width
+    order, at = rng.permutation(sum(need)).astype(np.int32), 0
+    table = np.full((len(ctx), width), -1, np.int32)
+    for b, n in enumerate(need):
+        table[b, :n] = order[at:at + n]
+        at += n
+    return _pool(rng, sum(need), H, D), table
+
+
+def _rows(rng, B, R, Hq, D):
+    return torch.from_numpy(rng.standard_normal((B, R, Hq, D)).astype(np.float32)).to(torch.bfloat16).cuda()
+
+
+@pytest.mark.parametrize("pages", [1025, 2049, 4097, 8193, 32768])
+@pytest.mark.parametrize("R,Hq,H,D,n", [(1, 4, 1, 128, 64), (1, 8, 2, 64, 300), (3, 8, 2, 128, 40), (8, 2, 1, 64, 128), (2, 12, 1, 128, 17)])
+def test_one_long_context(pages, R, Hq, H, D, n):
+    """Several steps of 32 pages a warp and, in the list, runs of more than 128 pages a warp; the last page partly filled."""
+    rng = np.random.default_rng(pages + R)
+    ctx = [pages * 16 - 5]
+    pool, table = _long(rng, ctx, H, D)
+    q = _rows(rng, 1, R, Hq, D)
+    np.testing.assert_array_equal(_select(q, pool, table, ctx, n, 1, 4), _want(q, pool, table, ctx, n, 1, 4))
+
+
+@pytest.mark.parametrize("R,Hq,D,n", [(1, 4, 128, 100), (1, 32, 64, 24), (2, 4, 64, 60)])
+def test_many_ragged_contexts(R, Hq, D, n):
+    rng = np.random.default_rng(R * 7 + Hq)
+    ctx = [int(x) for x in rng.integers(0, 1400 * 16, 64)]
+    ctx[5], ctx[9], ctx[40] = 0, 3, 1400 * 16
+    pool, table = _long(rng, ctx, 1, D)
+    q = _rows(rng, 64, R, Hq, D)
+    np.testing.assert_array_equal(_select(q, pool, table, ctx, n, 1, 2), _want(q, pool, table, ctx, n, 1, 2))
+
+
+@pytest.mark.parametrize("width", [600, 2048, 9000, 32768])
+@pytest.mark.parametrize("R,Hq,H,D", [(1, 8, 2, 128), (7, 8, 2, 128), (1, 40, 2, 64), (16, 4, 1, 64)])
+def test_tables_wider_than_the_contexts(width, R, Hq, H, D):
+    """Clusters and shared memory go by the table's width: up to the largest of both, and every smaller one."""
+    rng = np.random.default_rng(width + R)
+    ctx = [590 * 16, 100, 333 * 16 + 7]
+    pool, table = _long(rng, ctx, H, D, width)
+    q = _rows(rng, 3, R, Hq, D)
+    np.testing.assert_array_equal(_select(q, pool, table, ctx, 33, 2, 3), _want(q, pool, table, ctx, 33, 2, 3))
+
+
+@pytest.mark.parametrize("pages", [1500, 5000])
+def test_ties_across_a_long_context(pages):
+    """Equal scores over many runs of the list: the lower pages, whole and in order."""
+    rng = np.random.default_rng(pages)
+    pool, table = _long(rng, [pages * 16], 1, 64)
+    pool.summary.zero_()
+    pool.summary[0, torch.from_numpy(table[0, ::3].astype(np.int64)).cuda(), 0, 0] = 5
+    pool.summary_scale.fill_(0.5)
+    q = torch.ones((1, 1, 2, 64), dtype=torch.bfloat16, device="cuda")
+    for n in (7, 300, pages // 3 + 50, pages - 1):
+        np.testing.assert_array_equal(_select(q, pool, table, [pages * 16], n, 0, 1), _want(q, pool, table, [pages * 16], n, 0, 1))
