@@ -545,9 +545,9 @@ COSPEC_API int cospec_kv8_select(const cospec_attn_dims* dims, const cospec_kv8_
 /* cospec_verify_attn over an 8-bit cache: the softmax over the ctx_len[b] cached positions of
  * layer `layer` and the block's rows (their own bf16 keys and values), causal or full inside the
  * block.  With sel (cospec_kv8_select) row j of KV head h reads only the cached positions of the pages
- * sel[b][j][h][0..pages-1]: logical pages, no page twice, the list ended by -1; positions at or
- * after ctx_len[b] are not read.  A page outside the sequence or the pool sets COSPEC_DEVERR_PAGE and
- * is skipped.
+ * sel[b][j][h][0..pages-1]: logical pages, no page twice, the list ended by its first -1 (what stands
+ * behind that is not read); positions at or after ctx_len[b] are not read.  A page outside the sequence or
+ * the pool sets COSPEC_DEVERR_PAGE and is skipped.
  *
  *    q, k_blk, v_blk  bf16 with strides (layer unused); out bf16 [batch, rows, num_q_heads, head_dim]
  *    max_ctx, dims, flags, supported shapes: as for cospec_verify_attn */

@@ -542,6 +542,7 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint64_t recv_bar;
   __shared__ int seq_slot;
+  __shared__ int list_end;
   __shared__ float factor[L::QS ? L::NR : 1];
   __shared__ float weight[L::NR + MAX_SPLIT];              // [S][rows per owner]
   const int S = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
@@ -571,11 +572,22 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
   if (bad && rank == 0 && blockIdx.y == 0 && tid == 0) set_err(p.err, ERR_CTX);
   const int num = bad ? 0 : (C + KV8_PAGE - 1) / KV8_PAGE;           // pages of the context
   if (SEL && p.kv_stable) griddep_wait();                            // the list comes from the kernel before
-  const int entries = SEL ? (bad ? 0 : p.pages) : num;
+  const int32_t* list = SEL ? p.sel + (((size_t)b * p.R + jj) * p.Hkv + h) * p.pages : nullptr;
+  int entries = num;
+  if (SEL) {                                                         // up to the list's first -1
+    if (tid == 0) list_end = bad ? 0 : p.pages;
+    __syncthreads();
+    for (int i = tid; !bad && i < p.pages; i += NW * 32)
+      if (list[i] < 0) {
+        atomicMin(&list_end, i);
+        break;
+      }
+    __syncthreads();
+    entries = list_end;
+  }
   const int tiles = (entries + 1) >> 1, stride = S * KW, mine = rank * KW + kw;
   const int n = mine < tiles ? (tiles - mine + stride - 1) / stride : 0;      // tiles of this ring
   const int32_t* table = p.page_table + (size_t)b * p.max_pages;
-  const int32_t* list = SEL ? p.sel + (((size_t)b * p.R + jj) * p.Hkv + h) * p.pages : nullptr;
   const int block_groups = bad || rank != S - 1 ? 0 : ((SEL && !p.block_full ? jj + 1 : p.R) + 15) / 16;
 
   // ---------------------------------------------------------------- the stream of tiles
