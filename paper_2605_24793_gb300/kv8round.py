@@ -55,12 +55,14 @@ class Kv8Round(VerifyRound):
     """``inputs`` as VerifyRound's, their q and k_blk before the rotation and their cache (already
     rotated) quantised into ``self.pool``; ``rope`` None builds the usual tables.  ``pages``: with a number,
     each block row attends to that many cached pages (the first ``sink``, the last ``recent`` and
-    those of the largest scores) instead of all."""
+    those of the largest scores) instead of all.  ``max_ctx`` (the longest context that rounds will reach),
+    ``temperature``, ``seed`` and ``sps_q`` are VerifyRound's."""
 
     def __init__(self, inputs: Dict[str, object], draft: np.ndarray, lam: float = 0.6, mode: int = C.POLICY_MLP, keep_attn: bool = False,
-                 rope: Optional[C.Rope] = None, pages: Optional[int] = None, sink: int = 1, recent: int = 4):
+                 rope: Optional[C.Rope] = None, pages: Optional[int] = None, sink: int = 1, recent: int = 4, max_ctx: Optional[int] = None,
+                 temperature: Optional[float] = None, seed: int = 0, sps_q: Optional[torch.Tensor] = None):
         self.pages = None if pages is None else int(pages)
-        super().__init__(inputs, draft, lam, mode, keep_attn)
+        super().__init__(inputs, draft, lam, mode, keep_attn, max_ctx, temperature, seed, sps_q)
         cfg, dev = self.cfg, self.q.device
         if self.k_pages.shape[0] != cfg.layers:
             raise ValueError("the cache must hold every layer")
@@ -78,8 +80,9 @@ class Kv8Round(VerifyRound):
     def _count_launches(self) -> int:
         cfg = self.cfg
         per_layer = 1 if self.pages is None else 2
-        # rotation, layers, LM head (main and merge per launch), arbitration, accepted length, append
-        return 1 + cfg.layers * per_layer + 2 * ((cfg.m_rows + 1023) // 1024) + (1 if cfg.k > 0 else 0) + 1 + 1
+        decide = 2 if self.sps else (1 if cfg.k > 0 else 0)
+        # rotation, layers, LM head (main and merge per launch), arbitration or acceptance, accepted length, append
+        return 1 + cfg.layers * per_layer + 2 * ((cfg.m_rows + 1023) // 1024) + decide + 1 + 1
 
     def rotate(self) -> None:
         C.kv8_rotate(self.q, self.k_blk, self.rope, self.ctx_len, self.q_rot, self.k_rot)
@@ -97,7 +100,7 @@ class Kv8Round(VerifyRound):
         """Accepted lengths and tokens, then the accepted rows of every layer into the cache from
         where the context ended before."""
         self.start.copy_(self.ctx_len)
-        C.accept_commit(self.draft, self.argmax, self.accept, self.no_blk, self.no_blk, self.no_pool, self.no_pool, self.page_table,
+        C.accept_commit(self.draft, self.target if self.sps else self.argmax, self.accept, self.no_blk, self.no_blk, self.no_pool, self.no_pool, self.page_table,
                         self.ctx_len, self.accept_len, self.emitted)
         C.kv8_append(self.pool, self.k_blk, self.v_blk, self.page_table, self.start, self.accept_len, self.rope)
         return self.accept_len, self.emitted
@@ -109,7 +112,7 @@ class Kv8Round(VerifyRound):
         for l in range(self.cfg.layers):
             self.attention(l)
         self.lmhead()
-        if self.cfg.k > 0:
+        if self.cfg.k > 0 or self.sps:
             self.arbitrate()
         self.commit()
 
