@@ -4,8 +4,8 @@ layer over the cache (or over the pages that a cheap score selects for each bloc
 head, arbitration, accepted length, and the accepted rows of every layer appended to the cache,
 rotated and quantised on the way.
 
-The cache takes half the bytes of the bf16 one, so twice the context or batch in the same memory.
-Nothing in a round synchronises with the host; a round can be captured and replayed as ``VerifyRound``.
+The cache takes about half the bytes of the bf16 one.  A round is made from a bf16 cache, which it reads
+once and keeps no reference to: the memory is free when the caller lets go of it.  Nothing in a round synchronises with the host; a round can be captured and replayed as ``VerifyRound``.
 
   python -m paper_2605_24793_gb300.kv8round --config qwen3_8b_b1
   python -m paper_2605_24793_gb300.kv8round --config qwen3_8b_b16 --layers 4 --pages 64
@@ -67,6 +67,8 @@ class Kv8Round(VerifyRound):
         if self.k_pages.shape[0] != cfg.layers:
             raise ValueError("the cache must hold every layer")
         self.pool = quantise_cache(self.k_pages, self.v_pages, self.page_table, self.ctx_len)
+        self.k_pages = self.v_pages = None
+        self.inp = {n: t for n, t in self.inp.items() if n not in ("k_pages", "v_pages")}
         self.rope = rope if rope is not None else rope_tables(self.page_table.shape[1] * PAGE, cfg.head_dim, device=dev)
         self.q_rot, self.k_rot = torch.empty_like(self.q), torch.empty_like(self.k_blk)
         self.start = self.ctx_len.clone()

@@ -106,7 +106,6 @@ class VerifyRound:
         self.io_out = torch.zeros(lead + B * R, dtype=torch.int32, device=dev)
         self.accept_len = self.io_out[:B]
         self.emitted = self.io_out[lead:].view(B, R)
-        self.dims = C.attn_dims(self.q[0], self.k_pages[0], self.page_table)
 
     def _count_launches(self) -> int:
         """Kernels one round launches (attention: 1 per layer; LM head: a main

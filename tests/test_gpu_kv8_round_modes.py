@@ -63,3 +63,30 @@ def test_speculative_sampling_rounds():
     a.replay()
     torch.cuda.synchronize()
     assert C.get_device_error() == 0
+
+
+def test_the_bf16_cache_is_let_go():
+    """A round made from a bf16 cache holds no reference to it, and runs, packs its inputs and replays without it."""
+    import gc
+    import weakref
+    cfg = _cfg().replace(ctx_lo=2000, ctx_hi=3000)
+    draft = np.random.default_rng(2).integers(0, cfg.vocab, (cfg.batch, cfg.k)).astype(np.int32)
+    inp = W.make_round_inputs(cfg, device="cuda")
+    refs = [weakref.ref(inp[n]) for n in ("k_pages", "v_pages")]
+    nbytes = sum(inp[n].numel() * 2 for n in ("k_pages", "v_pages"))
+    rnd = Kv8Round(inp, draft, cfg.lam)
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    del inp
+    gc.collect()
+    assert all(r() is None for r in refs)
+    assert before - torch.cuda.memory_allocated() >= nbytes
+    rnd.run()
+    want = [t.clone() for t in (rnd.attn_out, rnd.accept_len, rnd.emitted)]
+    rnd.pack_step_io()
+    rnd.capture()
+    rnd.replay()
+    torch.cuda.synchronize()
+    assert C.get_device_error() == 0
+    for a, b in zip(want, (rnd.attn_out, rnd.accept_len, rnd.emitted)):
+        assert torch.equal(a, b)
