@@ -28,7 +28,7 @@
 // values' the weight's exponent, relative to a unit, the largest scale met that is within 2^8 of the least (the output is
 // rescaled, exactly, when it moves).  Pages that are further above or below would take weights out of f16, theirs or,
 // through the unit, all others', whatever the softmax makes of them: a tile with such a page takes bf16 weights
-// and codes (f16's range is the reason, not its precision: 2^-9 of each product is lost for 2^-12).
+// and codes (f16's range is the reason, not its precision: 2^-8 of each product can be lost for 2^-11).
 //
 // The contraction's order is free, so every lane converts what it can load wide: of a key it takes 32
 // (16) dimensions side by side, the query rows laid out alike, and of a dimension's values four tokens of
@@ -298,6 +298,12 @@ struct PageScale {
     rest = exp2f((float)(k - kx));
   }
 };
+// Two numbers in bf16, and what that leaves of them.
+CS_DEV uint32_t two_parts(float a, float b, uint32_t& rest) {
+  const uint32_t u = pack_bf16(a, b);
+  rest = pack_bf16(a - __uint_as_float(u << 16), b - __uint_as_float(u & 0xffff0000u));
+  return u;
+}
 // Four codes as bf16 (exact), the lower two in `a`.
 CS_DEV void codes_bf16(uint32_t w, uint32_t& a, uint32_t& b) {
   float x[4];
@@ -765,7 +771,7 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
 
   // ---------------------------------------------------------------- the block's own rows
   // 16 at a time to the rings, from the last one back.  Their values come as they are, so the weights hold the unit's inverse,
-  // in bf16, whose range that takes: 2^-9 of each product is lost.
+  // in bf16, whose range that takes; what bf16 drops (2^-8, where f16 drops 2^-11) is left over for a second product.
   float odd_values = 0.f;
   for (int kg = KW - 1 - kw; kg < block_groups; kg += KW) {
     const int k0 = kg * 16;
@@ -822,7 +828,7 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
           mma_16816(s[t], a1, qv.z, qv.w);
         }
       }
-      uint32_t pf[L::NT][2];
+      uint32_t pf[L::NT][2], pr[L::NT][2];
 #pragma unroll
       for (int t = 0; t < L::NT; ++t) {
 #pragma unroll
@@ -838,8 +844,12 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
           s[t][e] = exp2_approx(s[t][e] - base[e & 1]);
           st.l[t][e & 1] += s[t][e];
         }
-        pf[t][0] = turn8(pack_bf16(s[t][0] * iv, s[t][1] * iv));
-        pf[t][1] = turn8(pack_bf16(s[t][2] * iv, s[t][3] * iv));
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          uint32_t rest;
+          pf[t][i] = turn8(two_parts(s[t][2 * i] * iv, s[t][2 * i + 1] * iv, rest));
+          pr[t][i] = turn8(rest);
+        }
       }
       const int key = (lane & 7) + (lane >> 4) * 8;
 #pragma unroll
@@ -848,7 +858,10 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
         uint32_t a[4];
         ldsm_x4_t(smem_u32(vbuf) + (uint32_t)(key * (2 * D) + ((ch ^ (key & 7)) * 16)), a[0], a[1], a[2], a[3]);
 #pragma unroll
-        for (int t = 0; t < L::NT; ++t) mma_16816(st.o[t][i], a, pf[t][0], pf[t][1]);
+        for (int t = 0; t < L::NT; ++t) {
+          mma_16816(st.o[t][i], a, pf[t][0], pf[t][1]);
+          mma_16816(st.o[t][i], a, pr[t][0], pr[t][1]);
+        }
       }
     } else {
       float s[MT][2][4];
@@ -873,7 +886,7 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
           }
         }
       }
-      uint32_t pf[MT][4];
+      uint32_t pf[MT][4], pr[MT][4];
 #pragma unroll
       for (int t = 0; t < MT; ++t) {
 #pragma unroll
@@ -894,10 +907,8 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
             s[t][i][e] = exp2_approx(s[t][i][e] - base[e >> 1]);
             st.l[t][e >> 1] += s[t][i][e];
           }
-        pf[t][0] = pack_bf16(s[t][0][0] * iv, s[t][0][1] * iv);
-        pf[t][1] = pack_bf16(s[t][0][2] * iv, s[t][0][3] * iv);
-        pf[t][2] = pack_bf16(s[t][1][0] * iv, s[t][1][1] * iv);
-        pf[t][3] = pack_bf16(s[t][1][2] * iv, s[t][1][3] * iv);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pf[t][i] = two_parts(s[t][i >> 1][2 * (i & 1)] * iv, s[t][i >> 1][2 * (i & 1) + 1] * iv, pr[t][i]);
       }
       const int key = (lane & 7) + ((lane >> 3) & 1) * 8;
 #pragma unroll
@@ -908,7 +919,9 @@ __global__ void __launch_bounds__(NW * 32, Lay<D, MT, RW, NW>::CTAS) kv8_attn_ke
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
           mma_16816(st.o[t][d], pf[t], b0, b1);
+          mma_16816(st.o[t][d], pr[t], b0, b1);
           mma_16816(st.o[t][d + 1], pf[t], b2, b3);
+          mma_16816(st.o[t][d + 1], pr[t], b2, b3);
         }
       }
     }

@@ -2,8 +2,8 @@
 
 A page (or a token, a channel, a block row) of huge values that the softmax passes over, or whose small weight makes it
 count as much as the rest, must leave everything else as precise as ever.  Tolerance as in the attention's other tests, from
-the roundings: weights to bf16 at worst (2^-9 of each product, both ways), the output to bf16 (2^-9), scores in fp32
-below 2^-12 of it: within 2^-8 (|o| + sum p |v|), channel by channel."""
+the roundings: weights to bf16 at worst (2^-8 of each product), the output to bf16 (2^-8), scores in fp32 below 2^-12 of
+it: within 2^-8 (|o| + sum p |v|), channel by channel."""
 import math
 
 import numpy as np
