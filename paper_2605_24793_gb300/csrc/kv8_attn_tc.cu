@@ -346,7 +346,79 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
   auto is_odd = [&]() { return is_wide() || *(volatile int*)odd != 0; };
   const bool cut = (rank + (n - 1) * S) * TK + TK > C;    // the last cache tile is not all of the context's keys
 
-  if (warp < CONV) {
+  if (warp == MMA_WARP) {
+    // ---------------------------------------------------------------- MMA
+    if (T > 0) {
+      const uint32_t on = elect_one();
+      const uint32_t sbase = smem_u32(smem);
+      const uint64_t q_desc = smem_desc_sw128(sbase), k_desc = smem_desc_sw128(sbase + L::TILES);
+      constexpr uint64_t STAGE16 = (uint64_t)((L::KB + L::VB) >> 4);
+      bool ok = __all_sync(0xffffffffu, mbar_wait(q_full, 0, WAIT_NS) && mbar_wait(ends_bar, 0, WAIT_NS));
+      const bool wide = is_wide();
+      tc_fence_after();
+      auto issue_s = [&](int t) {
+        const int nk = do_blk && t == n ? KBR : TK;
+        const uint64_t kd = k_desc + (uint64_t)(t % NS) * STAGE16;
+        const uint32_t dst = tmem + (uint32_t)((t & 1) * TK), id = idesc_f16(TM, nk);
+#pragma unroll
+        for (int x = 0; x < H; ++x)
+          umma_k64_on(on, dst, q_desc + (uint64_t)(x * (L::QH >> 4)), kd + (uint64_t)(x * (L::KH >> 4)), id, x ? 1u : 0u);
+        umma_commit_on(on, &k_empty[t % NS]);
+        umma_commit_on(on, &s_full[t & 1]);
+      };
+      auto issue_pv = [&](int u, int x) {
+        const uint64_t vd = k_desc + (uint64_t)(u % NS) * STAGE16 + (uint64_t)((L::KB + x * L::VH) >> 4);
+        const uint32_t src = tmem + (uint32_t)((u & 1) * TK + x * 64), dst = tmem + L::OCOL + (uint32_t)(x * D);
+        if (do_blk && u == n) {
+#pragma unroll 1
+          for (int ks = 0; ks < KBR / 16; ++ks) {         // the weights' first parts, then the second
+            umma_bf16_tmem_a_on(on, dst, src + (uint32_t)(ks * 8), vd + (uint64_t)(ks * 2), idesc_f16(TM, D) | BF16_BOTH, (u | ks) != 0 ? 1u : 0u);
+            umma_bf16_tmem_a_on(on, dst, src + (uint32_t)(64 + ks * 8), vd + (uint64_t)(ks * 2), idesc_f16(TM, D) | BF16_BOTH, 1u);
+          }
+        } else {
+          if (wide) umma_tmem_a_k64_on(on, dst, src, vd, idesc_f16(TM, D) | BF16_BOTH, u ? 1u : 0u);
+          else umma_tmem_a_k64_on(on, dst, src, vd, idesc_f16(TM, D), u ? 1u : 0u);
+        }
+        umma_commit_on(on, &pv_done[x]);
+      };
+      // A fixed order with waits that sleep: S of tile t + 2 takes the buffer that the products of tile t read (as P), and
+      // goes behind them.  (A loop that polled for whatever was ready took 250 to 500 cycles a turn beside the busy
+      // converting and softmax warps: 118 -> 92 us at batch 16, K = 25.)
+      auto wait = [&](uint64_t* bar, int phase) { ok = ok && mbar_wait(bar, (uint32_t)phase & 1u, WAIT_NS); };
+      for (int t = 0; t < min(T, 2); ++t) {
+        wait(&k_full[t % NS], t / NS);
+        if (!(ok = __all_sync(0xffffffffu, ok))) break;
+        tc_fence_after();
+        issue_s(t);
+      }
+      for (int t = 0; t < T && ok; ++t) {
+        wait(&v_full[t % NS], t / NS);
+        wait(&p_full[2 * (t & 1)], t >> 1);
+        if (!(ok = __all_sync(0xffffffffu, ok))) break;
+        tc_fence_after();
+        issue_pv(t, 0);
+        if (t < n) {                                      // (the block's keys are all in half 0)
+          wait(&p_full[2 * (t & 1) + 1], t >> 1);
+          if (!(ok = __all_sync(0xffffffffu, ok))) break;
+          tc_fence_after();
+          issue_pv(t, 1);
+        }
+        umma_commit_on(on, &v_empty[t % NS]);
+        if (t + 2 < T) {
+          wait(&k_full[t % NS], t / NS + 1);
+          if (!(ok = __all_sync(0xffffffffu, ok))) break;
+          tc_fence_after();
+          issue_s(t + 2);
+        }
+      }
+      if (!ok && on) {
+        set_err(p.err, ERR_TIMEOUT);
+        *abort_flag = 1;
+      }
+      umma_commit_on(on, mma_done);
+      mbar_wait(mma_done, 0, WAIT_NS);
+    }
+  } else if (warp < CONV) {
     // ---------------------------------------------------------------- cache in, to f16
     // The work is pieces of two pages' keys or values, four to a group: the keys of tile 0, then for every tile t the
     // keys of t + 1 and the values of t, so that scores run ahead.  Piece u is warp u mod CONV's.  (Its fixed part,
@@ -556,78 +628,6 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
     if (!ok && lane == 0) {
       set_err(p.err, ERR_TIMEOUT);
       *abort_flag = 1;
-    }
-  } else if (warp == MMA_WARP) {
-    // ---------------------------------------------------------------- MMA
-    if (T > 0) {
-      const uint32_t on = elect_one();
-      const uint32_t sbase = smem_u32(smem);
-      const uint64_t q_desc = smem_desc_sw128(sbase), k_desc = smem_desc_sw128(sbase + L::TILES);
-      constexpr uint64_t STAGE16 = (uint64_t)((L::KB + L::VB) >> 4);
-      bool ok = __all_sync(0xffffffffu, mbar_wait(q_full, 0, WAIT_NS) && mbar_wait(ends_bar, 0, WAIT_NS));
-      const bool wide = is_wide();
-      tc_fence_after();
-      auto issue_s = [&](int t) {
-        const int nk = do_blk && t == n ? KBR : TK;
-        const uint64_t kd = k_desc + (uint64_t)(t % NS) * STAGE16;
-        const uint32_t dst = tmem + (uint32_t)((t & 1) * TK), id = idesc_f16(TM, nk);
-#pragma unroll
-        for (int x = 0; x < H; ++x)
-          umma_k64_on(on, dst, q_desc + (uint64_t)(x * (L::QH >> 4)), kd + (uint64_t)(x * (L::KH >> 4)), id, x ? 1u : 0u);
-        umma_commit_on(on, &k_empty[t % NS]);
-        umma_commit_on(on, &s_full[t & 1]);
-      };
-      auto issue_pv = [&](int u, int x) {
-        const uint64_t vd = k_desc + (uint64_t)(u % NS) * STAGE16 + (uint64_t)((L::KB + x * L::VH) >> 4);
-        const uint32_t src = tmem + (uint32_t)((u & 1) * TK + x * 64), dst = tmem + L::OCOL + (uint32_t)(x * D);
-        if (do_blk && u == n) {
-#pragma unroll 1
-          for (int ks = 0; ks < KBR / 16; ++ks) {         // the weights' first parts, then the second
-            umma_bf16_tmem_a_on(on, dst, src + (uint32_t)(ks * 8), vd + (uint64_t)(ks * 2), idesc_f16(TM, D) | BF16_BOTH, (u | ks) != 0 ? 1u : 0u);
-            umma_bf16_tmem_a_on(on, dst, src + (uint32_t)(64 + ks * 8), vd + (uint64_t)(ks * 2), idesc_f16(TM, D) | BF16_BOTH, 1u);
-          }
-        } else {
-          if (wide) umma_tmem_a_k64_on(on, dst, src, vd, idesc_f16(TM, D) | BF16_BOTH, u ? 1u : 0u);
-          else umma_tmem_a_k64_on(on, dst, src, vd, idesc_f16(TM, D), u ? 1u : 0u);
-        }
-        umma_commit_on(on, &pv_done[x]);
-      };
-      // A fixed order with waits that sleep: S of tile t + 2 takes the buffer that the products of tile t read (as P), and
-      // goes behind them.  (A loop that polled for whatever was ready took 250 to 500 cycles a turn beside the busy
-      // converting and softmax warps: 118 -> 92 us at batch 16, K = 25.)
-      auto wait = [&](uint64_t* bar, int phase) { ok = ok && mbar_wait(bar, (uint32_t)phase & 1u, WAIT_NS); };
-      for (int t = 0; t < min(T, 2); ++t) {
-        wait(&k_full[t % NS], t / NS);
-        if (!(ok = __all_sync(0xffffffffu, ok))) break;
-        tc_fence_after();
-        issue_s(t);
-      }
-      for (int t = 0; t < T && ok; ++t) {
-        wait(&v_full[t % NS], t / NS);
-        wait(&p_full[2 * (t & 1)], t >> 1);
-        if (!(ok = __all_sync(0xffffffffu, ok))) break;
-        tc_fence_after();
-        issue_pv(t, 0);
-        if (t < n) {                                      // (the block's keys are all in half 0)
-          wait(&p_full[2 * (t & 1) + 1], t >> 1);
-          if (!(ok = __all_sync(0xffffffffu, ok))) break;
-          tc_fence_after();
-          issue_pv(t, 1);
-        }
-        umma_commit_on(on, &v_empty[t % NS]);
-        if (t + 2 < T) {
-          wait(&k_full[t % NS], t / NS + 1);
-          if (!(ok = __all_sync(0xffffffffu, ok))) break;
-          tc_fence_after();
-          issue_s(t + 2);
-        }
-      }
-      if (!ok && on) {
-        set_err(p.err, ERR_TIMEOUT);
-        *abort_flag = 1;
-      }
-      umma_commit_on(on, mma_done);
-      mbar_wait(mma_done, 0, WAIT_NS);
     }
   } else {
     // ---------------------------------------------------------------- softmax
