@@ -77,8 +77,8 @@ _lib: Optional[ctypes.CDLL] = None
 
 _vp, _i, _sz, _f = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_float
 _PDIMS = ctypes.POINTER(AttnDims)
-# cospec_resident_fn: (kernel, rows, block_rows, splits, user) -> resident clusters
 _PPOOL, _PROPE, _PSTR = ctypes.POINTER(Kv8PoolC), ctypes.POINTER(RopeC), ctypes.POINTER(Strides)
+# cospec_resident_fn: (kernel, rows, block_rows, splits, user) -> resident clusters
 RESIDENT_FN = ctypes.CFUNCTYPE(ctypes.c_longlong, _i, _i, _i, _i, _vp)
 
 

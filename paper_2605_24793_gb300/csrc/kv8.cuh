@@ -75,6 +75,29 @@ CS_DEV void kv8_copy_wait() {               // all but the newest N groups have 
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
+CS_DEV uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+CS_DEV void mma_f16(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+CS_DEV void mma_f16(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) { mma_f16(c, a[0], a[1], a[2], a[3], b0, b1); }
+// A power of two, -126 <= k <= 127 (0 for -127), and the exponent of one (of 0: -127).
+CS_DEV float kv8_two_to(int k) { return __uint_as_float((uint32_t)(127 + k) << 23); }
+CS_DEV float kv8_exponent(float s) { return (float)((int)(__float_as_uint(s) >> 23) - 127); }
+// Four codes as bf16 (exact), the lower two in `a`.
+CS_DEV void kv8_codes_bf16(uint32_t w, uint32_t& a, uint32_t& b) {
+  float x[4];
+  kv8_floats4(w, x);
+  a = pack_bf16(x[0], x[1]);
+  b = pack_bf16(x[2], x[3]);
+}
+
 // Two bf16 with 0 in the place of infinities and NaN.
 CS_DEV uint32_t kv8_finite_bf16x2(uint32_t w) { return w & ~__vcmpeq2(w & 0x7f807f80u, 0x7f807f80u); }
 

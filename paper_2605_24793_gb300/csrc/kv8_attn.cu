@@ -58,10 +58,6 @@ namespace {
 // Larger clusters do not all find an SM for each CTA and start later: one user at 4096 tokens took 8.3 us with clusters of
 // 12, 9.6 with 14 and 9.2 with 16; with 6 rows of 24 queries 11.7, 13.2 and 12.5.
 constexpr int MAX_SPLIT = 12;
-constexpr float P_BITS = 6.f;             // weights are held times 2^6,
-constexpr float P_ROOM = 8.f;             // and may grow by 2^8 before the output is rescaled: below f16's 2^16
-constexpr int V_ROOM = 8;                 // values' scales up to 2^8 above the least are met with f16 weights,
-constexpr int V_FAR = 64;                 // and the unit is at most 2^64 below the largest: outputs stay within fp32
 
 // MT > 0: 16 MT rows a warp, padded to the products' rows; MT < 0: 8 NT = -8 MT rows, the products' columns.
 template <int D, int MT, int RW, int NW>
@@ -93,17 +89,6 @@ struct Lay {
 
 using Params = Kv8Params;
 
-CS_DEV void mma_f16(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-CS_DEV uint32_t pack_f16(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
 CS_DEV uint4 lds128(uint32_t a) {
   uint4 v;
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
@@ -120,8 +105,6 @@ CS_DEV uint32_t lds32(uint32_t a) {
   return v;
 }
 
-CS_DEV float pow2_of(int k) { return __uint_as_float((uint32_t)(127 + k) << 23); }       // -126 <= k <= 127, 0 for -127
-
 // The values' scale in whose units outputs and weights count.  Exponents of scales are biased as fp32 holds them; 0: none.
 struct Unit {
   int e = 0;                    // of the unit
@@ -130,9 +113,8 @@ struct Unit {
   CS_DEV bool covers(int x) const { return (unsigned)(e - x) < (unsigned)span; }
   CS_DEV float scale() const { return __uint_as_float((uint32_t)e << 23); }
 };
-constexpr int ZERO_EXP = 27;    // of 2^-100, the scale of a page of zeros: it moves no unit
 
-// The unit for a tile whose pages have the exponents e0 and e1 (0: no such page); outputs so far are to be multiplied by
+// The unit for a tile whose pages have the exponents e0 and e1 (0: no such page; a page of zeros moves none); outputs so far are to be multiplied by
 // 2^by.  Returns whether the tile needs bf16 weights.
 CS_DEV bool take_scales(Unit& u, int e0, int e1, int& by) {
   const int a0 = e0 > ZERO_EXP ? e0 : 0, a1 = e1 > ZERO_EXP ? e1 : 0;
@@ -261,7 +243,7 @@ CS_DEV void follow_max(Cols<D, NT>& st, int t, float mx0, float mx1, float (&bas
 }
 template <int D, int NT>
 CS_DEV void rescale(Cols<D, NT>& st, int by) {
-  const float a = pow2_of(by / 2), b = pow2_of(by - by / 2);               // (the whole may lie outside fp32)
+  const float a = kv8_two_to(by / 2), b = kv8_two_to(by - by / 2);               // (the whole may lie outside fp32)
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -278,7 +260,7 @@ CS_DEV uint32_t turn8(uint32_t x) {
 
 template <int D, int MT>
 CS_DEV void rescale(State<D, MT>& st, int by) {
-  const float a = pow2_of(by / 2), b = pow2_of(by - by / 2);               // (the whole may lie outside fp32)
+  const float a = kv8_two_to(by / 2), b = kv8_two_to(by - by / 2);               // (the whole may lie outside fp32)
 #pragma unroll
   for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -294,7 +276,7 @@ struct PageScale {
   CS_DEV PageScale(float scale, const Unit& u) {
     const int k = (int)(__float_as_uint(scale) >> 23) - u.e, kx = max(k, -60);
     to = (float)kx;
-    back = pow2_of(-kx);
+    back = kv8_two_to(-kx);
     rest = exp2f((float)(k - kx));
   }
 };
@@ -304,14 +286,6 @@ CS_DEV uint32_t two_parts(float a, float b, uint32_t& rest) {
   rest = pack_bf16(a - __uint_as_float(u << 16), b - __uint_as_float(u & 0xffff0000u));
   return u;
 }
-// Four codes as bf16 (exact), the lower two in `a`.
-CS_DEV void codes_bf16(uint32_t w, uint32_t& a, uint32_t& b) {
-  float x[4];
-  kv8_floats4(w, x);
-  a = pack_bf16(x[0], x[1]);
-  b = pack_bf16(x[2], x[3]);
-}
-
 // One tile: two pages' keys at sk and values at sv, ks / vs their scales, n their tokens (16 both
 // unless MASK); wide, with MASK only: with bf16 weights.
 template <int D, int MT, bool MASK>
@@ -415,7 +389,7 @@ CS_DEV void tile(State<D, MT>& st, uint32_t sk, uint32_t sv, const float (&ks)[2
 #pragma unroll
       for (int d = 0; d < D / 8; ++d) {
         uint32_t b0, b1;
-        codes_bf16(load(e, d), b0, b1);
+        kv8_codes_bf16(load(e, d), b0, b1);
 #pragma unroll
         for (int t = 0; t < MT; ++t) mma_16816(st.o[t][d], p[t][e], b0, b1);
       }
@@ -523,8 +497,8 @@ CS_DEV void tile(Cols<D, NT>& st, uint32_t sk, uint32_t sv, const float (&ks)[2]
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) {
         uint32_t a[4];
-        codes_bf16(load(e, 2 * i), a[0], a[2]);
-        codes_bf16(load(e, 2 * i + 1), a[1], a[3]);
+        kv8_codes_bf16(load(e, 2 * i), a[0], a[2]);
+        kv8_codes_bf16(load(e, 2 * i + 1), a[1], a[3]);
 #pragma unroll
         for (int t = 0; t < NT; ++t) mma_16816(st.o[t][i], a, p[t][e][0], p[t][e][1]);
       }

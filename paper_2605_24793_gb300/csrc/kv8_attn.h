@@ -5,6 +5,13 @@
 
 namespace cospec {
 
+// Weights are held times 2^P_BITS and may grow by 2^P_ROOM before the output is rescaled: below f16's 2^16.
+constexpr float P_BITS = 6.f, P_ROOM = 8.f;
+// Values' scales up to 2^V_ROOM above the least are met with f16 weights, and the unit that outputs count in is at most 2^V_FAR
+// below the largest scale, so that outputs stay within fp32.
+constexpr int V_ROOM = 8, V_FAR = 64;
+constexpr int ZERO_EXP = 27;              // biased exponent of 2^-100, the scale of a page of zeros
+
 struct Kv8Params {
   Kv8Pool pool;
   Kv8Src q, k_blk, v_blk;

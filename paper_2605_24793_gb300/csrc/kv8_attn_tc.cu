@@ -45,9 +45,6 @@ constexpr int THREADS = 16 * 32;
 constexpr int NS = 2;                     // operand stages
 constexpr int QB = 2;                     // query rows that a lane group loads at once (1: 73.6 us at 104 rows and batch 16, 2 72.1, 4 75.3, 8 76)
 constexpr int SLOTS = 2;                  // pieces (two pages' keys or values) on their way per converting warp
-constexpr float P_BITS = 6.f, P_ROOM = 8.f;
-constexpr int V_ROOM = 8, V_FAR = 64;     // as in kv8_attn.cu
-constexpr int ZERO_EXP = 27;
 constexpr float TINY = 1.2e-38f;          // a score factor is never 0: -inf stays -inf
 constexpr uint64_t WAIT_NS = 2000000000ull;
 
@@ -84,22 +81,15 @@ struct TL {
 constexpr uint32_t BF16_BOTH = (1u << 7) | (1u << 10);
 constexpr uint32_t idesc_f16(int M, int N) { return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24); }
 
-CS_DEV uint32_t pack_f16(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
 CS_DEV uint4 codes_f16(uint32_t a, uint32_t b) {        // eight codes
   return make_uint4(kv8_f16x2(a), kv8_f16x2_hi(a), kv8_f16x2(b), kv8_f16x2_hi(b));
 }
 CS_DEV uint4 codes_bf16(uint32_t a, uint32_t b) {       // the same in bf16 (exact)
-  float x[4], y[4];
-  kv8_floats4(a, x);
-  kv8_floats4(b, y);
-  return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+  uint4 r;
+  kv8_codes_bf16(a, r.x, r.y);
+  kv8_codes_bf16(b, r.z, r.w);
+  return r;
 }
-CS_DEV float exponent_of(float s) { return (float)((int)(__float_as_uint(s) >> 23) - 127); }
-CS_DEV float pow2_of(int k) { return __uint_as_float((uint32_t)(127 + k) << 23); }       // -126 <= k <= 127, 0 for -127
 CS_DEV float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 CS_DEV float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 CS_DEV float amax8(float m, uint4 v) {
@@ -215,7 +205,7 @@ CS_DEV RowState soft_parts(uint32_t srow, uint32_t orow, int parts, int lim, flo
   if (blk) {                                              // its values may not take the outputs out of fp32
     const int was = st.unit, far = most - V_FAR;
     st.unit = max(max(was, ZERO_EXP), was ? min(far, was + 126) : far);
-    if (was) alpha *= pow2_of(was - st.unit);
+    if (was) alpha *= kv8_two_to(was - st.unit);
   }
   st.ok = 1;
   if (__any_sync(0xffffffffu, alpha != 1.f && t > 0)) {
@@ -241,7 +231,7 @@ CS_DEV RowState soft_parts(uint32_t srow, uint32_t orow, int parts, int lim, flo
     // (no further down than 2^-60, which the sum needs; the rest of the way by a factor)
     const float vs = __shfl_sync(0xffffffffu, scales.y, (t & 7) * 4 + (c >> 1));
     const int k0 = blk ? 127 - st.unit : (int)(__float_as_uint(vs) >> 23) - st.unit, kx = blk ? 0 : max(k0, -60);
-    const float to = nb + (float)kx, w = pow2_of(max(k0 - kx, -127));
+    const float to = nb + (float)kx, w = kv8_two_to(max(k0 - kx, -127));
     float sum = 0.f;
     uint32_t pk[4], rest[4];
 #pragma unroll
@@ -251,7 +241,7 @@ CS_DEV RowState soft_parts(uint32_t srow, uint32_t orow, int parts, int lim, flo
       pk[k] = blk || wide ? pack_bf16(a * w, b * w) : pack_f16(a, b);
       rest[k] = pack_bf16(fmaf(a, w, -bf_lo(pk[k])), fmaf(b, w, -bf_hi(pk[k])));
     }
-    st.l = fmaf(sum, pow2_of(-kx), st.l);
+    st.l = fmaf(sum, kv8_two_to(-kx), st.l);
     tq_st4(srow + c * 4, pk);                             // over scores that have been read
     if (blk) tq_st4(srow + 64 + c * 4, rest);             // the other half's, which the block does not use
   }
@@ -812,7 +802,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
               pk[e * 8 + k] = pack_f16(a.x, a.y);
             }
             s2[0] = add2(s2[0], s2[1]);
-            l = fmaf(s2[0].x + s2[0].y, pow2_of(-kx), l);
+            l = fmaf(s2[0].x + s2[0].y, kv8_two_to(-kx), l);
           }
           tq_st16(srow + e0 * 8, pk);
         };
@@ -871,7 +861,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv8_attn_tc_kernel(const Kv8Params
     // (in one order in both groups: the sum is the same number)
     const float sum = grp ? lo * wo + l * wm : l * wm + lo * wo;
     // Outputs stay in units of the values' until a weight takes the exponent in: a product with the unit could leave fp32.
-    const float tm = mref + exponent_of(vref), to = mo + exponent_of(vo), most = fmaxf(tm, to);
+    const float tm = mref + kv8_exponent(vref), to = mo + kv8_exponent(vo), most = fmaxf(tm, to);
     const float pm = mref == -INFINITY ? 0.f : exp2_approx(tm - most), po = mo == -INFINITY ? 0.f : exp2_approx(to - most);
     const float w0 = grp ? po : pm, w1 = grp ? pm : po;
     const bool have1 = have && n > 0;       // half 1 holds cache tiles only

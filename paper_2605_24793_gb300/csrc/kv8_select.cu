@@ -47,17 +47,6 @@ CS_DEV uint32_t ordered(float x) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 CS_DEV float score_of(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
-CS_DEV void mma_f16(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint2 b) {
-  asm(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b.x), "r"(b.y));
-}
-CS_DEV uint32_t pack_f16(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
 
 // The sequence of the launch's z-th slot and its context, longest first (ties in order), so that long ones start early:
 // as sequence_by_rank, by all the block's threads over a copy in shared memory (16 sequences of 8 rows 36.3 -> 35.5 us).
@@ -256,7 +245,7 @@ __global__ void __launch_bounds__(CT, CTAS) kv8_select_kernel(const Kv8SelectArg
 #pragma unroll
         for (int i = 0; i < 2; ++i)
           mma_f16(acc[i], __byte_perm(y[2 * i], 0u, 0x4140), __byte_perm(y[2 * i + 1], 0u, 0x4140), __byte_perm(y[2 * i], 0u, 0x4342),
-                  __byte_perm(y[2 * i + 1], 0u, 0x4342), v);
+                  __byte_perm(y[2 * i + 1], 0u, 0x4342), v.x, v.y);
       }
       // page g + 8 i: its two columns are parts 2 (i & 1) and 2 (i & 1) + 1 of tile i >> 1
       const int jt = tiles_per_row ? t / tiles_per_row : t << (3 - pl.log_heads);
