@@ -546,7 +546,10 @@ COSPEC_API int cospec_kv8_select(const cospec_attn_dims* dims, const cospec_kv8_
  * layer `layer` and the block's rows (their own bf16 keys and values), causal or full inside the
  * block.  With sel (cospec_kv8_select) row j of KV head h reads only the cached positions of the pages
  * sel[b][j][h][0..pages-1]: logical pages, no page twice, the list ended by its first -1 (what stands
- * behind that is not read); positions at or after ctx_len[b] are not read.  A page outside the sequence or
+ * behind that is not read); positions at or after ctx_len[b] are not read.  What a row does not see does
+ * not reach it, infinities and NaN included, nor does the size of its values cost others precision: weights
+ * are held to 2^-11 and better, to 2^-8 where the values' scales of a sequence and head differ by more than
+ * 2^8, and those below 2^-22 of a row's largest may be 0 in the former case.  A page outside the sequence or
  * the pool sets COSPEC_DEVERR_PAGE and is skipped.
  *
  *    q, k_blk, v_blk  bf16 with strides (layer unused); out bf16 [batch, rows, num_q_heads, head_dim]

@@ -8,17 +8,18 @@
 //   columns: the query rows are the products' columns, eight at a time, keys and values their rows, so that up to 8 and 17
 //   to 24 rows are padded less than by 16.  A warp a ring and two CTAs an SM: six warps with rings of two tiles up to 8
 //   rows, four with rings of three at 24 (as registers allow).  Up to 8 rows, with six warps, four, eight (one CTA an SM)
-//   and padded: one user at 4096 tokens 7.3, 7.5, 7.9, 8.3 us, at 32768 20.5, 24.3, 20.2, 26.5; 128 selected pages for
-//   each of 128 rows 83, 91, -, 103.  At 24 rows: batch 16 at 2048 to 8192 tokens 50 us, padded 57; batch 64 at 8192 to
-//   32768 472, padded 538;
+//   and padded: one user at 4096 tokens 7.1, 7.1, 8.4, 7.9 us, at 32768 20.1, 22.8, 23.8, 25.5; 128 selected pages for
+//   each of 128 rows 84, 92, 107, 104.  At 24 rows: batch 16 at 2048 to 8192 tokens 49.5 us, padded 53.7; batch 64 at 8192
+//   to 32768 481, padded 547;
 //   rows: the query rows are the products' rows, by 16, which is as good where they fill them and has fewer shuffles: batch
-//   64 at 32 rows 538 us for 564, at 12 rows one user 8.3 for 9.2.  Up to 16 a warp a ring, four warps and two CTAs an SM
-//   or eight and one (long contexts of few users: one user at 32768 tokens 26.5 us and 22.3, at 4096 8.3 and 9.0); up to
+//   64 at 32 rows 552 us for 613, at 12 rows one user 8.4 for 9.1.  Up to 16 a warp a ring, four warps and two CTAs an SM
+//   or eight and one (long contexts of few users: one user at 32768 tokens 26.0 us and 21.7, at 4096 8.4 and 9.8); up to
 //   32 a warp of 32 rows a ring (each code converted once), or two of 16 (half the registers, shorter steps) with four
 //   warps and three CTAs an SM or with eight.  A warp of 32, two of four, two of eight at 32 rows: one user at 4096 tokens
-//   12.1, 11.7, 10.4 us; batch 32 at 2048 to 16384 138, 157, 164; batch 64 at 8192 to 32768 537, 627, 706.
-// More rows go to the tcgen05 kernel (kv8_attn_tc.cu): at 64 rows two groups of 32 here took 95 us where that takes 70
-// (batch 16, 2048 to 8192 tokens), at 40 91 and 70, at 32 66 and 68; batch 64 540 and 756 at 32 rows, 1011 and 759 at 40.
+//   11.3, 12.4, 10.3 us; batch 32 at 2048 to 16384 138, 161, 166; batch 64 at 8192 to 32768 552, 643, 710.
+// More rows go to the tcgen05 kernel (kv8_attn_tc.cu): at 64 rows two groups of 32 here take 89 us where that takes 68
+// (batch 16, 2048 to 8192 tokens), at 40 86 and 67, at 32 55 and 65; batch 64 552 and 666 at 32 rows, 1039 and 681 at 40.
+// One user's 64 rows: 9.1 and 13.2 us at 256 tokens, 10.8 and 12.8 at 1024, 15.3 and 14.1 at 4096, 49 and 35 at 32768.
 //
 // q . k^T and p . v run on mma.m16n8k16 with f16 operands.  An e4m3 code is exact in f16; q is brought
 // to f16 by a power of two per row (bf16's 8 bits fit f16's 11, values 2^-14 below the row's largest
@@ -37,11 +38,11 @@
 // the two pages' keys makes the loads conflict-free.
 //
 // The block's keys and values (bf16, up to 64) go 16 at a time to the warps of the cluster's last CTA, on
-// bf16 operands.  The warps' partial (max, sum, output) meet in shared memory, the CTAs' in
+// bf16 operands, the weights in two parts.  The warps' partial (max, sum, output) meet in shared memory, the CTAs' in
 // distributed shared memory, each CTA finishing a slice of the rows.
 //
 // One row at batch 64, 8192 to 32768 tokens (dimension 128, 8 KV heads): 400 us, 6.7 TB/s, the memory's rate.  32 rows
-// there: 538 us, 5.0 TB/s: a tile takes an SM 500 cycles, its 128 products 260 of them, the rest latencies that two warps
+// there: 552 us, 4.9 TB/s: a tile takes an SM 500 cycles, its 128 products 260 of them, the rest latencies that two warps
 // a scheduler leave.  One user is latency: at 4096 tokens 2 us to the first tile, 0.8 to 1.3 a tile, 2 to 3 for the parts.
 #include <math.h>
 
@@ -114,8 +115,8 @@ struct Unit {
   CS_DEV float scale() const { return __uint_as_float((uint32_t)e << 23); }
 };
 
-// The unit for a tile whose pages have the exponents e0 and e1 (0: no such page; a page of zeros moves none); outputs so far are to be multiplied by
-// 2^by.  Returns whether the tile needs bf16 weights.
+// The unit for a tile whose pages have the exponents e0 and e1 (0: no such page; a page of zeros moves none); outputs so far
+// are to be multiplied by 2^by.  Returns whether the tile needs bf16 weights.
 CS_DEV bool take_scales(Unit& u, int e0, int e1, int& by) {
   const int a0 = e0 > ZERO_EXP ? e0 : 0, a1 = e1 > ZERO_EXP ? e1 : 0;
   const int hi = max(a0, a1), lo = a0 && a1 ? min(a0, a1) : hi, was = u.e;

@@ -20,10 +20,11 @@
 // and values for all of them (kv8_attn.cu says why).  The block's keys come to f16 by a power of two per key, its values stay
 // bf16 and its weights are two bf16 numbers each, the second what the first leaves over.
 //
-// 104 rows, batch 16 at 2048 to 8192 tokens: 73 us.  A softmax warp works four fifths of a tile's time (a quarter of it on
-// the maxima of 64 keys, two fifths on their weights) beside the converting warps on its scheduler, which wait a quarter of
-// theirs for free stages: instructions bound it, and fetching them (75.6 us before the start and the block were in rolled
-// loops); the tensor pipe is busy for 25 %, shared memory for 23.  Codes loaded to registers past the ring, behind
+// 104 rows, batch 16 at 2048 to 8192 tokens: 75 us; 64 rows, batch 64 at 8192 to 32768: 684.  A softmax warp works four fifths
+// of a tile's time (a quarter of it on the maxima of 64 keys, two fifths on their weights) beside the converting warps on its
+// scheduler, which wait a quarter of theirs for free stages: instructions bound it, and fetching them (the roles' loops share
+// an instruction cache: masks and bf16 weights inside them cost a third, the order of the roles in this file up to 4 %); the
+// tensor pipe is busy for 20 %, shared memory for 26.  Codes loaded to registers past the ring, behind
 // prefetches to L2, cost 10 us, the next tile's scores loaded behind this one's weights 5.
 #include <math.h>
 
