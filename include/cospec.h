@@ -562,6 +562,101 @@ COSPEC_API int cospec_kv8_attn(const cospec_attn_dims* dims, int max_ctx,
                                const int32_t* ctx_len, const int32_t* sel, int pages,
                                uint16_t* out, void* stream);
 
+/* ------------------------------------------------------------------------ */
+/* 7. Low-rank adapters beside a shared projection (Sec. 3.3: the arbitrator is the draft's
+ *    backbone with adapters of rank 16, scale 32, dropout 0.05).  Every row of a batch has its own
+ *    adapter or none, so drafting rows, arbitrator rows and rows of several arbitrators share one pass.
+ *
+ *    With a = adapter[m] and c_a = scaling[a] / (1 - p):
+ *      u[m]  = c_a drop(x[m]) A_a^T                               (zeros where a = -1)
+ *      y[m]  = x[m] W^T + u[m] B_a^T
+ *    and for the gradients (W stays as it is), with t[m] = c_a dy[m] B_a:
+ *      dx[m] = dy[m] W + keep[m] * (t[m] A_a)
+ *      dA_a  = sum over the rows of a of t[m]^T drop(x[m]),   dB_a = sum of dy[m]^T u[m].
+ *    drop(x)[m][k] = keep[m][k] x[m][k].  keep[m][k] is 1 where the 16 bits number k mod 8 (low
+ *    half of a word first) of Philox4x32-10 at counter (floor(k / 8), m, site, 2) under the key (seed mod
+ *    2^32, floor(seed / 2^32)) are at least thr = floor(65536 dropout + 1/2), and p = thr / 65536.  The mask is
+ *    drawn anew wherever it is needed and never stored: a backward call with the forward call's seed, site and
+ *    dropout sees the same one.
+ *
+ *    Products are of bf16 values with fp32 sums; u and t are fp32 and enter the second products as two bf16
+ *    parts (16 bits; three, all of fp32, in dA and dB), y and dx are rounded once.  A row is not
+ *    reached by what stands in other rows or in other rows' adapters; where x, dy or a factor that a row uses holds
+ *    an infinity, an infinite result of that row may come out as NaN.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  int rows;              /* M >= 0 */
+  int in_features;       /* K: a multiple of 8 */
+  int out_features;      /* N: a multiple of 8 */
+  int rank;              /* r: a multiple of 8 up to 128; a smaller adapter's factors end in zeros */
+  int num_adapters;      /* 1 .. 65535 */
+  float dropout;         /* in [0, 1): 0 draws nothing */
+  uint32_t site;         /* number of the place (layer, projection) whose mask this is */
+  long long x_stride;    /* elements between rows of x, of y and dy, and of dx: multiples of 8, */
+  long long y_stride;    /* at least the row's length; 0: dense */
+  long long dx_stride;
+} cospec_lora_dims;
+
+#define COSPEC_DEVERR_ADAPTER 64 /* an adapter id outside [-1, num_adapters): the row has none */
+
+/*    x        bf16 [M, K]             w  bf16 [N, K] (nn.Linear layout)
+ *    a        bf16 [adapters, r, K]   b  bf16 [adapters, N, r]
+ *    scaling  float32 [adapters]: e.g. 32 / 16
+ *    adapter  int32 [M] in [-1, adapters)
+ *    seed     DEVICE pointer to one uint64 (8-byte aligned), read when the kernels run; may be NULL when
+ *             dropout = 0
+ *    u        float32 [M, r], written: the backward call reads it
+ *    y        bf16 [M, N]
+ *  All but scaling, adapter and seed 16-byte aligned; y and u may not alias inputs.  The call allocates nothing
+ *  and needs no workspace.  Rows of one adapter side by side are fastest. */
+COSPEC_API int cospec_lora_forward(const cospec_lora_dims* dims, const uint16_t* x, const uint16_t* w,
+                                   const uint16_t* a, const uint16_t* b, const float* scaling,
+                                   const int32_t* adapter, const uint64_t* seed, float* u, uint16_t* y,
+                                   void* stream);
+
+#define COSPEC_LORA_ACCUMULATE 1   /* da and db are added to, not set */
+
+/*    dy       bf16 [M, N];  x, w, a, b, scaling, adapter, seed as in the forward call;  u its result
+ *    t        float32 [M, r], written (scratch)
+ *    dx       bf16 [M, K], or NULL: not wanted (w is then not read)
+ *    da, db   float32 [adapters, r, K] and [adapters, N, r], each or NULL; an adapter without rows gets
+ *             zeros (or stays as it is, with COSPEC_LORA_ACCUMULATE)
+ *  Every sum has a fixed order: repeated calls agree bit for bit. */
+COSPEC_API int cospec_lora_backward(const cospec_lora_dims* dims, const uint16_t* dy, const uint16_t* x,
+                                    const uint16_t* w, const uint16_t* a, const uint16_t* b,
+                                    const float* scaling, const int32_t* adapter, const uint64_t* seed,
+                                    const float* u, float* t, uint16_t* dx, float* da, float* db,
+                                    int flags, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* 8. The RL stage's objective through the decision MLP, with its gradient (Sec. 3.4; the policy is
+ *    cospec_arbitrate's in mode 0).
+ *
+ *    For every effective decision -- eff[r][i] != 0 at a position where draft and argmax differ -- with the
+ *    features f of cospec_arbitrate, z = w2 . relu(W1 f + b1) + b2, p = sigma(z), pi(a) = p for accept != 0
+ *    and 1 - p else, ratio = pi(a) / pi_old(a) and A = adv:
+ *      loss[0] = sum min(ratio A, clip(ratio, 1 -+ clip_eps) A),  loss[1] = sum of the entropies of p,
+ *      loss[2] = sum KL(p || p_ref),  loss[3] = -loss[0] - beta_h loss[1] + beta_kl loss[2]
+ *    and the gradient of grad_scale * loss[3]: dz for the logits, dw1, db1, dw2, db2 for the weights.  (cospec_rl_advantages
+ *    gives eff and, as adv_dec, adv; cospec_arbitrate's p_out is p_old.)
+ *
+ *    draft int32 [R, K]; argmax int32 [R, K+1]; stats float32 [R, K+1, 5]; accept, eff uint8 [R, K];
+ *    adv, p_old, p_ref float32 [R, K], read at effective decisions: probabilities between 0 and 1, p_ref neither, p_old
+ *    not 0 for the action taken (else the terms are infinite or NaN, as the formulas say)
+ *    w1 float32 [mlp_hidden, 8], b1, w2 [mlp_hidden], b2 [1] (device)
+ *    loss float32 [4]; p_new, dz float32 [R, K] (0 outside effective decisions); dw1, db1, dw2, db2 as the weights
+ *    params: clip_eps >= 0, beta_h and beta_kl are used
+ *    ws >= cospec_arbitrate_loss_workspace(mlp_hidden) bytes, 16-byte aligned (no initialisation)
+ *    Supported: 1 <= K <= 64, R * K < 2^31 - 512, 1 <= mlp_hidden <= 1024.  Every sum has a fixed order. */
+COSPEC_API size_t cospec_arbitrate_loss_workspace(int mlp_hidden);
+COSPEC_API int cospec_arbitrate_loss(int num_rounds, int K, const int32_t* draft, const int32_t* argmax,
+                                     const float* stats, int mlp_hidden, const float* w1, const float* b1,
+                                     const float* w2, const float* b2, const uint8_t* accept,
+                                     const uint8_t* eff, const float* adv, const float* p_old,
+                                     const float* p_ref, const cospec_rl_params* params, float grad_scale,
+                                     float* loss, float* p_new, float* dz, float* dw1, float* db1,
+                                     float* dw2, float* db2, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

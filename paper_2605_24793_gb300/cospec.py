@@ -20,6 +20,7 @@ LIB_PATH = os.path.join(_HERE, "libcospec.so")
 POLICY_MLP, POLICY_TARGET, POLICY_DRAFT = 0, 1, 2
 DEVERR_PAGE, DEVERR_CTX, DEVERR_TOKEN, DEVERR_TIMEOUT, DEVERR_OFFSETS = 1, 2, 4, 8, 16
 DEVERR_POSITION = 32
+DEVERR_ADAPTER = 64
 
 EXPORTED = ("cospec_status_string", "cospec_last_cuda_error", "cospec_get_device_error", "cospec_num_sms",
             "cospec_verify_attn", "cospec_lmhead_workspace", "cospec_lmhead_argmax_features",
@@ -27,7 +28,8 @@ EXPORTED = ("cospec_status_string", "cospec_last_cuda_error", "cospec_get_device
             "cospec_lmhead_sample_features", "cospec_verify_attn_plan", "cospec_rl_workspace",
             "cospec_rl_advantages", "cospec_verify_attn_plan_model",
             "cospec_lmhead_logits_features", "cospec_sps_workspace", "cospec_sps_accept", "cospec_accept_commit_launches",
-            "cospec_verify_attn_variant", "cospec_kv8_append", "cospec_kv8_select", "cospec_kv8_attn")
+            "cospec_verify_attn_variant", "cospec_kv8_append", "cospec_kv8_select", "cospec_kv8_attn", "cospec_lora_forward",
+            "cospec_lora_backward", "cospec_arbitrate_loss_workspace", "cospec_arbitrate_loss")
 
 
 class AttnDims(ctypes.Structure):
@@ -67,6 +69,16 @@ class RopeC(ctypes.Structure):
 class Strides(ctypes.Structure):
     """cospec_kv8_strides."""
     _fields_ = [(n, ctypes.c_longlong) for n in ("layer", "batch", "row")]
+
+
+class LoraDims(ctypes.Structure):
+    """cospec_lora_dims."""
+    _fields_ = [(n, ctypes.c_int) for n in ("rows", "in_features", "out_features", "rank", "num_adapters")] + [
+        ("dropout", ctypes.c_float), ("site", ctypes.c_uint32)] + [
+        (n, ctypes.c_longlong) for n in ("x_stride", "y_stride", "dx_stride")]
+
+
+LORA_ACCUMULATE = 1
 
 
 class CospecError(RuntimeError):
@@ -124,6 +136,13 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "cospec_kv8_attn": (_i, [_PDIMS, _i, _PPOOL, _i, _vp, _PSTR, _vp, _PSTR, _vp, _PSTR, _vp, _vp, _vp, _i,
                                  _vp, _vp]),
     }
+    sig.update({
+        "cospec_lora_forward": (_i, [ctypes.POINTER(LoraDims)] + [_vp] * 10),
+        "cospec_lora_backward": (_i, [ctypes.POINTER(LoraDims)] + [_vp] * 13 + [_i, _vp]),
+        "cospec_arbitrate_loss_workspace": (_sz, [_i]),
+        "cospec_arbitrate_loss": (_i, [_i, _i, _vp, _vp, _vp, _i] + [_vp] * 9 + [ctypes.POINTER(RLParams), _f] + [_vp] * 8
+                                  + [_sz, _vp]),
+    })
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
         fn.restype = res
@@ -788,3 +807,117 @@ def get_device_error(stream=None) -> int:
     if st not in (0, -5):
         _check(st)
     return flags.value
+
+
+# ---------------------------------------------------------------- low-rank adapters
+def _req_rows(t: torch.Tensor, dtype, name: str, rows: int, width: int) -> int:
+    """A [rows, width] tensor whose rows may be parts of a wider buffer's; returns its row stride."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: must be a CUDA tensor")
+    _need(tuple(t.shape) == (rows, width), f"{name} must be [{rows}, {width}]")
+    _need(t.stride(1) == 1 or width == 1, f"{name}: values of a row must be side by side")
+    stride = t.stride(0) if rows > 1 else width
+    _need(stride >= width and stride % 8 == 0, f"{name}: rows must not overlap and lie a multiple of 8 elements apart")
+    return int(stride)
+
+
+def _lora_dims(w, a, b, scaling, adapter, dropout: float, seed, site: int) -> LoraDims:
+    """Checks what the two passes share: w [N, K], a [n, r, K], b [n, N, r], scaling [n], adapter [M], an int64 seed."""
+    for t, n, d in ((w, "w", 2), (a, "a", 3), (b, "b", 3)):
+        _req(t, torch.bfloat16, n, d)
+    _req(scaling, torch.float32, "scaling", 1)
+    _req(adapter, torch.int32, "adapter", 1)
+    N, K = w.shape
+    n, r = a.shape[:2]
+    _need(a.shape[2] == K, "a must be [adapters, rank, in_features]")
+    _need(tuple(b.shape) == (n, N, r), "b must be [adapters, out_features, rank]")
+    _need(scaling.shape[0] == n, "scaling must hold a value per adapter")
+    _need(0 <= site < 1 << 32, "site must be a 32-bit number")
+    if seed is not None:
+        _req(seed, torch.int64, "seed")
+        _need(seed.numel() == 1, "seed must hold one value")
+    return LoraDims(adapter.shape[0], K, N, r, n, float(dropout), int(site), 0, 0, 0)
+
+
+def lora_forward(x, w, a, b, scaling, adapter, y, u, dropout: float = 0.0, seed=None, site: int = 0, stream=None):
+    """y = x W^T + s_a drop(x) A_a^T B_a^T, every row with its own adapter (-1: none).  x [M, K], w [N, K], a [n, r, K],
+    b [n, N, r] bf16, scaling [n] float32, adapter [M] int32; fills y [M, N] bf16 and u [M, r] float32, which the backward
+    pass reads.  x and y may be columns of wider buffers.  ``seed``: an int64 device scalar, read when the kernels run;
+    ``site``: the number of the place whose dropout mask this is."""
+    d = _lora_dims(w, a, b, scaling, adapter, dropout, seed, site)
+    d.x_stride = _req_rows(x, torch.bfloat16, "x", d.rows, d.in_features)
+    d.y_stride = _req_rows(y, torch.bfloat16, "y", d.rows, d.out_features)
+    _req(u, torch.float32, "u", 2)
+    _need(tuple(u.shape) == (d.rows, d.rank), "u must be [rows, rank]")
+    _same_device(x, w, a, b, scaling, adapter, y, u, seed)
+    _check(load_library().cospec_lora_forward(ctypes.byref(d), _ptr(x), _ptr(w), _ptr(a), _ptr(b), _ptr(scaling), _ptr(adapter),
+                                              _ptr(seed), _ptr(u), _ptr(y), _stream(stream)))
+    return y
+
+
+def lora_backward(dy, x, w, a, b, scaling, adapter, u, dx, da, db, t, dropout: float = 0.0, seed=None, site: int = 0,
+                  accumulate: bool = False, stream=None):
+    """The gradients of lora_forward for x and the adapters: dx [M, K] bf16, da [n, r, K] and db [n, N, r] float32 (each
+    or None), from dy [M, N], the forward pass's inputs and its u.  t [M, r] float32 is scratch.  ``accumulate``: da and
+    db are added to."""
+    d = _lora_dims(w, a, b, scaling, adapter, dropout, seed, site)
+    d.y_stride = _req_rows(dy, torch.bfloat16, "dy", d.rows, d.out_features)
+    d.x_stride = _req_rows(x, torch.bfloat16, "x", d.rows, d.in_features)
+    for z, n in ((u, "u"), (t, "t")):
+        _req(z, torch.float32, n, 2)
+        _need(tuple(z.shape) == (d.rows, d.rank), f"{n} must be [rows, rank]")
+    if dx is not None:
+        d.dx_stride = _req_rows(dx, torch.bfloat16, "dx", d.rows, d.in_features)
+    for z, like, n in ((da, a, "da"), (db, b, "db")):
+        if z is not None:
+            _req(z, torch.float32, n, 3)
+            _need(z.shape == like.shape, f"{n} must have {n[1:]}'s shape")
+    _same_device(dy, x, w, a, b, scaling, adapter, u, dx, da, db, t, seed)
+    _check(load_library().cospec_lora_backward(ctypes.byref(d), _ptr(dy), _ptr(x), _ptr(w), _ptr(a), _ptr(b), _ptr(scaling),
+                                               _ptr(adapter), _ptr(seed), _ptr(u), _ptr(t), _ptr(dx), _ptr(da), _ptr(db),
+                                               LORA_ACCUMULATE if accumulate else 0, _stream(stream)))
+    return dx, da, db
+
+
+# ---------------------------------------------------------------- policy loss
+def arbitrate_loss(draft, argmax, stats, w1, b1, w2, b2, accept, eff, adv, p_old, p_ref, params: RLParams = None,
+                   grad_scale: float = 1.0, out: Optional[dict] = None, stream=None) -> dict:
+    """The RL stage's objective through the decision MLP and its gradient (Sec. 3.4) over R recorded rounds: draft
+    [R, K], argmax [R, K+1], stats [R, K+1, 5] as cospec_arbitrate takes them, accept / eff uint8 and adv / p_old / p_ref
+    float32 [R, K], the MLP's w1 [H, 8], b1, w2 [H], b2 [1].  Returns loss [4], p_new and dz [R, K], dw1, db1, dw2, db2 (the
+    gradients times ``grad_scale``) and ``ws``; ``out``: an earlier call's result, whose tensors are filled again."""
+    params = params if params is not None else RLParams()
+    _req(draft, torch.int32, "draft", 2)
+    _req(argmax, torch.int32, "argmax", 2)
+    _req(stats, torch.float32, "stats", 3)
+    R, K = draft.shape
+    _need(tuple(argmax.shape) == (R, K + 1) and tuple(stats.shape) == (R, K + 1, 5), "argmax / stats must hold K+1 rows per round")
+    _req(w1, torch.float32, "w1", 2)
+    H = w1.shape[0]
+    _need(w1.shape[1] == 8, "w1 must be [H, 8]")
+    for t, n, m in ((b1, "b1", H), (w2, "w2", H), (b2, "b2", 1)):
+        _req(t, torch.float32, n)
+        _need(t.numel() == m, f"{n} must hold {m} values")
+    for t, n, dt in ((accept, "accept", torch.uint8), (eff, "eff", torch.uint8), (adv, "adv", torch.float32),
+                     (p_old, "p_old", torch.float32), (p_ref, "p_ref", torch.float32)):
+        _req(t, dt, n, 2)
+        _need(tuple(t.shape) == (R, K), f"{n} must be [R, K]")
+    _same_device(draft, argmax, stats, w1, b1, w2, b2, accept, eff, adv, p_old, p_ref)
+    lib = load_library()
+    ws_bytes = lib.cospec_arbitrate_loss_workspace(H)
+    shapes = dict(loss=(4,), p_new=(R, K), dz=(R, K), dw1=(H, 8), db1=(H,), dw2=(H,), db2=(1,))
+    if out is None:
+        out = {n: torch.empty(s, dtype=torch.float32, device=draft.device) for n, s in shapes.items()}
+        out["ws"] = torch.empty(max(1, ws_bytes), dtype=torch.uint8, device=draft.device)
+    for n, s in shapes.items():
+        _req(out[n], torch.float32, n)
+        _need(tuple(out[n].shape) == s, f"{n} must be {list(s)}")
+    _req(out["ws"], torch.uint8, "ws", 1)
+    _same_device(*out.values())
+    _check(lib.cospec_arbitrate_loss(
+        R, K, _ptr(draft), _ptr(argmax), _ptr(stats), H, _ptr(w1), _ptr(b1), _ptr(w2), _ptr(b2), _ptr(accept), _ptr(eff), _ptr(adv),
+        _ptr(p_old), _ptr(p_ref), ctypes.byref(params), float(grad_scale), *(_ptr(out[n]) for n in shapes), _ptr(out["ws"]),
+        out["ws"].numel(), _stream(stream)))
+    return out

@@ -91,7 +91,7 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 bool encode_tensor_map_bf16(void* map, const void* base, int rank, const uint64_t* dims,
-                            const uint64_t* strides, const uint32_t* box) {
+                            const uint64_t* strides, const uint32_t* box, int swizzle) {
   static std::atomic<EncodeTiledFn> fn_cache{nullptr};
   EncodeTiledFn fn = fn_cache.load(std::memory_order_acquire);
   if (!fn) {
@@ -116,7 +116,7 @@ bool encode_tensor_map_bf16(void* map, const void* base, int rank, const uint64_
   }
   return fn(static_cast<CUtensorMap*>(map), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank,
             const_cast<void*>(base), d, st, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            swizzle == 32 ? CU_TENSOR_MAP_SWIZZLE_32B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -675,6 +675,132 @@ COSPEC_API int cospec_kv8_attn(const cospec_attn_dims* d, int max_ctx, const cos
   int* err = device_error_word();
   if (!err) return cuda_lookup_failed();
   return cuda_status(launch_kv8_attn(a, err, static_cast<cudaStream_t>(stream)));
+}
+
+// ---------------------------------------------------------------- low-rank adapters
+// The checks shared by the two passes; x or dy may be the rows that come in.
+static int lora_args(const cospec_lora_dims* d, const uint64_t* seed, LoraArgs* p) {
+  CS_CHECK_ARG(d && d->rows >= 0 && d->in_features >= 1 && d->out_features >= 1 && d->rank >= 1 && d->num_adapters >= 1);
+  CS_CHECK_ARG(d->dropout >= 0.f && d->dropout < 1.f);
+  if (d->in_features % 8 != 0 || d->out_features % 8 != 0 || d->rank % 8 != 0 || d->rank > 128 || d->num_adapters > 65535)
+    return COSPEC_ERR_UNSUPPORTED;
+  // 32-bit element offsets inside the kernels' tiles, and a launch's rows and columns
+  if (d->in_features > (1 << 24) || d->out_features > (1 << 24) || d->rows > 8 << 20) return COSPEC_ERR_UNSUPPORTED;
+  const double thr = floor((double)d->dropout * 65536.0 + 0.5);
+  if (thr > 65535.0) return COSPEC_ERR_UNSUPPORTED;
+  CS_CHECK_ARG(thr == 0.0 || (seed && (reinterpret_cast<uintptr_t>(seed) & 7u) == 0));
+  const long long K = d->in_features, N = d->out_features;
+  p->ldx = d->x_stride ? d->x_stride : K;
+  p->ldy = d->y_stride ? d->y_stride : N;
+  p->lddx = d->dx_stride ? d->dx_stride : K;
+  CS_CHECK_ARG(p->ldx >= K && p->ldy >= N && p->lddx >= K);
+  CS_CHECK_ARG(p->ldx % 8 == 0 && p->ldy % 8 == 0 && p->lddx % 8 == 0);
+  if (p->ldx > 1LL << 30 || p->ldy > 1LL << 30 || p->lddx > 1LL << 30) return COSPEC_ERR_UNSUPPORTED;
+  p->M = d->rows;
+  p->K = d->in_features;
+  p->N = d->out_features;
+  p->r = d->rank;
+  p->n = d->num_adapters;
+  p->thr = (uint32_t)thr;
+  p->site = d->site;
+  p->seed = reinterpret_cast<const unsigned long long*>(seed);
+  return COSPEC_OK;
+}
+
+COSPEC_API int cospec_lora_forward(const cospec_lora_dims* dims, const uint16_t* x, const uint16_t* w,
+                                   const uint16_t* a, const uint16_t* b, const float* scaling,
+                                   const int32_t* adapter, const uint64_t* seed, float* u, uint16_t* y,
+                                   void* stream) {
+  LoraArgs p{};
+  const int st = lora_args(dims, seed, &p);
+  if (st != COSPEC_OK) return st;
+  if (p.M == 0) return COSPEC_OK;
+  CS_CHECK_ARG(x && w && a && b && scaling && adapter && u && y);
+  CS_CHECK_ARG(aligned16(x) && aligned16(w) && aligned16(a) && aligned16(b) && aligned16(u) && aligned16(y));
+  p.x = reinterpret_cast<const __nv_bfloat16*>(x);
+  p.w = reinterpret_cast<const __nv_bfloat16*>(w);
+  p.a = reinterpret_cast<const __nv_bfloat16*>(a);
+  p.b = reinterpret_cast<const __nv_bfloat16*>(b);
+  p.scaling = scaling;
+  p.adapter = adapter;
+  p.u = u;
+  p.y = reinterpret_cast<__nv_bfloat16*>(y);
+  const int sms = device_num_sms();
+  if (sms <= 0) return cuda_lookup_failed();
+  int* err = device_error_word();
+  if (!err) return cuda_lookup_failed();
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = launch_lora_low(p, false, sms, err, s);
+  if (e != cudaSuccess) return cuda_status(e);
+  return cuda_status(launch_lora_gemm(p, false, sms, err, s));
+}
+
+COSPEC_API int cospec_lora_backward(const cospec_lora_dims* dims, const uint16_t* dy, const uint16_t* x,
+                                    const uint16_t* w, const uint16_t* a, const uint16_t* b,
+                                    const float* scaling, const int32_t* adapter, const uint64_t* seed,
+                                    const float* u, float* t, uint16_t* dx, float* da, float* db,
+                                    int flags, void* stream) {
+  LoraArgs p{};
+  const int st = lora_args(dims, seed, &p);
+  if (st != COSPEC_OK) return st;
+  CS_CHECK_ARG((flags & ~COSPEC_LORA_ACCUMULATE) == 0);
+  CS_CHECK_ARG(aligned16(da) && aligned16(db) && aligned16(dx));
+  if (p.M > 0 && (dx || da || db)) {
+    CS_CHECK_ARG(dy && adapter && aligned16(dy));
+    if (dx || da) CS_CHECK_ARG(b && scaling && t && aligned16(b) && aligned16(t));
+    if (dx) CS_CHECK_ARG(w && a && aligned16(w) && aligned16(a));
+    if (da) CS_CHECK_ARG(x && aligned16(x));
+    if (db) CS_CHECK_ARG(u && aligned16(u));
+  }
+  p.dy = reinterpret_cast<const __nv_bfloat16*>(dy);
+  p.x = reinterpret_cast<const __nv_bfloat16*>(x);
+  p.w = reinterpret_cast<const __nv_bfloat16*>(w);
+  p.a = reinterpret_cast<const __nv_bfloat16*>(a);
+  p.b = reinterpret_cast<const __nv_bfloat16*>(b);
+  p.scaling = scaling;
+  p.adapter = adapter;
+  p.u = const_cast<float*>(u);
+  p.t = t;
+  p.dx = reinterpret_cast<__nv_bfloat16*>(dx);
+  p.da = da;
+  p.db = db;
+  p.accumulate = flags & COSPEC_LORA_ACCUMULATE;
+  const int sms = device_num_sms();
+  if (sms <= 0) return cuda_lookup_failed();
+  int* err = device_error_word();
+  if (!err) return cuda_lookup_failed();
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e = cudaSuccess;
+  if (p.M > 0 && (dx || da)) e = launch_lora_low(p, true, sms, err, s);
+  if (e == cudaSuccess && (da || db)) e = launch_lora_grad(p, sms, s);
+  if (e == cudaSuccess && p.M > 0 && dx) e = launch_lora_gemm(p, true, sms, err, s);
+  return cuda_status(e);
+}
+
+// ---------------------------------------------------------------- policy loss
+COSPEC_API size_t cospec_arbitrate_loss_workspace(int mlp_hidden) {
+  return mlp_hidden < 1 || mlp_hidden > 1024 ? 0 : arb_loss_ws_bytes(mlp_hidden);
+}
+
+COSPEC_API int cospec_arbitrate_loss(int num_rounds, int K, const int32_t* draft, const int32_t* argmax,
+                                     const float* stats, int mlp_hidden, const float* w1, const float* b1,
+                                     const float* w2, const float* b2, const uint8_t* accept,
+                                     const uint8_t* eff, const float* adv, const float* p_old,
+                                     const float* p_ref, const cospec_rl_params* params, float grad_scale,
+                                     float* loss, float* p_new, float* dz, float* dw1, float* db1,
+                                     float* dw2, float* db2, void* ws, size_t ws_bytes, void* stream) {
+  CS_CHECK_ARG(num_rounds >= 0 && K >= 1 && mlp_hidden >= 1 && params);
+  CS_CHECK_ARG(params->clip_eps >= 0.f && isfinite(params->clip_eps) && isfinite(params->beta_h) && isfinite(params->beta_kl) &&
+               isfinite(grad_scale));
+  if (K > 64 || mlp_hidden > 1024 || (long long)num_rounds * K >= (1LL << 31) - 512) return COSPEC_ERR_UNSUPPORTED;
+  CS_CHECK_ARG(w1 && b1 && w2 && b2 && loss && dw1 && db1 && dw2 && db2);
+  CS_CHECK_ARG(num_rounds == 0 || (draft && argmax && stats && accept && eff && adv && p_old && p_ref && p_new && dz));
+  if (!ws || ws_bytes < arb_loss_ws_bytes(mlp_hidden) || !aligned16(ws)) return COSPEC_ERR_WORKSPACE;
+  const int sms = device_num_sms();
+  if (sms <= 0) return cuda_lookup_failed();
+  ArbLossArgs a{num_rounds, K, mlp_hidden, draft, argmax, stats, w1, b1, w2, b2, accept, eff, adv, p_old, p_ref,
+                params->clip_eps, params->beta_h, params->beta_kl, grad_scale, loss, p_new, dz, dw1, db1, dw2, db2, ws};
+  return cuda_status(launch_arb_loss(a, sms, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

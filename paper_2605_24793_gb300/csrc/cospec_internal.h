@@ -56,10 +56,10 @@ cudaError_t ensure_kernel_limits(const void* kern, KernelLimits& lim, size_t sme
                                  bool cluster);
 
 // cuTensorMapEncodeTiled for a bf16 tensor (rank 1..5, innermost first),
-// 128-byte swizzle, zero fill out of bounds.  dims/box in elements, strides
+// 128-byte (or 32-byte) swizzle, zero fill out of bounds.  dims/box in elements, strides
 // in bytes for dimensions 1..rank-1.
 bool encode_tensor_map_bf16(void* map, const void* base, int rank, const uint64_t* dims,
-                            const uint64_t* strides, const uint32_t* box);
+                            const uint64_t* strides, const uint32_t* box, int swizzle = 128);
 
 // ---------------------------------------------------------------- attention
 struct AttnArgs {
@@ -150,6 +150,59 @@ cudaError_t launch_arbitrate(int B, int K, const int32_t* draft, const int32_t* 
                              const float* stats, int H, const float* w1, const float* b1,
                              const float* w2, float b2, float lambda, int mode, float* p_out,
                              uint8_t* accept, cudaStream_t stream);
+
+// ---------------------------------------------------------------- policy loss
+struct ArbLossArgs {
+  int n, K, H;           // rounds, positions, hidden units
+  const int32_t* draft;
+  const int32_t* argmax;
+  const float* stats;
+  const float* w1;
+  const float* b1;
+  const float* w2;
+  const float* b2;
+  const uint8_t* accept;
+  const uint8_t* eff;
+  const float* adv;
+  const float* p_old;
+  const float* p_ref;
+  float clip_eps, beta_h, beta_kl, grad_scale;
+  float* loss;
+  float* p_new;
+  float* dz;
+  float* dw1;
+  float* db1;
+  float* dw2;
+  float* db2;
+  void* ws;
+};
+size_t arb_loss_ws_bytes(int H);
+cudaError_t launch_arb_loss(const ArbLossArgs& a, int num_sms, cudaStream_t stream);
+
+// ---------------------------------------------------------------- low-rank adapters
+struct LoraArgs {
+  int M, K, N, r, n;      // rows, features in and out, rank, adapters
+  const __nv_bfloat16* x;
+  const __nv_bfloat16* dy;
+  const __nv_bfloat16* w;        // [N][K]
+  const __nv_bfloat16* a;        // [n][r][K]
+  const __nv_bfloat16* b;        // [n][N][r]
+  const float* scaling;
+  const int32_t* adapter;
+  const unsigned long long* seed;
+  uint32_t thr, site;            // dropout: 16-bit threshold (0: none), the place's number
+  float* u;                      // [M][r]
+  float* t;
+  __nv_bfloat16* y;
+  __nv_bfloat16* dx;
+  float* da;
+  float* db;
+  long long ldx, ldy, lddx;
+  int accumulate;
+};
+cudaError_t launch_lora_low(const LoraArgs& a, bool backward, int num_sms, int* err, cudaStream_t stream);
+cudaError_t launch_lora_gemm(const LoraArgs& a, bool backward, int num_sms, int* err, cudaStream_t stream);
+cudaError_t launch_lora_grad(const LoraArgs& a, int num_sms, cudaStream_t stream);
 
 // ---------------------------------------------------------------- accept + commit
 struct CommitArgs {

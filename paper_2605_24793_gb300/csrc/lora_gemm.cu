@@ -1,0 +1,501 @@
+// The shared projection with the adapters' second product inside it, on tcgen05:
+//   forward   y[m][n]  = sum_k x[m][k] W[n][k]  + sum_j u[m][j] B_a[n][j]
+//   backward  dx[m][k] = sum_n dy[m][n] W[n][k] + keep[m][k] sum_j t[m][j] A_a[j][k]
+// a the row's adapter.  Features (n, or k) are the MMA's M dimension and rows its N, as in the LM head, so a few
+// rows still fill the tensor core; W comes by TMA with its contraction along the rows of shared memory
+// (forward) or along the features (backward: an MN-major operand), so neither pass transposes it.
+//
+// The adapters' part is a continuation of the same sum.  u (or t) is fp32; two bf16 parts of it, hi + lo, are
+// an operand of 32 columns per 16 ranks, which four warps write to shared memory beside the TMA's factor tile.
+// Rows of other adapters get zeros there, and the MMA of an adapter covers only the columns from its first
+// to its last row of the tile.  With dropout (backward) this part has an accumulator of its own: the mask
+// multiplies it alone.
+//
+// lora_tile_kernel: one CTA per 128 features x rows of a tile, the contraction split over a cluster and joined
+// in shared memory in a fixed order.
+#include <cuda.h>
+
+#include "lora.cuh"
+
+namespace cospec {
+
+namespace {
+
+constexpr int BM = 128;                  // features of a tile
+constexpr int BK = 64;                   // contraction of a stage
+constexpr int A_BYTES = BM * BK * 2;
+constexpr int UNIT = 16;                 // ranks of a unit
+constexpr int UNIT_BYTES = BM * UNIT * 2;
+constexpr int STEP_UNITS = 2;            // units of an adapter step: 64 columns of hi and lo
+constexpr int MAX_NT = 256;
+constexpr uint64_t WAIT_NS = 2000000000ull;
+
+struct GemmArgs {
+  const float* u;
+  const int32_t* adapter;
+  __nv_bfloat16* y;
+  long long ldy;
+  int M, F, C, r, n;
+  int nt;                // rows of a tile, a multiple of 16
+  int stages, tmem_cols;
+  LoraDrop drop;
+  int* err;
+};
+
+// Descriptor of a K-major operand of 16 columns in the 32-byte-swizzle layout: rows of 32 bytes, 8-row atoms
+// 256 bytes apart.
+CS_DEV uint64_t desc_k_sw32(uint32_t saddr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((saddr & 0x3FFFF) >> 4);
+  d |= (uint64_t)(16 >> 4) << 16;
+  d |= (uint64_t)(256 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)6 << 61;
+  return d;
+}
+
+// The adapters of a tile's rows in the order of their first rows: id, first and last row.
+struct TileList {
+  int ids[MAX_NT];             // of the rows: -1 none
+  int adapter[MAX_NT];
+  int span[MAX_NT];            // first | last << 16
+  int warp_count[4];
+  int count;
+};
+
+// By 128 threads (t = 0 .. 127, named barrier `bar`).  Every row is compared with every other one.
+CS_DEV void build_list(TileList& L, const GemmArgs& p, int row0, int t, int bar) {
+  const int rows = min(p.nt, p.M - row0);
+  for (int i = t; i < p.nt; i += 128) L.ids[i] = i < rows ? lora_adapter(p.adapter, row0 + i, p.n, p.err) : -1;
+  named_bar_sync(bar, 128);
+  int done = 0;
+  for (int i0 = 0; i0 < p.nt; i0 += 128) {
+    const int i = i0 + t;
+    const int id = i < p.nt ? L.ids[i] : -1;
+    bool first = id >= 0;
+    int last = i;
+    for (int j = 0; j < p.nt; j += 4) {
+      const int4 v = *reinterpret_cast<const int4*>(&L.ids[j]);
+      const int w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (w[e] == id) {
+          first = first && j + e >= i;
+          last = max(last, j + e);
+        }
+    }
+    const unsigned mask = __ballot_sync(0xffffffffu, first);
+    if ((t & 31) == 0) L.warp_count[t >> 5] = __popc(mask);
+    named_bar_sync(bar, 128);
+    int at = done + __popc(mask & ((1u << (t & 31)) - 1u));
+    for (int w = 0; w < 4; ++w) {
+      const int c = L.warp_count[w];
+      if (w < (t >> 5)) at += c;
+      done += c;
+    }
+    if (first) {
+      L.adapter[at] = id;
+      L.span[at] = i | last << 16;
+    }
+    named_bar_sync(bar, 128);
+  }
+  if (t == 0) L.count = done;
+}
+
+// One row's 16 ranks of a unit as hi and lo into the 128-byte row of the operand (columns 32 slot ..).
+CS_DEV void write_unit_row(uint8_t* tile, int row, int slot, const float* u, bool mine, int j0, int r) {
+  uint4 w[4] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+  if (mine) {
+    float v[16];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (j0 + 4 * q < r) f = *reinterpret_cast<const float4*>(u + j0 + 4 * q);
+      v[4 * q] = f.x, v[4 * q + 1] = f.y, v[4 * q + 2] = f.z, v[4 * q + 3] = f.w;
+    }
+    uint32_t hi[8], lo[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      float h0, l0, h1, l1;
+      lora_split2(v[2 * q], h0, l0);
+      lora_split2(v[2 * q + 1], h1, l1);
+      hi[q] = pack_bf16(h0, h1);
+      lo[q] = pack_bf16(l0, l1);
+    }
+    w[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    w[1] = make_uint4(hi[4], hi[5], hi[6], hi[7]);
+    w[2] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    w[3] = make_uint4(lo[4], lo[5], lo[6], lo[7]);
+  }
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+    *reinterpret_cast<uint4*>(tile + row * 128 + (((4 * slot + c) ^ (row & 7)) << 4)) = w[c];
+}
+
+// Bit j: whether feature f0 + lane of row row0 + j stays (f0 a multiple of 32).
+CS_DEV uint32_t keep_bits32(int f0, int row0, const LoraDrop& d, LoraKey key) {
+  const int lane = threadIdx.x & 31;
+  uint32_t w = 0;            // of row row0 + lane: bit i for feature f0 + i
+#pragma unroll
+  for (int q = 0; q < 4; ++q) w |= lora_keep8_bits((uint32_t)(f0 / 8 + q), (uint32_t)(row0 + lane), d, key) << (8 * q);
+  // transposed over the warp: lane i, bit j <- lane j, bit i
+#pragma unroll
+  for (int s = 16; s > 0; s >>= 1) {
+    const uint32_t m = s == 16 ? 0x0000ffffu : s == 8 ? 0x00ff00ffu : s == 4 ? 0x0f0f0f0fu : s == 2 ? 0x33333333u : 0x55555555u;
+    const uint32_t o = __shfl_xor_sync(0xffffffffu, w, s);
+    w = (lane & s) ? (w & ~m) | ((o >> s) & m) : (w & m) | ((o << s) & ~m);
+  }
+  return w;
+}
+
+struct TileSmem {
+  uint32_t b_off, list_off, bar_off, total;
+};
+__host__ __device__ inline TileSmem tile_layout(int stages, int nt) {
+  TileSmem L;
+  L.b_off = (uint32_t)stages * A_BYTES;
+  L.list_off = L.b_off + (uint32_t)stages * nt * 128;
+  L.bar_off = L.list_off + (uint32_t)((sizeof(TileList) + 15) / 16 * 16);
+  L.total = L.bar_off + (uint32_t)(4 * stages + 2) * 8 + 16;
+  return L;
+}
+
+// Warps: 0 loads W and the factors, 1 issues the MMAs, 2 loads the rows, 3 allocates TMEM, 4 to 7 list the
+// tile's adapters, write the u operand and read the accumulators.
+template <bool MN, bool DROP>
+__global__ void __launch_bounds__(256, 1)
+    lora_tile_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x,
+                     const __grid_constant__ CUtensorMap tmap_f, const GemmArgs p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  const TileSmem L = tile_layout(p.stages, p.nt);
+  TileList& list = *reinterpret_cast<TileList*>(smem + L.list_off);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + L.bar_off);
+  uint64_t* empty = full + p.stages;
+  uint64_t* ufull = empty + p.stages;      // the u operand of a stage is written
+  uint64_t* ugo = ufull + p.stages;        // the u operand of a stage may be written
+  uint64_t* lready = ugo + p.stages;       // the list is written
+  uint64_t* done = lready + 1;             // every MMA is done
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(done + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int S = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
+  const int f0 = ((int)blockIdx.x / S) * BM;
+  const int row0 = (int)blockIdx.y * p.nt;
+  const int kblocks = (p.C + BK - 1) / BK;
+  const int kb0 = (int)((long long)kblocks * rank / S), nk = (int)((long long)kblocks * (rank + 1) / S) - kb0;
+  const int upe = (p.r + UNIT - 1) / UNIT;           // units of an adapter
+  const uint32_t b_bytes = (uint32_t)p.nt * 128u;
+
+  if (tid == 0) {
+    for (int s = 0; s < p.stages; ++s) {
+      mbar_init(&full[s], 2);
+      mbar_init(&empty[s], 1);
+      mbar_init(&ufull[s], 4);
+      mbar_init(&ugo[s], 1);
+    }
+    mbar_init(lready, 4);
+    mbar_init(done, 1);
+    *abort_flag = 0;
+    fence_barrier_init();
+    tma_prefetch_desc(&tmap_w);
+    tma_prefetch_desc(&tmap_x);
+    tma_prefetch_desc(&tmap_f);
+  }
+  if (warp == 3) {
+    tmem_alloc(tmem_holder, (uint32_t)p.tmem_cols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_holder;
+  // u comes from the kernel before, which waited for what stands before itself: W, the factors, the rows and
+  // their adapters are there
+
+  // step i of the adapters that this CTA takes is step rank + i S of the tile
+  auto my_steps = [&]() {
+    const int steps = (list.count * upe + STEP_UNITS - 1) / STEP_UNITS;
+    return steps > rank ? (steps - rank + S - 1) / S : 0;
+  };
+  bool ok = true;
+  if (warp == 0 || warp == 2) {
+    if (lane == 0) {
+      const bool is_w = warp == 0;
+      // W is read again by the other row tiles, if there are any
+      const uint64_t pol = !is_w ? l2_policy_evict_last() : gridDim.y > 1 ? l2_policy_evict_normal() : l2_policy_evict_first();
+      const uint32_t a_buf = smem_u32(smem), b_buf = smem_u32(smem + L.b_off);
+      int issued = 0;
+      auto turn = [&](int li) {            // the stage of load li is free
+        return li < p.stages || (mbar_wait(&empty[li % p.stages], (uint32_t)(li / p.stages - 1) & 1u, WAIT_NS) && !*abort_flag);
+      };
+      for (int i = 0; i < nk; ++i) {
+        if (!turn(i)) {
+          ok = false;
+          break;
+        }
+        const int s = i % p.stages, x = (kb0 + i) * BK;
+        mbar_arrive_expect_tx(&full[s], is_w ? (uint32_t)A_BYTES : b_bytes);
+        if (!is_w) {
+          tma_load_3d(b_buf + (uint32_t)s * b_bytes, &tmap_x, &full[s], x, row0, 0, pol);
+        } else if (!MN) {
+          tma_load_3d(a_buf + (uint32_t)s * A_BYTES, &tmap_w, &full[s], x, f0, 0, pol);
+        } else {
+          tma_load_3d(a_buf + (uint32_t)s * A_BYTES, &tmap_w, &full[s], f0, x, 0, pol);
+          tma_load_3d(a_buf + (uint32_t)s * A_BYTES + A_BYTES / 2, &tmap_w, &full[s], f0 + 64, x, 0, pol);
+        }
+        issued = i + 1;
+      }
+      if (ok) ok = mbar_wait_idle(lready, 0, WAIT_NS) && !*abort_flag;
+      if (ok) {
+        const int units = list.count * upe, n = my_steps();
+        for (int i = 0; i < n; ++i) {
+          const int li = nk + i, s = li % p.stages;
+          if (!turn(li)) {
+            ok = false;
+            break;
+          }
+          if (!is_w) {
+            mbar_arrive(&full[s]);
+          } else {
+            const int u0 = (rank + i * S) * STEP_UNITS, nu = min(STEP_UNITS, units - u0);
+            // (the writers join only now: the stage's turns before passed without them, and a wait by parity
+            // would not tell those apart)
+            mbar_arrive(&ugo[s]);
+            mbar_arrive_expect_tx(&full[s], (uint32_t)nu * UNIT_BYTES);
+            for (int q = 0; q < nu; ++q) {
+              const int e = (u0 + q) / upe, j0 = ((u0 + q) % upe) * UNIT;
+              const uint32_t dst = a_buf + (uint32_t)s * A_BYTES + (uint32_t)q * UNIT_BYTES;
+              if (!MN) {
+                tma_load_3d(dst, &tmap_f, &full[s], j0, f0, list.adapter[e], pol);
+              } else {
+                tma_load_3d(dst, &tmap_f, &full[s], f0, j0, list.adapter[e], pol);
+                tma_load_3d(dst + UNIT_BYTES / 2, &tmap_f, &full[s], f0 + 64, j0, list.adapter[e], pol);
+              }
+            }
+          }
+          issued = li + 1;
+        }
+      }
+      if (!ok) {
+        set_err(p.err, ERR_TIMEOUT);
+        *abort_flag = 1;
+        // what was issued lands before the shared memory is given back
+        for (int li = issued > p.stages ? issued - p.stages : 0; li < issued; ++li)
+          mbar_wait(&full[li % p.stages], (uint32_t)(li / p.stages) & 1u, WAIT_NS);
+      }
+    }
+  } else if (warp == 1) {
+    const uint32_t on = elect_one();
+    constexpr uint32_t A_MN = MN ? 1u << 15 : 0u;      // the features' operand is MN-major
+    const uint32_t idesc = idesc_bf16_f32(BM, p.nt) | A_MN;
+    const uint64_t a_desc = MN ? tq_desc_mn_sw128(smem_u32(smem), A_BYTES / 2) : smem_desc_sw128(smem_u32(smem));
+    const uint64_t f_desc = MN ? tq_desc_mn_sw128(smem_u32(smem), UNIT_BYTES / 2) : desc_k_sw32(smem_u32(smem));
+    const uint64_t b_desc = smem_desc_sw128(smem_u32(smem + L.b_off));
+    for (int i = 0; i < nk && ok; ++i) {
+      const int s = i % p.stages;
+      ok = __all_sync(0xffffffffu, mbar_wait(&full[s], (uint32_t)(i / p.stages) & 1u, WAIT_NS)) && !*abort_flag;
+      if (!ok) break;
+      tc_fence_after();
+      const uint64_t a = a_desc + (uint64_t)(s * (A_BYTES >> 4)), b = b_desc + (uint64_t)((uint32_t)s * (b_bytes >> 4));
+#pragma unroll
+      for (int k = 0; k < BK / 16; ++k)
+        umma_bf16_on(on, tmem, a + (uint64_t)(MN ? k * 128 : k * 2), b + (uint64_t)(k * 2), idesc, (i | k) != 0 ? 1u : 0u);
+      umma_commit_on(on, &empty[s]);
+    }
+    if (ok) ok = __all_sync(0xffffffffu, mbar_wait_idle(lready, 0, WAIT_NS)) && !*abort_flag;
+    if (ok) {
+      const int units = list.count * upe, n = my_steps();
+      const uint32_t d2 = DROP ? tmem + (uint32_t)p.nt : tmem;
+      for (int i = 0; i < n; ++i) {
+        const int li = nk + i, s = li % p.stages;
+        ok = __all_sync(0xffffffffu, mbar_wait(&full[s], (uint32_t)(li / p.stages) & 1u, WAIT_NS) &&
+                                         mbar_wait(&ufull[s], (uint32_t)(i / p.stages) & 1u, WAIT_NS)) && !*abort_flag;
+        if (!ok) break;
+        tc_fence_after();
+        const int u0 = (rank + i * S) * STEP_UNITS, nu = min(STEP_UNITS, units - u0);
+        for (int q = 0; q < nu; ++q) {
+          const int span = list.span[(u0 + q) / upe];
+          // the first product of a second accumulator sets all of its columns
+          const bool all = DROP && i == 0 && q == 0;
+          const int lo = all ? 0 : (span & 0xffff) & ~15, hi = all ? p.nt : ((span >> 16) | 15) + 1;
+          const uint32_t id = idesc_bf16_f32(BM, hi - lo) | A_MN;
+          const uint64_t a = f_desc + (uint64_t)((s * A_BYTES + q * UNIT_BYTES) >> 4);
+          const uint64_t b = b_desc + (uint64_t)(((uint32_t)s * b_bytes + (uint32_t)lo * 128u) >> 4) + (uint64_t)(q * 4);
+          umma_bf16_on(on, d2 + (uint32_t)lo, a, b, id, all ? 0u : 1u);
+          umma_bf16_on(on, d2 + (uint32_t)lo, a, b + 2, id, 1u);
+        }
+        umma_commit_on(on, &empty[s]);
+      }
+    }
+    if (!ok && on) {
+      set_err(p.err, ERR_TIMEOUT);
+      *abort_flag = 1;
+    }
+    umma_commit_on(on, done);
+  } else if (warp >= 4) {
+    const int t = tid - 128;
+    build_list(list, p, row0, t, 1);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(lready);
+    named_bar_sync(1, 128);
+    const int units = list.count * upe, n = my_steps();
+    griddep_wait();                        // u
+    griddep_launch_dependents();
+    for (int i = 0; i < n; ++i) {
+      const int li = nk + i, s = li % p.stages;
+      ok = __all_sync(0xffffffffu, mbar_wait_idle(&ugo[s], (uint32_t)(i / p.stages) & 1u, WAIT_NS)) && !*abort_flag;
+      if (!ok) break;
+      uint8_t* tile = smem + L.b_off + (uint32_t)s * b_bytes;
+      const int u0 = (rank + i * S) * STEP_UNITS, nu = min(STEP_UNITS, units - u0);
+      for (int q = 0; q < nu; ++q) {
+        const int e = (u0 + q) / upe, j0 = ((u0 + q) % upe) * UNIT;
+        const int id = list.adapter[e], span = list.span[e];
+        const bool all = DROP && i == 0 && q == 0;
+        const int lo = all ? 0 : (span & 0xffff) & ~15, hi = all ? p.nt : ((span >> 16) | 15) + 1;
+        for (int row = lo + t; row < hi; row += 128)
+          write_unit_row(tile, row, q, p.u + (size_t)(row0 + row) * p.r, list.ids[row] == id, j0, p.r);
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ufull[s]);
+    }
+    if (!ok && lane == 0) {
+      set_err(p.err, ERR_TIMEOUT);
+      *abort_flag = 1;
+    }
+    // accumulators to shared memory, [row][feature]; the ring is idle once the last MMA is done
+    ok = __all_sync(0xffffffffu, mbar_wait_idle(done, 0, 2 * WAIT_NS)) && ok;
+    if (ok) {
+      tc_fence_after();
+      const int q = warp & 3;
+      const uint32_t tb = tmem + ((uint32_t)(q * 32) << 16);
+      float* part = reinterpret_cast<float*>(smem);
+      LoraKey key{0, 0};
+      if (DROP) key = lora_key(p.drop);
+      for (int c = 0; c < p.nt; c += 16) {
+        float v[16];
+        tq_ld16(tb + (uint32_t)c, v);
+        tq_wait_ld16(v);
+        if (DROP && n > 0) {
+          float w[16];
+          tq_ld16(tb + (uint32_t)(p.nt + c), w);
+          tq_wait_ld16(w);
+          const uint32_t keep = keep_bits32(f0 + q * 32, row0 + (c & ~31), p.drop, key) >> (c & 16);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) v[j] += (keep >> j) & 1u ? w[j] : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < 16; ++j) part[(c + j) * BM + q * 32 + lane] = v[j];
+      }
+      tc_fence_before();
+    }
+  }
+  __syncthreads();
+  __syncwarp();
+  cluster_arrive();
+  cluster_wait();
+  // each CTA adds up its share of the rows over the cluster, a row of 128 features a warp
+  if (!*abort_flag) {
+    const int r0 = p.nt * rank / S, r1 = p.nt * (rank + 1) / S;
+    const uint32_t base = smem_u32(smem);
+    const int f = f0 + lane * 4;
+    for (int row = r0 + warp; row < r1; row += 8) {
+      if (row0 + row >= p.M) break;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i = 0; i < S; ++i) {
+        float4 w;
+        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                     : "=f"(w.x), "=f"(w.y), "=f"(w.z), "=f"(w.w)
+                     : "r"(dsmem_map(base + (uint32_t)(row * BM + lane * 4) * 4u, (uint32_t)i))
+                     : "memory");
+        v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+      }
+      if (f < p.F)
+        *reinterpret_cast<uint2*>(p.y + (long long)(row0 + row) * p.ldy + f) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+    }
+  }
+  __syncwarp();
+  cluster_arrive();
+  cluster_wait();
+  if (warp == 3) {
+    tc_fence_after();
+    __syncwarp();
+    tmem_dealloc(tmem, (uint32_t)p.tmem_cols);
+  }
+}
+
+template <bool MN, bool DROP>
+cudaError_t launch_tile(const CUtensorMap& w, const CUtensorMap& x, const CUtensorMap& f, GemmArgs p, int splits, cudaStream_t stream) {
+  static KernelLimits lim;
+  const size_t smem = tile_layout(p.stages, p.nt).total + 1024;
+  const cudaError_t e = ensure_kernel_limits((const void*)lora_tile_kernel<MN, DROP>, lim, 227 * 1024, false);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((p.F + BM - 1) / BM * splits), (unsigned)((p.M + p.nt - 1) / p.nt));
+  cfg.blockDim = dim3(256);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)splits;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, lora_tile_kernel<MN, DROP>, w, x, f, p);
+}
+
+}  // namespace
+
+cudaError_t launch_lora_gemm(const LoraArgs& a, bool backward, int num_sms, int* err, cudaStream_t stream) {
+  GemmArgs p{};
+  p.u = backward ? a.t : a.u;
+  p.adapter = a.adapter;
+  p.y = backward ? a.dx : a.y;
+  p.ldy = backward ? a.lddx : a.ldy;
+  p.M = a.M;
+  p.F = backward ? a.K : a.N;
+  p.C = backward ? a.N : a.K;
+  p.r = a.r;
+  p.n = a.n;
+  p.drop = LoraDrop{a.seed, a.site, backward ? a.thr : 0u};
+  p.err = err;
+  const bool drop = p.drop.thr != 0u;
+  // rows of a tile: all of them, or equal parts of at most 256
+  const int row_tiles = (p.M + MAX_NT - 1) / MAX_NT;
+  p.nt = ((p.M + row_tiles - 1) / row_tiles + 15) / 16 * 16;
+  const int tiles = (p.F + BM - 1) / BM * row_tiles, kblocks = (p.C + BK - 1) / BK;
+  int splits = num_sms / tiles;
+  if (splits > 8) splits = 8;
+  if (splits > kblocks) splits = kblocks;
+  if (splits < 1) splits = 1;
+  const uint32_t budget = 226u * 1024u;
+  p.stages = (int)((budget - tile_layout(0, p.nt).total) / (A_BYTES + (uint32_t)p.nt * 128u + 24u));
+  if (p.stages > 10) p.stages = 10;
+  // the accumulators pass through the ring
+  const int cols = p.nt * (drop ? 2 : 1);
+  p.tmem_cols = 32;
+  while (p.tmem_cols < cols) p.tmem_cols *= 2;
+
+  CUtensorMap w, x, f;
+  const uint64_t wd[3] = {(uint64_t)a.K, (uint64_t)a.N, 1}, ws[2] = {(uint64_t)a.K * 2, (uint64_t)a.K * a.N * 2};
+  const uint32_t wb[3] = {64, backward ? 64u : (uint32_t)BM, 1};
+  const uint64_t xd[3] = {(uint64_t)p.C, (uint64_t)p.M, 1};
+  const uint64_t ldx = (uint64_t)(backward ? a.ldy : a.ldx), xs[2] = {ldx * 2, ldx * 2 * (uint64_t)p.M};
+  const uint32_t xb[3] = {64, (uint32_t)p.nt, 1};
+  const uint64_t fd[3] = {(uint64_t)(backward ? a.K : a.r), (uint64_t)(backward ? a.r : a.N), (uint64_t)a.n};
+  const uint64_t fs[2] = {fd[0] * 2, fd[0] * fd[1] * 2};
+  const uint32_t fb[3] = {backward ? 64u : (uint32_t)UNIT, backward ? (uint32_t)UNIT : (uint32_t)BM, 1};
+  if (!encode_tensor_map_bf16(&w, a.w, 3, wd, ws, wb) || !encode_tensor_map_bf16(&x, backward ? a.dy : a.x, 3, xd, xs, xb) ||
+      !encode_tensor_map_bf16(&f, backward ? a.a : a.b, 3, fd, fs, fb, backward ? 128 : 32))
+    return cudaErrorInvalidValue;
+  if (!backward) return launch_tile<false, false>(w, x, f, p, splits, stream);
+  if (drop) return launch_tile<true, true>(w, x, f, p, splits, stream);
+  return launch_tile<true, false>(w, x, f, p, splits, stream);
+}
+
+}  // namespace cospec
