@@ -449,6 +449,399 @@ cudaError_t launch_tile(const CUtensorMap& w, const CUtensorMap& x, const CUtens
   return cudaLaunchKernelEx(&cfg, lora_tile_kernel<MN, DROP>, w, x, f, p);
 }
 
+// ---------------------------------------------------------------- CTA pairs
+// One MMA of the pair with the features' operand advanced by ASTEP (in 16 bytes) per 16 of the contraction.
+template <int ASTEP>
+CS_DEV void pair_k64(uint32_t on, uint32_t d, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p, q, t;\n .reg .b64 a, b;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
+      " setp.eq.b32 t, %4, %4;\n"
+      " @q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n add.s64 a, %1, %6;\n add.s64 b, %2, 2;\n"
+      " @q tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %3, t;\n add.s64 a, a, %6;\n add.s64 b, b, 2;\n"
+      " @q tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %3, t;\n add.s64 a, a, %6;\n add.s64 b, b, 2;\n"
+      " @q tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %3, t;\n}\n" ::"r"(d),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(on), "n"(ASTEP)
+      : "memory");
+}
+CS_DEV void pair_mma(uint32_t on, uint32_t d, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
+      " @q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(on)
+      : "memory");
+}
+// A bounded wait whose acquire covers what the pair's other CTA wrote before it arrived.
+CS_DEV bool mbar_wait_pair(uint64_t* bar, uint32_t parity) {
+  uint64_t t0 = 0;
+#pragma unroll 1
+  for (int i = 0;; ++i) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    if (ok) return true;
+    if ((i & 63) == 63) {
+      const uint64_t now = global_timer_ns();
+      if (t0 == 0) t0 = now;
+      else if (now - t0 > WAIT_NS) return false;
+    }
+  }
+}
+
+constexpr int PBM = 2 * BM;              // features of a pair's tile
+constexpr int P_EPI = 8;                 // epilogue warps, two per TMEM lane quarter
+constexpr int P_XW = 2 + P_EPI;          // producer of the rows
+constexpr int P_UW = P_XW + 1;           // first of the four warps of the u operand
+constexpr int P_THREADS = 32 * (P_UW + 4);
+constexpr int P_CHUNKS = MAX_NT / 64;    // 32-row chunks of an epilogue warp
+
+struct PairSmem {
+  uint32_t b_off, list_off, bar_off, total;
+};
+__host__ __device__ inline PairSmem pair_layout(int stages, int nt) {
+  PairSmem L;
+  L.b_off = (uint32_t)stages * A_BYTES;
+  L.list_off = L.b_off + (uint32_t)stages * (nt / 2) * 128;
+  L.bar_off = L.list_off + 2 * (uint32_t)((sizeof(TileList) + 15) / 16 * 16);
+  L.total = L.bar_off + (uint32_t)(4 * stages + 9) * 8 + 16;
+  return L;
+}
+
+// Persistent pairs of CTAs (cta_group::2) walk tiles of 256 features x nt rows: each CTA loads its 128 features and
+// half of the rows, so an SM takes in 32 KB per 64 of the contraction.  Warps: 0 loads W and the factors, 10 the rows,
+// 1 of the leader issues the MMAs, 2 to 9 round finished accumulators while the next tile is multiplied, 11 to 14
+// list the tile's adapters and write the CTA's half of the u operand, one tile ahead of the MMAs.  With dropout
+// the two accumulators of a tile fill TMEM, so the epilogue is not overlapped; its mask is drawn before.
+template <bool MN, bool DROP>
+__global__ void __launch_bounds__(P_THREADS, 1)
+    lora_pair_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x,
+                     const __grid_constant__ CUtensorMap tmap_f, const GemmArgs p) {
+  constexpr int NACC = DROP ? 1 : 2;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  const PairSmem L = pair_layout(p.stages, p.nt);
+  constexpr uint32_t LIST_BYTES = (uint32_t)((sizeof(TileList) + 15) / 16 * 16);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + L.bar_off);
+  uint64_t* empty = full + p.stages;
+  uint64_t* ufull = empty + p.stages;      // (leader) both halves of a stage's u operand are written
+  uint64_t* ugo = ufull + p.stages;        // this CTA's half may be written
+  uint64_t* lready = ugo + p.stages;       // [2] a tile's list is written
+  uint64_t* lfree = lready + 2;            // [2] and read
+  uint64_t* tfull = lfree + 2;             // [2] accumulators
+  uint64_t* tempty = tfull + 2;            // [2]
+  uint64_t* done = tempty + 2;
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(done + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+  auto list_of = [&](int it) -> TileList& { return *reinterpret_cast<TileList*>(smem + L.list_off + (uint32_t)(it & 1) * LIST_BYTES); };
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = (int)cluster_ctarank();
+  const int pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
+  const int kblocks = (p.C + BK - 1) / BK, upe = (p.r + UNIT - 1) / UNIT;
+  const int ftiles = (p.F + PBM - 1) / PBM, tiles = ftiles * ((p.M + p.nt - 1) / p.nt);
+  const int half = p.nt / 2;
+  const uint32_t b_bytes = (uint32_t)half * 128u;
+
+  if (tid == 0) {
+    for (int s = 0; s < p.stages; ++s) {
+      mbar_init(&full[s], 2);              // (leader) its two producers
+      mbar_init(&empty[s], 1);
+      mbar_init(&ufull[s], 8);             // (leader) four warps of each CTA
+      mbar_init(&ugo[s], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&lready[i], 4);
+      mbar_init(&lfree[i], 2 + (rank == 0 ? 1 : 0) + (DROP ? P_EPI : 0));
+      mbar_init(&tfull[i], 1);
+      mbar_init(&tempty[i], 2 * P_EPI);    // (leader) the epilogue warps of both CTAs
+    }
+    mbar_init(done, 1);
+    *abort_flag = 0;
+    fence_barrier_init();
+    tma_prefetch_desc(&tmap_w);
+    tma_prefetch_desc(&tmap_x);
+    tma_prefetch_desc(&tmap_f);
+  }
+  if (warp == 1) tmem_alloc_pair(tmem_holder, (uint32_t)p.tmem_cols);
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_holder;
+  bool ok = true;
+
+  if (warp == 0 || warp == P_XW) {
+    if (lane == 0) {
+      const bool is_w = warp == 0;
+      const uint64_t pol = l2_policy_evict_normal();
+      const uint32_t a_buf = smem_u32(smem), b_buf = smem_u32(smem + L.b_off);
+      const uint32_t full0 = dsmem_map(smem_u32(full), 0);
+      int li = 0;
+      auto turn = [&](int s) {
+        return li < p.stages || (mbar_wait(&empty[s], (uint32_t)(li / p.stages - 1) & 1u, WAIT_NS) && !*abort_flag);
+      };
+      int it = 0;
+      for (int tile = pair; tile < tiles && ok; tile += pairs, ++it) {
+        const int f0 = (tile % ftiles) * PBM + rank * BM, row0 = (tile / ftiles) * p.nt + rank * half;
+        for (int kb = 0; kb < kblocks; ++kb, ++li) {
+          const int s = li % p.stages, x = kb * BK;
+          if (!turn(s)) {
+            ok = false;
+            break;
+          }
+          if (rank == 0) mbar_arrive_expect_tx(&full[s], 2 * (is_w ? (uint32_t)A_BYTES : b_bytes));
+          const uint32_t bar = full0 + (uint32_t)s * 8u;
+          if (!is_w) {
+            tma_load_3d_pair(b_buf + (uint32_t)s * b_bytes, &tmap_x, bar, x, row0, 0, pol);
+          } else if (!MN) {
+            tma_load_3d_pair(a_buf + (uint32_t)s * A_BYTES, &tmap_w, bar, x, f0, 0, pol);
+          } else {
+            tma_load_3d_pair(a_buf + (uint32_t)s * A_BYTES, &tmap_w, bar, f0, x, 0, pol);
+            tma_load_3d_pair(a_buf + (uint32_t)s * A_BYTES + A_BYTES / 2, &tmap_w, bar, f0 + 64, x, 0, pol);
+          }
+        }
+        if (ok) ok = mbar_wait_idle(&lready[it & 1], (uint32_t)(it >> 1) & 1u, WAIT_NS) && !*abort_flag;
+        if (!ok) break;
+        const TileList& list = list_of(it);
+        const int units = list.count * upe, steps = (units + STEP_UNITS - 1) / STEP_UNITS;
+        for (int i = 0; i < steps; ++i, ++li) {
+          const int s = li % p.stages;
+          if (!turn(s)) {
+            ok = false;
+            break;
+          }
+          if (!is_w) {
+            if (rank == 0) mbar_arrive(&full[s]);
+            continue;
+          }
+          const int nu = min(STEP_UNITS, units - i * STEP_UNITS);
+          mbar_arrive(&ugo[s]);
+          if (rank == 0) mbar_arrive_expect_tx(&full[s], 2 * (uint32_t)nu * UNIT_BYTES);
+          const uint32_t bar = full0 + (uint32_t)s * 8u;
+          for (int q = 0; q < nu; ++q) {
+            const int u = i * STEP_UNITS + q, e = list.adapter[u / upe], j0 = (u % upe) * UNIT;
+            const uint32_t dst = a_buf + (uint32_t)s * A_BYTES + (uint32_t)q * UNIT_BYTES;
+            if (!MN) {
+              tma_load_3d_pair(dst, &tmap_f, bar, j0, f0, e, pol);
+            } else {
+              tma_load_3d_pair(dst, &tmap_f, bar, f0, j0, e, pol);
+              tma_load_3d_pair(dst + UNIT_BYTES / 2, &tmap_f, bar, f0 + 64, j0, e, pol);
+            }
+          }
+        }
+        if (ok) mbar_arrive(&lfree[it & 1]);
+      }
+      if (!ok) {
+        set_err(p.err, ERR_TIMEOUT);
+        *abort_flag = 1;
+        // what was issued lands before the shared memory is given back (the peer's copies are counted on the leader's
+        // barriers, and both CTAs stay until the leader is through)
+        if (rank == 0)
+          for (int l = li > p.stages ? li - p.stages : 0; l < li; ++l) mbar_wait(&full[l % p.stages], (uint32_t)(l / p.stages) & 1u, WAIT_NS);
+      }
+    }
+  } else if (warp == 1) {
+    if (rank == 0) {
+      const uint32_t on = elect_one();
+      constexpr uint32_t A_MN = MN ? 1u << 15 : 0u;
+      const uint32_t idesc = idesc_bf16_f32(PBM, p.nt) | A_MN;
+      const uint64_t a_desc = MN ? tq_desc_mn_sw128(smem_u32(smem), A_BYTES / 2) : smem_desc_sw128(smem_u32(smem));
+      const uint64_t f_desc = MN ? tq_desc_mn_sw128(smem_u32(smem), UNIT_BYTES / 2) : desc_k_sw32(smem_u32(smem));
+      const uint64_t b_desc = smem_desc_sw128(smem_u32(smem + L.b_off));
+      int li = 0, it = 0;
+      uint32_t uphase = 0;                 // bit s: parity of stage s's next u operand
+      for (int tile = pair; tile < tiles && ok; tile += pairs, ++it) {
+        const int acc = it % NACC;
+        ok = __all_sync(0xffffffffu, mbar_wait(&tempty[acc], ((uint32_t)(it / NACC) & 1u) ^ 1u, WAIT_NS)) && !*abort_flag;
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t d = tmem + (uint32_t)(acc * p.nt), d2 = DROP ? d + (uint32_t)p.nt : d;
+        for (int kb = 0; kb < kblocks; ++kb, ++li) {
+          const int s = li % p.stages;
+          ok = __all_sync(0xffffffffu, mbar_wait(&full[s], (uint32_t)(li / p.stages) & 1u, WAIT_NS));
+          if (!ok) break;
+          tc_fence_after();
+          pair_k64<MN ? 128 : 2>(on, d, a_desc + (uint64_t)(s * (A_BYTES >> 4)), b_desc + (uint64_t)((uint32_t)s * (b_bytes >> 4)), idesc,
+                                 kb != 0 ? 1u : 0u);
+          umma_commit_pair_on(on, &empty[s], 3);
+        }
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait_idle(&lready[it & 1], (uint32_t)(it >> 1) & 1u, WAIT_NS)) && !*abort_flag;
+        if (!ok) break;
+        const int units = list_of(it).count * upe, steps = (units + STEP_UNITS - 1) / STEP_UNITS;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&lfree[it & 1]);
+        for (int i = 0; i < steps; ++i, ++li) {
+          const int s = li % p.stages;
+          ok = __all_sync(0xffffffffu, mbar_wait(&full[s], (uint32_t)(li / p.stages) & 1u, WAIT_NS) && mbar_wait_pair(&ufull[s], (uphase >> s) & 1u)) &&
+               !*abort_flag;
+          if (!ok) break;
+          uphase ^= 1u << s;
+          tc_fence_after();
+          const int nu = min(STEP_UNITS, units - i * STEP_UNITS);
+          for (int q = 0; q < nu; ++q) {
+            const uint64_t a = f_desc + (uint64_t)((s * A_BYTES + q * UNIT_BYTES) >> 4);
+            const uint64_t b = b_desc + (uint64_t)((uint32_t)s * (b_bytes >> 4)) + (uint64_t)(q * 4);
+            pair_mma(on, d2, a, b, idesc, DROP && i == 0 && q == 0 ? 0u : 1u);
+            pair_mma(on, d2, a, b + 2, idesc, 1u);
+          }
+          umma_commit_pair_on(on, &empty[s], 3);
+        }
+        if (!ok) break;
+        umma_commit_pair_on(on, &tfull[acc], 3);
+      }
+      if (!ok && on) {
+        set_err(p.err, ERR_TIMEOUT);
+        *abort_flag = 1;
+      }
+      umma_commit_pair_on(on, done, 3);
+    }
+  } else if (warp >= P_UW) {
+    const int t = tid - P_UW * 32;
+    const uint32_t ufull0 = dsmem_map(smem_u32(ufull), 0);
+    int li = 0, it = 0;
+    uint32_t gphase = 0;
+    griddep_wait();                        // u
+    griddep_launch_dependents();
+    for (int tile = pair; tile < tiles; tile += pairs, ++it) {
+      const int row0 = (tile / ftiles) * p.nt;
+      TileList& list = list_of(it);
+      if (it >= 2) ok = mbar_wait_idle(&lfree[it & 1], (uint32_t)((it >> 1) - 1) & 1u, 2 * WAIT_NS) && !*abort_flag;
+      if (!ok) *abort_flag = 1;
+      named_bar_sync(1, 128);
+      if (t == 0) list.count = *abort_flag ? -1 : 0;        // one thread's reading decides for all four warps
+      named_bar_sync(1, 128);
+      if (list.count < 0) break;
+      build_list(list, p, row0, t, 1);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&lready[it & 1]);
+      named_bar_sync(1, 128);
+      const int units = list.count * upe, steps = (units + STEP_UNITS - 1) / STEP_UNITS;
+      li += kblocks;
+      for (int i = 0; i < steps; ++i, ++li) {
+        const int s = li % p.stages;
+        ok = __all_sync(0xffffffffu, mbar_wait_idle(&ugo[s], (gphase >> s) & 1u, WAIT_NS)) && !*abort_flag;
+        if (!ok) break;
+        gphase ^= 1u << s;
+        const int nu = min(STEP_UNITS, units - i * STEP_UNITS);
+        uint8_t* buf = smem + L.b_off + (uint32_t)s * b_bytes;
+        if (t < half) {
+          const int row = rank * half + t;
+          for (int q = 0; q < nu; ++q) {
+            const int u = i * STEP_UNITS + q, id = list.adapter[u / upe];
+            write_unit_row(buf, t, q, p.u + (size_t)(row0 + row) * p.r, list.ids[row] == id, (u % upe) * UNIT, p.r);
+          }
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(ufull0 + (uint32_t)s * 8u);
+      }
+      if (!ok) *abort_flag = 1;            // (the others of the four see it at the next tile)
+    }
+    if (*abort_flag && lane == 0) set_err(p.err, ERR_TIMEOUT);
+  } else {
+    const int q = warp & 3, ew = warp - 2, hw = ew >> 2;
+    const uint32_t tempty0 = dsmem_map(smem_u32(tempty), 0);
+    LoraKey key{0, 0};
+    if (DROP) key = lora_key(p.drop);
+    int it = 0;
+    for (int tile = pair; tile < tiles; tile += pairs, ++it) {
+      const int acc = it % NACC;
+      const int f = (tile % ftiles) * PBM + rank * BM + q * 32, row0 = (tile / ftiles) * p.nt;
+      const int rows = min(p.nt, p.M - row0), chunks = (rows + 31) / 32;
+      uint32_t keep[P_CHUNKS];
+      bool has = !DROP;
+      if (DROP) {
+#pragma unroll
+        for (int c = 0; c < P_CHUNKS; ++c)
+          if (hw + 2 * c < chunks) keep[c] = keep_bits32(f, row0 + (hw + 2 * c) * 32, p.drop, key);
+        ok = __all_sync(0xffffffffu, mbar_wait_idle(&lready[it & 1], (uint32_t)(it >> 1) & 1u, 2 * WAIT_NS));
+        has = ok && list_of(it).count > 0;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&lfree[it & 1]);
+      }
+      ok = ok && __all_sync(0xffffffffu, mbar_wait_idle(&tfull[acc], (uint32_t)(it / NACC) & 1u, 2 * WAIT_NS));
+      if (!ok) {
+        if (lane == 0) {
+          set_err(p.err, ERR_TIMEOUT);
+          *abort_flag = 1;
+        }
+        break;
+      }
+      tc_fence_after();
+      const uint32_t tb = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * p.nt);
+      const bool odd = lane & 1;
+      const bool in = f + (lane & ~1) < p.F;
+#pragma unroll
+      for (int c = 0; c < P_CHUNKS; ++c) {
+        const int ch = hw + 2 * c;
+        if (ch >= chunks) break;
+        float v[32];
+        tmem_ld32(tb + (uint32_t)(ch * 32), v);
+        if (DROP) {
+          if (has) {
+            float w[32];
+            tmem_ld32(tb + (uint32_t)(p.nt + ch * 32), w);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] += (keep[c] >> j) & 1u ? w[j] : 0.f;
+          }
+        }
+        // neighbouring lanes exchange, so that each stores two features of one row
+        __nv_bfloat16* dst = p.y + (long long)(row0 + ch * 32 + (odd ? 1 : 0)) * p.ldy + f + (lane & ~1);
+        const int left = rows - ch * 32 - (odd ? 1 : 0);
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) {
+          const float o = __shfl_xor_sync(0xffffffffu, odd ? v[j] : v[j + 1], 1);
+          const uint32_t w = odd ? pack_bf16(o, v[j + 1]) : pack_bf16(v[j], o);
+          if (in && j < left) *reinterpret_cast<uint32_t*>(dst) = w;
+          dst += 2 * p.ldy;
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster_relaxed(tempty0 + (uint32_t)acc * 8u);
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  // (as in the LM head: neither CTA leaves before the last signal of the leader's MMAs is in both)
+  if (warp == 1) mbar_wait(done, 0, WAIT_NS);
+  __syncwarp();
+  cluster_arrive();
+  cluster_wait();
+  tc_fence_after();
+  if (warp == 1) {
+    __syncwarp();
+    tmem_dealloc_pair(tmem, (uint32_t)p.tmem_cols);
+  }
+}
+
+template <bool MN, bool DROP>
+cudaError_t launch_pair(const CUtensorMap& w, const CUtensorMap& x, const CUtensorMap& f, GemmArgs p, int pairs, cudaStream_t stream) {
+  static KernelLimits lim;
+  const size_t smem = pair_layout(p.stages, p.nt).total + 1024;
+  const cudaError_t e = ensure_kernel_limits((const void*)lora_pair_kernel<MN, DROP>, lim, 227 * 1024, false);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(2 * pairs));
+  cfg.blockDim = dim3(P_THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, lora_pair_kernel<MN, DROP>, w, x, f, p);
+}
+
 }  // namespace
 
 cudaError_t launch_lora_gemm(const LoraArgs& a, bool backward, int num_sms, int* err, cudaStream_t stream) {
@@ -465,19 +858,35 @@ cudaError_t launch_lora_gemm(const LoraArgs& a, bool backward, int num_sms, int*
   p.drop = LoraDrop{a.seed, a.site, backward ? a.thr : 0u};
   p.err = err;
   const bool drop = p.drop.thr != 0u;
-  // rows of a tile: all of them, or equal parts of at most 256
-  const int row_tiles = (p.M + MAX_NT - 1) / MAX_NT;
-  p.nt = ((p.M + row_tiles - 1) / row_tiles + 15) / 16 * 16;
-  const int tiles = (p.F + BM - 1) / BM * row_tiles, kblocks = (p.C + BK - 1) / BK;
-  int splits = num_sms / tiles;
-  if (splits > 8) splits = 8;
-  if (splits > kblocks) splits = kblocks;
-  if (splits < 1) splits = 1;
+  const int kblocks = (p.C + BK - 1) / BK;
+  // Above 256 rows a CTA pair's tiles, of the size that leaves the fewest pairs idle: a tile costs its rows
+  // and what does not depend on them (about 64 rows' worth).
+  const bool pairs = p.M > MAX_NT;
+  int grid = 0, splits = 1;
+  if (pairs) {
+    const int all = num_sms / 2, ftiles = (p.F + PBM - 1) / PBM;
+    long long best = 0;
+    for (int nt = MAX_NT; nt >= 64; nt -= 32) {
+      const long long t = (long long)ftiles * ((p.M + nt - 1) / nt), cost = (t + all - 1) / all * (nt + 64);
+      if (best == 0 || cost < best) {
+        best = cost;
+        p.nt = nt;
+        grid = t < all ? (int)t : all;
+      }
+    }
+  } else {
+    p.nt = (p.M + 15) / 16 * 16;
+    const int tiles = (p.F + BM - 1) / BM;
+    splits = num_sms / tiles;
+    if (splits > 8) splits = 8;
+    if (splits > kblocks) splits = kblocks;
+    if (splits < 1) splits = 1;
+  }
   const uint32_t budget = 226u * 1024u;
-  p.stages = (int)((budget - tile_layout(0, p.nt).total) / (A_BYTES + (uint32_t)p.nt * 128u + 24u));
+  p.stages = pairs ? (int)((budget - pair_layout(0, p.nt).total) / (A_BYTES + (uint32_t)p.nt * 64u + 32u))
+                   : (int)((budget - tile_layout(0, p.nt).total) / (A_BYTES + (uint32_t)p.nt * 128u + 32u));
   if (p.stages > 10) p.stages = 10;
-  // the accumulators pass through the ring
-  const int cols = p.nt * (drop ? 2 : 1);
+  const int cols = p.nt * (drop || pairs ? 2 : 1);
   p.tmem_cols = 32;
   while (p.tmem_cols < cols) p.tmem_cols *= 2;
 
@@ -486,13 +895,18 @@ cudaError_t launch_lora_gemm(const LoraArgs& a, bool backward, int num_sms, int*
   const uint32_t wb[3] = {64, backward ? 64u : (uint32_t)BM, 1};
   const uint64_t xd[3] = {(uint64_t)p.C, (uint64_t)p.M, 1};
   const uint64_t ldx = (uint64_t)(backward ? a.ldy : a.ldx), xs[2] = {ldx * 2, ldx * 2 * (uint64_t)p.M};
-  const uint32_t xb[3] = {64, (uint32_t)p.nt, 1};
+  const uint32_t xb[3] = {64, (uint32_t)(pairs ? p.nt / 2 : p.nt), 1};
   const uint64_t fd[3] = {(uint64_t)(backward ? a.K : a.r), (uint64_t)(backward ? a.r : a.N), (uint64_t)a.n};
   const uint64_t fs[2] = {fd[0] * 2, fd[0] * fd[1] * 2};
   const uint32_t fb[3] = {backward ? 64u : (uint32_t)UNIT, backward ? (uint32_t)UNIT : (uint32_t)BM, 1};
   if (!encode_tensor_map_bf16(&w, a.w, 3, wd, ws, wb) || !encode_tensor_map_bf16(&x, backward ? a.dy : a.x, 3, xd, xs, xb) ||
       !encode_tensor_map_bf16(&f, backward ? a.a : a.b, 3, fd, fs, fb, backward ? 128 : 32))
     return cudaErrorInvalidValue;
+  if (pairs) {
+    if (!backward) return launch_pair<false, false>(w, x, f, p, grid, stream);
+    if (drop) return launch_pair<true, true>(w, x, f, p, grid, stream);
+    return launch_pair<true, false>(w, x, f, p, grid, stream);
+  }
   if (!backward) return launch_tile<false, false>(w, x, f, p, splits, stream);
   if (drop) return launch_tile<true, true>(w, x, f, p, splits, stream);
   return launch_tile<true, false>(w, x, f, p, splits, stream);
