@@ -6,14 +6,15 @@
 // and, with S_h = sum dz 1[unit h is on] (f, 1) in nine numbers, all gradients follow from S alone:
 //   dW1_h = w2_h S_h,  db1_h = w2_h S_h8,  dw2_h = W1_h . S_h + b1_h S_h8   (relu(x) = 1[x > 0] x),  db2 = sum dz.
 //
-// About a tenth of the positions are effective, so a CTA takes 512 positions at a time, compacts the
+// About a tenth of the positions are effective, so a CTA takes up to 2048 positions at a time, lists the
 // effective ones and gathers what they need into shared memory.  Their products with the MLP run with the hidden
 // units on the lanes: a thread keeps one or two pairs of units' weights and their sums S in registers (pairs, so
 // that each instruction does two units), and every decision's features come by broadcast.  Each sum over the
 // decisions then needs no exchange between threads; z does, one butterfly for four decisions.  Which units are on
 // is kept as bits between the two walks.  H up to 64 units fits one warp, and the eight warps take
 // decisions in turn; 256 units take two.  All sums have a fixed order.
-// The terms of the loss are summed in 64 bits.  KL is p g(-d/p) + q g(d/q), d = p - p_ref, g(x) = x -
+// The terms of the loss, db2 and the CTAs' sums are added as pairs of floats (hi + lo): 64-bit additions, of which an
+// SM issues about two a clock, took 70 us in the second kernel.  KL is p g(-d/p) + q g(d/q), d = p - p_ref, g(x) = x -
 // log(1 + x), whose first-order terms are gone before they could cancel.
 #include <math.h>
 
@@ -25,15 +26,18 @@ namespace cospec {
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int STEP = 512;                 // positions of a step
+constexpr int STEP = 2048;                // positions of a step, at most
 constexpr int PER = STEP / THREADS;
+constexpr int BATCH = 512;                // decisions gathered at a time
 constexpr int MAX_CTAS = 512;
+constexpr int CLUSTER = 8;                // CTAs that join their sums
 constexpr int FIN_THREADS = 1024;
 
 struct LossSmem {
-  float feat[STEP][8];
-  float adv[STEP], old[STEP], ref[STEP], g[STEP];
-  int at[STEP];                           // position | action taken << 31
+  float feat[BATCH][8];
+  float adv[BATCH], old[BATCH], ref[BATCH], g[BATCH];
+  int at[BATCH];                          // position in the step | action taken << 31
+  uint16_t list[STEP];                    // effective positions of the step
   uint32_t match[STEP / 32 + 2], act[STEP / 32];
 };
 
@@ -56,6 +60,16 @@ CS_DEV float log_rest(float x) {
     return x * x * s;
   }
   return x - log1pf(x);
+}
+
+// hi + lo: a running sum with what its roundings lost (Knuth's two-sum), and the sum of two such
+CS_DEV float2 add_to(float2 s, float x) {
+  const float t = __fadd_rn(s.x, x), b = __fsub_rn(t, s.x);
+  return make_float2(t, __fadd_rn(s.y, __fadd_rn(__fsub_rn(s.x, __fsub_rn(t, b)), __fsub_rn(x, b))));
+}
+CS_DEV float2 add_pair(float2 s, float2 x) {
+  const float2 t = add_to(s, x.x);
+  return make_float2(t.x, __fadd_rn(t.y, x.y));
 }
 
 struct Decision {
@@ -83,13 +97,13 @@ CS_DEV Decision decide(float z, float adv, float old, float ref, bool took, cons
 
 // PP: pairs of units of a thread; TW: warps that hold all units.
 template <int PP, int TW>
-__global__ void __launch_bounds__(THREADS) arb_loss_kernel(const ArbLossArgs a, float* ws_s, double* ws_l) {
+__global__ void __launch_bounds__(THREADS) arb_loss_kernel(const ArbLossArgs a, float* ws_s, float2* ws_l, int step) {
   extern __shared__ __align__(16) uint8_t raw[];
   LossSmem& sm = *reinterpret_cast<LossSmem*>(raw);
   constexpr int TEAMS = 8 / TW;
   constexpr int HP = 64 * PP * TW;                     // units that the threads hold
-  float* zpart = reinterpret_cast<float*>(raw + sizeof(LossSmem));               // [TW][STEP]
-  uint16_t* on = reinterpret_cast<uint16_t*>(zpart + TW * STEP);                 // [STEP / 4][TW * 32]
+  float* zpart = reinterpret_cast<float*>(raw + sizeof(LossSmem));               // [TW][BATCH]
+  uint16_t* on = reinterpret_cast<uint16_t*>(zpart + TW * BATCH);                // [BATCH / 4][TW * 32]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int team = warp / TW, tw = warp % TW;
   griddep_wait();
@@ -111,27 +125,27 @@ __global__ void __launch_bounds__(THREADS) arb_loss_kernel(const ArbLossArgs a, 
   }
   const float b2 = *a.b2, inv_k = 1.f / (float)a.K;
   const int total = a.n * a.K;
-  double sums[4] = {0., 0., 0., 0.};
+  float2 sums[4];                          // hi + lo
+#pragma unroll
+  for (int k = 0; k < 4; ++k) sums[k] = make_float2(0.f, 0.f);
 
-  for (long long base = (long long)blockIdx.x * STEP; base < total; base += (long long)gridDim.x * STEP) {
-    int pos[PER];
-    bool act[PER];
+  for (long long base = (long long)blockIdx.x * step; base < total; base += (long long)gridDim.x * step) {
+    const int words = step / 32;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
+      if (j * THREADS >= step) break;
       const long long e = base + j * THREADS + tid;
-      bool match = false;
-      act[j] = false;
-      pos[j] = (int)e;
+      bool match = false, act = false;
       if (e < total) {
-        const int r = (int)e / a.K, i = (int)e - r * a.K;
-        match = a.draft[e] == a.argmax[(size_t)r * (a.K + 1) + i];
-        act[j] = !match && a.eff[e] != 0;
-        if (!act[j]) {
+        const int r = (int)e / a.K;
+        match = a.draft[e] == a.argmax[e + r];           // rows of K + 1
+        act = !match && a.eff[e] != 0;
+        if (!act) {
           a.p_new[e] = 0.f;
           a.dz[e] = 0.f;
         }
       }
-      const unsigned mm = __ballot_sync(0xffffffffu, match), aa = __ballot_sync(0xffffffffu, act[j]);
+      const unsigned mm = __ballot_sync(0xffffffffu, match), aa = __ballot_sync(0xffffffffu, act);
       if (lane == 0) {
         sm.match[2 + j * 8 + warp] = mm;
         sm.act[j * 8 + warp] = aa;
@@ -141,34 +155,39 @@ __global__ void __launch_bounds__(THREADS) arb_loss_kernel(const ArbLossArgs a, 
       const long long e = base - 64 + warp * 32 + lane;
       bool match = false;
       if (e >= 0) {
-        const int r = (int)e / a.K, i = (int)e - r * a.K;
-        match = a.draft[e] == a.argmax[(size_t)r * (a.K + 1) + i];
+        const int r = (int)e / a.K;
+        match = a.draft[e] == a.argmax[e + r];
       }
       const unsigned mm = __ballot_sync(0xffffffffu, match);
       if (lane == 0) sm.match[warp] = mm;
     }
     __syncthreads();
-    int count = 0;
+    // the effective positions in order: warp w lists words w, w + 8, ..
+    const int c0 = lane < words ? __popc(sm.act[lane]) : 0, c1 = lane + 32 < words ? __popc(sm.act[lane + 32]) : 0;
+    int p0 = c0, p1 = c1;
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      int at = 0;
-      count = 0;
-#pragma unroll
-      for (int w = 0; w < STEP / 32; ++w) {
-        const int c = __popc(sm.act[w]);
-        if (w < j * 8 + warp) at += c;
-        count += c;
-      }
-      if (act[j]) {
-        at += __popc(sm.act[j * 8 + warp] & ((1u << lane) - 1u));
-        const int e = pos[j], r = e / a.K, i = e - r * a.K;
-        const float* s0 = a.stats + ((size_t)r * (a.K + 1) + i) * 5;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, p0, o), y = __shfl_up_sync(0xffffffffu, p1, o);
+      if (lane >= o) p0 += x, p1 += y;
+    }
+    const int sum0 = __shfl_sync(0xffffffffu, p0, 31), decisions = sum0 + __shfl_sync(0xffffffffu, p1, 31);
+    for (int w = warp; w < words; w += 8) {
+      const int before = w < 32 ? __shfl_sync(0xffffffffu, p0 - c0, w) : sum0 + __shfl_sync(0xffffffffu, p1 - c1, w - 32);
+      const unsigned bits = sm.act[w];
+      if ((bits >> lane) & 1u) sm.list[before + __popc(bits & ((1u << lane) - 1u))] = (uint16_t)(w * 32 + lane);
+    }
+    __syncthreads();
+    for (int d0 = 0; d0 < decisions; d0 += BATCH) {
+      const int count = min(BATCH, decisions - d0), groups = (count + 3) / 4;
+      for (int d = tid; d < count; d += THREADS) {
+        const int off = sm.list[d0 + d], e = (int)base + off, r = e / a.K, i = e - r * a.K;
+        const float* s0 = a.stats + ((size_t)e + r) * 5;
         const float* s1 = s0 + 5;
         const float x0 = s0[0], x1 = s0[1], x2 = s0[2], x3 = s0[3], x4 = s0[4], y0 = s1[0], y2 = s1[2], y4 = s1[4];
         const float adv = a.adv[e], old = a.p_old[e], ref = a.p_ref[e];
         const bool took = a.accept[e] != 0;
         int before = 0;                      // matches of the round before position i: bits [lo, hi) of match
-        const int hi = 64 + j * THREADS + tid, lo = hi - i;
+        const int hi = 64 + off, lo = hi - i;
 #pragma unroll
         for (int w = 0; w < 3; ++w) {
           const int word = (hi >> 5) - w;
@@ -178,174 +197,205 @@ __global__ void __launch_bounds__(THREADS) arb_loss_kernel(const ArbLossArgs a, 
           if (word * 32 < lo) m &= 0xffffffffu << (lo & 31);
           before += __popc(m);
         }
-        float4* f = reinterpret_cast<float4*>(sm.feat[at]);
+        float4* f = reinterpret_cast<float4*>(sm.feat[d]);
         f[0] = make_float4(x4 - x2, x0 - x2, x0 - x1, x3);
         f[1] = make_float4(y0 - y2, i + 1 < a.K ? y4 - y2 : 0.f, (float)(i + 1) * inv_k, (float)before * inv_k);
-        sm.adv[at] = adv;
-        sm.old[at] = old;
-        sm.ref[at] = ref;
-        sm.at[at] = took ? (int)((unsigned)e | 0x80000000u) : e;
+        sm.adv[d] = adv;
+        sm.old[d] = old;
+        sm.ref[d] = ref;
+        sm.at[d] = took ? (int)((unsigned)off | 0x80000000u) : off;
       }
-    }
-    __syncthreads();
-    const int groups = (count + 3) / 4;
-    for (int q = team; q < groups; q += TEAMS) {
-      float z[4];
-      unsigned bits = 0;
+      __syncthreads();
+      for (int q = team; q < groups; q += TEAMS) {
+        float z[4];
+        unsigned bits = 0;
 #pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        const float4 fa = *reinterpret_cast<const float4*>(&sm.feat[4 * q + d][0]);
-        const float4 fb = *reinterpret_cast<const float4*>(&sm.feat[4 * q + d][4]);
-        const float f[8] = {fa.x, fa.y, fa.z, fa.w, fb.x, fb.y, fb.z, fb.w};
-        float2 zz = make_float2(0.f, 0.f);
+        for (int d = 0; d < 4; ++d) {
+          const float4 fa = *reinterpret_cast<const float4*>(&sm.feat[4 * q + d][0]);
+          const float4 fb = *reinterpret_cast<const float4*>(&sm.feat[4 * q + d][4]);
+          const float f[8] = {fa.x, fa.y, fa.z, fa.w, fb.x, fb.y, fb.z, fb.w};
+          float2 zz = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int i = 0; i < PP; ++i) {
-          float2 v = b1[i];
+          for (int i = 0; i < PP; ++i) {
+            float2 v = b1[i];
 #pragma unroll
-          for (int k = 0; k < 8; ++k) v = fma2(w1[i][k], make_float2(f[k], f[k]), v);
-          bits |= ((v.x > 0.f ? 1u : 0u) | (v.y > 0.f ? 2u : 0u)) << (4 * d + 2 * i);
-          zz = fma2(w2[i], make_float2(fmaxf(v.x, 0.f), fmaxf(v.y, 0.f)), zz);
+            for (int k = 0; k < 8; ++k) v = fma2(w1[i][k], make_float2(f[k], f[k]), v);
+            bits |= ((v.x > 0.f ? 1u : 0u) | (v.y > 0.f ? 2u : 0u)) << (4 * d + 2 * i);
+            zz = fma2(w2[i], make_float2(fmaxf(v.x, 0.f), fmaxf(v.y, 0.f)), zz);
+          }
+          z[d] = zz.x + zz.y;
         }
-        z[d] = zz.x + zz.y;
+        on[q * (TW * 32) + tw * 32 + lane] = (uint16_t)bits;
+        // four sums over the warp; lanes 0, 8, 16, 24 end with decisions 0, 1, 2, 3
+        const bool up = lane & 16, up2 = lane & 8;
+        const float s0 = __shfl_xor_sync(0xffffffffu, up ? z[0] : z[2], 16), s1 = __shfl_xor_sync(0xffffffffu, up ? z[1] : z[3], 16);
+        const float t0 = (up ? z[2] : z[0]) + s0, t1 = (up ? z[3] : z[1]) + s1;
+        float v = (up2 ? t1 : t0) + __shfl_xor_sync(0xffffffffu, up2 ? t0 : t1, 8);
+        v += __shfl_xor_sync(0xffffffffu, v, 4);
+        v += __shfl_xor_sync(0xffffffffu, v, 2);
+        v += __shfl_xor_sync(0xffffffffu, v, 1);
+        if ((lane & 7) == 0) zpart[tw * BATCH + 4 * q + (lane >> 3)] = v;
       }
-      on[q * (TW * 32) + tw * 32 + lane] = (uint16_t)bits;
-      // four sums over the warp; lanes 0, 8, 16, 24 end with decisions 0, 1, 2, 3
-      const bool up = lane & 16, up2 = lane & 8;
-      const float s0 = __shfl_xor_sync(0xffffffffu, up ? z[0] : z[2], 16), s1 = __shfl_xor_sync(0xffffffffu, up ? z[1] : z[3], 16);
-      const float t0 = (up ? z[2] : z[0]) + s0, t1 = (up ? z[3] : z[1]) + s1;
-      float v = (up2 ? t1 : t0) + __shfl_xor_sync(0xffffffffu, up2 ? t0 : t1, 8);
-      v += __shfl_xor_sync(0xffffffffu, v, 4);
-      v += __shfl_xor_sync(0xffffffffu, v, 2);
-      v += __shfl_xor_sync(0xffffffffu, v, 1);
-      if ((lane & 7) == 0) zpart[tw * STEP + 4 * q + (lane >> 3)] = v;
-    }
-    __syncthreads();
-    for (int d = tid; d < 4 * groups; d += THREADS) {
-      float g = 0.f;
-      if (d < count) {
-        float z = zpart[d];
+      __syncthreads();
+      for (int d = tid; d < 4 * groups; d += THREADS) {
+        float g = 0.f;
+        if (d < count) {
+          float z = zpart[d];
 #pragma unroll
-        for (int w = 1; w < TW; ++w) z += zpart[w * STEP + d];
-        const int at = sm.at[d];
-        const Decision x = decide(z + b2, sm.adv[d], sm.old[d], sm.ref[d], at < 0, a);
-        const int e = at & 0x7fffffff;
-        g = x.dz * a.grad_scale;
-        a.p_new[e] = x.p;
-        a.dz[e] = g;
-        sums[0] += (double)x.surr;
-        sums[1] += (double)x.ent;
-        sums[2] += (double)x.kl;
-        sums[3] += (double)g;
+          for (int w = 1; w < TW; ++w) z += zpart[w * BATCH + d];
+          const int at = sm.at[d];
+          const Decision x = decide(z + b2, sm.adv[d], sm.old[d], sm.ref[d], at < 0, a);
+          const int e = (int)base + (at & 0x7fffffff);
+          g = x.dz * a.grad_scale;
+          a.p_new[e] = x.p;
+          a.dz[e] = g;
+          sums[0] = add_to(sums[0], x.surr);
+          sums[1] = add_to(sums[1], x.ent);
+          sums[2] = add_to(sums[2], x.kl);
+          sums[3] = add_to(sums[3], g);
+        }
+        sm.g[d] = g;
       }
-      sm.g[d] = g;
-    }
-    __syncthreads();
-    for (int q = team; q < groups; q += TEAMS) {
-      const unsigned bits = on[q * (TW * 32) + tw * 32 + lane];
+      __syncthreads();
+      for (int q = team; q < groups; q += TEAMS) {
+        const unsigned bits = on[q * (TW * 32) + tw * 32 + lane];
 #pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        if (4 * q + d >= count) break;       // what stands there is of another step
-        const float4 fa = *reinterpret_cast<const float4*>(&sm.feat[4 * q + d][0]);
-        const float4 fb = *reinterpret_cast<const float4*>(&sm.feat[4 * q + d][4]);
-        const float f[8] = {fa.x, fa.y, fa.z, fa.w, fb.x, fb.y, fb.z, fb.w};
-        const float g = sm.g[4 * q + d];
+        for (int d = 0; d < 4; ++d) {
+          if (4 * q + d >= count) break;     // what stands there is of another batch
+          const float4 fa = *reinterpret_cast<const float4*>(&sm.feat[4 * q + d][0]);
+          const float4 fb = *reinterpret_cast<const float4*>(&sm.feat[4 * q + d][4]);
+          const float f[8] = {fa.x, fa.y, fa.z, fa.w, fb.x, fb.y, fb.z, fb.w};
+          const float g = sm.g[4 * q + d];
 #pragma unroll
-        for (int i = 0; i < PP; ++i) {
-          const float2 m = make_float2((bits >> (4 * d + 2 * i)) & 1u ? g : 0.f, (bits >> (4 * d + 2 * i)) & 2u ? g : 0.f);
+          for (int i = 0; i < PP; ++i) {
+            const float2 m = make_float2((bits >> (4 * d + 2 * i)) & 1u ? g : 0.f, (bits >> (4 * d + 2 * i)) & 2u ? g : 0.f);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) S[i][k] = fma2(m, make_float2(f[k], f[k]), S[i][k]);
-          S[i][8] = add2(S[i][8], m);
+            for (int k = 0; k < 8; ++k) S[i][k] = fma2(m, make_float2(f[k], f[k]), S[i][k]);
+            S[i][8] = add2(S[i][8], m);
+          }
         }
       }
+      __syncthreads();
     }
-    __syncthreads();
   }
 
-  // the teams' sums, then the CTA's to the workspace: [9][HP]
-  float* red = reinterpret_cast<float*>(raw);          // [TEAMS][9][HP]
+  // the teams' sums, then those of the cluster's CTAs: [9][HP] to the workspace, with the loss terms behind them
+  float* red = reinterpret_cast<float*>(raw);          // [TEAMS][9][HP], the first then the CTA's
+  float2* lsum = reinterpret_cast<float2*>(red + TEAMS * 9 * HP);    // [8][4], then [4]
 #pragma unroll
   for (int i = 0; i < PP; ++i)
 #pragma unroll
     for (int k = 0; k < 9; ++k)
       *reinterpret_cast<float2*>(&red[(team * 9 + k) * HP + 2 * ((i * TW + tw) * 32 + lane)]) = S[i][k];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    float2 v = sums[k];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+      v = add_pair(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
+    if (lane == 0) lsum[4 + warp * 4 + k] = v;
+  }
   __syncthreads();
   for (int e = tid; e < 9 * HP; e += THREADS) {
     float s = red[e];
 #pragma unroll
     for (int m = 1; m < TEAMS; ++m) s += red[m * 9 * HP + e];
-    ws_s[(size_t)blockIdx.x * 9 * HP + e] = s;
+    red[e] = s;
   }
-  __syncthreads();
-  double* wsum = reinterpret_cast<double*>(raw);       // [8][4]
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    double v = sums[k];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if (lane == 0) wsum[warp * 4 + k] = v;
-  }
-  __syncthreads();
   if (tid < 4) {
-    double v = 0.;
-    for (int w = 0; w < 8; ++w) v += wsum[w * 4 + tid];
-    ws_l[(size_t)blockIdx.x * 4 + tid] = v;
+    float2 v = make_float2(0.f, 0.f);
+    for (int w = 0; w < 8; ++w) v = add_pair(v, lsum[4 + w * 4 + tid]);
+    lsum[tid] = v;
   }
+  __syncthreads();
+  __syncwarp();
+  cluster_arrive();
+  cluster_wait();
+  const int CS = (int)cluster_nctarank(), rank = (int)cluster_ctarank(), group = (int)blockIdx.x / CS;
+  const uint32_t red0 = smem_u32(red);
+  float* out = ws_s + (size_t)group * 9 * HP;
+  for (int e = rank * THREADS + tid; e < 9 * HP; e += CS * THREADS) {
+    float s = 0.f;
+    for (int i = 0; i < CS; ++i) {
+      float w;
+      asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w) : "r"(dsmem_map(red0 + 4u * (uint32_t)e, (uint32_t)i)) : "memory");
+      s += w;
+    }
+    out[e] = s;
+  }
+  if (rank == 0 && tid < 4) {
+    float2 v = make_float2(0.f, 0.f);
+    for (int i = 0; i < CS; ++i) {
+      float2 w;
+      asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];"
+                   : "=f"(w.x), "=f"(w.y)
+                   : "r"(dsmem_map(smem_u32(&lsum[tid]), (uint32_t)i))
+                   : "memory");
+      v = add_pair(v, w);
+    }
+    ws_l[(size_t)group * 4 + tid] = v;
+  }
+  __syncwarp();
+  cluster_arrive();                        // nobody leaves while its sums are read
+  cluster_wait();
 }
 
-// The CTAs' sums of 32 units (a lane each; 32 warps take CTAs in turn), then the gradients; block 0 the loss.
-__global__ void __launch_bounds__(FIN_THREADS) arb_loss_finish_kernel(const ArbLossArgs a, const float* ws_s, const double* ws_l, int ctas, int hp) {
-  __shared__ double part[32][33];
-  __shared__ double tot[9][32];
+// The clusters' sums of 32 units (a lane each; of the 27 warps three share each of the nine numbers), then the
+// gradients; block 0 the loss.
+__global__ void __launch_bounds__(FIN_THREADS) arb_loss_finish_kernel(const ArbLossArgs a, const float* ws_s, const float2* ws_l, int groups, int hp) {
+  __shared__ float2 part[27][32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int h = blockIdx.x * 32 + lane;
+  float w1[8], b1 = 0.f, w2 = 0.f;
+  if (warp == 0 && h < a.H) {
+    // (weights: not written by the kernel before)
+    w2 = a.w2[h];
+    b1 = a.b1[h];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w1[k] = a.w1[(size_t)h * 8 + k];
+  }
   griddep_wait();
   griddep_launch_dependents();
-  float s[9];
-  double sd[9];
+  if (warp < 27) {
+    const int k = warp % 9;
+    float2 s = make_float2(0.f, 0.f);
+#pragma unroll 8
+    for (int c = warp / 9; c < groups; c += 3) s = add_to(s, ws_s[((size_t)c * 9 + k) * hp + h]);
+    part[warp][lane] = s;
+  } else if (blockIdx.x == 0 && warp == 27) {
+    float2 v[4];
 #pragma unroll
-  for (int k = 0; k < 9; ++k) sd[k] = 0.;
-  for (int c = warp; c < ctas; c += 32) {
+    for (int k = 0; k < 4; ++k) v[k] = make_float2(0.f, 0.f);
+    for (int c = lane; c < groups; c += 32)
 #pragma unroll
-    for (int k = 0; k < 9; ++k) s[k] = ws_s[((size_t)c * 9 + k) * hp + h];
-#pragma unroll
-    for (int k = 0; k < 9; ++k) sd[k] += (double)s[k];
-  }
-  for (int k = 0; k < 9; ++k) {
-    part[warp][lane] = sd[k];
-    __syncthreads();
-    double v = part[lane][warp];           // warp: unit, lane: part
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if (lane == 0) tot[k][warp] = v;
-    __syncthreads();
-  }
-  if (warp == 0 && h < a.H) {
-    const double w2 = (double)a.w2[h];
-    double dw2 = (double)a.b1[h] * tot[8][lane];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      a.dw1[(size_t)h * 8 + k] = (float)(w2 * tot[k][lane]);
-      dw2 += (double)a.w1[(size_t)h * 8 + k] * tot[k][lane];
-    }
-    a.db1[h] = (float)(w2 * tot[8][lane]);
-    a.dw2[h] = (float)dw2;
-  }
-  if (blockIdx.x == 0 && warp == 1) {
-    double v[4] = {0., 0., 0., 0.};
-    for (int c = lane; c < ctas; c += 32)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] += ws_l[(size_t)c * 4 + k];
+      for (int k = 0; k < 4; ++k) v[k] = add_pair(v[k], ws_l[(size_t)c * 4 + k]);
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+      for (int o = 16; o > 0; o >>= 1)
+        v[k] = add_pair(v[k], make_float2(__shfl_xor_sync(0xffffffffu, v[k].x, o), __shfl_xor_sync(0xffffffffu, v[k].y, o)));
     if (lane == 0) {
-      a.loss[0] = (float)v[0];
-      a.loss[1] = (float)v[1];
-      a.loss[2] = (float)v[2];
-      a.loss[3] = (float)(-v[0] - (double)a.beta_h * v[1] + (double)a.beta_kl * v[2]);
-      *a.db2 = (float)v[3];
+      const double surr = (double)v[0].x + (double)v[0].y, ent = (double)v[1].x + (double)v[1].y, kl = (double)v[2].x + (double)v[2].y;
+      a.loss[0] = (float)surr;
+      a.loss[1] = (float)ent;
+      a.loss[2] = (float)kl;
+      a.loss[3] = (float)(-surr - (double)a.beta_h * ent + (double)a.beta_kl * kl);
+      *a.db2 = v[3].x + v[3].y;
     }
+  }
+  __syncthreads();
+  if (warp == 0 && h < a.H) {
+    float2 dw2 = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < 9; ++k) {
+      const float2 t = add_pair(add_pair(part[k][lane], part[9 + k][lane]), part[18 + k][lane]);
+      if (k < 8) a.dw1[(size_t)h * 8 + k] = fmaf(w2, t.x, w2 * t.y);
+      else a.db1[h] = fmaf(w2, t.x, w2 * t.y);
+      // w1 . S + b1 S_8 cancels: the products as pairs
+      const float w = k < 8 ? w1[k & 7] : b1, prod = w * t.x;
+      dw2 = add_pair(dw2, make_float2(prod, fmaf(w, t.x, -prod) + w * t.y));
+    }
+    a.dw2[h] = dw2.x + dw2.y;
   }
 }
 
@@ -355,21 +405,42 @@ template <int PP, int TW>
 cudaError_t launch_loss(const ArbLossArgs& a, int num_sms, cudaStream_t stream) {
   static KernelLimits lim;
   constexpr int HP = 64 * PP * TW;
-  size_t smem = sizeof(LossSmem) + (size_t)TW * STEP * 4 + (size_t)(STEP / 4) * TW * 32 * 2;
-  const size_t red = (size_t)(8 / TW) * 9 * HP * 4;
+  size_t smem = sizeof(LossSmem) + (size_t)TW * BATCH * 4 + (size_t)(BATCH / 4) * TW * 32 * 2;
+  const size_t red = (size_t)(8 / TW) * 9 * HP * 4 + 36 * sizeof(float2);
   if (smem < red) smem = red;
   cudaError_t e = ensure_kernel_limits((const void*)arb_loss_kernel<PP, TW>, lim, smem, false);
   if (e != cudaSuccess) return e;
-  const long long steps = ((long long)a.n * a.K + STEP - 1) / STEP;
-  int ctas = 2 * num_sms;
-  if (ctas > MAX_CTAS) ctas = MAX_CTAS;
-  if (ctas > steps) ctas = (int)steps;
-  if (ctas < 1) ctas = 1;
-  double* ws_l = static_cast<double*>(a.ws);
+  // as many positions a step as give every CTA one, up to 2048; clusters of eight where there are that many CTAs
+  const long long total = (long long)a.n * a.K;
+  // (two CTAs an SM; of clusters of eight about 15 / 16 of the SMs' places are filled)
+  int most = 15 * num_sms / 8 / CLUSTER * CLUSTER;
+  if (most > MAX_CTAS) most = MAX_CTAS;
+  if (most < 1) most = 1;
+  long long step = ((total + most - 1) / most + THREADS - 1) / THREADS * THREADS;
+  step = step < THREADS ? THREADS : step > STEP ? STEP : step;
+  const long long steps = (total + step - 1) / step;
+  int ctas = steps < 1 ? 1 : steps < most ? (int)steps : most;
+  const int cs = ctas >= CLUSTER ? CLUSTER : 1;
+  ctas = (ctas + cs - 1) / cs * cs;
+  float2* ws_l = static_cast<float2*>(a.ws);
   float* ws_s = reinterpret_cast<float*>(ws_l + (size_t)MAX_CTAS * 4);
-  e = launch_pdl(arb_loss_kernel<PP, TW>, dim3(ctas), dim3(THREADS), smem, stream, a, ws_s, ws_l);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)cs;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  e = cudaLaunchKernelEx(&cfg, arb_loss_kernel<PP, TW>, a, ws_s, ws_l, (int)step);
   if (e != cudaSuccess) return e;
-  return launch_pdl(arb_loss_finish_kernel, dim3((a.H + 31) / 32), dim3(FIN_THREADS), 0, stream, a, (const float*)ws_s, (const double*)ws_l, ctas, HP);
+  return launch_pdl(arb_loss_finish_kernel, dim3((a.H + 31) / 32), dim3(FIN_THREADS), 0, stream, a, (const float*)ws_s, (const float2*)ws_l, ctas / cs, HP);
 }
 
 }  // namespace

@@ -5,13 +5,12 @@
 //
 // mma.sync with the rank as M, columns of Q as N and the rows as the contraction.  P enters as three
 // bf16 parts, which hold all 24 bits of it, so the sums are those of fp32 products (a gradient that is
-// summed over micro-batches starts from fp32).  A lane loads 16 bytes of a row of Q, and movmatrix turns the 8 x 8
-// blocks into fragments; the order of the columns inside a block of 32 that comes of it is undone when
-// the sums are written.  A lane's 16 bytes are one draw of the dropout mask.
+// summed over micro-batches starts from fp32).
 //
-// A CTA takes 128 columns of one adapter (and 64 of its ranks); the rows are split over the CTAs of a cluster
-// and four row groups of warps and joined in a fixed order.  The rows of the adapter are listed in shared memory
-// first, so rows of other adapters, and what they hold, are not read.
+// A CTA takes 256 columns of one adapter, 32 a warp; the adapter's rows, listed in shared memory first, so that rows
+// of other adapters and what they hold are not read, come 64 at a time: Q by cp.async into a ring, P through
+// registers, where it is split once for all warps.  A thread masks the 16-byte chunks of x that it copied itself, each one
+// draw of the generator.  The rows are split over the CTAs of a cluster and joined in a fixed order.
 #include "lora.cuh"
 
 namespace cospec {
@@ -19,8 +18,11 @@ namespace cospec {
 namespace {
 
 constexpr int GRAD_THREADS = 256;
-constexpr int CB = 128;              // columns of a CTA
+constexpr int CB = 256;              // columns of a CTA
+constexpr int BR = 64;               // rows of a batch
+constexpr int GDEPTH = 3;            // batches in the ring
 constexpr int WIN = 2048;            // rows listed at a time
+constexpr uint32_t Q_BYTES = BR * CB * 2;
 
 struct GradArgs {
   const __nv_bfloat16 *x, *dy;
@@ -38,47 +40,57 @@ struct GradArgs {
 struct GradSmem {
   int list[WIN];
   int warp_count[8];
-  int count;
 };
+// the ring of Q, two buffers of P's parts [3][64 rows][R], the list; then the sums, [R][CB + 8] or [CB][R + 4]
+__host__ __device__ constexpr uint32_t grad_p_bytes(int R) { return (uint32_t)(3 * BR * R * 2); }
+__host__ __device__ constexpr uint32_t grad_bytes(int R) {
+  return GDEPTH * Q_BYTES + 2 * grad_p_bytes(R) + (uint32_t)sizeof(GradSmem);
+}
 
 template <int RT>
 __global__ void __launch_bounds__(GRAD_THREADS) lora_grad_kernel(const GradArgs p) {
-  extern __shared__ __align__(16) uint8_t raw[];
-  GradSmem& sm = *reinterpret_cast<GradSmem*>(raw);
-  float* red = reinterpret_cast<float*>(raw + (sizeof(GradSmem) + 15) / 16 * 16);   // [4 warps][64 columns][16 RT]
+  extern __shared__ __align__(128) uint8_t raw[];
   constexpr int R = 16 * RT;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  constexpr int PV = BR * R / GRAD_THREADS;            // values of P a thread splits per batch
+  constexpr uint32_t P_PART = (uint32_t)(BR * R * 2);
+  GradSmem& sm = *reinterpret_cast<GradSmem*>(raw + GDEPTH * Q_BYTES + 2 * grad_p_bytes(R));
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const int S = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
   const int block = (int)blockIdx.x / S, which = block >= p.blocks0;
   const int c0 = (which ? block - p.blocks0 : block) * CB;
-  const int a = (int)blockIdx.y, j0 = (int)blockIdx.z * 64;
-  const int cw = c0 + (warp & 1) * 64, rg = warp >> 1;       // the warp's columns and row group
+  const int a = (int)blockIdx.y;
   const __nv_bfloat16* Q = which ? p.dy : p.x;
   const float* P = which ? p.u : p.t;
   const long long ld = which ? p.ldy : p.ldx;
   const int width = which ? p.N : p.K;
   const bool drop = which == 0 && p.drop.thr != 0u;
+  const uint32_t q0 = smem_u32(raw), p0 = q0 + GDEPTH * Q_BYTES;
   griddep_wait();
   griddep_launch_dependents();
   LoraKey key{0, 0};
   if (drop) key = lora_key(p.drop);
 
-  float acc[RT][8][4];
+  float acc[RT][4][4];
 #pragma unroll
   for (int i = 0; i < RT; ++i)
 #pragma unroll
-    for (int c = 0; c < 8; ++c)
+    for (int c = 0; c < 4; ++c)
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[i][c][e] = 0.f;
 
+  // 512-byte rows of Q, 2 R byte rows of P; the 16-byte chunks exchanged by the row, so that eight neighbouring rows lie
+  // on different banks
+  auto p_at = [&](int row, int c) {
+    const int sw = RT >= 4 ? row & 7 : RT == 2 ? (row >> 1) & 3 : (row >> 2) & 1;
+    return (uint32_t)(row * (R * 2) + ((c ^ sw) << 4));
+  };
   const int m_lo = (int)((long long)p.M * rank / S), m_hi = (int)((long long)p.M * (rank + 1) / S);
   for (int w0 = m_lo; w0 < m_hi; w0 += WIN) {
     // the adapter's rows of the window, in order
     const int w1 = min(w0 + WIN, m_hi);
     int have = 0;
-    __syncthreads();                     // the list before is read
     for (int b = w0; b < w1; b += GRAD_THREADS) {
-      const int m = b + (int)threadIdx.x;
+      const int m = b + tid;
       const bool in = m < w1 && p.adapter[m] == a;
       const unsigned mask = __ballot_sync(0xffffffffu, in);
       if (lane == 0) sm.warp_count[warp] = __popc(mask);
@@ -93,109 +105,123 @@ __global__ void __launch_bounds__(GRAD_THREADS) lora_grad_kernel(const GradArgs 
       if (in) sm.list[at] = m;
       __syncthreads();
     }
-    for (int b = rg * 16; b < have; b += 64) {
-      // rows of the fragments: loads by the lane's row g (and g + 8), products by 2 t, 2 t + 1 (and + 8)
-      uint4 v[2][2];
-      int row[2];
+    const int batches = (have + BR - 1) / BR;
+    // chunk i of a batch's Q: row (tid + 256 i) / 32, columns 8 (tid mod 32) ..
+    const int qc = tid & 31, col = c0 + 8 * qc;
+    auto load_q = [&](int b) {
+      if (b < batches) {
+        const uint32_t dst = q0 + (uint32_t)(b % GDEPTH) * Q_BYTES;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        row[h] = b + g + 8 * h < have ? sm.list[b + g + 8 * h] : -1;
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int col = cw + 32 * c + 8 * t;
-          v[h][c] = make_uint4(0, 0, 0, 0);
-          if (row[h] >= 0 && col < width) v[h][c] = ldg16(Q + (long long)row[h] * ld + col);
+        for (int i = 0; i < BR / 8; ++i) {
+          const int row = (tid >> 5) + 8 * i;
+          const bool on = b * BR + row < have && col < width;
+          cp_async16(dst + (uint32_t)(row * 512 + ((qc ^ (row & 7)) << 4)), on ? Q + (long long)sm.list[b * BR + row] * ld + col : Q, on);
         }
       }
-      uint32_t pa[RT][3][4];
+      cp_async_commit();
+    };
+    // value i of a batch's P: pairs along the rank, (tid + 256 i) counts pairs
+    float2 pv[PV / 2];
+    auto load_p = [&](int b) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {       // rows 8 h + 2 t, + 1
-        const int i0 = b + 8 * h + 2 * t;
-        const int m0 = i0 < have ? sm.list[i0] : -1, m1 = i0 + 1 < have ? sm.list[i0 + 1] : -1;
+      for (int i = 0; i < PV / 2; ++i) {
+        const int e = tid + GRAD_THREADS * i, row = e / (R / 2), j = 2 * (e % (R / 2));
+        pv[i] = make_float2(0.f, 0.f);
+        if (b * BR + row < have && j < p.r) pv[i] = __ldg(reinterpret_cast<const float2*>(P + (size_t)sm.list[b * BR + row] * p.r + j));
+      }
+    };
+    auto store_p = [&](int b) {
+      const uint32_t dst = (uint32_t)(b & 1) * grad_p_bytes(R);
+#pragma unroll
+      for (int i = 0; i < PV / 2; ++i) {
+        const int e = tid + GRAD_THREADS * i, row = e / (R / 2), j = 2 * (e % (R / 2));
+        float x = pv[i].x, y = pv[i].y;
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+          float hx, lx, hy, ly;
+          lora_split2(x, hx, lx);
+          lora_split2(y, hy, ly);
+          *reinterpret_cast<uint32_t*>(raw + GDEPTH * Q_BYTES + dst + k * P_PART + p_at(row, j >> 3) + (j & 7) * 2) = pack_bf16(hx, hy);
+          x = lx;
+          y = ly;
+        }
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < GDEPTH - 1; ++i) load_q(i);
+    load_p(0);
+    for (int b = 0; b < batches; ++b) {
+      store_p(b);
+      cp_async_wait<GDEPTH - 2>();
+      const uint32_t qb = q0 + (uint32_t)(b % GDEPTH) * Q_BYTES;
+      if (drop) {
+#pragma unroll 2
+        for (int i = 0; i < BR / 8; ++i) {
+          const int row = (tid >> 5) + 8 * i;
+          if (b * BR + row >= have) break;
+          uint4* q = reinterpret_cast<uint4*>(raw + (qb - q0) + row * 512 + ((qc ^ (row & 7)) << 4));
+          *q = and4(*q, lora_keep8((uint32_t)(col >> 3), (uint32_t)sm.list[b * BR + row], p.drop, key));
+        }
+      }
+      __syncthreads();
+      load_q(b + GDEPTH - 1);
+      if (b + 1 < batches) load_p(b + 1);
+      const uint32_t pb = p0 + (uint32_t)(b & 1) * grad_p_bytes(R);
+      const int steps = min(BR / 16, (have - b * BR + 15) / 16);
+      for (int ks = 0; ks < steps; ++ks) {
+        const int row = ks * 16 + (lane & 15);
+        uint32_t bq[4][2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {      // 16 columns: (k 0-7, 8-15) of the first eight, then of the others
+          const int cc = warp * 4 + 2 * c + (lane >> 4);
+          ldsm_x4_t(qb + (uint32_t)(row * 512 + ((cc ^ (row & 7)) << 4)), bq[2 * c][0], bq[2 * c][1], bq[2 * c + 1][0], bq[2 * c + 1][1]);
+        }
+        // the rank's blocks: (ranks 0-7, k 0-7), (8-15, 0-7), (0-7, 8-15), (8-15, 8-15), stored with k along the rows
+        const int pr = ks * 16 + (lane & 7) + ((lane >> 4) << 3);
 #pragma unroll
         for (int i = 0; i < RT; ++i)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int j = j0 + 16 * i + 8 * e + g;
-            float x = m0 >= 0 && j < p.r ? __ldg(P + (size_t)m0 * p.r + j) : 0.f;
-            float y = m1 >= 0 && j < p.r ? __ldg(P + (size_t)m1 * p.r + j) : 0.f;
+          for (int k = 0; k < 3; ++k) {
+            uint32_t pa[4];
+            ldsm_x4_t(pb + (uint32_t)k * P_PART + p_at(pr, 2 * i + ((lane >> 3) & 1)), pa[0], pa[1], pa[2], pa[3]);
 #pragma unroll
-            for (int k = 0; k < 3; ++k) {
-              float hx, lx, hy, ly;
-              lora_split2(x, hx, lx);
-              lora_split2(y, hy, ly);
-              pa[i][k][2 * h + e] = pack_bf16(hx, hy);
-              x = lx;
-              y = ly;
-            }
+            for (int c = 0; c < 4; ++c) mma_16816(acc[i][c], pa, bq[c][0], bq[c][1]);
           }
       }
-      if (drop) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int c = 0; c < 2; ++c)
-            v[h][c] = and4(v[h][c], lora_keep8((uint32_t)((cw + 32 * c) / 8 + t), (uint32_t)row[h], p.drop, key));
-      }
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const uint32_t lo[4] = {v[0][c].x, v[0][c].y, v[0][c].z, v[0][c].w}, hi[4] = {v[1][c].x, v[1][c].y, v[1][c].z, v[1][c].w};
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const uint32_t b0 = movmatrix_t(lo[q]), b1 = movmatrix_t(hi[q]);
-#pragma unroll
-          for (int i = 0; i < RT; ++i)
-#pragma unroll
-            for (int k = 0; k < 3; ++k) mma_16816(acc[i][4 * c + q], pa[i][k], b0, b1);
-        }
-      }
     }
+    cp_async_wait<0>();
+    __syncthreads();                       // the list and the ring are read
   }
 
-  // Row groups 2, 3 into 0, 1, then 1 into 0.  A buffer holds a warp's sums as [column][rank]; its column of
-  // block c of 32, group q, fragment column 2 t + e is 32 c + 8 t + 2 q + e.
-  auto each = [&](auto&& f) {
+  float* red = reinterpret_cast<float*>(raw);
+  constexpr int LA = CB + 8, LB = R + 4;
 #pragma unroll
-    for (int i = 0; i < RT; ++i)
+  for (int i = 0; i < RT; ++i)
 #pragma unroll
-      for (int c = 0; c < 8; ++c)
+    for (int c = 0; c < 4; ++c)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int col = 32 * (c >> 2) + 8 * t + 2 * (c & 3) + (e & 1), j = 16 * i + g + 8 * (e >> 1);
-          f(col * R + j, acc[i][c][e]);
-        }
-  };
-#pragma unroll
-  for (int half = 2; half >= 1; half >>= 1) {
-    __syncthreads();
-    if (rg >= half && rg < 2 * half) each([&](int at, float& x) { red[((rg - half) * 2 + (warp & 1)) * 64 * R + at] = x; });
-    __syncthreads();
-    if (rg < half) each([&](int at, float& x) { x += red[(rg * 2 + (warp & 1)) * 64 * R + at]; });
-  }
+      for (int e = 0; e < 4; ++e) {
+        const int n = warp * 32 + c * 8 + 2 * t + (e & 1), j = 16 * i + g + 8 * (e >> 1);
+        red[which ? n * LB + j : j * LA + n] = acc[i][c][e];
+      }
   __syncthreads();
-  if (rg == 0) each([&](int at, float& x) { red[(warp & 1) * 64 * R + at] = x; });       // [CB columns][R]
-  __syncthreads();
+  __syncwarp();
   cluster_arrive();
   cluster_wait();
   const uint32_t base = smem_u32(red);
   const int e0 = CB * R * rank / S, e1 = CB * R * (rank + 1) / S;
   float* out = which ? p.db : p.da;
-  for (int e = e0 + (int)threadIdx.x; e < e1; e += GRAD_THREADS) {
-    // dB: [column][rank] as it stands; dA: neighbouring threads take neighbouring columns
-    int col, j;
-    if (which) {
-      col = e / R, j = e % R;
-    } else {
-      col = e % CB, j = e / CB;
-    }
-    if (c0 + col >= width || j0 + j >= p.r) continue;
+  for (int e = e0 + tid; e < e1; e += GRAD_THREADS) {
+    const int n = which ? e / R : e % CB, j = which ? e % R : e / CB;
+    if (c0 + n >= width || j >= p.r) continue;
+    const uint32_t at = base + 4u * (uint32_t)(which ? n * LB + j : j * LA + n);
     float s = 0.f;
     for (int i = 0; i < S; ++i) {
       float w;
-      asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w) : "r"(dsmem_map(base + 4u * (uint32_t)(col * R + j), (uint32_t)i)) : "memory");
+      asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w) : "r"(dsmem_map(at, (uint32_t)i)) : "memory");
       s += w;
     }
-    float* o = which ? out + ((size_t)a * width + c0 + col) * p.r + j0 + j : out + ((size_t)a * p.r + j0 + j) * width + c0 + col;
+    float* o = which ? out + ((size_t)a * width + c0 + n) * p.r + j : out + ((size_t)a * p.r + j) * width + c0 + n;
     *o = p.accumulate ? *o + s : s;
   }
   __syncwarp();
@@ -204,13 +230,16 @@ __global__ void __launch_bounds__(GRAD_THREADS) lora_grad_kernel(const GradArgs 
 }
 
 template <int RT>
-cudaError_t launch_grad(const GradArgs& p, int blocks, int n, int chunks, int splits, cudaStream_t stream) {
+cudaError_t launch_grad(const GradArgs& p, int blocks, int n, int splits, cudaStream_t stream) {
   static KernelLimits lim;
-  const size_t smem = (sizeof(GradSmem) + 15) / 16 * 16 + (size_t)4 * 64 * 16 * RT * sizeof(float);
+  constexpr int R = 16 * RT;
+  size_t smem = grad_bytes(R);
+  const size_t red = (size_t)(R * (CB + 8) > CB * (R + 4) ? R * (CB + 8) : CB * (R + 4)) * sizeof(float);
+  if (smem < red) smem = red;
   const cudaError_t e = ensure_kernel_limits((const void*)lora_grad_kernel<RT>, lim, smem, false);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(blocks * splits), (unsigned)n, (unsigned)chunks);
+  cfg.gridDim = dim3((unsigned)(blocks * splits), (unsigned)n);
   cfg.blockDim = dim3(GRAD_THREADS);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
@@ -243,13 +272,13 @@ cudaError_t launch_lora_grad(const LoraArgs& a, int num_sms, cudaStream_t stream
   p.drop = LoraDrop{a.seed, a.site, a.thr};
   const int blocks = p.blocks0 + (p.N + CB - 1) / CB;
   if (blocks == 0) return cudaSuccess;
-  // a split has at least 64 rows: a block of 16 for each row group
-  const int chunks = (a.r + 63) / 64;
+  // a split has at least two batches
   int splits = 1;
-  while (splits < 8 && (long long)blocks * a.n * chunks * splits < 2 * num_sms && a.M >= 128 * splits) splits *= 2;
-  if (a.r <= 16) return launch_grad<1>(p, blocks, a.n, chunks, splits, stream);
-  if (a.r <= 32) return launch_grad<2>(p, blocks, a.n, chunks, splits, stream);
-  return launch_grad<4>(p, blocks, a.n, chunks, splits, stream);
+  while (splits < 8 && (long long)blocks * a.n * splits < num_sms && a.M >= 4 * BR * splits) splits *= 2;
+  if (a.r <= 16) return launch_grad<1>(p, blocks, a.n, splits, stream);
+  if (a.r <= 32) return launch_grad<2>(p, blocks, a.n, splits, stream);
+  if (a.r <= 64) return launch_grad<4>(p, blocks, a.n, splits, stream);
+  return launch_grad<8>(p, blocks, a.n, splits, stream);
 }
 
 }  // namespace cospec

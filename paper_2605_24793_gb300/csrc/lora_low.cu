@@ -4,24 +4,22 @@
 // with a the row's adapter and c_a = scaling[a] / (1 - p); rows without one get zeros.  Both are fp32,
 // and both are bound by reading x or dy once (and, for a few rows, by the latency of one read of the factor).
 //
-// Two kernels.  low_mma_kernel: warps of 16 rows on mma.sync; every operand goes from global memory to the
-// fragments by 16-byte loads, without shared memory, because the order of the contraction inside a
-// product of 32 is free: lane t of a quad takes elements 8t .. 8t + 7 of both operands.  A factor whose rows run
-// along the rank is turned by movmatrix.  Rows of several adapters in one warp: the warp goes over
-// the adapters and zeroes the other rows' elements, so that all of them add into one accumulator.  The contraction
-// is split over the warps of a CTA and the CTAs of a cluster, joined in shared memory in a fixed order.
+// low_tile_kernel: a CTA takes 32 to 128 rows, in chunks of 64 of the contraction that come by cp.async into a ring
+// ahead of the products (mma.sync).  Rows of several adapters: a chunk of x stays while the factors of the
+// tile's adapters pass, and each warp zeroes the other rows' elements of its fragments, so that all of
+// them add into one accumulator.  The contraction is split over the CTAs of a cluster (and, for few rows, the
+// warps of a CTA) and joined in shared memory in a fixed order.
+// Dropout: a thread masks the 16-byte chunks that it copied itself, each one draw of the generator, before the
+// barrier that hands them on.
 // low_row_kernel, for a few rows (rows x rank <= LOW_ROW_MAX): a CTA per row, which reads its adapter's factor
-// in one wave of loads; 16 rows of as many adapters would keep one warp of the other kernel busy for 16
-// round trips to memory.
-//
-// Dropout: a lane's eight elements of a row are one draw of the generator.
+// in one wave of loads; a tile's rows of as many adapters would pass one after another.
 #include "lora.cuh"
 
 namespace cospec {
 
 namespace {
 
-constexpr int LOW_THREADS = 256;
+constexpr int LOW_THREADS = 256;         // 8 warps
 constexpr int LOW_ROW_MAX = 2048;
 constexpr int ROW_THREADS = 512;
 
@@ -39,142 +37,185 @@ struct LowArgs {
   int* err;
 };
 
-// NT: rank in groups of 8, rounded up to 2, 4, 8 or 16.  The rank that column 2 t + e of group nt stands for
-// follows from how the factor is loaded.
-template <int NT, bool RM>
-CS_DEV int low_rank_of(int nt, int col) {
-  const int t = col >> 1, e = col & 1;
-  if (!RM) return nt * 8 + col;
-  if (NT == 2) return 4 * t + 2 * nt + e;
-  return 32 * (nt >> 2) + 8 * t + 2 * (nt & 3) + e;
+constexpr int CK = 64;                   // contraction of a chunk
+constexpr int DEPTH = 4;                 // items in flight: a chunk and an adapter's factor for it
+constexpr int LOW_MAX_ROWS = 128;
+
+struct LowSmem {
+  int ids[LOW_MAX_ROWS];
+  int adapters[LOW_MAX_ROWS];
+  int warp_count[4];
+  int count;
+};
+__host__ __device__ constexpr uint32_t low_bytes(int rows, int R) {
+  return (uint32_t)DEPTH * (uint32_t)(rows * 128 + R * 128) + (uint32_t)sizeof(LowSmem);
 }
 
+// NT: rank in groups of 8 (2, 4, 8 or 16).  RM: the factor's rows run along the rank.
 template <int NT, bool RM>
-__global__ void __launch_bounds__(LOW_THREADS) low_mma_kernel(const LowArgs p) {
-  extern __shared__ float red[];        // [8 warps][16][NT * 8]
+__global__ void __launch_bounds__(LOW_THREADS) low_tile_kernel(const LowArgs p) {
+  extern __shared__ __align__(128) uint8_t sraw[];
   constexpr int R = NT * 8;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2;
   const int S = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
-  const int tile = (int)blockIdx.x / S;
-  const int RW = 1 << p.rw_log2, KW = 8 >> p.rw_log2;
+  const int RW = 1 << p.rw_log2, KW = 8 >> p.rw_log2, rows = 16 * RW;
   const int rw = warp & (RW - 1), kw = warp >> p.rw_log2;
-  const long long m0 = ((long long)tile * RW + rw) * 16;
+  const int m0 = ((int)blockIdx.x / S) * rows;
+  const uint32_t x_off = smem_u32(sraw), f_off = x_off + (uint32_t)(DEPTH * rows * 128);
+  LowSmem& sm = *reinterpret_cast<LowSmem*>(sraw + DEPTH * (rows * 128 + R * 128));
   griddep_wait();
   griddep_launch_dependents();
 
-  const int steps = (p.C + 31) / 32, parts = S * KW, part = rank * KW + kw;
-  const int s0 = (int)((long long)steps * part / parts), s1 = (int)((long long)steps * (part + 1) / parts);
-  int mine = -1;
-  if (lane < 16 && m0 + lane < p.M) mine = lora_adapter(p.adapter, (int)m0 + lane, p.n, p.err);
-  unsigned todo = __ballot_sync(0xffffffffu, mine >= 0);
+  // the adapters of the tile, in the order of their first rows
+  if (threadIdx.x < LOW_MAX_ROWS) {
+    const int m = m0 + (int)threadIdx.x;
+    sm.ids[threadIdx.x] = (int)threadIdx.x < rows && m < p.M ? lora_adapter(p.adapter, m, p.n, p.err) : -1;
+  }
+  __syncthreads();
+  bool first = false;
+  unsigned mask = 0;
+  if (threadIdx.x < LOW_MAX_ROWS) {
+    const int id = sm.ids[threadIdx.x];
+    first = id >= 0;
+    for (int j = 0; j < (int)threadIdx.x && first; ++j) first = sm.ids[j] != id;
+    mask = __ballot_sync(0xffffffffu, first);
+    if (lane == 0) sm.warp_count[warp] = __popc(mask);
+  }
+  __syncthreads();
+  if (threadIdx.x < LOW_MAX_ROWS) {
+    int at = __popc(mask & ((1u << lane) - 1u));
+    for (int w = 0; w < warp; ++w) at += sm.warp_count[w];
+    if (first) sm.adapters[at] = sm.ids[threadIdx.x];
+  }
+  const int count = sm.warp_count[0] + sm.warp_count[1] + sm.warp_count[2] + sm.warp_count[3];
+  __syncthreads();
+
+  const int chunks = (p.C + CK - 1) / CK;
+  const int c0 = (int)((long long)chunks * rank / S), c1 = (int)((long long)chunks * (rank + 1) / S);
+  const int items = (c1 - c0) * count;
   const bool drop = p.drop.thr != 0u;
   LoraKey key{0, 0};
   if (drop) key = lora_key(p.drop);
+
+  // thread's 16-byte chunk i of an x chunk: row (tid + 256 i) / 8, columns 8 (tid mod 8) ..
+  const int xc = (int)threadIdx.x & 7;
+  auto load = [&](int item) {
+    if (item < items) {
+      const int ci = item / count, ai = item - ci * count, k0 = (c0 + ci) * CK;
+      if (ai == 0) {
+        const uint32_t dst = x_off + (uint32_t)((ci % DEPTH) * rows * 128);
+        for (int i = (int)threadIdx.x; i < rows * 8; i += LOW_THREADS) {
+          const int row = i >> 3, k = k0 + 8 * xc;
+          const bool on = m0 + row < p.M && k < p.C;
+          cp_async16(dst + (uint32_t)(row * 128 + ((xc ^ (row & 7)) << 4)), on ? p.x + (long long)(m0 + row) * p.ldx + k : p.x, on);
+        }
+      }
+      const __nv_bfloat16* f = p.f + (size_t)sm.adapters[ai] * p.r * p.C;
+      const uint32_t dst = f_off + (uint32_t)((item % DEPTH) * R * 128);
+      if (!RM) {                           // [rank][64]
+        for (int i = (int)threadIdx.x; i < R * 8; i += LOW_THREADS) {
+          const int row = i >> 3, k = k0 + 8 * xc;
+          const bool on = row < p.r && k < p.C;
+          cp_async16(dst + (uint32_t)(row * 128 + ((xc ^ (row & 7)) << 4)), on ? f + (size_t)row * p.C + k : f, on);
+        }
+      } else {                             // [64][rank]: rows of 2 R bytes; 8 neighbouring rows on different banks
+        for (int i = (int)threadIdx.x; i < 64 * NT; i += LOW_THREADS) {
+          const int row = i / NT, c = i % NT, k = k0 + row;
+          const bool on = k < p.C && 8 * c < p.r;
+          const int sw = NT >= 8 ? row & 7 : NT == 4 ? (row >> 1) & 3 : (row >> 2) & 1;
+          cp_async16(dst + (uint32_t)(row * (R * 2) + ((c ^ sw) << 4)), on ? f + (size_t)k * p.r + 8 * c : f, on);
+        }
+      }
+    }
+    cp_async_commit();
+  };
 
   float acc[NT][4];
 #pragma unroll
   for (int i = 0; i < NT; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+  const int id0 = sm.ids[rw * 16 + g], id1 = sm.ids[rw * 16 + g + 8];
+  const int lr = lane & 15, lc = lane >> 4;         // ldmatrix: the lane's row and 16-byte column of a 16 x 16 block
 
-  while (todo) {
-    const int a = __shfl_sync(0xffffffffu, mine, __ffs(todo) - 1);
-    const unsigned who = __ballot_sync(0xffffffffu, mine == a) & 0xffffu;
-    todo &= ~who;
-    const bool on0 = (who >> g) & 1u, on1 = (who >> (g + 8)) & 1u;
-    const __nv_bfloat16* x0 = p.x + (m0 + g) * p.ldx;
-    const __nv_bfloat16* x1 = p.x + (m0 + g + 8) * p.ldx;
-    const __nv_bfloat16* f = p.f + (size_t)a * p.r * p.C;
-#pragma unroll 2
-    for (int s = s0; s < s1; ++s) {
-      const int k = s * 32 + 8 * t;
-      const bool in = k < p.C;
-      uint4 a0 = make_uint4(0, 0, 0, 0), a1 = a0;
-      if (on0 && in) a0 = ldg16(x0 + k);
-      if (on1 && in) a1 = ldg16(x1 + k);
-      uint32_t b[NT][4];
-      if (!RM) {
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          const int j = i * 8 + g;
-          uint4 v = make_uint4(0, 0, 0, 0);
-          if (j < p.r && in) v = ldg16(f + (size_t)j * p.C + k);
-          b[i][0] = v.x, b[i][1] = v.y, b[i][2] = v.z, b[i][3] = v.w;
-        }
-      } else {
-        // matrix q: its rows 2 t + e are the contraction's elements 8 t + 2 q + e
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int kk = s * 32 + 8 * (g >> 1) + 2 * q + (g & 1);
-          const bool kin = kk < p.C;
-          const __nv_bfloat16* row = f + (size_t)kk * p.r;
-          if constexpr (NT == 2) {
-            uint2 v = make_uint2(0, 0);
-            if (kin && 4 * t < p.r) v = __ldg(reinterpret_cast<const uint2*>(row + 4 * t));
-            b[0][q] = v.x, b[1][q] = v.y;
-          } else {
-#pragma unroll
-            for (int i = 0; i < NT; i += 4) {
-              uint4 v = make_uint4(0, 0, 0, 0);
-              if (kin && 8 * i + 8 * t < p.r) v = ldg16(row + 8 * i + 8 * t);
-              b[i][q] = v.x, b[i + 1][q] = v.y, b[i + 2][q] = v.z, b[i + 3][q] = v.w;
-            }
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < NT; ++i)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) b[i][q] = movmatrix_t(b[i][q]);
+  for (int i = 0; i < DEPTH - 1; ++i) load(i);
+  for (int item = 0; item < items; ++item) {
+    const int ci = item / count, ai = item - ci * count, k0 = (c0 + ci) * CK;
+    cp_async_wait<DEPTH - 2>();
+    const uint32_t xb = x_off + (uint32_t)((ci % DEPTH) * rows * 128), fb = f_off + (uint32_t)((item % DEPTH) * R * 128);
+    if (drop && ai == 0) {
+      for (int i = (int)threadIdx.x; i < rows * 8; i += LOW_THREADS) {
+        const int row = i >> 3;
+        uint4* q = reinterpret_cast<uint4*>(sraw + (xb - x_off) + row * 128 + ((xc ^ (row & 7)) << 4));
+        *q = and4(*q, lora_keep8((uint32_t)((k0 >> 3) + xc), (uint32_t)(m0 + row), p.drop, key));
       }
-      if (drop) {
-        a0 = and4(a0, lora_keep8((uint32_t)(k >> 3), (uint32_t)(m0 + g), p.drop, key));
-        a1 = and4(a1, lora_keep8((uint32_t)(k >> 3), (uint32_t)(m0 + g + 8), p.drop, key));
-      }
-      const uint32_t q0[4] = {a0.x, a1.x, a0.y, a1.y}, q1[4] = {a0.z, a1.z, a0.w, a1.w};
+    }
+    __syncthreads();
+    load(item + DEPTH - 1);
+    const int a = sm.adapters[ai];
+    const bool on0 = id0 == a, on1 = id1 == a;
+    if (!__any_sync(0xffffffffu, on0 || on1)) continue;
+    for (int ks = kw; ks < CK / 16; ks += KW) {
+      uint32_t q[4];
+      const int row = rw * 16 + lr;
+      ldsm_x4(xb + (uint32_t)(row * 128 + (((2 * ks + lc) ^ (row & 7)) << 4)), q[0], q[1], q[2], q[3]);
+      q[0] = on0 ? q[0] : 0u, q[2] = on0 ? q[2] : 0u;
+      q[1] = on1 ? q[1] : 0u, q[3] = on1 ? q[3] : 0u;
 #pragma unroll
-      for (int i = 0; i < NT; ++i) {
-        mma_16816(acc[i], q0, b[i][0], b[i][1]);
-        mma_16816(acc[i], q1, b[i][2], b[i][3]);
+      for (int i = 0; i < NT; i += 2) {
+        uint32_t b[4];
+        if (!RM) {                         // (ranks 8 i .. + 7, k 0-7), (same, k 8-15), (the next 8 ranks, ..)
+          const int fr = i * 8 + (lane & 7) + ((lane >> 4) << 3), fc = 2 * ks + ((lane >> 3) & 1);
+          ldsm_x4(fb + (uint32_t)(fr * 128 + ((fc ^ (fr & 7)) << 4)), b[0], b[1], b[2], b[3]);
+        } else {
+          const int fr = ks * 16 + lr, fc = i + lc;
+          const int sw = NT >= 8 ? fr & 7 : NT == 4 ? (fr >> 1) & 3 : (fr >> 2) & 1;
+          ldsm_x4_t(fb + (uint32_t)(fr * (R * 2) + ((fc ^ sw) << 4)), b[0], b[1], b[2], b[3]);
+        }
+        mma_16816(acc[i], q, b[0], b[1]);
+        mma_16816(acc[i + 1], q, b[2], b[3]);
       }
     }
   }
+  cp_async_wait<0>();
+  __syncthreads();
 
-  float* mine_red = red + (size_t)warp * 16 * R;
+  // [warps][16][R + 4]: neighbouring rows on different banks
+  constexpr int RP = R + 4;
+  float* red = reinterpret_cast<float*>(sraw);
+  float* mine = red + (size_t)warp * 16 * RP;
+  const int t = lane & 3;
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
-    mine_red[g * R + low_rank_of<NT, RM>(i, 2 * t)] = acc[i][0];
-    mine_red[g * R + low_rank_of<NT, RM>(i, 2 * t + 1)] = acc[i][1];
-    mine_red[(g + 8) * R + low_rank_of<NT, RM>(i, 2 * t)] = acc[i][2];
-    mine_red[(g + 8) * R + low_rank_of<NT, RM>(i, 2 * t + 1)] = acc[i][3];
+    *reinterpret_cast<float2*>(&mine[g * RP + i * 8 + 2 * t]) = make_float2(acc[i][0], acc[i][1]);
+    *reinterpret_cast<float2*>(&mine[(g + 8) * RP + i * 8 + 2 * t]) = make_float2(acc[i][2], acc[i][3]);
   }
   __syncthreads();
-  const int total = RW * 16 * R;
-  for (int e = threadIdx.x; e < total; e += LOW_THREADS) {
-    float v = red[e];
-    for (int i = 1; i < KW; ++i) v += red[i * total + e];
-    red[e] = v;
-  }
-  __syncwarp();                          // (the cluster's barriers are a warp's together)
-  cluster_arrive();
+  __syncwarp();
+  cluster_arrive();                        // (the cluster's barriers are a warp's together)
   cluster_wait();
-  const int e0 = (int)((long long)total * rank / S), e1 = (int)((long long)total * (rank + 1) / S);
+  const int total = rows * R, e0 = (int)((long long)total * rank / S), e1 = (int)((long long)total * (rank + 1) / S);
   const uint32_t base = smem_u32(red);
-  for (int e = e0 + threadIdx.x; e < e1; e += LOW_THREADS) {
-    const int j = e % R;
-    const long long m = (long long)tile * RW * 16 + e / R;
+  for (int e = e0 + (int)threadIdx.x; e < e1; e += LOW_THREADS) {
+    const int j = e % R, row = e / R;
+    const long long m = (long long)m0 + row;
     if (j >= p.r || m >= p.M) continue;
     float v = 0.f;
-    for (int i = 0; i < S; ++i) {
-      float w;
-      asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w) : "r"(dsmem_map(base + 4u * e, (uint32_t)i)) : "memory");
-      v += w;
-    }
+    for (int i = 0; i < S; ++i)
+      for (int w = 0; w < KW; ++w) {
+        float x;
+        asm volatile("ld.shared::cluster.f32 %0, [%1];"
+                     : "=f"(x)
+                     : "r"(dsmem_map(base + 4u * (uint32_t)((w * rows + row) * RP + j), (uint32_t)i))
+                     : "memory");
+        v += x;
+      }
     const int a = p.adapter[m];
-    const float c = a >= 0 && a < p.n ? p.scaling[a] * p.keep_inv : 0.f;
-    p.u[(size_t)m * p.r + j] = a >= 0 && a < p.n ? v * c : 0.f;
+    p.u[(size_t)m * p.r + j] = a >= 0 && a < p.n ? v * (p.scaling[a] * p.keep_inv) : 0.f;
   }
   __syncwarp();
-  cluster_arrive();                      // nobody leaves while its sums are read
+  cluster_arrive();                        // nobody leaves while its sums are read
   cluster_wait();
 }
 
@@ -265,10 +306,13 @@ __global__ void __launch_bounds__(ROW_THREADS) low_row_kernel(const LowArgs p) {
 }
 
 template <int NT, bool RM>
-cudaError_t launch_low_mma(const LowArgs& p, int tiles, int splits, cudaStream_t stream) {
+cudaError_t launch_low_tile(const LowArgs& p, int tiles, int splits, cudaStream_t stream) {
   static KernelLimits lim;
-  const size_t smem = (size_t)8 * 16 * NT * 8 * sizeof(float);
-  const cudaError_t e = ensure_kernel_limits((const void*)low_mma_kernel<NT, RM>, lim, smem, false);
+  const int rows = 16 << p.rw_log2;
+  size_t smem = low_bytes(rows, NT * 8);
+  const size_t red = (size_t)8 * 16 * (NT * 8 + 4) * sizeof(float);
+  if (smem < red) smem = red;
+  const cudaError_t e = ensure_kernel_limits((const void*)low_tile_kernel<NT, RM>, lim, smem, false);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * splits));
@@ -284,25 +328,25 @@ cudaError_t launch_low_mma(const LowArgs& p, int tiles, int splits, cudaStream_t
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, low_mma_kernel<NT, RM>, p);
+  return cudaLaunchKernelEx(&cfg, low_tile_kernel<NT, RM>, p);
 }
 
 template <bool RM>
 cudaError_t launch_low(LowArgs p, int num_sms, cudaStream_t stream) {
   if ((long long)p.M * p.r <= LOW_ROW_MAX)
     return launch_pdl(low_row_kernel<RM>, dim3((unsigned)p.M), dim3(ROW_THREADS), 0, stream, p);
-  // Four row groups a CTA share the factor's lines in L1; fewer where that leaves SMs without work.
-  p.rw_log2 = 2;
-  while (p.rw_log2 > 0 && (p.M + (16 << p.rw_log2) - 1) / (16 << p.rw_log2) * 8 < num_sms) --p.rw_log2;
+  // 128 rows a CTA share an adapter's factor; fewer where that leaves SMs without work
+  const int chunks = (p.C + CK - 1) / CK;
+  p.rw_log2 = 3;
+  while (p.rw_log2 > 1 && (p.M + (16 << p.rw_log2) - 1) / (16 << p.rw_log2) * 8 < num_sms) --p.rw_log2;
   const int tiles = (p.M + (16 << p.rw_log2) - 1) / (16 << p.rw_log2);
-  const int steps = (p.C + 31) / 32, kw = 8 >> p.rw_log2;
   int splits = 1;
-  while (splits < 8 && tiles * splits < 2 * num_sms && steps >= 4 * splits * kw) splits *= 2;
+  while (splits < 8 && tiles * splits < 2 * num_sms && chunks >= 4 * splits) splits *= 2;
   const int nt = (p.r + 7) / 8;
-  if (nt <= 2) return launch_low_mma<2, RM>(p, tiles, splits, stream);
-  if (nt <= 4) return launch_low_mma<4, RM>(p, tiles, splits, stream);
-  if (nt <= 8) return launch_low_mma<8, RM>(p, tiles, splits, stream);
-  return launch_low_mma<16, RM>(p, tiles, splits, stream);
+  if (nt <= 2) return launch_low_tile<2, RM>(p, tiles, splits, stream);
+  if (nt <= 4) return launch_low_tile<4, RM>(p, tiles, splits, stream);
+  if (nt <= 8) return launch_low_tile<8, RM>(p, tiles, splits, stream);
+  return launch_low_tile<16, RM>(p, tiles, splits, stream);
 }
 
 }  // namespace
