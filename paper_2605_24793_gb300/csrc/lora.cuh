@@ -16,8 +16,7 @@ CS_DEV int lora_adapter(const int32_t* adapter, int m, int n, int* err) {
   return a;
 }
 
-// Dropout of eight neighbouring columns of a row: masks of two bf16 each, all ones where the element
-// stays.  Columns 8 c .. 8 c + 7 of row m take the eight 16-bit halves, low before high, of Philox4x32-10
+// Dropout of eight neighbouring columns of a row.  Columns 8 c .. 8 c + 7 of row m take the eight 16-bit halves, low before high, of Philox4x32-10
 // at counter (c, m, site, 2); an element stays where its half is at least the threshold.  The mask is a
 // function of the element's place, so the passes that need it draw it again instead of storing it.
 struct LoraDrop {
@@ -31,29 +30,37 @@ CS_DEV LoraKey lora_key(const LoraDrop& d) {
   const unsigned long long s = *d.seed;
   return LoraKey{(uint32_t)s, (uint32_t)(s >> 32)};
 }
-CS_DEV uint4 lora_keep8(uint32_t c, uint32_t m, const LoraDrop& d, LoraKey key) {
-  const uint4 r = philox4x32_10(make_uint4(c, m, d.site, 2u), key.lo, key.hi);
-  auto two = [&](uint32_t w) {
-    return ((w & 0xffffu) >= d.thr ? 0xffffu : 0u) | ((w >> 16) >= d.thr ? 0xffff0000u : 0u);
-  };
-  return make_uint4(two(r.x), two(r.y), two(r.z), two(r.w));
+// (the draw is half of the passes' instructions at rank 16: products of 64 bits in one instruction each)
+CS_DEV uint4 lora_draw(uint32_t c, uint32_t m, const LoraDrop& d, LoraKey key) {
+  uint4 v = make_uint4(c, m, d.site, 2u);
+#pragma unroll
+  for (int r = 0; r < 10; ++r) {
+    const uint64_t a = (uint64_t)0xD2511F53u * v.x, b = (uint64_t)0xCD9E8D57u * v.z;
+    v = make_uint4((uint32_t)(b >> 32) ^ v.y ^ (key.lo + (uint32_t)r * 0x9E3779B9u), (uint32_t)b,
+                   (uint32_t)(a >> 32) ^ v.w ^ (key.hi + (uint32_t)r * 0xBB67AE85u), (uint32_t)a);
+  }
+  return v;
 }
-// The same as eight bits, column 8 c in the lowest.
+// x with its dropped elements zero.
+CS_DEV uint4 lora_dropped8(uint4 x, uint32_t c, uint32_t m, const LoraDrop& d, LoraKey key) {
+  const uint4 r = lora_draw(c, m, d, key);
+  const uint32_t t = d.thr << 16;
+  auto two = [&](uint32_t v, uint32_t w) {
+    if ((w << 16) < t) v &= 0xffff0000u;
+    if (w < t) v &= 0x0000ffffu;
+    return v;
+  };
+  return make_uint4(two(x.x, r.x), two(x.y, r.y), two(x.z, r.z), two(x.w, r.w));
+}
+// The mask of the eight as bits, column 8 c in the lowest.
 CS_DEV uint32_t lora_keep8_bits(uint32_t c, uint32_t m, const LoraDrop& d, LoraKey key) {
-  const uint4 r = philox4x32_10(make_uint4(c, m, d.site, 2u), key.lo, key.hi);
-  auto two = [&](uint32_t w) { return ((w & 0xffffu) >= d.thr ? 1u : 0u) | ((w >> 16) >= d.thr ? 2u : 0u); };
+  const uint4 r = lora_draw(c, m, d, key);
+  const uint32_t t = d.thr << 16;
+  auto two = [&](uint32_t w) { return ((w << 16) >= t ? 1u : 0u) | (w >= t ? 2u : 0u); };
   return two(r.x) | two(r.y) << 2 | two(r.z) << 4 | two(r.w) << 6;
 }
 
-CS_DEV uint4 and4(uint4 a, uint4 b) { return make_uint4(a.x & b.x, a.y & b.y, a.z & b.z, a.w & b.w); }
 CS_DEV uint4 ldg16(const void* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
-
-// Transposes an 8 x 8 matrix of 16-bit values held as the mma fragments are.
-CS_DEV uint32_t movmatrix_t(uint32_t x) {
-  uint32_t y;
-  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-  return y;
-}
 
 // x as hi + lo, each rounded to bf16: 16 bits of its mantissa.  What is not finite stays in hi.
 CS_DEV void lora_split2(float x, float& hi, float& lo) {

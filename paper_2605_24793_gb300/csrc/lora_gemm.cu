@@ -226,16 +226,21 @@ __global__ void __launch_bounds__(256, 1)
       // W is read again by the other row tiles, if there are any
       const uint64_t pol = !is_w ? l2_policy_evict_last() : gridDim.y > 1 ? l2_policy_evict_normal() : l2_policy_evict_first();
       const uint32_t a_buf = smem_u32(smem), b_buf = smem_u32(smem + L.b_off);
-      int issued = 0;
-      auto turn = [&](int li) {            // the stage of load li is free
-        return li < p.stages || (mbar_wait(&empty[li % p.stages], (uint32_t)(li / p.stages - 1) & 1u, WAIT_NS) && !*abort_flag);
+      int li = 0, st = 0;
+      uint32_t ph = 0;
+      auto turn = [&]() {                  // the next stage, free (turns are counted: a division costs a hundred cycles)
+        if (li >= p.stages && (!mbar_wait(&empty[st], ph ^ 1u, WAIT_NS) || *abort_flag)) return -1;
+        const int s = st;
+        ++li;
+        if (++st == p.stages) st = 0, ph ^= 1u;
+        return s;
       };
       for (int i = 0; i < nk; ++i) {
-        if (!turn(i)) {
+        const int s = turn(), x = (kb0 + i) * BK;
+        if (s < 0) {
           ok = false;
           break;
         }
-        const int s = i % p.stages, x = (kb0 + i) * BK;
         mbar_arrive_expect_tx(&full[s], is_w ? (uint32_t)A_BYTES : b_bytes);
         if (!is_w) {
           tma_load_3d(b_buf + (uint32_t)s * b_bytes, &tmap_x, &full[s], x, row0, 0, pol);
@@ -245,14 +250,13 @@ __global__ void __launch_bounds__(256, 1)
           tma_load_3d(a_buf + (uint32_t)s * A_BYTES, &tmap_w, &full[s], f0, x, 0, pol);
           tma_load_3d(a_buf + (uint32_t)s * A_BYTES + A_BYTES / 2, &tmap_w, &full[s], f0 + 64, x, 0, pol);
         }
-        issued = i + 1;
       }
       if (ok) ok = mbar_wait_idle(lready, 0, WAIT_NS) && !*abort_flag;
       if (ok) {
         const int units = list.count * upe, n = my_steps();
         for (int i = 0; i < n; ++i) {
-          const int li = nk + i, s = li % p.stages;
-          if (!turn(li)) {
+          const int s = turn();
+          if (s < 0) {
             ok = false;
             break;
           }
@@ -275,15 +279,13 @@ __global__ void __launch_bounds__(256, 1)
               }
             }
           }
-          issued = li + 1;
         }
       }
       if (!ok) {
         set_err(p.err, ERR_TIMEOUT);
         *abort_flag = 1;
         // what was issued lands before the shared memory is given back
-        for (int li = issued > p.stages ? issued - p.stages : 0; li < issued; ++li)
-          mbar_wait(&full[li % p.stages], (uint32_t)(li / p.stages) & 1u, WAIT_NS);
+        for (int l = li > p.stages ? li - p.stages : 0; l < li; ++l) mbar_wait(&full[l % p.stages], (uint32_t)(l / p.stages) & 1u, WAIT_NS);
       }
     }
   } else if (warp == 1) {
@@ -293,10 +295,13 @@ __global__ void __launch_bounds__(256, 1)
     const uint64_t a_desc = MN ? tq_desc_mn_sw128(smem_u32(smem), A_BYTES / 2) : smem_desc_sw128(smem_u32(smem));
     const uint64_t f_desc = MN ? tq_desc_mn_sw128(smem_u32(smem), UNIT_BYTES / 2) : desc_k_sw32(smem_u32(smem));
     const uint64_t b_desc = smem_desc_sw128(smem_u32(smem + L.b_off));
+    int st = 0;
+    uint32_t ph = 0, uphase = 0;           // uphase, bit s: parity of stage s's next u operand
     for (int i = 0; i < nk && ok; ++i) {
-      const int s = i % p.stages;
-      ok = __all_sync(0xffffffffu, mbar_wait(&full[s], (uint32_t)(i / p.stages) & 1u, WAIT_NS)) && !*abort_flag;
+      const int s = st;
+      ok = __all_sync(0xffffffffu, mbar_wait(&full[s], ph, WAIT_NS)) && !*abort_flag;
       if (!ok) break;
+      if (++st == p.stages) st = 0, ph ^= 1u;
       tc_fence_after();
       const uint64_t a = a_desc + (uint64_t)(s * (A_BYTES >> 4)), b = b_desc + (uint64_t)((uint32_t)s * (b_bytes >> 4));
 #pragma unroll
@@ -309,10 +314,11 @@ __global__ void __launch_bounds__(256, 1)
       const int units = list.count * upe, n = my_steps();
       const uint32_t d2 = DROP ? tmem + (uint32_t)p.nt : tmem;
       for (int i = 0; i < n; ++i) {
-        const int li = nk + i, s = li % p.stages;
-        ok = __all_sync(0xffffffffu, mbar_wait(&full[s], (uint32_t)(li / p.stages) & 1u, WAIT_NS) &&
-                                         mbar_wait(&ufull[s], (uint32_t)(i / p.stages) & 1u, WAIT_NS)) && !*abort_flag;
+        const int s = st;
+        ok = __all_sync(0xffffffffu, mbar_wait(&full[s], ph, WAIT_NS) && mbar_wait(&ufull[s], (uphase >> s) & 1u, WAIT_NS)) && !*abort_flag;
         if (!ok) break;
+        uphase ^= 1u << s;
+        if (++st == p.stages) st = 0, ph ^= 1u;
         tc_fence_after();
         const int u0 = (rank + i * S) * STEP_UNITS, nu = min(STEP_UNITS, units - u0);
         for (int q = 0; q < nu; ++q) {
@@ -343,10 +349,14 @@ __global__ void __launch_bounds__(256, 1)
     const int units = list.count * upe, n = my_steps();
     griddep_wait();                        // u
     griddep_launch_dependents();
+    int st = nk % p.stages;
+    uint32_t gphase = 0;
     for (int i = 0; i < n; ++i) {
-      const int li = nk + i, s = li % p.stages;
-      ok = __all_sync(0xffffffffu, mbar_wait_idle(&ugo[s], (uint32_t)(i / p.stages) & 1u, WAIT_NS)) && !*abort_flag;
+      const int s = st;
+      ok = __all_sync(0xffffffffu, mbar_wait(&ugo[s], (gphase >> s) & 1u, WAIT_NS)) && !*abort_flag;
       if (!ok) break;
+      gphase ^= 1u << s;
+      if (++st == p.stages) st = 0;
       uint8_t* tile = smem + L.b_off + (uint32_t)s * b_bytes;
       const int u0 = (rank + i * S) * STEP_UNITS, nu = min(STEP_UNITS, units - u0);
       for (int q = 0; q < nu; ++q) {
@@ -579,16 +589,23 @@ __global__ void __launch_bounds__(P_THREADS, 1)
       const uint64_t pol = l2_policy_evict_normal();
       const uint32_t a_buf = smem_u32(smem), b_buf = smem_u32(smem + L.b_off);
       const uint32_t full0 = dsmem_map(smem_u32(full), 0);
-      int li = 0;
-      auto turn = [&](int s) {
-        return li < p.stages || (mbar_wait(&empty[s], (uint32_t)(li / p.stages - 1) & 1u, WAIT_NS) && !*abort_flag);
+      int li = 0, st = 0;
+      uint32_t ph = 0;
+      // the next stage, free: the turns are counted (a division per turn, twice in the chain from one stage to the next, cost
+      // 82 -> 107 us at 4096 rows 2560 -> 6144)
+      auto turn = [&]() {
+        if (li >= p.stages && (!mbar_wait(&empty[st], ph ^ 1u, WAIT_NS) || *abort_flag)) return -1;
+        const int s = st;
+        ++li;
+        if (++st == p.stages) st = 0, ph ^= 1u;
+        return s;
       };
       int it = 0;
       for (int tile = pair; tile < tiles && ok; tile += pairs, ++it) {
         const int f0 = (tile % ftiles) * PBM + rank * BM, row0 = (tile / ftiles) * p.nt + rank * half;
-        for (int kb = 0; kb < kblocks; ++kb, ++li) {
-          const int s = li % p.stages, x = kb * BK;
-          if (!turn(s)) {
+        for (int kb = 0; kb < kblocks; ++kb) {
+          const int s = turn(), x = kb * BK;
+          if (s < 0) {
             ok = false;
             break;
           }
@@ -603,13 +620,13 @@ __global__ void __launch_bounds__(P_THREADS, 1)
             tma_load_3d_pair(a_buf + (uint32_t)s * A_BYTES + A_BYTES / 2, &tmap_w, bar, f0 + 64, x, 0, pol);
           }
         }
-        if (ok) ok = mbar_wait_idle(&lready[it & 1], (uint32_t)(it >> 1) & 1u, WAIT_NS) && !*abort_flag;
+        if (ok) ok = mbar_wait(&lready[it & 1], (uint32_t)(it >> 1) & 1u, WAIT_NS) && !*abort_flag;
         if (!ok) break;
         const TileList& list = list_of(it);
         const int units = list.count * upe, steps = (units + STEP_UNITS - 1) / STEP_UNITS;
-        for (int i = 0; i < steps; ++i, ++li) {
-          const int s = li % p.stages;
-          if (!turn(s)) {
+        for (int i = 0; i < steps; ++i) {
+          const int s = turn();
+          if (s < 0) {
             ok = false;
             break;
           }
@@ -651,33 +668,34 @@ __global__ void __launch_bounds__(P_THREADS, 1)
       const uint64_t a_desc = MN ? tq_desc_mn_sw128(smem_u32(smem), A_BYTES / 2) : smem_desc_sw128(smem_u32(smem));
       const uint64_t f_desc = MN ? tq_desc_mn_sw128(smem_u32(smem), UNIT_BYTES / 2) : desc_k_sw32(smem_u32(smem));
       const uint64_t b_desc = smem_desc_sw128(smem_u32(smem + L.b_off));
-      int li = 0, it = 0;
-      uint32_t uphase = 0;                 // bit s: parity of stage s's next u operand
+      int st = 0, it = 0;
+      uint32_t ph = 0, uphase = 0;                 // bit s: parity of stage s's next u operand
       for (int tile = pair; tile < tiles && ok; tile += pairs, ++it) {
         const int acc = it % NACC;
         ok = __all_sync(0xffffffffu, mbar_wait(&tempty[acc], ((uint32_t)(it / NACC) & 1u) ^ 1u, WAIT_NS)) && !*abort_flag;
         if (!ok) break;
         tc_fence_after();
         const uint32_t d = tmem + (uint32_t)(acc * p.nt), d2 = DROP ? d + (uint32_t)p.nt : d;
-        for (int kb = 0; kb < kblocks; ++kb, ++li) {
-          const int s = li % p.stages;
-          ok = __all_sync(0xffffffffu, mbar_wait(&full[s], (uint32_t)(li / p.stages) & 1u, WAIT_NS));
+        for (int kb = 0; kb < kblocks; ++kb) {
+          const int s = st;
+          ok = __all_sync(0xffffffffu, mbar_wait(&full[s], ph, WAIT_NS));
           if (!ok) break;
+          if (++st == p.stages) st = 0, ph ^= 1u;
           tc_fence_after();
           pair_k64<MN ? 128 : 2>(on, d, a_desc + (uint64_t)(s * (A_BYTES >> 4)), b_desc + (uint64_t)((uint32_t)s * (b_bytes >> 4)), idesc,
                                  kb != 0 ? 1u : 0u);
           umma_commit_pair_on(on, &empty[s], 3);
         }
-        if (ok) ok = __all_sync(0xffffffffu, mbar_wait_idle(&lready[it & 1], (uint32_t)(it >> 1) & 1u, WAIT_NS)) && !*abort_flag;
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&lready[it & 1], (uint32_t)(it >> 1) & 1u, WAIT_NS)) && !*abort_flag;
         if (!ok) break;
         const int units = list_of(it).count * upe, steps = (units + STEP_UNITS - 1) / STEP_UNITS;
         __syncwarp();
         if (lane == 0) mbar_arrive(&lfree[it & 1]);
-        for (int i = 0; i < steps; ++i, ++li) {
-          const int s = li % p.stages;
-          ok = __all_sync(0xffffffffu, mbar_wait(&full[s], (uint32_t)(li / p.stages) & 1u, WAIT_NS) && mbar_wait_pair(&ufull[s], (uphase >> s) & 1u)) &&
-               !*abort_flag;
+        for (int i = 0; i < steps; ++i) {
+          const int s = st;
+          ok = __all_sync(0xffffffffu, mbar_wait(&full[s], ph, WAIT_NS) && mbar_wait_pair(&ufull[s], (uphase >> s) & 1u)) && !*abort_flag;
           if (!ok) break;
+          if (++st == p.stages) st = 0, ph ^= 1u;
           uphase ^= 1u << s;
           tc_fence_after();
           const int nu = min(STEP_UNITS, units - i * STEP_UNITS);
@@ -701,14 +719,14 @@ __global__ void __launch_bounds__(P_THREADS, 1)
   } else if (warp >= P_UW) {
     const int t = tid - P_UW * 32;
     const uint32_t ufull0 = dsmem_map(smem_u32(ufull), 0);
-    int li = 0, it = 0;
+    int st = 0, it = 0;
     uint32_t gphase = 0;
     griddep_wait();                        // u
     griddep_launch_dependents();
     for (int tile = pair; tile < tiles; tile += pairs, ++it) {
       const int row0 = (tile / ftiles) * p.nt;
       TileList& list = list_of(it);
-      if (it >= 2) ok = mbar_wait_idle(&lfree[it & 1], (uint32_t)((it >> 1) - 1) & 1u, 2 * WAIT_NS) && !*abort_flag;
+      if (it >= 2) ok = mbar_wait_idle(&lfree[it & 1], (uint32_t)((it >> 1) - 1) & 1u, 2 * WAIT_NS, 500u) && !*abort_flag;
       if (!ok) *abort_flag = 1;
       named_bar_sync(1, 128);
       if (t == 0) list.count = *abort_flag ? -1 : 0;        // one thread's reading decides for all four warps
@@ -719,10 +737,11 @@ __global__ void __launch_bounds__(P_THREADS, 1)
       if (lane == 0) mbar_arrive(&lready[it & 1]);
       named_bar_sync(1, 128);
       const int units = list.count * upe, steps = (units + STEP_UNITS - 1) / STEP_UNITS;
-      li += kblocks;
-      for (int i = 0; i < steps; ++i, ++li) {
-        const int s = li % p.stages;
-        ok = __all_sync(0xffffffffu, mbar_wait_idle(&ugo[s], (gphase >> s) & 1u, WAIT_NS)) && !*abort_flag;
+      st = (st + kblocks) % p.stages;
+      for (int i = 0; i < steps; ++i) {
+        const int s = st;
+        if (++st == p.stages) st = 0;
+        ok = __all_sync(0xffffffffu, mbar_wait_idle(&ugo[s], (gphase >> s) & 1u, WAIT_NS, 500u)) && !*abort_flag;
         if (!ok) break;
         gphase ^= 1u << s;
         const int nu = min(STEP_UNITS, units - i * STEP_UNITS);
@@ -757,12 +776,12 @@ __global__ void __launch_bounds__(P_THREADS, 1)
 #pragma unroll
         for (int c = 0; c < P_CHUNKS; ++c)
           if (hw + 2 * c < chunks) keep[c] = keep_bits32(f, row0 + (hw + 2 * c) * 32, p.drop, key);
-        ok = __all_sync(0xffffffffu, mbar_wait_idle(&lready[it & 1], (uint32_t)(it >> 1) & 1u, 2 * WAIT_NS));
+        ok = __all_sync(0xffffffffu, mbar_wait(&lready[it & 1], (uint32_t)(it >> 1) & 1u, 2 * WAIT_NS));
         has = ok && list_of(it).count > 0;
         __syncwarp();
         if (lane == 0) mbar_arrive(&lfree[it & 1]);
       }
-      ok = ok && __all_sync(0xffffffffu, mbar_wait_idle(&tfull[acc], (uint32_t)(it / NACC) & 1u, 2 * WAIT_NS));
+      ok = ok && __all_sync(0xffffffffu, mbar_wait(&tfull[acc], (uint32_t)(it / NACC) & 1u, 2 * WAIT_NS));
       if (!ok) {
         if (lane == 0) {
           set_err(p.err, ERR_TIMEOUT);

@@ -8,7 +8,7 @@
 // summed over micro-batches starts from fp32).
 //
 // A CTA takes 256 columns of one adapter, 32 a warp; the adapter's rows, listed in shared memory first, so that rows
-// of other adapters and what they hold are not read, come 64 at a time: Q by cp.async into a ring, P through
+// of other adapters and what they hold are not read, come 32 at a time: Q by cp.async into a ring, P through
 // registers, where it is split once for all warps.  A thread masks the 16-byte chunks of x that it copied itself, each one
 // draw of the generator.  The rows are split over the CTAs of a cluster and joined in a fixed order.
 #include "lora.cuh"
@@ -19,8 +19,8 @@ namespace {
 
 constexpr int GRAD_THREADS = 256;
 constexpr int CB = 256;              // columns of a CTA
-constexpr int BR = 64;               // rows of a batch
-constexpr int GDEPTH = 3;            // batches in the ring
+constexpr int BR = 32;               // rows of a batch
+constexpr int GDEPTH = 4;            // batches in the ring
 constexpr int WIN = 2048;            // rows listed at a time
 constexpr uint32_t Q_BYTES = BR * CB * 2;
 
@@ -41,7 +41,7 @@ struct GradSmem {
   int list[WIN];
   int warp_count[8];
 };
-// the ring of Q, two buffers of P's parts [3][64 rows][R], the list; then the sums, [R][CB + 8] or [CB][R + 4]
+// the ring of Q, two buffers of P's parts [3][BR rows][R], the list; then the sums, [R][CB + 8] or [CB][R + 4]
 __host__ __device__ constexpr uint32_t grad_p_bytes(int R) { return (uint32_t)(3 * BR * R * 2); }
 __host__ __device__ constexpr uint32_t grad_bytes(int R) {
   return GDEPTH * Q_BYTES + 2 * grad_p_bytes(R) + (uint32_t)sizeof(GradSmem);
@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(GRAD_THREADS) lora_grad_kernel(const GradArgs 
     const int qc = tid & 31, col = c0 + 8 * qc;
     auto load_q = [&](int b) {
       if (b < batches) {
-        const uint32_t dst = q0 + (uint32_t)(b % GDEPTH) * Q_BYTES;
+        const uint32_t dst = q0 + (uint32_t)(b & (GDEPTH - 1)) * Q_BYTES;
 #pragma unroll
         for (int i = 0; i < BR / 8; ++i) {
           const int row = (tid >> 5) + 8 * i;
@@ -153,14 +153,14 @@ __global__ void __launch_bounds__(GRAD_THREADS) lora_grad_kernel(const GradArgs 
     for (int b = 0; b < batches; ++b) {
       store_p(b);
       cp_async_wait<GDEPTH - 2>();
-      const uint32_t qb = q0 + (uint32_t)(b % GDEPTH) * Q_BYTES;
+      const uint32_t qb = q0 + (uint32_t)(b & (GDEPTH - 1)) * Q_BYTES;
       if (drop) {
 #pragma unroll 2
         for (int i = 0; i < BR / 8; ++i) {
           const int row = (tid >> 5) + 8 * i;
           if (b * BR + row >= have) break;
           uint4* q = reinterpret_cast<uint4*>(raw + (qb - q0) + row * 512 + ((qc ^ (row & 7)) << 4));
-          *q = and4(*q, lora_keep8((uint32_t)(col >> 3), (uint32_t)sm.list[b * BR + row], p.drop, key));
+          *q = lora_dropped8(*q, (uint32_t)(col >> 3), (uint32_t)sm.list[b * BR + row], p.drop, key);
         }
       }
       __syncthreads();
@@ -272,9 +272,9 @@ cudaError_t launch_lora_grad(const LoraArgs& a, int num_sms, cudaStream_t stream
   p.drop = LoraDrop{a.seed, a.site, a.thr};
   const int blocks = p.blocks0 + (p.N + CB - 1) / CB;
   if (blocks == 0) return cudaSuccess;
-  // a split has at least two batches
+  // a split has at least four batches
   int splits = 1;
-  while (splits < 8 && (long long)blocks * a.n * splits < num_sms && a.M >= 4 * BR * splits) splits *= 2;
+  while (splits < 8 && (long long)blocks * a.n * splits < num_sms && a.M >= 8 * BR * splits) splits *= 2;
   if (a.r <= 16) return launch_grad<1>(p, blocks, a.n, splits, stream);
   if (a.r <= 32) return launch_grad<2>(p, blocks, a.n, splits, stream);
   if (a.r <= 64) return launch_grad<4>(p, blocks, a.n, splits, stream);

@@ -97,26 +97,35 @@ __global__ void __launch_bounds__(LOW_THREADS) low_tile_kernel(const LowArgs p) 
   LoraKey key{0, 0};
   if (drop) key = lora_key(p.drop);
 
-  // thread's 16-byte chunk i of an x chunk: row (tid + 256 i) / 8, columns 8 (tid mod 8) ..
-  const int xc = (int)threadIdx.x & 7;
-  auto load = [&](int item) {
-    if (item < items) {
-      const int ci = item / count, ai = item - ci * count, k0 = (c0 + ci) * CK;
-      if (ai == 0) {
-        const uint32_t dst = x_off + (uint32_t)((ci % DEPTH) * rows * 128);
-        for (int i = (int)threadIdx.x; i < rows * 8; i += LOW_THREADS) {
-          const int row = i >> 3, k = k0 + 8 * xc;
-          const bool on = m0 + row < p.M && k < p.C;
-          cp_async16(dst + (uint32_t)(row * 128 + ((xc ^ (row & 7)) << 4)), on ? p.x + (long long)(m0 + row) * p.ldx + k : p.x, on);
+  // The thread's 16-byte chunk i of an x chunk: row tid / 8 + 32 i, columns 8 (tid mod 8) ..; its swizzled place in the
+  // 128-byte rows is the same for all i.  Items are walked with counters, without divisions.
+  const int xc = (int)threadIdx.x & 7, xr = (int)threadIdx.x >> 3;
+  const uint32_t xs = (uint32_t)(xr * 128 + ((xc ^ (xr & 7)) << 4));
+  const __nv_bfloat16* xp = p.x + (long long)(m0 + xr) * p.ldx + (long long)c0 * CK + 8 * xc;
+  const int x_rows = min(rows, p.M - m0);                // rows of the tile that exist
+  int l_ci = 0, l_ai = 0, l_item = 0;                    // the next item to load
+  auto load = [&]() {
+    if (l_item < items) {
+      const int k0 = (c0 + l_ci) * CK;
+      const bool kin = k0 + 8 * xc < p.C;
+      if (l_ai == 0) {
+        const uint32_t dst = x_off + (uint32_t)((l_ci & (DEPTH - 1)) * rows * 128) + xs;
+        const __nv_bfloat16* src = xp + l_ci * CK;
+#pragma unroll 4
+        for (int i = 0; 32 * i + xr < rows; ++i) {
+          const bool on = kin && 32 * i + xr < x_rows;
+          cp_async16(dst + (uint32_t)(i * 4096), on ? src + (long long)(32 * i) * p.ldx : p.x, on);
         }
       }
-      const __nv_bfloat16* f = p.f + (size_t)sm.adapters[ai] * p.r * p.C;
-      const uint32_t dst = f_off + (uint32_t)((item % DEPTH) * R * 128);
+      const __nv_bfloat16* f = p.f + (size_t)sm.adapters[l_ai] * p.r * p.C;
+      const uint32_t dst = f_off + (uint32_t)((l_item & (DEPTH - 1)) * R * 128);
       if (!RM) {                           // [rank][64]
-        for (int i = (int)threadIdx.x; i < R * 8; i += LOW_THREADS) {
-          const int row = i >> 3, k = k0 + 8 * xc;
-          const bool on = row < p.r && k < p.C;
-          cp_async16(dst + (uint32_t)(row * 128 + ((xc ^ (row & 7)) << 4)), on ? f + (size_t)row * p.C + k : f, on);
+#pragma unroll
+        for (int i = 0; 32 * i < R; ++i) {
+          const int row = xr + 32 * i;
+          if (row >= R) break;
+          const bool on = row < p.r && kin;
+          cp_async16(dst + (uint32_t)(i * 4096) + xs, on ? f + (size_t)row * p.C + k0 + 8 * xc : f, on);
         }
       } else {                             // [64][rank]: rows of 2 R bytes; 8 neighbouring rows on different banks
         for (int i = (int)threadIdx.x; i < 64 * NT; i += LOW_THREADS) {
@@ -126,6 +135,8 @@ __global__ void __launch_bounds__(LOW_THREADS) low_tile_kernel(const LowArgs p) 
           cp_async16(dst + (uint32_t)(row * (R * 2) + ((c ^ sw) << 4)), on ? f + (size_t)k * p.r + 8 * c : f, on);
         }
       }
+      ++l_item;
+      if (++l_ai == count) l_ai = 0, ++l_ci;
     }
     cp_async_commit();
   };
@@ -139,20 +150,22 @@ __global__ void __launch_bounds__(LOW_THREADS) low_tile_kernel(const LowArgs p) 
   const int lr = lane & 15, lc = lane >> 4;         // ldmatrix: the lane's row and 16-byte column of a 16 x 16 block
 
 #pragma unroll
-  for (int i = 0; i < DEPTH - 1; ++i) load(i);
+  for (int i = 0; i < DEPTH - 1; ++i) load();
+  int ci = 0, ai = -1;
   for (int item = 0; item < items; ++item) {
-    const int ci = item / count, ai = item - ci * count, k0 = (c0 + ci) * CK;
+    if (++ai == count) ai = 0, ++ci;
     cp_async_wait<DEPTH - 2>();
-    const uint32_t xb = x_off + (uint32_t)((ci % DEPTH) * rows * 128), fb = f_off + (uint32_t)((item % DEPTH) * R * 128);
+    const uint32_t xb = x_off + (uint32_t)((ci & (DEPTH - 1)) * rows * 128), fb = f_off + (uint32_t)((item & (DEPTH - 1)) * R * 128);
     if (drop && ai == 0) {
-      for (int i = (int)threadIdx.x; i < rows * 8; i += LOW_THREADS) {
-        const int row = i >> 3;
-        uint4* q = reinterpret_cast<uint4*>(sraw + (xb - x_off) + row * 128 + ((xc ^ (row & 7)) << 4));
-        *q = and4(*q, lora_keep8((uint32_t)((k0 >> 3) + xc), (uint32_t)(m0 + row), p.drop, key));
+      const uint32_t c = (uint32_t)((c0 + ci) * (CK / 8) + xc);
+#pragma unroll 2
+      for (int row = xr; row < x_rows; row += 32) {
+        uint4* q = reinterpret_cast<uint4*>(sraw + (xb - x_off) + (row - xr) * 128 + xs);
+        *q = lora_dropped8(*q, c, (uint32_t)(m0 + row), p.drop, key);
       }
     }
     __syncthreads();
-    load(item + DEPTH - 1);
+    load();
     const int a = sm.adapters[ai];
     const bool on0 = id0 == a, on1 = id1 == a;
     if (!__any_sync(0xffffffffu, on0 || on1)) continue;
@@ -255,7 +268,7 @@ __global__ void __launch_bounds__(ROW_THREADS) low_row_kernel(const LowArgs p) {
       for (int o = o0 + lane; o < o1; o += 32) {
         uint4 xv = ldg16(x + 8 * o);
         const uint4 a0 = ldg16(f0 + 8 * o), a1 = ldg16(f0 + p.C + 8 * o);
-        if (drop) xv = and4(xv, lora_keep8((uint32_t)o, (uint32_t)m, p.drop, key));
+        if (drop) xv = lora_dropped8(xv, (uint32_t)o, (uint32_t)m, p.drop, key);
         v0 = dot8(xv, a0, v0);
         v1 = dot8(xv, a1, v1);
       }
