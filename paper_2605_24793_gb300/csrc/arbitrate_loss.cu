@@ -34,7 +34,7 @@ constexpr int CLUSTER = 8;                // CTAs that join their sums
 constexpr int FIN_THREADS = 1024;
 
 struct LossSmem {
-  float feat[BATCH][8];
+  float feat[BATCH][16];                  // every feature twice: an operand of both units of a pair
   float adv[BATCH], old[BATCH], ref[BATCH], g[BATCH];
   int at[BATCH];                          // position in the step | action taken << 31
   uint16_t list[STEP];                    // effective positions of the step
@@ -131,19 +131,28 @@ __global__ void __launch_bounds__(THREADS) arb_loss_kernel(const ArbLossArgs a, 
 
   for (long long base = (long long)blockIdx.x * step; base < total; base += (long long)gridDim.x * step) {
     const int words = step / 32;
+    // every load of the step goes out before the first is used
+    int dr[PER], ar[PER];
+    uint32_t ef[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const long long e = base + j * THREADS + tid;
+      dr[j] = ar[j] = 0;
+      ef[j] = 0;
+      if (j * THREADS < step && e < total) {
+        dr[j] = __ldg(a.draft + e);
+        ar[j] = __ldg(a.argmax + e + (int)e / a.K);          // rows of K + 1
+        ef[j] = __ldg(a.eff + e);
+      }
+    }
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       if (j * THREADS >= step) break;
       const long long e = base + j * THREADS + tid;
-      bool match = false, act = false;
-      if (e < total) {
-        const int r = (int)e / a.K;
-        match = a.draft[e] == a.argmax[e + r];           // rows of K + 1
-        act = !match && a.eff[e] != 0;
-        if (!act) {
-          a.p_new[e] = 0.f;
-          a.dz[e] = 0.f;
-        }
+      const bool match = e < total && dr[j] == ar[j], act = dr[j] != ar[j] && ef[j] != 0;
+      if (e < total && !act) {
+        a.p_new[e] = 0.f;
+        a.dz[e] = 0.f;
       }
       const unsigned mm = __ballot_sync(0xffffffffu, match), aa = __ballot_sync(0xffffffffu, act);
       if (lane == 0) {
@@ -197,9 +206,10 @@ __global__ void __launch_bounds__(THREADS) arb_loss_kernel(const ArbLossArgs a, 
           if (word * 32 < lo) m &= 0xffffffffu << (lo & 31);
           before += __popc(m);
         }
-        float4* f = reinterpret_cast<float4*>(sm.feat[d]);
-        f[0] = make_float4(x4 - x2, x0 - x2, x0 - x1, x3);
-        f[1] = make_float4(y0 - y2, i + 1 < a.K ? y4 - y2 : 0.f, (float)(i + 1) * inv_k, (float)before * inv_k);
+        const float f[8] = {x4 - x2, x0 - x2, x0 - x1, x3, y0 - y2, i + 1 < a.K ? y4 - y2 : 0.f, (float)(i + 1) * inv_k, (float)before * inv_k};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          *reinterpret_cast<float4*>(&sm.feat[d][4 * k]) = make_float4(f[2 * k], f[2 * k], f[2 * k + 1], f[2 * k + 1]);
         sm.adv[d] = adv;
         sm.old[d] = old;
         sm.ref[d] = ref;
@@ -211,15 +221,19 @@ __global__ void __launch_bounds__(THREADS) arb_loss_kernel(const ArbLossArgs a, 
         unsigned bits = 0;
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
-          const float4 fa = *reinterpret_cast<const float4*>(&sm.feat[4 * q + d][0]);
-          const float4 fb = *reinterpret_cast<const float4*>(&sm.feat[4 * q + d][4]);
-          const float f[8] = {fa.x, fa.y, fa.z, fa.w, fb.x, fb.y, fb.z, fb.w};
+          float2 f[8];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float4 v = *reinterpret_cast<const float4*>(&sm.feat[4 * q + d][4 * k]);
+            f[2 * k] = make_float2(v.x, v.y);
+            f[2 * k + 1] = make_float2(v.z, v.w);
+          }
           float2 zz = make_float2(0.f, 0.f);
 #pragma unroll
           for (int i = 0; i < PP; ++i) {
             float2 v = b1[i];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v = fma2(w1[i][k], make_float2(f[k], f[k]), v);
+            for (int k = 0; k < 8; ++k) v = fma2(w1[i][k], f[k], v);
             bits |= ((v.x > 0.f ? 1u : 0u) | (v.y > 0.f ? 2u : 0u)) << (4 * d + 2 * i);
             zz = fma2(w2[i], make_float2(fmaxf(v.x, 0.f), fmaxf(v.y, 0.f)), zz);
           }
@@ -262,15 +276,19 @@ __global__ void __launch_bounds__(THREADS) arb_loss_kernel(const ArbLossArgs a, 
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
           if (4 * q + d >= count) break;     // what stands there is of another batch
-          const float4 fa = *reinterpret_cast<const float4*>(&sm.feat[4 * q + d][0]);
-          const float4 fb = *reinterpret_cast<const float4*>(&sm.feat[4 * q + d][4]);
-          const float f[8] = {fa.x, fa.y, fa.z, fa.w, fb.x, fb.y, fb.z, fb.w};
+          float2 f[8];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float4 v = *reinterpret_cast<const float4*>(&sm.feat[4 * q + d][4 * k]);
+            f[2 * k] = make_float2(v.x, v.y);
+            f[2 * k + 1] = make_float2(v.z, v.w);
+          }
           const float g = sm.g[4 * q + d];
 #pragma unroll
           for (int i = 0; i < PP; ++i) {
             const float2 m = make_float2((bits >> (4 * d + 2 * i)) & 1u ? g : 0.f, (bits >> (4 * d + 2 * i)) & 2u ? g : 0.f);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) S[i][k] = fma2(m, make_float2(f[k], f[k]), S[i][k]);
+            for (int k = 0; k < 8; ++k) S[i][k] = fma2(m, f[k], S[i][k]);
             S[i][8] = add2(S[i][8], m);
           }
         }
@@ -315,13 +333,7 @@ __global__ void __launch_bounds__(THREADS) arb_loss_kernel(const ArbLossArgs a, 
   const uint32_t red0 = smem_u32(red);
   float* out = ws_s + (size_t)group * 9 * HP;
   for (int e = rank * THREADS + tid; e < 9 * HP; e += CS * THREADS) {
-    float s = 0.f;
-    for (int i = 0; i < CS; ++i) {
-      float w;
-      asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w) : "r"(dsmem_map(red0 + 4u * (uint32_t)e, (uint32_t)i)) : "memory");
-      s += w;
-    }
-    out[e] = s;
+    out[e] = dsmem_sum(red0 + 4u * (uint32_t)e, CS);
   }
   if (rank == 0 && tid < 4) {
     float2 v = make_float2(0.f, 0.f);

@@ -213,6 +213,34 @@ CS_DEV uint32_t dsmem_map(uint32_t local, uint32_t rank) {
 CS_DEV void dsmem_store_u32(uint32_t addr_cluster, uint32_t v) {
   asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr_cluster), "r"(v) : "memory");
 }
+// The sum of one float at the same place of the cluster's first S <= 8 CTAs, in their order; the loads go out together.
+CS_DEV float dsmem_sum(uint32_t local, int S) {
+  float w[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    w[i] = 0.f;
+    if (i < S) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w[i]) : "r"(dsmem_map(local, (uint32_t)i)));
+  }
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s += w[i];
+  return s;
+}
+CS_DEV float4 dsmem_sum4(uint32_t local, int S) {
+  float4 w[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    w[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (i < S)
+      asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                   : "=f"(w[i].x), "=f"(w[i].y), "=f"(w[i].z), "=f"(w[i].w)
+                   : "r"(dsmem_map(local, (uint32_t)i)));
+  }
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s.x += w[i].x, s.y += w[i].y, s.z += w[i].z, s.w += w[i].w;
+  return s;
+}
 // Bulk copy of `bytes` (multiple of 16) from this CTA's shared memory to
 // another CTA's shared memory in the cluster; completion is counted on the
 // destination CTA's mbarrier (cluster address).

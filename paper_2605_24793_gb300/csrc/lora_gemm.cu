@@ -15,6 +15,8 @@
 // in shared memory in a fixed order.
 #include <cuda.h>
 
+#include <atomic>
+
 #include "lora.cuh"
 
 namespace cospec {
@@ -28,6 +30,7 @@ constexpr int UNIT = 16;                 // ranks of a unit
 constexpr int UNIT_BYTES = BM * UNIT * 2;
 constexpr int STEP_UNITS = 2;            // units of an adapter step: 64 columns of hi and lo
 constexpr int MAX_NT = 256;
+constexpr int TWO_PER_SM = 96;            // rows of a tile up to which two CTAs share an SM
 constexpr uint64_t WAIT_NS = 2000000000ull;
 
 struct GemmArgs {
@@ -413,15 +416,7 @@ __global__ void __launch_bounds__(256, 1)
     const int f = f0 + lane * 4;
     for (int row = r0 + warp; row < r1; row += 8) {
       if (row0 + row >= p.M) break;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int i = 0; i < S; ++i) {
-        float4 w;
-        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                     : "=f"(w.x), "=f"(w.y), "=f"(w.z), "=f"(w.w)
-                     : "r"(dsmem_map(base + (uint32_t)(row * BM + lane * 4) * 4u, (uint32_t)i))
-                     : "memory");
-        v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
-      }
+      const float4 v = dsmem_sum4(base + (uint32_t)(row * BM + lane * 4) * 4u, S);
       if (f < p.F)
         *reinterpret_cast<uint2*>(p.y + (long long)(row0 + row) * p.ldy + f) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
     }
@@ -436,12 +431,50 @@ __global__ void __launch_bounds__(256, 1)
   }
 }
 
+// Clusters of S CTAs of the kernel resident at once, one or two CTAs an SM (by `kind`; asked once per device).
 template <bool MN, bool DROP>
-cudaError_t launch_tile(const CUtensorMap& w, const CUtensorMap& x, const CUtensorMap& f, GemmArgs p, int splits, cudaStream_t stream) {
+int resident_clusters(int S, size_t smem, int kind, int num_sms) {
+  static std::atomic<int> cache[KL_MAX_DEV][2][9];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= KL_MAX_DEV) return num_sms / S;
+  int n = cache[dev][kind][S].load(std::memory_order_relaxed);
+  if (n == 0) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(S * num_sms));
+    cfg.blockDim = dim3(256);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)S;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, lora_tile_kernel<MN, DROP>, &cfg) != cudaSuccess || n < 1) {
+      cudaGetLastError();
+      return num_sms / S;
+    }
+    cache[dev][kind][S].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
+template <bool MN, bool DROP>
+cudaError_t launch_tile(const CUtensorMap& w, const CUtensorMap& x, const CUtensorMap& f, GemmArgs p, int num_sms, cudaStream_t stream) {
   static KernelLimits lim;
   const size_t smem = tile_layout(p.stages, p.nt).total + 1024;
   const cudaError_t e = ensure_kernel_limits((const void*)lora_tile_kernel<MN, DROP>, lim, 227 * 1024, false);
   if (e != cudaSuccess) return e;
+  // The split with the least blocks of the contraction one after another: waves of resident clusters, each a split's
+  // share and what a CTA costs besides (about eight blocks' time).
+  const int tiles = (p.F + BM - 1) / BM * ((p.M + p.nt - 1) / p.nt), kblocks = (p.C + BK - 1) / BK;
+  int splits = 1;
+  long long best = 0;
+  for (int s = 1; s <= 8 && s <= kblocks; ++s) {
+    const int room = resident_clusters<MN, DROP>(s, smem, p.nt <= TWO_PER_SM ? 1 : 0, num_sms);
+    const long long cost = (long long)((tiles + room - 1) / room) * ((kblocks + s - 1) / s + 8);
+    if (best == 0 || cost < best) best = cost, splits = s;
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((p.F + BM - 1) / BM * splits), (unsigned)((p.M + p.nt - 1) / p.nt));
   cfg.blockDim = dim3(256);
@@ -878,33 +911,31 @@ cudaError_t launch_lora_gemm(const LoraArgs& a, bool backward, int num_sms, int*
   p.err = err;
   const bool drop = p.drop.thr != 0u;
   const int kblocks = (p.C + BK - 1) / BK;
-  // Above 256 rows a CTA pair's tiles, of the size that leaves the fewest pairs idle: a tile costs its rows
-  // and what does not depend on them (about 64 rows' worth).
+  // Above 256 rows a CTA pair's tiles, of the size that leaves the fewest pairs idle: a tile takes the bytes of its
+  // operands (its rows and 256 features) and about eight blocks' time besides.
   const bool pairs = p.M > MAX_NT;
-  int grid = 0, splits = 1;
+  int grid = 0;
   if (pairs) {
     const int all = num_sms / 2, ftiles = (p.F + PBM - 1) / PBM;
     long long best = 0;
     for (int nt = MAX_NT; nt >= 64; nt -= 32) {
-      const long long t = (long long)ftiles * ((p.M + nt - 1) / nt), cost = (t + all - 1) / all * (nt + 64);
+      const long long t = (long long)ftiles * ((p.M + nt - 1) / nt), cost = (t + all - 1) / all * (nt + 256 + 4096 / kblocks);
       if (best == 0 || cost < best) {
         best = cost;
         p.nt = nt;
         grid = t < all ? (int)t : all;
       }
     }
+    p.stages = (int)((226u * 1024u - pair_layout(0, p.nt).total) / (A_BYTES + (uint32_t)p.nt * 64u + 32u));
+    if (p.stages > 10) p.stages = 10;
   } else {
-    p.nt = (p.M + 15) / 16 * 16;
-    const int tiles = (p.F + BM - 1) / BM;
-    splits = num_sms / tiles;
-    if (splits > 8) splits = 8;
-    if (splits > kblocks) splits = kblocks;
-    if (splits < 1) splits = 1;
+    // one row tile, or equal parts of at most 256; two CTAs an SM while rings of half the shared memory hold three stages
+    const int row_tiles = (p.M + MAX_NT - 1) / MAX_NT;
+    p.nt = ((p.M + row_tiles - 1) / row_tiles + 15) / 16 * 16;
+    const uint32_t budget = p.nt <= TWO_PER_SM ? 112u * 1024u : 226u * 1024u;
+    p.stages = (int)((budget - tile_layout(0, p.nt).total) / (A_BYTES + (uint32_t)p.nt * 128u + 32u));
+    if (p.stages > 6) p.stages = 6;
   }
-  const uint32_t budget = 226u * 1024u;
-  p.stages = pairs ? (int)((budget - pair_layout(0, p.nt).total) / (A_BYTES + (uint32_t)p.nt * 64u + 32u))
-                   : (int)((budget - tile_layout(0, p.nt).total) / (A_BYTES + (uint32_t)p.nt * 128u + 32u));
-  if (p.stages > 10) p.stages = 10;
   const int cols = p.nt * (drop || pairs ? 2 : 1);
   p.tmem_cols = 32;
   while (p.tmem_cols < cols) p.tmem_cols *= 2;
@@ -926,9 +957,9 @@ cudaError_t launch_lora_gemm(const LoraArgs& a, bool backward, int num_sms, int*
     if (drop) return launch_pair<true, true>(w, x, f, p, grid, stream);
     return launch_pair<true, false>(w, x, f, p, grid, stream);
   }
-  if (!backward) return launch_tile<false, false>(w, x, f, p, splits, stream);
-  if (drop) return launch_tile<true, true>(w, x, f, p, splits, stream);
-  return launch_tile<true, false>(w, x, f, p, splits, stream);
+  if (!backward) return launch_tile<false, false>(w, x, f, p, num_sms, stream);
+  if (drop) return launch_tile<true, true>(w, x, f, p, num_sms, stream);
+  return launch_tile<true, false>(w, x, f, p, num_sms, stream);
 }
 
 }  // namespace cospec

@@ -215,12 +215,7 @@ __global__ void __launch_bounds__(GRAD_THREADS) lora_grad_kernel(const GradArgs 
     const int n = which ? e / R : e % CB, j = which ? e % R : e / CB;
     if (c0 + n >= width || j >= p.r) continue;
     const uint32_t at = base + 4u * (uint32_t)(which ? n * LB + j : j * LA + n);
-    float s = 0.f;
-    for (int i = 0; i < S; ++i) {
-      float w;
-      asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w) : "r"(dsmem_map(at, (uint32_t)i)) : "memory");
-      s += w;
-    }
+    const float s = dsmem_sum(at, S);
     float* o = which ? out + ((size_t)a * width + c0 + n) * p.r + j : out + ((size_t)a * p.r + j) * width + c0 + n;
     *o = p.accumulate ? *o + s : s;
   }

@@ -76,8 +76,15 @@ __global__ void __launch_bounds__(LOW_THREADS) low_tile_kernel(const LowArgs p) 
   unsigned mask = 0;
   if (threadIdx.x < LOW_MAX_ROWS) {
     const int id = sm.ids[threadIdx.x];
-    first = id >= 0;
-    for (int j = 0; j < (int)threadIdx.x && first; ++j) first = sm.ids[j] != id;
+    first = id >= 0 && (threadIdx.x == 0 || sm.ids[threadIdx.x - 1] != id);       // (most rows follow one of their own)
+    if (first) {
+      for (int j = 0; j < (int)threadIdx.x; j += 4) {
+        const int4 v = *reinterpret_cast<const int4*>(&sm.ids[j]);
+        first = first && v.x != id && (j + 1 >= (int)threadIdx.x || v.y != id) && (j + 2 >= (int)threadIdx.x || v.z != id) &&
+                (j + 3 >= (int)threadIdx.x || v.w != id);
+      }
+    }
+    __syncwarp();
     mask = __ballot_sync(0xffffffffu, first);
     if (lane == 0) sm.warp_count[warp] = __popc(mask);
   }
@@ -215,15 +222,7 @@ __global__ void __launch_bounds__(LOW_THREADS) low_tile_kernel(const LowArgs p) 
     const long long m = (long long)m0 + row;
     if (j >= p.r || m >= p.M) continue;
     float v = 0.f;
-    for (int i = 0; i < S; ++i)
-      for (int w = 0; w < KW; ++w) {
-        float x;
-        asm volatile("ld.shared::cluster.f32 %0, [%1];"
-                     : "=f"(x)
-                     : "r"(dsmem_map(base + 4u * (uint32_t)((w * rows + row) * RP + j), (uint32_t)i))
-                     : "memory");
-        v += x;
-      }
+    for (int w = 0; w < KW; ++w) v += dsmem_sum(base + 4u * (uint32_t)((w * rows + row) * RP + j), S);
     const int a = p.adapter[m];
     p.u[(size_t)m * p.r + j] = a >= 0 && a < p.n ? v * (p.scaling[a] * p.keep_inv) : 0.f;
   }
