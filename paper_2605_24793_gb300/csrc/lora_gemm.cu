@@ -30,7 +30,6 @@ constexpr int UNIT = 16;                 // ranks of a unit
 constexpr int UNIT_BYTES = BM * UNIT * 2;
 constexpr int STEP_UNITS = 2;            // units of an adapter step: 64 columns of hi and lo
 constexpr int MAX_NT = 256;
-constexpr int TWO_PER_SM = 96;            // rows of a tile up to which two CTAs share an SM
 constexpr uint64_t WAIT_NS = 2000000000ull;
 
 struct GemmArgs {
@@ -105,9 +104,11 @@ CS_DEV void build_list(TileList& L, const GemmArgs& p, int row0, int t, int bar)
   if (t == 0) L.count = done;
 }
 
-// One row's 16 ranks of a unit as hi and lo into the 128-byte row of the operand (columns 32 slot ..).
-CS_DEV void write_unit_row(uint8_t* tile, int row, int slot, const float* u, bool mine, int j0, int r) {
-  uint4 w[4] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+// One row's 16 ranks of a unit as hi and lo: four 16-byte chunks of the operand's 128-byte row.
+CS_DEV void unit_row(uint4 (&w)[4], const float* u, bool mine, int j0, int r) {
+  const uint4 zero[4] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+#pragma unroll
+  for (int c = 0; c < 4; ++c) w[c] = zero[c];
   if (mine) {
     float v[16];
 #pragma unroll
@@ -130,6 +131,9 @@ CS_DEV void write_unit_row(uint8_t* tile, int row, int slot, const float* u, boo
     w[2] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
     w[3] = make_uint4(lo[4], lo[5], lo[6], lo[7]);
   }
+}
+// Stored in columns 32 slot .. of the row.
+CS_DEV void store_unit_row(uint8_t* tile, int row, int slot, const uint4 (&w)[4]) {
 #pragma unroll
   for (int c = 0; c < 4; ++c)
     *reinterpret_cast<uint4*>(tile + row * 128 + (((4 * slot + c) ^ (row & 7)) << 4)) = w[c];
@@ -159,8 +163,28 @@ __host__ __device__ inline TileSmem tile_layout(int stages, int nt) {
   L.b_off = (uint32_t)stages * A_BYTES;
   L.list_off = L.b_off + (uint32_t)stages * nt * 128;
   L.bar_off = L.list_off + (uint32_t)((sizeof(TileList) + 15) / 16 * 16);
-  L.total = L.bar_off + (uint32_t)(4 * stages + 2) * 8 + 16;
+  L.total = L.bar_off + (uint32_t)(3 * stages + 2) * 8 + 16;
   return L;
+}
+
+CS_DEV void st_release_cta(int* p, int v) {
+  asm volatile("st.release.cta.shared.s32 [%0], %1;" ::"r"(smem_u32(p)), "r"(v) : "memory");
+}
+// Waits until *p >= v, for two seconds at most.
+CS_DEV bool wait_count(const int* p, int v) {
+  uint64_t t0 = 0;
+#pragma unroll 1
+  for (int i = 0;; ++i) {
+    int x;
+    asm volatile("ld.acquire.cta.shared.s32 %0, [%1];" : "=r"(x) : "r"(smem_u32(p)) : "memory");
+    if (x >= v) return true;
+    __nanosleep(20);
+    if ((i & 63) == 63) {
+      const uint64_t now = global_timer_ns();
+      if (t0 == 0) t0 = now;
+      else if (now - t0 > WAIT_NS) return false;
+    }
+  }
 }
 
 // Warps: 0 loads W and the factors, 1 issues the MMAs, 2 loads the rows, 3 allocates TMEM, 4 to 7 list the
@@ -176,11 +200,11 @@ __global__ void __launch_bounds__(256, 1)
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L.bar_off);
   uint64_t* empty = full + p.stages;
   uint64_t* ufull = empty + p.stages;      // the u operand of a stage is written
-  uint64_t* ugo = ufull + p.stages;        // the u operand of a stage may be written
-  uint64_t* lready = ugo + p.stages;       // the list is written
+  uint64_t* lready = ufull + p.stages;     // the list is written
   uint64_t* done = lready + 1;             // every MMA is done
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(done + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+  int* ugo = reinterpret_cast<int*>(tmem_holder + 2);      // adapter steps whose stage is free
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int S = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
@@ -195,12 +219,12 @@ __global__ void __launch_bounds__(256, 1)
     for (int s = 0; s < p.stages; ++s) {
       mbar_init(&full[s], 2);
       mbar_init(&empty[s], 1);
-      mbar_init(&ufull[s], 4);
-      mbar_init(&ugo[s], 1);
+      mbar_init(&ufull[s], 1);
     }
     mbar_init(lready, 4);
     mbar_init(done, 1);
     *abort_flag = 0;
+    *ugo = 0;
     fence_barrier_init();
     tma_prefetch_desc(&tmap_w);
     tma_prefetch_desc(&tmap_x);
@@ -267,9 +291,8 @@ __global__ void __launch_bounds__(256, 1)
             mbar_arrive(&full[s]);
           } else {
             const int u0 = (rank + i * S) * STEP_UNITS, nu = min(STEP_UNITS, units - u0);
-            // (the writers join only now: the stage's turns before passed without them, and a wait by parity
-            // would not tell those apart)
-            mbar_arrive(&ugo[s]);
+            // (a count, not a barrier's parity: the writers pass over stages' turns that are not theirs)
+            st_release_cta(ugo, i + 1);
             mbar_arrive_expect_tx(&full[s], (uint32_t)nu * UNIT_BYTES);
             for (int q = 0; q < nu; ++q) {
               const int e = (u0 + q) / upe, j0 = ((u0 + q) % upe) * UNIT;
@@ -352,14 +375,14 @@ __global__ void __launch_bounds__(256, 1)
     const int units = list.count * upe, n = my_steps();
     griddep_wait();                        // u
     griddep_launch_dependents();
-    int st = nk % p.stages;
-    uint32_t gphase = 0;
-    for (int i = 0; i < n; ++i) {
-      const int s = st;
-      ok = __all_sync(0xffffffffu, mbar_wait(&ugo[s], (gphase >> s) & 1u, WAIT_NS)) && !*abort_flag;
-      if (!ok) break;
-      gphase ^= 1u << s;
-      if (++st == p.stages) st = 0;
+    // a warp per step, so that four steps' reads of u are under way at once
+    for (int i = warp - 4; i < n; i += 4) {
+      const int s = (nk + i) % p.stages;
+      ok = wait_count(ugo, i + 1) && !*abort_flag;
+      if (!__all_sync(0xffffffffu, ok)) {
+        ok = false;
+        break;
+      }
       uint8_t* tile = smem + L.b_off + (uint32_t)s * b_bytes;
       const int u0 = (rank + i * S) * STEP_UNITS, nu = min(STEP_UNITS, units - u0);
       for (int q = 0; q < nu; ++q) {
@@ -367,8 +390,11 @@ __global__ void __launch_bounds__(256, 1)
         const int id = list.adapter[e], span = list.span[e];
         const bool all = DROP && i == 0 && q == 0;
         const int lo = all ? 0 : (span & 0xffff) & ~15, hi = all ? p.nt : ((span >> 16) | 15) + 1;
-        for (int row = lo + t; row < hi; row += 128)
-          write_unit_row(tile, row, q, p.u + (size_t)(row0 + row) * p.r, list.ids[row] == id, j0, p.r);
+        for (int row = lo + lane; row < hi; row += 32) {
+          uint4 w[4];
+          unit_row(w, p.u + (size_t)(row0 + row) * p.r, list.ids[row] == id, j0, p.r);
+          store_unit_row(tile, row, q, w);
+        }
       }
       fence_proxy_async_smem();
       __syncwarp();
@@ -431,18 +457,18 @@ __global__ void __launch_bounds__(256, 1)
   }
 }
 
-// Clusters of S CTAs of the kernel resident at once, one or two CTAs an SM (by `kind`; asked once per device).
+// Clusters of S CTAs of the kernel resident at once, one CTA an SM (asked once per device).
 template <bool MN, bool DROP>
-int resident_clusters(int S, size_t smem, int kind, int num_sms) {
-  static std::atomic<int> cache[KL_MAX_DEV][2][9];
+int resident_clusters(int S, int num_sms) {
+  static std::atomic<int> cache[KL_MAX_DEV][9];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= KL_MAX_DEV) return num_sms / S;
-  int n = cache[dev][kind][S].load(std::memory_order_relaxed);
+  int n = cache[dev][S].load(std::memory_order_relaxed);
   if (n == 0) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(S * num_sms));
     cfg.blockDim = dim3(256);
-    cfg.dynamicSmemBytes = smem;
+    cfg.dynamicSmemBytes = 227 * 1024;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = (unsigned)S;
@@ -454,7 +480,7 @@ int resident_clusters(int S, size_t smem, int kind, int num_sms) {
       cudaGetLastError();
       return num_sms / S;
     }
-    cache[dev][kind][S].store(n, std::memory_order_relaxed);
+    cache[dev][S].store(n, std::memory_order_relaxed);
   }
   return n;
 }
@@ -471,7 +497,7 @@ cudaError_t launch_tile(const CUtensorMap& w, const CUtensorMap& x, const CUtens
   int splits = 1;
   long long best = 0;
   for (int s = 1; s <= 8 && s <= kblocks; ++s) {
-    const int room = resident_clusters<MN, DROP>(s, smem, p.nt <= TWO_PER_SM ? 1 : 0, num_sms);
+    const int room = resident_clusters<MN, DROP>(s, num_sms);
     const long long cost = (long long)((tiles + room - 1) / room) * ((kblocks + s - 1) / s + 8);
     if (best == 0 || cost < best) best = cost, splits = s;
   }
@@ -774,18 +800,20 @@ __global__ void __launch_bounds__(P_THREADS, 1)
       for (int i = 0; i < steps; ++i) {
         const int s = st;
         if (++st == p.stages) st = 0;
+        // u is read before the stage is free
+        const int nu = min(STEP_UNITS, units - i * STEP_UNITS), row = min(rank * half + t, p.nt - 1);
+        uint4 w[STEP_UNITS][4];
+#pragma unroll
+        for (int q = 0; q < STEP_UNITS; ++q) {
+          const int u = i * STEP_UNITS + min(q, nu - 1), id = list.adapter[u / upe];
+          unit_row(w[q], p.u + (size_t)(row0 + row) * p.r, list.ids[row] == id, (u % upe) * UNIT, p.r);
+        }
         ok = __all_sync(0xffffffffu, mbar_wait_idle(&ugo[s], (gphase >> s) & 1u, WAIT_NS, 500u)) && !*abort_flag;
         if (!ok) break;
         gphase ^= 1u << s;
-        const int nu = min(STEP_UNITS, units - i * STEP_UNITS);
         uint8_t* buf = smem + L.b_off + (uint32_t)s * b_bytes;
-        if (t < half) {
-          const int row = rank * half + t;
-          for (int q = 0; q < nu; ++q) {
-            const int u = i * STEP_UNITS + q, id = list.adapter[u / upe];
-            write_unit_row(buf, t, q, p.u + (size_t)(row0 + row) * p.r, list.ids[row] == id, (u % upe) * UNIT, p.r);
-          }
-        }
+        if (t < half)
+          for (int q = 0; q < nu; ++q) store_unit_row(buf, t, q, w[q]);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(ufull0 + (uint32_t)s * 8u);
@@ -929,12 +957,11 @@ cudaError_t launch_lora_gemm(const LoraArgs& a, bool backward, int num_sms, int*
     p.stages = (int)((226u * 1024u - pair_layout(0, p.nt).total) / (A_BYTES + (uint32_t)p.nt * 64u + 32u));
     if (p.stages > 10) p.stages = 10;
   } else {
-    // one row tile, or equal parts of at most 256; two CTAs an SM while rings of half the shared memory hold three stages
+    // one row tile, or equal parts of at most 256
     const int row_tiles = (p.M + MAX_NT - 1) / MAX_NT;
     p.nt = ((p.M + row_tiles - 1) / row_tiles + 15) / 16 * 16;
-    const uint32_t budget = p.nt <= TWO_PER_SM ? 112u * 1024u : 226u * 1024u;
-    p.stages = (int)((budget - tile_layout(0, p.nt).total) / (A_BYTES + (uint32_t)p.nt * 128u + 32u));
-    if (p.stages > 6) p.stages = 6;
+    p.stages = (int)((226u * 1024u - tile_layout(0, p.nt).total) / (A_BYTES + (uint32_t)p.nt * 128u + 32u));
+    if (p.stages > 12) p.stages = 12;
   }
   const int cols = p.nt * (drop || pairs ? 2 : 1);
   p.tmem_cols = 32;
