@@ -810,35 +810,64 @@ def get_device_error(stream=None) -> int:
 
 
 # ---------------------------------------------------------------- low-rank adapters
-def _req_rows(t: torch.Tensor, dtype, name: str, rows: int, width: int) -> int:
-    """A [rows, width] tensor whose rows may be parts of a wider buffer's; returns its row stride."""
-    if t.dtype != dtype:
-        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+# These calls take many tensors and some take a few microseconds on the GPU, so what is right is checked in one pass over
+# (tensor, dtype, shape), and only what is not goes through the checks that name it.
+_BF16, _F32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+
+
+def _all_fit(dev: int, specs) -> bool:
+    for t, dtype, shape in specs:
+        if t.dtype is not dtype or t.get_device() != dev or t.shape != shape or not t.is_contiguous():
+            return False
+    return True
+
+
+def _name_misfit(dev: int, specs, names) -> None:
+    for (t, dtype, shape), name in zip(specs, names):
+        _req(t, dtype, name)
+        _need(tuple(t.shape) == tuple(shape), f"{name} must be {list(shape)}")
+        if t.get_device() != dev:
+            raise ValueError(f"{name}: tensor on {t.device}, but the current device is cuda:{dev}")
+
+
+def _current(stream):
+    """(current device, the stream's handle)."""
+    dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else torch.cuda.current_device() if torch.cuda.is_available() else 0
+    if stream is not None:
+        return dev, stream.cuda_stream
+    return dev, torch._C._cuda_getCurrentRawStream(dev) if torch.cuda.is_initialized() else 0
+
+
+def _rows_stride(t: torch.Tensor, name: str, dev: int, rows: int, width: int) -> int:
+    """Row stride of a bf16 [rows, width] tensor whose rows may be parts of a wider buffer's (0: dense)."""
+    if t.dtype is _BF16 and t.get_device() == dev and t.shape == (rows, width):
+        a, b = t.stride()
+        if rows <= 1 and (b == 1 or width == 1):
+            return 0
+        if b == 1 and a >= width and a % 8 == 0:
+            return a
+    if t.dtype != _BF16:
+        raise TypeError(f"{name}: expected {_BF16}, got {t.dtype}")
     if not t.is_cuda:
         raise ValueError(f"{name}: must be a CUDA tensor")
     _need(tuple(t.shape) == (rows, width), f"{name} must be [{rows}, {width}]")
-    _need(t.stride(1) == 1 or width == 1, f"{name}: values of a row must be side by side")
-    stride = t.stride(0) if rows > 1 else width
-    _need(stride >= width and stride % 8 == 0, f"{name}: rows must not overlap and lie a multiple of 8 elements apart")
-    return int(stride)
+    if t.get_device() != dev:
+        raise ValueError(f"{name}: tensor on {t.device}, but the current device is cuda:{dev}")
+    raise ValueError(f"{name}: values of a row must be side by side, rows apart by a multiple of 8 elements, not overlapping")
 
 
-def _lora_dims(w, a, b, scaling, adapter, dropout: float, seed, site: int) -> LoraDims:
-    """Checks what the two passes share: w [N, K], a [n, r, K], b [n, N, r], scaling [n], adapter [M], an int64 seed."""
-    for t, n, d in ((w, "w", 2), (a, "a", 3), (b, "b", 3)):
-        _req(t, torch.bfloat16, n, d)
-    _req(scaling, torch.float32, "scaling", 1)
-    _req(adapter, torch.int32, "adapter", 1)
-    N, K = w.shape
-    n, r = a.shape[:2]
-    _need(a.shape[2] == K, "a must be [adapters, rank, in_features]")
-    _need(tuple(b.shape) == (n, N, r), "b must be [adapters, out_features, rank]")
-    _need(scaling.shape[0] == n, "scaling must hold a value per adapter")
+def _check_seed(seed, site: int, dev: int) -> None:
     _need(0 <= site < 1 << 32, "site must be a 32-bit number")
     if seed is not None:
         _req(seed, torch.int64, "seed")
         _need(seed.numel() == 1, "seed must hold one value")
-    return LoraDims(adapter.shape[0], K, N, r, n, float(dropout), int(site), 0, 0, 0)
+        if seed.get_device() != dev:
+            raise ValueError(f"seed: tensor on {seed.device}, but the current device is cuda:{dev}")
+
+
+def _lora_sizes(w, a, adapter):
+    _need(w.dim() == 2 and a.dim() == 3 and adapter.dim() == 1, "w must be [N, K], a [adapters, rank, K], adapter [rows]")
+    return (*w.shape, *a.shape[:2], adapter.shape[0])
 
 
 def lora_forward(x, w, a, b, scaling, adapter, y, u, dropout: float = 0.0, seed=None, site: int = 0, stream=None):
@@ -846,14 +875,16 @@ def lora_forward(x, w, a, b, scaling, adapter, y, u, dropout: float = 0.0, seed=
     b [n, N, r] bf16, scaling [n] float32, adapter [M] int32; fills y [M, N] bf16 and u [M, r] float32, which the backward
     pass reads.  x and y may be columns of wider buffers.  ``seed``: an int64 device scalar, read when the kernels run;
     ``site``: the number of the place whose dropout mask this is."""
-    d = _lora_dims(w, a, b, scaling, adapter, dropout, seed, site)
-    d.x_stride = _req_rows(x, torch.bfloat16, "x", d.rows, d.in_features)
-    d.y_stride = _req_rows(y, torch.bfloat16, "y", d.rows, d.out_features)
-    _req(u, torch.float32, "u", 2)
-    _need(tuple(u.shape) == (d.rows, d.rank), "u must be [rows, rank]")
-    _same_device(x, w, a, b, scaling, adapter, y, u, seed)
-    _check(load_library().cospec_lora_forward(ctypes.byref(d), _ptr(x), _ptr(w), _ptr(a), _ptr(b), _ptr(scaling), _ptr(adapter),
-                                              _ptr(seed), _ptr(u), _ptr(y), _stream(stream)))
+    dev, handle = _current(stream)
+    N, K, n, r, M = _lora_sizes(w, a, adapter)
+    specs = ((w, _BF16, (N, K)), (a, _BF16, (n, r, K)), (b, _BF16, (n, N, r)), (scaling, _F32, (n,)), (adapter, _I32, (M,)), (u, _F32, (M, r)))
+    if not _all_fit(dev, specs):
+        _name_misfit(dev, specs, ("w", "a", "b", "scaling", "adapter", "u"))
+    _check_seed(seed, site, dev)
+    d = LoraDims(M, K, N, r, n, dropout, site, _rows_stride(x, "x", dev, M, K), _rows_stride(y, "y", dev, M, N), 0)
+    _check(load_library().cospec_lora_forward(
+        ctypes.byref(d), x.data_ptr(), w.data_ptr(), a.data_ptr(), b.data_ptr(), scaling.data_ptr(), adapter.data_ptr(),
+        None if seed is None else seed.data_ptr(), u.data_ptr(), y.data_ptr(), handle))
     return y
 
 
@@ -862,62 +893,60 @@ def lora_backward(dy, x, w, a, b, scaling, adapter, u, dx, da, db, t, dropout: f
     """The gradients of lora_forward for x and the adapters: dx [M, K] bf16, da [n, r, K] and db [n, N, r] float32 (each
     or None), from dy [M, N], the forward pass's inputs and its u.  t [M, r] float32 is scratch.  ``accumulate``: da and
     db are added to."""
-    d = _lora_dims(w, a, b, scaling, adapter, dropout, seed, site)
-    d.y_stride = _req_rows(dy, torch.bfloat16, "dy", d.rows, d.out_features)
-    d.x_stride = _req_rows(x, torch.bfloat16, "x", d.rows, d.in_features)
-    for z, n in ((u, "u"), (t, "t")):
-        _req(z, torch.float32, n, 2)
-        _need(tuple(z.shape) == (d.rows, d.rank), f"{n} must be [rows, rank]")
-    if dx is not None:
-        d.dx_stride = _req_rows(dx, torch.bfloat16, "dx", d.rows, d.in_features)
-    for z, like, n in ((da, a, "da"), (db, b, "db")):
-        if z is not None:
-            _req(z, torch.float32, n, 3)
-            _need(z.shape == like.shape, f"{n} must have {n[1:]}'s shape")
-    _same_device(dy, x, w, a, b, scaling, adapter, u, dx, da, db, t, seed)
-    _check(load_library().cospec_lora_backward(ctypes.byref(d), _ptr(dy), _ptr(x), _ptr(w), _ptr(a), _ptr(b), _ptr(scaling),
-                                               _ptr(adapter), _ptr(seed), _ptr(u), _ptr(t), _ptr(dx), _ptr(da), _ptr(db),
-                                               LORA_ACCUMULATE if accumulate else 0, _stream(stream)))
+    dev, handle = _current(stream)
+    N, K, n, r, M = _lora_sizes(w, a, adapter)
+    specs = [(w, _BF16, (N, K)), (a, _BF16, (n, r, K)), (b, _BF16, (n, N, r)), (scaling, _F32, (n,)), (adapter, _I32, (M,)), (u, _F32, (M, r)),
+             (t, _F32, (M, r))]
+    if da is not None:
+        specs.append((da, _F32, (n, r, K)))
+    if db is not None:
+        specs.append((db, _F32, (n, N, r)))
+    if not _all_fit(dev, specs):
+        _name_misfit(dev, specs, ["w", "a", "b", "scaling", "adapter", "u", "t"] + ["da"] * (da is not None) + ["db"] * (db is not None))
+    _check_seed(seed, site, dev)
+    d = LoraDims(M, K, N, r, n, dropout, site, _rows_stride(x, "x", dev, M, K), _rows_stride(dy, "dy", dev, M, N),
+                 0 if dx is None else _rows_stride(dx, "dx", dev, M, K))
+    _check(load_library().cospec_lora_backward(
+        ctypes.byref(d), dy.data_ptr(), x.data_ptr(), w.data_ptr(), a.data_ptr(), b.data_ptr(), scaling.data_ptr(), adapter.data_ptr(),
+        None if seed is None else seed.data_ptr(), u.data_ptr(), t.data_ptr(), None if dx is None else dx.data_ptr(),
+        None if da is None else da.data_ptr(), None if db is None else db.data_ptr(), LORA_ACCUMULATE if accumulate else 0, handle))
     return dx, da, db
 
 
 # ---------------------------------------------------------------- policy loss
+_LOSS_OUT = ("loss", "p_new", "dz", "dw1", "db1", "dw2", "db2")
+_LOSS_IN = ("draft", "argmax", "stats", "w1", "b1", "w2", "b2", "accept", "eff", "adv", "p_old", "p_ref")
+
+
 def arbitrate_loss(draft, argmax, stats, w1, b1, w2, b2, accept, eff, adv, p_old, p_ref, params: RLParams = None,
                    grad_scale: float = 1.0, out: Optional[dict] = None, stream=None) -> dict:
     """The RL stage's objective through the decision MLP and its gradient (Sec. 3.4) over R recorded rounds: draft
     [R, K], argmax [R, K+1], stats [R, K+1, 5] as cospec_arbitrate takes them, accept / eff uint8 and adv / p_old / p_ref
     float32 [R, K], the MLP's w1 [H, 8], b1, w2 [H], b2 [1].  Returns loss [4], p_new and dz [R, K], dw1, db1, dw2, db2 (the
-    gradients times ``grad_scale``) and ``ws``; ``out``: an earlier call's result, whose tensors are filled again."""
+    gradients times ``grad_scale``) and ``ws``; ``out``: an earlier call's result, whose tensors are filled again (give one
+    where ``stream`` is not the current stream)."""
     params = params if params is not None else RLParams()
-    _req(draft, torch.int32, "draft", 2)
-    _req(argmax, torch.int32, "argmax", 2)
-    _req(stats, torch.float32, "stats", 3)
-    R, K = draft.shape
-    _need(tuple(argmax.shape) == (R, K + 1) and tuple(stats.shape) == (R, K + 1, 5), "argmax / stats must hold K+1 rows per round")
-    _req(w1, torch.float32, "w1", 2)
-    H = w1.shape[0]
-    _need(w1.shape[1] == 8, "w1 must be [H, 8]")
-    for t, n, m in ((b1, "b1", H), (w2, "w2", H), (b2, "b2", 1)):
-        _req(t, torch.float32, n)
-        _need(t.numel() == m, f"{n} must hold {m} values")
-    for t, n, dt in ((accept, "accept", torch.uint8), (eff, "eff", torch.uint8), (adv, "adv", torch.float32),
-                     (p_old, "p_old", torch.float32), (p_ref, "p_ref", torch.float32)):
-        _req(t, dt, n, 2)
-        _need(tuple(t.shape) == (R, K), f"{n} must be [R, K]")
-    _same_device(draft, argmax, stats, w1, b1, w2, b2, accept, eff, adv, p_old, p_ref)
+    dev, handle = _current(stream)
+    _need(draft.dim() == 2 and w1.dim() == 2, "draft must be [R, K], w1 [H, 8]")
+    (R, K), H = draft.shape, w1.shape[0]
+    specs = ((draft, _I32, (R, K)), (argmax, _I32, (R, K + 1)), (stats, _F32, (R, K + 1, 5)), (w1, _F32, (H, 8)), (b1, _F32, (H,)), (w2, _F32, (H,)),
+             (b2, _F32, (1,)), (accept, _U8, (R, K)), (eff, _U8, (R, K)), (adv, _F32, (R, K)), (p_old, _F32, (R, K)), (p_ref, _F32, (R, K)))
+    if not _all_fit(dev, specs):
+        _name_misfit(dev, specs, _LOSS_IN)
     lib = load_library()
-    ws_bytes = lib.cospec_arbitrate_loss_workspace(H)
-    shapes = dict(loss=(4,), p_new=(R, K), dz=(R, K), dw1=(H, 8), db1=(H,), dw2=(H,), db2=(1,))
+    shapes = ((4,), (R, K), (R, K), (H, 8), (H,), (H,), (1,))
     if out is None:
-        out = {n: torch.empty(s, dtype=torch.float32, device=draft.device) for n, s in shapes.items()}
-        out["ws"] = torch.empty(max(1, ws_bytes), dtype=torch.uint8, device=draft.device)
-    for n, s in shapes.items():
-        _req(out[n], torch.float32, n)
-        _need(tuple(out[n].shape) == s, f"{n} must be {list(s)}")
-    _req(out["ws"], torch.uint8, "ws", 1)
-    _same_device(*out.values())
+        if stream is not None and stream.cuda_stream != _current(None)[1]:
+            raise ValueError("out must be given where stream is not the current stream (its tensors belong to the current one)")
+        out = {n: torch.empty(s, dtype=_F32, device=draft.device) for n, s in zip(_LOSS_OUT, shapes)}
+        out["ws"] = torch.empty(max(1, lib.cospec_arbitrate_loss_workspace(H)), dtype=_U8, device=draft.device)
+    res = [out[n] for n in _LOSS_OUT]
+    ws = out["ws"]
+    specs = [(t, _F32, s) for t, s in zip(res, shapes)] + [(ws, _U8, (ws.numel(),))]
+    if not _all_fit(dev, specs):
+        _name_misfit(dev, specs, _LOSS_OUT + ("ws",))
     _check(lib.cospec_arbitrate_loss(
-        R, K, _ptr(draft), _ptr(argmax), _ptr(stats), H, _ptr(w1), _ptr(b1), _ptr(w2), _ptr(b2), _ptr(accept), _ptr(eff), _ptr(adv),
-        _ptr(p_old), _ptr(p_ref), ctypes.byref(params), float(grad_scale), *(_ptr(out[n]) for n in shapes), _ptr(out["ws"]),
-        out["ws"].numel(), _stream(stream)))
+        R, K, draft.data_ptr(), argmax.data_ptr(), stats.data_ptr(), H, w1.data_ptr(), b1.data_ptr(), w2.data_ptr(), b2.data_ptr(), accept.data_ptr(),
+        eff.data_ptr(), adv.data_ptr(), p_old.data_ptr(), p_ref.data_ptr(), ctypes.byref(params), grad_scale, *[t.data_ptr() for t in res],
+        ws.data_ptr(), ws.numel(), handle))
     return out

@@ -97,7 +97,7 @@ CS_DEV Decision decide(float z, float adv, float old, float ref, bool took, cons
 
 // PP: pairs of units of a thread; TW: warps that hold all units.
 template <int PP, int TW>
-__global__ void __launch_bounds__(THREADS, PP == 1 ? 3 : 2) arb_loss_kernel(const ArbLossArgs a, float* ws_s, float2* ws_l, int step) {
+__global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs a, float* ws_s, float2* ws_l, int step) {
   extern __shared__ __align__(16) uint8_t raw[];
   LossSmem& sm = *reinterpret_cast<LossSmem*>(raw);
   constexpr int TEAMS = 8 / TW;
@@ -425,7 +425,7 @@ cudaError_t launch_loss(const ArbLossArgs& a, int num_sms, cudaStream_t stream) 
   // as many positions a step as give every CTA one, up to 2048; clusters of eight where there are that many CTAs
   const long long total = (long long)a.n * a.K;
   // (two CTAs an SM; of clusters of eight about 15 / 16 of the SMs' places are filled)
-  int most = (PP == 1 ? 45 : 30) * num_sms / 16 / CLUSTER * CLUSTER;
+  int most = 15 * num_sms / 8 / CLUSTER * CLUSTER;
   if (most > MAX_CTAS) most = MAX_CTAS;
   if (most < 1) most = 1;
   long long step = ((total + most - 1) / most + THREADS - 1) / THREADS * THREADS;
@@ -461,8 +461,8 @@ size_t arb_loss_ws_bytes(int H) { return (size_t)MAX_CTAS * (32 + (size_t)9 * pa
 
 cudaError_t launch_arb_loss(const ArbLossArgs& a, int num_sms, cudaStream_t stream) {
   if (a.H <= 64) return launch_loss<1, 1>(a, num_sms, stream);
-  if (a.H <= 128) return launch_loss<1, 2>(a, num_sms, stream);
-  if (a.H <= 256) return launch_loss<1, 4>(a, num_sms, stream);
+  if (a.H <= 128) return launch_loss<2, 1>(a, num_sms, stream);
+  if (a.H <= 256) return launch_loss<2, 2>(a, num_sms, stream);
   if (a.H <= 512) return launch_loss<2, 4>(a, num_sms, stream);
   return launch_loss<2, 8>(a, num_sms, stream);
 }

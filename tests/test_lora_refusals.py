@@ -114,6 +114,9 @@ class _Cuda:
 
     is_cuda = True
 
+    def get_device(self):
+        return 0
+
     def __getattr__(self, n):
         return getattr(self.t, n)
 
