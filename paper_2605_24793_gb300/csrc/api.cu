@@ -85,6 +85,32 @@ cudaError_t ensure_kernel_limits(const void* kern, KernelLimits& lim, size_t sme
   return cudaSuccess;
 }
 
+int resident_clusters(const void* kern, KernelLimits& lim, int key, int threads, size_t smem_bytes, int S, int num_sms) {
+  const int dev = current_device();
+  if (dev < 0 || dev >= KL_MAX_DEV) return num_sms / S > 0 ? num_sms / S : 1;
+  int n = lim.resident[dev][key].load(std::memory_order_relaxed);
+  if (n == 0) {
+    cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(S * num_sms));
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem_bytes;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)S;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n < 1) {
+      cudaGetLastError();
+      n = num_sms / S > 0 ? num_sms / S : 1;
+    }
+    lim.resident[dev][key].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
                                   const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                   const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,

@@ -424,8 +424,7 @@ cudaError_t launch_loss(const ArbLossArgs& a, int num_sms, cudaStream_t stream) 
   if (e != cudaSuccess) return e;
   // as many positions a step as give every CTA one, up to 2048; clusters of eight where there are that many CTAs
   const long long total = (long long)a.n * a.K;
-  // (two CTAs an SM; of clusters of eight about 15 / 16 of the SMs' places are filled)
-  int most = 15 * num_sms / 8 / CLUSTER * CLUSTER;
+  int most = CLUSTER * resident_clusters((const void*)arb_loss_kernel<PP, TW>, lim, 0, THREADS, smem, CLUSTER, num_sms);
   if (most > MAX_CTAS) most = MAX_CTAS;
   if (most < 1) most = 1;
   long long step = ((total + most - 1) / most + THREADS - 1) / THREADS * THREADS;

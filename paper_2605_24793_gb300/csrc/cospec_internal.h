@@ -39,6 +39,7 @@ constexpr int KL_MAX_DEV = 64;
 struct KernelLimits {
   std::atomic<size_t> smem[KL_MAX_DEV];   // dynamic shared-memory limit set so far
   std::atomic<bool> cluster[KL_MAX_DEV];  // non-portable cluster sizes allowed
+  std::atomic<int> resident[KL_MAX_DEV][16];  // resident_clusters' answers
 };
 // Raise `kern`'s dynamic shared-memory limit on the current device to at
 // least `smem_bytes` (never lowering it, so graphs captured earlier stay
@@ -54,6 +55,24 @@ int cuda_lookup_failed();
 
 cudaError_t ensure_kernel_limits(const void* kern, KernelLimits& lim, size_t smem_bytes,
                                  bool cluster);
+
+// How many clusters of S CTAs of `kern` are resident at once on the current device, asked
+// once per device and `key` (0 .. 15: the caller's number for this S, block and shared memory).
+// The first question also asks for the whole of an SM's shared memory: with the carve-out the
+// driver picks by itself an SM took one CTA where two fit.
+int resident_clusters(const void* kern, KernelLimits& lim, int key, int threads, size_t smem_bytes, int S, int num_sms);
+// The S in {1, 2, 4, 8} with the least time for `units` clusters that share out `work` steps each: waves
+// of resident clusters, each a CTA's share and `fixed` steps besides.  `work` >= 1.
+template <typename Room>
+int pick_splits(long long units, long long work, long long fixed, Room&& room) {
+  int best_s = 1;
+  long long best = 0;
+  for (int s = 1; s <= 8 && (s == 1 || s <= work); s *= 2) {
+    const long long r = room(s), cost = (units + r - 1) / r * ((work + s - 1) / s + fixed);
+    if (best == 0 || cost < best) best = cost, best_s = s;
+  }
+  return best_s;
+}
 
 // cuTensorMapEncodeTiled for a bf16 tensor (rank 1..5, innermost first),
 // 128-byte (or 32-byte) swizzle, zero fill out of bounds.  dims/box in elements, strides

@@ -15,8 +15,6 @@
 // in shared memory in a fixed order.
 #include <cuda.h>
 
-#include <atomic>
-
 #include "lora.cuh"
 
 namespace cospec {
@@ -457,34 +455,6 @@ __global__ void __launch_bounds__(256, 1)
   }
 }
 
-// Clusters of S CTAs of the kernel resident at once, one CTA an SM (asked once per device).
-template <bool MN, bool DROP>
-int resident_clusters(int S, int num_sms) {
-  static std::atomic<int> cache[KL_MAX_DEV][9];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= KL_MAX_DEV) return num_sms / S;
-  int n = cache[dev][S].load(std::memory_order_relaxed);
-  if (n == 0) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(S * num_sms));
-    cfg.blockDim = dim3(256);
-    cfg.dynamicSmemBytes = 227 * 1024;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)S;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (cudaOccupancyMaxActiveClusters(&n, lora_tile_kernel<MN, DROP>, &cfg) != cudaSuccess || n < 1) {
-      cudaGetLastError();
-      return num_sms / S;
-    }
-    cache[dev][S].store(n, std::memory_order_relaxed);
-  }
-  return n;
-}
-
 template <bool MN, bool DROP>
 cudaError_t launch_tile(const CUtensorMap& w, const CUtensorMap& x, const CUtensorMap& f, GemmArgs p, int num_sms, cudaStream_t stream) {
   static KernelLimits lim;
@@ -497,7 +467,7 @@ cudaError_t launch_tile(const CUtensorMap& w, const CUtensorMap& x, const CUtens
   int splits = 1;
   long long best = 0;
   for (int s = 1; s <= 8 && s <= kblocks; ++s) {
-    const int room = resident_clusters<MN, DROP>(s, num_sms);
+    const int room = resident_clusters((const void*)lora_tile_kernel<MN, DROP>, lim, s, 256, 227 * 1024, s, num_sms);
     const long long cost = (long long)((tiles + room - 1) / room) * ((kblocks + s - 1) / s + 8);
     if (best == 0 || cost < best) best = cost, splits = s;
   }

@@ -7,9 +7,10 @@
 // bf16 parts, which hold all 24 bits of it, so the sums are those of fp32 products (a gradient that is
 // summed over micro-batches starts from fp32).
 //
-// A CTA takes 256 columns of one adapter, 32 a warp; the adapter's rows, listed in shared memory first, so that rows
+// A CTA takes 256 columns of one adapter, 32 a warp (two warps share the rows, so that an SM has 16 or 32 of them; with eight
+// each waited on its own products: 35 us at 4096 rows of 2560 + 6144); the adapter's rows, listed in shared memory first, so that rows
 // of other adapters and what they hold are not read, come 32 at a time: Q by cp.async into a ring, P through
-// registers, where it is split once for all warps.  A thread masks the 16-byte chunks of x that it copied itself, each one
+// the same ring and is split once for all warps.  A thread masks the 16-byte chunks of x that it copied itself, each one
 // draw of the generator.  The rows are split over the CTAs of a cluster and joined in a fixed order.
 #include "lora.cuh"
 
@@ -17,7 +18,6 @@ namespace cospec {
 
 namespace {
 
-constexpr int GRAD_THREADS = 256;
 constexpr int CB = 256;              // columns of a CTA
 constexpr int BR = 32;               // rows of a batch
 constexpr int GDEPTH = 4;            // batches in the ring
@@ -39,32 +39,35 @@ struct GradArgs {
 
 struct GradSmem {
   int list[WIN];
-  int warp_count[8];
+  int warp_count[16];
 };
-// the ring of Q, two buffers of P's parts [3][BR rows][R], the list; then the sums, [R][CB + 8] or [CB][R + 4]
+// the ring of Q and of P [BR rows][R] fp32, two buffers of P's parts [3][BR rows][R], the list; then the sums,
+// [R][CB + 8] or [CB][R + 4]
 __host__ __device__ constexpr uint32_t grad_p_bytes(int R) { return (uint32_t)(3 * BR * R * 2); }
+__host__ __device__ constexpr uint32_t grad_slot(int R) { return Q_BYTES + (uint32_t)(BR * R * 4); }
 __host__ __device__ constexpr uint32_t grad_bytes(int R) {
-  return GDEPTH * Q_BYTES + 2 * grad_p_bytes(R) + (uint32_t)sizeof(GradSmem);
+  return GDEPTH * grad_slot(R) + 2 * grad_p_bytes(R) + (uint32_t)sizeof(GradSmem);
 }
 
-template <int RT>
-__global__ void __launch_bounds__(GRAD_THREADS) lora_grad_kernel(const GradArgs p) {
+// RT: ranks of 16.  NG: groups of eight warps, each with all columns and its share of a batch's rows.
+template <int RT, int NG>
+__global__ void __launch_bounds__(256 * NG) lora_grad_kernel(const GradArgs p) {
   extern __shared__ __align__(128) uint8_t raw[];
-  constexpr int R = 16 * RT;
-  constexpr int PV = BR * R / GRAD_THREADS;            // values of P a thread splits per batch
-  constexpr uint32_t P_PART = (uint32_t)(BR * R * 2);
-  GradSmem& sm = *reinterpret_cast<GradSmem*>(raw + GDEPTH * Q_BYTES + 2 * grad_p_bytes(R));
+  constexpr int R = 16 * RT, GRAD_THREADS = 256 * NG, WARPS = 8 * NG;
+  constexpr int PC = BR * R / 4;                       // 16-byte chunks of a batch's P
+  constexpr uint32_t P_PART = (uint32_t)(BR * R * 2), SLOT = grad_slot(R), P_OFF = GDEPTH * SLOT;
+  GradSmem& sm = *reinterpret_cast<GradSmem*>(raw + P_OFF + 2 * grad_p_bytes(R));
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const int S = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
   const int block = (int)blockIdx.x / S, which = block >= p.blocks0;
   const int c0 = (which ? block - p.blocks0 : block) * CB;
-  const int a = (int)blockIdx.y;
+  const int a = (int)blockIdx.y, wc = warp & 7, wg = warp >> 3;
   const __nv_bfloat16* Q = which ? p.dy : p.x;
   const float* P = which ? p.u : p.t;
   const long long ld = which ? p.ldy : p.ldx;
   const int width = which ? p.N : p.K;
   const bool drop = which == 0 && p.drop.thr != 0u;
-  const uint32_t q0 = smem_u32(raw), p0 = q0 + GDEPTH * Q_BYTES;
+  const uint32_t q0 = smem_u32(raw), p0 = q0 + P_OFF;
   griddep_wait();
   griddep_launch_dependents();
   LoraKey key{0, 0};
@@ -97,7 +100,7 @@ __global__ void __launch_bounds__(GRAD_THREADS) lora_grad_kernel(const GradArgs 
       __syncthreads();
       int at = have + __popc(mask & ((1u << lane) - 1u));
 #pragma unroll
-      for (int w = 0; w < 8; ++w) {
+      for (int w = 0; w < WARPS; ++w) {
         const int c = sm.warp_count[w];
         if (w < warp) at += c;
         have += c;
@@ -106,74 +109,74 @@ __global__ void __launch_bounds__(GRAD_THREADS) lora_grad_kernel(const GradArgs 
       __syncthreads();
     }
     const int batches = (have + BR - 1) / BR;
-    // chunk i of a batch's Q: row (tid + 256 i) / 32, columns 8 (tid mod 32) ..
+    // chunk i of a batch's Q: row warp + WARPS i, columns 8 (tid mod 32) ..
     const int qc = tid & 31, col = c0 + 8 * qc;
-    auto load_q = [&](int b) {
+    // chunk tid + GRAD_THREADS i of its P: row / (R / 4), ranks 4 ..
+    auto load = [&](int b) {
       if (b < batches) {
-        const uint32_t dst = q0 + (uint32_t)(b & (GDEPTH - 1)) * Q_BYTES;
+        const uint32_t dst = q0 + (uint32_t)(b & (GDEPTH - 1)) * SLOT;
 #pragma unroll
-        for (int i = 0; i < BR / 8; ++i) {
-          const int row = (tid >> 5) + 8 * i;
+        for (int i = 0; i < BR / WARPS; ++i) {
+          const int row = warp + WARPS * i;
           const bool on = b * BR + row < have && col < width;
           cp_async16(dst + (uint32_t)(row * 512 + ((qc ^ (row & 7)) << 4)), on ? Q + (long long)sm.list[b * BR + row] * ld + col : Q, on);
+        }
+#pragma unroll
+        for (int i = 0; i * GRAD_THREADS < PC; ++i) {
+          const int e = tid + GRAD_THREADS * i, row = e / (R / 4), j = 4 * (e % (R / 4));
+          if (e >= PC) break;
+          const bool on = b * BR + row < have && j < p.r;
+          cp_async16(dst + Q_BYTES + (uint32_t)e * 16u, on ? P + (size_t)sm.list[b * BR + row] * p.r + j : P, on);
         }
       }
       cp_async_commit();
     };
-    // value i of a batch's P: pairs along the rank, (tid + 256 i) counts pairs
-    float2 pv[PV / 2];
-    auto load_p = [&](int b) {
+    // a thread splits the chunks of P that it copied itself
+    auto split_p = [&](int b) {
+      const uint8_t* src = raw + (uint32_t)(b & (GDEPTH - 1)) * SLOT + Q_BYTES;
+      uint8_t* dst = raw + P_OFF + (uint32_t)(b & 1) * grad_p_bytes(R);
 #pragma unroll
-      for (int i = 0; i < PV / 2; ++i) {
-        const int e = tid + GRAD_THREADS * i, row = e / (R / 2), j = 2 * (e % (R / 2));
-        pv[i] = make_float2(0.f, 0.f);
-        if (b * BR + row < have && j < p.r) pv[i] = __ldg(reinterpret_cast<const float2*>(P + (size_t)sm.list[b * BR + row] * p.r + j));
-      }
-    };
-    auto store_p = [&](int b) {
-      const uint32_t dst = (uint32_t)(b & 1) * grad_p_bytes(R);
-#pragma unroll
-      for (int i = 0; i < PV / 2; ++i) {
-        const int e = tid + GRAD_THREADS * i, row = e / (R / 2), j = 2 * (e % (R / 2));
-        float x = pv[i].x, y = pv[i].y;
+      for (int i = 0; i * GRAD_THREADS < PC; ++i) {
+        const int e = tid + GRAD_THREADS * i, row = e / (R / 4), j = 4 * (e % (R / 4));
+        if (e >= PC) break;
+        float4 v = *reinterpret_cast<const float4*>(src + (uint32_t)e * 16u);
 #pragma unroll
         for (int k = 0; k < 3; ++k) {
-          float hx, lx, hy, ly;
-          lora_split2(x, hx, lx);
-          lora_split2(y, hy, ly);
-          *reinterpret_cast<uint32_t*>(raw + GDEPTH * Q_BYTES + dst + k * P_PART + p_at(row, j >> 3) + (j & 7) * 2) = pack_bf16(hx, hy);
-          x = lx;
-          y = ly;
+          float h[4], l[4];
+          lora_split2(v.x, h[0], l[0]);
+          lora_split2(v.y, h[1], l[1]);
+          lora_split2(v.z, h[2], l[2]);
+          lora_split2(v.w, h[3], l[3]);
+          *reinterpret_cast<uint2*>(dst + k * P_PART + p_at(row, j >> 3) + (j & 4) * 2) = make_uint2(pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3]));
+          v = make_float4(l[0], l[1], l[2], l[3]);
         }
       }
     };
 #pragma unroll
-    for (int i = 0; i < GDEPTH - 1; ++i) load_q(i);
-    load_p(0);
+    for (int i = 0; i < GDEPTH - 1; ++i) load(i);
     for (int b = 0; b < batches; ++b) {
-      store_p(b);
       cp_async_wait<GDEPTH - 2>();
-      const uint32_t qb = q0 + (uint32_t)(b & (GDEPTH - 1)) * Q_BYTES;
+      split_p(b);
+      const uint32_t qb = q0 + (uint32_t)(b & (GDEPTH - 1)) * SLOT;
       if (drop) {
 #pragma unroll 2
-        for (int i = 0; i < BR / 8; ++i) {
-          const int row = (tid >> 5) + 8 * i;
+        for (int i = 0; i < BR / WARPS; ++i) {
+          const int row = warp + WARPS * i;
           if (b * BR + row >= have) break;
           uint4* q = reinterpret_cast<uint4*>(raw + (qb - q0) + row * 512 + ((qc ^ (row & 7)) << 4));
           *q = lora_dropped8(*q, (uint32_t)(col >> 3), (uint32_t)sm.list[b * BR + row], p.drop, key);
         }
       }
       __syncthreads();
-      load_q(b + GDEPTH - 1);
-      if (b + 1 < batches) load_p(b + 1);
+      load(b + GDEPTH - 1);
       const uint32_t pb = p0 + (uint32_t)(b & 1) * grad_p_bytes(R);
       const int steps = min(BR / 16, (have - b * BR + 15) / 16);
-      for (int ks = 0; ks < steps; ++ks) {
+      for (int ks = wg; ks < steps; ks += NG) {
         const int row = ks * 16 + (lane & 15);
         uint32_t bq[4][2];
 #pragma unroll
         for (int c = 0; c < 2; ++c) {      // 16 columns: (k 0-7, 8-15) of the first eight, then of the others
-          const int cc = warp * 4 + 2 * c + (lane >> 4);
+          const int cc = wc * 4 + 2 * c + (lane >> 4);
           ldsm_x4_t(qb + (uint32_t)(row * 512 + ((cc ^ (row & 7)) << 4)), bq[2 * c][0], bq[2 * c][1], bq[2 * c + 1][0], bq[2 * c + 1][1]);
         }
         // the rank's blocks: (ranks 0-7, k 0-7), (8-15, 0-7), (0-7, 8-15), (8-15, 8-15), stored with k along the rows
@@ -193,49 +196,65 @@ __global__ void __launch_bounds__(GRAD_THREADS) lora_grad_kernel(const GradArgs 
     __syncthreads();                       // the list and the ring are read
   }
 
+  // the groups' sums, one group after another
   float* red = reinterpret_cast<float*>(raw);
   constexpr int LA = CB + 8, LB = R + 4;
 #pragma unroll
-  for (int i = 0; i < RT; ++i)
+  for (int grp = 0; grp < NG; ++grp) {
+    if (wg == grp) {
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
+      for (int i = 0; i < RT; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int n = warp * 32 + c * 8 + 2 * t + (e & 1), j = 16 * i + g + 8 * (e >> 1);
-        red[which ? n * LB + j : j * LA + n] = acc[i][c][e];
-      }
-  __syncthreads();
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int n = wc * 32 + c * 8 + 2 * t + (e & 1), j = 16 * i + g + 8 * (e >> 1);
+            float& at = red[which ? n * LB + j : j * LA + n];
+            at = grp ? at + acc[i][c][e] : acc[i][c][e];
+          }
+    }
+    __syncthreads();
+  }
   __syncwarp();
   cluster_arrive();
   cluster_wait();
+  // four neighbouring columns (dA) or ranks (dB) a thread
   const uint32_t base = smem_u32(red);
-  const int e0 = CB * R * rank / S, e1 = CB * R * (rank + 1) / S;
-  float* out = which ? p.db : p.da;
+  const int e0 = CB * R / 4 * rank / S, e1 = CB * R / 4 * (rank + 1) / S;
   for (int e = e0 + tid; e < e1; e += GRAD_THREADS) {
-    const int n = which ? e / R : e % CB, j = which ? e % R : e / CB;
+    const int n = which ? e / (R / 4) : 4 * (e % (CB / 4)), j = which ? 4 * (e % (R / 4)) : e / (CB / 4);
     if (c0 + n >= width || j >= p.r) continue;
     const uint32_t at = base + 4u * (uint32_t)(which ? n * LB + j : j * LA + n);
-    const float s = dsmem_sum(at, S);
-    float* o = which ? out + ((size_t)a * width + c0 + n) * p.r + j : out + ((size_t)a * p.r + j) * width + c0 + n;
-    *o = p.accumulate ? *o + s : s;
+    float4 s = S > 1 ? dsmem_sum4(at, S) : *reinterpret_cast<const float4*>(red + (which ? n * LB + j : j * LA + n));
+    float4* o = reinterpret_cast<float4*>(which ? p.db + ((size_t)a * width + c0 + n) * p.r + j : p.da + ((size_t)a * p.r + j) * width + c0 + n);
+    if (p.accumulate) {
+      const float4 v = *o;
+      s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+    }
+    *o = s;
   }
   __syncwarp();
   cluster_arrive();
   cluster_wait();
 }
 
-template <int RT>
-cudaError_t launch_grad(const GradArgs& p, int blocks, int n, int splits, cudaStream_t stream) {
+template <int RT, int NG>
+cudaError_t launch_grad(const GradArgs& p, int blocks, int n, int num_sms, cudaStream_t stream) {
   static KernelLimits lim;
   constexpr int R = 16 * RT;
   size_t smem = grad_bytes(R);
   const size_t red = (size_t)(R * (CB + 8) > CB * (R + 4) ? R * (CB + 8) : CB * (R + 4)) * sizeof(float);
   if (smem < red) smem = red;
-  const cudaError_t e = ensure_kernel_limits((const void*)lora_grad_kernel<RT>, lim, smem, false);
+  const void* kern = (const void*)lora_grad_kernel<RT, NG>;
+  const cudaError_t e = ensure_kernel_limits(kern, lim, smem, false);
   if (e != cudaSuccess) return e;
+  // (as if every adapter had as many rows; a CTA costs about eight batches' time besides its own)
+  const int splits = pick_splits((long long)blocks * n, 1 + p.M / n / BR, 8, [&](int s) {
+    return resident_clusters(kern, lim, s == 8 ? 3 : s / 2, 256 * NG, smem, s, num_sms);
+  });
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(blocks * splits), (unsigned)n);
-  cfg.blockDim = dim3(GRAD_THREADS);
+  cfg.blockDim = dim3(256 * NG);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
@@ -247,7 +266,7 @@ cudaError_t launch_grad(const GradArgs& p, int blocks, int n, int splits, cudaSt
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, lora_grad_kernel<RT>, p);
+  return cudaLaunchKernelEx(&cfg, lora_grad_kernel<RT, NG>, p);
 }
 
 }  // namespace
@@ -267,13 +286,10 @@ cudaError_t launch_lora_grad(const LoraArgs& a, int num_sms, cudaStream_t stream
   p.drop = LoraDrop{a.seed, a.site, a.thr};
   const int blocks = p.blocks0 + (p.N + CB - 1) / CB;
   if (blocks == 0) return cudaSuccess;
-  // a split has at least four batches
-  int splits = 1;
-  while (splits < 8 && (long long)blocks * a.n * splits < num_sms && a.M >= 8 * BR * splits) splits *= 2;
-  if (a.r <= 16) return launch_grad<1>(p, blocks, a.n, splits, stream);
-  if (a.r <= 32) return launch_grad<2>(p, blocks, a.n, splits, stream);
-  if (a.r <= 64) return launch_grad<4>(p, blocks, a.n, splits, stream);
-  return launch_grad<8>(p, blocks, a.n, splits, stream);
+  if (a.r <= 16) return launch_grad<1, 2>(p, blocks, a.n, num_sms, stream);
+  if (a.r <= 32) return launch_grad<2, 2>(p, blocks, a.n, num_sms, stream);
+  if (a.r <= 64) return launch_grad<4, 2>(p, blocks, a.n, num_sms, stream);
+  return launch_grad<8, 1>(p, blocks, a.n, num_sms, stream);
 }
 
 }  // namespace cospec

@@ -66,6 +66,32 @@ __global__ void __launch_bounds__(LOW_THREADS) low_tile_kernel(const LowArgs p) 
   griddep_wait();
   griddep_launch_dependents();
 
+  const int chunks = (p.C + CK - 1) / CK;
+  const int c0 = (int)((long long)chunks * rank / S), c1 = (int)((long long)chunks * (rank + 1) / S);
+  const bool drop = p.drop.thr != 0u;
+  LoraKey key{0, 0};
+  if (drop) key = lora_key(p.drop);
+
+  // The thread's 16-byte chunk i of an x chunk: row tid / 8 + 32 i, columns 8 (tid mod 8) ..; its swizzled place in the
+  // 128-byte rows is the same for all i.  Items are walked with counters, without divisions.
+  const int xc = (int)threadIdx.x & 7, xr = (int)threadIdx.x >> 3;
+  const uint32_t xs = (uint32_t)(xr * 128 + ((xc ^ (xr & 7)) << 4));
+  const __nv_bfloat16* xp = p.x + (long long)(m0 + xr) * p.ldx + (long long)c0 * CK + 8 * xc;
+  const int x_rows = min(rows, p.M - m0);                // rows of the tile that exist
+  auto load_x = [&](int ci) {
+    const uint32_t dst = x_off + (uint32_t)((ci & (DEPTH - 1)) * rows * 128) + xs;
+    const bool kin = (c0 + ci) * CK + 8 * xc < p.C;
+    const __nv_bfloat16* src = xp + ci * CK;
+#pragma unroll 4
+    for (int i = 0; 32 * i + xr < rows; ++i) {
+      const bool on = kin && 32 * i + xr < x_rows;
+      cp_async16(dst + (uint32_t)(i * 4096), on ? src + (long long)(32 * i) * p.ldx : p.x, on);
+    }
+  };
+  // the first chunks set out before the tile's adapters are known
+  const int early = min(DEPTH - 1, c1 - c0);
+  for (int i = 0; i < early; ++i) load_x(i);
+
   // the adapters of the tile, in the order of their first rows
   if (threadIdx.x < LOW_MAX_ROWS) {
     const int m = m0 + (int)threadIdx.x;
@@ -97,33 +123,13 @@ __global__ void __launch_bounds__(LOW_THREADS) low_tile_kernel(const LowArgs p) 
   const int count = sm.warp_count[0] + sm.warp_count[1] + sm.warp_count[2] + sm.warp_count[3];
   __syncthreads();
 
-  const int chunks = (p.C + CK - 1) / CK;
-  const int c0 = (int)((long long)chunks * rank / S), c1 = (int)((long long)chunks * (rank + 1) / S);
   const int items = (c1 - c0) * count;
-  const bool drop = p.drop.thr != 0u;
-  LoraKey key{0, 0};
-  if (drop) key = lora_key(p.drop);
-
-  // The thread's 16-byte chunk i of an x chunk: row tid / 8 + 32 i, columns 8 (tid mod 8) ..; its swizzled place in the
-  // 128-byte rows is the same for all i.  Items are walked with counters, without divisions.
-  const int xc = (int)threadIdx.x & 7, xr = (int)threadIdx.x >> 3;
-  const uint32_t xs = (uint32_t)(xr * 128 + ((xc ^ (xr & 7)) << 4));
-  const __nv_bfloat16* xp = p.x + (long long)(m0 + xr) * p.ldx + (long long)c0 * CK + 8 * xc;
-  const int x_rows = min(rows, p.M - m0);                // rows of the tile that exist
   int l_ci = 0, l_ai = 0, l_item = 0;                    // the next item to load
   auto load = [&]() {
     if (l_item < items) {
       const int k0 = (c0 + l_ci) * CK;
       const bool kin = k0 + 8 * xc < p.C;
-      if (l_ai == 0) {
-        const uint32_t dst = x_off + (uint32_t)((l_ci & (DEPTH - 1)) * rows * 128) + xs;
-        const __nv_bfloat16* src = xp + l_ci * CK;
-#pragma unroll 4
-        for (int i = 0; 32 * i + xr < rows; ++i) {
-          const bool on = kin && 32 * i + xr < x_rows;
-          cp_async16(dst + (uint32_t)(i * 4096), on ? src + (long long)(32 * i) * p.ldx : p.x, on);
-        }
-      }
+      if (l_ai == 0 && l_ci >= early) load_x(l_ci);
       const __nv_bfloat16* f = p.f + (size_t)sm.adapters[l_ai] * p.r * p.C;
       const uint32_t dst = f_off + (uint32_t)((l_item & (DEPTH - 1)) * R * 128);
       if (!RM) {                           // [rank][64]
@@ -154,7 +160,18 @@ __global__ void __launch_bounds__(LOW_THREADS) low_tile_kernel(const LowArgs p) 
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
   const int id0 = sm.ids[rw * 16 + g], id1 = sm.ids[rw * 16 + g + 8];
-  const int lr = lane & 15, lc = lane >> 4;         // ldmatrix: the lane's row and 16-byte column of a 16 x 16 block
+  // ldmatrix: the lane's row and 16-byte column of a 16 x 16 block; the swizzled places are the first block's, others differ by an
+  // exclusive or
+  const int lr = lane & 15, lc = lane >> 4;
+  const uint32_t xa = (uint32_t)((rw * 16 + lr) * 128 + ((lc ^ (lr & 7)) << 4));
+  uint32_t fa;
+  if (!RM) {
+    const int fr = (lane & 7) + ((lane >> 4) << 3);
+    fa = (uint32_t)(fr * 128 + ((((lane >> 3) & 1) ^ (fr & 7)) << 4));
+  } else {
+    const int sw = NT >= 8 ? lr & 7 : NT == 4 ? (lr >> 1) & 3 : (lr >> 2) & 1;
+    fa = (uint32_t)(lr * (R * 2) + ((lc ^ sw) << 4));
+  }
 
 #pragma unroll
   for (int i = 0; i < DEPTH - 1; ++i) load();
@@ -176,22 +193,20 @@ __global__ void __launch_bounds__(LOW_THREADS) low_tile_kernel(const LowArgs p) 
     const int a = sm.adapters[ai];
     const bool on0 = id0 == a, on1 = id1 == a;
     if (!__any_sync(0xffffffffu, on0 || on1)) continue;
-    for (int ks = kw; ks < CK / 16; ks += KW) {
+#pragma unroll
+    for (int ks = 0; ks < CK / 16; ++ks) {
+      if ((ks & (KW - 1)) != kw) continue;
       uint32_t q[4];
-      const int row = rw * 16 + lr;
-      ldsm_x4(xb + (uint32_t)(row * 128 + (((2 * ks + lc) ^ (row & 7)) << 4)), q[0], q[1], q[2], q[3]);
+      ldsm_x4(xb + (xa ^ (uint32_t)(ks << 5)), q[0], q[1], q[2], q[3]);
       q[0] = on0 ? q[0] : 0u, q[2] = on0 ? q[2] : 0u;
       q[1] = on1 ? q[1] : 0u, q[3] = on1 ? q[3] : 0u;
 #pragma unroll
       for (int i = 0; i < NT; i += 2) {
         uint32_t b[4];
         if (!RM) {                         // (ranks 8 i .. + 7, k 0-7), (same, k 8-15), (the next 8 ranks, ..)
-          const int fr = i * 8 + (lane & 7) + ((lane >> 4) << 3), fc = 2 * ks + ((lane >> 3) & 1);
-          ldsm_x4(fb + (uint32_t)(fr * 128 + ((fc ^ (fr & 7)) << 4)), b[0], b[1], b[2], b[3]);
+          ldsm_x4(fb + (uint32_t)(i * 1024) + (fa ^ (uint32_t)(ks << 5)), b[0], b[1], b[2], b[3]);
         } else {
-          const int fr = ks * 16 + lr, fc = i + lc;
-          const int sw = NT >= 8 ? fr & 7 : NT == 4 ? (fr >> 1) & 3 : (fr >> 2) & 1;
-          ldsm_x4_t(fb + (uint32_t)(fr * (R * 2) + ((fc ^ sw) << 4)), b[0], b[1], b[2], b[3]);
+          ldsm_x4_t(fb + (uint32_t)(ks * 16 * R * 2) + (fa ^ (uint32_t)(i << 4)), b[0], b[1], b[2], b[3]);
         }
         mma_16816(acc[i], q, b[0], b[1]);
         mma_16816(acc[i + 1], q, b[2], b[3]);
@@ -318,14 +333,19 @@ __global__ void __launch_bounds__(ROW_THREADS) low_row_kernel(const LowArgs p) {
 }
 
 template <int NT, bool RM>
-cudaError_t launch_low_tile(const LowArgs& p, int tiles, int splits, cudaStream_t stream) {
+cudaError_t launch_low_tile(const LowArgs& p, int tiles, int num_sms, cudaStream_t stream) {
   static KernelLimits lim;
   const int rows = 16 << p.rw_log2;
   size_t smem = low_bytes(rows, NT * 8);
   const size_t red = (size_t)8 * 16 * (NT * 8 + 4) * sizeof(float);
   if (smem < red) smem = red;
-  const cudaError_t e = ensure_kernel_limits((const void*)low_tile_kernel<NT, RM>, lim, smem, false);
+  const void* kern = (const void*)low_tile_kernel<NT, RM>;
+  const cudaError_t e = ensure_kernel_limits(kern, lim, smem, false);
   if (e != cudaSuccess) return e;
+  // (a CTA costs about ten chunks' time besides its chunks)
+  const int splits = pick_splits(tiles, (p.C + CK - 1) / CK, 10, [&](int s) {
+    return resident_clusters(kern, lim, 4 * p.rw_log2 - 4 + (s == 8 ? 3 : s / 2), LOW_THREADS, smem, s, num_sms);
+  });
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * splits));
   cfg.blockDim = dim3(LOW_THREADS);
@@ -348,17 +368,14 @@ cudaError_t launch_low(LowArgs p, int num_sms, cudaStream_t stream) {
   if ((long long)p.M * p.r <= LOW_ROW_MAX)
     return launch_pdl(low_row_kernel<RM>, dim3((unsigned)p.M), dim3(ROW_THREADS), 0, stream, p);
   // 128 rows a CTA share an adapter's factor; fewer where that leaves SMs without work
-  const int chunks = (p.C + CK - 1) / CK;
   p.rw_log2 = 3;
   while (p.rw_log2 > 1 && (p.M + (16 << p.rw_log2) - 1) / (16 << p.rw_log2) * 8 < num_sms) --p.rw_log2;
   const int tiles = (p.M + (16 << p.rw_log2) - 1) / (16 << p.rw_log2);
-  int splits = 1;
-  while (splits < 8 && tiles * splits < 2 * num_sms && chunks >= 4 * splits) splits *= 2;
   const int nt = (p.r + 7) / 8;
-  if (nt <= 2) return launch_low_tile<2, RM>(p, tiles, splits, stream);
-  if (nt <= 4) return launch_low_tile<4, RM>(p, tiles, splits, stream);
-  if (nt <= 8) return launch_low_tile<8, RM>(p, tiles, splits, stream);
-  return launch_low_tile<16, RM>(p, tiles, splits, stream);
+  if (nt <= 2) return launch_low_tile<2, RM>(p, tiles, num_sms, stream);
+  if (nt <= 4) return launch_low_tile<4, RM>(p, tiles, num_sms, stream);
+  if (nt <= 8) return launch_low_tile<8, RM>(p, tiles, num_sms, stream);
+  return launch_low_tile<16, RM>(p, tiles, num_sms, stream);
 }
 
 }  // namespace
