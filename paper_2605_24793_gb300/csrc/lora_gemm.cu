@@ -59,45 +59,57 @@ struct TileList {
   int ids[MAX_NT];             // of the rows: -1 none
   int adapter[MAX_NT];
   int span[MAX_NT];            // first | last << 16
-  int warp_count[4];
+  int warp_count[8];
   int count;
 };
 
-// By 128 threads (t = 0 .. 127, named barrier `bar`).  Every row is compared with every other one.
-CS_DEV void build_list(TileList& L, const GemmArgs& p, int row0, int t, int bar) {
+// Where the rows meet by their adapters: open addressing, twice as many places as rows.
+constexpr int HASH = 512;
+struct ListScratch {
+  int key[HASH], first[HASH], last[HASH];
+};
+
+// By 128 threads (t = 0 .. 127, named barrier `bar`).  Which place an adapter takes depends on the order of the threads, its
+// first and last row and so the list do not.  (Every row against every other one took 5 us for 256 rows.)
+CS_DEV void build_list(TileList& L, ListScratch& H, const GemmArgs& p, int row0, int t, int bar) {
   const int rows = min(p.nt, p.M - row0);
+  for (int i = t; i < HASH; i += 128) H.key[i] = -1, H.first[i] = MAX_NT, H.last[i] = -1;
   for (int i = t; i < p.nt; i += 128) L.ids[i] = i < rows ? lora_adapter(p.adapter, row0 + i, p.n, p.err) : -1;
   named_bar_sync(bar, 128);
-  int done = 0;
-  for (int i0 = 0; i0 < p.nt; i0 += 128) {
-    const int i = i0 + t;
-    const int id = i < p.nt ? L.ids[i] : -1;
-    bool first = id >= 0;
-    int last = i;
-    for (int j = 0; j < p.nt; j += 4) {
-      const int4 v = *reinterpret_cast<const int4*>(&L.ids[j]);
-      const int w[4] = {v.x, v.y, v.z, v.w};
+  int place[2] = {-1, -1};
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (w[e] == id) {
-          first = first && j + e >= i;
-          last = max(last, j + e);
-        }
+  for (int q = 0; q < 2; ++q) {
+    const int i = t + 128 * q, id = i < p.nt ? L.ids[i] : -1;
+    if (id < 0) continue;
+    int h = (int)(((uint32_t)id * 2654435761u) >> 23);            // 9 bits
+    while (true) {
+      const int was = atomicCAS(&H.key[h], -1, id);
+      if (was == -1 || was == id) break;
+      h = (h + 1) & (HASH - 1);
     }
+    atomicMin(&H.first[h], i);
+    atomicMax(&H.last[h], i);
+    place[q] = h;
+  }
+  named_bar_sync(bar, 128);
+  int done = 0;
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const int i = t + 128 * q, h = place[q];
+    const bool first = h >= 0 && H.first[h] == i;
     const unsigned mask = __ballot_sync(0xffffffffu, first);
-    if ((t & 31) == 0) L.warp_count[t >> 5] = __popc(mask);
+    if ((t & 31) == 0) L.warp_count[4 * q + (t >> 5)] = __popc(mask);
     named_bar_sync(bar, 128);
     int at = done + __popc(mask & ((1u << (t & 31)) - 1u));
     for (int w = 0; w < 4; ++w) {
-      const int c = L.warp_count[w];
+      const int c = L.warp_count[4 * q + w];
       if (w < (t >> 5)) at += c;
       done += c;
     }
     if (first) {
-      L.adapter[at] = id;
-      L.span[at] = i | last << 16;
+      L.adapter[at] = L.ids[i];
+      L.span[at] = i | H.last[h] << 16;
     }
-    named_bar_sync(bar, 128);
   }
   if (t == 0) L.count = done;
 }
@@ -160,7 +172,7 @@ __host__ __device__ inline TileSmem tile_layout(int stages, int nt) {
   TileSmem L;
   L.b_off = (uint32_t)stages * A_BYTES;
   L.list_off = L.b_off + (uint32_t)stages * nt * 128;
-  L.bar_off = L.list_off + (uint32_t)((sizeof(TileList) + 15) / 16 * 16);
+  L.bar_off = L.list_off + (uint32_t)((sizeof(TileList) + 15) / 16 * 16) + (uint32_t)sizeof(ListScratch);
   L.total = L.bar_off + (uint32_t)(3 * stages + 2) * 8 + 16;
   return L;
 }
@@ -366,7 +378,7 @@ __global__ void __launch_bounds__(256, 1)
     umma_commit_on(on, done);
   } else if (warp >= 4) {
     const int t = tid - 128;
-    build_list(list, p, row0, t, 1);
+    build_list(list, *reinterpret_cast<ListScratch*>(smem + L.list_off + (sizeof(TileList) + 15) / 16 * 16), p, row0, t, 1);
     __syncwarp();
     if (lane == 0) mbar_arrive(lready);
     named_bar_sync(1, 128);
@@ -543,7 +555,7 @@ __host__ __device__ inline PairSmem pair_layout(int stages, int nt) {
   PairSmem L;
   L.b_off = (uint32_t)stages * A_BYTES;
   L.list_off = L.b_off + (uint32_t)stages * (nt / 2) * 128;
-  L.bar_off = L.list_off + 2 * (uint32_t)((sizeof(TileList) + 15) / 16 * 16);
+  L.bar_off = L.list_off + 2 * (uint32_t)((sizeof(TileList) + 15) / 16 * 16) + (uint32_t)sizeof(ListScratch);
   L.total = L.bar_off + (uint32_t)(4 * stages + 9) * 8 + 16;
   return L;
 }
@@ -761,7 +773,7 @@ __global__ void __launch_bounds__(P_THREADS, 1)
       if (t == 0) list.count = *abort_flag ? -1 : 0;        // one thread's reading decides for all four warps
       named_bar_sync(1, 128);
       if (list.count < 0) break;
-      build_list(list, p, row0, t, 1);
+      build_list(list, *reinterpret_cast<ListScratch*>(smem + L.list_off + 2 * LIST_BYTES), p, row0, t, 1);
       __syncwarp();
       if (lane == 0) mbar_arrive(&lready[it & 1]);
       named_bar_sync(1, 128);
