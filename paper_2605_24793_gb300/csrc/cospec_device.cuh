@@ -532,6 +532,33 @@ CS_DEV void tma_load_4d_pair(uint32_t dst, const void* map, uint32_t bar_cluster
       : "memory");
 }
 
+// Loads and arrivals issued by a whole, converged warp, of which one thread (`on`) acts: from one diverged thread a load took
+// about 300 cycles, since its operands have to become uniform first.
+CS_DEV void tma_load_3d_on(uint32_t on, uint32_t dst, const void* map, uint32_t bar, int x, int y, int z, uint64_t policy) {
+  asm volatile(
+      "{\n .reg .pred q;\n setp.ne.b32 q, %7, 0;\n"
+      " @q cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0], [%1, {%3, %4, %5}], [%2], %6;\n}\n" ::"r"(dst),
+      "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "l"(policy), "r"(on)
+      : "memory");
+}
+CS_DEV void tma_load_3d_pair_on(uint32_t on, uint32_t dst, const void* map, uint32_t bar_cluster, int x, int y, int z, uint64_t policy) {
+  asm volatile(
+      "{\n .reg .pred q;\n setp.ne.b32 q, %7, 0;\n"
+      " @q cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0], [%1, {%3, %4, %5}], [%2], %6;\n}\n" ::"r"(dst),
+      "l"(map), "r"(bar_cluster), "r"(x), "r"(y), "r"(z), "l"(policy), "r"(on)
+      : "memory");
+}
+CS_DEV void mbar_arrive_expect_tx_on(uint32_t on, uint32_t bar, uint32_t bytes) {
+  asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %2, 0;\n @q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n}\n" ::"r"(bar),
+               "r"(bytes), "r"(on)
+               : "memory");
+}
+CS_DEV void mbar_arrive_on(uint32_t on, uint32_t bar) {
+  asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n @q mbarrier.arrive.shared::cta.b64 _, [%0];\n}\n" ::"r"(bar), "r"(on) : "memory");
+}
+
 // Two 32-bit operations in one instruction, each rounded as by itself.
 CS_DEV float2 fma2(float2 a, float2 b, float2 c) {
   float2 d;

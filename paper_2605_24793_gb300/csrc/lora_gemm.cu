@@ -197,7 +197,8 @@ CS_DEV bool wait_count(const int* p, int v) {
   }
 }
 
-// Warps: 0 loads W and the factors, 1 issues the MMAs, 2 loads the rows, 3 allocates TMEM, 4 to 7 list the
+// Warps: 0 and 3 load W and the factors, half each (a warp's copies are done one after another, 16 KB in 0.26 us: with one
+// warp that was the least time of a stage), 1 issues the MMAs, 2 loads the rows, 3 allocates TMEM, 4 to 7 list the
 // tile's adapters, write the u operand and read the accumulators.
 template <bool MN, bool DROP>
 __global__ void __launch_bounds__(256, 1)
@@ -227,7 +228,7 @@ __global__ void __launch_bounds__(256, 1)
 
   if (tid == 0) {
     for (int s = 0; s < p.stages; ++s) {
-      mbar_init(&full[s], 2);
+      mbar_init(&full[s], 3);
       mbar_init(&empty[s], 1);
       mbar_init(&ufull[s], 1);
     }
@@ -257,72 +258,72 @@ __global__ void __launch_bounds__(256, 1)
     return steps > rank ? (steps - rank + S - 1) / S : 0;
   };
   bool ok = true;
-  if (warp == 0 || warp == 2) {
-    if (lane == 0) {
-      const bool is_w = warp == 0;
-      // W is read again by the other row tiles, if there are any
-      const uint64_t pol = !is_w ? l2_policy_evict_last() : gridDim.y > 1 ? l2_policy_evict_normal() : l2_policy_evict_first();
-      const uint32_t a_buf = smem_u32(smem), b_buf = smem_u32(smem + L.b_off);
-      int li = 0, st = 0;
-      uint32_t ph = 0;
-      auto turn = [&]() {                  // the next stage, free (turns are counted: a division costs a hundred cycles)
-        if (li >= p.stages && (!mbar_wait(&empty[st], ph ^ 1u, WAIT_NS) || *abort_flag)) return -1;
-        const int s = st;
-        ++li;
-        if (++st == p.stages) st = 0, ph ^= 1u;
-        return s;
-      };
-      for (int i = 0; i < nk; ++i) {
-        const int s = turn(), x = (kb0 + i) * BK;
+  if (warp == 0 || warp == 2 || warp == 3) {
+    // (the whole warp walks along; one elected thread acts)
+    const uint32_t on = elect_one();
+    const bool is_w = warp != 2;
+    const int part = warp == 3;
+    // W is read again by the other row tiles, if there are any
+    const uint64_t pol = !is_w ? l2_policy_evict_last() : gridDim.y > 1 ? l2_policy_evict_normal() : l2_policy_evict_first();
+    const uint32_t a_buf = smem_u32(smem) + (uint32_t)part * (A_BYTES / 2), b_buf = smem_u32(smem + L.b_off), full0 = smem_u32(full);
+    const int f = f0 + 64 * part;
+    int li = 0, st = 0;
+    uint32_t ph = 0;
+    auto turn = [&]() {                    // the next stage, free (turns are counted: a division costs a hundred cycles)
+      if (li >= p.stages && (!__all_sync(0xffffffffu, mbar_wait(&empty[st], ph ^ 1u, WAIT_NS)) || *abort_flag)) return -1;
+      const int s = st;
+      ++li;
+      if (++st == p.stages) st = 0, ph ^= 1u;
+      return s;
+    };
+    for (int i = 0; i < nk; ++i) {
+      const int s = turn(), x = (kb0 + i) * BK;
+      if (s < 0) {
+        ok = false;
+        break;
+      }
+      const uint32_t bar = full0 + (uint32_t)s * 8u;
+      mbar_arrive_expect_tx_on(on, bar, is_w ? (uint32_t)A_BYTES / 2 : b_bytes);
+      if (is_w)
+        tma_load_3d_on(on, a_buf + (uint32_t)(s * A_BYTES), &tmap_w, bar, MN ? f : x, MN ? x : f, 0, pol);
+      else
+        tma_load_3d_on(on, b_buf + (uint32_t)s * b_bytes, &tmap_x, bar, x, row0, 0, pol);
+    }
+    if (ok) ok = __all_sync(0xffffffffu, mbar_wait(lready, 0, WAIT_NS)) && !*abort_flag;
+    if (ok) {
+      const int units = list.count * upe, n = my_steps();
+      for (int i = 0; i < n; ++i) {
+        const int s = turn();
         if (s < 0) {
           ok = false;
           break;
         }
-        mbar_arrive_expect_tx(&full[s], is_w ? (uint32_t)A_BYTES : b_bytes);
-        if (!is_w) {
-          tma_load_3d(b_buf + (uint32_t)s * b_bytes, &tmap_x, &full[s], x, row0, 0, pol);
-        } else if (!MN) {
-          tma_load_3d(a_buf + (uint32_t)s * A_BYTES, &tmap_w, &full[s], x, f0, 0, pol);
+        const uint32_t bar = full0 + (uint32_t)s * 8u;
+        const int u = (rank + i * S) * STEP_UNITS + part;      // the second producer loads the step's second unit
+        // (a count, not a barrier's parity: the writers pass over stages' turns that are not theirs)
+        if (warp == 0 && on) st_release_cta(ugo, i + 1);
+        if (!is_w || u >= units) {
+          mbar_arrive_on(on, bar);
         } else {
-          tma_load_3d(a_buf + (uint32_t)s * A_BYTES, &tmap_w, &full[s], f0, x, 0, pol);
-          tma_load_3d(a_buf + (uint32_t)s * A_BYTES + A_BYTES / 2, &tmap_w, &full[s], f0 + 64, x, 0, pol);
-        }
-      }
-      if (ok) ok = mbar_wait_idle(lready, 0, WAIT_NS) && !*abort_flag;
-      if (ok) {
-        const int units = list.count * upe, n = my_steps();
-        for (int i = 0; i < n; ++i) {
-          const int s = turn();
-          if (s < 0) {
-            ok = false;
-            break;
-          }
-          if (!is_w) {
-            mbar_arrive(&full[s]);
+          mbar_arrive_expect_tx_on(on, bar, (uint32_t)UNIT_BYTES);
+          const int e = list.adapter[u / upe], j0 = (u % upe) * UNIT;
+          const uint32_t dst = smem_u32(smem) + (uint32_t)(s * A_BYTES + part * UNIT_BYTES);
+          if (!MN) {
+            tma_load_3d_on(on, dst, &tmap_f, bar, j0, f0, e, pol);
           } else {
-            const int u0 = (rank + i * S) * STEP_UNITS, nu = min(STEP_UNITS, units - u0);
-            // (a count, not a barrier's parity: the writers pass over stages' turns that are not theirs)
-            st_release_cta(ugo, i + 1);
-            mbar_arrive_expect_tx(&full[s], (uint32_t)nu * UNIT_BYTES);
-            for (int q = 0; q < nu; ++q) {
-              const int e = (u0 + q) / upe, j0 = ((u0 + q) % upe) * UNIT;
-              const uint32_t dst = a_buf + (uint32_t)s * A_BYTES + (uint32_t)q * UNIT_BYTES;
-              if (!MN) {
-                tma_load_3d(dst, &tmap_f, &full[s], j0, f0, list.adapter[e], pol);
-              } else {
-                tma_load_3d(dst, &tmap_f, &full[s], f0, j0, list.adapter[e], pol);
-                tma_load_3d(dst + UNIT_BYTES / 2, &tmap_f, &full[s], f0 + 64, j0, list.adapter[e], pol);
-              }
-            }
+            tma_load_3d_on(on, dst, &tmap_f, bar, f0, j0, e, pol);
+            tma_load_3d_on(on, dst + UNIT_BYTES / 2, &tmap_f, bar, f0 + 64, j0, e, pol);
           }
         }
       }
-      if (!ok) {
+    }
+    if (!ok) {
+      if (on) {
         set_err(p.err, ERR_TIMEOUT);
         *abort_flag = 1;
-        // what was issued lands before the shared memory is given back
-        for (int l = li > p.stages ? li - p.stages : 0; l < li; ++l) mbar_wait(&full[l % p.stages], (uint32_t)(l / p.stages) & 1u, WAIT_NS);
       }
+      // what was issued lands before the shared memory is given back
+      for (int l = li > p.stages ? li - p.stages : 0; l < li; ++l) mbar_wait(&full[l % p.stages], (uint32_t)(l / p.stages) & 1u, WAIT_NS);
     }
   } else if (warp == 1) {
     const uint32_t on = elect_one();
@@ -545,7 +546,8 @@ constexpr int PBM = 2 * BM;              // features of a pair's tile
 constexpr int P_EPI = 8;                 // epilogue warps, two per TMEM lane quarter
 constexpr int P_XW = 2 + P_EPI;          // producer of the rows
 constexpr int P_UW = P_XW + 1;           // first of the four warps of the u operand
-constexpr int P_THREADS = 32 * (P_UW + 4);
+constexpr int P_W2 = P_UW + 4;           // second producer of W
+constexpr int P_THREADS = 32 * (P_W2 + 1);
 constexpr int P_CHUNKS = MAX_NT / 64;    // 32-row chunks of an epilogue warp
 
 struct PairSmem {
@@ -561,7 +563,7 @@ __host__ __device__ inline PairSmem pair_layout(int stages, int nt) {
 }
 
 // Persistent pairs of CTAs (cta_group::2) walk tiles of 256 features x nt rows: each CTA loads its 128 features and
-// half of the rows, so an SM takes in 32 KB per 64 of the contraction.  Warps: 0 loads W and the factors, 10 the rows,
+// half of the rows, so an SM takes in 32 KB per 64 of the contraction.  Warps: 0 and 15 load W and the factors, half each, 10 the rows,
 // 1 of the leader issues the MMAs, 2 to 9 round finished accumulators while the next tile is multiplied, 11 to 14
 // list the tile's adapters and write the CTA's half of the u operand, one tile ahead of the MMAs.  With dropout
 // the two accumulators of a tile fill TMEM, so the epilogue is not overlapped; its mask is drawn before.
@@ -597,14 +599,14 @@ __global__ void __launch_bounds__(P_THREADS, 1)
 
   if (tid == 0) {
     for (int s = 0; s < p.stages; ++s) {
-      mbar_init(&full[s], 2);              // (leader) its two producers
+      mbar_init(&full[s], 3);              // (leader) its three producers
       mbar_init(&empty[s], 1);
       mbar_init(&ufull[s], 8);             // (leader) four warps of each CTA
       mbar_init(&ugo[s], 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&lready[i], 4);
-      mbar_init(&lfree[i], 2 + (rank == 0 ? 1 : 0) + (DROP ? P_EPI : 0));
+      mbar_init(&lfree[i], 3 + (rank == 0 ? 1 : 0) + (DROP ? P_EPI : 0));
       mbar_init(&tfull[i], 1);
       mbar_init(&tempty[i], 2 * P_EPI);    // (leader) the epilogue warps of both CTAs
     }
@@ -624,82 +626,82 @@ __global__ void __launch_bounds__(P_THREADS, 1)
   const uint32_t tmem = *tmem_holder;
   bool ok = true;
 
-  if (warp == 0 || warp == P_XW) {
-    if (lane == 0) {
-      const bool is_w = warp == 0;
-      const uint64_t pol = l2_policy_evict_normal();
-      const uint32_t a_buf = smem_u32(smem), b_buf = smem_u32(smem + L.b_off);
-      const uint32_t full0 = dsmem_map(smem_u32(full), 0);
-      int li = 0, st = 0;
-      uint32_t ph = 0;
-      // the next stage, free: the turns are counted (a division per turn, twice in the chain from one stage to the next, cost
-      // 82 -> 107 us at 4096 rows 2560 -> 6144)
-      auto turn = [&]() {
-        if (li >= p.stages && (!mbar_wait(&empty[st], ph ^ 1u, WAIT_NS) || *abort_flag)) return -1;
-        const int s = st;
-        ++li;
-        if (++st == p.stages) st = 0, ph ^= 1u;
-        return s;
-      };
-      int it = 0;
-      for (int tile = pair; tile < tiles && ok; tile += pairs, ++it) {
-        const int f0 = (tile % ftiles) * PBM + rank * BM, row0 = (tile / ftiles) * p.nt + rank * half;
-        for (int kb = 0; kb < kblocks; ++kb) {
-          const int s = turn(), x = kb * BK;
-          if (s < 0) {
-            ok = false;
-            break;
-          }
-          if (rank == 0) mbar_arrive_expect_tx(&full[s], 2 * (is_w ? (uint32_t)A_BYTES : b_bytes));
-          const uint32_t bar = full0 + (uint32_t)s * 8u;
-          if (!is_w) {
-            tma_load_3d_pair(b_buf + (uint32_t)s * b_bytes, &tmap_x, bar, x, row0, 0, pol);
-          } else if (!MN) {
-            tma_load_3d_pair(a_buf + (uint32_t)s * A_BYTES, &tmap_w, bar, x, f0, 0, pol);
-          } else {
-            tma_load_3d_pair(a_buf + (uint32_t)s * A_BYTES, &tmap_w, bar, f0, x, 0, pol);
-            tma_load_3d_pair(a_buf + (uint32_t)s * A_BYTES + A_BYTES / 2, &tmap_w, bar, f0 + 64, x, 0, pol);
-          }
+  if (warp == 0 || warp == P_W2 || warp == P_XW) {
+    // (the whole warp walks along; one elected thread acts)
+    const uint32_t on = elect_one(), lead = rank == 0 ? on : 0u;
+    const bool is_w = warp != P_XW;
+    const int part = warp == P_W2;
+    const uint64_t pol = l2_policy_evict_normal();
+    const uint32_t a_buf = smem_u32(smem) + (uint32_t)part * (A_BYTES / 2), b_buf = smem_u32(smem + L.b_off);
+    const uint32_t full0 = dsmem_map(smem_u32(full), 0), own0 = smem_u32(full);
+    int li = 0, st = 0;
+    uint32_t ph = 0;
+    // the next stage, free: the turns are counted (a division per turn, twice in the chain from one stage to the next, cost
+    // 82 -> 107 us at 4096 rows 2560 -> 6144)
+    auto turn = [&]() {
+      if (li >= p.stages && (!__all_sync(0xffffffffu, mbar_wait(&empty[st], ph ^ 1u, WAIT_NS)) || *abort_flag)) return -1;
+      const int s = st;
+      ++li;
+      if (++st == p.stages) st = 0, ph ^= 1u;
+      return s;
+    };
+    int it = 0;
+    for (int tile = pair; tile < tiles && ok; tile += pairs, ++it) {
+      const int f0 = (tile % ftiles) * PBM + rank * BM, f = f0 + 64 * part, row0 = (tile / ftiles) * p.nt + rank * half;
+      for (int kb = 0; kb < kblocks; ++kb) {
+        const int s = turn(), x = kb * BK;
+        if (s < 0) {
+          ok = false;
+          break;
         }
-        if (ok) ok = mbar_wait(&lready[it & 1], (uint32_t)(it >> 1) & 1u, WAIT_NS) && !*abort_flag;
-        if (!ok) break;
-        const TileList& list = list_of(it);
-        const int units = list.count * upe, steps = (units + STEP_UNITS - 1) / STEP_UNITS;
-        for (int i = 0; i < steps; ++i) {
-          const int s = turn();
-          if (s < 0) {
-            ok = false;
-            break;
-          }
-          if (!is_w) {
-            if (rank == 0) mbar_arrive(&full[s]);
-            continue;
-          }
-          const int nu = min(STEP_UNITS, units - i * STEP_UNITS);
-          mbar_arrive(&ugo[s]);
-          if (rank == 0) mbar_arrive_expect_tx(&full[s], 2 * (uint32_t)nu * UNIT_BYTES);
-          const uint32_t bar = full0 + (uint32_t)s * 8u;
-          for (int q = 0; q < nu; ++q) {
-            const int u = i * STEP_UNITS + q, e = list.adapter[u / upe], j0 = (u % upe) * UNIT;
-            const uint32_t dst = a_buf + (uint32_t)s * A_BYTES + (uint32_t)q * UNIT_BYTES;
-            if (!MN) {
-              tma_load_3d_pair(dst, &tmap_f, bar, j0, f0, e, pol);
-            } else {
-              tma_load_3d_pair(dst, &tmap_f, bar, f0, j0, e, pol);
-              tma_load_3d_pair(dst + UNIT_BYTES / 2, &tmap_f, bar, f0 + 64, j0, e, pol);
-            }
-          }
-        }
-        if (ok) mbar_arrive(&lfree[it & 1]);
+        const uint32_t bar = full0 + (uint32_t)s * 8u;
+        mbar_arrive_expect_tx_on(lead, own0 + (uint32_t)s * 8u, is_w ? (uint32_t)A_BYTES : 2 * b_bytes);
+        if (is_w)
+          tma_load_3d_pair_on(on, a_buf + (uint32_t)(s * A_BYTES), &tmap_w, bar, MN ? f : x, MN ? x : f, 0, pol);
+        else
+          tma_load_3d_pair_on(on, b_buf + (uint32_t)s * b_bytes, &tmap_x, bar, x, row0, 0, pol);
       }
-      if (!ok) {
+      if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&lready[it & 1], (uint32_t)(it >> 1) & 1u, WAIT_NS)) && !*abort_flag;
+      if (!ok) break;
+      const TileList& list = list_of(it);
+      const int units = list.count * upe, steps = (units + STEP_UNITS - 1) / STEP_UNITS;
+      for (int i = 0; i < steps; ++i) {
+        const int s = turn();
+        if (s < 0) {
+          ok = false;
+          break;
+        }
+        const uint32_t bar = full0 + (uint32_t)s * 8u, own = own0 + (uint32_t)s * 8u;
+        const int u = i * STEP_UNITS + part;                   // the second producer loads the step's second unit
+        if (warp == 0) mbar_arrive_on(on, smem_u32(&ugo[s]));
+        if (!is_w || u >= units) {
+          mbar_arrive_on(lead, own);
+        } else {
+          mbar_arrive_expect_tx_on(lead, own, 2 * (uint32_t)UNIT_BYTES);
+          const int e = list.adapter[u / upe], j0 = (u % upe) * UNIT;
+          const uint32_t dst = smem_u32(smem) + (uint32_t)(s * A_BYTES + part * UNIT_BYTES);
+          if (!MN) {
+            tma_load_3d_pair_on(on, dst, &tmap_f, bar, j0, f0, e, pol);
+          } else {
+            tma_load_3d_pair_on(on, dst, &tmap_f, bar, f0, j0, e, pol);
+            tma_load_3d_pair_on(on, dst + UNIT_BYTES / 2, &tmap_f, bar, f0 + 64, j0, e, pol);
+          }
+        }
+      }
+      if (ok) {
+        __syncwarp();                      // every lane has read the list
+        mbar_arrive_on(on, smem_u32(&lfree[it & 1]));
+      }
+    }
+    if (!ok) {
+      if (on) {
         set_err(p.err, ERR_TIMEOUT);
         *abort_flag = 1;
-        // what was issued lands before the shared memory is given back (the peer's copies are counted on the leader's
-        // barriers, and both CTAs stay until the leader is through)
-        if (rank == 0)
-          for (int l = li > p.stages ? li - p.stages : 0; l < li; ++l) mbar_wait(&full[l % p.stages], (uint32_t)(l / p.stages) & 1u, WAIT_NS);
       }
+      // what was issued lands before the shared memory is given back (the peer's copies are counted on the leader's
+      // barriers, and both CTAs stay until the leader is through)
+      if (rank == 0)
+        for (int l = li > p.stages ? li - p.stages : 0; l < li; ++l) mbar_wait(&full[l % p.stages], (uint32_t)(l / p.stages) & 1u, WAIT_NS);
     }
   } else if (warp == 1) {
     if (rank == 0) {
@@ -757,7 +759,7 @@ __global__ void __launch_bounds__(P_THREADS, 1)
       }
       umma_commit_pair_on(on, done, 3);
     }
-  } else if (warp >= P_UW) {
+  } else if (warp >= P_UW && warp < P_W2) {
     const int t = tid - P_UW * 32;
     const uint32_t ufull0 = dsmem_map(smem_u32(ufull), 0);
     int st = 0, it = 0;
@@ -951,7 +953,7 @@ cudaError_t launch_lora_gemm(const LoraArgs& a, bool backward, int num_sms, int*
 
   CUtensorMap w, x, f;
   const uint64_t wd[3] = {(uint64_t)a.K, (uint64_t)a.N, 1}, ws[2] = {(uint64_t)a.K * 2, (uint64_t)a.K * a.N * 2};
-  const uint32_t wb[3] = {64, backward ? 64u : (uint32_t)BM, 1};
+  const uint32_t wb[3] = {64, 64, 1};
   const uint64_t xd[3] = {(uint64_t)p.C, (uint64_t)p.M, 1};
   const uint64_t ldx = (uint64_t)(backward ? a.ldy : a.ldx), xs[2] = {ldx * 2, ldx * 2 * (uint64_t)p.M};
   const uint32_t xb[3] = {64, (uint32_t)(pairs ? p.nt / 2 : p.nt), 1};
