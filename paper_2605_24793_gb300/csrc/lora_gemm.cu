@@ -22,11 +22,12 @@ namespace cospec {
 namespace {
 
 constexpr int BM = 128;                  // features of a tile
-constexpr int BK = 64;                   // contraction of a stage
-constexpr int A_BYTES = BM * BK * 2;
+constexpr int BK = 128;                  // contraction of a stage: two boxes of 64
+constexpr int A_BYTES = BM * 64 * 2;     // a box of the features' operand
+constexpr int A_STAGE = 2 * A_BYTES;
 constexpr int UNIT = 16;                 // ranks of a unit
 constexpr int UNIT_BYTES = BM * UNIT * 2;
-constexpr int STEP_UNITS = 2;            // units of an adapter step: 64 columns of hi and lo
+constexpr int STEP_UNITS = 4;            // units of an adapter step: two boxes' 64 columns of hi and lo
 constexpr int MAX_NT = 256;
 constexpr uint64_t WAIT_NS = 2000000000ull;
 
@@ -170,8 +171,8 @@ struct TileSmem {
 };
 __host__ __device__ inline TileSmem tile_layout(int stages, int nt) {
   TileSmem L;
-  L.b_off = (uint32_t)stages * A_BYTES;
-  L.list_off = L.b_off + (uint32_t)stages * nt * 128;
+  L.b_off = (uint32_t)stages * A_STAGE;
+  L.list_off = L.b_off + (uint32_t)stages * nt * 256;
   L.bar_off = L.list_off + (uint32_t)((sizeof(TileList) + 15) / 16 * 16) + (uint32_t)sizeof(ListScratch);
   L.total = L.bar_off + (uint32_t)(3 * stages + 2) * 8 + 16;
   return L;
@@ -224,7 +225,7 @@ __global__ void __launch_bounds__(256, 1)
   const int kblocks = (p.C + BK - 1) / BK;
   const int kb0 = (int)((long long)kblocks * rank / S), nk = (int)((long long)kblocks * (rank + 1) / S) - kb0;
   const int upe = (p.r + UNIT - 1) / UNIT;           // units of an adapter
-  const uint32_t b_bytes = (uint32_t)p.nt * 128u;
+  const uint32_t b_bytes = (uint32_t)p.nt * 128u, b_stage = 2 * b_bytes;
 
   if (tid == 0) {
     for (int s = 0; s < p.stages; ++s) {
@@ -265,8 +266,7 @@ __global__ void __launch_bounds__(256, 1)
     const int part = warp == 3;
     // W is read again by the other row tiles, if there are any
     const uint64_t pol = !is_w ? l2_policy_evict_last() : gridDim.y > 1 ? l2_policy_evict_normal() : l2_policy_evict_first();
-    const uint32_t a_buf = smem_u32(smem) + (uint32_t)part * (A_BYTES / 2), b_buf = smem_u32(smem + L.b_off), full0 = smem_u32(full);
-    const int f = f0 + 64 * part;
+    const uint32_t a_buf = smem_u32(smem) + (uint32_t)part * A_BYTES, b_buf = smem_u32(smem + L.b_off), full0 = smem_u32(full);
     int li = 0, st = 0;
     uint32_t ph = 0;
     auto turn = [&]() {                    // the next stage, free (turns are counted: a division costs a hundred cycles)
@@ -283,11 +283,17 @@ __global__ void __launch_bounds__(256, 1)
         break;
       }
       const uint32_t bar = full0 + (uint32_t)s * 8u;
-      mbar_arrive_expect_tx_on(on, bar, is_w ? (uint32_t)A_BYTES / 2 : b_bytes);
-      if (is_w)
-        tma_load_3d_on(on, a_buf + (uint32_t)(s * A_BYTES), &tmap_w, bar, MN ? f : x, MN ? x : f, 0, pol);
-      else
-        tma_load_3d_on(on, b_buf + (uint32_t)s * b_bytes, &tmap_x, bar, x, row0, 0, pol);
+      const uint32_t dst = a_buf + (uint32_t)(s * A_STAGE);
+      mbar_arrive_expect_tx_on(on, bar, is_w ? (uint32_t)A_BYTES : b_stage);
+      if (!is_w) {
+        tma_load_3d_on(on, b_buf + (uint32_t)s * b_stage, &tmap_x, bar, x, row0, 0, pol);
+        tma_load_3d_on(on, b_buf + (uint32_t)s * b_stage + b_bytes, &tmap_x, bar, x + 64, row0, 0, pol);
+      } else if (!MN) {
+        tma_load_3d_on(on, dst, &tmap_w, bar, x + 64 * part, f0, 0, pol);
+      } else {
+        tma_load_3d_on(on, dst, &tmap_w, bar, f0, x + 64 * part, 0, pol);
+        tma_load_3d_on(on, dst + A_BYTES / 2, &tmap_w, bar, f0 + 64, x + 64 * part, 0, pol);
+      }
     }
     if (ok) ok = __all_sync(0xffffffffu, mbar_wait(lready, 0, WAIT_NS)) && !*abort_flag;
     if (ok) {
@@ -299,15 +305,15 @@ __global__ void __launch_bounds__(256, 1)
           break;
         }
         const uint32_t bar = full0 + (uint32_t)s * 8u;
-        const int u = (rank + i * S) * STEP_UNITS + part;      // the second producer loads the step's second unit
+        const int u0 = (rank + i * S) * STEP_UNITS, nu = min(STEP_UNITS, units - u0);      // the second producer loads the odd units
         // (a count, not a barrier's parity: the writers pass over stages' turns that are not theirs)
         if (warp == 0 && on) st_release_cta(ugo, i + 1);
-        if (!is_w || u >= units) {
-          mbar_arrive_on(on, bar);
-        } else {
-          mbar_arrive_expect_tx_on(on, bar, (uint32_t)UNIT_BYTES);
-          const int e = list.adapter[u / upe], j0 = (u % upe) * UNIT;
-          const uint32_t dst = smem_u32(smem) + (uint32_t)(s * A_BYTES + part * UNIT_BYTES);
+        const int mine = is_w ? (nu + 1 - part) >> 1 : 0;
+        if (mine == 0) mbar_arrive_on(on, bar);
+        else mbar_arrive_expect_tx_on(on, bar, (uint32_t)(mine * UNIT_BYTES));
+        for (int q = part; q < 2 * mine; q += 2) {
+          const int e = list.adapter[(u0 + q) / upe], j0 = ((u0 + q) % upe) * UNIT;
+          const uint32_t dst = smem_u32(smem) + (uint32_t)(s * A_STAGE + q * UNIT_BYTES);
           if (!MN) {
             tma_load_3d_on(on, dst, &tmap_f, bar, j0, f0, e, pol);
           } else {
@@ -340,10 +346,11 @@ __global__ void __launch_bounds__(256, 1)
       if (!ok) break;
       if (++st == p.stages) st = 0, ph ^= 1u;
       tc_fence_after();
-      const uint64_t a = a_desc + (uint64_t)(s * (A_BYTES >> 4)), b = b_desc + (uint64_t)((uint32_t)s * (b_bytes >> 4));
+      const uint64_t a = a_desc + (uint64_t)(s * (A_STAGE >> 4)), b = b_desc + (uint64_t)((uint32_t)s * (b_stage >> 4));
 #pragma unroll
       for (int k = 0; k < BK / 16; ++k)
-        umma_bf16_on(on, tmem, a + (uint64_t)(MN ? k * 128 : k * 2), b + (uint64_t)(k * 2), idesc, (i | k) != 0 ? 1u : 0u);
+        umma_bf16_on(on, tmem, a + (uint64_t)((k >> 2) * (A_BYTES >> 4) + (k & 3) * (MN ? 128 : 2)),
+                     b + (uint64_t)((uint32_t)(k >> 2) * (b_bytes >> 4) + (uint32_t)(k & 3) * 2), idesc, (i | k) != 0 ? 1u : 0u);
       umma_commit_on(on, &empty[s]);
     }
     if (ok) ok = __all_sync(0xffffffffu, mbar_wait_idle(lready, 0, WAIT_NS)) && !*abort_flag;
@@ -364,8 +371,8 @@ __global__ void __launch_bounds__(256, 1)
           const bool all = DROP && i == 0 && q == 0;
           const int lo = all ? 0 : (span & 0xffff) & ~15, hi = all ? p.nt : ((span >> 16) | 15) + 1;
           const uint32_t id = idesc_bf16_f32(BM, hi - lo) | A_MN;
-          const uint64_t a = f_desc + (uint64_t)((s * A_BYTES + q * UNIT_BYTES) >> 4);
-          const uint64_t b = b_desc + (uint64_t)(((uint32_t)s * b_bytes + (uint32_t)lo * 128u) >> 4) + (uint64_t)(q * 4);
+          const uint64_t a = f_desc + (uint64_t)((s * A_STAGE + q * UNIT_BYTES) >> 4);
+          const uint64_t b = b_desc + (uint64_t)(((uint32_t)s * b_stage + (uint32_t)(q >> 1) * b_bytes + (uint32_t)lo * 128u) >> 4) + (uint64_t)((q & 1) * 4);
           umma_bf16_on(on, d2 + (uint32_t)lo, a, b, id, all ? 0u : 1u);
           umma_bf16_on(on, d2 + (uint32_t)lo, a, b + 2, id, 1u);
         }
@@ -394,7 +401,7 @@ __global__ void __launch_bounds__(256, 1)
         ok = false;
         break;
       }
-      uint8_t* tile = smem + L.b_off + (uint32_t)s * b_bytes;
+      uint8_t* tile = smem + L.b_off + (uint32_t)s * b_stage;
       const int u0 = (rank + i * S) * STEP_UNITS, nu = min(STEP_UNITS, units - u0);
       for (int q = 0; q < nu; ++q) {
         const int e = (u0 + q) / upe, j0 = ((u0 + q) % upe) * UNIT;
@@ -404,7 +411,7 @@ __global__ void __launch_bounds__(256, 1)
         for (int row = lo + lane; row < hi; row += 32) {
           uint4 w[4];
           unit_row(w, p.u + (size_t)(row0 + row) * p.r, list.ids[row] == id, j0, p.r);
-          store_unit_row(tile, row, q, w);
+          store_unit_row(tile + (q >> 1) * b_bytes, row, q & 1, w);
         }
       }
       fence_proxy_async_smem();
@@ -475,7 +482,7 @@ cudaError_t launch_tile(const CUtensorMap& w, const CUtensorMap& x, const CUtens
   const cudaError_t e = ensure_kernel_limits((const void*)lora_tile_kernel<MN, DROP>, lim, 227 * 1024, false);
   if (e != cudaSuccess) return e;
   // The split with the least blocks of the contraction one after another: waves of resident clusters, each a split's
-  // share and what a CTA costs besides (about eight blocks' time).
+  // share and what a CTA costs besides (about four stages' time).
   const int tiles = (p.F + BM - 1) / BM * ((p.M + p.nt - 1) / p.nt), kblocks = (p.C + BK - 1) / BK;
   int splits = 1;
   long long best = 0;
@@ -543,6 +550,10 @@ CS_DEV bool mbar_wait_pair(uint64_t* bar, uint32_t parity) {
 }
 
 constexpr int PBM = 2 * BM;              // features of a pair's tile
+// Boxes of 64 of the contraction in a stage.  A stage costs its warps about 480 cycles of waits, arrivals and issue, and its MMAs
+// two cycles a row and box: up to 160 rows a stage has two boxes (848 rows 2560 -> 6144 34 -> 31 us), above that one, which
+// makes six stages of the ring instead of three (8192 rows 5120 -> 8192 417 -> 394 us; at 192 rows, 4096 rows 6144 -> 2560, 90 -> 81).
+constexpr int PAIR_TWO_BOXES = 160;
 constexpr int P_EPI = 8;                 // epilogue warps, two per TMEM lane quarter
 constexpr int P_XW = 2 + P_EPI;          // producer of the rows
 constexpr int P_UW = P_XW + 1;           // first of the four warps of the u operand
@@ -553,10 +564,10 @@ constexpr int P_CHUNKS = MAX_NT / 64;    // 32-row chunks of an epilogue warp
 struct PairSmem {
   uint32_t b_off, list_off, bar_off, total;
 };
-__host__ __device__ inline PairSmem pair_layout(int stages, int nt) {
+__host__ __device__ inline PairSmem pair_layout(int stages, int nt, int sub) {
   PairSmem L;
-  L.b_off = (uint32_t)stages * A_BYTES;
-  L.list_off = L.b_off + (uint32_t)stages * (nt / 2) * 128;
+  L.b_off = (uint32_t)(stages * sub) * A_BYTES;
+  L.list_off = L.b_off + (uint32_t)(stages * sub) * (nt / 2) * 128;
   L.bar_off = L.list_off + 2 * (uint32_t)((sizeof(TileList) + 15) / 16 * 16) + (uint32_t)sizeof(ListScratch);
   L.total = L.bar_off + (uint32_t)(4 * stages + 9) * 8 + 16;
   return L;
@@ -567,14 +578,15 @@ __host__ __device__ inline PairSmem pair_layout(int stages, int nt) {
 // 1 of the leader issues the MMAs, 2 to 9 round finished accumulators while the next tile is multiplied, 11 to 14
 // list the tile's adapters and write the CTA's half of the u operand, one tile ahead of the MMAs.  With dropout
 // the two accumulators of a tile fill TMEM, so the epilogue is not overlapped; its mask is drawn before.
-template <bool MN, bool DROP>
+template <bool MN, bool DROP, int SUB>
 __global__ void __launch_bounds__(P_THREADS, 1)
     lora_pair_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x,
                      const __grid_constant__ CUtensorMap tmap_f, const GemmArgs p) {
-  constexpr int NACC = DROP ? 1 : 2;
+  constexpr int NACC = DROP ? 1 : 2, PBK = 64 * SUB, PU = 2 * SUB;       // units of an adapter step
+  constexpr uint32_t P_STAGE = (uint32_t)SUB * A_BYTES;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  const PairSmem L = pair_layout(p.stages, p.nt);
+  const PairSmem L = pair_layout(p.stages, p.nt, SUB);
   constexpr uint32_t LIST_BYTES = (uint32_t)((sizeof(TileList) + 15) / 16 * 16);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L.bar_off);
   uint64_t* empty = full + p.stages;
@@ -592,10 +604,10 @@ __global__ void __launch_bounds__(P_THREADS, 1)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = (int)cluster_ctarank();
   const int pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
-  const int kblocks = (p.C + BK - 1) / BK, upe = (p.r + UNIT - 1) / UNIT;
+  const int kblocks = (p.C + PBK - 1) / PBK, upe = (p.r + UNIT - 1) / UNIT;
   const int ftiles = (p.F + PBM - 1) / PBM, tiles = ftiles * ((p.M + p.nt - 1) / p.nt);
   const int half = p.nt / 2;
-  const uint32_t b_bytes = (uint32_t)half * 128u;
+  const uint32_t b_bytes = (uint32_t)half * 128u, b_stage = (uint32_t)SUB * b_bytes;
 
   if (tid == 0) {
     for (int s = 0; s < p.stages; ++s) {
@@ -632,7 +644,7 @@ __global__ void __launch_bounds__(P_THREADS, 1)
     const bool is_w = warp != P_XW;
     const int part = warp == P_W2;
     const uint64_t pol = l2_policy_evict_normal();
-    const uint32_t a_buf = smem_u32(smem) + (uint32_t)part * (A_BYTES / 2), b_buf = smem_u32(smem + L.b_off);
+    const uint32_t a_buf = smem_u32(smem) + (uint32_t)part * (P_STAGE / 2), b_buf = smem_u32(smem + L.b_off);
     const uint32_t full0 = dsmem_map(smem_u32(full), 0), own0 = smem_u32(full);
     int li = 0, st = 0;
     uint32_t ph = 0;
@@ -647,24 +659,33 @@ __global__ void __launch_bounds__(P_THREADS, 1)
     };
     int it = 0;
     for (int tile = pair; tile < tiles && ok; tile += pairs, ++it) {
-      const int f0 = (tile % ftiles) * PBM + rank * BM, f = f0 + 64 * part, row0 = (tile / ftiles) * p.nt + rank * half;
+      const int f0 = (tile % ftiles) * PBM + rank * BM, row0 = (tile / ftiles) * p.nt + rank * half;
       for (int kb = 0; kb < kblocks; ++kb) {
-        const int s = turn(), x = kb * BK;
+        const int s = turn(), x = kb * PBK;
         if (s < 0) {
           ok = false;
           break;
         }
         const uint32_t bar = full0 + (uint32_t)s * 8u;
-        mbar_arrive_expect_tx_on(lead, own0 + (uint32_t)s * 8u, is_w ? (uint32_t)A_BYTES : 2 * b_bytes);
-        if (is_w)
-          tma_load_3d_pair_on(on, a_buf + (uint32_t)(s * A_BYTES), &tmap_w, bar, MN ? f : x, MN ? x : f, 0, pol);
-        else
-          tma_load_3d_pair_on(on, b_buf + (uint32_t)s * b_bytes, &tmap_x, bar, x, row0, 0, pol);
+        const uint32_t dst = a_buf + (uint32_t)s * P_STAGE, xdst = b_buf + (uint32_t)s * b_stage;
+        mbar_arrive_expect_tx_on(lead, own0 + (uint32_t)s * 8u, is_w ? P_STAGE : 2 * b_stage);
+        if (!is_w) {
+          tma_load_3d_pair_on(on, xdst, &tmap_x, bar, x, row0, 0, pol);
+          if (SUB == 2) tma_load_3d_pair_on(on, xdst + b_bytes, &tmap_x, bar, x + 64, row0, 0, pol);
+        } else if (SUB == 1) {             // each producer: 64 of the features
+          const int f = f0 + 64 * part;
+          tma_load_3d_pair_on(on, dst, &tmap_w, bar, MN ? f : x, MN ? x : f, 0, pol);
+        } else if (!MN) {                  // each producer: a box of the contraction
+          tma_load_3d_pair_on(on, dst, &tmap_w, bar, x + 64 * part, f0, 0, pol);
+        } else {
+          tma_load_3d_pair_on(on, dst, &tmap_w, bar, f0, x + 64 * part, 0, pol);
+          tma_load_3d_pair_on(on, dst + A_BYTES / 2, &tmap_w, bar, f0 + 64, x + 64 * part, 0, pol);
+        }
       }
       if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&lready[it & 1], (uint32_t)(it >> 1) & 1u, WAIT_NS)) && !*abort_flag;
       if (!ok) break;
       const TileList& list = list_of(it);
-      const int units = list.count * upe, steps = (units + STEP_UNITS - 1) / STEP_UNITS;
+      const int units = list.count * upe, steps = (units + PU - 1) / PU;
       for (int i = 0; i < steps; ++i) {
         const int s = turn();
         if (s < 0) {
@@ -672,14 +693,13 @@ __global__ void __launch_bounds__(P_THREADS, 1)
           break;
         }
         const uint32_t bar = full0 + (uint32_t)s * 8u, own = own0 + (uint32_t)s * 8u;
-        const int u = i * STEP_UNITS + part;                   // the second producer loads the step's second unit
+        const int nu = min(PU, units - i * PU), mine = is_w ? (nu + 1 - part) >> 1 : 0;      // the second producer's: the odd units
         if (warp == 0) mbar_arrive_on(on, smem_u32(&ugo[s]));
-        if (!is_w || u >= units) {
-          mbar_arrive_on(lead, own);
-        } else {
-          mbar_arrive_expect_tx_on(lead, own, 2 * (uint32_t)UNIT_BYTES);
-          const int e = list.adapter[u / upe], j0 = (u % upe) * UNIT;
-          const uint32_t dst = smem_u32(smem) + (uint32_t)(s * A_BYTES + part * UNIT_BYTES);
+        if (mine == 0) mbar_arrive_on(lead, own);
+        else mbar_arrive_expect_tx_on(lead, own, (uint32_t)(2 * mine * UNIT_BYTES));
+        for (int q = part; q < 2 * mine; q += 2) {
+          const int u = i * PU + q, e = list.adapter[u / upe], j0 = (u % upe) * UNIT;
+          const uint32_t dst = smem_u32(smem) + (uint32_t)s * P_STAGE + (uint32_t)(q * UNIT_BYTES);
           if (!MN) {
             tma_load_3d_pair_on(on, dst, &tmap_f, bar, j0, f0, e, pol);
           } else {
@@ -725,13 +745,14 @@ __global__ void __launch_bounds__(P_THREADS, 1)
           if (!ok) break;
           if (++st == p.stages) st = 0, ph ^= 1u;
           tc_fence_after();
-          pair_k64<MN ? 128 : 2>(on, d, a_desc + (uint64_t)(s * (A_BYTES >> 4)), b_desc + (uint64_t)((uint32_t)s * (b_bytes >> 4)), idesc,
-                                 kb != 0 ? 1u : 0u);
+          const uint64_t a = a_desc + (uint64_t)((uint32_t)s * (P_STAGE >> 4)), b = b_desc + (uint64_t)((uint32_t)s * (b_stage >> 4));
+          pair_k64<MN ? 128 : 2>(on, d, a, b, idesc, kb != 0 ? 1u : 0u);
+          if (SUB == 2) pair_k64<MN ? 128 : 2>(on, d, a + (uint64_t)(A_BYTES >> 4), b + (uint64_t)(b_bytes >> 4), idesc, 1u);
           umma_commit_pair_on(on, &empty[s], 3);
         }
         if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&lready[it & 1], (uint32_t)(it >> 1) & 1u, WAIT_NS)) && !*abort_flag;
         if (!ok) break;
-        const int units = list_of(it).count * upe, steps = (units + STEP_UNITS - 1) / STEP_UNITS;
+        const int units = list_of(it).count * upe, steps = (units + PU - 1) / PU;
         __syncwarp();
         if (lane == 0) mbar_arrive(&lfree[it & 1]);
         for (int i = 0; i < steps; ++i) {
@@ -741,10 +762,10 @@ __global__ void __launch_bounds__(P_THREADS, 1)
           if (++st == p.stages) st = 0, ph ^= 1u;
           uphase ^= 1u << s;
           tc_fence_after();
-          const int nu = min(STEP_UNITS, units - i * STEP_UNITS);
+          const int nu = min(PU, units - i * PU);
           for (int q = 0; q < nu; ++q) {
-            const uint64_t a = f_desc + (uint64_t)((s * A_BYTES + q * UNIT_BYTES) >> 4);
-            const uint64_t b = b_desc + (uint64_t)((uint32_t)s * (b_bytes >> 4)) + (uint64_t)(q * 4);
+            const uint64_t a = f_desc + (uint64_t)(((uint32_t)s * P_STAGE + (uint32_t)(q * UNIT_BYTES)) >> 4);
+            const uint64_t b = b_desc + (uint64_t)(((uint32_t)s * b_stage + (uint32_t)(q >> 1) * b_bytes) >> 4) + (uint64_t)((q & 1) * 4);
             pair_mma(on, d2, a, b, idesc, DROP && i == 0 && q == 0 ? 0u : 1u);
             pair_mma(on, d2, a, b + 2, idesc, 1u);
           }
@@ -779,25 +800,34 @@ __global__ void __launch_bounds__(P_THREADS, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(&lready[it & 1]);
       named_bar_sync(1, 128);
-      const int units = list.count * upe, steps = (units + STEP_UNITS - 1) / STEP_UNITS;
+      const int units = list.count * upe, steps = (units + PU - 1) / PU;
       st = (st + kblocks) % p.stages;
       for (int i = 0; i < steps; ++i) {
         const int s = st;
         if (++st == p.stages) st = 0;
-        // u is read before the stage is free
-        const int nu = min(STEP_UNITS, units - i * STEP_UNITS), row = min(rank * half + t, p.nt - 1);
-        uint4 w[STEP_UNITS][4];
-#pragma unroll
-        for (int q = 0; q < STEP_UNITS; ++q) {
-          const int u = i * STEP_UNITS + min(q, nu - 1), id = list.adapter[u / upe];
-          unit_row(w[q], p.u + (size_t)(row0 + row) * p.r, list.ids[row] == id, (u % upe) * UNIT, p.r);
-        }
-        ok = __all_sync(0xffffffffu, mbar_wait_idle(&ugo[s], (gphase >> s) & 1u, WAIT_NS, 500u)) && !*abort_flag;
+        // u of two units is read before the stage is free
+        const int nu = min(PU, units - i * PU), row = min(rank * half + t, p.nt - 1);
+        uint4 w[2][4];
+        auto read = [&](int q, uint4 (&v)[4]) {
+          const int u = i * PU + min(q, nu - 1), id = list.adapter[u / upe];
+          unit_row(v, p.u + (size_t)(row0 + row) * p.r, list.ids[row] == id, (u % upe) * UNIT, p.r);
+        };
+        read(0, w[0]);
+        read(1, w[1]);
+        ok = __all_sync(0xffffffffu, mbar_wait_idle(&ugo[s], (gphase >> s) & 1u, WAIT_NS, 100u)) && !*abort_flag;
         if (!ok) break;
         gphase ^= 1u << s;
-        uint8_t* buf = smem + L.b_off + (uint32_t)s * b_bytes;
-        if (t < half)
-          for (int q = 0; q < nu; ++q) store_unit_row(buf, t, q, w[q]);
+        uint8_t* buf = smem + L.b_off + (uint32_t)s * b_stage;
+        if (t < half) {
+          store_unit_row(buf, t, 0, w[0]);
+          if (nu > 1) store_unit_row(buf, t, 1, w[1]);
+          if (PU == 4 && nu > 2) {
+            read(2, w[0]);
+            read(3, w[1]);
+            store_unit_row(buf + b_bytes, t, 0, w[0]);
+            if (nu > 3) store_unit_row(buf + b_bytes, t, 1, w[1]);
+          }
+        }
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(ufull0 + (uint32_t)s * 8u);
@@ -883,11 +913,11 @@ __global__ void __launch_bounds__(P_THREADS, 1)
   }
 }
 
-template <bool MN, bool DROP>
+template <bool MN, bool DROP, int SUB>
 cudaError_t launch_pair(const CUtensorMap& w, const CUtensorMap& x, const CUtensorMap& f, GemmArgs p, int pairs, cudaStream_t stream) {
   static KernelLimits lim;
-  const size_t smem = pair_layout(p.stages, p.nt).total + 1024;
-  const cudaError_t e = ensure_kernel_limits((const void*)lora_pair_kernel<MN, DROP>, lim, 227 * 1024, false);
+  const size_t smem = pair_layout(p.stages, p.nt, SUB).total + 1024;
+  const cudaError_t e = ensure_kernel_limits((const void*)lora_pair_kernel<MN, DROP, SUB>, lim, 227 * 1024, false);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(2 * pairs));
@@ -903,7 +933,7 @@ cudaError_t launch_pair(const CUtensorMap& w, const CUtensorMap& x, const CUtens
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, lora_pair_kernel<MN, DROP>, w, x, f, p);
+  return cudaLaunchKernelEx(&cfg, lora_pair_kernel<MN, DROP, SUB>, w, x, f, p);
 }
 
 }  // namespace
@@ -924,28 +954,29 @@ cudaError_t launch_lora_gemm(const LoraArgs& a, bool backward, int num_sms, int*
   const bool drop = p.drop.thr != 0u;
   const int kblocks = (p.C + BK - 1) / BK;
   // Above 256 rows a CTA pair's tiles, of the size that leaves the fewest pairs idle: a tile takes the bytes of its
-  // operands (its rows and 256 features) and about eight blocks' time besides.
+  // operands (its rows and 256 features) and about four stages' time besides.
   const bool pairs = p.M > MAX_NT;
-  int grid = 0;
+  int grid = 0, sub = 2;
   if (pairs) {
     const int all = num_sms / 2, ftiles = (p.F + PBM - 1) / PBM;
     long long best = 0;
     for (int nt = MAX_NT; nt >= 64; nt -= 32) {
-      const long long t = (long long)ftiles * ((p.M + nt - 1) / nt), cost = (t + all - 1) / all * (nt + 256 + 4096 / kblocks);
+      const long long t = (long long)ftiles * ((p.M + nt - 1) / nt), cost = (t + all - 1) / all * (nt + 256 + 2048 / kblocks);
       if (best == 0 || cost < best) {
         best = cost;
         p.nt = nt;
         grid = t < all ? (int)t : all;
       }
     }
-    p.stages = (int)((226u * 1024u - pair_layout(0, p.nt).total) / (A_BYTES + (uint32_t)p.nt * 64u + 32u));
-    if (p.stages > 10) p.stages = 10;
+    sub = p.nt <= PAIR_TWO_BOXES ? 2 : 1;
+    p.stages = (int)((226u * 1024u - pair_layout(0, p.nt, sub).total) / ((uint32_t)sub * (A_BYTES + (uint32_t)p.nt * 64u) + 32u));
+    if (p.stages > 6) p.stages = 6;
   } else {
     // one row tile, or equal parts of at most 256
     const int row_tiles = (p.M + MAX_NT - 1) / MAX_NT;
     p.nt = ((p.M + row_tiles - 1) / row_tiles + 15) / 16 * 16;
-    p.stages = (int)((226u * 1024u - tile_layout(0, p.nt).total) / (A_BYTES + (uint32_t)p.nt * 128u + 32u));
-    if (p.stages > 12) p.stages = 12;
+    p.stages = (int)((226u * 1024u - tile_layout(0, p.nt).total) / (A_STAGE + (uint32_t)p.nt * 256u + 32u));
+    if (p.stages > 6) p.stages = 6;
   }
   const int cols = p.nt * (drop || pairs ? 2 : 1);
   p.tmem_cols = 32;
@@ -953,7 +984,7 @@ cudaError_t launch_lora_gemm(const LoraArgs& a, bool backward, int num_sms, int*
 
   CUtensorMap w, x, f;
   const uint64_t wd[3] = {(uint64_t)a.K, (uint64_t)a.N, 1}, ws[2] = {(uint64_t)a.K * 2, (uint64_t)a.K * a.N * 2};
-  const uint32_t wb[3] = {64, 64, 1};
+  const uint32_t wb[3] = {64, backward || sub == 1 ? 64u : (uint32_t)BM, 1};
   const uint64_t xd[3] = {(uint64_t)p.C, (uint64_t)p.M, 1};
   const uint64_t ldx = (uint64_t)(backward ? a.ldy : a.ldx), xs[2] = {ldx * 2, ldx * 2 * (uint64_t)p.M};
   const uint32_t xb[3] = {64, (uint32_t)(pairs ? p.nt / 2 : p.nt), 1};
@@ -964,9 +995,9 @@ cudaError_t launch_lora_gemm(const LoraArgs& a, bool backward, int num_sms, int*
       !encode_tensor_map_bf16(&f, backward ? a.a : a.b, 3, fd, fs, fb, backward ? 128 : 32))
     return cudaErrorInvalidValue;
   if (pairs) {
-    if (!backward) return launch_pair<false, false>(w, x, f, p, grid, stream);
-    if (drop) return launch_pair<true, true>(w, x, f, p, grid, stream);
-    return launch_pair<true, false>(w, x, f, p, grid, stream);
+    if (!backward) return sub == 2 ? launch_pair<false, false, 2>(w, x, f, p, grid, stream) : launch_pair<false, false, 1>(w, x, f, p, grid, stream);
+    if (drop) return sub == 2 ? launch_pair<true, true, 2>(w, x, f, p, grid, stream) : launch_pair<true, true, 1>(w, x, f, p, grid, stream);
+    return sub == 2 ? launch_pair<true, false, 2>(w, x, f, p, grid, stream) : launch_pair<true, false, 1>(w, x, f, p, grid, stream);
   }
   if (!backward) return launch_tile<false, false>(w, x, f, p, num_sms, stream);
   if (drop) return launch_tile<true, true>(w, x, f, p, num_sms, stream);
