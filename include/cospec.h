@@ -643,11 +643,11 @@ COSPEC_API int cospec_lora_backward(const cospec_lora_dims* dims, const uint16_t
  *    draft int32 [R, K]; argmax int32 [R, K+1]; stats float32 [R, K+1, 5]; accept, eff uint8 [R, K];
  *    adv, p_old, p_ref float32 [R, K], read at effective decisions: probabilities between 0 and 1, p_ref neither, p_old
  *    not 0 for the action taken (else the terms are infinite or NaN, as the formulas say)
- *    w1 float32 [mlp_hidden, 8], b1, w2 [mlp_hidden], b2 [1] (device)
+ *    w1 float32 [mlp_hidden, 8] (16-byte aligned), b1, w2 [mlp_hidden], b2 [1] (device)
  *    loss float32 [4]; p_new, dz float32 [R, K] (0 outside effective decisions); dw1, db1, dw2, db2 as the weights
  *    params: clip_eps >= 0, beta_h and beta_kl are used
  *    ws >= cospec_arbitrate_loss_workspace(mlp_hidden) bytes, 16-byte aligned (no initialisation)
- *    Supported: 1 <= K <= 64, R * K < 2^31 - 512, 1 <= mlp_hidden <= 1024.  Every sum has a fixed order. */
+ *    Supported: 1 <= K <= 64, R * K <= 2^31 - 4096, 1 <= mlp_hidden <= 1024.  Every sum has a fixed order. */
 COSPEC_API size_t cospec_arbitrate_loss_workspace(int mlp_hidden);
 COSPEC_API int cospec_arbitrate_loss(int num_rounds, int K, const int32_t* draft, const int32_t* argmax,
                                      const float* stats, int mlp_hidden, const float* w1, const float* b1,

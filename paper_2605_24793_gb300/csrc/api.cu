@@ -818,8 +818,8 @@ COSPEC_API int cospec_arbitrate_loss(int num_rounds, int K, const int32_t* draft
   CS_CHECK_ARG(num_rounds >= 0 && K >= 1 && mlp_hidden >= 1 && params);
   CS_CHECK_ARG(params->clip_eps >= 0.f && isfinite(params->clip_eps) && isfinite(params->beta_h) && isfinite(params->beta_kl) &&
                isfinite(grad_scale));
-  if (K > 64 || mlp_hidden > 1024 || (long long)num_rounds * K >= (1LL << 31) - 512) return COSPEC_ERR_UNSUPPORTED;
-  CS_CHECK_ARG(w1 && b1 && w2 && b2 && loss && dw1 && db1 && dw2 && db2);
+  if (K > 64 || mlp_hidden > 1024 || (long long)num_rounds * K > (1LL << 31) - 4096) return COSPEC_ERR_UNSUPPORTED;
+  CS_CHECK_ARG(w1 && b1 && w2 && b2 && loss && dw1 && db1 && dw2 && db2 && aligned16(w1));
   CS_CHECK_ARG(num_rounds == 0 || (draft && argmax && stats && accept && eff && adv && p_old && p_ref && p_new && dz));
   if (!ws || ws_bytes < arb_loss_ws_bytes(mlp_hidden) || !aligned16(ws)) return COSPEC_ERR_WORKSPACE;
   const int sms = device_num_sms();

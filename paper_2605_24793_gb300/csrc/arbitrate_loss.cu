@@ -38,7 +38,10 @@ struct LossSmem {
   float adv[BATCH], old[BATCH], ref[BATCH], g[BATCH];
   int at[BATCH];                          // position in the step | action taken << 31
   uint16_t list[STEP];                    // effective positions of the step
-  uint32_t match[STEP / 32 + 2], act[STEP / 32];
+  uint32_t match[STEP / 32 + 2];
+  int warp_count[8];
+  int draft[STEP], argmax[STEP];          // of the next step, under way while this one is computed
+  __align__(16) uint8_t eff[STEP];
 };
 
 // g(x) = x - log(1 + x), x >= -1
@@ -109,17 +112,26 @@ __global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs 
   griddep_wait();
   griddep_launch_dependents();
 
-  // units 2 j, 2 j + 1 of pair j = (i TW + tw) 32 + lane
+  // Units 2 j, 2 j + 1 of pair j = (i TW + tw) 32 + lane.  W1 and b1 negated: the sign bit of -(W1 f + b1) says that the
+  // unit is on, and one shift collects it.
   float2 w1[PP][8], b1[PP], w2[PP], S[PP][9];
 #pragma unroll
   for (int i = 0; i < PP; ++i) {
     const int h = 2 * ((i * TW + tw) * 32 + lane);
-    const bool x = h < a.H, y = h + 1 < a.H;
+    float4 v[4];
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      w1[i][k] = make_float2(x ? a.w1[(size_t)h * 8 + k] : 0.f, y ? a.w1[(size_t)(h + 1) * 8 + k] : 0.f);
-    b1[i] = make_float2(x ? a.b1[h] : 0.f, y ? a.b1[h + 1] : 0.f);
-    w2[i] = make_float2(x ? a.w2[h] : 0.f, y ? a.w2[h + 1] : 0.f);
+    for (int k = 0; k < 4; ++k)
+      v[k] = h + (k >> 1) < a.H ? __ldg(reinterpret_cast<const float4*>(a.w1 + (size_t)h * 8) + k) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      w1[i][4 * k] = make_float2(-v[k].x, -v[2 + k].x);
+      w1[i][4 * k + 1] = make_float2(-v[k].y, -v[2 + k].y);
+      w1[i][4 * k + 2] = make_float2(-v[k].z, -v[2 + k].z);
+      w1[i][4 * k + 3] = make_float2(-v[k].w, -v[2 + k].w);
+    }
+    // (0 - b: a zero keeps its positive sign, and so does every sum that comes to zero)
+    b1[i] = make_float2(h < a.H ? 0.f - __ldg(a.b1 + h) : 0.f, h + 1 < a.H ? 0.f - __ldg(a.b1 + h + 1) : 0.f);
+    w2[i] = make_float2(h < a.H ? __ldg(a.w2 + h) : 0.f, h + 1 < a.H ? __ldg(a.w2 + h + 1) : 0.f);
 #pragma unroll
     for (int k = 0; k < 9; ++k) S[i][k] = make_float2(0.f, 0.f);
   }
@@ -129,67 +141,98 @@ __global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs 
 #pragma unroll
   for (int k = 0; k < 4; ++k) sums[k] = make_float2(0.f, 0.f);
 
-  for (long long base = (long long)blockIdx.x * step; base < total; base += (long long)gridDim.x * step) {
-    const int words = step / 32;
-    // every load of the step goes out before the first is used
-    int dr[PER], ar[PER];
-    uint32_t ef[PER];
+  // A warp takes step / 8 positions in a row, 32 at a time.  A step's ids and flags are copied to shared memory while the
+  // step before is computed (the flags by plain loads where they do not lie on four bytes).
+  const int words = step / 256;
+  const bool by4 = (reinterpret_cast<uintptr_t>(a.eff) & 3u) == 0;
+  const bool by16 = ((reinterpret_cast<uintptr_t>(a.p_new) | reinterpret_cast<uintptr_t>(a.dz)) & 15u) == 0;
+  const int q32 = 32 / a.K, m32 = 32 - q32 * a.K;        // 32 positions on: rounds and position
+  const int first = warp * words * 32;                   // the warp's first position of a step
+  auto fetch = [&](int base) {
+    const int e0 = base + first + lane;
+    int r = e0 / a.K, i = e0 - r * a.K;
+    const uint32_t d = smem_u32(&sm.draft[first + lane]), m = smem_u32(&sm.argmax[first + lane]);
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-      const long long e = base + j * THREADS + tid;
-      dr[j] = ar[j] = 0;
-      ef[j] = 0;
-      if (j * THREADS < step && e < total) {
-        dr[j] = __ldg(a.draft + e);
-        ar[j] = __ldg(a.argmax + e + (int)e / a.K);          // rows of K + 1
-        ef[j] = __ldg(a.eff + e);
+      const int e = e0 + 32 * j;
+      if (j < words && e < total) {
+        cp_async4(d + 128u * j, a.draft + e);
+        cp_async4(m + 128u * j, a.argmax + (long long)e + r);          // rows of K + 1
+      }
+      r += q32, i += m32;
+      if (i >= a.K) i -= a.K, ++r;
+    }
+    if (by4) {
+#pragma unroll
+      for (int j = 0; j < PER / 4; ++j) {
+        const int off = lane * 4 + j * 128;
+        if (off < words * 32 && base + first + off + 3 < total) cp_async4(smem_u32(&sm.eff[first + off]), a.eff + base + first + off);
       }
     }
+    cp_async_commit();
+  };
+  if ((long long)blockIdx.x * step < total) fetch((int)blockIdx.x * step);
+  for (long long base64 = (long long)blockIdx.x * step; base64 < total; base64 += (long long)gridDim.x * step) {
+    const int base = (int)base64;
+    // zeros first; the effective positions are written over them after the next barriers
+    if (by16) {
+#pragma unroll
+      for (int j = 0; j < PER / 4; ++j) {
+        const int off = tid * 4 + j * 4 * THREADS;
+        if (off < step && base + off + 3 < total) {
+          *reinterpret_cast<float4*>(a.p_new + base + off) = make_float4(0.f, 0.f, 0.f, 0.f);
+          *reinterpret_cast<float4*>(a.dz + base + off) = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+      }
+    }
+    for (int off = by16 ? (min(step, total - base) & ~3) + tid : tid; off < step && base + off < total; off += THREADS) {
+      a.p_new[base + off] = 0.f;
+      a.dz[base + off] = 0.f;
+    }
+    cp_async_wait<0>();
+    __syncwarp();                            // (a warp reads what its own lanes copied)
+    unsigned aa[PER];
+    int mine = 0;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-      if (j * THREADS >= step) break;
-      const long long e = base + j * THREADS + tid;
-      const bool match = e < total && dr[j] == ar[j], act = dr[j] != ar[j] && ef[j] != 0;
-      if (e < total && !act) {
-        a.p_new[e] = 0.f;
-        a.dz[e] = 0.f;
-      }
-      const unsigned mm = __ballot_sync(0xffffffffu, match), aa = __ballot_sync(0xffffffffu, act);
-      if (lane == 0) {
-        sm.match[2 + j * 8 + warp] = mm;
-        sm.act[j * 8 + warp] = aa;
-      }
+      const int off = first + j * 32 + lane, e = base + off;
+      const bool in = j < words && e < total;
+      const int at = in ? off : 0;           // (in bounds, and not used)
+      const int dr = sm.draft[at], ar = sm.argmax[at];
+      uint32_t ef = sm.eff[at];
+      if (in && !(by4 && base + (off & ~3) + 3 < total)) ef = __ldg(a.eff + e);
+      const unsigned mm = __ballot_sync(0xffffffffu, in && dr == ar);
+      aa[j] = __ballot_sync(0xffffffffu, in && dr != ar && ef != 0);
+      mine += __popc(aa[j]);
+      if (lane == 0 && j < words) sm.match[2 + warp * words + j] = mm;
     }
     if (warp < 2) {                          // the positions before the step that may be of its first round
-      const long long e = base - 64 + warp * 32 + lane;
+      const int e = base - 64 + warp * 32 + lane;
       bool match = false;
-      if (e >= 0) {
-        const int r = (int)e / a.K;
-        match = a.draft[e] == a.argmax[e + r];
-      }
+      if (e >= 0) match = __ldg(a.draft + e) == __ldg(a.argmax + (long long)e + e / a.K);
       const unsigned mm = __ballot_sync(0xffffffffu, match);
       if (lane == 0) sm.match[warp] = mm;
     }
+    if (lane == 0) sm.warp_count[warp] = mine;
     __syncthreads();
-    // the effective positions in order: warp w lists words w, w + 8, ..
-    const int c0 = lane < words ? __popc(sm.act[lane]) : 0, c1 = lane + 32 < words ? __popc(sm.act[lane + 32]) : 0;
-    int p0 = c0, p1 = c1;
+    if (base64 + (long long)gridDim.x * step < total) fetch((int)(base64 + (long long)gridDim.x * step));
+    int before = 0, decisions = 0;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int x = __shfl_up_sync(0xffffffffu, p0, o), y = __shfl_up_sync(0xffffffffu, p1, o);
-      if (lane >= o) p0 += x, p1 += y;
+    for (int w = 0; w < 8; ++w) {
+      const int c = sm.warp_count[w];
+      if (w < warp) before += c;
+      decisions += c;
     }
-    const int sum0 = __shfl_sync(0xffffffffu, p0, 31), decisions = sum0 + __shfl_sync(0xffffffffu, p1, 31);
-    for (int w = warp; w < words; w += 8) {
-      const int before = w < 32 ? __shfl_sync(0xffffffffu, p0 - c0, w) : sum0 + __shfl_sync(0xffffffffu, p1 - c1, w - 32);
-      const unsigned bits = sm.act[w];
-      if ((bits >> lane) & 1u) sm.list[before + __popc(bits & ((1u << lane) - 1u))] = (uint16_t)(w * 32 + lane);
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      if ((aa[j] >> lane) & 1u) sm.list[before + __popc(aa[j] & ((1u << lane) - 1u))] = (uint16_t)(first + j * 32 + lane);
+      before += __popc(aa[j]);
     }
     __syncthreads();
     for (int d0 = 0; d0 < decisions; d0 += BATCH) {
       const int count = min(BATCH, decisions - d0), groups = (count + 3) / 4;
       for (int d = tid; d < count; d += THREADS) {
-        const int off = sm.list[d0 + d], e = (int)base + off, r = e / a.K, i = e - r * a.K;
+        const int off = sm.list[d0 + d], e = base + off, r = e / a.K, i = e - r * a.K;
         const float* s0 = a.stats + ((size_t)e + r) * 5;
         const float* s1 = s0 + 5;
         const float x0 = s0[0], x1 = s0[1], x2 = s0[2], x3 = s0[3], x4 = s0[4], y0 = s1[0], y2 = s1[2], y4 = s1[4];
@@ -234,8 +277,9 @@ __global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs 
             float2 v = b1[i];
 #pragma unroll
             for (int k = 0; k < 8; ++k) v = fma2(w1[i][k], f[k], v);
-            bits |= ((v.x > 0.f ? 1u : 0u) | (v.y > 0.f ? 2u : 0u)) << (4 * d + 2 * i);
-            zz = fma2(w2[i], make_float2(fmaxf(v.x, 0.f), fmaxf(v.y, 0.f)), zz);
+            bits = __funnelshift_l(__float_as_uint(v.x), bits, 1);
+            bits = __funnelshift_l(__float_as_uint(v.y), bits, 1);
+            zz = fma2(w2[i], make_float2(fmaxf(-v.x, 0.f), fmaxf(-v.y, 0.f)), zz);
           }
           z[d] = zz.x + zz.y;
         }
@@ -259,7 +303,7 @@ __global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs 
           for (int w = 1; w < TW; ++w) z += zpart[w * BATCH + d];
           const int at = sm.at[d];
           const Decision x = decide(z + b2, sm.adv[d], sm.old[d], sm.ref[d], at < 0, a);
-          const int e = (int)base + (at & 0x7fffffff);
+          const int e = base + (at & 0x7fffffff);
           g = x.dz * a.grad_scale;
           a.p_new[e] = x.p;
           a.dz[e] = g;
@@ -286,7 +330,8 @@ __global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs 
           const float g = sm.g[4 * q + d];
 #pragma unroll
           for (int i = 0; i < PP; ++i) {
-            const float2 m = make_float2((bits >> (4 * d + 2 * i)) & 1u ? g : 0.f, (bits >> (4 * d + 2 * i)) & 2u ? g : 0.f);
+            constexpr int TOP = 8 * PP - 1;          // the first unit's bit
+          const float2 m = make_float2((bits >> (TOP - 2 * (PP * d + i))) & 1u ? g : 0.f, (bits >> (TOP - 1 - 2 * (PP * d + i))) & 1u ? g : 0.f);
 #pragma unroll
             for (int k = 0; k < 8; ++k) S[i][k] = fma2(m, f[k], S[i][k]);
             S[i][8] = add2(S[i][8], m);
@@ -322,6 +367,7 @@ __global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs 
   }
   if (tid < 4) {
     float2 v = make_float2(0.f, 0.f);
+#pragma unroll
     for (int w = 0; w < 8; ++w) v = add_pair(v, lsum[4 + w * 4 + tid]);
     lsum[tid] = v;
   }
@@ -336,15 +382,17 @@ __global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs 
     out[e] = dsmem_sum(red0 + 4u * (uint32_t)e, CS);
   }
   if (rank == 0 && tid < 4) {
-    float2 v = make_float2(0.f, 0.f);
-    for (int i = 0; i < CS; ++i) {
-      float2 w;
-      asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];"
-                   : "=f"(w.x), "=f"(w.y)
-                   : "r"(dsmem_map(smem_u32(&lsum[tid]), (uint32_t)i))
-                   : "memory");
-      v = add_pair(v, w);
+    float2 w[CLUSTER], v = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < CLUSTER; ++i) {
+      w[i] = make_float2(0.f, 0.f);
+      if (i < CS)
+        asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];"
+                     : "=f"(w[i].x), "=f"(w[i].y)
+                     : "r"(dsmem_map(smem_u32(&lsum[tid]), (uint32_t)i)));
     }
+#pragma unroll
+    for (int i = 0; i < CLUSTER; ++i) v = add_pair(v, w[i]);
     ws_l[(size_t)group * 4 + tid] = v;
   }
   __syncwarp();

@@ -955,7 +955,7 @@ cudaError_t launch_lora_gemm(const LoraArgs& a, bool backward, int num_sms, int*
   const int kblocks = (p.C + BK - 1) / BK;
   // Above 256 rows a CTA pair's tiles, of the size that leaves the fewest pairs idle: a tile takes the bytes of its
   // operands (its rows and 256 features) and about four stages' time besides.
-  const bool pairs = p.M > MAX_NT;
+  const bool pairs = p.M > 96;
   int grid = 0, sub = 2;
   if (pairs) {
     const int all = num_sms / 2, ftiles = (p.F + PBM - 1) / PBM;

@@ -90,6 +90,17 @@ def test_against_the_reference(R, K, H):
     _check(_run(c), o, c)
 
 
+@pytest.mark.parametrize("shift", [1, 2, 3, 4])
+def test_flags_at_any_address(shift):
+    c, o = _sure(97 + shift, 130, 7, 64)
+    dev = {k: torch.from_numpy(v).cuda() for k, v in c.items()}
+    for k in ("eff", "accept"):
+        buf = torch.full((c[k].size + 16,), 1, dtype=torch.uint8, device="cuda")
+        dev[k] = buf[shift:shift + c[k].size].view(c[k].shape)
+        dev[k].copy_(torch.from_numpy(c[k]))
+    _check(C.arbitrate_loss(**dev, params=C.RLParams(), grad_scale=0.125), o, c)
+
+
 def test_every_position_a_decision():
     c, o = _sure(5, 30, 40, 64, mismatch=1.0, dense=True)
     assert int(c["eff"].sum()) == 1200

@@ -94,7 +94,7 @@ def _loss(lib, R=4, K=5, H=16, ws_bytes=1 << 30, params=None, scale=1.0, **kw):
     (dict(R=-1), INVALID), (dict(K=0), INVALID), (dict(H=0), INVALID), (dict(K=65), UNSUPPORTED), (dict(H=1025), UNSUPPORTED),
     (dict(R=1 << 27, K=16), UNSUPPORTED), (dict(scale=float("inf")), INVALID), (dict(params=C.RLParams(clip_eps=-0.1)), INVALID),
     (dict(params=C.RLParams(clip_eps=float("nan"))), INVALID), (dict(params=C.RLParams(beta_kl=float("inf"))), INVALID),
-    (dict(ws_bytes=64), WORKSPACE), (dict(ws=None), WORKSPACE), (dict(ws=ODD), WORKSPACE)] + [
+    (dict(ws_bytes=64), WORKSPACE), (dict(ws=None), WORKSPACE), (dict(ws=ODD), WORKSPACE), (dict(w1=ODD), INVALID)] + [
     ({n: None}, INVALID) for n in ("draft", "argmax", "stats", "w1", "b1", "w2", "b2", "accept", "eff", "adv", "p_old", "p_ref", "loss", "p_new", "dz",
                                    "dw1", "db1", "dw2", "db2")])
 def test_loss(lib, kw, want):
