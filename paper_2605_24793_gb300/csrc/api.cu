@@ -798,7 +798,7 @@ COSPEC_API int cospec_lora_backward(const cospec_lora_dims* dims, const uint16_t
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
   if (p.M > 0 && (dx || da)) e = launch_lora_low(p, true, sms, err, s);
-  if (e == cudaSuccess && (da || db)) e = launch_lora_grad(p, sms, s);
+  if (e == cudaSuccess && (da || db)) e = launch_lora_grad(p, sms, err, s);
   if (e == cudaSuccess && p.M > 0 && dx) e = launch_lora_gemm(p, true, sms, err, s);
   return cuda_status(e);
 }

@@ -64,6 +64,10 @@ CS_DEV void cp_async16(uint32_t dst, const void* src, bool on) {
 CS_DEV void cp_async4(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
+// The calling thread arrives on `bar` (whose count includes it) when its cp.async so far have landed.
+CS_DEV void cp_async_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
 CS_DEV void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 CS_DEV void cp_async_wait() {
@@ -588,6 +592,15 @@ CS_DEV void griddep_launch_dependents() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
+// A barrier of `nthreads` that tells whether `ok` held in all of them.
+CS_DEV bool named_bar_all(int id, int nthreads, bool ok) {
+  uint32_t r;
+  asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %3, 0;\n barrier.cta.red.and.pred q, %1, %2, p;\n selp.u32 %0, 1, 0, q;\n}\n"
+               : "=r"(r)
+               : "r"(id), "r"(nthreads), "r"(ok ? 1u : 0u)
+               : "memory");
+  return r != 0;
+}
 CS_DEV void named_bar_sync(int id, int nthreads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(nthreads) : "memory");
 }

@@ -221,7 +221,7 @@ struct LoraArgs {
 };
 cudaError_t launch_lora_low(const LoraArgs& a, bool backward, int num_sms, int* err, cudaStream_t stream);
 cudaError_t launch_lora_gemm(const LoraArgs& a, bool backward, int num_sms, int* err, cudaStream_t stream);
-cudaError_t launch_lora_grad(const LoraArgs& a, int num_sms, cudaStream_t stream);
+cudaError_t launch_lora_grad(const LoraArgs& a, int num_sms, int* err, cudaStream_t stream);
 
 // ---------------------------------------------------------------- accept + commit
 struct CommitArgs {

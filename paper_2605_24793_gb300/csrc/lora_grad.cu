@@ -7,11 +7,11 @@
 // bf16 parts, which hold all 24 bits of it, so the sums are those of fp32 products (a gradient that is
 // summed over micro-batches starts from fp32).
 //
-// A CTA takes 256 columns of one adapter, 32 a warp (two warps share the rows, so that an SM has 16 or 32 of them; with eight
-// each waited on its own products: 35 us at 4096 rows of 2560 + 6144); the adapter's rows, listed in shared memory first, so that rows
-// of other adapters and what they hold are not read, come 32 at a time: Q by cp.async into a ring, P through
-// the same ring and is split once for all warps.  A thread masks the 16-byte chunks of x that it copied itself, each one
-// draw of the generator.  The rows are split over the CTAs of a cluster and joined in a fixed order.
+// A CTA takes 256 columns of one adapter, 32 a warp; the adapter's rows, listed in shared memory first, so that rows of
+// other adapters and what they hold are not read, come 32 at a time into a ring.  Four warps of their own copy them: by the
+// computing warps the copies took half of a batch's time, and bulk copies of 512 bytes, a lane a row, are done one
+// after another and took twice as long altogether.  While a batch is multiplied the next one's P is split, once for all
+// warps, and its dropped elements are set to zero.  The rows are split over the CTAs of a cluster and joined in a fixed order.
 #include "lora.cuh"
 
 namespace cospec {
@@ -20,9 +20,12 @@ namespace {
 
 constexpr int CB = 256;              // columns of a CTA
 constexpr int BR = 32;               // rows of a batch
-constexpr int GDEPTH = 4;            // batches in the ring
+constexpr int GDEPTH = 4;            // batches in the ring, a power of two
+constexpr int GRAD_THREADS = 256;    // eight warps that compute
+constexpr int COPY_THREADS = 128;    // four that copy
 constexpr int WIN = 2048;            // rows listed at a time
-constexpr uint32_t Q_BYTES = BR * CB * 2;
+constexpr uint32_t Q_PITCH = CB * 2 + 16;   // of a row of Q: eight neighbouring rows start on different banks
+constexpr uint32_t Q_BYTES = BR * Q_PITCH;
 
 struct GradArgs {
   const __nv_bfloat16 *x, *dy;
@@ -35,11 +38,13 @@ struct GradArgs {
   int M, r;
   int accumulate;
   LoraDrop drop;
+  int* err;
 };
 
 struct GradSmem {
   int list[WIN];
   int warp_count[16];
+  uint64_t full[GDEPTH], empty[GDEPTH];
 };
 // the ring of Q and of P [BR rows][R] fp32, two buffers of P's parts [3][BR rows][R], the list; then the sums,
 // [R][CB + 8] or [CB][R + 4]
@@ -49,11 +54,11 @@ __host__ __device__ constexpr uint32_t grad_bytes(int R) {
   return GDEPTH * grad_slot(R) + 2 * grad_p_bytes(R) + (uint32_t)sizeof(GradSmem);
 }
 
-// RT: ranks of 16.  NG: groups of eight warps, each with all columns and its share of a batch's rows.
-template <int RT, int NG>
-__global__ void __launch_bounds__(256 * NG) lora_grad_kernel(const GradArgs p) {
+// RT: ranks in sixteens.
+template <int RT>
+__global__ void __launch_bounds__(GRAD_THREADS + COPY_THREADS) lora_grad_kernel(const GradArgs p) {
   extern __shared__ __align__(128) uint8_t raw[];
-  constexpr int R = 16 * RT, GRAD_THREADS = 256 * NG, WARPS = 8 * NG;
+  constexpr int R = 16 * RT, WARPS = GRAD_THREADS / 32;
   constexpr int PC = BR * R / 4;                       // 16-byte chunks of a batch's P
   constexpr uint32_t P_PART = (uint32_t)(BR * R * 2), SLOT = grad_slot(R), P_OFF = GDEPTH * SLOT;
   GradSmem& sm = *reinterpret_cast<GradSmem*>(raw + P_OFF + 2 * grad_p_bytes(R));
@@ -61,13 +66,20 @@ __global__ void __launch_bounds__(256 * NG) lora_grad_kernel(const GradArgs p) {
   const int S = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
   const int block = (int)blockIdx.x / S, which = block >= p.blocks0;
   const int c0 = (which ? block - p.blocks0 : block) * CB;
-  const int a = (int)blockIdx.y, wc = warp & 7, wg = warp >> 3;
+  const int a = (int)blockIdx.y;
   const __nv_bfloat16* Q = which ? p.dy : p.x;
   const float* P = which ? p.u : p.t;
   const long long ld = which ? p.ldy : p.ldx;
   const int width = which ? p.N : p.K;
   const bool drop = which == 0 && p.drop.thr != 0u;
   const uint32_t q0 = smem_u32(raw), p0 = q0 + P_OFF;
+  if (tid == 0) {
+    for (int i = 0; i < GDEPTH; ++i) {
+      mbar_init(&sm.full[i], COPY_THREADS);
+      mbar_init(&sm.empty[i], WARPS);
+    }
+    fence_barrier_init();
+  }
   griddep_wait();
   griddep_launch_dependents();
   LoraKey key{0, 0};
@@ -81,22 +93,22 @@ __global__ void __launch_bounds__(256 * NG) lora_grad_kernel(const GradArgs p) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[i][c][e] = 0.f;
 
-  // 512-byte rows of Q, 2 R byte rows of P; the 16-byte chunks exchanged by the row, so that eight neighbouring rows lie
-  // on different banks
+  // 2 R byte rows of P's parts; the 16-byte chunks exchanged by the row, so that eight neighbouring rows lie on different banks
   auto p_at = [&](int row, int c) {
     const int sw = RT >= 4 ? row & 7 : RT == 2 ? (row >> 1) & 3 : (row >> 2) & 1;
     return (uint32_t)(row * (R * 2) + ((c ^ sw) << 4));
   };
   const int m_lo = (int)((long long)p.M * rank / S), m_hi = (int)((long long)p.M * (rank + 1) / S);
+  int turn = 0;                            // batches so far
   for (int w0 = m_lo; w0 < m_hi; w0 += WIN) {
     // the adapter's rows of the window, in order
     const int w1 = min(w0 + WIN, m_hi);
     int have = 0;
     for (int b = w0; b < w1; b += GRAD_THREADS) {
       const int m = b + tid;
-      const bool in = m < w1 && p.adapter[m] == a;
+      const bool in = warp < WARPS && m < w1 && p.adapter[m] == a;
       const unsigned mask = __ballot_sync(0xffffffffu, in);
-      if (lane == 0) sm.warp_count[warp] = __popc(mask);
+      if (lane == 0 && warp < WARPS) sm.warp_count[warp] = __popc(mask);
       __syncthreads();
       int at = have + __popc(mask & ((1u << lane) - 1u));
 #pragma unroll
@@ -109,119 +121,125 @@ __global__ void __launch_bounds__(256 * NG) lora_grad_kernel(const GradArgs p) {
       __syncthreads();
     }
     const int batches = (have + BR - 1) / BR;
-    // chunk i of a batch's Q: row warp + WARPS i, columns 8 (tid mod 32) ..
-    const int qc = tid & 31, col = c0 + 8 * qc;
-    // chunk tid + GRAD_THREADS i of its P: row / (R / 4), ranks 4 ..
-    auto load = [&](int b) {
-      if (b < batches) {
-        const uint32_t dst = q0 + (uint32_t)(b & (GDEPTH - 1)) * SLOT;
-#pragma unroll
-        for (int i = 0; i < BR / WARPS; ++i) {
-          const int row = warp + WARPS * i;
-          const bool on = b * BR + row < have && col < width;
-          cp_async16(dst + (uint32_t)(row * 512 + ((qc ^ (row & 7)) << 4)), on ? Q + (long long)sm.list[b * BR + row] * ld + col : Q, on);
+    if (warp >= WARPS) {
+      // a warp a row of Q, every fourth row; rows behind the last, columns behind the width and ranks behind the rank as zeros
+      const int ct = tid - GRAD_THREADS, cw = ct >> 5, col = c0 + 8 * lane;
+      for (int b = 0; b < batches; ++b, ++turn) {
+        const int slot = turn & (GDEPTH - 1), rows = min(BR, have - b * BR);
+        if (turn >= GDEPTH && !__all_sync(0xffffffffu, mbar_wait(&sm.empty[slot], (uint32_t)(turn / GDEPTH - 1) & 1u))) {
+          if (lane == 0) set_err(p.err, ERR_TIMEOUT);
+          break;
         }
+        const uint32_t dst = q0 + (uint32_t)slot * SLOT;
+        const int* list = sm.list + b * BR;
+#pragma unroll
+        for (int i = 0; i < BR / 4; ++i) {
+          const int row = cw + 4 * i;
+          const bool on = row < rows && col < width;
+          cp_async16(dst + (uint32_t)row * Q_PITCH + (uint32_t)lane * 16u, on ? Q + (long long)list[row] * ld + col : Q, on);
+        }
+#pragma unroll
+        for (int i = 0; i * COPY_THREADS < PC; ++i) {
+          const int e = ct + COPY_THREADS * i, row = e / (R / 4), j = 4 * (e % (R / 4));
+          if (e >= PC) break;
+          const bool on = row < rows && j < p.r;
+          cp_async16(dst + Q_BYTES + (uint32_t)e * 16u, on ? P + (size_t)list[row] * p.r + j : P, on);
+        }
+        cp_async_arrive(&sm.full[slot]);
+      }
+    } else {
+      // P of batch b as three parts, and Q's dropped elements set to zero
+      auto make = [&](int b) {
+        const int slot = (turn + b) & (GDEPTH - 1), rows = min(BR, have - b * BR);
+        const bool ok = mbar_wait(&sm.full[slot], (uint32_t)((turn + b) / GDEPTH) & 1u);
+        const uint8_t* src = raw + (uint32_t)slot * SLOT + Q_BYTES;
+        uint8_t* dst = raw + P_OFF + (uint32_t)(b & 1) * grad_p_bytes(R);
 #pragma unroll
         for (int i = 0; i * GRAD_THREADS < PC; ++i) {
           const int e = tid + GRAD_THREADS * i, row = e / (R / 4), j = 4 * (e % (R / 4));
           if (e >= PC) break;
-          const bool on = b * BR + row < have && j < p.r;
-          cp_async16(dst + Q_BYTES + (uint32_t)e * 16u, on ? P + (size_t)sm.list[b * BR + row] * p.r + j : P, on);
-        }
-      }
-      cp_async_commit();
-    };
-    // a thread splits the chunks of P that it copied itself
-    auto split_p = [&](int b) {
-      const uint8_t* src = raw + (uint32_t)(b & (GDEPTH - 1)) * SLOT + Q_BYTES;
-      uint8_t* dst = raw + P_OFF + (uint32_t)(b & 1) * grad_p_bytes(R);
-#pragma unroll
-      for (int i = 0; i * GRAD_THREADS < PC; ++i) {
-        const int e = tid + GRAD_THREADS * i, row = e / (R / 4), j = 4 * (e % (R / 4));
-        if (e >= PC) break;
-        float4 v = *reinterpret_cast<const float4*>(src + (uint32_t)e * 16u);
-#pragma unroll
-        for (int k = 0; k < 3; ++k) {
-          float h[4], l[4];
-          lora_split2(v.x, h[0], l[0]);
-          lora_split2(v.y, h[1], l[1]);
-          lora_split2(v.z, h[2], l[2]);
-          lora_split2(v.w, h[3], l[3]);
-          *reinterpret_cast<uint2*>(dst + k * P_PART + p_at(row, j >> 3) + (j & 4) * 2) = make_uint2(pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3]));
-          v = make_float4(l[0], l[1], l[2], l[3]);
-        }
-      }
-    };
-#pragma unroll
-    for (int i = 0; i < GDEPTH - 1; ++i) load(i);
-    for (int b = 0; b < batches; ++b) {
-      cp_async_wait<GDEPTH - 2>();
-      split_p(b);
-      const uint32_t qb = q0 + (uint32_t)(b & (GDEPTH - 1)) * SLOT;
-      if (drop) {
-#pragma unroll 2
-        for (int i = 0; i < BR / WARPS; ++i) {
-          const int row = warp + WARPS * i;
-          if (b * BR + row >= have) break;
-          uint4* q = reinterpret_cast<uint4*>(raw + (qb - q0) + row * 512 + ((qc ^ (row & 7)) << 4));
-          *q = lora_dropped8(*q, (uint32_t)(col >> 3), (uint32_t)sm.list[b * BR + row], p.drop, key);
-        }
-      }
-      __syncthreads();
-      load(b + GDEPTH - 1);
-      const uint32_t pb = p0 + (uint32_t)(b & 1) * grad_p_bytes(R);
-      const int steps = min(BR / 16, (have - b * BR + 15) / 16);
-      for (int ks = wg; ks < steps; ks += NG) {
-        const int row = ks * 16 + (lane & 15);
-        uint32_t bq[4][2];
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {      // 16 columns: (k 0-7, 8-15) of the first eight, then of the others
-          const int cc = wc * 4 + 2 * c + (lane >> 4);
-          ldsm_x4_t(qb + (uint32_t)(row * 512 + ((cc ^ (row & 7)) << 4)), bq[2 * c][0], bq[2 * c][1], bq[2 * c + 1][0], bq[2 * c + 1][1]);
-        }
-        // the rank's blocks: (ranks 0-7, k 0-7), (8-15, 0-7), (0-7, 8-15), (8-15, 8-15), stored with k along the rows
-        const int pr = ks * 16 + (lane & 7) + ((lane >> 4) << 3);
-#pragma unroll
-        for (int i = 0; i < RT; ++i)
+          float4 v = *reinterpret_cast<const float4*>(src + (uint32_t)e * 16u);
 #pragma unroll
           for (int k = 0; k < 3; ++k) {
-            uint32_t pa[4];
-            ldsm_x4_t(pb + (uint32_t)k * P_PART + p_at(pr, 2 * i + ((lane >> 3) & 1)), pa[0], pa[1], pa[2], pa[3]);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) mma_16816(acc[i][c], pa, bq[c][0], bq[c][1]);
+            float h[4], l[4];
+            lora_split2(v.x, h[0], l[0]);
+            lora_split2(v.y, h[1], l[1]);
+            lora_split2(v.z, h[2], l[2]);
+            lora_split2(v.w, h[3], l[3]);
+            *reinterpret_cast<uint2*>(dst + k * P_PART + p_at(row, j >> 3) + (j & 4) * 2) = make_uint2(pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3]));
+            v = make_float4(l[0], l[1], l[2], l[3]);
           }
+        }
+        if (drop) {
+#pragma unroll 2
+          for (int i = 0; i < BR / WARPS; ++i) {
+            const int row = warp + WARPS * i;
+            uint4* q = reinterpret_cast<uint4*>(raw + (uint32_t)slot * SLOT + (uint32_t)row * Q_PITCH + lane * 16);
+            if (row < rows) *q = lora_dropped8(*q, (uint32_t)(c0 / 8 + lane), (uint32_t)sm.list[b * BR + row], p.drop, key);
+          }
+        }
+        return ok;
+      };
+      bool ok = batches == 0 || make(0);
+      for (int b = 0; b < batches; ++b) {
+        // batch b is made, and batch b - 1 (whose buffer b + 1 takes) multiplied
+        if (!named_bar_all(1, GRAD_THREADS, ok)) {
+          if (tid == 0) set_err(p.err, ERR_TIMEOUT);
+          break;
+        }
+        if (b + 1 < batches) ok = make(b + 1);
+        const int slot = (turn + b) & (GDEPTH - 1);
+        const uint32_t qb = q0 + (uint32_t)slot * SLOT, pb = p0 + (uint32_t)(b & 1) * grad_p_bytes(R);
+        const int steps = min(BR / 16, (have - b * BR + 15) / 16);
+        for (int ks = 0; ks < steps; ++ks) {
+          const int row = ks * 16 + (lane & 15);
+          uint32_t bq[4][2];
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {      // 16 columns: (k 0-7, 8-15) of the first eight, then of the others
+            const int cc = warp * 4 + 2 * c + (lane >> 4);
+            ldsm_x4_t(qb + (uint32_t)row * Q_PITCH + (uint32_t)(cc * 16), bq[2 * c][0], bq[2 * c][1], bq[2 * c + 1][0], bq[2 * c + 1][1]);
+          }
+          // the rank's blocks: (ranks 0-7, k 0-7), (8-15, 0-7), (0-7, 8-15), (8-15, 8-15), stored with k along the rows
+          const int pr = ks * 16 + (lane & 7) + ((lane >> 4) << 3);
+#pragma unroll
+          for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+              uint32_t pa[4];
+              ldsm_x4_t(pb + (uint32_t)k * P_PART + p_at(pr, 2 * i + ((lane >> 3) & 1)), pa[0], pa[1], pa[2], pa[3]);
+#pragma unroll
+              for (int c = 0; c < 4; ++c) mma_16816(acc[i][c], pa, bq[c][0], bq[c][1]);
+            }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.empty[slot]);
       }
+      turn += batches;
     }
-    cp_async_wait<0>();
     __syncthreads();                       // the list and the ring are read
   }
 
-  // the groups' sums, one group after another
   float* red = reinterpret_cast<float*>(raw);
   constexpr int LA = CB + 8, LB = R + 4;
+  if (warp < WARPS) {
 #pragma unroll
-  for (int grp = 0; grp < NG; ++grp) {
-    if (wg == grp) {
+    for (int i = 0; i < RT; ++i)
 #pragma unroll
-      for (int i = 0; i < RT; ++i)
+      for (int c = 0; c < 4; ++c)
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int n = wc * 32 + c * 8 + 2 * t + (e & 1), j = 16 * i + g + 8 * (e >> 1);
-            float& at = red[which ? n * LB + j : j * LA + n];
-            at = grp ? at + acc[i][c][e] : acc[i][c][e];
-          }
-    }
-    __syncthreads();
+        for (int e = 0; e < 4; ++e) {
+          const int n = warp * 32 + c * 8 + 2 * t + (e & 1), j = 16 * i + g + 8 * (e >> 1);
+          red[which ? n * LB + j : j * LA + n] = acc[i][c][e];
+        }
   }
+  __syncthreads();
   __syncwarp();
   cluster_arrive();
   cluster_wait();
   // four neighbouring columns (dA) or ranks (dB) a thread
   const uint32_t base = smem_u32(red);
   const int e0 = CB * R / 4 * rank / S, e1 = CB * R / 4 * (rank + 1) / S;
-  for (int e = e0 + tid; e < e1; e += GRAD_THREADS) {
+  for (int e = e0 + tid; e < e1; e += GRAD_THREADS + COPY_THREADS) {
     const int n = which ? e / (R / 4) : 4 * (e % (CB / 4)), j = which ? 4 * (e % (R / 4)) : e / (CB / 4);
     if (c0 + n >= width || j >= p.r) continue;
     const uint32_t at = base + 4u * (uint32_t)(which ? n * LB + j : j * LA + n);
@@ -238,23 +256,23 @@ __global__ void __launch_bounds__(256 * NG) lora_grad_kernel(const GradArgs p) {
   cluster_wait();
 }
 
-template <int RT, int NG>
+template <int RT>
 cudaError_t launch_grad(const GradArgs& p, int blocks, int n, int num_sms, cudaStream_t stream) {
   static KernelLimits lim;
   constexpr int R = 16 * RT;
   size_t smem = grad_bytes(R);
   const size_t red = (size_t)(R * (CB + 8) > CB * (R + 4) ? R * (CB + 8) : CB * (R + 4)) * sizeof(float);
   if (smem < red) smem = red;
-  const void* kern = (const void*)lora_grad_kernel<RT, NG>;
+  const void* kern = (const void*)lora_grad_kernel<RT>;
   const cudaError_t e = ensure_kernel_limits(kern, lim, smem, false);
   if (e != cudaSuccess) return e;
   // (as if every adapter had as many rows; a CTA costs about eight batches' time besides its own)
   const int splits = pick_splits((long long)blocks * n, 1 + p.M / n / BR, 8, [&](int s) {
-    return resident_clusters(kern, lim, s == 8 ? 3 : s / 2, 256 * NG, smem, s, num_sms);
+    return resident_clusters(kern, lim, s == 8 ? 3 : s / 2, GRAD_THREADS + COPY_THREADS, smem, s, num_sms);
   });
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(blocks * splits), (unsigned)n);
-  cfg.blockDim = dim3(256 * NG);
+  cfg.blockDim = dim3(GRAD_THREADS + COPY_THREADS);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
@@ -266,12 +284,12 @@ cudaError_t launch_grad(const GradArgs& p, int blocks, int n, int num_sms, cudaS
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, lora_grad_kernel<RT, NG>, p);
+  return cudaLaunchKernelEx(&cfg, lora_grad_kernel<RT>, p);
 }
 
 }  // namespace
 
-cudaError_t launch_lora_grad(const LoraArgs& a, int num_sms, cudaStream_t stream) {
+cudaError_t launch_lora_grad(const LoraArgs& a, int num_sms, int* err, cudaStream_t stream) {
   GradArgs p{};
   p.x = a.x, p.dy = a.dy;
   p.t = a.t, p.u = a.u;
@@ -283,13 +301,14 @@ cudaError_t launch_lora_grad(const LoraArgs& a, int num_sms, cudaStream_t stream
   p.M = a.M;
   p.r = a.r;
   p.accumulate = a.accumulate;
+  p.err = err;
   p.drop = LoraDrop{a.seed, a.site, a.thr};
   const int blocks = p.blocks0 + (p.N + CB - 1) / CB;
   if (blocks == 0) return cudaSuccess;
-  if (a.r <= 16) return launch_grad<1, 2>(p, blocks, a.n, num_sms, stream);
-  if (a.r <= 32) return launch_grad<2, 2>(p, blocks, a.n, num_sms, stream);
-  if (a.r <= 64) return launch_grad<4, 2>(p, blocks, a.n, num_sms, stream);
-  return launch_grad<8, 1>(p, blocks, a.n, num_sms, stream);
+  if (a.r <= 16) return launch_grad<1>(p, blocks, a.n, num_sms, stream);
+  if (a.r <= 32) return launch_grad<2>(p, blocks, a.n, num_sms, stream);
+  if (a.r <= 64) return launch_grad<4>(p, blocks, a.n, num_sms, stream);
+  return launch_grad<8>(p, blocks, a.n, num_sms, stream);
 }
 
 }  // namespace cospec
