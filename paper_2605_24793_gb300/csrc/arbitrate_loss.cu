@@ -75,6 +75,12 @@ CS_DEV float2 add_pair(float2 s, float2 x) {
   return make_float2(t.x, __fadd_rn(t.y, x.y));
 }
 
+// Asks for [from, to) in L2: the 16-byte pieces that lie whole inside.
+CS_DEV void l2_prefetch(const void* from, const void* to) {
+  const uint64_t a = (reinterpret_cast<uint64_t>(from) + 15) & ~15ull, b = reinterpret_cast<uint64_t>(to) & ~15ull;
+  if (b > a) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a), "r"((uint32_t)(b - a)) : "memory");
+}
+
 struct Decision {
   float p, dz, surr, ent, kl;
 };
@@ -170,6 +176,15 @@ __global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs 
       }
     }
     cp_async_commit();
+    // what the step's decisions will gather comes to L2
+    if (tid == 0) {
+      const int e1 = min(base + step, total) - 1, r0 = base / a.K, r1 = e1 / a.K;
+      l2_prefetch(a.stats + ((long long)base + r0) * 5, a.stats + ((long long)e1 + r1 + 2) * 5);
+      l2_prefetch(a.adv + base, a.adv + e1 + 1);
+      l2_prefetch(a.p_old + base, a.p_old + e1 + 1);
+      l2_prefetch(a.p_ref + base, a.p_ref + e1 + 1);
+      l2_prefetch(a.accept + base, a.accept + e1 + 1);
+    }
   };
   if ((long long)blockIdx.x * step < total) fetch((int)blockIdx.x * step);
   for (long long base64 = (long long)blockIdx.x * step; base64 < total; base64 += (long long)gridDim.x * step) {

@@ -8,7 +8,7 @@
 // summed over micro-batches starts from fp32).
 //
 // A CTA takes 256 columns of one adapter, 32 a warp; the adapter's rows, listed in shared memory first, so that rows of
-// other adapters and what they hold are not read, come 32 at a time into a ring.  Four warps of their own copy them: by the
+// other adapters and what they hold are not read, come 32 at a time into a ring.  Warps of their own copy them: by the
 // computing warps the copies took half of a batch's time, and bulk copies of 512 bytes, a lane a row, are done one
 // after another and took twice as long altogether.  While a batch is multiplied the next one's P is split, once for all
 // warps, and its dropped elements are set to zero.  The rows are split over the CTAs of a cluster and joined in a fixed order.
@@ -22,7 +22,6 @@ constexpr int CB = 256;              // columns of a CTA
 constexpr int BR = 32;               // rows of a batch
 constexpr int GDEPTH = 4;            // batches in the ring, a power of two
 constexpr int GRAD_THREADS = 256;    // eight warps that compute
-constexpr int COPY_THREADS = 128;    // four that copy
 constexpr int WIN = 2048;            // rows listed at a time
 constexpr uint32_t Q_PITCH = CB * 2 + 16;   // of a row of Q: eight neighbouring rows start on different banks
 constexpr uint32_t Q_BYTES = BR * Q_PITCH;
@@ -54,11 +53,15 @@ __host__ __device__ constexpr uint32_t grad_bytes(int R) {
   return GDEPTH * grad_slot(R) + 2 * grad_p_bytes(R) + (uint32_t)sizeof(GradSmem);
 }
 
+// Threads that copy: two warps, so that two CTAs share an SM, or four (4096 rows of 2560 + 6144 at rank 16: 34 us with two, 38
+// with four; 2048 rows of 4096 + 4096 at rank 64: 63 and 57).
+__host__ __device__ constexpr int copy_threads(int rt) { return rt <= 2 ? 64 : 128; }
+
 // RT: ranks in sixteens.
 template <int RT>
-__global__ void __launch_bounds__(GRAD_THREADS + COPY_THREADS) lora_grad_kernel(const GradArgs p) {
+__global__ void __launch_bounds__(GRAD_THREADS + copy_threads(RT)) lora_grad_kernel(const GradArgs p) {
   extern __shared__ __align__(128) uint8_t raw[];
-  constexpr int R = 16 * RT, WARPS = GRAD_THREADS / 32;
+  constexpr int R = 16 * RT, WARPS = GRAD_THREADS / 32, COPY_THREADS = copy_threads(RT), COPY_WARPS = COPY_THREADS / 32;
   constexpr int PC = BR * R / 4;                       // 16-byte chunks of a batch's P
   constexpr uint32_t P_PART = (uint32_t)(BR * R * 2), SLOT = grad_slot(R), P_OFF = GDEPTH * SLOT;
   GradSmem& sm = *reinterpret_cast<GradSmem*>(raw + P_OFF + 2 * grad_p_bytes(R));
@@ -66,7 +69,7 @@ __global__ void __launch_bounds__(GRAD_THREADS + COPY_THREADS) lora_grad_kernel(
   const int S = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
   const int block = (int)blockIdx.x / S, which = block >= p.blocks0;
   const int c0 = (which ? block - p.blocks0 : block) * CB;
-  const int a = (int)blockIdx.y;
+  const int a = (int)blockIdx.y, j0 = (int)blockIdx.z * 64;      // adapter, first rank
   const __nv_bfloat16* Q = which ? p.dy : p.x;
   const float* P = which ? p.u : p.t;
   const long long ld = which ? p.ldy : p.ldx;
@@ -85,13 +88,19 @@ __global__ void __launch_bounds__(GRAD_THREADS + COPY_THREADS) lora_grad_kernel(
   LoraKey key{0, 0};
   if (drop) key = lora_key(p.drop);
 
-  float acc[RT][4][4];
+  // An mma truncates its running sum: after every eight batches the sums move on by rounded additions (4096 rows: relative error
+  // 3e-6 -> 1e-6).
+  float acc[RT][4][4], sum[RT][4][4];
+  auto each = [&](auto&& f) {
 #pragma unroll
-  for (int i = 0; i < RT; ++i)
+    for (int i = 0; i < RT; ++i)
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
+      for (int c = 0; c < 4; ++c)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[i][c][e] = 0.f;
+        for (int e = 0; e < 4; ++e) f(i, c, e);
+  };
+  each([&](int i, int c, int e) { acc[i][c][e] = sum[i][c][e] = 0.f; });
+  auto settle = [&]() { each([&](int i, int c, int e) { sum[i][c][e] += acc[i][c][e], acc[i][c][e] = 0.f; }); };
 
   // 2 R byte rows of P's parts; the 16-byte chunks exchanged by the row, so that eight neighbouring rows lie on different banks
   auto p_at = [&](int row, int c) {
@@ -122,7 +131,7 @@ __global__ void __launch_bounds__(GRAD_THREADS + COPY_THREADS) lora_grad_kernel(
     }
     const int batches = (have + BR - 1) / BR;
     if (warp >= WARPS) {
-      // a warp a row of Q, every fourth row; rows behind the last, columns behind the width and ranks behind the rank as zeros
+      // a warp a row of Q; rows behind the last, columns behind the width and ranks behind the rank as zeros
       const int ct = tid - GRAD_THREADS, cw = ct >> 5, col = c0 + 8 * lane;
       for (int b = 0; b < batches; ++b, ++turn) {
         const int slot = turn & (GDEPTH - 1), rows = min(BR, have - b * BR);
@@ -133,8 +142,8 @@ __global__ void __launch_bounds__(GRAD_THREADS + COPY_THREADS) lora_grad_kernel(
         const uint32_t dst = q0 + (uint32_t)slot * SLOT;
         const int* list = sm.list + b * BR;
 #pragma unroll
-        for (int i = 0; i < BR / 4; ++i) {
-          const int row = cw + 4 * i;
+        for (int i = 0; i < BR / COPY_WARPS; ++i) {
+          const int row = cw + COPY_WARPS * i;
           const bool on = row < rows && col < width;
           cp_async16(dst + (uint32_t)row * Q_PITCH + (uint32_t)lane * 16u, on ? Q + (long long)list[row] * ld + col : Q, on);
         }
@@ -142,8 +151,8 @@ __global__ void __launch_bounds__(GRAD_THREADS + COPY_THREADS) lora_grad_kernel(
         for (int i = 0; i * COPY_THREADS < PC; ++i) {
           const int e = ct + COPY_THREADS * i, row = e / (R / 4), j = 4 * (e % (R / 4));
           if (e >= PC) break;
-          const bool on = row < rows && j < p.r;
-          cp_async16(dst + Q_BYTES + (uint32_t)e * 16u, on ? P + (size_t)list[row] * p.r + j : P, on);
+          const bool on = row < rows && j0 + j < p.r;
+          cp_async16(dst + Q_BYTES + (uint32_t)e * 16u, on ? P + (size_t)list[row] * p.r + j0 + j : P, on);
         }
         cp_async_arrive(&sm.full[slot]);
       }
@@ -213,6 +222,7 @@ __global__ void __launch_bounds__(GRAD_THREADS + COPY_THREADS) lora_grad_kernel(
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.empty[slot]);
+        if ((b & 7) == 7 && b + 1 < batches) settle();
       }
       turn += batches;
     }
@@ -222,15 +232,10 @@ __global__ void __launch_bounds__(GRAD_THREADS + COPY_THREADS) lora_grad_kernel(
   float* red = reinterpret_cast<float*>(raw);
   constexpr int LA = CB + 8, LB = R + 4;
   if (warp < WARPS) {
-#pragma unroll
-    for (int i = 0; i < RT; ++i)
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int n = warp * 32 + c * 8 + 2 * t + (e & 1), j = 16 * i + g + 8 * (e >> 1);
-          red[which ? n * LB + j : j * LA + n] = acc[i][c][e];
-        }
+    each([&](int i, int c, int e) {
+      const int n = warp * 32 + c * 8 + 2 * t + (e & 1), j = 16 * i + g + 8 * (e >> 1);
+      red[which ? n * LB + j : j * LA + n] = sum[i][c][e] + acc[i][c][e];
+    });
   }
   __syncthreads();
   __syncwarp();
@@ -241,10 +246,10 @@ __global__ void __launch_bounds__(GRAD_THREADS + COPY_THREADS) lora_grad_kernel(
   const int e0 = CB * R / 4 * rank / S, e1 = CB * R / 4 * (rank + 1) / S;
   for (int e = e0 + tid; e < e1; e += GRAD_THREADS + COPY_THREADS) {
     const int n = which ? e / (R / 4) : 4 * (e % (CB / 4)), j = which ? 4 * (e % (R / 4)) : e / (CB / 4);
-    if (c0 + n >= width || j >= p.r) continue;
+    if (c0 + n >= width || j0 + j >= p.r) continue;
     const uint32_t at = base + 4u * (uint32_t)(which ? n * LB + j : j * LA + n);
     float4 s = S > 1 ? dsmem_sum4(at, S) : *reinterpret_cast<const float4*>(red + (which ? n * LB + j : j * LA + n));
-    float4* o = reinterpret_cast<float4*>(which ? p.db + ((size_t)a * width + c0 + n) * p.r + j : p.da + ((size_t)a * p.r + j) * width + c0 + n);
+    float4* o = reinterpret_cast<float4*>(which ? p.db + ((size_t)a * width + c0 + n) * p.r + j0 + j : p.da + ((size_t)a * p.r + j0 + j) * width + c0 + n);
     if (p.accumulate) {
       const float4 v = *o;
       s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
@@ -267,12 +272,12 @@ cudaError_t launch_grad(const GradArgs& p, int blocks, int n, int num_sms, cudaS
   const cudaError_t e = ensure_kernel_limits(kern, lim, smem, false);
   if (e != cudaSuccess) return e;
   // (as if every adapter had as many rows; a CTA costs about eight batches' time besides its own)
-  const int splits = pick_splits((long long)blocks * n, 1 + p.M / n / BR, 8, [&](int s) {
-    return resident_clusters(kern, lim, s == 8 ? 3 : s / 2, GRAD_THREADS + COPY_THREADS, smem, s, num_sms);
+  const int splits = pick_splits((long long)blocks * n * ((p.r + 63) / 64), 1 + p.M / n / BR, 8, [&](int s) {
+    return resident_clusters(kern, lim, s == 8 ? 3 : s / 2, GRAD_THREADS + copy_threads(RT), smem, s, num_sms);
   });
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(blocks * splits), (unsigned)n);
-  cfg.blockDim = dim3(GRAD_THREADS + COPY_THREADS);
+  cfg.gridDim = dim3((unsigned)(blocks * splits), (unsigned)n, (unsigned)((p.r + 63) / 64));
+  cfg.blockDim = dim3(GRAD_THREADS + copy_threads(RT));
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
@@ -307,8 +312,7 @@ cudaError_t launch_lora_grad(const LoraArgs& a, int num_sms, int* err, cudaStrea
   if (blocks == 0) return cudaSuccess;
   if (a.r <= 16) return launch_grad<1>(p, blocks, a.n, num_sms, stream);
   if (a.r <= 32) return launch_grad<2>(p, blocks, a.n, num_sms, stream);
-  if (a.r <= 64) return launch_grad<4>(p, blocks, a.n, num_sms, stream);
-  return launch_grad<8>(p, blocks, a.n, num_sms, stream);
+  return launch_grad<4>(p, blocks, a.n, num_sms, stream);
 }
 
 }  // namespace cospec
