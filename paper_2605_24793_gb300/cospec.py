@@ -812,7 +812,7 @@ def get_device_error(stream=None) -> int:
 # ---------------------------------------------------------------- low-rank adapters
 # These calls take many tensors and some take a few microseconds on the GPU, so what is right is checked in one pass over
 # (tensor, dtype, shape), and only what is not goes through the checks that name it.
-_BF16, _F32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+_U8 = torch.uint8
 
 
 def _all_fit(dev: int, specs) -> bool:
@@ -830,12 +830,8 @@ def _name_misfit(dev: int, specs, names) -> None:
             raise ValueError(f"{name}: tensor on {t.device}, but the current device is cuda:{dev}")
 
 
-def _current(stream):
-    """(current device, the stream's handle)."""
-    dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else torch.cuda.current_device() if torch.cuda.is_available() else 0
-    if stream is not None:
-        return dev, stream.cuda_stream
-    return dev, torch._C._cuda_getCurrentRawStream(dev) if torch.cuda.is_initialized() else 0
+def _device_now() -> int:
+    return _current() if torch.cuda.is_initialized() else 0
 
 
 def _rows_stride(t: torch.Tensor, name: str, dev: int, rows: int, width: int) -> int:
@@ -875,7 +871,7 @@ def lora_forward(x, w, a, b, scaling, adapter, y, u, dropout: float = 0.0, seed=
     b [n, N, r] bf16, scaling [n] float32, adapter [M] int32; fills y [M, N] bf16 and u [M, r] float32, which the backward
     pass reads.  x and y may be columns of wider buffers.  ``seed``: an int64 device scalar, read when the kernels run;
     ``site``: the number of the place whose dropout mask this is."""
-    dev, handle = _current(stream)
+    dev = _device_now()
     N, K, n, r, M = _lora_sizes(w, a, adapter)
     specs = ((w, _BF16, (N, K)), (a, _BF16, (n, r, K)), (b, _BF16, (n, N, r)), (scaling, _F32, (n,)), (adapter, _I32, (M,)), (u, _F32, (M, r)))
     if not _all_fit(dev, specs):
@@ -884,7 +880,7 @@ def lora_forward(x, w, a, b, scaling, adapter, y, u, dropout: float = 0.0, seed=
     d = LoraDims(M, K, N, r, n, dropout, site, _rows_stride(x, "x", dev, M, K), _rows_stride(y, "y", dev, M, N), 0)
     _check(load_library().cospec_lora_forward(
         ctypes.byref(d), x.data_ptr(), w.data_ptr(), a.data_ptr(), b.data_ptr(), scaling.data_ptr(), adapter.data_ptr(),
-        None if seed is None else seed.data_ptr(), u.data_ptr(), y.data_ptr(), handle))
+        _at(seed), u.data_ptr(), y.data_ptr(), _stream_ptr(stream, dev)))
     return y
 
 
@@ -893,7 +889,7 @@ def lora_backward(dy, x, w, a, b, scaling, adapter, u, dx, da, db, t, dropout: f
     """The gradients of lora_forward for x and the adapters: dx [M, K] bf16, da [n, r, K] and db [n, N, r] float32 (each
     or None), from dy [M, N], the forward pass's inputs and its u.  t [M, r] float32 is scratch.  ``accumulate``: da and
     db are added to."""
-    dev, handle = _current(stream)
+    dev = _device_now()
     N, K, n, r, M = _lora_sizes(w, a, adapter)
     specs = [(w, _BF16, (N, K)), (a, _BF16, (n, r, K)), (b, _BF16, (n, N, r)), (scaling, _F32, (n,)), (adapter, _I32, (M,)), (u, _F32, (M, r)),
              (t, _F32, (M, r))]
@@ -908,8 +904,8 @@ def lora_backward(dy, x, w, a, b, scaling, adapter, u, dx, da, db, t, dropout: f
                  0 if dx is None else _rows_stride(dx, "dx", dev, M, K))
     _check(load_library().cospec_lora_backward(
         ctypes.byref(d), dy.data_ptr(), x.data_ptr(), w.data_ptr(), a.data_ptr(), b.data_ptr(), scaling.data_ptr(), adapter.data_ptr(),
-        None if seed is None else seed.data_ptr(), u.data_ptr(), t.data_ptr(), None if dx is None else dx.data_ptr(),
-        None if da is None else da.data_ptr(), None if db is None else db.data_ptr(), LORA_ACCUMULATE if accumulate else 0, handle))
+        _at(seed), u.data_ptr(), t.data_ptr(), _at(dx),
+        _at(da), _at(db), LORA_ACCUMULATE if accumulate else 0, _stream_ptr(stream, dev)))
     return dx, da, db
 
 
@@ -926,7 +922,7 @@ def arbitrate_loss(draft, argmax, stats, w1, b1, w2, b2, accept, eff, adv, p_old
     gradients times ``grad_scale``) and ``ws``; ``out``: an earlier call's result, whose tensors are filled again (give one
     where ``stream`` is not the current stream)."""
     params = params if params is not None else RLParams()
-    dev, handle = _current(stream)
+    dev = _device_now()
     _need(draft.dim() == 2 and w1.dim() == 2, "draft must be [R, K], w1 [H, 8]")
     (R, K), H = draft.shape, w1.shape[0]
     specs = ((draft, _I32, (R, K)), (argmax, _I32, (R, K + 1)), (stats, _F32, (R, K + 1, 5)), (w1, _F32, (H, 8)), (b1, _F32, (H,)), (w2, _F32, (H,)),
@@ -936,7 +932,7 @@ def arbitrate_loss(draft, argmax, stats, w1, b1, w2, b2, accept, eff, adv, p_old
     lib = load_library()
     shapes = ((4,), (R, K), (R, K), (H, 8), (H,), (H,), (1,))
     if out is None:
-        if stream is not None and stream.cuda_stream != _current(None)[1]:
+        if stream is not None and stream.cuda_stream != _stream_ptr(None, dev):
             raise ValueError("out must be given where stream is not the current stream (its tensors belong to the current one)")
         out = {n: torch.empty(s, dtype=_F32, device=draft.device) for n, s in zip(_LOSS_OUT, shapes)}
         out["ws"] = torch.empty(max(1, lib.cospec_arbitrate_loss_workspace(H)), dtype=_U8, device=draft.device)
@@ -948,5 +944,5 @@ def arbitrate_loss(draft, argmax, stats, w1, b1, w2, b2, accept, eff, adv, p_old
     _check(lib.cospec_arbitrate_loss(
         R, K, draft.data_ptr(), argmax.data_ptr(), stats.data_ptr(), H, w1.data_ptr(), b1.data_ptr(), w2.data_ptr(), b2.data_ptr(), accept.data_ptr(),
         eff.data_ptr(), adv.data_ptr(), p_old.data_ptr(), p_ref.data_ptr(), ctypes.byref(params), grad_scale, *[t.data_ptr() for t in res],
-        ws.data_ptr(), ws.numel(), handle))
+        ws.data_ptr(), ws.numel(), _stream_ptr(stream, dev)))
     return out

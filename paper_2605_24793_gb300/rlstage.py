@@ -1,7 +1,8 @@
-"""Timing of the RL stage's reward shaping and advantages (Sec. 3.4) on a
-synthetic rollout batch, through ``cospec_rl_advantages``.
+"""One policy update's arithmetic of the RL stage (Sec. 3.4) on a synthetic rollout batch: reward
+shaping and advantages (``cospec_rl_advantages``), then the clipped objective through the decision MLP with the
+gradients of its weights (``cospec_arbitrate_loss``).
 
-  python -m paper_2605_24793_gb300.rlstage --groups 256 --rollouts 8 --rounds 64 --k 25
+  python -m paper_2605_24793_gb300.rlstage --groups 256 --rollouts 8 --rounds 64 --k 25 --hidden 256
 """
 from __future__ import annotations
 
@@ -14,12 +15,40 @@ from . import cospec as C
 from . import workload as W
 
 
+class PolicyStep:
+    """Recorded rounds and a decision MLP; ``run`` fills the advantages and the loss with its gradients.  The records:
+    draft, argmax, stats as cospec_arbitrate takes them, p_old and accept as it gave them, ell = log p_T of the drafts, the rollouts'
+    offsets and outcomes as cospec_rl_advantages takes them."""
+
+    def __init__(self, group_off, correct, round_off, draft, argmax, stats, mlp, p_old, p_ref, accept, params: C.RLParams = None):
+        self.offsets = (group_off, correct, round_off)
+        self.draft, self.argmax, self.stats, self.mlp = draft, argmax, stats, mlp
+        self.p_old, self.p_ref, self.accept = p_old, p_ref, accept
+        self.params = params if params is not None else C.RLParams()
+        K = draft.shape[1]
+        self.match = (draft == argmax[:, :K]).to(torch.uint8)
+        self.ell = (stats[:, :K, 4] - stats[:, :K, 2]).contiguous()
+        self.out = None
+
+    def advantages(self) -> dict:
+        go, co, ro = self.offsets
+        return C.rl_advantages(go, co, ro, self.match, self.accept, self.ell, self.params)
+
+    def run(self) -> dict:
+        adv = self.advantages()
+        n = max(1, self.draft.shape[0])
+        self.out = C.arbitrate_loss(self.draft, self.argmax, self.stats, *self.mlp, self.accept, adv["eff"], adv["adv_dec"], self.p_old, self.p_ref,
+                                    self.params, grad_scale=1.0 / n, out=self.out)
+        return self.out
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--groups", type=int, default=256)
     ap.add_argument("--rollouts", type=int, default=8)
     ap.add_argument("--rounds", type=int, default=64)
     ap.add_argument("--k", type=int, default=25)
+    ap.add_argument("--hidden", type=int, default=256, help="units of the decision MLP")
     ap.add_argument("--steps", type=int, default=50)
     args = ap.parse_args()
     from . import build as B
@@ -42,6 +71,24 @@ def main():
     print(json.dumps({"groups": args.groups, "rollouts": args.groups * args.rollouts, "rounds": R,
                       "k": args.k, "decisions": R * args.k, "ms_per_call": ms,
                       "note": "per call incl. output allocation in the binding",
+                      "device_error": C.get_device_error()}))
+    draft, argmax, stats, w1, b1, w2, b2 = [torch.from_numpy(a).cuda() for a in W.policy_rounds(1, R, args.k, args.hidden)]
+    p = torch.empty((R, args.k), device="cuda")
+    act = torch.empty((R, args.k), dtype=torch.uint8, device="cuda")
+    C.arbitrate(draft, argmax, stats, w1, b1, w2, float(b2), 0.5, C.POLICY_MLP, p, act)
+    act |= torch.rand((R, args.k), device="cuda") < 0.5             # the behaviour policy draws
+    p.clamp_(0.02, 0.98)
+    step = PolicyStep(go, co, ro, draft, argmax, stats, (w1, b1, w2, b2), p, (p + 0.05 * torch.randn_like(p)).clamp_(0.02, 0.98), act)
+    for _ in range(3):
+        step.run()
+    torch.cuda.synchronize()
+    e0.record()
+    for _ in range(args.steps):
+        step.run()
+    e1.record()
+    e1.synchronize()
+    print(json.dumps({"rounds": R, "k": args.k, "hidden": args.hidden, "ms_per_step": e0.elapsed_time(e1) / args.steps,
+                      "loss": step.out["loss"].tolist(), "what": "advantages, then the loss and its gradients",
                       "device_error": C.get_device_error()}))
 
 

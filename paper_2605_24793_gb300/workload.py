@@ -306,6 +306,25 @@ def rl_batch(seed: int, groups: int, rollouts: int, rounds: int, k: int,
     return group_off, correct, round_off, match, accept, ell
 
 
+def policy_rounds(seed: int, rounds: int, k: int, hidden: int, mismatch_rate: float = 0.3):
+    """Synthetic records of ``rounds`` rounds for the policy loss, and a decision MLP with nn.Linear's default law: draft, argmax,
+    the LM head's statistics (the bonus row scores no draft) and w1, b1, w2, b2.  NumPy arrays."""
+    rng = np.random.default_rng(seed)
+    argmax = rng.integers(0, 1 << 17, (rounds, k + 1)).astype(np.int32)
+    match = rng.random((rounds, k)) >= mismatch_rate
+    draft = np.where(match, argmax[:, :k], argmax[:, :k] + 1).astype(np.int32)
+    top = rng.normal(6.0, 1.5, (rounds, k + 1))
+    st = np.empty((rounds, k + 1, 5), dtype=np.float32)
+    st[..., 0] = top
+    st[..., 1] = top - rng.exponential(0.7, top.shape)
+    st[..., 2] = top + 4.0 * rng.random(top.shape)
+    st[..., 3] = 4.0 * rng.random(top.shape)
+    st[:, :k, 4] = np.where(match, st[:, :k, 0], st[:, :k, 0] - rng.exponential(1.5, (rounds, k)))
+    st[:, k, 4] = np.nan
+    uni = lambda n, fan: (rng.uniform(-1, 1, n) / math.sqrt(fan)).astype(np.float32)  # noqa: E731
+    return draft, argmax, st, uni((hidden, NUM_FEATURES), NUM_FEATURES), uni(hidden, NUM_FEATURES), uni(hidden, hidden), uni(1, hidden)
+
+
 def draft_distributions(cfg: RoundConfig, logits: np.ndarray, noise: float = 1.0,
                         temperature: float = 1.0, round_index: int = 0) -> np.ndarray:
     """A stand-in for the draft model's distributions at the K draft
