@@ -34,7 +34,7 @@ constexpr int CLUSTER = 8;                // CTAs that join their sums
 constexpr int FIN_THREADS = 1024;
 
 struct LossSmem {
-  float feat[BATCH][16];                  // every feature twice: an operand of both units of a pair
+  float feat[BATCH][8];
   float adv[BATCH], old[BATCH], ref[BATCH], g[BATCH];
   int at[BATCH];                          // position in the step | action taken << 31
   uint16_t list[STEP];                    // effective positions of the step
@@ -80,6 +80,11 @@ CS_DEV void l2_prefetch(const void* from, const void* to) {
   const uint64_t a = (reinterpret_cast<uint64_t>(from) + 15) & ~15ull, b = reinterpret_cast<uint64_t>(to) & ~15ull;
   if (b > a) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a), "r"((uint32_t)(b - a)) : "memory");
 }
+
+// Two multiply-adds by one factor.  (Not as one packed instruction: that takes the same time in the pipe and wants the factor
+// twice, and features held twice made the shared memory's 128 bytes a clock the bound: a step's products 288 cycles where
+// these take 195.)
+CS_DEV float2 fma_pair(float2 a, float f, float2 c) { return make_float2(fmaf(a.x, f, c.x), fmaf(a.y, f, c.y)); }
 
 struct Decision {
   float p, dz, surr, ent, kl;
@@ -264,10 +269,9 @@ __global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs 
           if (word * 32 < lo) m &= 0xffffffffu << (lo & 31);
           before += __popc(m);
         }
-        const float f[8] = {x4 - x2, x0 - x2, x0 - x1, x3, y0 - y2, i + 1 < a.K ? y4 - y2 : 0.f, (float)(i + 1) * inv_k, (float)before * inv_k};
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          *reinterpret_cast<float4*>(&sm.feat[d][4 * k]) = make_float4(f[2 * k], f[2 * k], f[2 * k + 1], f[2 * k + 1]);
+        float4* f = reinterpret_cast<float4*>(sm.feat[d]);
+        f[0] = make_float4(x4 - x2, x0 - x2, x0 - x1, x3);
+        f[1] = make_float4(y0 - y2, i + 1 < a.K ? y4 - y2 : 0.f, (float)(i + 1) * inv_k, (float)before * inv_k);
         sm.adv[d] = adv;
         sm.old[d] = old;
         sm.ref[d] = ref;
@@ -279,19 +283,14 @@ __global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs 
         unsigned bits = 0;
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
-          float2 f[8];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float4 v = *reinterpret_cast<const float4*>(&sm.feat[4 * q + d][4 * k]);
-            f[2 * k] = make_float2(v.x, v.y);
-            f[2 * k + 1] = make_float2(v.z, v.w);
-          }
+          const float4 fa = *reinterpret_cast<const float4*>(&sm.feat[4 * q + d][0]), fb = *reinterpret_cast<const float4*>(&sm.feat[4 * q + d][4]);
+          const float f[8] = {fa.x, fa.y, fa.z, fa.w, fb.x, fb.y, fb.z, fb.w};
           float2 zz = make_float2(0.f, 0.f);
 #pragma unroll
           for (int i = 0; i < PP; ++i) {
             float2 v = b1[i];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v = fma2(w1[i][k], f[k], v);
+            for (int k = 0; k < 8; ++k) v = fma_pair(w1[i][k], f[k], v);
             bits = __funnelshift_l(__float_as_uint(v.x), bits, 1);
             bits = __funnelshift_l(__float_as_uint(v.y), bits, 1);
             zz = fma2(w2[i], make_float2(fmaxf(-v.x, 0.f), fmaxf(-v.y, 0.f)), zz);
@@ -335,20 +334,15 @@ __global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs 
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
           if (4 * q + d >= count) break;     // what stands there is of another batch
-          float2 f[8];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float4 v = *reinterpret_cast<const float4*>(&sm.feat[4 * q + d][4 * k]);
-            f[2 * k] = make_float2(v.x, v.y);
-            f[2 * k + 1] = make_float2(v.z, v.w);
-          }
+          const float4 fa = *reinterpret_cast<const float4*>(&sm.feat[4 * q + d][0]), fb = *reinterpret_cast<const float4*>(&sm.feat[4 * q + d][4]);
+          const float f[8] = {fa.x, fa.y, fa.z, fa.w, fb.x, fb.y, fb.z, fb.w};
           const float g = sm.g[4 * q + d];
 #pragma unroll
           for (int i = 0; i < PP; ++i) {
             constexpr int TOP = 8 * PP - 1;          // the first unit's bit
           const float2 m = make_float2((bits >> (TOP - 2 * (PP * d + i))) & 1u ? g : 0.f, (bits >> (TOP - 1 - 2 * (PP * d + i))) & 1u ? g : 0.f);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) S[i][k] = fma2(m, f[k], S[i][k]);
+            for (int k = 0; k < 8; ++k) S[i][k] = fma_pair(m, f[k], S[i][k]);
             S[i][8] = add2(S[i][8], m);
           }
         }
