@@ -813,6 +813,7 @@ def get_device_error(stream=None) -> int:
 # These calls take many tensors and some take a few microseconds on the GPU, so what is right is checked in one pass over
 # (tensor, dtype, shape), and only what is not goes through the checks that name it.
 _U8 = torch.uint8
+_lora_dims_kept: dict = {}
 
 
 def _all_fit(dev: int, specs) -> bool:
@@ -877,9 +878,9 @@ def lora_forward(x, w, a, b, scaling, adapter, y, u, dropout: float = 0.0, seed=
     if not _all_fit(dev, specs):
         _name_misfit(dev, specs, ("w", "a", "b", "scaling", "adapter", "u"))
     _check_seed(seed, site, dev)
-    d = LoraDims(M, K, N, r, n, dropout, site, _rows_stride(x, "x", dev, M, K), _rows_stride(y, "y", dev, M, N), 0)
+    key = (M, K, N, r, n, dropout, site, _rows_stride(x, "x", dev, M, K), _rows_stride(y, "y", dev, M, N), 0)
     _check(load_library().cospec_lora_forward(
-        ctypes.byref(d), x.data_ptr(), w.data_ptr(), a.data_ptr(), b.data_ptr(), scaling.data_ptr(), adapter.data_ptr(),
+        _lora_dims_kept.get(key) or _keep(_lora_dims_kept, key, lambda: LoraDims(*key)), x.data_ptr(), w.data_ptr(), a.data_ptr(), b.data_ptr(), scaling.data_ptr(), adapter.data_ptr(),
         _at(seed), u.data_ptr(), y.data_ptr(), _stream_ptr(stream, dev)))
     return y
 
@@ -900,10 +901,10 @@ def lora_backward(dy, x, w, a, b, scaling, adapter, u, dx, da, db, t, dropout: f
     if not _all_fit(dev, specs):
         _name_misfit(dev, specs, ["w", "a", "b", "scaling", "adapter", "u", "t"] + ["da"] * (da is not None) + ["db"] * (db is not None))
     _check_seed(seed, site, dev)
-    d = LoraDims(M, K, N, r, n, dropout, site, _rows_stride(x, "x", dev, M, K), _rows_stride(dy, "dy", dev, M, N),
-                 0 if dx is None else _rows_stride(dx, "dx", dev, M, K))
+    key = (M, K, N, r, n, dropout, site, _rows_stride(x, "x", dev, M, K), _rows_stride(dy, "dy", dev, M, N),
+           0 if dx is None else _rows_stride(dx, "dx", dev, M, K))
     _check(load_library().cospec_lora_backward(
-        ctypes.byref(d), dy.data_ptr(), x.data_ptr(), w.data_ptr(), a.data_ptr(), b.data_ptr(), scaling.data_ptr(), adapter.data_ptr(),
+        _lora_dims_kept.get(key) or _keep(_lora_dims_kept, key, lambda: LoraDims(*key)), dy.data_ptr(), x.data_ptr(), w.data_ptr(), a.data_ptr(), b.data_ptr(), scaling.data_ptr(), adapter.data_ptr(),
         _at(seed), u.data_ptr(), t.data_ptr(), _at(dx),
         _at(da), _at(db), LORA_ACCUMULATE if accumulate else 0, _stream_ptr(stream, dev)))
     return dx, da, db

@@ -24,6 +24,8 @@ std::mutex g_limits_mutex;
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+}  // namespace
+
 // The calling thread's device, with its primary context made current the
 // first time (a host thread that has made no CUDA call yet has no current
 // context, and the tensor-map encoder needs one).
@@ -37,7 +39,6 @@ int current_device() {
   }
   return dev;
 }
-}  // namespace
 
 int device_num_sms() {
   const int dev = current_device();
@@ -85,8 +86,7 @@ cudaError_t ensure_kernel_limits(const void* kern, KernelLimits& lim, size_t sme
   return cudaSuccess;
 }
 
-int resident_clusters(const void* kern, KernelLimits& lim, int key, int threads, size_t smem_bytes, int S, int num_sms) {
-  const int dev = current_device();
+int resident_clusters(const void* kern, KernelLimits& lim, int dev, int key, int threads, size_t smem_bytes, int S, int num_sms) {
   if (dev < 0 || dev >= KL_MAX_DEV) return num_sms / S > 0 ? num_sms / S : 1;
   int n = lim.resident[dev][key].load(std::memory_order_relaxed);
   if (n == 0) {

@@ -109,6 +109,29 @@ CS_DEV Decision decide(float z, float adv, float old, float ref, bool took, cons
   return d;
 }
 
+// The gradients of unit h from its nine sums (hi + lo).  w1 . S + b1 S_8 cancels: its products as pairs.
+CS_DEV void unit_gradients(const ArbLossArgs& a, int h, const float2 (&t)[9]) {
+  const float w2 = a.w2[h];
+  float2 dw2 = make_float2(0.f, 0.f);
+#pragma unroll
+  for (int k = 0; k < 9; ++k) {
+    if (k < 8) a.dw1[(size_t)h * 8 + k] = fmaf(w2, t[k].x, w2 * t[k].y);
+    else a.db1[h] = fmaf(w2, t[k].x, w2 * t[k].y);
+    const float w = k < 8 ? a.w1[(size_t)h * 8 + k] : a.b1[h], prod = w * t[k].x;
+    dw2 = add_pair(dw2, make_float2(prod, fmaf(w, t[k].x, -prod) + w * t[k].y));
+  }
+  a.dw2[h] = dw2.x + dw2.y;
+}
+// The loss from its terms and the sum of dz.
+CS_DEV void write_loss(const ArbLossArgs& a, const float2 (&v)[4]) {
+  const double surr = (double)v[0].x + (double)v[0].y, ent = (double)v[1].x + (double)v[1].y, kl = (double)v[2].x + (double)v[2].y;
+  a.loss[0] = (float)surr;
+  a.loss[1] = (float)ent;
+  a.loss[2] = (float)kl;
+  a.loss[3] = (float)(-surr - (double)a.beta_h * ent + (double)a.beta_kl * kl);
+  *a.db2 = v[3].x + v[3].y;
+}
+
 // PP: pairs of units of a thread; TW: warps that hold all units.
 template <int PP, int TW>
 __global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs a, float* ws_s, float2* ws_l, int step) {
@@ -386,23 +409,37 @@ __global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs 
   cluster_wait();
   const int CS = (int)cluster_nctarank(), rank = (int)cluster_ctarank(), group = (int)blockIdx.x / CS;
   const uint32_t red0 = smem_u32(red);
-  float* out = ws_s + (size_t)group * 9 * HP;
-  for (int e = rank * THREADS + tid; e < 9 * HP; e += CS * THREADS) {
-    out[e] = dsmem_sum(red0 + 4u * (uint32_t)e, CS);
+  if ((int)gridDim.x == CS) {              // one cluster: its sums are all there is
+    for (int h = rank * THREADS + tid; h < a.H; h += CS * THREADS) {
+      float2 t[9];
+#pragma unroll
+      for (int k = 0; k < 9; ++k) t[k] = make_float2(dsmem_sum(red0 + 4u * (uint32_t)(k * HP + h), CS), 0.f);
+      unit_gradients(a, h, t);
+    }
+  } else {
+    float* out = ws_s + (size_t)group * 9 * HP;
+    for (int e = rank * THREADS + tid; e < 9 * HP; e += CS * THREADS) out[e] = dsmem_sum(red0 + 4u * (uint32_t)e, CS);
   }
-  if (rank == 0 && tid < 4) {
+  if (rank == 0 && warp == 0) {
     float2 w[CLUSTER], v = make_float2(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < CLUSTER; ++i) {
       w[i] = make_float2(0.f, 0.f);
-      if (i < CS)
+      if (i < CS && lane < 4)
         asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];"
                      : "=f"(w[i].x), "=f"(w[i].y)
-                     : "r"(dsmem_map(smem_u32(&lsum[tid]), (uint32_t)i)));
+                     : "r"(dsmem_map(smem_u32(&lsum[lane]), (uint32_t)i)));
     }
 #pragma unroll
     for (int i = 0; i < CLUSTER; ++i) v = add_pair(v, w[i]);
-    ws_l[(size_t)group * 4 + tid] = v;
+    if ((int)gridDim.x == CS) {
+      float2 all[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) all[k] = make_float2(__shfl_sync(0xffffffffu, v.x, k), __shfl_sync(0xffffffffu, v.y, k));
+      if (lane == 0) write_loss(a, all);
+    } else if (lane < 4) {
+      ws_l[(size_t)group * 4 + lane] = v;
+    }
   }
   __syncwarp();
   cluster_arrive();                        // nobody leaves while its sums are read
@@ -415,14 +452,6 @@ __global__ void __launch_bounds__(FIN_THREADS) arb_loss_finish_kernel(const ArbL
   __shared__ float2 part[27][32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int h = blockIdx.x * 32 + lane;
-  float w1[8], b1 = 0.f, w2 = 0.f;
-  if (warp == 0 && h < a.H) {
-    // (weights: not written by the kernel before)
-    w2 = a.w2[h];
-    b1 = a.b1[h];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) w1[k] = a.w1[(size_t)h * 8 + k];
-  }
   griddep_wait();
   griddep_launch_dependents();
   if (warp < 27) {
@@ -443,28 +472,14 @@ __global__ void __launch_bounds__(FIN_THREADS) arb_loss_finish_kernel(const ArbL
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1)
         v[k] = add_pair(v[k], make_float2(__shfl_xor_sync(0xffffffffu, v[k].x, o), __shfl_xor_sync(0xffffffffu, v[k].y, o)));
-    if (lane == 0) {
-      const double surr = (double)v[0].x + (double)v[0].y, ent = (double)v[1].x + (double)v[1].y, kl = (double)v[2].x + (double)v[2].y;
-      a.loss[0] = (float)surr;
-      a.loss[1] = (float)ent;
-      a.loss[2] = (float)kl;
-      a.loss[3] = (float)(-surr - (double)a.beta_h * ent + (double)a.beta_kl * kl);
-      *a.db2 = v[3].x + v[3].y;
-    }
+    if (lane == 0) write_loss(a, v);
   }
   __syncthreads();
   if (warp == 0 && h < a.H) {
-    float2 dw2 = make_float2(0.f, 0.f);
+    float2 t[9];
 #pragma unroll
-    for (int k = 0; k < 9; ++k) {
-      const float2 t = add_pair(add_pair(part[k][lane], part[9 + k][lane]), part[18 + k][lane]);
-      if (k < 8) a.dw1[(size_t)h * 8 + k] = fmaf(w2, t.x, w2 * t.y);
-      else a.db1[h] = fmaf(w2, t.x, w2 * t.y);
-      // w1 . S + b1 S_8 cancels: the products as pairs
-      const float w = k < 8 ? w1[k & 7] : b1, prod = w * t.x;
-      dw2 = add_pair(dw2, make_float2(prod, fmaf(w, t.x, -prod) + w * t.y));
-    }
-    a.dw2[h] = dw2.x + dw2.y;
+    for (int k = 0; k < 9; ++k) t[k] = add_pair(add_pair(part[k][lane], part[9 + k][lane]), part[18 + k][lane]);
+    unit_gradients(a, h, t);
   }
 }
 
@@ -481,14 +496,14 @@ cudaError_t launch_loss(const ArbLossArgs& a, int num_sms, cudaStream_t stream) 
   if (e != cudaSuccess) return e;
   // as many positions a step as give every CTA one, up to 2048; clusters of eight where there are that many CTAs
   const long long total = (long long)a.n * a.K;
-  int most = CLUSTER * resident_clusters((const void*)arb_loss_kernel<PP, TW>, lim, 0, THREADS, smem, CLUSTER, num_sms);
+  int most = CLUSTER * resident_clusters((const void*)arb_loss_kernel<PP, TW>, lim, current_device(), 0, THREADS, smem, CLUSTER, num_sms);
   if (most > MAX_CTAS) most = MAX_CTAS;
   if (most < 1) most = 1;
   long long step = ((total + most - 1) / most + THREADS - 1) / THREADS * THREADS;
   step = step < THREADS ? THREADS : step > STEP ? STEP : step;
   const long long steps = (total + step - 1) / step;
   int ctas = steps < 1 ? 1 : steps < most ? (int)steps : most;
-  const int cs = ctas >= CLUSTER ? CLUSTER : 1;
+  const int cs = ctas < CLUSTER ? ctas : CLUSTER;        // up to eight CTAs are one cluster, which finishes by itself
   ctas = (ctas + cs - 1) / cs * cs;
   float2* ws_l = static_cast<float2*>(a.ws);
   float* ws_s = reinterpret_cast<float*>(ws_l + (size_t)MAX_CTAS * 4);
@@ -507,7 +522,7 @@ cudaError_t launch_loss(const ArbLossArgs& a, int num_sms, cudaStream_t stream) 
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   e = cudaLaunchKernelEx(&cfg, arb_loss_kernel<PP, TW>, a, ws_s, ws_l, (int)step);
-  if (e != cudaSuccess) return e;
+  if (e != cudaSuccess || ctas == cs) return e;
   return launch_pdl(arb_loss_finish_kernel, dim3((a.H + 31) / 32), dim3(FIN_THREADS), 0, stream, a, (const float*)ws_s, (const float2*)ws_l, ctas / cs, HP);
 }
 

@@ -31,6 +31,7 @@ cudaError_t launch_pdl(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t sme
   return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
+int current_device();        // the calling thread's, its primary context current; -1 on failure
 int device_num_sms();
 int* device_error_word();  // device address of the error word of the current device
 
@@ -56,11 +57,11 @@ int cuda_lookup_failed();
 cudaError_t ensure_kernel_limits(const void* kern, KernelLimits& lim, size_t smem_bytes,
                                  bool cluster);
 
-// How many clusters of S CTAs of `kern` are resident at once on the current device, asked
+// How many clusters of S CTAs of `kern` are resident at once on the current device, `dev`, asked
 // once per device and `key` (0 .. 15: the caller's number for this S, block and shared memory).
 // The first question also asks for the whole of an SM's shared memory: with the carve-out the
 // driver picks by itself an SM took one CTA where two fit.
-int resident_clusters(const void* kern, KernelLimits& lim, int key, int threads, size_t smem_bytes, int S, int num_sms);
+int resident_clusters(const void* kern, KernelLimits& lim, int dev, int key, int threads, size_t smem_bytes, int S, int num_sms);
 // The S in {1, 2, 4, 8} with the least time for `units` clusters that share out `work` steps each: waves
 // of resident clusters, each a CTA's share and `fixed` steps besides.  `work` >= 1.
 template <typename Room>

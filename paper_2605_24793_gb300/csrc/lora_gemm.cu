@@ -484,10 +484,11 @@ cudaError_t launch_tile(const CUtensorMap& w, const CUtensorMap& x, const CUtens
   // The split with the least blocks of the contraction one after another: waves of resident clusters, each a split's
   // share and what a CTA costs besides (about four stages' time).
   const int tiles = (p.F + BM - 1) / BM * ((p.M + p.nt - 1) / p.nt), kblocks = (p.C + BK - 1) / BK;
+  const int dev = current_device();
   int splits = 1;
   long long best = 0;
   for (int s = 1; s <= 8 && s <= kblocks; ++s) {
-    const int room = resident_clusters((const void*)lora_tile_kernel<MN, DROP>, lim, s, 256, 227 * 1024, s, num_sms);
+    const int room = resident_clusters((const void*)lora_tile_kernel<MN, DROP>, lim, dev, s, 256, 227 * 1024, s, num_sms);
     const long long cost = (long long)((tiles + room - 1) / room) * ((kblocks + s - 1) / s + 8);
     if (best == 0 || cost < best) best = cost, splits = s;
   }

@@ -272,8 +272,9 @@ cudaError_t launch_grad(const GradArgs& p, int blocks, int n, int num_sms, cudaS
   const cudaError_t e = ensure_kernel_limits(kern, lim, smem, false);
   if (e != cudaSuccess) return e;
   // (as if every adapter had as many rows; a CTA costs about eight batches' time besides its own)
+  const int dev = current_device();
   const int splits = pick_splits((long long)blocks * n * ((p.r + 63) / 64), 1 + p.M / n / BR, 8, [&](int s) {
-    return resident_clusters(kern, lim, s == 8 ? 3 : s / 2, GRAD_THREADS + copy_threads(RT), smem, s, num_sms);
+    return resident_clusters(kern, lim, dev, s == 8 ? 3 : s / 2, GRAD_THREADS + copy_threads(RT), smem, s, num_sms);
   });
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(blocks * splits), (unsigned)n, (unsigned)((p.r + 63) / 64));

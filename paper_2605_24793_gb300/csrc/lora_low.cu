@@ -353,8 +353,9 @@ cudaError_t launch_low_tile(const LowArgs& p, int tiles, int num_sms, cudaStream
   const cudaError_t e = ensure_kernel_limits(kern, lim, smem, false);
   if (e != cudaSuccess) return e;
   // (a CTA costs about ten chunks' time besides its chunks)
+  const int dev = current_device();
   const int splits = pick_splits(tiles, (p.C + CK - 1) / CK, 10, [&](int s) {
-    return resident_clusters(kern, lim, 4 * p.rw_log2 - 4 + (s == 8 ? 3 : s / 2), LOW_THREADS, smem, s, num_sms);
+    return resident_clusters(kern, lim, dev, 4 * p.rw_log2 - 4 + (s == 8 ? 3 : s / 2), LOW_THREADS, smem, s, num_sms);
   });
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * splits));
