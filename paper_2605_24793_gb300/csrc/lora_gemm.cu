@@ -954,8 +954,9 @@ cudaError_t launch_lora_gemm(const LoraArgs& a, bool backward, int num_sms, int*
   p.err = err;
   const bool drop = p.drop.thr != 0u;
   const int kblocks = (p.C + BK - 1) / BK;
-  // Above 256 rows a CTA pair's tiles, of the size that leaves the fewest pairs idle: a tile takes the bytes of its
-  // operands (its rows and 256 features) and about four stages' time besides.
+  // Above 96 rows a CTA pair's tiles (whole forward passes in us, one CTA a tile / pairs: 64 rows 2560 -> 6144 13.7 / 16.2, 4096 -> 1024
+  // 10.0 / 21.8; 160 rows 512 -> 512 13.4 / 11.4, 4096 -> 4096 20.1 / 21.6; 256 rows 2048 -> 2048 17.3 / 13.4), of the size that leaves the
+  // fewest pairs idle: a tile takes the bytes of its operands (its rows and 256 features) and about four stages' time besides.
   const bool pairs = p.M > 96;
   int grid = 0, sub = 2;
   if (pairs) {

@@ -11,8 +11,10 @@
 // warps of a CTA) and joined in shared memory in a fixed order.
 // Dropout: a thread masks the 16-byte chunks that it copied itself, each one draw of the generator, before the
 // barrier that hands them on.
-// low_row_kernel, for a few rows (rows x rank <= LOW_ROW_MAX): a CTA per row, which reads its adapter's factor
-// in one wave of loads; a tile's rows of as many adapters would pass one after another.
+// low_row_kernel, for a few rows: a CTA per row, which reads its adapter's factor in one wave of loads; a tile's rows of as many
+// adapters would pass one after another.  It is taken while the factors read, one a row, are at most 20 MB (LOW_ROW_MAX elements;
+// whole forward passes in us, row / tile kernel: rank 16, 64 rows of 4096 13.6 / 19.2, 256 of 1000 11.5 / 11.6, 256 of 4096 (34 MB)
+// 22.7 / 20.2, 848 of 2560 32 / 26; rank 64, 128 rows of 1000 13.6 / 15.6, 128 of 4096 (67 MB) 29 / 21).
 #include "lora.cuh"
 
 namespace cospec {
@@ -20,7 +22,7 @@ namespace cospec {
 namespace {
 
 constexpr int LOW_THREADS = 256;         // 8 warps
-constexpr int LOW_ROW_MAX = 2048;
+constexpr long long LOW_ROW_MAX = 10000000;
 constexpr int ROW_THREADS = 512;
 
 struct LowArgs {
@@ -376,7 +378,7 @@ cudaError_t launch_low_tile(const LowArgs& p, int tiles, int num_sms, cudaStream
 
 template <bool RM>
 cudaError_t launch_low(LowArgs p, int num_sms, cudaStream_t stream) {
-  if ((long long)p.M * p.r <= LOW_ROW_MAX)
+  if ((long long)p.M * p.r * p.C <= LOW_ROW_MAX)
     return launch_pdl(low_row_kernel<RM>, dim3((unsigned)p.M), dim3(ROW_THREADS), 0, stream, p);
   // 128 rows a CTA share an adapter's factor; fewer where that leaves SMs without work
   p.rw_log2 = 3;
