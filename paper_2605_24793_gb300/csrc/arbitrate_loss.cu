@@ -8,11 +8,14 @@
 //
 // About a tenth of the positions are effective, so a CTA takes up to 2048 positions at a time, lists the
 // effective ones and gathers what they need into shared memory.  Their products with the MLP run with the hidden
-// units on the lanes: a thread keeps one or two pairs of units' weights and their sums S in registers (pairs, so
-// that each instruction does two units), and every decision's features come by broadcast.  Each sum over the
-// decisions then needs no exchange between threads; z does, one butterfly for four decisions.  Which units are on
-// is kept as bits between the two walks.  H up to 64 units fits one warp, and the eight warps take
-// decisions in turn; 256 units take two.  All sums have a fixed order.
+// units on the lanes: a thread keeps one or two pairs of units' weights and their sums S in registers, and every
+// decision's features come by broadcast.  Each sum over the decisions then needs no exchange between threads; z does, one
+// butterfly for four decisions.  Which units are on is kept as bits between the two walks.  H up to 64 units fits one warp,
+// and the eight warps take decisions in turn; 256 units take two.  All sums have a fixed order.
+// Work: 36 H flops at each effective decision; bytes: ids, flags, p_new and dz of every position and what a decision
+// gathers.  66560 rounds, K = 25, H = 256: 53 us, of which the multiply-adds alone would be 17 us and the bytes 13 us: the
+// walks issue their multiply-adds at about half rate, and listing a step's decisions is a chain of barriers that the SM's
+// other CTA hides in part.  64 rounds, K = 5, H = 64: 7.7 us, latency: the launch, one chain of loads, the cluster's exchange.
 // The terms of the loss, db2 and the CTAs' sums are added as pairs of floats (hi + lo): 64-bit additions, of which an
 // SM issues about two a clock, took 70 us in the second kernel.  KL is p g(-d/p) + q g(d/q), d = p - p_ref, g(x) = x -
 // log(1 + x), whose first-order terms are gone before they could cancel.
@@ -75,6 +78,9 @@ CS_DEV float2 add_pair(float2 s, float2 x) {
   return make_float2(t.x, __fadd_rn(t.y, x.y));
 }
 
+// A sum's value; one that left the finite numbers has no lower part.
+CS_DEV float value(float2 s) { return s.y == s.y && fabsf(s.x) <= 3.4028235e38f ? s.x + s.y : s.x; }
+
 // Asks for [from, to) in L2: the 16-byte pieces that lie whole inside.
 CS_DEV void l2_prefetch(const void* from, const void* to) {
   const uint64_t a = (reinterpret_cast<uint64_t>(from) + 15) & ~15ull, b = reinterpret_cast<uint64_t>(to) & ~15ull;
@@ -86,26 +92,78 @@ CS_DEV void l2_prefetch(const void* from, const void* to) {
 // these take 195.)
 CS_DEV float2 fma_pair(float2 a, float f, float2 c) { return make_float2(fmaf(a.x, f, c.x), fmaf(a.y, f, c.y)); }
 
+// Products and quotients of such pairs, to about 2^-45 (Dekker's, with fused multiply-adds).
+CS_DEV float2 quick_pair(float a, float b) {               // |a| >= |b|
+  const float s = __fadd_rn(a, b);
+  return make_float2(s, __fsub_rn(b, __fsub_rn(s, a)));
+}
+CS_DEV float2 mul_pair(float2 a, float2 b) {
+  const float p = __fmul_rn(a.x, b.x);
+  return quick_pair(p, __fmaf_rn(a.x, b.y, __fmaf_rn(a.y, b.x, __fmaf_rn(a.x, b.x, -p))));
+}
+CS_DEV float2 div_pair(float2 a, float2 b) {
+  const float q = a.x / b.x;
+  if (!(fabsf(q) <= 3.4028235e38f)) return make_float2(q, 0.f);      // an infinity or NaN has no lower part
+  const float r = __fmaf_rn(-q, b.y, __fadd_rn(__fmaf_rn(-q, b.x, a.x), a.y));
+  return quick_pair(q, r / b.x);
+}
+// e^t for -80 < t <= 0 as a pair, relative error below 2^-28: t = k log 2 + r with log 2 in two parts after Cody and Waite
+// (355/512, whose product with k is exact, and the rest), then 1 + r + r^2 / 2 in pairs and the rest of the series, below 1/100, in 32 bits.
+CS_DEV float2 exp_pair(float t) {
+  const float k = rintf(t * 1.44269504f);
+  const float2 r = add_to(make_float2(__fmaf_rn(-k, 355.f / 512.f, t), 0.f), k * 2.12194440e-4f);
+  float c = 1.f / 40320.f;
+  c = fmaf(c, r.x, 1.f / 5040.f);
+  c = fmaf(c, r.x, 1.f / 720.f);
+  c = fmaf(c, r.x, 1.f / 120.f);
+  c = fmaf(c, r.x, 1.f / 24.f);
+  c = fmaf(c, r.x, 1.f / 6.f);
+  const float2 sq = mul_pair(r, r);
+  const float2 s = add_to(add_pair(add_pair(make_float2(1.f, 0.f), r), make_float2(0.5f * sq.x, 0.5f * sq.y)), c * r.x * sq.x);
+  const float two_k = __int_as_float(((int)k + 127) << 23);
+  return make_float2(s.x * two_k, s.y * two_k);
+}
+
 struct Decision {
   float p, dz, surr, ent, kl;
 };
 
+// p, the ratio and the surrogate's gradient are carried as pairs and rounded once: db2 is a sum of dz whose terms nearly
+// cancel, so that each one's roundings (six in 32 bits) would stand before it a thousandfold.
 CS_DEV Decision decide(float z, float adv, float old, float ref, bool took, const ArbLossArgs& a) {
   Decision d;
-  const float e = expf(-fabsf(z)), big = 1.f / (1.f + e), small = e * big;
-  const float p = z >= 0.f ? big : small, q = z >= 0.f ? small : z < 0.f ? big : z;
-  d.p = z >= 0.f ? big : z < 0.f ? small : z;          // NaN stays
-  const float ratio = (took ? p : q) / (took ? old : 1.f - old);
-  const float plain = ratio * adv, cut = fminf(fmaxf(ratio, 1.f - a.clip_eps), 1.f + a.clip_eps) * adv;
+  float2 big, small;                       // the larger and the smaller of p and 1 - p
+  if (fabsf(z) < 80.f) {
+    const float2 e = exp_pair(-fabsf(z)), one = add_pair(make_float2(1.f, 0.f), e);
+    big = div_pair(make_float2(1.f, 0.f), one);
+    small = mul_pair(e, big);
+  } else {                                 // infinities and NaN too
+    const float e = expf(-fabsf(z));
+    big = make_float2(1.f / (1.f + e), 0.f);
+    small = make_float2(e, 0.f);
+  }
+  const float2 pp = z >= 0.f ? big : small, qq = z >= 0.f ? small : z < 0.f ? big : make_float2(z, 0.f);
+  const float p = pp.x + pp.y, q = qq.x + qq.y;
+  d.p = z >= 0.f ? p : z < 0.f ? p : z;    // NaN stays
+  const float2 ratio = div_pair(took ? pp : qq, took ? make_float2(old, 0.f) : add_to(make_float2(1.f, 0.f), -old));
+  const float rt = ratio.x + ratio.y, plain = rt * adv, cut = fminf(fmaxf(rt, 1.f - a.clip_eps), 1.f + a.clip_eps) * adv;
   const bool inside = !(plain > cut);
   d.surr = inside ? plain : cut;
-  d.ent = log1pf(e) + (small > 0.f ? fabsf(z) * small : 0.f);
+  const float e = expf(-fabsf(z)), lean = small.x;
+  d.ent = log1pf(e) + (lean > 0.f ? fabsf(z) * lean : 0.f);
   // p - p_ref from the sides that are not near 1
   const float diff = z >= 0.f ? (1.f - ref) - q : p - ref;
   d.kl = (p > 0.f ? p * log_rest(-diff / p) : -diff) + (q > 0.f ? q * log_rest(diff / q) : diff);
   const float pq = p * q;
   const float pull = pq > 0.f ? pq * (a.beta_h * z + a.beta_kl * (z - logf(ref / (1.f - ref)))) : pq;
-  d.dz = (inside ? -plain * (took ? q : -p) : 0.f) + pull;
+  float2 g = make_float2(0.f, 0.f);
+  if (inside) {
+    const float2 other = took ? qq : make_float2(-pp.x, -pp.y);
+    g = mul_pair(mul_pair(ratio, make_float2(-adv, 0.f)), other);
+    if (!(fabsf(g.y) <= 3.4028235e38f)) g = make_float2(-plain * (other.x + other.y), 0.f);       // past fp32's end
+  }
+  g = add_to(g, pull);
+  d.dz = value(g);
   return d;
 }
 
@@ -115,21 +173,23 @@ CS_DEV void unit_gradients(const ArbLossArgs& a, int h, const float2 (&t)[9]) {
   float2 dw2 = make_float2(0.f, 0.f);
 #pragma unroll
   for (int k = 0; k < 9; ++k) {
-    if (k < 8) a.dw1[(size_t)h * 8 + k] = fmaf(w2, t[k].x, w2 * t[k].y);
-    else a.db1[h] = fmaf(w2, t[k].x, w2 * t[k].y);
+    const float2 down = make_float2(w2 * t[k].x, fmaf(w2, t[k].x, -(w2 * t[k].x)) + w2 * t[k].y);
+    if (k < 8) a.dw1[(size_t)h * 8 + k] = value(down);
+    else a.db1[h] = value(down);
     const float w = k < 8 ? a.w1[(size_t)h * 8 + k] : a.b1[h], prod = w * t[k].x;
     dw2 = add_pair(dw2, make_float2(prod, fmaf(w, t[k].x, -prod) + w * t[k].y));
   }
-  a.dw2[h] = dw2.x + dw2.y;
+  a.dw2[h] = value(dw2);
 }
 // The loss from its terms and the sum of dz.
 CS_DEV void write_loss(const ArbLossArgs& a, const float2 (&v)[4]) {
-  const double surr = (double)v[0].x + (double)v[0].y, ent = (double)v[1].x + (double)v[1].y, kl = (double)v[2].x + (double)v[2].y;
+  auto both = [](float2 s) { return s.y == s.y ? (double)s.x + (double)s.y : (double)s.x; };
+  const double surr = both(v[0]), ent = both(v[1]), kl = both(v[2]);
   a.loss[0] = (float)surr;
   a.loss[1] = (float)ent;
   a.loss[2] = (float)kl;
   a.loss[3] = (float)(-surr - (double)a.beta_h * ent + (double)a.beta_kl * kl);
-  *a.db2 = v[3].x + v[3].y;
+  *a.db2 = value(v[3]);
 }
 
 // PP: pairs of units of a thread; TW: warps that hold all units.
@@ -169,7 +229,7 @@ __global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs 
 #pragma unroll
     for (int k = 0; k < 9; ++k) S[i][k] = make_float2(0.f, 0.f);
   }
-  const float b2 = *a.b2, inv_k = 1.f / (float)a.K;
+  const float b2 = *a.b2;
   const int total = a.n * a.K;
   float2 sums[4];                          // hi + lo
 #pragma unroll
@@ -294,7 +354,7 @@ __global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs 
         }
         float4* f = reinterpret_cast<float4*>(sm.feat[d]);
         f[0] = make_float4(x4 - x2, x0 - x2, x0 - x1, x3);
-        f[1] = make_float4(y0 - y2, i + 1 < a.K ? y4 - y2 : 0.f, (float)(i + 1) * inv_k, (float)before * inv_k);
+        f[1] = make_float4(y0 - y2, i + 1 < a.K ? y4 - y2 : 0.f, (float)(i + 1) / (float)a.K, (float)before / (float)a.K);
         sm.adv[d] = adv;
         sm.old[d] = old;
         sm.ref[d] = ref;
@@ -311,9 +371,11 @@ __global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs 
           float2 zz = make_float2(0.f, 0.f);
 #pragma unroll
           for (int i = 0; i < PP; ++i) {
-            float2 v = b1[i];
+            float2 v = make_float2(0.f, 0.f);
 #pragma unroll
             for (int k = 0; k < 8; ++k) v = fma_pair(w1[i][k], f[k], v);
+            v.x += b1[i].x;
+            v.y += b1[i].y;
             bits = __funnelshift_l(__float_as_uint(v.x), bits, 1);
             bits = __funnelshift_l(__float_as_uint(v.y), bits, 1);
             zz = fma2(w2[i], make_float2(fmaxf(-v.x, 0.f), fmaxf(-v.y, 0.f)), zz);

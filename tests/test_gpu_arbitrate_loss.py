@@ -172,6 +172,43 @@ def test_logits_far_out():
         assert np.abs(g["dz"].cpu().numpy()).max() < 1e-20
 
 
+@pytest.mark.parametrize("z", [-79.99, -40.25, -17.5, -5.0, -0.7, -1e-4, 0.0, 1e-4, 0.346, 0.347, 3.0, 20.0, 79.99, 80.0, 85.0])
+def test_p_and_dz_over_the_logits_range(z):
+    """p to its rounding (2^-24 of it, and 2^-24 of the pair's terms), dz of a ratio of one to two roundings more."""
+    c = _case(47, 2, 3, 4, mismatch=1.0, dense=True)
+    c["eff"][:], c["w2"][:], c["b2"][:] = 1, 0, z
+    zz = float(c["b2"][0])
+    p, q = 1 / (1 + math.exp(-zz)), 1 / (1 + math.exp(zz))
+    for took in (1, 0):
+        c["accept"][:] = took
+        c["p_old"][:] = p if took else 1 - q
+        dev = {k: torch.from_numpy(v).cuda() for k, v in c.items()}
+        g = C.arbitrate_loss(**dev, params=C.RLParams(beta_h=0.0, beta_kl=0.0, clip_eps=0.9))
+        assert (np.abs(g["p_new"].double().cpu().numpy() - p) <= 2.0 ** -23 * p).all()
+        old, A = c["p_old"].astype(np.float64), c["adv"].astype(np.float64)
+        with np.errstate(divide="ignore"):
+            ratio = (p if took else q) / (old if took else 1 - old)
+        inside = ratio * A <= np.clip(ratio, 1 - np.float64(np.float32(0.9)), 1 + np.float64(np.float32(0.9))) * A
+        want = np.where(inside, -A * ratio * (q if took else -p), 0.0)
+        fine = np.isfinite(want)
+        assert (np.abs(g["dz"].double().cpu().numpy() - want)[fine] <= 2.0 ** -21 * np.abs(want)[fine] + 2.0 ** -126).all()
+
+
+def test_an_old_probability_of_zero():
+    """The ratio is infinite: clipped where A > 0, so that nothing else is lost; infinite where A < 0."""
+    c = _case(53, 3, 4, 8, mismatch=1.0, dense=True)
+    c["eff"][:], c["accept"][:], c["p_old"][:] = 1, 1, 0.5
+    c["adv"][:] = 1.0
+    c["p_old"][1, 2] = 0.0
+    dev = {k: torch.from_numpy(v).cuda() for k, v in c.items()}
+    g = C.arbitrate_loss(**dev, params=C.RLParams())
+    assert all(torch.isfinite(g[k]).all() for k in ("loss", "p_new", "dz", "dw1", "db1", "dw2", "db2"))
+    dev["adv"][1, 2] = -1.0
+    g = C.arbitrate_loss(**dev, params=C.RLParams())
+    assert float(g["loss"][0]) == -math.inf and float(g["loss"][3]) == math.inf and float(g["dz"][1, 2]) == math.inf
+    assert float(g["db2"][0]) == math.inf and torch.isfinite(g["loss"][1:3]).all()
+
+
 def test_repeated_captured_and_filled_again():
     c, o = _sure(51, 200, 25, 256)
     a = _run(c)
