@@ -11,8 +11,8 @@
 // to its last row of the tile.  With dropout (backward) this part has an accumulator of its own: the mask
 // multiplies it alone.
 //
-// lora_tile_kernel: one CTA per 128 features x rows of a tile, the contraction split over a cluster and joined
-// in shared memory in a fixed order.
+// lora_tile_kernel, up to 96 rows: one CTA per 128 features of all rows, the contraction split over a cluster and joined
+// in shared memory in a fixed order.  lora_pair_kernel, above: CTA pairs walk tiles of 256 features.
 #include <cuda.h>
 
 #include "lora.cuh"
@@ -32,6 +32,8 @@ constexpr int MAX_NT = 256;
 constexpr uint64_t WAIT_NS = 2000000000ull;
 
 struct GemmArgs {
+  const __nv_bfloat16 *x, *w, *f;      // (for the elements that are computed again)
+  long long ldx;
   const float* u;
   const int32_t* adapter;
   __nv_bfloat16* y;
@@ -57,7 +59,7 @@ CS_DEV uint64_t desc_k_sw32(uint32_t saddr) {
 
 // The adapters of a tile's rows in the order of their first rows: id, first and last row.
 struct TileList {
-  int ids[MAX_NT];             // of the rows: -1 none
+  int at[MAX_NT];              // the rows' places in the list, -1 without an adapter
   int adapter[MAX_NT];
   int span[MAX_NT];            // first | last << 16
   int warp_count[8];
@@ -75,12 +77,12 @@ struct ListScratch {
 CS_DEV void build_list(TileList& L, ListScratch& H, const GemmArgs& p, int row0, int t, int bar) {
   const int rows = min(p.nt, p.M - row0);
   for (int i = t; i < HASH; i += 128) H.key[i] = -1, H.first[i] = MAX_NT, H.last[i] = -1;
-  for (int i = t; i < p.nt; i += 128) L.ids[i] = i < rows ? lora_adapter(p.adapter, row0 + i, p.n, p.err) : -1;
+  for (int i = t; i < p.nt; i += 128) L.at[i] = i < rows ? lora_adapter(p.adapter, row0 + i, p.n, p.err) : -1;
   named_bar_sync(bar, 128);
   int place[2] = {-1, -1};
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
-    const int i = t + 128 * q, id = i < p.nt ? L.ids[i] : -1;
+    const int i = t + 128 * q, id = i < p.nt ? L.at[i] : -1;
     if (id < 0) continue;
     int h = (int)(((uint32_t)id * 2654435761u) >> 23);            // 9 bits
     while (true) {
@@ -108,26 +110,32 @@ CS_DEV void build_list(TileList& L, ListScratch& H, const GemmArgs& p, int row0,
       done += c;
     }
     if (first) {
-      L.adapter[at] = L.ids[i];
+      L.adapter[at] = L.at[i];
       L.span[at] = i | H.last[h] << 16;
+      H.key[h] = at;
     }
   }
   if (t == 0) L.count = done;
+  named_bar_sync(bar, 128);
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+    if (place[q] >= 0) L.at[t + 128 * q] = H.key[place[q]];
 }
 
-// One row's 16 ranks of a unit as hi and lo: four 16-byte chunks of the operand's 128-byte row.
-CS_DEV void unit_row(uint4 (&w)[4], const float* u, bool mine, int j0, int r) {
-  const uint4 zero[4] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+// One row's 16 ranks of a unit, and as hi and lo: four 16-byte chunks of the operand's 128-byte row; zeros where the unit is
+// not the row's.
+CS_DEV void unit_load(float (&v)[16], const float* u, int j0, int r) {
 #pragma unroll
-  for (int c = 0; c < 4; ++c) w[c] = zero[c];
+  for (int q = 0; q < 4; ++q) {
+    float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (j0 + 4 * q < r) f = *reinterpret_cast<const float4*>(u + j0 + 4 * q);
+    v[4 * q] = f.x, v[4 * q + 1] = f.y, v[4 * q + 2] = f.z, v[4 * q + 3] = f.w;
+  }
+}
+CS_DEV void unit_row(uint4 (&w)[4], bool mine, const float (&v)[16]) {
+#pragma unroll
+  for (int c = 0; c < 4; ++c) w[c] = make_uint4(0, 0, 0, 0);
   if (mine) {
-    float v[16];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (j0 + 4 * q < r) f = *reinterpret_cast<const float4*>(u + j0 + 4 * q);
-      v[4 * q] = f.x, v[4 * q + 1] = f.y, v[4 * q + 2] = f.z, v[4 * q + 3] = f.w;
-    }
     uint32_t hi[8], lo[8];
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
@@ -164,6 +172,44 @@ CS_DEV uint32_t keep_bits32(int f0, int row0, const LoraDrop& d, LoraKey key) {
     w = (lane & s) ? (w & ~m) | ((o >> s) & m) : (w & m) | ((o << s) & ~m);
   }
   return w;
+}
+
+// An adapter's factor that holds an infinity or NaN turns the other rows' zeros in its product to NaN, in the features
+// concerned.  So a result that is not finite is looked at: where another adapter of the tile's rows (tile0, tile_rows) has such
+// a value in feature f, rows m0 .. m1 - 1 of the feature that came out not finite are computed again, term by term.  Rare, and
+// slow by the standards of this file.
+template <bool MN, bool DROP>
+__device__ __noinline__ void again(const GemmArgs& p, int f, int m0, int m1, int tile0, int tile_rows) {
+  if (f >= p.F) return;
+  auto factor = [&](int id, int j) {
+    return __bfloat162float(p.f[MN ? ((size_t)id * p.r + j) * p.F + f : ((size_t)id * p.F + f) * p.r + j]);
+  };
+  auto finite = [](float v) { return fabsf(v) <= 3.4028235e38f; };
+  bool spoilt = false;
+  int last = -1;
+  for (int i = tile0; i < min(tile0 + tile_rows, p.M) && !spoilt; ++i) {
+    const int id = p.adapter[i];
+    if (id == last || id < 0 || id >= p.n) continue;
+    last = id;
+    for (int j = 0; j < p.r; ++j) spoilt = spoilt || !finite(factor(id, j));
+  }
+  if (!spoilt) return;
+  LoraKey key{0, 0};
+  if (DROP) key = lora_key(p.drop);
+  for (int m = m0; m < min(m1, p.M); ++m) {
+    __nv_bfloat16* y = p.y + (long long)m * p.ldy + f;
+    if (finite(__bfloat162float(*y))) continue;
+    float v[4] = {0.f, 0.f, 0.f, 0.f}, low = 0.f;
+    const __nv_bfloat16* x = p.x + (long long)m * p.ldx;
+    for (int k = 0; k < p.C; k += 4)         // (a multiple of 8)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        v[q] = fmaf(__bfloat162float(x[k + q]), __bfloat162float(p.w[MN ? (size_t)(k + q) * p.F + f : (size_t)f * p.C + k + q]), v[q]);
+    const int id = p.adapter[m];
+    if (id >= 0 && id < p.n && (!DROP || ((lora_keep8_bits((uint32_t)(f / 8), (uint32_t)m, p.drop, key) >> (f & 7)) & 1u)))
+      for (int j = 0; j < p.r; ++j) low = fmaf(p.u[(size_t)m * p.r + j], factor(id, j), low);
+    *y = __float2bfloat16((v[0] + v[1]) + (v[2] + v[3]) + low);
+  }
 }
 
 struct TileSmem {
@@ -204,7 +250,7 @@ CS_DEV bool wait_count(const int* p, int v) {
 template <bool MN, bool DROP>
 __global__ void __launch_bounds__(256, 1)
     lora_tile_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x,
-                     const __grid_constant__ CUtensorMap tmap_f, const GemmArgs p) {
+                     const __grid_constant__ CUtensorMap tmap_f, const __grid_constant__ GemmArgs p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   const TileSmem L = tile_layout(p.stages, p.nt);
@@ -221,7 +267,6 @@ __global__ void __launch_bounds__(256, 1)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int S = (int)cluster_nctarank(), rank = (int)cluster_ctarank();
   const int f0 = ((int)blockIdx.x / S) * BM;
-  const int row0 = (int)blockIdx.y * p.nt;
   const int kblocks = (p.C + BK - 1) / BK;
   const int kb0 = (int)((long long)kblocks * rank / S), nk = (int)((long long)kblocks * (rank + 1) / S) - kb0;
   const int upe = (p.r + UNIT - 1) / UNIT;           // units of an adapter
@@ -264,8 +309,7 @@ __global__ void __launch_bounds__(256, 1)
     const uint32_t on = elect_one();
     const bool is_w = warp != 2;
     const int part = warp == 3;
-    // W is read again by the other row tiles, if there are any
-    const uint64_t pol = !is_w ? l2_policy_evict_last() : gridDim.y > 1 ? l2_policy_evict_normal() : l2_policy_evict_first();
+    const uint64_t pol = is_w ? l2_policy_evict_first() : l2_policy_evict_last();      // (no other CTA reads this W)
     const uint32_t a_buf = smem_u32(smem) + (uint32_t)part * A_BYTES, b_buf = smem_u32(smem + L.b_off), full0 = smem_u32(full);
     int li = 0, st = 0;
     uint32_t ph = 0;
@@ -286,8 +330,8 @@ __global__ void __launch_bounds__(256, 1)
       const uint32_t dst = a_buf + (uint32_t)(s * A_STAGE);
       mbar_arrive_expect_tx_on(on, bar, is_w ? (uint32_t)A_BYTES : b_stage);
       if (!is_w) {
-        tma_load_3d_on(on, b_buf + (uint32_t)s * b_stage, &tmap_x, bar, x, row0, 0, pol);
-        tma_load_3d_on(on, b_buf + (uint32_t)s * b_stage + b_bytes, &tmap_x, bar, x + 64, row0, 0, pol);
+        tma_load_3d_on(on, b_buf + (uint32_t)s * b_stage, &tmap_x, bar, x, 0, 0, pol);
+        tma_load_3d_on(on, b_buf + (uint32_t)s * b_stage + b_bytes, &tmap_x, bar, x + 64, 0, 0, pol);
       } else if (!MN) {
         tma_load_3d_on(on, dst, &tmap_w, bar, x + 64 * part, f0, 0, pol);
       } else {
@@ -386,7 +430,7 @@ __global__ void __launch_bounds__(256, 1)
     umma_commit_on(on, done);
   } else if (warp >= 4) {
     const int t = tid - 128;
-    build_list(list, *reinterpret_cast<ListScratch*>(smem + L.list_off + (sizeof(TileList) + 15) / 16 * 16), p, row0, t, 1);
+    build_list(list, *reinterpret_cast<ListScratch*>(smem + L.list_off + (sizeof(TileList) + 15) / 16 * 16), p, 0, t, 1);
     __syncwarp();
     if (lane == 0) mbar_arrive(lready);
     named_bar_sync(1, 128);
@@ -405,12 +449,15 @@ __global__ void __launch_bounds__(256, 1)
       const int u0 = (rank + i * S) * STEP_UNITS, nu = min(STEP_UNITS, units - u0);
       for (int q = 0; q < nu; ++q) {
         const int e = (u0 + q) / upe, j0 = ((u0 + q) % upe) * UNIT;
-        const int id = list.adapter[e], span = list.span[e];
+        const int span = list.span[e];
         const bool all = DROP && i == 0 && q == 0;
         const int lo = all ? 0 : (span & 0xffff) & ~15, hi = all ? p.nt : ((span >> 16) | 15) + 1;
         for (int row = lo + lane; row < hi; row += 32) {
           uint4 w[4];
-          unit_row(w, p.u + (size_t)(row0 + row) * p.r, list.ids[row] == id, j0, p.r);
+          float v[16];
+          const bool mine = list.at[row] == e;
+          if (mine) unit_load(v, p.u + (size_t)row * p.r, j0, p.r);
+          unit_row(w, mine, v);
           store_unit_row(tile + (q >> 1) * b_bytes, row, q & 1, w);
         }
       }
@@ -439,7 +486,7 @@ __global__ void __launch_bounds__(256, 1)
           float w[16];
           tq_ld16(tb + (uint32_t)(p.nt + c), w);
           tq_wait_ld16(w);
-          const uint32_t keep = keep_bits32(f0 + q * 32, row0 + (c & ~31), p.drop, key) >> (c & 16);
+          const uint32_t keep = keep_bits32(f0 + q * 32, c & ~31, p.drop, key) >> (c & 16);
 #pragma unroll
           for (int j = 0; j < 16; ++j) v[j] += (keep >> j) & 1u ? w[j] : 0.f;
         }
@@ -458,12 +505,16 @@ __global__ void __launch_bounds__(256, 1)
     const int r0 = p.nt * rank / S, r1 = p.nt * (rank + 1) / S;
     const uint32_t base = smem_u32(smem);
     const int f = f0 + lane * 4;
+    float nil = 0.f;                       // NaN once a result is not finite
     for (int row = r0 + warp; row < r1; row += 8) {
-      if (row0 + row >= p.M) break;
+      if (row >= p.M) break;
       const float4 v = dsmem_sum4(base + (uint32_t)(row * BM + lane * 4) * 4u, S);
       if (f < p.F)
-        *reinterpret_cast<uint2*>(p.y + (long long)(row0 + row) * p.ldy + f) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+        *reinterpret_cast<uint2*>(p.y + (long long)row * p.ldy + f) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+      nil = fmaf(v.x, 0.f, fmaf(v.y, 0.f, fmaf(v.z, 0.f, fmaf(v.w, 0.f, nil))));
     }
+    if (nil != 0.f)
+      for (int e = 4 * (r0 + warp); e < 4 * r1; e += (e & 3) == 3 ? 29 : 1) again<MN, DROP>(p, f + (e & 3), e >> 2, (e >> 2) + 1, 0, p.M);
   }
   __syncwarp();
   cluster_arrive();
@@ -483,7 +534,7 @@ cudaError_t launch_tile(const CUtensorMap& w, const CUtensorMap& x, const CUtens
   if (e != cudaSuccess) return e;
   // The split with the least blocks of the contraction one after another: waves of resident clusters, each a split's
   // share and what a CTA costs besides (about four stages' time).
-  const int tiles = (p.F + BM - 1) / BM * ((p.M + p.nt - 1) / p.nt), kblocks = (p.C + BK - 1) / BK;
+  const int tiles = (p.F + BM - 1) / BM, kblocks = (p.C + BK - 1) / BK;
   const int dev = current_device();
   int splits = 1;
   long long best = 0;
@@ -493,7 +544,7 @@ cudaError_t launch_tile(const CUtensorMap& w, const CUtensorMap& x, const CUtens
     if (best == 0 || cost < best) best = cost, splits = s;
   }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((p.F + BM - 1) / BM * splits), (unsigned)((p.M + p.nt - 1) / p.nt));
+  cfg.gridDim = dim3((unsigned)(tiles * splits));
   cfg.blockDim = dim3(256);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
@@ -582,7 +633,7 @@ __host__ __device__ inline PairSmem pair_layout(int stages, int nt, int sub) {
 template <bool MN, bool DROP, int SUB>
 __global__ void __launch_bounds__(P_THREADS, 1)
     lora_pair_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x,
-                     const __grid_constant__ CUtensorMap tmap_f, const GemmArgs p) {
+                     const __grid_constant__ CUtensorMap tmap_f, const __grid_constant__ GemmArgs p) {
   constexpr int NACC = DROP ? 1 : 2, PBK = 64 * SUB, PU = 2 * SUB;       // units of an adapter step
   constexpr uint32_t P_STAGE = (uint32_t)SUB * A_BYTES;
   extern __shared__ uint8_t smem_raw[];
@@ -687,6 +738,7 @@ __global__ void __launch_bounds__(P_THREADS, 1)
       if (!ok) break;
       const TileList& list = list_of(it);
       const int units = list.count * upe, steps = (units + PU - 1) / PU;
+      int le = 0, lj = 0;                  // the next unit's adapter and place in it
       for (int i = 0; i < steps; ++i) {
         const int s = turn();
         if (s < 0) {
@@ -698,8 +750,11 @@ __global__ void __launch_bounds__(P_THREADS, 1)
         if (warp == 0) mbar_arrive_on(on, smem_u32(&ugo[s]));
         if (mine == 0) mbar_arrive_on(lead, own);
         else mbar_arrive_expect_tx_on(lead, own, (uint32_t)(2 * mine * UNIT_BYTES));
-        for (int q = part; q < 2 * mine; q += 2) {
-          const int u = i * PU + q, e = list.adapter[u / upe], j0 = (u % upe) * UNIT;
+        if (!is_w) continue;
+        for (int q = 0; q < nu; ++q) {
+          const int e = list.adapter[le], j0 = lj * UNIT;
+          if (++lj == upe) lj = 0, ++le;
+          if ((q & 1) != part) continue;
           const uint32_t dst = smem_u32(smem) + (uint32_t)s * P_STAGE + (uint32_t)(q * UNIT_BYTES);
           if (!MN) {
             tma_load_3d_pair_on(on, dst, &tmap_f, bar, j0, f0, e, pol);
@@ -803,31 +858,35 @@ __global__ void __launch_bounds__(P_THREADS, 1)
       named_bar_sync(1, 128);
       const int units = list.count * upe, steps = (units + PU - 1) / PU;
       st = (st + kblocks) % p.stages;
+      // The row's own units follow one another: two of them are read ahead.  (Read when their step came, and with divisions to find
+      // it: 64 adapters of rank 32, rows in turn, 4096 rows 4096 -> 4096, 510 us for what takes 360.)
+      const int place = t < half ? list.at[rank * half + t] : -1;
+      const float* u = p.u + (size_t)(row0 + rank * half + t) * p.r;
+      int k = place >= 0 ? -place * upe : -(1 << 30);        // the next unit, counted from the row's first
+      float v0[16], v1[16];
+      if (place >= 0) {
+        unit_load(v0, u, 0, p.r);
+        unit_load(v1, u, UNIT, p.r);
+      }
       for (int i = 0; i < steps; ++i) {
         const int s = st;
         if (++st == p.stages) st = 0;
-        // u of two units is read before the stage is free
-        const int nu = min(PU, units - i * PU), row = min(rank * half + t, p.nt - 1);
-        uint4 w[2][4];
-        auto read = [&](int q, uint4 (&v)[4]) {
-          const int u = i * PU + min(q, nu - 1), id = list.adapter[u / upe];
-          unit_row(v, p.u + (size_t)(row0 + row) * p.r, list.ids[row] == id, (u % upe) * UNIT, p.r);
-        };
-        read(0, w[0]);
-        read(1, w[1]);
+        const int nu = min(PU, units - i * PU);
         ok = __all_sync(0xffffffffu, mbar_wait_idle(&ugo[s], (gphase >> s) & 1u, WAIT_NS, 100u)) && !*abort_flag;
         if (!ok) break;
         gphase ^= 1u << s;
         uint8_t* buf = smem + L.b_off + (uint32_t)s * b_stage;
-        if (t < half) {
-          store_unit_row(buf, t, 0, w[0]);
-          if (nu > 1) store_unit_row(buf, t, 1, w[1]);
-          if (PU == 4 && nu > 2) {
-            read(2, w[0]);
-            read(3, w[1]);
-            store_unit_row(buf + b_bytes, t, 0, w[0]);
-            if (nu > 3) store_unit_row(buf + b_bytes, t, 1, w[1]);
+        for (int q = 0; q < nu; ++q, ++k) {
+          const bool mine = k >= 0 && k < upe;
+          uint4 w[4];
+          if (k & 1) {
+            unit_row(w, mine, v1);
+            if (mine) unit_load(v1, u, (k + 2) * UNIT, p.r);
+          } else {
+            unit_row(w, mine, v0);
+            if (mine) unit_load(v0, u, (k + 2) * UNIT, p.r);
           }
+          if (t < half) store_unit_row(buf + (q >> 1) * b_bytes, t, q & 1, w);
         }
         fence_proxy_async_smem();
         __syncwarp();
@@ -869,6 +928,7 @@ __global__ void __launch_bounds__(P_THREADS, 1)
       const uint32_t tb = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * p.nt);
       const bool odd = lane & 1;
       const bool in = f + (lane & ~1) < p.F;
+      float nil[4] = {0.f, 0.f, 0.f, 0.f}; // NaN once a result is not finite
 #pragma unroll
       for (int c = 0; c < P_CHUNKS; ++c) {
         const int ch = hw + 2 * c;
@@ -883,6 +943,8 @@ __global__ void __launch_bounds__(P_THREADS, 1)
             for (int j = 0; j < 32; ++j) v[j] += (keep[c] >> j) & 1u ? w[j] : 0.f;
           }
         }
+#pragma unroll
+        for (int j = 0; j < 32; ++j) nil[j & 3] = fmaf(v[j], 0.f, nil[j & 3]);
         // neighbouring lanes exchange, so that each stores two features of one row
         __nv_bfloat16* dst = p.y + (long long)(row0 + ch * 32 + (odd ? 1 : 0)) * p.ldy + f + (lane & ~1);
         const int left = rows - ch * 32 - (odd ? 1 : 0);
@@ -897,6 +959,11 @@ __global__ void __launch_bounds__(P_THREADS, 1)
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster_relaxed(tempty0 + (uint32_t)acc * 8u);
+      if (__any_sync(0xffffffffu, (nil[0] + nil[1]) + (nil[2] + nil[3]) != 0.f)) {
+        __syncwarp();
+        for (int ch = hw; ch < chunks; ch += 2) again<MN, DROP>(p, f + lane, row0 + ch * 32, row0 + min(ch * 32 + 32, rows), row0, p.nt);
+        __syncwarp();
+      }
     }
   }
 
@@ -941,6 +1008,10 @@ cudaError_t launch_pair(const CUtensorMap& w, const CUtensorMap& x, const CUtens
 
 cudaError_t launch_lora_gemm(const LoraArgs& a, bool backward, int num_sms, int* err, cudaStream_t stream) {
   GemmArgs p{};
+  p.x = backward ? a.dy : a.x;
+  p.ldx = backward ? a.ldy : a.ldx;
+  p.w = a.w;
+  p.f = backward ? a.a : a.b;
   p.u = backward ? a.t : a.u;
   p.adapter = a.adapter;
   p.y = backward ? a.dx : a.y;
@@ -974,9 +1045,7 @@ cudaError_t launch_lora_gemm(const LoraArgs& a, bool backward, int num_sms, int*
     p.stages = (int)((226u * 1024u - pair_layout(0, p.nt, sub).total) / ((uint32_t)sub * (A_BYTES + (uint32_t)p.nt * 64u) + 32u));
     if (p.stages > 6) p.stages = 6;
   } else {
-    // one row tile, or equal parts of at most 256
-    const int row_tiles = (p.M + MAX_NT - 1) / MAX_NT;
-    p.nt = ((p.M + row_tiles - 1) / row_tiles + 15) / 16 * 16;
+    p.nt = (p.M + 15) / 16 * 16;
     p.stages = (int)((226u * 1024u - tile_layout(0, p.nt).total) / (A_STAGE + (uint32_t)p.nt * 256u + 32u));
     if (p.stages > 6) p.stages = 6;
   }

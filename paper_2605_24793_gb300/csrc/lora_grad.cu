@@ -42,7 +42,7 @@ struct GradArgs {
 
 struct GradSmem {
   int list[WIN];
-  int warp_count[16];
+  unsigned mine[WIN / 32];             // which rows of 32 are the adapter's
   uint64_t full[GDEPTH], empty[GDEPTH];
 };
 // the ring of Q and of P [BR rows][R] fp32, two buffers of P's parts [3][BR rows][R], the list; then the sums,
@@ -112,23 +112,37 @@ __global__ void __launch_bounds__(GRAD_THREADS + copy_threads(RT)) lora_grad_ker
   for (int w0 = m_lo; w0 < m_hi; w0 += WIN) {
     // the adapter's rows of the window, in order
     const int w1 = min(w0 + WIN, m_hi);
-    int have = 0;
-    for (int b = w0; b < w1; b += GRAD_THREADS) {
-      const int m = b + tid;
-      const bool in = warp < WARPS && m < w1 && p.adapter[m] == a;
-      const unsigned mask = __ballot_sync(0xffffffffu, in);
-      if (lane == 0 && warp < WARPS) sm.warp_count[warp] = __popc(mask);
-      __syncthreads();
-      int at = have + __popc(mask & ((1u << lane) - 1u));
+    if (warp < WARPS) {
 #pragma unroll
-      for (int w = 0; w < WARPS; ++w) {
-        const int c = sm.warp_count[w];
-        if (w < warp) at += c;
-        have += c;
+      for (int i = 0; i < WIN / GRAD_THREADS; ++i) {
+        const int m = w0 + i * GRAD_THREADS + tid;
+        unsigned mask = 0;
+        if (w0 + i * GRAD_THREADS < w1) mask = __ballot_sync(0xffffffffu, m < w1 && p.adapter[m] == a);
+        if (lane == 0) sm.mine[i * WARPS + warp] = mask;
       }
-      if (in) sm.list[at] = m;
-      __syncthreads();
     }
+    __syncthreads();
+    // the counts' running sums, two a lane
+    static_assert(WIN / 32 == 64, "two counts a lane");
+    const int v0 = __popc(sm.mine[2 * lane]), v1 = __popc(sm.mine[2 * lane + 1]);
+    int upto = v0 + v1;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += v;
+    }
+    const int have = __shfl_sync(0xffffffffu, upto, 31);
+    if (warp < WARPS) {
+#pragma unroll
+      for (int i = 0; i < WIN / GRAD_THREADS; ++i) {
+        const int c = i * WARPS + warp;
+        if (w0 + i * GRAD_THREADS >= w1) break;
+        const unsigned mask = sm.mine[c];
+        const int at = __shfl_sync(0xffffffffu, upto - ((c & 1) ? v1 : v0 + v1), c >> 1) + __popc(mask & ((1u << lane) - 1u));
+        if ((mask >> lane) & 1u) sm.list[at] = w0 + i * GRAD_THREADS + tid;
+      }
+    }
+    __syncthreads();
     const int batches = (have + BR - 1) / BR;
     if (warp >= WARPS) {
       // a warp a row of Q; rows behind the last, columns behind the width and ranks behind the rank as zeros

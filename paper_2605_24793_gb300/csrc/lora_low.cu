@@ -6,15 +6,22 @@
 //
 // low_tile_kernel: a CTA takes 32 to 128 rows, in chunks of 64 of the contraction that come by cp.async into a ring
 // ahead of the products (mma.sync).  Rows of several adapters: a chunk of x stays while the factors of the
-// tile's adapters pass, and each warp zeroes the other rows' elements of its fragments, so that all of
-// them add into one accumulator.  The contraction is split over the CTAs of a cluster (and, for few rows, the
+// tile's adapters pass, and a warp whose rows differ adds each product to the sums of that adapter's rows alone (what another
+// adapter's factor holds, infinities or NaN, reaches no other row).  The contraction is split over the CTAs of a cluster (and, for few rows, the
 // warps of a CTA) and joined in shared memory in a fixed order.
 // Dropout: a thread masks the 16-byte chunks that it copied itself, each one draw of the generator, before the
 // barrier that hands them on.
-// low_row_kernel, for a few rows: a CTA per row, which reads its adapter's factor in one wave of loads; a tile's rows of as many
-// adapters would pass one after another.  It is taken while the factors read, one a row, are at most 20 MB (LOW_ROW_MAX elements;
-// whole forward passes in us, row / tile kernel: rank 16, 64 rows of 4096 13.6 / 19.2, 256 of 1000 11.5 / 11.6, 256 of 4096 (34 MB)
-// 22.7 / 20.2, 848 of 2560 32 / 26; rank 64, 128 rows of 1000 13.6 / 15.6, 128 of 4096 (67 MB) 29 / 21).
+// Rows of many adapters in turn (requests of a batch in the order they came): above three changes a tile, the tiles take their
+// rows in the order of the adapters, 2048 at a time, so that a tile's factors stay two or three (64 adapters of rank 32, 4096 rows of
+// 4096: 251 -> 54 us).
+// low_row_kernel, for a few rows: CTAs per row, which read its adapter's factor in one wave of loads; a tile's rows of as many
+// adapters would pass one after another.  What it costs is the factors read, one a row; what the tiles cost is their chain of chunks.
+// Taken up to LOW_ROW_MANY elements (128 MB) for at most 64 rows, or 256 of at least four adapters, else up to LOW_ROW_MAX (20 MB).
+// (Whole forward passes 4096 -> 4096 in us, row / tile kernel: 64 rows of 1 adapter at rank 64 16.9 / 19.8, of 16 18.7 / 64; 28 rows of
+// 6584 at rank 128 13.3 / 34.5; 256 rows of 4 adapters side by side 18.8 / 25 at rank 16, 23.1 / 26.1 at rank 32; 160 of 8 at rank 64 30 / 51;
+// 256 of one adapter at rank 16 22.7 / 20.2; 848 of 2560 of four 33.6 / 30.9.)
+// Bounds: low_tile_kernel 8192 x 5120 at rank 64 with dropout 64 us (84 MB, 12 us of memory: the products' and the draw's
+// instructions), 4096 x 2560 at rank 16 16 us; low_row_kernel 4 to 9 us, latency.
 #include "lora.cuh"
 
 namespace cospec {
@@ -22,8 +29,11 @@ namespace cospec {
 namespace {
 
 constexpr int LOW_THREADS = 256;         // 8 warps
-constexpr long long LOW_ROW_MAX = 10000000;
+constexpr long long LOW_ROW_MAX = 10000000, LOW_ROW_MANY = 64000000;
 constexpr int ROW_THREADS = 512;
+// Rows ordered by their adapters at a time, and ids that leave room for a row in a 32-bit key
+constexpr int SORT_WIN = 2048;
+constexpr int SORT_MAX_N = 1 << 20;
 
 struct LowArgs {
   const __nv_bfloat16* x;
@@ -36,6 +46,8 @@ struct LowArgs {
   float keep_inv;       // 1 / (1 - p)
   LoraDrop drop;
   int rw_log2;          // log2 of the row groups of a CTA
+  int sort;             // tiles may take their rows in the order of the adapters
+  int ranks;            // (row kernel) ranks of a CTA, a multiple of 16
   int* err;
 };
 
@@ -46,16 +58,49 @@ constexpr int LOW_MAX_ROWS = 128;
 struct LowSmem {
   int ids[LOW_MAX_ROWS];
   int adapters[LOW_MAX_ROWS];
-  int warp_count[4];
-  int count;
+  int row[LOW_MAX_ROWS];       // of x
+  int warp_count[8];
 };
 __host__ __device__ constexpr uint32_t low_bytes(int rows, int R) {
   return (uint32_t)DEPTH * (uint32_t)(rows * 128 + R * 128) + (uint32_t)sizeof(LowSmem);
 }
 
+// A window is SORT_WIN rows from w0 on, or what is left.  Whether its tiles take its rows in the order of the adapters: above three
+// changes of the adapter a tile, by 256 pairs of neighbours.  (The same in all CTAs of the window.)
+CS_DEV bool rows_in_turn(const LowArgs& p, int w0, int rows) {
+  const int wn = min(SORT_WIN, p.M - w0), i = w0 + (((int)threadIdx.x * (wn - 1)) >> 8);
+  const bool change = wn > 1 && p.adapter[i] != p.adapter[i + 1];
+  static_assert(LOW_THREADS == 256, "a pair a thread");
+  return __syncthreads_count(change) * rows > 3 * LOW_THREADS;
+}
+// The tile's share of the window's rows in that order: a sort of keys that hold the adapter and the place.
+CS_DEV void order_rows(const LowArgs& p, uint32_t* key, LowSmem& sm, int w0, int m0, int rows) {
+  const int tid = (int)threadIdx.x, wn = min(SORT_WIN, p.M - w0);
+  int P = 2 * LOW_THREADS;
+  while (P < wn) P <<= 1;
+  for (int i = tid; i < P; i += LOW_THREADS) {
+    const int id = i < wn ? p.adapter[w0 + i] : 0;
+    key[i] = i >= wn ? 0xffffffffu : (uint32_t)(id < 0 || id >= p.n ? SORT_MAX_N : id) << 11 | (uint32_t)i;
+  }
+  __syncthreads();
+  for (int k = 2; k <= P; k <<= 1)
+    for (int j = k >> 1; j > 0; j >>= 1) {
+      for (int e = tid; e < P / 2; e += LOW_THREADS) {
+        const int i = 2 * e - (e & (j - 1));
+        const uint32_t a = key[i], b = key[i + j];
+        if ((a > b) == ((i & k) == 0)) key[i] = b, key[i + j] = a;
+      }
+      // (below a distance of 64, a warp's pairs lie in 64 keys of its own)
+      if (j > 32 || (j == 1 && k >= 32)) __syncthreads();
+      else __syncwarp();
+    }
+  for (int i = tid; i < rows; i += LOW_THREADS) sm.row[i] = m0 + i < p.M ? w0 + (int)(key[m0 - w0 + i] & (SORT_WIN - 1)) : 0;
+  __syncthreads();
+}
+
 // NT: rank in groups of 8 (2, 4, 8 or 16).  RM: the factor's rows run along the rank.
 template <int NT, bool RM>
-__global__ void __launch_bounds__(LOW_THREADS) low_tile_kernel(const LowArgs p) {
+__global__ void __launch_bounds__(LOW_THREADS, NT <= 2 ? 3 : NT <= 8 ? 2 : 1) low_tile_kernel(const LowArgs p) {
   extern __shared__ __align__(128) uint8_t sraw[];
   constexpr int R = NT * 8;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2;
@@ -78,26 +123,44 @@ __global__ void __launch_bounds__(LOW_THREADS) low_tile_kernel(const LowArgs p) 
   // 128-byte rows is the same for all i.  Items are walked with counters, without divisions.
   const int xc = (int)threadIdx.x & 7, xr = (int)threadIdx.x >> 3;
   const uint32_t xs = (uint32_t)(xr * 128 + ((xc ^ (xr & 7)) << 4));
-  const __nv_bfloat16* xp = p.x + (long long)(m0 + xr) * p.ldx + (long long)c0 * CK + 8 * xc;
+  int m_of[LOW_MAX_ROWS / 32];             // the rows of x that it copies
+#pragma unroll
+  for (int i = 0; i < LOW_MAX_ROWS / 32; ++i) m_of[i] = m0 + xr + 32 * i;
+  const __nv_bfloat16* xp = p.x + (long long)c0 * CK + 8 * xc;
   const int x_rows = min(rows, p.M - m0);                // rows of the tile that exist
   auto load_x = [&](int ci) {
     const uint32_t dst = x_off + (uint32_t)((ci & (DEPTH - 1)) * rows * 128) + xs;
     const bool kin = (c0 + ci) * CK + 8 * xc < p.C;
     const __nv_bfloat16* src = xp + ci * CK;
-#pragma unroll 4
-    for (int i = 0; 32 * i + xr < rows; ++i) {
+#pragma unroll
+    for (int i = 0; i < LOW_MAX_ROWS / 32; ++i) {
+      if (32 * i + xr >= rows) break;
       const bool on = kin && 32 * i + xr < x_rows;
-      cp_async16(dst + (uint32_t)(i * 4096), on ? src + (long long)(32 * i) * p.ldx : p.x, on);
+      cp_async16(dst + (uint32_t)(i * 4096), on ? src + (long long)m_of[i] * p.ldx : p.x, on);
     }
   };
   // the first chunks set out before the tile's adapters are known
   const int early = min(DEPTH - 1, c1 - c0);
   for (int i = 0; i < early; ++i) load_x(i);
+  static_assert(SORT_WIN * 4 <= DEPTH * R * 128, "the keys take the factors' place");
+  const int w0 = m0 & ~(SORT_WIN - 1);
+  const bool sorted = p.sort && rows_in_turn(p, w0, rows);
+  if (sorted) {                            // other rows than those that are under way
+    order_rows(p, reinterpret_cast<uint32_t*>(sraw + (f_off - x_off)), sm, w0, m0, rows);
+    cp_async_commit();
+    cp_async_wait<0>();
+#pragma unroll
+    for (int i = 0; i < LOW_MAX_ROWS / 32; ++i)
+      if (xr + 32 * i < rows) m_of[i] = sm.row[xr + 32 * i];
+    for (int i = 0; i < early; ++i) load_x(i);
+  }
 
   // the adapters of the tile, in the order of their first rows
   if (threadIdx.x < LOW_MAX_ROWS) {
-    const int m = m0 + (int)threadIdx.x;
-    sm.ids[threadIdx.x] = (int)threadIdx.x < rows && m < p.M ? lora_adapter(p.adapter, m, p.n, p.err) : -1;
+    const bool in = (int)threadIdx.x < x_rows;
+    const int m = sorted && in ? sm.row[threadIdx.x] : m0 + (int)threadIdx.x;
+    sm.row[threadIdx.x] = m;
+    sm.ids[threadIdx.x] = in ? lora_adapter(p.adapter, m, p.n, p.err) : -1;
   }
   __syncthreads();
   bool first = false;
@@ -163,13 +226,17 @@ __global__ void __launch_bounds__(LOW_THREADS) low_tile_kernel(const LowArgs p) 
   for (int i = 0; i < NT; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = sum[i][j] = 0.f;
-  auto settle = [&]() {
+  auto settle = [&](bool on0, bool on1) {
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) sum[i][j] += acc[i][j], acc[i][j] = 0.f;
+      for (int j = 0; j < 4; ++j) sum[i][j] += (j < 2 ? on0 : on1) ? acc[i][j] : 0.f, acc[i][j] = 0.f;
   };
   const int id0 = sm.ids[rw * 16 + g], id1 = sm.ids[rw * 16 + g + 8];
+  // whether the warp's rows are of one adapter (those of none end as zeros): one of them, the largest, is then every row's
+  const int top = (int)__reduce_max_sync(0xffffffffu, (unsigned)(max(id0, id1) + 1)) - 1;
+  const bool one = __all_sync(0xffffffffu, (id0 < 0 || id0 == top) && (id1 < 0 || id1 == top));
+  int turns = 0;
   // ldmatrix: the lane's row and 16-byte column of a 16 x 16 block; the swizzled places are the first block's, others differ by an
   // exclusive or
   const int lr = lane & 15, lc = lane >> 4;
@@ -195,12 +262,11 @@ __global__ void __launch_bounds__(LOW_THREADS) low_tile_kernel(const LowArgs p) 
 #pragma unroll 2
       for (int row = xr; row < x_rows; row += 32) {
         uint4* q = reinterpret_cast<uint4*>(sraw + (xb - x_off) + (row - xr) * 128 + xs);
-        *q = lora_dropped8(*q, c, (uint32_t)(m0 + row), p.drop, key);
+        *q = lora_dropped8(*q, c, (uint32_t)sm.row[row], p.drop, key);
       }
     }
     __syncthreads();
     load();
-    if ((item & 3) == 3) settle();
     const int a = sm.adapters[ai];
     const bool on0 = id0 == a, on1 = id1 == a;
     if (!__any_sync(0xffffffffu, on0 || on1)) continue;
@@ -209,8 +275,6 @@ __global__ void __launch_bounds__(LOW_THREADS) low_tile_kernel(const LowArgs p) 
       if ((ks & (KW - 1)) != kw) continue;
       uint32_t q[4];
       ldsm_x4(xb + (xa ^ (uint32_t)(ks << 5)), q[0], q[1], q[2], q[3]);
-      q[0] = on0 ? q[0] : 0u, q[2] = on0 ? q[2] : 0u;
-      q[1] = on1 ? q[1] : 0u, q[3] = on1 ? q[3] : 0u;
 #pragma unroll
       for (int i = 0; i < NT; i += 2) {
         uint32_t b[4];
@@ -223,8 +287,9 @@ __global__ void __launch_bounds__(LOW_THREADS) low_tile_kernel(const LowArgs p) 
         mma_16816(acc[i + 1], q, b[2], b[3]);
       }
     }
+    if (!one || (++turns & 3) == 0) settle(on0 || one, on1 || one);
   }
-  settle();
+  settle(true, true);
   cp_async_wait<0>();
   __syncthreads();
 
@@ -246,8 +311,8 @@ __global__ void __launch_bounds__(LOW_THREADS) low_tile_kernel(const LowArgs p) 
   const uint32_t base = smem_u32(red);
   for (int e = e0 + (int)threadIdx.x; e < e1; e += LOW_THREADS) {
     const int j = e % R, row = e / R;
-    const long long m = (long long)m0 + row;
-    if (j >= p.r || m >= p.M) continue;
+    if (j >= p.r || row >= x_rows) continue;
+    const int m = sm.row[row];
     float v = 0.f;
     for (int w = 0; w < KW; ++w) v += dsmem_sum(base + 4u * (uint32_t)((w * rows + row) * RP + j), S);
     const int a = p.adapter[m];
@@ -264,18 +329,19 @@ CS_DEV float dot2(uint32_t a, uint32_t b, float c) {
 }
 CS_DEV float dot8(uint4 a, uint4 b, float c) { return dot2(a.w, b.w, dot2(a.z, b.z, dot2(a.y, b.y, dot2(a.x, b.x, c)))); }
 
-// A CTA per row.  Rows of the factor along the contraction: a warp takes two ranks and half of the
-// contraction; along the rank: a thread takes eight ranks and every few rows of the factor.
+// A CTA per row and p.ranks of its ranks (one row at rank 64, 5576 columns: 13 us by one CTA, 5 by four).  Rows of the factor along
+// the contraction: a warp takes two ranks and half of the contraction; along the rank: a thread takes eight ranks and every
+// few rows of the factor.
 template <bool RM>
 __global__ void __launch_bounds__(ROW_THREADS) low_row_kernel(const LowArgs p) {
   __shared__ float part[16][128];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int m = (int)blockIdx.x;
+  const int m = (int)blockIdx.x, j0 = (int)blockIdx.y * p.ranks, j1 = min(p.r, j0 + p.ranks);
   griddep_wait();
   griddep_launch_dependents();
   const int a = lora_adapter(p.adapter, m, p.n, p.err);
   if (a < 0) {
-    for (int j = threadIdx.x; j < p.r; j += ROW_THREADS) p.u[(size_t)m * p.r + j] = 0.f;
+    for (int j = j0 + threadIdx.x; j < j1; j += ROW_THREADS) p.u[(size_t)m * p.r + j] = 0.f;
     return;
   }
   const __nv_bfloat16* x = p.x + (long long)m * p.ldx;
@@ -287,7 +353,7 @@ __global__ void __launch_bounds__(ROW_THREADS) low_row_kernel(const LowArgs p) {
     if (drop) key = lora_key(p.drop);
     const int octets = p.C / 8, half = warp >> 3;
     const int o0 = half ? (octets + 1) / 2 : 0, o1 = half ? octets : (octets + 1) / 2;
-    for (int j = 2 * (warp & 7); j < p.r; j += 16) {
+    for (int j = j0 + 2 * (warp & 7); j < j1; j += 16) {
       const __nv_bfloat16* f0 = f + (size_t)j * p.C;
       float v0 = 0.f, v1 = 0.f;
 #pragma unroll 8
@@ -306,19 +372,19 @@ __global__ void __launch_bounds__(ROW_THREADS) low_row_kernel(const LowArgs p) {
       if (lane == 0) part[half][j] = v0, part[half][j + 1] = v1;
     }
     __syncthreads();
-    for (int j = threadIdx.x; j < p.r; j += ROW_THREADS) p.u[(size_t)m * p.r + j] = (part[0][j] + part[1][j]) * c;
+    for (int j = j0 + threadIdx.x; j < j1; j += ROW_THREADS) p.u[(size_t)m * p.r + j] = (part[0][j] + part[1][j]) * c;
   } else {
-    int og = 1;                          // octets of the rank, rounded up to a power of two
-    while (og * 8 < p.r) og <<= 1;
+    int og = 1;                          // octets of the ranks, rounded up to a power of two
+    while (og * 8 < j1 - j0) og <<= 1;
     const int j = threadIdx.x & (og - 1), step = ROW_THREADS / og;
     float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = 0.f;
-    if (8 * j < p.r) {
+    if (j0 + 8 * j < j1) {
 #pragma unroll 8
       for (int k = threadIdx.x / og; k < p.C; k += step) {
         const float xv = __bfloat162float(x[k]);
-        const uint4 b = ldg16(f + (size_t)k * p.r + 8 * j);
+        const uint4 b = ldg16(f + (size_t)k * p.r + j0 + 8 * j);
         const uint32_t w[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -335,11 +401,11 @@ __global__ void __launch_bounds__(ROW_THREADS) low_row_kernel(const LowArgs p) {
       for (int i = 0; i < 8; ++i) part[warp][lane * 8 + i] = v[i];
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < p.r; i += ROW_THREADS) {
+    for (int i = threadIdx.x; i < j1 - j0; i += ROW_THREADS) {
       float s = 0.f;
 #pragma unroll
       for (int w = 0; w < 16; ++w) s += part[w][i];
-      p.u[(size_t)m * p.r + i] = s * c;
+      p.u[(size_t)m * p.r + j0 + i] = s * c;
     }
   }
 }
@@ -348,9 +414,8 @@ template <int NT, bool RM>
 cudaError_t launch_low_tile(const LowArgs& p, int tiles, int num_sms, cudaStream_t stream) {
   static KernelLimits lim;
   const int rows = 16 << p.rw_log2;
-  size_t smem = low_bytes(rows, NT * 8);
-  const size_t red = (size_t)8 * 16 * (NT * 8 + 4) * sizeof(float);
-  if (smem < red) smem = red;
+  const size_t smem = low_bytes(rows, NT * 8);
+  static_assert(8 * 16 * (NT * 8 + 4) * sizeof(float) <= low_bytes(32, NT * 8) - sizeof(LowSmem), "the sums take the ring's place");
   const void* kern = (const void*)low_tile_kernel<NT, RM>;
   const cudaError_t e = ensure_kernel_limits(kern, lim, smem, false);
   if (e != cudaSuccess) return e;
@@ -378,12 +443,17 @@ cudaError_t launch_low_tile(const LowArgs& p, int tiles, int num_sms, cudaStream
 
 template <bool RM>
 cudaError_t launch_low(LowArgs p, int num_sms, cudaStream_t stream) {
-  if ((long long)p.M * p.r * p.C <= LOW_ROW_MAX)
-    return launch_pdl(low_row_kernel<RM>, dim3((unsigned)p.M), dim3(ROW_THREADS), 0, stream, p);
+  if ((long long)p.M * p.r * p.C <= (p.M <= 64 || (p.M <= 256 && p.n >= 4) ? LOW_ROW_MANY : LOW_ROW_MAX)) {
+    // as many CTAs as the SMs hold at once
+    p.ranks = 16;
+    while (p.ranks < p.r && (long long)p.M * ((p.r + p.ranks - 1) / p.ranks) > 4 * num_sms) p.ranks += 16;
+    return launch_pdl(low_row_kernel<RM>, dim3((unsigned)p.M, (unsigned)((p.r + p.ranks - 1) / p.ranks)), dim3(ROW_THREADS), 0, stream, p);
+  }
   // 128 rows a CTA share an adapter's factor; fewer where that leaves SMs without work
   p.rw_log2 = 3;
   while (p.rw_log2 > 1 && (p.M + (16 << p.rw_log2) - 1) / (16 << p.rw_log2) * 8 < num_sms) --p.rw_log2;
   const int tiles = (p.M + (16 << p.rw_log2) - 1) / (16 << p.rw_log2);
+  p.sort = p.n >= 4 && p.n <= SORT_MAX_N && tiles > 1;
   const int nt = (p.r + 7) / 8;
   if (nt <= 2) return launch_low_tile<2, RM>(p, tiles, num_sms, stream);
   if (nt <= 4) return launch_low_tile<4, RM>(p, tiles, num_sms, stream);

@@ -120,6 +120,51 @@ def test_long_contractions(M, K, N, r, n):
         _check_backward(c, dy, u, _backward(c, dy, u, dropout), dropout)
 
 
+# rows of many adapters in turn, more than one window of ordered rows, a window that ends inside a tile; more ranks than a CTA takes
+MANY = [(2500, 520, 136, 16, 40), (4200, 200, 264, 64, 13), (600, 1160, 264, 32, 64), (900, 136, 1344, 128, 6), (4100, 264, 136, 24, 4)]
+
+
+@pytest.mark.parametrize("M,K,N,r,n", MANY)
+@pytest.mark.parametrize("dropout", [0.0, 0.2])
+def test_rows_of_many_adapters_in_turn(M, K, N, r, n, dropout):
+    c, dy = _make(M + n, M, K, N, r, n, wide=dropout > 0, runs=False)
+    y, u = _forward(c, dropout)
+    _check_forward(c, y, u, dropout)
+    _check_backward(c, dy, u, _backward(c, dy, u, dropout), dropout)
+
+
+@pytest.mark.parametrize("M,K,N,r,n", [(1, 5576, 136, 64, 1), (2, 2752, 80, 128, 15), (5, 120, 2000, 72, 3), (130, 264, 136, 40, 7)])
+def test_a_row_by_several_ctas(M, K, N, r, n):
+    c, dy = _make(M + n, M, K, N, r, n, none=0.1)
+    y, u = _forward(c, 0.2)
+    _check_forward(c, y, u, 0.2)
+    _check_backward(c, dy, u, _backward(c, dy, u, 0.2), 0.2)
+
+
+@pytest.mark.parametrize("M,K,N,n", [(40, 192, 256, 3), (90, 136, 264, 40), (300, 192, 520, 3), (3000, 520, 136, 9)])
+@pytest.mark.parametrize("dropout", [0.0, 0.3])
+def test_an_adapter_that_is_not_finite_spoils_its_own_rows_only(M, K, N, n, dropout):
+    c, dy = _make(M + 9, M, K, N, 16, n, none=0.2, runs=False)
+    y0, u0 = _forward(c, dropout)
+    g0 = _backward(c, dy, u0, dropout)
+    bad = {k: v.clone() for k, v in c.items()}
+    bad["a"][1, 3, ::7], bad["b"][1, 5::11, 2], bad["b"][1, 4] = float("inf"), float("nan"), float("-inf")
+    others = c["adapter"] != 1
+    assert others.any() and not others.all()
+    y1, u1 = _forward(bad, dropout)
+    assert torch.equal(u0[others], u1[others]) and not torch.isfinite(y1[~others]).all()
+    dx, da, db, t = _backward(bad, dy, u0, dropout)
+    assert not torch.isfinite(dx[~others]).all()
+    # rows of other adapters as before, but for what is summed in another order: half a step and the sums' terms
+    for a, b, size in ((y0, y1, _np(c["x"]).__abs__() @ _np(c["w"]).__abs__().T), (g0[0], dx, _np(dy).__abs__() @ _np(c["w"]).__abs__())):
+        a, b = _np(a)[others.cpu()], _np(b)[others.cpu()]
+        assert np.isfinite(b).all()
+        low = 2.0 ** -10 * np.abs(size[others.cpu()])       # u's and t's terms: 2^-17 of them, and they are below 100 x the others
+        assert (np.abs(a - b) <= 2.0 ** -7 * np.abs(a) + low).all()
+    keep = [i for i in range(n) if i != 1]
+    assert torch.equal(da[keep], g0[1][keep]) and torch.equal(db[keep], g0[2][keep])
+
+
 @pytest.mark.parametrize("M,K,N,r,n,wide,runs", [SHAPES[i] for i in (0, 3, 4, 7, 9)])
 @pytest.mark.parametrize("dropout", [0.05, 0.5])
 def test_forward_dropout(M, K, N, r, n, wide, runs, dropout):
