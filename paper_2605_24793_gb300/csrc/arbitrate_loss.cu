@@ -13,7 +13,7 @@
 // butterfly for four decisions.  Which units are on is kept as bits between the two walks.  H up to 64 units fits one warp,
 // and the eight warps take decisions in turn; 256 units take two.  All sums have a fixed order.
 // Work: 36 H flops at each effective decision; bytes: ids, flags, p_new and dz of every position and what a decision
-// gathers.  66560 rounds, K = 25, H = 256: 53 us, of which the multiply-adds alone would be 17 us and the bytes 13 us: the
+// gathers.  66560 rounds, K = 25, H = 256: 52 us, of which the multiply-adds alone would be 17 us and the bytes 13 us: the
 // walks issue their multiply-adds at about half rate, and listing a step's decisions is a chain of barriers that the SM's
 // other CTA hides in part.  64 rounds, K = 5, H = 64: 7.7 us, latency: the launch, one chain of loads, the cluster's exchange.
 // The terms of the loss, db2 and the CTAs' sums are added as pairs of floats (hi + lo): 64-bit additions, of which an
@@ -133,14 +133,17 @@ struct Decision {
 CS_DEV Decision decide(float z, float adv, float old, float ref, bool took, const ArbLossArgs& a) {
   Decision d;
   float2 big, small;                       // the larger and the smaller of p and 1 - p
+  float ez;                                // e^-|z|
   if (fabsf(z) < 80.f) {
     const float2 e = exp_pair(-fabsf(z)), one = add_pair(make_float2(1.f, 0.f), e);
-    big = div_pair(make_float2(1.f, 0.f), one);
+    const float q = 1.f / one.x;           // (one is between 1 and 2: the lower part may take the fast quotient)
+    big = quick_pair(q, __fdividef(__fmaf_rn(-q, one.y, __fmaf_rn(-q, one.x, 1.f)), one.x));
     small = mul_pair(e, big);
+    ez = e.x + e.y;
   } else {                                 // infinities and NaN too
-    const float e = expf(-fabsf(z));
-    big = make_float2(1.f / (1.f + e), 0.f);
-    small = make_float2(e, 0.f);
+    ez = expf(-fabsf(z));
+    big = make_float2(1.f / (1.f + ez), 0.f);
+    small = make_float2(ez, 0.f);
   }
   const float2 pp = z >= 0.f ? big : small, qq = z >= 0.f ? small : z < 0.f ? big : make_float2(z, 0.f);
   const float p = pp.x + pp.y, q = qq.x + qq.y;
@@ -149,8 +152,8 @@ CS_DEV Decision decide(float z, float adv, float old, float ref, bool took, cons
   const float rt = ratio.x + ratio.y, plain = rt * adv, cut = fminf(fmaxf(rt, 1.f - a.clip_eps), 1.f + a.clip_eps) * adv;
   const bool inside = !(plain > cut);
   d.surr = inside ? plain : cut;
-  const float e = expf(-fabsf(z)), lean = small.x;
-  d.ent = log1pf(e) + (lean > 0.f ? fabsf(z) * lean : 0.f);
+  const float lean = small.x;
+  d.ent = log1pf(ez) + (lean > 0.f ? fabsf(z) * lean : 0.f);
   // p - p_ref from the sides that are not near 1
   const float diff = z >= 0.f ? (1.f - ref) - q : p - ref;
   d.kl = (p > 0.f ? p * log_rest(-diff / p) : -diff) + (q > 0.f ? q * log_rest(diff / q) : diff);
@@ -371,11 +374,9 @@ __global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs 
           float2 zz = make_float2(0.f, 0.f);
 #pragma unroll
           for (int i = 0; i < PP; ++i) {
-            float2 v = make_float2(0.f, 0.f);
+            float2 v = b1[i];
 #pragma unroll
             for (int k = 0; k < 8; ++k) v = fma_pair(w1[i][k], f[k], v);
-            v.x += b1[i].x;
-            v.y += b1[i].y;
             bits = __funnelshift_l(__float_as_uint(v.x), bits, 1);
             bits = __funnelshift_l(__float_as_uint(v.y), bits, 1);
             zz = fma2(w2[i], make_float2(fmaxf(-v.x, 0.f), fmaxf(-v.y, 0.f)), zz);
