@@ -1,7 +1,9 @@
 // Gradients of the adapters' factors (cospec_lora_backward): sums over the rows m of one adapter,
 //   dA_a[j][k] = sum_m t[m][j] drop(x)[m][k]        dB_a[n][j] = sum_m u[m][j] dy[m][n]
 // Both are P^T Q with P fp32 [rows, rank] and Q bf16 [rows, width], and both are one launch: the column blocks of x
-// come first, then those of dy.  Bound by reading x and dy once each.
+// come first, then those of dy.  The floor is reading x and dy once; what bounds it is the instructions a batch takes (P's parts,
+// dropped elements, three products an element): 4096 rows of 2560 + 6144 at rank 16 with dropout 38 us for 72 MB (11 us of memory),
+// 2048 rows of 4096 + 4096, 8 adapters of rank 64, 60 us for 34 MB.
 //
 // mma.sync with the rank as M, columns of Q as N and the rows as the contraction.  P enters as three
 // bf16 parts, which hold all 24 bits of it, so the sums are those of fp32 products (a gradient that is
