@@ -59,9 +59,10 @@ __host__ __device__ constexpr uint32_t grad_bytes(int R) {
 // with four; 2048 rows of 4096 + 4096 at rank 64: 63 and 57).
 __host__ __device__ constexpr int copy_threads(int rt) { return rt <= 2 ? 64 : 128; }
 
-// RT: ranks in sixteens.
-template <int RT>
-__global__ void __launch_bounds__(GRAD_THREADS + copy_threads(RT)) lora_grad_kernel(const GradArgs p) {
+// RT: ranks in sixteens.  PER_SM: CTAs that share an SM, two where there are more CTAs than SMs (64 adapters of rank 32, 4096 rows of
+// 4096 + 4096: a backward pass 590 -> 530 us; with fewer one is faster, 301 rows of 1000 + 1048 19.9 for 22.0).
+template <int RT, int PER_SM>
+__global__ void __launch_bounds__(GRAD_THREADS + copy_threads(RT), PER_SM) lora_grad_kernel(const GradArgs p) {
   extern __shared__ __align__(128) uint8_t raw[];
   constexpr int R = 16 * RT, WARPS = GRAD_THREADS / 32, COPY_THREADS = copy_threads(RT), COPY_WARPS = COPY_THREADS / 32;
   constexpr int PC = BR * R / 4;                       // 16-byte chunks of a batch's P
@@ -277,14 +278,14 @@ __global__ void __launch_bounds__(GRAD_THREADS + copy_threads(RT)) lora_grad_ker
   cluster_wait();
 }
 
-template <int RT>
+template <int RT, int PER_SM>
 cudaError_t launch_grad(const GradArgs& p, int blocks, int n, int num_sms, cudaStream_t stream) {
   static KernelLimits lim;
   constexpr int R = 16 * RT;
   size_t smem = grad_bytes(R);
   const size_t red = (size_t)(R * (CB + 8) > CB * (R + 4) ? R * (CB + 8) : CB * (R + 4)) * sizeof(float);
   if (smem < red) smem = red;
-  const void* kern = (const void*)lora_grad_kernel<RT>;
+  const void* kern = (const void*)lora_grad_kernel<RT, PER_SM>;
   const cudaError_t e = ensure_kernel_limits(kern, lim, smem, false);
   if (e != cudaSuccess) return e;
   // (as if every adapter had as many rows; a CTA costs about eight batches' time besides its own)
@@ -306,7 +307,7 @@ cudaError_t launch_grad(const GradArgs& p, int blocks, int n, int num_sms, cudaS
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, lora_grad_kernel<RT>, p);
+  return cudaLaunchKernelEx(&cfg, lora_grad_kernel<RT, PER_SM>, p);
 }
 
 }  // namespace
@@ -327,9 +328,10 @@ cudaError_t launch_lora_grad(const LoraArgs& a, int num_sms, int* err, cudaStrea
   p.drop = LoraDrop{a.seed, a.site, a.thr};
   const int blocks = p.blocks0 + (p.N + CB - 1) / CB;
   if (blocks == 0) return cudaSuccess;
-  if (a.r <= 16) return launch_grad<1>(p, blocks, a.n, num_sms, stream);
-  if (a.r <= 32) return launch_grad<2>(p, blocks, a.n, num_sms, stream);
-  return launch_grad<4>(p, blocks, a.n, num_sms, stream);
+  if (a.r <= 16) return launch_grad<1, 2>(p, blocks, a.n, num_sms, stream);
+  if (a.r <= 32)
+    return (long long)blocks * a.n > num_sms ? launch_grad<2, 2>(p, blocks, a.n, num_sms, stream) : launch_grad<2, 1>(p, blocks, a.n, num_sms, stream);
+  return launch_grad<4, 1>(p, blocks, a.n, num_sms, stream);
 }
 
 }  // namespace cospec

@@ -13,7 +13,7 @@
 // barrier that hands them on.
 // Rows of many adapters in turn (requests of a batch in the order they came): above three changes a tile, the tiles take their
 // rows in the order of the adapters, 2048 at a time, so that a tile's factors stay two or three (64 adapters of rank 32, 4096 rows of
-// 4096: 251 -> 54 us).
+// 4096: 251 -> 41 us).
 // low_row_kernel, for a few rows: CTAs per row, which read its adapter's factor in one wave of loads; a tile's rows of as many
 // adapters would pass one after another.  What it costs is the factors read, one a row; what the tiles cost is their chain of chunks.
 // Taken up to LOW_ROW_MANY elements (128 MB) for at most 64 rows, or 256 of at least four adapters, else up to LOW_ROW_MAX (20 MB).
@@ -31,9 +31,7 @@ namespace {
 constexpr int LOW_THREADS = 256;         // 8 warps
 constexpr long long LOW_ROW_MAX = 10000000, LOW_ROW_MANY = 64000000;
 constexpr int ROW_THREADS = 512;
-// Rows ordered by their adapters at a time, and ids that leave room for a row in a 32-bit key
-constexpr int SORT_WIN = 2048;
-constexpr int SORT_MAX_N = 1 << 20;
+constexpr int SORT_WIN = 2048;           // rows ordered by their adapters at a time
 
 struct LowArgs {
   const __nv_bfloat16* x;
@@ -73,28 +71,69 @@ CS_DEV bool rows_in_turn(const LowArgs& p, int w0, int rows) {
   static_assert(LOW_THREADS == 256, "a pair a thread");
   return __syncthreads_count(change) * rows > 3 * LOW_THREADS;
 }
-// The tile's share of the window's rows in that order: a sort of keys that hold the adapter and the place.
-CS_DEV void order_rows(const LowArgs& p, uint32_t* key, LowSmem& sm, int w0, int m0, int rows) {
-  const int tid = (int)threadIdx.x, wn = min(SORT_WIN, p.M - w0);
-  int P = 2 * LOW_THREADS;
-  while (P < wn) P <<= 1;
-  for (int i = tid; i < P; i += LOW_THREADS) {
-    const int id = i < wn ? p.adapter[w0 + i] : 0;
-    key[i] = i >= wn ? 0xffffffffu : (uint32_t)(id < 0 || id >= p.n ? SORT_MAX_N : id) << 11 | (uint32_t)i;
-  }
-  __syncthreads();
-  for (int k = 2; k <= P; k <<= 1)
-    for (int j = k >> 1; j > 0; j >>= 1) {
-      for (int e = tid; e < P / 2; e += LOW_THREADS) {
-        const int i = 2 * e - (e & (j - 1));
-        const uint32_t a = key[i], b = key[i + j];
-        if ((a > b) == ((i & k) == 0)) key[i] = b, key[i + j] = a;
-      }
-      // (below a distance of 64, a warp's pairs lie in 64 keys of its own)
-      if (j > 32 || (j == 1 && k >= 32)) __syncthreads();
-      else __syncwarp();
+// The tile's share of the window's rows in that order, rows without an adapter behind: a counting sort by 8 bits of the adapter at
+// a time, which keeps the order of equal ones.  A warp ranks 256 rows, 32 at a time.  (A sort by exchanges of 2048 keys took some
+// 15 us, longer than many a tile's products.)
+struct OrderSmem {
+  uint16_t count[LOW_THREADS / 32][256];
+  uint16_t row[SORT_WIN];
+};
+CS_DEV void order_rows(const LowArgs& p, OrderSmem& o, LowSmem& sm, int w0, int m0, int rows) {
+  constexpr int PER = SORT_WIN / LOW_THREADS;
+  static_assert(LOW_THREADS == 256 && PER * 32 * (LOW_THREADS / 32) == SORT_WIN, "a thread a digit");
+  const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31, wn = min(SORT_WIN, p.M - w0);
+  const int passes = p.n < 256 ? 1 : 2;
+  for (int pass = 0; pass < passes; ++pass) {
+    int row[PER], digit[PER], before[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const int i = warp * (32 * PER) + k * 32 + lane;
+      row[k] = i >= wn ? -1 : pass == 0 ? i : o.row[i];
     }
-  for (int i = tid; i < rows; i += LOW_THREADS) sm.row[i] = m0 + i < p.M ? w0 + (int)(key[m0 - w0 + i] & (SORT_WIN - 1)) : 0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const int id = row[k] >= 0 ? p.adapter[w0 + row[k]] : 0;
+      digit[k] = row[k] < 0 ? -1 : ((id < 0 || id >= p.n ? p.n : id) >> (8 * pass)) & 255;
+    }
+    for (int e = tid; e < (int)sizeof(o.count) / 4; e += LOW_THREADS) reinterpret_cast<uint32_t*>(o.count)[e] = 0u;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const unsigned same = __match_any_sync(0xffffffffu, digit[k]);
+      const int have = digit[k] >= 0 ? o.count[warp][digit[k]] : 0;
+      before[k] = have + __popc(same & ((1u << lane) - 1u));
+      __syncwarp();
+      if (digit[k] >= 0 && (same >> lane) == 1u) o.count[warp][digit[k]] = (uint16_t)(before[k] + 1);      // the last of its kind
+      __syncwarp();
+    }
+    __syncthreads();
+    int total = 0;                         // of digit tid
+#pragma unroll
+    for (int w = 0; w < LOW_THREADS / 32; ++w) total += o.count[w][tid];
+    int upto = total;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += v;
+    }
+    if (lane == 31) sm.warp_count[warp] = upto;
+    __syncthreads();
+    int at = upto - total;
+#pragma unroll
+    for (int w = 0; w < LOW_THREADS / 32; ++w) at += w < warp ? sm.warp_count[w] : 0;
+#pragma unroll
+    for (int w = 0; w < LOW_THREADS / 32; ++w) {
+      const int c = o.count[w][tid];
+      o.count[w][tid] = (uint16_t)at;
+      at += c;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+      if (digit[k] >= 0) o.row[o.count[warp][digit[k]] + before[k]] = (uint16_t)row[k];
+    __syncthreads();
+  }
+  for (int i = tid; i < rows; i += LOW_THREADS) sm.row[i] = m0 + i < p.M ? w0 + o.row[m0 - w0 + i] : 0;
   __syncthreads();
 }
 
@@ -142,11 +181,11 @@ __global__ void __launch_bounds__(LOW_THREADS, NT <= 2 ? 3 : NT <= 8 ? 2 : 1) lo
   // the first chunks set out before the tile's adapters are known
   const int early = min(DEPTH - 1, c1 - c0);
   for (int i = 0; i < early; ++i) load_x(i);
-  static_assert(SORT_WIN * 4 <= DEPTH * R * 128, "the keys take the factors' place");
+  static_assert(sizeof(OrderSmem) <= DEPTH * R * 128, "the order is made in the factors' place");
   const int w0 = m0 & ~(SORT_WIN - 1);
   const bool sorted = p.sort && rows_in_turn(p, w0, rows);
   if (sorted) {                            // other rows than those that are under way
-    order_rows(p, reinterpret_cast<uint32_t*>(sraw + (f_off - x_off)), sm, w0, m0, rows);
+    order_rows(p, *reinterpret_cast<OrderSmem*>(sraw + (f_off - x_off)), sm, w0, m0, rows);
     cp_async_commit();
     cp_async_wait<0>();
 #pragma unroll
@@ -453,7 +492,7 @@ cudaError_t launch_low(LowArgs p, int num_sms, cudaStream_t stream) {
   p.rw_log2 = 3;
   while (p.rw_log2 > 1 && (p.M + (16 << p.rw_log2) - 1) / (16 << p.rw_log2) * 8 < num_sms) --p.rw_log2;
   const int tiles = (p.M + (16 << p.rw_log2) - 1) / (16 << p.rw_log2);
-  p.sort = p.n >= 4 && p.n <= SORT_MAX_N && tiles > 1;
+  p.sort = p.n >= 4 && tiles > 1;
   const int nt = (p.r + 7) / 8;
   if (nt <= 2) return launch_low_tile<2, RM>(p, tiles, num_sms, stream);
   if (nt <= 4) return launch_low_tile<4, RM>(p, tiles, num_sms, stream);

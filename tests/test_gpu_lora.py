@@ -121,7 +121,8 @@ def test_long_contractions(M, K, N, r, n):
 
 
 # rows of many adapters in turn, more than one window of ordered rows, a window that ends inside a tile; more ranks than a CTA takes
-MANY = [(2500, 520, 136, 16, 40), (4200, 200, 264, 64, 13), (600, 1160, 264, 32, 64), (900, 136, 1344, 128, 6), (4100, 264, 136, 24, 4)]
+MANY = [(2500, 520, 136, 16, 40), (4200, 200, 264, 64, 13), (600, 1160, 264, 32, 64), (900, 136, 1344, 128, 6), (4100, 264, 136, 24, 4), (2300, 328, 136, 16, 700),
+        (2100, 264, 136, 8, 255), (2100, 264, 136, 8, 256)]
 
 
 @pytest.mark.parametrize("M,K,N,r,n", MANY)
@@ -301,6 +302,23 @@ def test_bad_adapter_ids_are_flagged_and_count_as_none():
         C._check(C.load_library().cospec_get_device_error(__import__("ctypes").byref(__import__("ctypes").c_int()), None))
     y1, u1 = _forward(dict(c, adapter=good))
     assert torch.equal(y, y1) and torch.equal(u, u1)
+
+
+def test_bad_ids_among_rows_in_turn():
+    """More rows than one window, a fifth of the ids outside the adapters: flagged, and as rows without one."""
+    M, n = 2300, 12
+    c, _ = _make(11, M, 1160, 136, 16, n, runs=False)
+    good = c["adapter"].clone()
+    rng = np.random.default_rng(3)
+    bad = torch.from_numpy(rng.random(M) < 0.2).cuda()
+    c["adapter"][bad] = torch.from_numpy(rng.choice(np.array([-2, n, 65535, 2 ** 31 - 1, -2 ** 31], dtype=np.int64), int(bad.sum())).astype(np.int32)).cuda()
+    y = torch.empty((M, 136), dtype=torch.bfloat16, device="cuda")
+    u = torch.empty((M, 16), device="cuda")
+    C.lora_forward(**c, y=y, u=u)
+    assert C.get_device_error() == C.DEVERR_ADAPTER
+    good[bad] = -1
+    c["adapter"] = good
+    _check_forward(c, y, u)
 
 
 def test_repeated_and_captured():
