@@ -615,6 +615,9 @@ constexpr int P_XW = 2 + P_EPI;          // producer of the rows
 constexpr int P_UW = P_XW + 1;           // first of the four warps of the u operand
 constexpr int P_W2 = P_UW + 4;           // second producer of W
 constexpr int P_THREADS = 32 * (P_W2 + 1);
+// Adapter steps whose operand is written before one fence hands them on, fewer than the ring has stages (four to six): 64 adapters of
+// rank 32 in turn, 4096 rows 4096 -> 4096, 374 us one at a time, 349 two, 331 three.
+constexpr int GROUP = 3;
 constexpr int P_CHUNKS = MAX_NT / 64;    // 32-row chunks of an epilogue warp
 
 struct PairSmem {
@@ -872,29 +875,36 @@ __global__ void __launch_bounds__(P_THREADS, 1)
         unit_load(v0, u, 0, p.r);
         unit_load(v1, u, UNIT, p.r);
       }
-      for (int i = 0; i < steps; ++i) {
-        const int s = st;
-        if (++st == p.stages) st = 0;
-        const int nu = min(PU, units - i * PU);
-        ok = __all_sync(0xffffffffu, mbar_wait_idle(&ugo[s], (gphase >> s) & 1u, WAIT_NS, 100u)) && !*abort_flag;
-        if (!ok) break;
-        gphase ^= 1u << s;
-        uint8_t* buf = smem + L.b_off + (uint32_t)s * b_stage;
-        for (int q = 0; q < nu; ++q, ++k) {
-          const bool mine = k >= 0 && k < upe;
-          uint4 w[4];
-          if (k & 1) {
-            unit_row(w, mine, v1);
-            if (mine) unit_load(v1, u, (k + 2) * UNIT, p.r);
-          } else {
-            unit_row(w, mine, v0);
-            if (mine) unit_load(v0, u, (k + 2) * UNIT, p.r);
+      for (int i = 0; i < steps; i += GROUP) {
+        const int first = st, group = min(GROUP, steps - i);
+        for (int g = 0; g < group && ok; ++g) {
+          const int s = st;
+          if (++st == p.stages) st = 0;
+          const int nu = min(PU, units - (i + g) * PU);
+          ok = __all_sync(0xffffffffu, mbar_wait_idle(&ugo[s], (gphase >> s) & 1u, WAIT_NS, 100u)) && !*abort_flag;
+          if (!ok) break;
+          gphase ^= 1u << s;
+          uint8_t* buf = smem + L.b_off + (uint32_t)s * b_stage;
+          for (int q = 0; q < nu; ++q, ++k) {
+            const bool mine = k >= 0 && k < upe;
+            uint4 w[4];
+            if (k & 1) {
+              unit_row(w, mine, v1);
+              if (mine) unit_load(v1, u, (k + 2) * UNIT, p.r);
+            } else {
+              unit_row(w, mine, v0);
+              if (mine) unit_load(v0, u, (k + 2) * UNIT, p.r);
+            }
+            if (t < half) store_unit_row(buf + (q >> 1) * b_bytes, t, q & 1, w);
           }
-          if (t < half) store_unit_row(buf + (q >> 1) * b_bytes, t, q & 1, w);
         }
+        if (!ok) break;
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(ufull0 + (uint32_t)s * 8u);
+        for (int g = 0, s = first; g < group; ++g) {
+          if (lane == 0) mbar_arrive_cluster(ufull0 + (uint32_t)s * 8u);
+          if (++s == p.stages) s = 0;
+        }
       }
       if (!ok) *abort_flag = 1;            // (the others of the four see it at the next tile)
     }
