@@ -13,9 +13,9 @@
 // butterfly for four decisions.  Which units are on is kept as bits between the two walks.  H up to 64 units fits one warp,
 // and the eight warps take decisions in turn; 256 units take two.  All sums have a fixed order.
 // Work: 36 H flops at each effective decision; bytes: ids, flags, p_new and dz of every position and what a decision
-// gathers.  66560 rounds, K = 25, H = 256: 52 us, of which the multiply-adds alone would be 17 us and the bytes 13 us: the
+// gathers.  66560 rounds, K = 25, H = 256: 57 us (4 of them the units near their border), of which the multiply-adds alone would be 17 us and the bytes 13 us: the
 // walks issue their multiply-adds at about half rate, and listing a step's decisions is a chain of barriers that the SM's
-// other CTA hides in part.  64 rounds, K = 5, H = 64: 7.7 us, latency: the launch, one chain of loads, the cluster's exchange.
+// other CTA hides in part.  64 rounds, K = 5, H = 64: 8.0 us, latency: the launch, one chain of loads, the cluster's exchange.
 // The terms of the loss, db2 and the CTAs' sums are added as pairs of floats (hi + lo): 64-bit additions, of which an
 // SM issues about two a clock, took 70 us in the second kernel.  KL is p g(-d/p) + q g(d/q), d = p - p_ref, g(x) = x -
 // log(1 + x), whose first-order terms are gone before they could cancel.
@@ -33,6 +33,7 @@ constexpr int STEP = 2048;                // positions of a step, at most
 constexpr int PER = STEP / THREADS;
 constexpr int BATCH = 512;                // decisions gathered at a time
 constexpr int MAX_CTAS = 512;
+constexpr int TODO = 128;
 constexpr int CLUSTER = 8;                // CTAs that join their sums
 constexpr int FIN_THREADS = 1024;
 
@@ -43,6 +44,9 @@ struct LossSmem {
   uint16_t list[STEP];                    // effective positions of the step
   uint32_t match[STEP / 32 + 2];
   int warp_count[8];
+  uint32_t top[8];                        // the warps' largest |feature| of a batch, as bits
+  int todo_n;                             // units near their border: group of four decisions << 8 | thread
+  int todo[TODO];
   int draft[STEP], argmax[STEP];          // of the next step, under way while this one is computed
   __align__(16) uint8_t eff[STEP];
 };
@@ -195,9 +199,25 @@ CS_DEV void write_loss(const ArbLossArgs& a, const float2 (&v)[4]) {
   *a.db2 = value(v[3]);
 }
 
+// A unit's input in 64 bits, from the records of position e (decision d of the batch).
+CS_DEV double exact_input(const ArbLossArgs& a, const LossSmem& sm, int e, int d, int h) {
+  const int r = e / a.K, i = e - r * a.K;
+  const float* s0 = a.stats + ((size_t)e + r) * 5;
+  const float* w = a.w1 + (size_t)h * 8;
+  const double k = (double)a.K, x2 = (double)s0[2], y2 = (double)s0[7];
+  double v = fma((double)w[0], (double)s0[4] - x2, (double)a.b1[h]);
+  v = fma((double)w[1], (double)s0[0] - x2, v);
+  v = fma((double)w[2], (double)s0[0] - (double)s0[1], v);
+  v = fma((double)w[3], (double)s0[3], v);
+  v = fma((double)w[4], (double)s0[5] - y2, v);
+  v = fma((double)w[5], i + 1 < a.K ? (double)s0[9] - y2 : 0.0, v);
+  v = fma((double)w[6], (double)(i + 1) / k, v);
+  return fma((double)w[7], (double)rintf(sm.feat[d][7] * (float)a.K) / k, v);
+}
+
 // PP: pairs of units of a thread; TW: warps that hold all units.
 template <int PP, int TW>
-__global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs a, float* ws_s, float2* ws_l, int step) {
+__global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const __grid_constant__ ArbLossArgs a, float* ws_s, float2* ws_l, int step) {
   extern __shared__ __align__(16) uint8_t raw[];
   LossSmem& sm = *reinterpret_cast<LossSmem*>(raw);
   constexpr int TEAMS = 8 / TW;
@@ -226,11 +246,22 @@ __global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs 
       w1[i][4 * k + 2] = make_float2(-v[k].z, -v[2 + k].z);
       w1[i][4 * k + 3] = make_float2(-v[k].w, -v[2 + k].w);
     }
-    // (0 - b: a zero keeps its positive sign, and so does every sum that comes to zero)
-    b1[i] = make_float2(h < a.H ? 0.f - __ldg(a.b1 + h) : 0.f, h + 1 < a.H ? 0.f - __ldg(a.b1 + h + 1) : 0.f);
+    // (0 - b: a zero keeps its positive sign, and so does every sum that comes to zero; units that are not there are off, and far from on)
+    b1[i] = make_float2(h < a.H ? 0.f - __ldg(a.b1 + h) : 1.f, h + 1 < a.H ? 0.f - __ldg(a.b1 + h + 1) : 1.f);
     w2[i] = make_float2(h < a.H ? __ldg(a.w2 + h) : 0.f, h + 1 < a.H ? __ldg(a.w2 + h + 1) : 0.f);
 #pragma unroll
     for (int k = 0; k < 9; ++k) S[i][k] = make_float2(0.f, 0.f);
+  }
+  // A unit's input is off by less than `slack` times the largest feature (or 1): nine sums and a feature's own rounding, 2^-24 each, of
+  // at most |b1| + sum |w1|.  Closer to zero its sign, whether it is on, is taken in 64 bits: one decision more or less, of 200,000, is
+  // 5e-5 of the gradients.
+  float slack = 0.f;
+#pragma unroll
+  for (int i = 0; i < PP; ++i) {
+    float2 s = make_float2(fabsf(b1[i].x), fabsf(b1[i].y));
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s.x += fabsf(w1[i][k].x), s.y += fabsf(w1[i][k].y);
+    slack = fmaxf(slack, fmaxf(s.x, s.y) * 6.5e-7f);
   }
   const float b2 = *a.b2;
   const int total = a.n * a.K;
@@ -337,6 +368,8 @@ __global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs 
     __syncthreads();
     for (int d0 = 0; d0 < decisions; d0 += BATCH) {
       const int count = min(BATCH, decisions - d0), groups = (count + 3) / 4;
+      uint32_t top = 0x3f800000u;            // 1
+      if (tid == 0) sm.todo_n = 0;
       for (int d = tid; d < count; d += THREADS) {
         const int off = sm.list[d0 + d], e = base + off, r = e / a.K, i = e - r * a.K;
         const float* s0 = a.stats + ((size_t)e + r) * 5;
@@ -358,15 +391,23 @@ __global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs 
         float4* f = reinterpret_cast<float4*>(sm.feat[d]);
         f[0] = make_float4(x4 - x2, x0 - x2, x0 - x1, x3);
         f[1] = make_float4(y0 - y2, i + 1 < a.K ? y4 - y2 : 0.f, (float)(i + 1) / (float)a.K, (float)before / (float)a.K);
+        const float4 fa = f[0], fb = f[1];
+        top = max(top, __float_as_uint(fmaxf(fmaxf(fmaxf(fabsf(fa.x), fabsf(fa.y)), fmaxf(fabsf(fa.z), fabsf(fa.w))), fmaxf(fabsf(fb.x), fabsf(fb.y)))));
         sm.adv[d] = adv;
         sm.old[d] = old;
         sm.ref[d] = ref;
         sm.at[d] = took ? (int)((unsigned)off | 0x80000000u) : off;
       }
+      top = __reduce_max_sync(0xffffffffu, top);
+      if (lane == 0) sm.top[warp] = top;
       __syncthreads();
+#pragma unroll
+      for (int w = 0; w < 8; ++w) top = max(top, sm.top[w]);
+      const float near = slack * __uint_as_float(top);
       for (int q = team; q < groups; q += TEAMS) {
         float z[4];
         unsigned bits = 0;
+        float least = near;
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
           const float4 fa = *reinterpret_cast<const float4*>(&sm.feat[4 * q + d][0]), fb = *reinterpret_cast<const float4*>(&sm.feat[4 * q + d][4]);
@@ -377,11 +418,16 @@ __global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs 
             float2 v = b1[i];
 #pragma unroll
             for (int k = 0; k < 8; ++k) v = fma_pair(w1[i][k], f[k], v);
+            least = fminf(least, fminf(fabsf(v.x), fabsf(v.y)));
             bits = __funnelshift_l(__float_as_uint(v.x), bits, 1);
             bits = __funnelshift_l(__float_as_uint(v.y), bits, 1);
             zz = fma2(w2[i], make_float2(fmaxf(-v.x, 0.f), fmaxf(-v.y, 0.f)), zz);
           }
           z[d] = zz.x + zz.y;
+        }
+        if (least < near) {
+          const int at = atomicAdd(&sm.todo_n, 1);
+          if (at < TODO) sm.todo[at] = q << 8 | (tw * 32 + lane);
         }
         on[q * (TW * 32) + tw * 32 + lane] = (uint16_t)bits;
         // four sums over the warp; lanes 0, 8, 16, 24 end with decisions 0, 1, 2, 3
@@ -395,6 +441,21 @@ __global__ void __launch_bounds__(THREADS, 2) arb_loss_kernel(const ArbLossArgs 
         if ((lane & 7) == 0) zpart[tw * BATCH + 4 * q + (lane >> 3)] = v;
       }
       __syncthreads();
+      // The units near their border, a warp the four decisions and units of a thread; more than the list holds: all of them.
+      const int listed = sm.todo_n, items = listed > TODO ? groups * TW * 32 : listed;
+      for (int t = warp; t < items; t += 8) {
+        const int item = listed > TODO ? t / (TW * 32) << 8 | t % (TW * 32) : sm.todo[t];
+        const int q = item >> 8, slot = item & 255, d = 4 * q + lane / (2 * PP), j = lane % (2 * PP);
+        const int h = 2 * slot + (j >> 1) * 64 * TW + (j & 1);
+        bool sure = lane < 8 * PP && d < count && h < a.H;
+        const double v = sure ? exact_input(a, sm, base + (sm.at[d] & 0x7fffffff), d, h) : 0.0;
+        sure = sure && v == v;
+        const unsigned is = __brev(__ballot_sync(0xffffffffu, sure)) >> (32 - 8 * PP), now = __brev(__ballot_sync(0xffffffffu, v > 0.0)) >> (32 - 8 * PP);
+        if (lane == 0) {
+          uint16_t* w = &on[q * (TW * 32) + slot];
+          *w = (uint16_t)((*w & ~is) | (now & is));
+        }
+      }
       for (int d = tid; d < 4 * groups; d += THREADS) {
         float g = 0.f;
         if (d < count) {

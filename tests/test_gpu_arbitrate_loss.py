@@ -194,6 +194,28 @@ def test_p_and_dz_over_the_logits_range(z):
         assert (np.abs(g["dz"].double().cpu().numpy()[fine] - want[fine]) <= 2.0 ** -21 * np.abs(want[fine]) + 2.0 ** -126).all()
 
 
+@pytest.mark.parametrize("H", [7, 64, 100, 256, 600])
+@pytest.mark.parametrize("K,pos", [(1, 0), (7, 3), (7, 6)])
+def test_units_at_their_border(H, K, pos):
+    """b1 is the rounded negative of W1 f, so that a unit's input is a rounding of it, 2^-25 relative: on and off as in 64 bits."""
+    from oracle.cospec_oracle import arbitration_features
+    for seed in range(6):
+        c = _case(1000 + seed, 1, K, H, mismatch=0.5)
+        c["draft"][0, pos] = c["argmax"][0, pos] + 1
+        c["eff"][:] = 0
+        c["eff"][0, pos], c["accept"][0, pos] = 1, 1
+        c["p_old"][:], c["adv"][:] = 0.5, -1.0                       # an unclipped gradient that is not zero
+        f = np.asarray(arbitration_features(c["draft"], c["argmax"], c["stats"].astype(np.float64)))[0][pos]
+        w = c["w1"].astype(np.float64)
+        c["b1"] = (-(w @ f)).astype(np.float32)
+        pre = w @ f + c["b1"].astype(np.float64)
+        assert (np.abs(pre) > 2.0 ** -45).any()
+        g = _run(c)
+        on = g["db1"].cpu().numpy() != 0
+        clear = np.abs(pre) > 2.0 ** -45                             # the 64-bit sums' own roundings
+        assert (on == (pre > 0))[clear & (c["w2"] != 0)].all()
+
+
 def test_an_old_probability_of_zero():
     """The ratio is infinite: clipped where A > 0, so that nothing else is lost; infinite where A < 0."""
     c = _case(53, 3, 4, 8, mismatch=1.0, dense=True)
