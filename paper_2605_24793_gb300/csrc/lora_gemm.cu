@@ -203,14 +203,18 @@ __device__ __noinline__ void again(const GemmArgs& p, int f, int m0, int m1, int
   for (int m = m0; m < min(m1, p.M); ++m) {
     __nv_bfloat16* y = p.y + (long long)m * p.ldy + f;
     if (finite(__bfloat162float(*y))) continue;
+    const int id = p.adapter[m];
+    const bool has = id >= 0 && id < p.n && (!DROP || ((lora_keep8_bits((uint32_t)(f / 8), (uint32_t)m, p.drop, key) >> (f & 7)) & 1u));
+    bool own = false;                      // the row's own factor is the cause: so it stays
+    for (int j = 0; has && j < p.r; ++j) own = own || !finite(factor(id, j));
+    if (own) continue;
     float v[4] = {0.f, 0.f, 0.f, 0.f}, low = 0.f;
     const __nv_bfloat16* x = p.x + (long long)m * p.ldx;
     for (int k = 0; k < p.C; k += 4)         // (a multiple of 8)
 #pragma unroll
       for (int q = 0; q < 4; ++q)
         v[q] = fmaf(__bfloat162float(x[k + q]), __bfloat162float(p.w[MN ? (size_t)(k + q) * p.F + f : (size_t)f * p.C + k + q]), v[q]);
-    const int id = p.adapter[m];
-    if (id >= 0 && id < p.n && (!DROP || ((lora_keep8_bits((uint32_t)(f / 8), (uint32_t)m, p.drop, key) >> (f & 7)) & 1u)))
+    if (has)
       for (int j = 0; j < p.r; ++j) low = fmaf(p.u[(size_t)m * p.r + j], factor(id, j), low);
     *y = __float2bfloat16((v[0] + v[1]) + (v[2] + v[3]) + low);
   }
